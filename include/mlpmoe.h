@@ -41,7 +41,9 @@ typedef enum {
   MLPMOE_ERR_DEVICE_TIMEOUT = 8   /* a bounded wait inside a kernel ran out (see mlpmoe_get_status) */
 } mlpmoe_status_t;
 
-typedef enum { MLPMOE_BF16 = 0, MLPMOE_FP32 = 1 } mlpmoe_dtype_t;
+/* MLPMOE_E4M3 (8-bit floats: 4 significant bits, largest value 448) is a type of activations only: the output of
+ * mlpmoe_add_rmsnorm and the input of mlpmoe_w4_forward, always with fp32 scales beside the codes. */
+typedef enum { MLPMOE_BF16 = 0, MLPMOE_FP32 = 1, MLPMOE_E4M3 = 2 } mlpmoe_dtype_t;
 
 typedef enum {
   MLPMOE_LAYOUT_PAPER = 0,  /* W_gate, W_up: [d_model x d_inter]; W_down: [d_inter x d_model]; row-major (Section 3.1) */
@@ -254,6 +256,135 @@ mlpmoe_status_t mlpmoe_stack_forward(const mlpmoe_handle_t* layers, int32_t n_la
 mlpmoe_status_t mlpmoe_stack_forward_host(const mlpmoe_handle_t* layers, int32_t n_layers,
                                           const float* x_host, float* y_host,
                                           int64_t n_tokens, float eps, void* stream);
+
+/* ------------------------------------------------------------------------- *
+ * Operators around a routed layer step (not in the paper): the norm before the
+ * layer, the router that makes the selection, and the layer on 4-bit weights for
+ * a few tokens.  They need no handle: every buffer is the caller's, the calls only
+ * enqueue on `stream`, allocate nothing, never synchronise and can be captured into
+ * a graph.  A workspace is scratch of one call: two calls that may overlap (other
+ * streams, replays of two graphs at the same time) need one each.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Residual addition and RMSNorm in one pass, per token:
+ *     s = x + r;   x_out = s;   v = s / sqrt(mean(s^2) + eps) * gain
+ * in fp32 (the norm takes the unrounded sum also where x_out is bf16); out = v, or in 8 bits with scales:
+ *     scale = max(max_group |v| / 448, 2^-126),   out = e4m3(v * (1 / scale)),   v ~ out * scale.
+ *   x        device, [n_tokens x d_model] of x_dtype (MLPMOE_FP32 or MLPMOE_BF16), rows x_stride elements apart
+ *   r        device, the same shape, of r_dtype (fp32 or bf16), or NULL: nothing is added
+ *   gain     device fp32 [d_model], or NULL: 1
+ *   x_out    device, of x_dtype: receives s; may be x itself (same stride); NULL: s is not stored
+ *   out      device, of out_dtype (fp32, bf16 or e4m3); must not overlap an input
+ *   scales   device fp32 [n_tokens x ceil(d_model / group)], contiguous; e4m3 only, else ignored
+ *   group    columns per scale: 32, 64 or 128 (the last group may be shorter), or 0: one scale per token
+ * A stride of 0 means d_model.  Any d_model up to 32768 (more: MLPMOE_ERR_UNSUPPORTED), any element alignment;
+ * rows that start on 16 bytes (8 for e4m3) with d_model a multiple of 8 take wide loads.  Errors:
+ * MLPMOE_ERR_INVALID_ARG (NULL, a size or stride that does not fit, a pointer off its element's alignment, another type or group).
+ */
+mlpmoe_status_t mlpmoe_add_rmsnorm(const void* x, mlpmoe_dtype_t x_dtype, int64_t x_stride, const void* r, mlpmoe_dtype_t r_dtype,
+                                   int64_t r_stride, const float* gain, void* x_out, int64_t x_out_stride, void* out,
+                                   mlpmoe_dtype_t out_dtype, int64_t out_stride, float* scales, int64_t group, int64_t n_tokens,
+                                   int64_t d_model, float eps, void* stream);
+
+/*
+ * The router: from logits [n_tokens x B] the selection that mlpmoe_forward_routed and mlpmoe_w4_forward take, the
+ * tokens per branch, and a balance loss (the paper defines no router; the rule is this library's own).
+ * A pair (t, b) is eligible if valid[t] and avail[b] are non-zero (NULL: all are) and logit[t, b] > -infinity (a NaN is
+ * not; +infinity counts as the largest finite value); what stands in places that are not eligible is never used.
+ *     select[t, b] = 1 for the min(top_k, number eligible) largest eligible logits of token t, ties to the lowest b
+ *     p[t, :]      = softmax of the eligible logits of token t, 0 elsewhere
+ *     counts[b]    = sum_t select[t, b];   counts[B] = T, the tokens with an eligible branch
+ *     prob[b]      = sum_t p[t, b] / T
+ *     loss         = B' * sum_b f_b * prob[b],  f_b = counts[b] / sum_b' counts[b'],  B' = number of available branches
+ * (1 when both the counts and the probabilities are uniform; 0 if T = 0).  Sums are fp32 in a fixed order, the same
+ * bits on every call.
+ *   logits    device, fp32 or bf16, rows `stride` elements apart (0 = B)
+ *   select    device uint8 [n_tokens x B], contiguous
+ *   counts    device int32 [B + 1];  prob  device fp32 [B];  loss  device fp32 [1]
+ *   avail     device uint8 [B] or NULL;  valid  device uint8 [n_tokens] or NULL
+ *   workspace device, 16-byte aligned, of the size that mlpmoe_route_workspace gives
+ * 1 <= B <= 256 (more: MLPMOE_ERR_UNSUPPORTED), 1 <= top_k <= B.  n_tokens = 0 clears counts, prob and loss.
+ */
+mlpmoe_status_t mlpmoe_route(const void* logits, mlpmoe_dtype_t dtype, int64_t stride, int64_t n_tokens, int32_t B, int32_t top_k,
+                             const uint8_t* avail, const uint8_t* valid, uint8_t* select, int32_t* counts, float* prob, float* loss,
+                             void* workspace, int64_t workspace_bytes, void* stream);
+mlpmoe_status_t mlpmoe_route_workspace(int64_t n_tokens, int32_t B, int64_t* bytes);
+
+/*
+ * Gradient of grad_loss * loss with respect to the logits, the counts held constant (they are whole numbers):
+ *     grad[t, j] = grad_loss * B' / T * p[t, j] * (f_j - sum_b f_b p[t, b]),   0 where (t, j) is not eligible.
+ *   logits, dtype, stride, avail, valid   as mlpmoe_route was given
+ *   counts     device int32 [B + 1], as mlpmoe_route left it
+ *   grad_loss  device fp32 [1], or NULL: 1
+ *   grad       device, of dtype, rows grad_stride elements apart (0 = B); may be logits itself (same stride)
+ */
+mlpmoe_status_t mlpmoe_route_backward(const void* logits, mlpmoe_dtype_t dtype, int64_t stride, int64_t n_tokens, int32_t B,
+                                      const uint8_t* avail, const uint8_t* valid, const int32_t* counts, const float* grad_loss,
+                                      void* grad, int64_t grad_stride, void* stream);
+
+/*
+ * A matrix [rows x cols] on 4 bits: W[r, c] = (code[r, c] - zero[r, c / group]) * scale[r, c / group].
+ *   q      device, 16-byte aligned: code[r, c] in bits 4 (c % 2) .. of byte c / 2 of row r; a row is 16 ceil(cols / 32) bytes
+ *   scale  device bf16, 16-byte aligned: [ceil(cols / group) x rows16], rows16 = rows rounded up to 16
+ *   zero   device uint8 (0..15), 16-byte aligned, laid out as scale; NULL: 8 everywhere
+ * What stands in the padding (columns past cols, rows past rows) does not matter.  group: 32, 64 or 128.
+ */
+typedef struct {
+  const uint8_t* q;
+  const void* scale;
+  const uint8_t* zero;
+} mlpmoe_w4_matrix_t;
+
+/*
+ * Weights to 4 bits: per row and group of columns, with w the group's values,
+ *     zero == NULL:  s = bf16(max |w| / 7),                          code = clamp(rint(w / s) + 8, 0, 15)
+ *     otherwise:     s = bf16((max(w, 0) - min(w, 0)) / 15),  z = clamp(rint(-min(w, 0) / s), 0, 15),
+ *                    code = clamp(rint(w / s) + z, 0, 15)
+ * (s = 0: code = z, z = 0 where it is stored).  Columns past cols are coded 0 up to the row's end.
+ *   W       device, fp32 or bf16: [rows x cols] with rows `stride` apart (MLPMOE_LAYOUT_LINEAR), or its transpose
+ *           [cols x rows] (MLPMOE_LAYOUT_PAPER); stride 0 = contiguous
+ * mlpmoe_w4_dequantize writes (code - zero) * scale back, rounded to dtype: for a prefill layer made of the same weights
+ * (mlpmoe_create), or to look at the error.
+ */
+mlpmoe_status_t mlpmoe_w4_quantize(const void* W, mlpmoe_dtype_t dtype, mlpmoe_layout_t layout, int64_t stride, int64_t rows,
+                                   int64_t cols, int32_t group, uint8_t* q, void* scale, uint8_t* zero, void* stream);
+mlpmoe_status_t mlpmoe_w4_dequantize(const uint8_t* q, const void* scale, const uint8_t* zero, int64_t rows, int64_t cols, int32_t group,
+                                     void* W, mlpmoe_dtype_t dtype, mlpmoe_layout_t layout, int64_t stride, void* stream);
+
+/* A layer on 4-bit weights: gate, up [d_inter x d_model] and down [d_model x d_inter], groups along the columns.
+ * d_b (length B) and alpha (length B, NULL = 1) are host arrays with the meaning of mlpmoe_create; alpha_b = 0 drops a branch. */
+typedef struct {
+  int64_t d_model, d_inter;
+  const int64_t* d_b;
+  const float* alpha;
+  int32_t B, group;
+  mlpmoe_w4_matrix_t gate, up, down;
+} mlpmoe_w4_layer_t;
+
+/*
+ * The layer equation of Section 3.1 on 4-bit weights, for decode (the weights are streamed once per 64 tokens or fewer;
+ * it pays up to about 64 tokens, any count is computed):
+ *     y_t = residual_t + c_t * sum_{b in S_t} alpha_b W_down^(b) [ silu(W_gate^(b) x_t) (.) W_up^(b) x_t ]
+ * with S_t and c_t as in mlpmoe_forward_routed (select NULL: every branch with alpha_b != 0, c_t = 1).  Branches that
+ * no token selects are not read.  Products and sums are fp32; the intermediate activation is held as two (y bf16) or three
+ * (y fp32) bf16 pieces, x in fp32 as three.
+ *   x        device, [n_tokens x d_model] of x_dtype (bf16, fp32, or e4m3 with scales), rows x_stride elements apart
+ *            (0 = d_model), 16-byte aligned, x_stride a multiple of 8
+ *   x_scale  device fp32 [n_tokens x ceil(d_model / x_group)] for e4m3 (x_group = 0: one per token), else ignored;
+ *            x_group: 0, 32, 64 or 128, not below the layer's group
+ *   select   device uint8 [n_tokens x B] or NULL
+ *   residual device fp32 [n_tokens x d_model] or NULL; may be y when y_dtype is fp32
+ *   y        device, [n_tokens x d_model] of y_dtype (fp32 or bf16), 16-byte aligned
+ *   workspace device, 256-byte aligned, of the size that mlpmoe_w4_workspace gives
+ * d_model a multiple of 8, d_b multiples of 16, B <= 256, d_model and d_inter up to 2^20, n_tokens up to 65536.
+ * The same call gives the same bits every time.  Errors as mlpmoe_create and mlpmoe_forward_ex.
+ */
+mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x, mlpmoe_dtype_t x_dtype, int64_t x_stride,
+                                  const float* x_scale, int64_t x_group, const uint8_t* select, int32_t compensate,
+                                  const float* residual, void* y, mlpmoe_dtype_t y_dtype, int64_t n_tokens, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+mlpmoe_status_t mlpmoe_w4_workspace(const mlpmoe_w4_layer_t* layer, int64_t n_tokens, int64_t* bytes);
 
 /* ------------------------------------------------------------------------- *
  * Queries (host outputs; used by the parity harness)

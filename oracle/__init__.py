@@ -27,3 +27,15 @@ from .mlpmoe_oracle import (  # noqa: F401
     rmsnorm,
     stack_forward,
 )
+from .operators_oracle import (  # noqa: F401
+    round_to_e4m3,
+    add_rmsnorm,
+    quantize_e4m3,
+    route,
+    route_grad,
+    w4_quantize,
+    w4_dequantize,
+    w4_pack,
+    w4_unpack,
+    w4_layer_forward,
+)

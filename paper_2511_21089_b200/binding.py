@@ -28,8 +28,18 @@ MLPMOE_ERR_CUDA = 7
 MLPMOE_ERR_DEVICE_TIMEOUT = 8
 MLPMOE_BF16 = 0
 MLPMOE_FP32 = 1
+MLPMOE_E4M3 = 2
 MLPMOE_LAYOUT_PAPER = 0
 MLPMOE_LAYOUT_LINEAR = 1
+
+class mlpmoe_w4_matrix_t(ctypes.Structure):
+    _fields_ = [("q", c_void_p), ("scale", c_void_p), ("zero", c_void_p)]
+
+
+class mlpmoe_w4_layer_t(ctypes.Structure):
+    _fields_ = [("d_model", c_int64), ("d_inter", c_int64), ("d_b", POINTER(c_int64)), ("alpha", POINTER(c_float)), ("B", c_int32),
+                ("group", c_int32), ("gate", mlpmoe_w4_matrix_t), ("up", mlpmoe_w4_matrix_t), ("down", mlpmoe_w4_matrix_t)]
+
 
 # name -> (restype, argtypes): every symbol include/mlpmoe.h declares
 SIGNATURES = {
@@ -47,6 +57,18 @@ SIGNATURES = {
     "mlpmoe_forward_routed": (c_int32, [c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int32, c_void_p]),
     "mlpmoe_forward_host": (c_int32, [c_void_p, c_void_p, c_void_p, c_int64, c_void_p]),
     "mlpmoe_rmsnorm": (c_int32, [c_void_p, c_void_p, c_int64, c_int64, c_float, c_int32, c_void_p]),
+    "mlpmoe_add_rmsnorm": (c_int32, [c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_int32,
+                                     c_int64, c_void_p, c_int64, c_int64, c_int64, c_float, c_void_p]),
+    "mlpmoe_route": (c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                               c_void_p, c_void_p, c_int64, c_void_p]),
+    "mlpmoe_route_workspace": (c_int32, [c_int64, c_int32, POINTER(c_int64)]),
+    "mlpmoe_route_backward": (c_int32, [c_void_p, c_int32, c_int64, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                        c_int64, c_void_p]),
+    "mlpmoe_w4_quantize": (c_int32, [c_void_p, c_int32, c_int32, c_int64, c_int64, c_int64, c_int32, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "mlpmoe_w4_dequantize": (c_int32, [c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_int32, c_void_p, c_int32, c_int32, c_int64, c_void_p]),
+    "mlpmoe_w4_forward": (c_int32, [POINTER(mlpmoe_w4_layer_t), c_void_p, c_int32, c_int64, c_void_p, c_int64, c_void_p, c_int32, c_void_p,
+                                    c_void_p, c_int32, c_int64, c_void_p, c_int64, c_void_p]),
+    "mlpmoe_w4_workspace": (c_int32, [POINTER(mlpmoe_w4_layer_t), c_int64, POINTER(c_int64)]),
     "mlpmoe_stack_prepare": (c_int32, [POINTER(c_void_p), c_int32, c_int64, c_void_p]),
     "mlpmoe_debug_set_wait": (c_int32, [c_void_p, ctypes.c_uint64, ctypes.c_uint32]),
     "mlpmoe_debug_set_decode_kernel": (c_int32, [c_void_p, c_int32]),
@@ -188,6 +210,72 @@ def mlpmoe_forward_host(h: int, x_host, y_host, n_tokens: int, stream=None) -> N
 
 def mlpmoe_rmsnorm(x, r, n_tokens: int, d_model: int, eps: float = 1e-6, out_dtype: int = MLPMOE_BF16, stream=None) -> None:
     _check(lib.mlpmoe_rmsnorm(_ptr(x), _ptr(r), n_tokens, d_model, eps, out_dtype, _stream(stream)), "mlpmoe_rmsnorm")
+
+
+def mlpmoe_add_rmsnorm(x, r, x_out, out, n_tokens: int, d_model: int, gain=None, scales=None, group: int = 0, eps: float = 1e-6,
+                       x_dtype: int = MLPMOE_FP32, r_dtype: int = MLPMOE_FP32, out_dtype: int = MLPMOE_BF16, x_stride: int = 0,
+                       r_stride: int = 0, x_out_stride: int = 0, out_stride: int = 0, stream=None) -> None:
+    """x_out = x + r and out = its RMSNorm; strides in elements (0 = d_model); r, x_out and gain may be None."""
+    _check(lib.mlpmoe_add_rmsnorm(_ptr(x), x_dtype, x_stride, _ptr(r), r_dtype, r_stride, _ptr(gain), _ptr(x_out), x_out_stride, _ptr(out),
+                                  out_dtype, out_stride, _ptr(scales), group, n_tokens, d_model, eps, _stream(stream)), "mlpmoe_add_rmsnorm")
+
+
+def mlpmoe_route_workspace(n_tokens: int, B: int) -> int:
+    """Bytes of workspace that mlpmoe_route needs."""
+    v = c_int64()
+    _check(lib.mlpmoe_route_workspace(n_tokens, B, ctypes.byref(v)), "mlpmoe_route_workspace")
+    return v.value
+
+
+def mlpmoe_route(logits, n_tokens: int, B: int, top_k: int, select, counts, prob, loss, workspace, workspace_bytes: int,
+                 dtype: int = MLPMOE_FP32, stride: int = 0, avail=None, valid=None, stream=None) -> None:
+    """select: uint8 [n_tokens x B], counts: int32 [B + 1], prob: fp32 [B], loss: fp32 [1], all on the device."""
+    _check(lib.mlpmoe_route(_ptr(logits), dtype, stride, n_tokens, B, top_k, _ptr(avail), _ptr(valid), _ptr(select), _ptr(counts), _ptr(prob),
+                            _ptr(loss), _ptr(workspace), workspace_bytes, _stream(stream)), "mlpmoe_route")
+
+
+def mlpmoe_route_backward(logits, counts, grad, n_tokens: int, B: int, grad_loss=None, dtype: int = MLPMOE_FP32, stride: int = 0,
+                          grad_stride: int = 0, avail=None, valid=None, stream=None) -> None:
+    """grad: [n_tokens x B] of dtype; counts as mlpmoe_route left them; grad_loss: fp32 [1] on the device or None for 1."""
+    _check(lib.mlpmoe_route_backward(_ptr(logits), dtype, stride, n_tokens, B, _ptr(avail), _ptr(valid), _ptr(counts), _ptr(grad_loss),
+                                     _ptr(grad), grad_stride, _stream(stream)), "mlpmoe_route_backward")
+
+
+def mlpmoe_w4_quantize(W, rows: int, cols: int, group: int, q, scale, zero=None, dtype: int = MLPMOE_BF16,
+                       layout: int = MLPMOE_LAYOUT_LINEAR, stride: int = 0, stream=None) -> None:
+    _check(lib.mlpmoe_w4_quantize(_ptr(W), dtype, layout, stride, rows, cols, group, _ptr(q), _ptr(scale), _ptr(zero), _stream(stream)),
+           "mlpmoe_w4_quantize")
+
+
+def mlpmoe_w4_dequantize(q, scale, zero, rows: int, cols: int, group: int, W, dtype: int = MLPMOE_BF16,
+                         layout: int = MLPMOE_LAYOUT_LINEAR, stride: int = 0, stream=None) -> None:
+    _check(lib.mlpmoe_w4_dequantize(_ptr(q), _ptr(scale), _ptr(zero), rows, cols, group, _ptr(W), dtype, layout, stride, _stream(stream)),
+           "mlpmoe_w4_dequantize")
+
+
+def mlpmoe_w4_layer(d_model: int, d_inter: int, d_b: Sequence[int], group: int, gate, up, down, alpha=None) -> mlpmoe_w4_layer_t:
+    """The description of a layer on 4-bit weights; gate, up and down are (q, scale, zero or None).  It keeps the
+    host arrays it points to, and the tensors as long as it lives."""
+    layer = mlpmoe_w4_layer_t(d_model, d_inter, _arr(d_b, c_int64), _arr(alpha, c_float), len(d_b), group,
+                              *(mlpmoe_w4_matrix_t(_ptr(q), _ptr(s), _ptr(z)) for q, s, z in (gate, up, down)))
+    layer._tensors = (gate, up, down)
+    return layer
+
+
+def mlpmoe_w4_workspace(layer: mlpmoe_w4_layer_t, n_tokens: int) -> int:
+    """Bytes of workspace that mlpmoe_w4_forward needs for n_tokens tokens."""
+    v = c_int64()
+    _check(lib.mlpmoe_w4_workspace(layer, n_tokens, ctypes.byref(v)), "mlpmoe_w4_workspace")
+    return v.value
+
+
+def mlpmoe_w4_forward(layer: mlpmoe_w4_layer_t, x, y, n_tokens: int, workspace, workspace_bytes: int, x_dtype: int = MLPMOE_BF16,
+                      x_stride: int = 0, x_scale=None, x_group: int = 0, select=None, compensate: bool = True, residual=None,
+                      y_dtype: int = MLPMOE_FP32, stream=None) -> None:
+    """layer: from mlpmoe_w4_layer; select: device uint8 [n_tokens x B] or None."""
+    _check(lib.mlpmoe_w4_forward(layer, _ptr(x), x_dtype, x_stride, _ptr(x_scale), x_group, _ptr(select), 1 if compensate else 0,
+                                 _ptr(residual), _ptr(y), y_dtype, n_tokens, _ptr(workspace), workspace_bytes, _stream(stream)),
+           "mlpmoe_w4_forward")
 
 
 def mlpmoe_stack_forward(layers: Sequence[int], x, n_tokens: int, eps: float = 1e-6, stream=None) -> None:

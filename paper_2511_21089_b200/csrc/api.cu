@@ -1263,6 +1263,7 @@ mlpmoe_status_t mlpmoe_forward_host(mlpmoe_handle_t h, const void* x_host, float
 mlpmoe_status_t mlpmoe_rmsnorm(const float* x, void* r, int64_t n_tokens, int64_t d_model, float eps,
                                mlpmoe_dtype_t out_dtype, void* stream) {
   if (n_tokens < 0 || d_model <= 0 || d_model % 4 != 0) return MLPMOE_ERR_INVALID_ARG;
+  if (out_dtype != MLPMOE_BF16 && out_dtype != MLPMOE_FP32) return MLPMOE_ERR_INVALID_ARG;
   if (n_tokens == 0) return MLPMOE_OK;
   if (!x || !r || !aligned16(x) || !aligned16(r)) return MLPMOE_ERR_INVALID_ARG;
   pdl_overlap_enabled() = true;

@@ -1,0 +1,489 @@
+// The router's selection, its balance loss and the loss's gradient (mlpmoe_route, mlpmoe_route_backward).
+//     p[t, :] = softmax of the eligible logits;  S_t = the k largest;  counts[b], prob[b] = mean of p[:, b];
+//     loss = B' sum_b f_b prob[b];   d loss / d logit[t, j] = B' / T p[t, j] (f_j - sum_b f_b p[t, b]).
+// One pass over the logits each way.  A row belongs to LPR lanes of a warp with VPT neighbouring columns each, so a
+// lane's columns never change and the column sums live in its registers until the kernel's end.
+#include <math.h>
+
+#include "../../include/mlpmoe.h"
+#include "internal.h"
+#include "ptx.cuh"
+
+namespace mlpmoe {
+namespace {
+
+constexpr int kMaxB = 256;
+constexpr int kRouteThreads = 256;
+constexpr int kRouteCtas = 296;        // forward: two blocks on each of the 148 SMs, so that the sums to join stay few
+constexpr int kBackwardCtas = 148 * 8;
+constexpr int kFinishThreads = 1024;
+
+// One block's contribution: B probability sums, then B counts and the number of routed tokens as int32.
+__host__ __device__ inline int64_t partial_words(int B) { return 2 * B + 1; }
+
+struct RouteArgs {
+  const void* logits;
+  const uint8_t* avail;
+  const uint8_t* valid;
+  int64_t stride, n;
+  int B, k;
+  uint8_t* select;
+  uint32_t* partial;     // [gridDim.x][2 B + 1]
+  int32_t* counts;
+  float* prob;
+  float* loss;
+  // backward
+  const int32_t* counts_in;
+  const float* grad_loss;
+  void* grad;
+  int64_t grad_stride;
+};
+
+template <int W>
+__device__ __forceinline__ float seg_max(float v) {
+#pragma unroll
+  for (int o = W / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+  return v;
+}
+template <int W>
+__device__ __forceinline__ float seg_sum(float v) {
+#pragma unroll
+  for (int o = W / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+  return v;
+}
+template <int W>
+__device__ __forceinline__ uint32_t seg_max_u32(uint32_t v) {
+  if constexpr (W == 32) {
+    return __reduce_max_sync(0xFFFFFFFFu, v);
+  } else {
+#pragma unroll
+    for (int o = W / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    return v;
+  }
+}
+
+// The row's values of one lane; places that are not eligible become -infinity, +infinity the largest finite value.
+template <typename T, int VPT, bool VEC>
+__device__ __forceinline__ void load_row(const T* row, int c0, int B, uint32_t avail_mask, bool live, float (&x)[VPT]) {
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) x[i] = -INFINITY;
+  if (!live) return;
+  if (VEC) {                                       // B % 4 == 0 and rows on 16 (fp32) or 8 (bf16) bytes
+#pragma unroll
+    for (int i = 0; i < VPT; i += 4) {
+      if (c0 + i >= B) continue;
+      if (sizeof(T) == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(row + c0 + i);
+        x[i] = v.x, x[i + 1] = v.y, x[i + 2] = v.z, x[i + 3] = v.w;
+      } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(row + c0 + i);
+        x[i] = __uint_as_float(v.x << 16), x[i + 1] = __uint_as_float(v.x & 0xFFFF0000u);
+        x[i + 2] = __uint_as_float(v.y << 16), x[i + 3] = __uint_as_float(v.y & 0xFFFF0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i)
+      if (c0 + i < B) x[i] = static_cast<float>(row[c0 + i]);
+  }
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const bool ok = ((avail_mask >> i) & 1u) && x[i] > -INFINITY;   // false for a NaN
+    x[i] = ok ? fminf(x[i], 3.402823466e38f) : -INFINITY;
+  }
+}
+
+template <int VPT>
+__device__ __forceinline__ uint32_t avail_mask_of(const uint8_t* avail, int c0, int B) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i)
+    if (c0 + i < B && (avail == nullptr || avail[c0 + i] != 0)) m |= 1u << i;
+  return m;
+}
+
+// Order-preserving bits of a float; 0 stands for "not eligible" (a float's own image is never 0: -infinity is excluded).
+__device__ __forceinline__ uint32_t key_of(float x) {
+  if (x == -INFINITY) return 0u;
+  const uint32_t u = __float_as_uint(x + 0.0f);    // -0 and +0 are equal: both become +0
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+
+// A block's rows; its column sums go to a.partial, added up in the order of its warps and row segments.
+template <typename T, int LPR, int VPT, bool VEC>
+__global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_constant__ RouteArgs a) {
+  constexpr int kWarps = kRouteThreads / 32, kRows = 32 / LPR;    // kRows: rows of a warp at a time
+  constexpr int kSlots = kWarps * kRows, kCols = LPR * VPT;
+  __shared__ float s_prob[kSlots * kCols];
+  __shared__ int s_count[kSlots * kCols];
+  __shared__ int s_routed[kWarps];
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int seg = lane / LPR, l = lane % LPR, c0 = l * VPT;
+  const uint32_t avail_mask = avail_mask_of<VPT>(a.avail, c0, a.B);
+  const uint32_t seg_lanes = (LPR == 32 ? 0xFFFFFFFFu : ((1u << (LPR % 32)) - 1u)) << (seg * LPR);
+  const bool byte_vec = a.B % 4 == 0 && reinterpret_cast<uintptr_t>(a.select) % 4 == 0;
+  float prob[VPT];
+  int count[VPT], routed = 0;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) prob[i] = 0.0f, count[i] = 0;
+
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps * kRows;
+  for (int64_t base = (static_cast<int64_t>(blockIdx.x) * kWarps + warp) * kRows; base < a.n; base += step) {
+    const int64_t t = base + seg;
+    const bool live = t < a.n && (a.valid == nullptr || a.valid[t] != 0);
+    float x[VPT];
+    load_row<T, VPT, VEC>(static_cast<const T*>(a.logits) + (t < a.n ? t : 0) * a.stride, c0, a.B, avail_mask, live, x);
+    // softmax
+    float m = x[0];
+#pragma unroll
+    for (int i = 1; i < VPT; ++i) m = fmaxf(m, x[i]);
+    m = seg_max<LPR>(m);
+    const bool any = m > -INFINITY;
+    float e[VPT], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      e[i] = x[i] > -INFINITY ? expf(x[i] - m) : 0.0f;
+      sum += e[i];
+    }
+    sum = seg_sum<LPR>(sum);
+    const float inv = any ? 1.0f / sum : 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) prob[i] += e[i] * inv;
+    routed += any && l == 0 ? 1 : 0;
+    // top k: each lane offers the largest of its columns that is not taken yet; the first lane with the row's largest
+    // key takes it (columns ascend with the lane, and inside a lane the lowest index wins a tie)
+    uint32_t key[VPT], taken = 0;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) key[i] = key_of(x[i]);
+    for (int r = 0; r < a.k; ++r) {
+      uint32_t best = key[0];
+      int at = 0;
+#pragma unroll
+      for (int i = 1; i < VPT; ++i)
+        if (key[i] > best) best = key[i], at = i;
+      const uint32_t top = seg_max_u32<LPR>(best);
+      const uint32_t who = __ballot_sync(0xFFFFFFFFu, best == top && top != 0u) & seg_lanes;
+      if (who != 0u && lane == __ffs(who) - 1) {
+        taken |= 1u << at;
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+          if (i == at) key[i] = 0u;
+      }
+      if (__ballot_sync(0xFFFFFFFFu, who != 0u) == 0u) break;     // no row of the warp has an eligible place left
+    }
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) count[i] += (taken >> i) & 1u;
+    if (t < a.n) {
+      uint8_t* out = a.select + t * a.B + c0;
+      if (byte_vec) {
+#pragma unroll
+        for (int i = 0; i < VPT; i += 4) {
+          const uint32_t b = taken >> i;
+          if (c0 + i < a.B)
+            *reinterpret_cast<uint32_t*>(out + i) = (b & 1u) | ((b & 2u) << 7) | ((b & 4u) << 14) | ((b & 8u) << 21);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+          if (c0 + i < a.B) out[i] = (taken >> i) & 1u;
+      }
+    }
+  }
+
+  const int slot = warp * kRows + seg;
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    s_prob[slot * kCols + c0 + i] = prob[i];
+    s_count[slot * kCols + c0 + i] = count[i];
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) routed += __shfl_xor_sync(0xFFFFFFFFu, routed, o);
+  if (lane == 0) s_routed[warp] = routed;
+  __syncthreads();
+  uint32_t* out = a.partial + static_cast<int64_t>(blockIdx.x) * partial_words(a.B);
+  for (int b = threadIdx.x; b < a.B; b += kRouteThreads) {
+    float p = 0.0f;
+    int c = 0;
+    for (int s = 0; s < kSlots; ++s) {
+      p += s_prob[s * kCols + b];
+      c += s_count[s * kCols + b];
+    }
+    out[b] = __float_as_uint(p);
+    out[a.B + b] = static_cast<uint32_t>(c);
+  }
+  if (threadIdx.x == 0) {
+    int c = 0;
+    for (int w = 0; w < kWarps; ++w) c += s_routed[w];
+    out[2 * a.B] = static_cast<uint32_t>(c);
+  }
+}
+
+// Adds the blocks' contributions (in block order), then the loss.  One block.
+__global__ void __launch_bounds__(kFinishThreads) route_finish_kernel(const __grid_constant__ RouteArgs a, int n_partial) {
+  __shared__ float s_prob[kFinishThreads];
+  __shared__ int s_count[kFinishThreads];
+  __shared__ int s_avail;
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int words = static_cast<int>(partial_words(a.B));
+  // thread (part, b): every parts-th block's sums of column b
+  int cols = 8;
+  while (cols < a.B) cols *= 2;
+  const int parts = kFinishThreads / cols, b = threadIdx.x % cols, part = threadIdx.x / cols;
+  float p = 0.0f;
+  int c = 0, routed = 0;
+  if (b < a.B) {
+    for (int i = part; i < n_partial; i += parts) {
+      p += __uint_as_float(a.partial[static_cast<int64_t>(i) * words + b]);
+      c += static_cast<int>(a.partial[static_cast<int64_t>(i) * words + a.B + b]);
+    }
+  }
+  s_prob[threadIdx.x] = p;
+  s_count[threadIdx.x] = c;
+  if (threadIdx.x == 0) s_avail = 0;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    for (int i = threadIdx.x; i < n_partial; i += 32) routed += static_cast<int>(a.partial[static_cast<int64_t>(i) * words + 2 * a.B]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) routed += __shfl_xor_sync(0xFFFFFFFFu, routed, o);
+    if (threadIdx.x == 0) a.counts[a.B] = routed;
+  }
+  if (part == 0 && b < a.B) {
+    p = 0.0f;
+    c = 0;
+    for (int i = 0; i < parts; ++i) {
+      p += s_prob[i * cols + b];
+      c += s_count[i * cols + b];
+    }
+    a.counts[b] = c;
+    if (a.avail == nullptr || a.avail[b] != 0) atomicAdd(&s_avail, 1);
+  }
+  __syncthreads();
+  if (part == 0) {
+    s_prob[b] = b < a.B ? p : 0.0f;
+    s_count[b] = b < a.B ? c : 0;
+  }
+  __syncthreads();
+  const int total_routed = a.counts[a.B];
+  if (threadIdx.x < 32) {
+    double dot = 0.0;
+    int64_t total = 0;
+    for (int i = threadIdx.x; i < cols; i += 32) {
+      dot += static_cast<double>(s_count[i]) * static_cast<double>(s_prob[i]);
+      total += s_count[i];
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
+      total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+    }
+    if (threadIdx.x == 0)
+      a.loss[0] = total > 0 ? static_cast<float>(s_avail * dot / (static_cast<double>(total) * total_routed)) : 0.0f;
+  }
+  if (part == 0 && b < a.B) a.prob[b] = total_routed > 0 ? p / static_cast<float>(total_routed) : 0.0f;
+}
+
+template <typename T, int LPR, int VPT, bool VEC>
+__global__ void __launch_bounds__(kRouteThreads) route_backward_kernel(const __grid_constant__ RouteArgs a) {
+  constexpr int kWarps = kRouteThreads / 32, kRows = 32 / LPR;
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int seg = lane / LPR, l = lane % LPR, c0 = l * VPT;
+  const uint32_t avail_mask = avail_mask_of<VPT>(a.avail, c0, a.B);
+  // f of the lane's columns, and the factor grad_loss B' / T
+  int total = 0, n_avail = 0;
+  float f[VPT];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const int c = c0 + i < a.B ? a.counts_in[c0 + i] : 0;
+    f[i] = static_cast<float>(c);
+    total += c;
+  }
+  n_avail = __popc(avail_mask);
+#pragma unroll
+  for (int o = LPR / 2; o > 0; o >>= 1) {
+    total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+    n_avail += __shfl_xor_sync(0xFFFFFFFFu, n_avail, o);
+  }
+  const int routed = a.counts_in[a.B];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) f[i] = total > 0 ? f[i] / static_cast<float>(total) : 0.0f;
+  const float g = a.grad_loss != nullptr ? a.grad_loss[0] : 1.0f;
+  const float scale = routed > 0 ? g * static_cast<float>(n_avail) / static_cast<float>(routed) : 0.0f;
+
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps * kRows;
+  for (int64_t base = (static_cast<int64_t>(blockIdx.x) * kWarps + warp) * kRows; base < a.n; base += step) {
+    const int64_t t = base + seg;
+    const bool live = t < a.n && (a.valid == nullptr || a.valid[t] != 0);
+    float x[VPT];
+    load_row<T, VPT, VEC>(static_cast<const T*>(a.logits) + (t < a.n ? t : 0) * a.stride, c0, a.B, avail_mask, live, x);
+    float m = x[0];
+#pragma unroll
+    for (int i = 1; i < VPT; ++i) m = fmaxf(m, x[i]);
+    m = seg_max<LPR>(m);
+    float sum = 0.0f, dot = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+      x[i] = x[i] > -INFINITY ? expf(x[i] - m) : 0.0f;
+      sum += x[i];
+      dot += x[i] * f[i];
+    }
+    sum = seg_sum<LPR>(sum);
+    dot = seg_sum<LPR>(dot);
+    const float inv = m > -INFINITY ? 1.0f / sum : 0.0f;
+    const float mean_f = dot * inv, c = scale * inv;
+    if (t >= a.n) continue;
+    T* out = static_cast<T*>(a.grad) + t * a.grad_stride + c0;
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) x[i] = c * x[i] * (f[i] - mean_f);
+    if (VEC) {
+#pragma unroll
+      for (int i = 0; i < VPT; i += 4) {
+        if (c0 + i >= a.B) continue;
+        if (sizeof(T) == 4) {
+          *reinterpret_cast<float4*>(out + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        } else {
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(x[i], x[i + 1]), hi = __floats2bfloat162_rn(x[i + 2], x[i + 3]);
+          *reinterpret_cast<uint2*>(out + i) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < VPT; ++i)
+        if (c0 + i < a.B) out[i] = static_cast<T>(x[i]);
+    }
+  }
+}
+
+enum Op { FORWARD, BACKWARD };
+
+// Lanes of a row: the narrowest power of two that holds B columns, four to a lane (eight above 128).
+int lanes_per_row(int B) {
+  int lanes = 2;
+  while (lanes < 32 && lanes * 4 < B) lanes *= 2;
+  return lanes;
+}
+
+// Blocks for n rows, at most `most`: the rest of the rows in further turns of the same blocks.
+unsigned row_blocks(int64_t n, int B, int most) {
+  const int64_t rows = 32 / lanes_per_row(B) * (kRouteThreads / 32);
+  const int64_t need = (n + rows - 1) / rows;
+  return static_cast<unsigned>(need < most ? need : most);
+}
+
+template <typename T, int LPR, int VPT, bool VEC>
+cudaError_t launch_op(Op op, const RouteArgs& a, cudaStream_t st) {
+  if (op == FORWARD)
+    return launch_pdl(route_kernel<T, LPR, VPT, VEC>, dim3(row_blocks(a.n, a.B, kRouteCtas)), dim3(kRouteThreads), 0, st, a);
+  return launch_pdl(route_backward_kernel<T, LPR, VPT, VEC>, dim3(row_blocks(a.n, a.B, kBackwardCtas)), dim3(kRouteThreads), 0, st, a);
+}
+
+template <typename T, bool VEC>
+cudaError_t launch_width(Op op, const RouteArgs& a, cudaStream_t st) {
+  switch (lanes_per_row(a.B)) {
+    case 2: return launch_op<T, 2, 4, VEC>(op, a, st);
+    case 4: return launch_op<T, 4, 4, VEC>(op, a, st);
+    case 8: return launch_op<T, 8, 4, VEC>(op, a, st);
+    case 16: return launch_op<T, 16, 4, VEC>(op, a, st);
+    default: return a.B <= 128 ? launch_op<T, 32, 4, VEC>(op, a, st) : launch_op<T, 32, 8, VEC>(op, a, st);
+  }
+}
+
+cudaError_t launch_any(Op op, const RouteArgs& a, mlpmoe_dtype_t dtype, cudaStream_t st) {
+  const uintptr_t word = dtype == MLPMOE_FP32 ? 16 : 8;
+  bool vec = a.B % 4 == 0 && a.stride % 4 == 0 && reinterpret_cast<uintptr_t>(a.logits) % word == 0;
+  if (op == BACKWARD) vec = vec && a.grad_stride % 4 == 0 && reinterpret_cast<uintptr_t>(a.grad) % word == 0;
+  if (dtype == MLPMOE_FP32) return vec ? launch_width<float, true>(op, a, st) : launch_width<float, false>(op, a, st);
+  return vec ? launch_width<__nv_bfloat16, true>(op, a, st) : launch_width<__nv_bfloat16, false>(op, a, st);
+}
+
+mlpmoe_status_t check_router(const void* logits, mlpmoe_dtype_t dtype, int64_t* stride, int64_t n, int32_t B) {
+  if (n < 0 || n > INT32_MAX || B <= 0) return MLPMOE_ERR_INVALID_ARG;
+  if (dtype != MLPMOE_FP32 && dtype != MLPMOE_BF16) return MLPMOE_ERR_INVALID_ARG;
+  if (B > kMaxB) return MLPMOE_ERR_UNSUPPORTED;
+  if (*stride == 0) *stride = B;
+  if (*stride < B) return MLPMOE_ERR_INVALID_ARG;
+  if (n > 0 && (!logits || reinterpret_cast<uintptr_t>(logits) % (dtype == MLPMOE_FP32 ? 4 : 2) != 0)) return MLPMOE_ERR_INVALID_ARG;
+  return MLPMOE_OK;
+}
+
+inline bool on4(const void* p) { return reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
+}  // namespace
+}  // namespace mlpmoe
+
+using namespace mlpmoe;
+
+extern "C" {
+
+mlpmoe_status_t mlpmoe_route_workspace(int64_t n_tokens, int32_t B, int64_t* bytes) {
+  if (n_tokens < 0 || n_tokens > INT32_MAX || B <= 0 || !bytes) return MLPMOE_ERR_INVALID_ARG;
+  if (B > kMaxB) return MLPMOE_ERR_UNSUPPORTED;
+  *bytes = (kRouteCtas * partial_words(B) * 4 + 15) / 16 * 16;
+  return MLPMOE_OK;
+}
+
+mlpmoe_status_t mlpmoe_route(const void* logits, mlpmoe_dtype_t dtype, int64_t stride, int64_t n_tokens, int32_t B, int32_t top_k,
+                             const uint8_t* avail, const uint8_t* valid, uint8_t* select, int32_t* counts, float* prob, float* loss,
+                             void* workspace, int64_t workspace_bytes, void* stream) {
+  mlpmoe_status_t rc = check_router(logits, dtype, &stride, n_tokens, B);
+  if (rc != MLPMOE_OK) return rc;
+  if (top_k < 1 || top_k > B) return MLPMOE_ERR_INVALID_ARG;
+  if (!counts || !prob || !loss || !on4(counts) || !on4(prob) || !on4(loss) || (n_tokens > 0 && !select)) return MLPMOE_ERR_INVALID_ARG;
+  int64_t need = 0;
+  mlpmoe_route_workspace(n_tokens, B, &need);
+  if (!workspace || workspace_bytes < need || reinterpret_cast<uintptr_t>(workspace) % 16 != 0) return MLPMOE_ERR_INVALID_ARG;
+  RouteArgs a = {};
+  a.logits = logits;
+  a.avail = avail;
+  a.valid = valid;
+  a.stride = stride;
+  a.n = n_tokens;
+  a.B = B;
+  a.k = top_k;
+  a.select = select;
+  a.partial = static_cast<uint32_t*>(workspace);
+  a.counts = counts;
+  a.prob = prob;
+  a.loss = loss;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  pdl_overlap_enabled() = true;
+  int n_partial = 0;
+  if (n_tokens > 0) {
+    n_partial = static_cast<int>(row_blocks(n_tokens, B, kRouteCtas));
+    if (launch_any(FORWARD, a, dtype, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
+  }
+  if (launch_pdl(route_finish_kernel, dim3(1), dim3(kFinishThreads), 0, st, a, n_partial) != cudaSuccess) return MLPMOE_ERR_CUDA;
+  return MLPMOE_OK;
+}
+
+mlpmoe_status_t mlpmoe_route_backward(const void* logits, mlpmoe_dtype_t dtype, int64_t stride, int64_t n_tokens, int32_t B,
+                                      const uint8_t* avail, const uint8_t* valid, const int32_t* counts, const float* grad_loss,
+                                      void* grad, int64_t grad_stride, void* stream) {
+  mlpmoe_status_t rc = check_router(logits, dtype, &stride, n_tokens, B);
+  if (rc != MLPMOE_OK) return rc;
+  if (grad_stride == 0) grad_stride = B;
+  if (grad_stride < B) return MLPMOE_ERR_INVALID_ARG;
+  if (n_tokens == 0) return MLPMOE_OK;
+  if (!counts || !grad || !on4(counts) || !on4(grad_loss)) return MLPMOE_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(grad) % (dtype == MLPMOE_FP32 ? 4 : 2) != 0) return MLPMOE_ERR_INVALID_ARG;
+  if (grad == logits && grad_stride != stride && n_tokens > 1) return MLPMOE_ERR_INVALID_ARG;
+  RouteArgs a = {};
+  a.logits = logits;
+  a.avail = avail;
+  a.valid = valid;
+  a.stride = stride;
+  a.n = n_tokens;
+  a.B = B;
+  a.counts_in = counts;
+  a.grad_loss = grad_loss;
+  a.grad = grad;
+  a.grad_stride = grad_stride;
+  pdl_overlap_enabled() = true;
+  return launch_any(BACKWARD, a, dtype, static_cast<cudaStream_t>(stream)) == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
+}
+
+}  // extern "C"
