@@ -363,8 +363,8 @@ typedef struct {
 } mlpmoe_w4_layer_t;
 
 /*
- * The layer equation of Section 3.1 on 4-bit weights, for decode (the weights are streamed once per 64 tokens or fewer;
- * it pays up to about 64 tokens, any count is computed):
+ * The layer equation of Section 3.1 on 4-bit weights, for decode (any token count is computed, but the weights are read
+ * once per a few tokens, so a layer of mlpmoe_create is faster for long inputs):
  *     y_t = residual_t + c_t * sum_{b in S_t} alpha_b W_down^(b) [ silu(W_gate^(b) x_t) (.) W_up^(b) x_t ]
  * with S_t and c_t as in mlpmoe_forward_routed (select NULL: every branch with alpha_b != 0, c_t = 1).  Branches that
  * no token selects are not read.  Products and sums are fp32; the intermediate activation is held as two (y bf16) or three
@@ -377,7 +377,7 @@ typedef struct {
  *   residual device fp32 [n_tokens x d_model] or NULL; may be y when y_dtype is fp32
  *   y        device, [n_tokens x d_model] of y_dtype (fp32 or bf16), 16-byte aligned
  *   workspace device, 256-byte aligned, of the size that mlpmoe_w4_workspace gives
- * d_model a multiple of 8, d_b multiples of 16, B <= 256, d_model and d_inter up to 2^20, n_tokens up to 65536.
+ * d_model a multiple of 8, d_b multiples of 16, B <= 256, d_model and d_inter up to 65536, n_tokens up to 65536.
  * The same call gives the same bits every time.  Errors as mlpmoe_create and mlpmoe_forward_ex.
  */
 mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x, mlpmoe_dtype_t x_dtype, int64_t x_stride,

@@ -9,6 +9,7 @@ namespace mlpmoe {
 namespace {
 
 constexpr int kRows = 32, kCols = 128, kThreads = 256;
+constexpr int64_t kMaxDim = int64_t(1) << 20;      // keeps the grid within its limits
 
 struct QuantArgs {
   const void* w_in;
@@ -156,7 +157,7 @@ mlpmoe_status_t run(bool back, const void* W, mlpmoe_dtype_t dtype, mlpmoe_layou
   if (rows < 0 || cols < 0 || (dtype != MLPMOE_FP32 && dtype != MLPMOE_BF16)) return MLPMOE_ERR_INVALID_ARG;
   if (layout != MLPMOE_LAYOUT_LINEAR && layout != MLPMOE_LAYOUT_PAPER) return MLPMOE_ERR_INVALID_ARG;
   if (group != 32 && group != 64 && group != 128) return MLPMOE_ERR_UNSUPPORTED;
-  if (rows > kW4MaxDim || cols > kW4MaxDim) return MLPMOE_ERR_UNSUPPORTED;
+  if (rows > kMaxDim || cols > kMaxDim) return MLPMOE_ERR_UNSUPPORTED;
   const int64_t inner = layout == MLPMOE_LAYOUT_LINEAR ? cols : rows;
   if (stride == 0) stride = inner;
   if (stride < inner) return MLPMOE_ERR_INVALID_ARG;
