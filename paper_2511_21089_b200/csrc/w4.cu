@@ -31,16 +31,16 @@ int w4_plan(W4Args* a, int pieces, int group) {
       for (; tokens > 0; --tokens) {
         const int cols = pieces * tokens, nt = (cols + 7) / 8;
         const int64_t ring = w4::kWarps * (nt == 1 ? 4 : 3) * stage;
-        const int64_t x = static_cast<int64_t>(entries) * cols * 256, sx = a->x_groups > 1 ? static_cast<int64_t>(entries) * gpb * nt * 32 : 0;
+        const int64_t x = static_cast<int64_t>(entries) * nt * 1024, units = static_cast<int64_t>(entries) * gpb * nt * 64;
         const int64_t sums = static_cast<int64_t>(w4::kWarps - 1 + per) * nt * 8 * w4::kColPitch * 4;
         const int64_t own = static_cast<int64_t>(per) * tokens * 64;
-        if (ring + x + sx + sums + entries * 4 + per * 4 > w4::kSmemMax || own > ring + x) continue;
+        if (ring + x + units + sums + entries * 4 + per * 4 > w4::kSmemMax || own > ring + x) continue;
         const int chunks = (a->n + tokens - 1) / tokens;
         const int even = (a->n + chunks - 1) / chunks;
         const int64_t blocks = static_cast<int64_t>((a->tiles + per - 1) / per) * chunks;
         const int64_t waves = (blocks + kResident[i] - 1) / kResident[i];
         const int64_t steps = (static_cast<int64_t>(per) * (entries / 2) + w4::kWarps - 1) / w4::kWarps;
-        const int64_t cost = waves * (steps * w4::kWarps * stage + static_cast<int64_t>(entries) * even * pieces * 256 +
+        const int64_t cost = waves * (steps * w4::kWarps * stage + static_cast<int64_t>(entries) * even * 512 +
                                       static_cast<int64_t>(per) * even * 128 + (cluster > 1 ? 32768 : 0));
         if (cost < best_cost) {
           best_cost = cost;
@@ -90,23 +90,7 @@ W4Mat matrix(const mlpmoe_w4_matrix_t& m, int64_t rows, int64_t cols, int group)
   return r;
 }
 
-// The down product of n tokens, split; *cluster receives its cluster.
-W4Args down_args(const mlpmoe_w4_layer_t* l, int n, int pieces, int* cluster) {
-  W4Args w = {};
-  w.m[0] = w.m[1] = matrix(l->down, l->d_model, l->d_inter, l->group);
-  w.rows = static_cast<int>(l->d_model);
-  w.tiles = (w.rows + 15) / 16;
-  w.K = static_cast<int>(l->d_inter);
-  w.kblocks = (w.K + 127) / 128;
-  w.n = n;
-  *cluster = w4_plan(&w, pieces, l->group);
-  return w;
-}
-
-// Bytes of the intermediate activations of a split.
-int64_t h_bytes(const W4Args& w) {
-  return (static_cast<int64_t>(w.c.chunks) * w.kblocks * w.c.cols() * 256 + 255) / 256 * 256;
-}
+inline int64_t h_bytes(const mlpmoe_w4_layer_t* l, int64_t n) { return (n * l->d_inter * 4 + 255) / 256 * 256; }
 
 }  // namespace
 }  // namespace mlpmoe
@@ -121,13 +105,7 @@ mlpmoe_status_t mlpmoe_w4_workspace(const mlpmoe_w4_layer_t* layer, int64_t n_to
   if (rc != MLPMOE_OK) return rc;
   if (n_tokens < 0) return MLPMOE_ERR_INVALID_ARG;
   if (n_tokens > kW4MaxTokens) return MLPMOE_ERR_UNSUPPORTED;
-  *bytes = 256;
-  for (int pieces = 2; pieces <= 3 && n_tokens > 0; ++pieces) {
-    int cluster = 0;
-    const int64_t need = h_bytes(down_args(layer, static_cast<int>(n_tokens), pieces, &cluster));
-    if (cluster == 0) return MLPMOE_ERR_UNSUPPORTED;
-    *bytes = need > *bytes ? need : *bytes;
-  }
+  *bytes = h_bytes(layer, n_tokens);
   return MLPMOE_OK;
 }
 
@@ -153,12 +131,9 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
   if (!x || !y || !on(x, 16) || !on(y, 16) || !on(residual, 16) || (scaled && (!x_scale || !on(x_scale, 4)))) return MLPMOE_ERR_INVALID_ARG;
   if (residual && residual == y && y_dtype != MLPMOE_FP32) return MLPMOE_ERR_INVALID_ARG;
 
-  const int group = layer->group, n = static_cast<int>(n_tokens);
-  int u_cluster = 0, w_cluster = 0;
-  W4Args w = down_args(layer, n, y_dtype == MLPMOE_FP32 ? 3 : 2, &w_cluster);
-  if (w_cluster == 0) return MLPMOE_ERR_UNSUPPORTED;
-  if (!workspace || workspace_bytes < h_bytes(w) || !on(workspace, 256)) return MLPMOE_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < h_bytes(layer, n_tokens) || !on(workspace, 256)) return MLPMOE_ERR_INVALID_ARG;
 
+  const int group = layer->group, n = static_cast<int>(n_tokens), digits = y_dtype == MLPMOE_FP32 ? 3 : 2;
   W4Args u = {};
   u.m[0] = matrix(layer->gate, I, d, group);
   u.m[1] = matrix(layer->up, I, d, group);
@@ -172,14 +147,11 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
     u.x_groups = x_group == 0 ? 1 : static_cast<int>((d + x_group - 1) / x_group);
     for (int64_t g = group; x_group != 0 && g < x_group; g *= 2) ++u.x_shift;
   }
-  u_cluster = w4_plan(&u, x_dtype == MLPMOE_FP32 ? 3 : 1, group);
-  if (u_cluster == 0) return MLPMOE_ERR_UNSUPPORTED;
+  const int u_cluster = w4_plan(&u, digits, group);
   u.x = x;
   u.x_kind = x_dtype;
   u.x_stride = x_stride;
-  u.hc = w.c;
-  u.h_kblocks = w.kblocks;
-  u.h = static_cast<__nv_bfloat16*>(workspace);
+  u.h = static_cast<float*>(workspace);
   u.B = layer->B;
   u.select = select;
   u.dense = select == nullptr;
@@ -188,12 +160,24 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
     u.alpha[b] = layer->alpha ? layer->alpha[b] : 1.0f;
     if (u.alpha[b] == 0.0f) u.dense = 0;
   }
+
+  W4Args w = {};
+  w.m[0] = w.m[1] = matrix(layer->down, d, I, group);
+  w.rows = static_cast<int>(d);
+  w.tiles = static_cast<int>((d + 15) / 16);
+  w.K = static_cast<int>(I);
+  w.kblocks = static_cast<int>((I + 127) / 128);
+  w.n = n;
+  const int w_cluster = w4_plan(&w, digits, group);
+  if (u_cluster == 0 || w_cluster == 0) return MLPMOE_ERR_UNSUPPORTED;
+  w.x = workspace;
+  w.x_kind = MLPMOE_FP32;
+  w.x_stride = I;
   w.B = u.B;
   w.select = select;
   w.dense = u.dense;
   memcpy(w.off, u.off, sizeof(u.off));
   memcpy(w.alpha, u.alpha, sizeof(u.alpha));
-  w.h_in = static_cast<const uint4*>(workspace);
   w.compensate = compensate ? 1 : 0;
   w.residual = residual;
   w.y = y;

@@ -11,8 +11,8 @@ constexpr int kW4MaxBranches = 256;
 __host__ __device__ inline int64_t w4_pitch(int64_t cols) { return (cols + 31) / 32 * 16; }     // bytes of a row of codes
 __host__ __device__ inline int64_t w4_rows16(int64_t rows) { return (rows + 15) / 16 * 16; }    // elements of a row of scales
 
-// The columns of a product: a token is `pieces` columns (bf16 pieces whose sum is the activation); the tokens are cut
-// into `chunks` of `tokens` each, and column c of a chunk is piece c / tokens of its token c % tokens.
+// The columns of a product: a token is `pieces` columns (digits of its activations); the tokens are cut into `chunks` of
+// `tokens` each, and column c of a chunk is digit c / tokens of its token c % tokens.
 struct W4Cols {
   int pieces, tokens, chunks;
   __host__ __device__ int cols() const { return pieces * tokens; }
@@ -39,17 +39,14 @@ struct W4Args {
   // the branches: neurons of branch b are off[b] .. off[b + 1]
   int B, dense;             // dense: every branch is computed for every token, nothing of the selection is read
   const uint8_t* select;    // [n x B] or null
-  // gate|up
+  // activations: the layer's input (gate|up), or the intermediate activations (down)
   const void* x;
   int x_kind;
   int64_t x_stride;
-  const float* x_scale;     // [n x x_groups] (null: 1)
-  int x_groups, x_shift;    // scale of the activations of weight group g: g >> x_shift; x_groups = 1: applied to the sums
-  W4Cols hc;                // columns of the down product
-  int h_kblocks;
-  __nv_bfloat16* h;         // intermediate activations in unit order: [chunk][kblock][4][cols][4] units of 8 bf16
+  const float* x_scale;     // [n x x_groups] or null
+  int x_groups, x_shift;    // group of x_scale of weight group g: g >> x_shift (x_groups = 1: 0)
+  float* h;                 // gate|up: intermediate activations [n x rows]
   // down
-  const uint4* h_in;
   int compensate;
   const float* residual;
   void* y;

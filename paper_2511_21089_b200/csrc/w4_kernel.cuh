@@ -3,12 +3,17 @@
 //     down:     y[m, t] = residual + c_t sum_j Wd[m, j] h[j, t]
 // with W[r, k] = (code - zero) * scale, one scale and zero per row and group of K.
 //
-// Bound by HBM: the codes are read once.  Between the copy and the tensor core a code costs about 1.4 integer and
-// half-precision operations, which has to stay below the copy's time: a word of eight codes becomes four pairs
-// (128 + code) as bf16 with one AND-OR each (the codes slide into the mantissa of 128.0), less (128 + zero), exact in
-// bf16; mma.sync then multiplies whole numbers of at most 5 bits with the activations and adds in fp32, and the
-// group's scale is applied to the group's sums in fp32.  mma.sync and not tcgen05: the weights would have to go back
-// through shared memory as bf16 (four times the bytes) for a product whose time is the copy's anyway.
+// Bound by HBM: the codes are read once.  Between the copy and the result an SM issues only a few operations per code, and
+// that is what limits such a kernel, so the products are taken on whole numbers (mma.sync, u8 x s8 in s32, exact): a
+// word of eight codes becomes two operand registers with two ANDs and a shift, where a bf16 product needs eleven
+// operations (210 against 256 issued per 16 x 128 block of codes even after tuning).  The activations are held as
+// fixed point inside each group of K: x = (d0 + 256 d1 + 65536 d2) * unit with digits of 8 bits, unit = the group's
+// largest |x| / 8323072; every digit is a column of the product, so up to eight columns (two tokens of three digits)
+// cost what one does.  Three digits (an fp32 y) keep 2^-23 of the group's largest, which is what an fp32 sum keeps;
+// two (y rounded to bf16, 2^-8) keep 2^-16.  sum (code - zero) x = sum code x - zero sum x exactly, the second sum being
+// the group's own; scale and unit are applied to the group's whole-number sum in fp32.
+// mma.sync and not tcgen05: a scale per group of K means reading the accumulators back after every 32 to 128 columns of
+// K, and for a few tokens the product's time is the copy's anyway.
 //
 // One block per SM takes an equal share of the 16-row tiles (gate|up: the gate and up rows of eight neurons, so that a
 // lane ends with both sums of its neurons).  Its steps, (tile, 256 columns of K), are dealt to the 16 warps in equal
@@ -16,8 +21,8 @@
 // on every call.  Blocks of a cluster share K where the activations of all of K would not fit in shared memory, or
 // where there are few rows.  Every warp keeps its own ring of stages filled by cp.async: no barrier in the loop.
 //
-// A pair of codes in a register is (k, k + 4) of eight consecutive k, and the four lanes of a row hold different
-// eights: the activations stand in shared memory to match, one 16-byte unit for eight consecutive k of one column.
+// The four lanes of a row hold different eights of consecutive k, and a register of codes is the even or the odd four of an
+// eight: the activations stand in shared memory to match, eight bytes (even four, odd four) for each eight.
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_fp8.h>
@@ -49,9 +54,6 @@ template <int GPB>
 __host__ __device__ constexpr int unit_k8(int w, int t) {
   return GPB == 1 ? 4 * t + w : (GPB == 2 ? 8 * (w >> 1) + 2 * t + (w & 1) : 4 * w + t);
 }
-// Place of element e of a unit: (0, 4), (1, 5), (2, 6), (3, 7).
-__host__ __device__ constexpr int unit_pos(int e) { return e < 4 ? 2 * e : 2 * (e - 4) + 1; }
-
 // A stage: two K-blocks of 16 rows x 64 bytes of codes, then the scales and the zeros of their 8-row halves.
 template <int GPB>
 __host__ __device__ constexpr int stage_bytes() {
@@ -64,14 +66,14 @@ __host__ __device__ constexpr int stages() {
 
 // Dynamic shared memory, in bytes from its start.
 struct Smem {
-  int x, sx, sums, list, tiles, total;
+  int x, unit, sums, list, tiles, total;
 };
 template <int NT, int GPB>
 __host__ __device__ inline Smem smem_of(const W4Args& a) {
   Smem s;
-  s.x = kWarps * stages<NT>() * stage_bytes<GPB>();                       // activations: [entry][4][cols][4] units
-  s.sx = s.x + a.entries * a.c.cols() * 256;                              // their scales: [entry][GPB][8 NT]
-  s.sums = s.sx + (a.x_groups > 1 ? a.entries * GPB * NT * 8 * 4 : 0);    // parts of the sums: [warp + tile][column][16 rows]
+  s.x = kWarps * stages<NT>() * stage_bytes<GPB>();                       // digits: [entry][2][8 NT][4] pairs of eights
+  s.unit = s.x + a.entries * NT * 8 * 128;                                // their (unit, - sum of digits): [entry][GPB][8 NT]
+  s.sums = s.unit + a.entries * GPB * NT * 8 * 8;                         // parts of the sums: [warp + tile][column][16 rows]
   s.list = s.sums + (kWarps - 1 + a.tiles_per_block) * NT * 8 * kColPitch * 4;
   s.tiles = s.list + a.entries * 4;                                       // the block's K-blocks, then its tiles
   s.total = s.tiles + a.tiles_per_block * 4;
@@ -88,19 +90,10 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Eight codes -> four bf16 pairs code - zero, in the order of unit_pos; bias = (128 + zero) twice.
-__device__ __forceinline__ void unpack(uint32_t w, uint32_t bias, uint32_t (&p)[4]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t u = ((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u;
-    const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u), *reinterpret_cast<const __nv_bfloat162*>(&bias));
-    p[i] = *reinterpret_cast<const uint32_t*>(&v);
-  }
-}
-
-__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+// d += a x b on whole numbers: a 16 rows x 32 codes (u8), b 32 digits x 8 columns (s8).
+__device__ __forceinline__ void mma(int (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
@@ -121,23 +114,19 @@ __device__ __forceinline__ int branch_of(const W4Args& a, int neuron) {
   return lo;
 }
 
-// Eight consecutive activations of one token -> `pieces` units of bf16 whose sum they are.
-__device__ __forceinline__ void stage_activations(const W4Args& a, int64_t at, bool in, uint4* unit, int piece_step) {
-  float v[8];
-  if (!in) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-  } else if (a.x_kind == MLPMOE_FP32) {
-    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(a.x) + at);
+// Eight consecutive activations of one token, from element `at` of x (gate|up) or h (down, fp32).
+__device__ __forceinline__ void load_eight(const void* x, int kind, int64_t at, float (&v)[8]) {
+  if (kind == MLPMOE_FP32) {
+    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + at);
     const float4 lo = p[0], hi = p[1];
     v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
-  } else if (a.x_kind == MLPMOE_BF16) {
-    const uint4 w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.x) + at);
+  } else if (kind == MLPMOE_BF16) {
+    const uint4 w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(x) + at);
     v[0] = __uint_as_float(w.x << 16), v[1] = __uint_as_float(w.x & 0xFFFF0000u), v[2] = __uint_as_float(w.y << 16),
     v[3] = __uint_as_float(w.y & 0xFFFF0000u), v[4] = __uint_as_float(w.z << 16), v[5] = __uint_as_float(w.z & 0xFFFF0000u),
     v[6] = __uint_as_float(w.w << 16), v[7] = __uint_as_float(w.w & 0xFFFF0000u);
   } else {
-    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(a.x) + at);
+    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(x) + at);
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
       const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>((e < 4 ? w.x : w.y) >> (8 * (e & 3))), __NV_E4M3);
@@ -145,21 +134,10 @@ __device__ __forceinline__ void stage_activations(const W4Args& a, int64_t at, b
       v[e] = f.x, v[e + 1] = f.y;
     }
   }
-  for (int p = 0; p < a.c.pieces; ++p) {
-    uint32_t o[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const __nv_bfloat162 pair = __floats2bfloat162_rn(v[e], v[e + 4]);
-      v[e] -= __low2float(pair);
-      v[e + 4] -= __high2float(pair);
-      o[e] = *reinterpret_cast<const uint32_t*>(&pair);
-    }
-    unit[p * piece_step] = make_uint4(o[0], o[1], o[2], o[3]);
-  }
 }
 
 // grid: (shares of the row tiles, cluster along K, chunks of tokens)
-template <int NT, int GPB, bool GATEUP>
+template <int NT, int GPB, bool GATEUP, bool ZERO>
 __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__ W4Args a) {
   constexpr int kStages = stages<NT>(), kStage = stage_bytes<GPB>(), kWords = 4 / GPB;
   extern __shared__ __align__(128) uint8_t smem[];
@@ -260,7 +238,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   const uint32_t q_dst = ring + g * 64 + (t ^ ((g >> 1) & 3)) * 16;
   const int s_block = (lane / (2 * GPB)) & 1, s_half = (lane / GPB) & 1, s_group = lane % GPB;   // lanes below 4 GPB
   const W4Mat& sm = a.m[s_half];
-  const bool s_lane = lane < 4 * GPB, z_lane = s_lane && sm.zero != nullptr;
+  const bool s_lane = lane < 4 * GPB, z_lane = ZERO && s_lane && sm.zero != nullptr;
   const uint8_t* q_src[2];
   bool q_ok[2], s_ok = false;
   int s_row = 0;
@@ -277,6 +255,10 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
     s_ok = s_row < a.rows;
   };
   if (i_left > 0) open_tile();
+  if (ZERO && s_lane && sm.zero == nullptr) {        // a half without stored zeros beside one with them: 8 in every slot, for good
+    for (int i = 0; i < kStages; ++i)
+      *reinterpret_cast<uint2*>(smem + (warp * kStages + i) * kStage + 2048 + 4 * GPB * 16 + lane * 8) = make_uint2(0x08080808u, 0x08080808u);
+  }
   auto issue = [&](int slot) {
     if (i_left > 0) {
       const int2 kb = *reinterpret_cast<const int2*>(s_list + 2 * i_step);
@@ -309,51 +291,81 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
 #pragma unroll
   for (int i = 0; i < kStages - 1; ++i) issue(i);
 
-  // ---- the activations of this block's K-blocks
-  uint4* s_x = reinterpret_cast<uint4*>(smem + L.x);
-  float* s_sx = reinterpret_cast<float*>(smem + L.sx);
+  // ---- the activations of this block's K-blocks as digits: a thread takes eight k of one token, the group's 4, 8 or 16
+  // threads are neighbours
+  uint2* s_x = reinterpret_cast<uint2*>(smem + L.x);
+  float2* s_unit = reinterpret_cast<float2*>(smem + L.unit);
   const int even_entries = 2 * steps;
-  if (GATEUP) {
-    for (int i = threadIdx.x; i < even_entries * 16 * tokens; i += kThreads) {
-      const int k8 = i & 15, entry = (i >> 4) % even_entries, tok = (i >> 4) / even_entries;
-      const int block = s_list[entry], token = chunk * tokens + tok, k = block * 128 + k8 * 8;
-      stage_activations(a, token * a.x_stride + k, block >= 0 && k < a.K && token < a.n,
-                        s_x + ((entry * 4 + unit_word<GPB>(k8)) * cols + tok) * 4 + unit_lane<GPB>(k8), tokens * 4);
+  if (!GATEUP) ptx::griddep_wait();     // h is complete
+  for (int i = threadIdx.x; i < even_entries * GPB * NT * 8; i += kThreads)
+    if (i % (NT * 8) >= cols) s_unit[i] = make_float2(0.0f, 0.0f);
+  for (int i = threadIdx.x; i < even_entries * 16 * tokens; i += kThreads) {      // a multiple of 32 threads take part
+    const int k8 = i & 15, entry = (i >> 4) % even_entries, tok = (i >> 4) / even_entries;
+    const int block = s_list[entry], token = chunk * tokens + tok, k = block * 128 + k8 * 8;
+    bool in = block >= 0 && k < a.K && token < a.n;
+    if (!GATEUP && in && !a.dense) {    // what the token does not compute is 0, and gate|up may have left it unwritten
+      const int b = branch_of(a, k);
+      in = s_active[b] != 0 && (a.select == nullptr || a.select[static_cast<int64_t>(token) * a.B + b] != 0);
     }
-    if (a.x_groups > 1) {
-      for (int i = threadIdx.x; i < even_entries * GPB * NT * 8; i += kThreads) {
-        const int c = i % (NT * 8), j = i / (NT * 8) % GPB, entry = i / (NT * 8) / GPB, token = chunk * tokens + c;
-        const int xg = (s_list[entry] * GPB + j) >> a.x_shift;
-        s_sx[i] = s_list[entry] >= 0 && c < tokens && token < a.n && xg < a.x_groups ? a.x_scale[static_cast<int64_t>(token) * a.x_groups + xg] : 0.0f;
+    float v[8], top = 0.0f;
+    if (in) {
+      load_eight(a.x, a.x_kind, token * a.x_stride + k, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+#pragma unroll
+    for (int o = 1; o < 16 / GPB; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    // the largest becomes 127 in the highest digit and 0 below; a group all below 2^-100 counts as 0 (its unit would leave
+    // the range of fp32)
+    const float most = a.c.pieces == 3 ? 8323072.0f : 32512.0f;
+    const bool some = top >= 7.8886091e-31f;
+    const float inv = some ? most / top : 0.0f;
+    float unit = some ? top / most : 0.0f;
+    int fixed[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) fixed[e] = __float2int_rn(v[e] * inv);
+    const int j = k8 / (16 / GPB);
+    if (GATEUP && a.x_scale != nullptr && in) {
+      const int xg = a.x_groups == 1 ? 0 : (block * GPB + j) >> a.x_shift;
+      unit *= a.x_scale[static_cast<int64_t>(token) * a.x_groups + xg];
+    }
+    const int word = unit_word<GPB>(k8);
+    uint2* out = s_x + (((entry * 2 + (word >> 1)) * (NT * 8) + tok) * 4 + unit_lane<GPB>(k8)) * 2 + (word & 1);
+    for (int p = 0; p < a.c.pieces; ++p) {
+      // the lowest digit, -128 .. 127, and what is left above it
+      uint32_t even = 0, odd = 0;
+      int sum = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int digit = static_cast<int8_t>(fixed[e]);
+        fixed[e] = (fixed[e] - digit) >> 8;
+        sum += digit;
+        const uint32_t byte = static_cast<uint32_t>(digit & 255) << (8 * (e / 2));
+        if (e & 1) odd |= byte;
+        else even |= byte;
       }
+#pragma unroll
+      for (int o = 1; o < 16 / GPB; o *= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+      out[p * tokens * 8] = make_uint2(even, odd);
+      if (k8 % (16 / GPB) == 0)
+        s_unit[(entry * GPB + j) * (NT * 8) + p * tokens + tok] = make_float2(unit, __int_as_float(-sum));
+      unit *= 256.0f;
     }
-  } else {
-    ptx::griddep_wait();                // h is complete
-    const uint4* h = a.h_in + static_cast<int64_t>(chunk) * a.kblocks * (cols * 16);
-    for (int i = threadIdx.x; i < even_entries * cols * 16; i += kThreads) {
-      const int entry = i / (cols * 16), u = i % (cols * 16), block = s_list[entry];
-      const int neuron = block * 128 + unit_k8<GPB>(u / (cols * 4), u & 3) * 8, token = chunk * tokens + (u >> 2) % cols % tokens;
-      bool in = block >= 0 && neuron < a.K && token < a.n;
-      if (in && !a.dense) {             // what the token does not compute is 0, and gate|up may have left it unwritten
-        const int b = branch_of(a, neuron);
-        in = s_active[b] != 0 && (a.select == nullptr || a.select[static_cast<int64_t>(token) * a.B + b] != 0);
-      }
-      cp_async16(ptx::smem_u32(s_x + i), h + (in ? static_cast<int64_t>(block) * (cols * 16) + u : 0), in);
-    }
-    cp_async_commit();
-    cp_async_wait<0>();
   }
   __syncthreads();
 
   // columns 8 nt + g: the lanes of a column that stands for no token keep zeros
   bool col_ok[NT];
-  uint4 xb[NT][4];
+  uint4 xb[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int c = nt * 8 + g;
     col_ok[nt] = c < cols && chunk * tokens + c % tokens < a.n;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) xb[nt][w] = make_uint4(0u, 0u, 0u, 0u);
+    for (int w = 0; w < 2; ++w) xb[nt][w] = make_uint4(0u, 0u, 0u, 0u);
   }
   float acc[NT][4];
 #pragma unroll
@@ -361,7 +373,6 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
 #pragma unroll
     for (int i = 0; i < 4; ++i) acc[nt][i] = 0.0f;
   float* sums = reinterpret_cast<float*>(smem + L.sums);
-  const bool scaled = GATEUP && a.x_groups > 1;
 
   int slot = 0, c_tile = steps > 0 ? run_begin / steps : 0, c_step = steps > 0 ? run_begin % steps : 0;
   for (int i = 0; i < count; ++i) {
@@ -373,19 +384,15 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
     for (int j = 0; j < 2 * GPB; ++j) {
       const int block = j / GPB;
       if (j % GPB == 0) {
-        const uint4* xp = s_x + (2 * c_step + block) * (cols * 16) + lane;
+        const uint4* xp = reinterpret_cast<const uint4*>(s_x) + (2 * c_step + block) * (NT * 64) + lane;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int w = 0; w < 4; ++w)
-            if (col_ok[nt]) xb[nt][w] = xp[w * cols * 4 + nt * 32];
+          for (int w = 0; w < 2; ++w)
+            if (col_ok[nt]) xb[nt][w] = xp[w * (NT * 32) + nt * 32];
       }
-      float part[NT][4];
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) part[nt][e] = 0.0f;
-      uint32_t q[2][kWords], bias[2];
+      uint32_t q[2][kWords];
+      int zero[2];
       float s[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -403,39 +410,39 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
         }
         const int piece = (block * 2 + h) * GPB + j % GPB;
         s[h] = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(st + 2048 + piece * 16 + g * 2));
-        const uint32_t z = a.m[h].zero != nullptr ? st[2048 + 4 * GPB * 16 + piece * 8 + g] : 8u;
-        bias[h] = 0x43004300u + z * 0x00010001u;
+        zero[h] = ZERO ? st[2048 + 4 * GPB * 16 + piece * 8 + g] : 8;
+      }
+      // - zero * sum of digits first, then the codes' products
+      const float4* up = reinterpret_cast<const float4*>(s_unit + ((2 * c_step) * GPB + j) * (NT * 8)) + t;
+      int part[NT][4];
+      float2 unit[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float4 u = up[nt * 4];
+        unit[nt] = make_float2(u.x, u.z);
+        part[nt][0] = zero[0] * __float_as_int(u.y);
+        part[nt][1] = zero[0] * __float_as_int(u.w);
+        part[nt][2] = ZERO ? zero[1] * __float_as_int(u.y) : part[nt][0];
+        part[nt][3] = ZERO ? zero[1] * __float_as_int(u.w) : part[nt][1];
       }
 #pragma unroll
       for (int w = 0; w < kWords; ++w) {
-        uint32_t lo[4], hi[4];
-        unpack(q[0][w], bias[0], lo);
-        unpack(q[1][w], bias[1], hi);
+        const int at = (j % GPB) * kWords + w;
+        const uint32_t a0 = q[0][w] & 0x0F0F0F0Fu, a1 = q[1][w] & 0x0F0F0F0Fu;
+        const uint32_t a2 = (q[0][w] >> 4) & 0x0F0F0F0Fu, a3 = (q[1][w] >> 4) & 0x0F0F0F0Fu;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          const uint4 b = xb[nt][(j % GPB) * kWords + w];
-          mma(part[nt], lo[0], hi[0], lo[1], hi[1], b.x, b.y);
-          mma(part[nt], lo[2], hi[2], lo[3], hi[3], b.z, b.w);
+          const uint4 b = xb[nt][at >> 1];
+          mma(part[nt], a0, a1, a2, a3, at & 1 ? b.z : b.x, at & 1 ? b.w : b.y);
         }
       }
-      if (scaled) {
-        const float* sx = s_sx + ((2 * c_step) * GPB + j) * (NT * 8) + 2 * t;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float2 f = *reinterpret_cast<const float2*>(sx + nt * 8);
-          acc[nt][0] += part[nt][0] * (s[0] * f.x);
-          acc[nt][1] += part[nt][1] * (s[0] * f.y);
-          acc[nt][2] += part[nt][2] * (s[1] * f.x);
-          acc[nt][3] += part[nt][3] * (s[1] * f.y);
-        }
-      } else {
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          acc[nt][0] += part[nt][0] * s[0];
-          acc[nt][1] += part[nt][1] * s[0];
-          acc[nt][2] += part[nt][2] * s[1];
-          acc[nt][3] += part[nt][3] * s[1];
-        }
+      for (int nt = 0; nt < NT; ++nt) {
+        // at most 15 * 128 * 256 in magnitude: exact in fp32
+        acc[nt][0] += __int2float_rn(part[nt][0]) * (s[0] * unit[nt].x);
+        acc[nt][1] += __int2float_rn(part[nt][1]) * (s[0] * unit[nt].y);
+        acc[nt][2] += __int2float_rn(part[nt][2]) * (s[1] * unit[nt].x);
+        acc[nt][3] += __int2float_rn(part[nt][3]) * (s[1] * unit[nt].y);
       }
     }
     slot = slot + 1 == kStages ? 0 : slot + 1;
@@ -489,22 +496,10 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
       const bool on = a.dense || (s_active[b] != 0 && (a.select == nullptr || a.select[static_cast<int64_t>(token) * a.B + b] != 0));
       float h = 0.0f;
       if (on) {
-        float gate = total_of(tile, tok, e), up = total_of(tile, tok, 8 + e);
-        if (a.x_scale != nullptr && a.x_groups == 1) {
-          gate *= a.x_scale[token];
-          up *= a.x_scale[token];
-        }
+        const float gate = total_of(tile, tok, e), up = total_of(tile, tok, 8 + e);
         h = gate / (1.0f + expf(-gate)) * up * a.alpha[b];
       }
-      // h as bf16 pieces: two keep 2^-16 of it (y is rounded to 2^-8), three all 24 bits
-      const int hc = a.hc.cols(), k8 = (neuron % 128) / 8, h_tok = token % a.hc.tokens;
-      const int64_t block = static_cast<int64_t>(token / a.hc.tokens) * a.h_kblocks + neuron / 128;
-      __nv_bfloat16* out = a.h + ((block * 4 + unit_word<GPB>(k8)) * hc * 4 + unit_lane<GPB>(k8)) * 8 + unit_pos(e);
-      for (int p = 0; p < a.hc.pieces; ++p) {
-        const __nv_bfloat16 piece = __float2bfloat16_rn(h);
-        h -= __bfloat162float(piece);
-        out[(p * a.hc.tokens + h_tok) * 32] = piece;
-      }
+      a.h[static_cast<int64_t>(token) * a.rows + neuron] = h;
     }
   } else {
     for (int i = rank * kThreads + threadIdx.x; i < n_tiles * tokens * 16; i += cluster * kThreads) {
@@ -536,9 +531,9 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   }
 }
 
-template <int NT, int GPB, bool GATEUP>
+template <int NT, int GPB, bool GATEUP, bool ZERO>
 cudaError_t launch(const W4Args& a, int cluster, cudaStream_t st) {
-  auto kernel = w4_kernel<NT, GPB, GATEUP>;
+  auto kernel = w4_kernel<NT, GPB, GATEUP, ZERO>;
   const int smem = smem_of<NT, GPB>(a).total;
   if (smem > kSmemMax) return cudaErrorInvalidValue;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -561,14 +556,20 @@ cudaError_t launch(const W4Args& a, int cluster, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-template <int GPB, bool GATEUP>
+template <int GPB, bool GATEUP, bool ZERO>
 cudaError_t launch_nt(const W4Args& a, int cluster, cudaStream_t st) {
   switch ((a.c.cols() + 7) / 8) {
-    case 1: return launch<1, GPB, GATEUP>(a, cluster, st);
-    case 2: return launch<2, GPB, GATEUP>(a, cluster, st);
-    case 3: return launch<3, GPB, GATEUP>(a, cluster, st);
+    case 1: return launch<1, GPB, GATEUP, ZERO>(a, cluster, st);
+    case 2: return launch<2, GPB, GATEUP, ZERO>(a, cluster, st);
+    case 3: return launch<3, GPB, GATEUP, ZERO>(a, cluster, st);
     default: return cudaErrorInvalidValue;
   }
+}
+
+template <int GPB, bool GATEUP>
+cudaError_t launch_zero(const W4Args& a, int cluster, cudaStream_t st) {
+  return a.m[0].zero != nullptr || a.m[1].zero != nullptr ? launch_nt<GPB, GATEUP, true>(a, cluster, st)
+                                                          : launch_nt<GPB, GATEUP, false>(a, cluster, st);
 }
 
 }  // namespace w4

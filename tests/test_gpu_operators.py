@@ -299,21 +299,30 @@ class W4Case:
         y.check()
         return y.t
 
+    def tolerance(self, r, xh, yt):
+        """Inside a group of K the activations are whole multiples of unit = max / 8323072 (y fp32) or max / 32512 (y bf16): off
+        by half a unit, and by two roundings of x / unit (each u of at most max / unit, so 1 unit more for the finer one):
+        1.5 / 8323072 or 0.51 / 32512 of the group's largest.  The products are exact.  Sums in fp32: one term per group
+        and digit, up to 16 + 8 parts to join, and six roundings of a term (scale times unit, the product, unit's own, a factor
+        for e4m3's scale); the digits of x add up to at most 3 |x| in magnitude."""
+        q = 1.5 / 8323072 if yt == "fp32" else 0.51 / 32512
+        starts = np.arange(0, self.d, self.group)
+        top = np.maximum.reduceat(np.abs(xh), starts, axis=1)
+
+        def product(K, size, tops, W, starts):
+            return 3 * U * (K / self.group + 30) * size + q * (tops @ np.add.reduceat(np.abs(W), starts, axis=1).T)
+        e_gate, e_up = product(self.d, r["abs_gate"], top, self.W[0], starts), product(self.d, r["abs_up"], top, self.W[1], starts)
+        # |silu'| <= 1.1; expf, the quotient and the two products cost 2^-20 of h (and |g| u from the exponent)
+        h_err = np.abs(r["alpha"]) * (1.1 * e_gate * (np.abs(r["up"]) + e_up) + np.abs(oracle.silu(r["gate"])) * e_up)
+        h_err = np.where(r["on"], h_err, 0.0) + (2.0 ** -20 + np.abs(r["gate"]) * 2 * U) * np.abs(r["h"])
+        starts = np.arange(0, self.I, self.group)
+        tops = np.maximum.reduceat(np.abs(r["h"]) + h_err, starts, axis=1)
+        size = np.abs(r["h"]) @ np.abs(self.W[2]).T
+        return r["coef"][:, None] * (h_err @ np.abs(self.W[2]).T + product(self.I, size, tops, self.W[2], starts)) + 4 * U * np.abs(r["y"])
+
     def check(self, y, xh, xt, yt, select=None, compensate=True, residual=None):
         r = oracle.w4_layer_forward(xh, *self.W, self.d_b, self.alpha, select, compensate, residual)
-        # A sum of K products: inside a group the tensor core adds 16 exact products at a time, an addition good to 2^-22 of
-        # the magnitudes it joins; a group is up to 8 such steps, then one product with the scale and one addition per
-        # group, at most 8 + 8 further partial sums.  fp32 activations are three pieces (2^-24 of the value is dropped),
-        # e4m3 ones carry a scale product.
-        def length(K):
-            return 9 + K / self.group + 24
-        e_gate, e_up = (length(self.d) * 2.0 ** -22 + 2 * U) * r["abs_gate"], (length(self.d) * 2.0 ** -22 + 2 * U) * r["abs_up"]
-        # |silu'| <= 1.1; expf, the quotient and the two products cost 2^-20 of h (and |g| u from the exponent)
-        sig = np.abs(r["gate"] * 0 + 1.0)
-        h_err = np.abs(r["alpha"]) * (1.1 * e_gate * (np.abs(r["up"]) + e_up) + np.abs(oracle.silu(r["gate"])) * e_up) * sig
-        h_err = np.where(r["on"], h_err, 0.0) + (2.0 ** -20 + np.abs(r["gate"]) * 2 * U) * np.abs(r["h"])
-        h_err += np.abs(r["h"]) * (2.0 ** -16 if yt == "bf16" else 2.0 ** -24)             # what the bf16 pieces leave
-        tol = r["coef"][:, None] * ((h_err + length(self.I) * 2.0 ** -22 * np.abs(r["h"])) @ np.abs(self.W[2]).T) + 4 * U * np.abs(r["y"])
+        tol = self.tolerance(r, xh, yt)
         if residual is not None:
             tol = tol + 2 * U * np.abs(np.asarray(residual, dtype=np.float64))
         if yt == "bf16":
@@ -427,10 +436,15 @@ def test_w4_forward_full_size(lib, d, I, n):
     xd = x.double()
     g, u = xd @ deq[0].t(), xd @ deq[1].t()
     h = torch.nn.functional.silu(g) * u
-    ag, au = xd.abs() @ deq[0].abs().t(), xd.abs() @ deq[1].abs().t()
-    eg, eu = (9 + d / group + 24) * 2.0 ** -22 * ag, (9 + d / group + 24) * 2.0 ** -22 * au
+    # as W4Case.tolerance, on the device
+    q = 1.5 / 8323072
+
+    def product(K, size, v, W):
+        tops = v.abs().view(n, -1, group).amax(2)
+        return 3 * U * (K / group + 30) * size + q * (tops @ W.abs().view(W.shape[0], -1, group).sum(2).t())
+    eg, eu = (product(d, xd.abs() @ w.abs().t(), xd, w) for w in deq[:2])
     h_err = 1.1 * eg * (u.abs() + eu) + torch.nn.functional.silu(g).abs() * eu + (2.0 ** -20 + g.abs() * 2 * U) * h.abs()
-    tol = (h_err + ((9 + I / group + 24) * 2.0 ** -22 + U) * h.abs()) @ deq[2].abs().t() + 1e-30
+    tol = h_err @ deq[2].abs().t() + product(I, h.abs() @ deq[2].abs().t(), h.abs() + h_err, deq[2]) + 4 * U * (h @ deq[2].t()).abs() + 1e-30
     assert bool(((y.double() - h @ deq[2].t()).abs() <= tol).all())
 
 
