@@ -34,7 +34,7 @@ int w4_plan(W4Args* a, int pieces, int group) {
         const int64_t x = static_cast<int64_t>(entries) * nt * 1024, units = static_cast<int64_t>(entries) * gpb * nt * 64;
         const int64_t sums = static_cast<int64_t>(w4::kWarps - 1 + per) * nt * 8 * w4::kColPitch * 4;
         const int64_t own = static_cast<int64_t>(per) * tokens * 64;
-        if (ring + x + units + sums + entries * 4 + per * 4 > w4::kSmemMax || own > ring + x) continue;
+        if (ring + x + units + sums + entries * 4 + per * 12 + (a->dense ? 0 : 8 * (a->B + 1) + tokens * a->B) > w4::kSmemMax || own > ring + x) continue;
         const int chunks = (a->n + tokens - 1) / tokens;
         const int even = (a->n + chunks - 1) / chunks;
         const int64_t blocks = static_cast<int64_t>((a->tiles + per - 1) / per) * chunks;
@@ -147,11 +147,6 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
     u.x_groups = x_group == 0 ? 1 : static_cast<int>((d + x_group - 1) / x_group);
     for (int64_t g = group; x_group != 0 && g < x_group; g *= 2) ++u.x_shift;
   }
-  const int u_cluster = w4_plan(&u, digits, group);
-  u.x = x;
-  u.x_kind = x_dtype;
-  u.x_stride = x_stride;
-  u.h = static_cast<float*>(workspace);
   u.B = layer->B;
   u.select = select;
   u.dense = select == nullptr;
@@ -160,6 +155,11 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
     u.alpha[b] = layer->alpha ? layer->alpha[b] : 1.0f;
     if (u.alpha[b] == 0.0f) u.dense = 0;
   }
+  const int u_cluster = w4_plan(&u, digits, group);
+  u.x = x;
+  u.x_kind = x_dtype;
+  u.x_stride = x_stride;
+  u.h = static_cast<float*>(workspace);
 
   W4Args w = {};
   w.m[0] = w.m[1] = matrix(layer->down, d, I, group);
@@ -168,14 +168,14 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
   w.K = static_cast<int>(I);
   w.kblocks = static_cast<int>((I + 127) / 128);
   w.n = n;
+  w.B = u.B;
+  w.dense = u.dense;
   const int w_cluster = w4_plan(&w, digits, group);
   if (u_cluster == 0 || w_cluster == 0) return MLPMOE_ERR_UNSUPPORTED;
   w.x = workspace;
   w.x_kind = MLPMOE_FP32;
   w.x_stride = I;
-  w.B = u.B;
   w.select = select;
-  w.dense = u.dense;
   memcpy(w.off, u.off, sizeof(u.off));
   memcpy(w.alpha, u.alpha, sizeof(u.alpha));
   w.compensate = compensate ? 1 : 0;

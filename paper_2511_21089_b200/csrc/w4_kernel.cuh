@@ -66,7 +66,7 @@ __host__ __device__ constexpr int stages() {
 
 // Dynamic shared memory, in bytes from its start.
 struct Smem {
-  int x, unit, sums, list, tiles, total;
+  int x, unit, sums, list, tiles, branch, total;
 };
 template <int NT, int GPB>
 __host__ __device__ inline Smem smem_of(const W4Args& a) {
@@ -75,16 +75,17 @@ __host__ __device__ inline Smem smem_of(const W4Args& a) {
   s.unit = s.x + a.entries * NT * 8 * 128;                                // their (unit, - sum of digits): [entry][GPB][8 NT]
   s.sums = s.unit + a.entries * GPB * NT * 8 * 8;                         // parts of the sums: [warp + tile][column][16 rows]
   s.list = s.sums + (kWarps - 1 + a.tiles_per_block) * NT * 8 * kColPitch * 4;
-  s.tiles = s.list + a.entries * 4;                                       // the block's K-blocks, then its tiles
-  s.total = s.tiles + a.tiles_per_block * 4;
+  s.tiles = s.list + a.entries * 4;                                       // the block's K-blocks; its tiles: place, first and last warp
+  s.branch = s.tiles + a.tiles_per_block * 12;                            // first neurons, running counts, then [tokens][B] computed or not
+  s.total = s.branch + (a.dense ? 0 : (2 * (a.B + 1) * 4 + a.c.tokens * a.B));
   return s;
 }
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool ok) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src, bool ok) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(ok ? 8 : 0) : "memory");
+__device__ __forceinline__ void cp_async8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -104,32 +105,49 @@ __device__ __forceinline__ float ld_cluster_f32(const float* p, uint32_t rank) {
   return v;
 }
 
-__device__ __forceinline__ int branch_of(const W4Args& a, int neuron) {
-  int lo = 0, hi = a.B;                 // off[lo] <= neuron < off[hi]
+// The last b with first[b] <= value, first ascending.
+__device__ __forceinline__ int find_branch(const int* first, int B, int value) {
+  int lo = 0, hi = B;
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
-    if (a.off[mid] <= neuron) lo = mid;
+    if (first[mid] <= value) lo = mid;
     else hi = mid;
   }
   return lo;
 }
 
-// Eight consecutive activations of one token, from element `at` of x (gate|up) or h (down, fp32).
-__device__ __forceinline__ void load_eight(const void* x, int kind, int64_t at, float (&v)[8]) {
+// Eight consecutive activations of one token from element `at`, as they stand in memory, and as fp32.
+struct Raw {
+  uint4 lo, hi;
+};
+__device__ __forceinline__ Raw load_raw(const void* x, int kind, int64_t at) {
+  Raw r;
+  r.lo = r.hi = make_uint4(0u, 0u, 0u, 0u);
   if (kind == MLPMOE_FP32) {
-    const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(x) + at);
-    const float4 lo = p[0], hi = p[1];
-    v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(x) + at);
+    r.lo = p[0];
+    r.hi = p[1];
   } else if (kind == MLPMOE_BF16) {
-    const uint4 w = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(x) + at);
-    v[0] = __uint_as_float(w.x << 16), v[1] = __uint_as_float(w.x & 0xFFFF0000u), v[2] = __uint_as_float(w.y << 16),
-    v[3] = __uint_as_float(w.y & 0xFFFF0000u), v[4] = __uint_as_float(w.z << 16), v[5] = __uint_as_float(w.z & 0xFFFF0000u),
-    v[6] = __uint_as_float(w.w << 16), v[7] = __uint_as_float(w.w & 0xFFFF0000u);
+    r.lo = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(x) + at);
   } else {
     const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(x) + at);
+    r.lo.x = w.x;
+    r.lo.y = w.y;
+  }
+  return r;
+}
+__device__ __forceinline__ void to_f32(const Raw& r, int kind, float (&v)[8]) {
+  if (kind == MLPMOE_FP32) {
+    v[0] = __uint_as_float(r.lo.x), v[1] = __uint_as_float(r.lo.y), v[2] = __uint_as_float(r.lo.z), v[3] = __uint_as_float(r.lo.w);
+    v[4] = __uint_as_float(r.hi.x), v[5] = __uint_as_float(r.hi.y), v[6] = __uint_as_float(r.hi.z), v[7] = __uint_as_float(r.hi.w);
+  } else if (kind == MLPMOE_BF16) {
+    v[0] = __uint_as_float(r.lo.x << 16), v[1] = __uint_as_float(r.lo.x & 0xFFFF0000u), v[2] = __uint_as_float(r.lo.y << 16),
+    v[3] = __uint_as_float(r.lo.y & 0xFFFF0000u), v[4] = __uint_as_float(r.lo.z << 16), v[5] = __uint_as_float(r.lo.z & 0xFFFF0000u),
+    v[6] = __uint_as_float(r.lo.w << 16), v[7] = __uint_as_float(r.lo.w & 0xFFFF0000u);
+  } else {
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
-      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>((e < 4 ? w.x : w.y) >> (8 * (e & 3))), __NV_E4M3);
+      const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>((e < 4 ? r.lo.x : r.lo.y) >> (8 * (e & 3))), __NV_E4M3);
       const float2 f = __half22float2(__half2(h));
       v[e] = f.x, v[e + 1] = f.y;
     }
@@ -140,222 +158,243 @@ __device__ __forceinline__ void load_eight(const void* x, int kind, int64_t at, 
 template <int NT, int GPB, bool GATEUP, bool ZERO>
 __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__ W4Args a) {
   constexpr int kStages = stages<NT>(), kStage = stage_bytes<GPB>(), kWords = 4 / GPB;
+  constexpr int kLanes = 16 / GPB;      // threads that hold one group of a token's activations, eight each
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ uint8_t s_active[kW4MaxBranches];
   __shared__ int s_scan[kWarps];
-  __shared__ int s_n[2];                // K-blocks and tiles of this block
-  // gate|up waits for everything before it on the stream; by the time all its blocks have passed here only gate|up
-  // itself is outstanding, so the down kernel, which then may start, reads weights and selection without a wait.
-  if (GATEUP) ptx::griddep_wait();
-  ptx::griddep_launch_dependents();
+  __shared__ float s_coef[24];
   const Smem L = smem_of<NT, GPB>(a);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
   const int chunk = blockIdx.z, rank = blockIdx.y, cluster = gridDim.y;
   const int tokens = a.c.tokens, cols = a.c.cols();
   int* s_list = reinterpret_cast<int*>(smem + L.list);
   int* s_tiles = reinterpret_cast<int*>(smem + L.tiles);
+  int* s_first = s_tiles + a.tiles_per_block;      // first and last warp with a part of the tile
+  int* s_last = s_first + a.tiles_per_block;
+  int* s_off = reinterpret_cast<int*>(smem + L.branch);
+  int* s_run = s_off + a.B + 1;
+  uint8_t* s_on = reinterpret_cast<uint8_t*>(s_run + a.B + 1);
+  // gate|up waits for everything before it on the stream; by the time all its blocks have passed here only gate|up
+  // itself is outstanding, so the down kernel, which then may start, reads weights and selection without a wait.
+  if (GATEUP) {
+    ptx::griddep_wait();
+  }
+  ptx::griddep_launch_dependents();
 
   // ---- this block's K-blocks and tiles
-  int n_entries, n_tiles;
-  if (a.dense) {
-    const int per = (a.kblocks + cluster - 1) / cluster;
-    n_entries = max(0, min(per, a.kblocks - rank * per));
-    n_tiles = min(a.tiles_per_block, a.tiles - static_cast<int>(blockIdx.x) * a.tiles_per_block);
-    for (int i = threadIdx.x; i < a.entries; i += kThreads) s_list[i] = i < n_entries ? rank * per + i : -1;
-    for (int i = threadIdx.x; i < n_tiles; i += kThreads) s_tiles[i] = blockIdx.x * a.tiles_per_block + i;
-    __syncthreads();
-  } else {
-    // the branches that a token of this chunk computes
-    const int n_here = min(tokens, a.n - chunk * tokens);
-    for (int b = threadIdx.x; b < a.B; b += kThreads) s_active[b] = a.select == nullptr && a.alpha[b] != 0.0f;
-    __syncthreads();
-    if (a.select != nullptr) {
-      const uint8_t* sel = a.select + static_cast<int64_t>(chunk) * tokens * a.B;
-      for (int i = threadIdx.x; i < n_here * a.B; i += kThreads)
-        if (sel[i] != 0 && a.alpha[i % a.B] != 0.0f) s_active[i % a.B] = 1;
+  const int k_share = (a.kblocks + cluster - 1) / cluster;
+  int n_entries = max(0, min(k_share, a.kblocks - rank * k_share));
+  int n_tiles = min(a.tiles_per_block, a.tiles - static_cast<int>(blockIdx.x) * a.tiles_per_block);
+  if (!a.dense) {
+    // what the chunk's tokens compute: [token][branch], and the branches of all of them
+    for (int b = threadIdx.x; b <= a.B; b += kThreads) s_off[b] = a.off[b];
+    for (int i = threadIdx.x; i < tokens * a.B; i += kThreads) {
+      const int token = chunk * tokens + i / a.B;
+      s_on[i] = token < a.n && a.alpha[i % a.B] != 0.0f && (a.select == nullptr || a.select[static_cast<int64_t>(token) * a.B + i % a.B] != 0);
     }
     __syncthreads();
-    // gate|up: the computed tiles in order, an equal share to every block; down: the K-blocks with a computed neuron
-    const int total = GATEUP ? a.tiles : a.kblocks;
-    int live_total = 0, share = 0, first = 0;
-    for (int pass = 0; pass < 2; ++pass) {              // count, then list this block's share
-      int running = 0;
-      for (int base = 0; base < total; base += kThreads) {
-        const int i = base + threadIdx.x;
-        bool live = false;
-        if (i < total) {
-          if (GATEUP) {
-            live = s_active[branch_of(a, i * 8)] != 0;
-          } else {
-            for (int b = branch_of(a, i * 128); b < a.B && a.off[b] < (i + 1) * 128; ++b) live = live || s_active[b] != 0;
-          }
+    if (!GATEUP && a.select != nullptr) {
+      // c_t: the quotient and the root in double, rounded once, as the routed forward does
+      for (int tok = warp; tok < tokens; tok += kWarps) {
+        int k = 0, n_avail = 0;
+        for (int b = lane; b < a.B; b += 32) {
+          k += s_on[tok * a.B + b];
+          n_avail += a.alpha[b] != 0.0f ? 1 : 0;
         }
-        const unsigned ballot = __ballot_sync(0xFFFFFFFFu, live);
-        if (lane == 0) s_scan[warp] = __popc(ballot);
-        __syncthreads();
-        int before = running, all = running;
-        for (int w = 0; w < kWarps; ++w) {
-          if (w < warp) before += s_scan[w];
-          all += s_scan[w];
-        }
-        if (pass == 1 && live) {
-          const int at = before + __popc(ballot & ((1u << lane) - 1u)) - first;
-          if (at >= 0 && at < share) (GATEUP ? s_tiles : s_list)[at] = i;
-        }
-        running = all;
-        __syncthreads();
-      }
-      if (pass == 0) {
-        live_total = running;
-        const int shares = GATEUP ? static_cast<int>(gridDim.x) : cluster, mine = GATEUP ? static_cast<int>(blockIdx.x) : rank;
-        const int per = (live_total + shares - 1) / shares;
-        first = mine * per;
-        share = max(0, min(per, live_total - first));
+        k = __reduce_add_sync(0xFFFFFFFFu, k);
+        n_avail = __reduce_add_sync(0xFFFFFFFFu, n_avail);
+        if (lane == 0) s_coef[tok] = k == 0 ? 0.0f : (a.compensate ? static_cast<float>(sqrt(static_cast<double>(n_avail) / static_cast<double>(k))) : 1.0f);
       }
     }
+    // running count of what is live: gate|up counts tiles branch by branch, down K-blocks with a live neuron
+    int live = 0;
     if (GATEUP) {
-      const int per = (a.kblocks + cluster - 1) / cluster;
-      n_entries = max(0, min(per, a.kblocks - rank * per));
-      n_tiles = share;
-      for (int i = threadIdx.x; i < a.entries; i += kThreads) s_list[i] = i < n_entries ? rank * per + i : -1;
-    } else {
-      n_entries = share;
-      n_tiles = min(a.tiles_per_block, a.tiles - static_cast<int>(blockIdx.x) * a.tiles_per_block);
-      for (int i = threadIdx.x; i < n_tiles; i += kThreads) s_tiles[i] = blockIdx.x * a.tiles_per_block + i;
-      for (int i = share + threadIdx.x; i < a.entries; i += kThreads) s_list[i] = -1;
+      if (threadIdx.x < a.B) {
+        for (int tok = 0; tok < tokens; ++tok) live |= s_on[tok * a.B + threadIdx.x];
+        live *= (s_off[threadIdx.x + 1] - s_off[threadIdx.x]) / 8;
+      }
+    } else if (threadIdx.x < a.kblocks) {
+      for (int b = find_branch(s_off, a.B, threadIdx.x * 128); b < a.B && s_off[b] < (static_cast<int>(threadIdx.x) + 1) * 128; ++b)
+        for (int tok = 0; tok < tokens; ++tok) live |= s_on[tok * a.B + b];
+    }
+    int sum = live;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xFFFFFFFFu, sum, o);
+      if (lane >= o) sum += u;
+    }
+    if (lane == 31) s_scan[warp] = sum;
+    __syncthreads();
+    int total = 0;
+    for (int w = 0; w < kWarps; ++w) {
+      if (w < warp) sum += s_scan[w];
+      total += s_scan[w];
+    }
+    const int shares = GATEUP ? static_cast<int>(gridDim.x) : cluster, mine = GATEUP ? static_cast<int>(blockIdx.x) : rank;
+    const int share = (total + shares - 1) / shares, first = mine * share;
+    (GATEUP ? n_tiles : n_entries) = max(0, min(share, total - first));
+    if (GATEUP) {
+      if (threadIdx.x < a.B) s_run[threadIdx.x] = sum - live;      // live tiles before the branch
+    } else if (live && sum - 1 >= first && sum - 1 < first + n_entries) {
+      s_list[sum - 1 - first] = threadIdx.x;
     }
     __syncthreads();
+    if (GATEUP) {
+      for (int i = threadIdx.x; i < n_tiles; i += kThreads) {
+        // the last branch with at most `first + i` live tiles before it: a branch without any shares its count with the next
+        const int b = find_branch(s_run, a.B, first + i);
+        s_tiles[i] = s_off[b] / 8 + first + i - s_run[b];
+      }
+    } else if (threadIdx.x < a.entries && static_cast<int>(threadIdx.x) >= n_entries && n_entries > 0) {
+      s_list[threadIdx.x] = s_list[n_entries - 1];
+    }
   }
+  if (GATEUP || a.dense)
+    for (int i = threadIdx.x; i < a.entries; i += kThreads) s_list[i] = rank * k_share + max(0, min(i, n_entries - 1));
+  if (!GATEUP || a.dense)
+    for (int i = threadIdx.x; i < n_tiles; i += kThreads) s_tiles[i] = blockIdx.x * a.tiles_per_block + i;
+  __syncthreads();
 
   // ---- this warp's run of steps (tile, two K-blocks)
   const int steps = (n_entries + 1) / 2;
   const int per_warp = (n_tiles * steps + kWarps - 1) / kWarps;
-  const int run_begin = min(n_tiles * steps, warp * per_warp), run_end = min(n_tiles * steps, run_begin + per_warp);
-  const int count = run_end - run_begin;
+  const int run_begin = min(n_tiles * steps, warp * per_warp);
+  const int count = min(n_tiles * steps, run_begin + per_warp) - run_begin;
+  const int tile_begin = steps > 0 ? run_begin / steps : 0, step_begin = run_begin - tile_begin * steps;
 
   // ---- copies of one stage: 16 bytes of codes per lane, K-block and half; scales and zeros by the first lanes
   const uint32_t ring = ptx::smem_u32(smem) + warp * kStages * kStage;
   const uint32_t q_dst = ring + g * 64 + (t ^ ((g >> 1) & 3)) * 16;
   const int s_block = (lane / (2 * GPB)) & 1, s_half = (lane / GPB) & 1, s_group = lane % GPB;   // lanes below 4 GPB
-  const W4Mat& sm = a.m[s_half];
-  const bool s_lane = lane < 4 * GPB, z_lane = ZERO && s_lane && sm.zero != nullptr;
+  const bool s_lane = lane < 4 * GPB;
+  const uint8_t* const z_base = ZERO && s_lane ? (s_half ? a.m[1].zero : a.m[0].zero) : nullptr;
+  const __nv_bfloat16* const s_base = s_half ? a.m[1].scale : a.m[0].scale;
+  const uint32_t last_byte = static_cast<uint32_t>(a.m[0].pitch) - 16, last_group = static_cast<uint32_t>(a.m[0].n_groups) - 1;
+  const uint32_t rows16 = static_cast<uint32_t>(a.m[0].rows16);
+  // Rows past the last, K-blocks past the last and columns past K are read from the nearest valid place: their results
+  // are not used, or their digits and units are 0.
   const uint8_t* q_src[2];
-  bool q_ok[2], s_ok = false;
-  int s_row = 0;
-  int i_tile = steps > 0 ? run_begin / steps : 0, i_step = steps > 0 ? run_begin % steps : 0, i_left = count;
-  auto open_tile = [&]() {
-    const int tile = s_tiles[i_tile];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int row = (GATEUP ? tile * 8 : tile * 16 + 8 * h) + g;
-      q_ok[h] = row < a.rows;
-      q_src[h] = a.m[h].q + (q_ok[h] ? row * a.m[h].pitch : 0);
-    }
-    s_row = GATEUP ? tile * 8 : tile * 16 + 8 * s_half;
-    s_ok = s_row < a.rows;
-  };
-  if (i_left > 0) open_tile();
-  if (ZERO && s_lane && sm.zero == nullptr) {        // a half without stored zeros beside one with them: 8 in every slot, for good
+  uint32_t s_row = 0;
+  int i_tile = tile_begin, i_step = step_begin, i_left = count;
+  if (ZERO && s_lane && z_base == nullptr) {         // a half without stored zeros beside one with them: 8 in every slot, for good
     for (int i = 0; i < kStages; ++i)
       *reinterpret_cast<uint2*>(smem + (warp * kStages + i) * kStage + 2048 + 4 * GPB * 16 + lane * 8) = make_uint2(0x08080808u, 0x08080808u);
   }
+  bool open = true;
   auto issue = [&](int slot) {
     if (i_left > 0) {
-      const int2 kb = *reinterpret_cast<const int2*>(s_list + 2 * i_step);
+      if (open) {                       // the first step of a tile
+        const int tile = s_tiles[i_tile];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int row = GATEUP ? tile * 8 + g : min(tile * 16 + 8 * h + g, a.rows - 1);
+          q_src[h] = a.m[h].q + row * a.m[h].pitch;
+        }
+        s_row = static_cast<uint32_t>(GATEUP ? tile * 8 : min(tile * 16 + 8 * s_half, a.rows - 8));
+      }
+      const uint2 kb = *reinterpret_cast<const uint2*>(s_list + 2 * i_step);
       const uint32_t dst = q_dst + slot * kStage;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const int block = j == 0 ? kb.x : kb.y;
-        const int byte = block * 64 + t * 16;
-        const bool in = block >= 0 && byte < a.m[0].pitch;
+        const uint32_t byte = min((j == 0 ? kb.x : kb.y) * 64 + t * 16, last_byte);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) cp_async16(dst + (j * 2 + h) * 512, q_src[h] + (in ? byte : 0), in && q_ok[h]);
+        for (int h = 0; h < 2; ++h) cp_async16(dst + (j * 2 + h) * 512, q_src[h] + byte);
       }
       if (s_lane) {
-        const int block = s_block == 0 ? kb.x : kb.y;
-        const int group = block * GPB + s_group;
-        const bool in = s_ok && block >= 0 && group < sm.n_groups;
-        const int64_t at = in ? group * sm.rows16 + s_row : 0;
-        cp_async16(ring + slot * kStage + 2048 + lane * 16, sm.scale + at, in);
-        if (z_lane) cp_async8(ring + slot * kStage + 2048 + 4 * GPB * 16 + lane * 8, sm.zero + at, in);
+        const uint32_t at = min((s_block == 0 ? kb.x : kb.y) * GPB + s_group, last_group) * rows16 + s_row;
+        cp_async16(ring + slot * kStage + 2048 + lane * 16, s_base + at);
+        if (ZERO && z_base != nullptr) cp_async8(ring + slot * kStage + 2048 + 4 * GPB * 16 + lane * 8, z_base + at);
       }
       --i_left;
-      if (++i_step == steps && i_left > 0) {
+      open = ++i_step == steps;
+      if (open) {
         i_step = 0;
         ++i_tile;
-        open_tile();
       }
     }
     cp_async_commit();
   };
-#pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) issue(i);
 
-  // ---- the activations of this block's K-blocks as digits: a thread takes eight k of one token, the group's 4, 8 or 16
-  // threads are neighbours
+  // ---- the activations of this block's K-blocks as digits: a thread takes eight k of one token, the group's kLanes
+  // threads are neighbours; four such loads are under way at a time
   uint2* s_x = reinterpret_cast<uint2*>(smem + L.x);
   float2* s_unit = reinterpret_cast<float2*>(smem + L.unit);
-  const int even_entries = 2 * steps;
-  if (!GATEUP) ptx::griddep_wait();     // h is complete
-  for (int i = threadIdx.x; i < even_entries * GPB * NT * 8; i += kThreads)
-    if (i % (NT * 8) >= cols) s_unit[i] = make_float2(0.0f, 0.0f);
-  for (int i = threadIdx.x; i < even_entries * 16 * tokens; i += kThreads) {      // a multiple of 32 threads take part
-    const int k8 = i & 15, entry = (i >> 4) % even_entries, tok = (i >> 4) / even_entries;
-    const int block = s_list[entry], token = chunk * tokens + tok, k = block * 128 + k8 * 8;
-    bool in = block >= 0 && k < a.K && token < a.n;
-    if (!GATEUP && in && !a.dense) {    // what the token does not compute is 0, and gate|up may have left it unwritten
-      const int b = branch_of(a, k);
-      in = s_active[b] != 0 && (a.select == nullptr || a.select[static_cast<int64_t>(token) * a.B + b] != 0);
-    }
-    float v[8], top = 0.0f;
-    if (in) {
-      load_eight(a.x, a.x_kind, token * a.x_stride + k, v);
-    } else {
+  const int even_entries = 2 * steps, units_per_token = even_entries * 16;
+  const int kind = GATEUP ? a.x_kind : MLPMOE_FP32;
+  auto stage_activations = [&]() {
+    constexpr int kBatch = 4;
+    for (int i = threadIdx.x; i < even_entries * GPB * NT * 8; i += kThreads)
+      if (i % (NT * 8) >= cols) s_unit[i] = make_float2(0.0f, 0.0f);
+    if (!GATEUP) ptx::griddep_wait();   // h is complete
+    // unit i of token tok; units_per_token is a multiple of 32, so a warp stays inside a token and is whole
+    int tok = 0, i = threadIdx.x;
+    while (tok < tokens) {
+      Raw raw[kBatch];
+      int toks[kBatch], is[kBatch];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
-#pragma unroll
-    for (int o = 1; o < 16 / GPB; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    // the largest becomes 127 in the highest digit and 0 below; a group all below 2^-100 counts as 0 (its unit would leave
-    // the range of fp32)
-    const float most = a.c.pieces == 3 ? 8323072.0f : 32512.0f;
-    const bool some = top >= 7.8886091e-31f;
-    const float inv = some ? most / top : 0.0f;
-    float unit = some ? top / most : 0.0f;
-    int fixed[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) fixed[e] = __float2int_rn(v[e] * inv);
-    const int j = k8 / (16 / GPB);
-    if (GATEUP && a.x_scale != nullptr && in) {
-      const int xg = a.x_groups == 1 ? 0 : (block * GPB + j) >> a.x_shift;
-      unit *= a.x_scale[static_cast<int64_t>(token) * a.x_groups + xg];
-    }
-    const int word = unit_word<GPB>(k8);
-    uint2* out = s_x + (((entry * 2 + (word >> 1)) * (NT * 8) + tok) * 4 + unit_lane<GPB>(k8)) * 2 + (word & 1);
-    for (int p = 0; p < a.c.pieces; ++p) {
-      // the lowest digit, -128 .. 127, and what is left above it
-      uint32_t even = 0, odd = 0;
-      int sum = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int digit = static_cast<int8_t>(fixed[e]);
-        fixed[e] = (fixed[e] - digit) >> 8;
-        sum += digit;
-        const uint32_t byte = static_cast<uint32_t>(digit & 255) << (8 * (e / 2));
-        if (e & 1) odd |= byte;
-        else even |= byte;
+      for (int u = 0; u < kBatch; ++u) {
+        while (tok < tokens && i >= units_per_token) i -= units_per_token, ++tok;
+        toks[u] = tok;
+        is[u] = i;
+        i += kThreads;
+        raw[u].lo = raw[u].hi = make_uint4(0u, 0u, 0u, 0u);
+        if (toks[u] < tokens) {
+          const int entry = is[u] >> 4, k = s_list[entry] * 128 + (is[u] & 15) * 8, token = chunk * tokens + toks[u];
+          bool in = entry < n_entries && k < a.K && token < a.n;
+          // what the token does not compute is 0, and gate|up may have left it unwritten
+          if (!GATEUP && in && !a.dense) in = s_on[toks[u] * a.B + find_branch(s_off, a.B, k)] != 0;
+          if (in) raw[u] = load_raw(a.x, kind, token * a.x_stride + k);
+        }
       }
 #pragma unroll
-      for (int o = 1; o < 16 / GPB; o *= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-      out[p * tokens * 8] = make_uint2(even, odd);
-      if (k8 % (16 / GPB) == 0)
-        s_unit[(entry * GPB + j) * (NT * 8) + p * tokens + tok] = make_float2(unit, __int_as_float(-sum));
-      unit *= 256.0f;
+      for (int u = 0; u < kBatch; ++u) {
+        if (toks[u] >= tokens) break;
+        const int k8 = is[u] & 15, entry = is[u] >> 4;
+        float v[8], top = 0.0f;
+        to_f32(raw[u], kind, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+#pragma unroll
+        for (int o = 1; o < kLanes; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        // the largest becomes 127 in the highest digit and 0 below; a group all below 2^-100 counts as 0 (its unit would
+        // leave the range of fp32)
+        const float most = a.c.pieces == 3 ? 8323072.0f : 32512.0f;
+        const bool some = top >= 7.8886091e-31f;
+        const float inv = some ? most / top : 0.0f;
+        float unit = some ? top / most : 0.0f;
+        // bytes of (m + 0x808080) ^ 0x808080: the digits -128 .. 127 whose sum of powers of 256 is m
+        uint32_t m[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m[e] = (static_cast<uint32_t>(__float2int_rn(v[e] * inv)) + 0x00808080u) ^ 0x00808080u;
+        const int j = k8 / kLanes, word = unit_word<GPB>(k8);
+        if (GATEUP && a.x_scale != nullptr && k8 % kLanes == 0 && some) {
+          const int xg = a.x_groups == 1 ? 0 : (s_list[entry] * GPB + j) >> a.x_shift;
+          unit *= a.x_scale[static_cast<int64_t>(chunk * tokens + toks[u]) * a.x_groups + xg];
+        }
+        uint2* out = s_x + (((entry * 2 + (word >> 1)) * (NT * 8) + toks[u]) * 4 + unit_lane<GPB>(k8)) * 2 + (word & 1);
+        float2* units = s_unit + (entry * GPB + j) * (NT * 8) + toks[u];
+        const uint32_t e01 = __byte_perm(m[0], m[2], 0x5140), e23 = __byte_perm(m[4], m[6], 0x5140);   // digits 0 0 1 1 of a pair
+        const uint32_t o01 = __byte_perm(m[1], m[3], 0x5140), o23 = __byte_perm(m[5], m[7], 0x5140);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) {
+          if (p == a.c.pieces) break;
+          uint2 digits;
+          if (p < 2) {
+            digits = make_uint2(__byte_perm(e01, e23, p == 0 ? 0x5410 : 0x7632), __byte_perm(o01, o23, p == 0 ? 0x5410 : 0x7632));
+          } else {
+            digits = make_uint2(__byte_perm(__byte_perm(m[0], m[2], 0x0062), __byte_perm(m[4], m[6], 0x0062), 0x5410),
+                                __byte_perm(__byte_perm(m[1], m[3], 0x0062), __byte_perm(m[5], m[7], 0x0062), 0x5410));
+          }
+          int sum = __dp4a(static_cast<int>(digits.x), 0x01010101, __dp4a(static_cast<int>(digits.y), 0x01010101, 0));
+#pragma unroll
+          for (int o = 1; o < kLanes; o *= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+          out[p * tokens * 8] = digits;
+          if (k8 % kLanes == 0) units[p * tokens] = make_float2(unit, __int_as_float(-sum));
+          unit *= 256.0f;
+        }
+      }
     }
-  }
-  __syncthreads();
+    __syncthreads();
+  };
 
   // columns 8 nt + g: the lanes of a column that stands for no token keep zeros
   bool col_ok[NT];
@@ -374,12 +413,20 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
     for (int i = 0; i < 4; ++i) acc[nt][i] = 0.0f;
   float* sums = reinterpret_cast<float*>(smem + L.sums);
 
-  int slot = 0, c_tile = steps > 0 ? run_begin / steps : 0, c_step = steps > 0 ? run_begin % steps : 0;
-  for (int i = 0; i < count; ++i) {
-    cp_async_wait<kStages - 2>();
+  // turns below 0 fill the ring, and the activations are staged while the first copies are under way: one copy of the
+  // code of `issue`, since a block runs it cold
+  int slot = 0, c_tile = tile_begin, c_step = step_begin;
+  bool from_start = step_begin == 0;    // the run holds the current tile's first step
+#pragma unroll 1
+  for (int i = 1 - kStages; i < count; ++i) {
+    if (i >= 0) cp_async_wait<kStages - 2>();
     __syncwarp();                       // the stage is in shared memory for all lanes, and the slot before it has been read by all
     const uint8_t* st = smem + (warp * kStages + slot) * kStage;
-    issue(slot == 0 ? kStages - 1 : slot - 1);
+    issue(i < 0 ? i + kStages - 1 : (slot == 0 ? kStages - 1 : slot - 1));
+    if (i < 0) {
+      if (i == -1) stage_activations();
+      continue;
+    }
 #pragma unroll
     for (int j = 0; j < 2 * GPB; ++j) {
       const int block = j / GPB;
@@ -412,7 +459,8 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
         s[h] = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(st + 2048 + piece * 16 + g * 2));
         zero[h] = ZERO ? st[2048 + 4 * GPB * 16 + piece * 8 + g] : 8;
       }
-      // - zero * sum of digits first, then the codes' products
+      // - zero * sum of digits first, then the codes' products; on top of the bits of 12582912 = 1.5 * 2^23, so that the bits
+      // of the result (at most 15 * 128 * 128 in magnitude) are those of 12582912 + result in fp32
       const float4* up = reinterpret_cast<const float4*>(s_unit + ((2 * c_step) * GPB + j) * (NT * 8)) + t;
       int part[NT][4];
       float2 unit[NT];
@@ -420,10 +468,10 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
       for (int nt = 0; nt < NT; ++nt) {
         const float4 u = up[nt * 4];
         unit[nt] = make_float2(u.x, u.z);
-        part[nt][0] = zero[0] * __float_as_int(u.y);
-        part[nt][1] = zero[0] * __float_as_int(u.w);
-        part[nt][2] = ZERO ? zero[1] * __float_as_int(u.y) : part[nt][0];
-        part[nt][3] = ZERO ? zero[1] * __float_as_int(u.w) : part[nt][1];
+        part[nt][0] = zero[0] * __float_as_int(u.y) + 0x4B400000;
+        part[nt][1] = zero[0] * __float_as_int(u.w) + 0x4B400000;
+        part[nt][2] = ZERO ? zero[1] * __float_as_int(u.y) + 0x4B400000 : part[nt][0];
+        part[nt][3] = ZERO ? zero[1] * __float_as_int(u.w) + 0x4B400000 : part[nt][1];
       }
 #pragma unroll
       for (int w = 0; w < kWords; ++w) {
@@ -438,15 +486,17 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
       }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        // at most 15 * 128 * 256 in magnitude: exact in fp32
-        acc[nt][0] += __int2float_rn(part[nt][0]) * (s[0] * unit[nt].x);
-        acc[nt][1] += __int2float_rn(part[nt][1]) * (s[0] * unit[nt].y);
-        acc[nt][2] += __int2float_rn(part[nt][2]) * (s[1] * unit[nt].x);
-        acc[nt][3] += __int2float_rn(part[nt][3]) * (s[1] * unit[nt].y);
+        acc[nt][0] += (__int_as_float(part[nt][0]) - 12582912.0f) * (s[0] * unit[nt].x);
+        acc[nt][1] += (__int_as_float(part[nt][1]) - 12582912.0f) * (s[0] * unit[nt].y);
+        acc[nt][2] += (__int_as_float(part[nt][2]) - 12582912.0f) * (s[1] * unit[nt].x);
+        acc[nt][3] += (__int_as_float(part[nt][3]) - 12582912.0f) * (s[1] * unit[nt].y);
       }
     }
     slot = slot + 1 == kStages ? 0 : slot + 1;
     if (++c_step == steps || i + 1 == count) {      // the run leaves this tile: its part of the tile's sums
+      if (lane == 0 && from_start) s_first[c_tile] = warp;
+      if (lane == 0 && c_step == steps) s_last[c_tile] = warp;
+      from_start = true;
       float* p = sums + (warp + c_tile) * (NT * 8 * kColPitch) + (2 * t) * kColPitch + g;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -465,64 +515,56 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   cp_async_wait<0>();
   __syncthreads();
 
-  // ---- sums of a tile: the parts of the warps that worked on it, in order, and the pieces of the token
-  auto sum_of = [&](int tile, int tok, int row) {
+  // ---- a warp takes a tile, its half-warps a token each: the parts of the warps that worked on the tile, in order, and
+  // the digits of the token
+  const int row = lane & 15, half = lane >> 4;
+  float* own = reinterpret_cast<float*>(smem);       // of a cluster: this block's sums, over the ring
+  auto sum_of = [&](int w0, int w1, int tile, int tok) {
     float v = 0.0f;
-    if (steps == 0) return v;
-    const int w0 = tile * steps / per_warp, w1 = ((tile + 1) * steps - 1) / per_warp;
     for (int w = w0; w <= w1; ++w) {
       const float* p = sums + (w + tile) * (NT * 8 * kColPitch) + row;
       for (int c = tok; c < cols; c += tokens) v += p[c * kColPitch];
     }
     return v;
   };
-  float* own = reinterpret_cast<float*>(smem);       // of a cluster: this block's sums, over the ring
   if (cluster > 1) {
-    for (int i = threadIdx.x; i < n_tiles * tokens * 16; i += kThreads) own[i] = sum_of((i >> 4) / tokens, (i >> 4) % tokens, i & 15);
+    for (int tile = warp; tile < n_tiles; tile += kWarps) {
+      const int w0 = steps > 0 ? s_first[tile] : 0, w1 = steps > 0 ? s_last[tile] : -1;
+      for (int tok = half; tok < tokens; tok += 2) own[(tile * tokens + tok) * 16 + row] = sum_of(w0, w1, tile, tok);
+    }
     __syncthreads();
     ptx::cluster_sync_all();
   }
-  auto total_of = [&](int tile, int tok, int row) {
-    if (cluster == 1) return sum_of(tile, tok, row);
-    float v = 0.0f;
-    for (int r = 0; r < cluster; ++r) v += ld_cluster_f32(own + (tile * tokens + tok) * 16 + row, r);
-    return v;
-  };
-  if (GATEUP) {
-    for (int i = rank * kThreads + threadIdx.x; i < n_tiles * tokens * 8; i += cluster * kThreads) {
-      const int e = i & 7, tok = (i >> 3) % tokens, tile = (i >> 3) / tokens, token = chunk * tokens + tok;
-      if (token >= a.n) continue;
-      const int neuron = s_tiles[tile] * 8 + e, b = branch_of(a, neuron);
-      const bool on = a.dense || (s_active[b] != 0 && (a.select == nullptr || a.select[static_cast<int64_t>(token) * a.B + b] != 0));
-      float h = 0.0f;
-      if (on) {
-        const float gate = total_of(tile, tok, e), up = total_of(tile, tok, 8 + e);
-        h = gate / (1.0f + expf(-gate)) * up * a.alpha[b];
-      }
-      a.h[static_cast<int64_t>(token) * a.rows + neuron] = h;
-    }
-  } else {
-    for (int i = rank * kThreads + threadIdx.x; i < n_tiles * tokens * 16; i += cluster * kThreads) {
-      const int row = i & 15, tok = (i >> 4) % tokens, tile = (i >> 4) / tokens;
-      const int m = s_tiles[tile] * 16 + row, token = chunk * tokens + tok;
-      if (m >= a.rows || token >= a.n) continue;
-      float v = total_of(tile, tok, row);
-      if (a.select != nullptr) {
-        // c_t: the quotient and the root in double, rounded once, as the routed forward does
-        int k = 0, n_avail = 0;
-        for (int b = 0; b < a.B; ++b) {
-          const bool avail = a.alpha[b] != 0.0f;
-          n_avail += avail ? 1 : 0;
-          k += avail && a.select[static_cast<int64_t>(token) * a.B + b] != 0 ? 1 : 0;
+  for (int tile = rank * kWarps + warp; tile < n_tiles; tile += cluster * kWarps) {
+    const int w0 = steps > 0 ? s_first[tile] : 0, w1 = steps > 0 ? s_last[tile] : -1;
+    const int place = s_tiles[tile];
+    const int b = GATEUP ? find_branch(a.off, a.B, place * 8) : 0;
+    const int even_tokens = (tokens + 1) & ~1;
+    for (int tok = half; tok < even_tokens; tok += 2) {                     // whole warps: gate|up exchanges its halves below
+      const int token = chunk * tokens + tok;
+      const bool real = tok < tokens && token < a.n;
+      float v = 0.0f;
+      if (real) {
+        if (cluster == 1) {
+          v = sum_of(w0, w1, tile, tok);
+        } else {
+          for (int r = 0; r < cluster; ++r) v += ld_cluster_f32(own + (tile * tokens + tok) * 16 + row, r);
         }
-        float coef = k > 0 ? 1.0f : 0.0f;
-        if (k > 0 && a.compensate) coef = static_cast<float>(sqrt(static_cast<double>(n_avail) / static_cast<double>(k)));
-        v *= coef;
       }
-      const int64_t at = static_cast<int64_t>(token) * a.rows + m;
-      if (a.residual != nullptr) v += a.residual[at];
-      if (a.y_bf16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
-      else static_cast<float*>(a.y)[at] = v;
+      if (GATEUP) {
+        const float up = __shfl_down_sync(0xFFFFFFFFu, v, 8);               // rows 8..15 are the up rows of rows 0..7
+        if (!real || row >= 8) continue;
+        const bool on = a.dense || s_on[tok * a.B + b] != 0;
+        a.h[static_cast<int64_t>(token) * a.rows + place * 8 + row] = on ? v / (1.0f + expf(-v)) * up * a.alpha[b] : 0.0f;
+      } else {
+        const int m = place * 16 + row;
+        if (!real || m >= a.rows) continue;
+        if (a.select != nullptr) v *= s_coef[tok];
+        const int64_t at = static_cast<int64_t>(token) * a.rows + m;
+        if (a.residual != nullptr) v += a.residual[at];
+        if (a.y_bf16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
+        else static_cast<float*>(a.y)[at] = v;
+      }
     }
   }
   if (cluster > 1) {
