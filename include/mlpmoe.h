@@ -368,8 +368,8 @@ typedef struct {
  *     y_t = residual_t + c_t * sum_{b in S_t} alpha_b W_down^(b) [ silu(W_gate^(b) x_t) (.) W_up^(b) x_t ]
  * with S_t and c_t as in mlpmoe_forward_routed (select NULL: every branch with alpha_b != 0, c_t = 1).  Branches that
  * no token selects are not read.  Inside each group of columns x and the intermediate activation are held as fixed
- * point, 2^-23 (y fp32) or 2^-16 (y bf16) of the group's largest magnitude apart (a group all below 2^-100 counts as 0);
- * their products with the codes are exact, scales and sums are fp32.
+ * point, off by at most 2^-23 (y fp32) or 2^-15 (y bf16) of the group's largest magnitude (a group all below 2^-100
+ * counts as 0); their products with the codes are exact, scales and sums are fp32.
  *   x        device, [n_tokens x d_model] of x_dtype (bf16, fp32, or e4m3 with scales), rows x_stride elements apart
  *            (0 = d_model), 16-byte aligned, x_stride a multiple of 8
  *   x_scale  device fp32 [n_tokens x ceil(d_model / x_group)] for e4m3 (x_group = 0: one per token), else ignored;

@@ -128,17 +128,16 @@ def _ptr(t) -> Optional[int]:
     """Address of a torch tensor / numpy array / raw int, or None."""
     if t is None:
         return None
-    if isinstance(t, int):
-        return t
-    if isinstance(t, np.ndarray):
-        return t.ctypes.data
-    return t.data_ptr()
+    try:
+        return t.data_ptr()        # torch first: the call's host time is mostly this
+    except AttributeError:
+        return t.ctypes.data if isinstance(t, np.ndarray) else t
 
 
 def _stream(stream) -> Optional[int]:
-    if stream is None:
-        return None
-    return stream if isinstance(stream, int) else stream.cuda_stream
+    if stream is None or type(stream) is int:
+        return stream
+    return stream.cuda_stream
 
 
 def _arr(values, ctype):

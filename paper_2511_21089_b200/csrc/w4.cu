@@ -30,7 +30,7 @@ int w4_plan(W4Args* a, int pieces, int group) {
       int tokens = 24 / pieces < a->n ? 24 / pieces : a->n;
       for (; tokens > 0; --tokens) {
         const int cols = pieces * tokens, nt = (cols + 7) / 8;
-        const int64_t ring = w4::kWarps * (nt == 1 ? 4 : 3) * stage;
+        const int64_t ring = w4::kWarps * w4::stages(nt) * stage;
         const int64_t x = static_cast<int64_t>(entries) * nt * 1024, units = static_cast<int64_t>(entries) * gpb * nt * 64;
         const int64_t sums = static_cast<int64_t>(w4::kWarps - 1 + per) * nt * 8 * w4::kColPitch * 4;
         const int64_t own = static_cast<int64_t>(per) * tokens * 64;

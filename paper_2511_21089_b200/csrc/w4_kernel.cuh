@@ -6,11 +6,11 @@
 // Bound by HBM: the codes are read once.  Between the copy and the result an SM issues only a few operations per code, and
 // that is what limits such a kernel, so the products are taken on whole numbers (mma.sync, u8 x s8 in s32, exact): a
 // word of eight codes becomes two operand registers with two ANDs and a shift, where a bf16 product needs eleven
-// operations (210 against 256 issued per 16 x 128 block of codes even after tuning).  The activations are held as
-// fixed point inside each group of K: x = (d0 + 256 d1 + 65536 d2) * unit with digits of 8 bits, unit = the group's
-// largest |x| / 8323072; every digit is a column of the product, so up to eight columns (two tokens of three digits)
-// cost what one does.  Three digits (an fp32 y) keep 2^-23 of the group's largest, which is what an fp32 sum keeps;
-// two (y rounded to bf16, 2^-8) keep 2^-16.  sum (code - zero) x = sum code x - zero sum x exactly, the second sum being
+// operations (120 instructions in all against 210 per 16 x 128 block of codes).  The activations are held as fixed
+// point inside each group of K: x = (d0 + 256 d1 + 65536 d2) * unit with digits of 8 bits and unit a power of two;
+// every digit is a column of the product, so up to eight columns (two tokens of three digits) cost what one does.
+// Three digits (an fp32 y) are off by at most 2^-23 of the group's largest |x|, which is what an fp32 sum loses; two (y
+// rounded to bf16, 2^-8) by 2^-15.  sum (code - zero) x = sum code x - zero sum x exactly, the second sum being
 // the group's own; scale and unit are applied to the group's whole-number sum in fp32.
 // mma.sync and not tcgen05: a scale per group of K means reading the accumulators back after every 32 to 128 columns of
 // K, and for a few tokens the product's time is the copy's anyway.
@@ -59,10 +59,8 @@ template <int GPB>
 __host__ __device__ constexpr int stage_bytes() {
   return 2048 + 4 * GPB * 16 + 4 * GPB * 8;
 }
-template <int NT>
-__host__ __device__ constexpr int stages() {
-  return NT == 1 ? 4 : 3;
-}
+// Stages of a warp's ring: about 100 KB under way in an SM; a fifth stage measured the same.
+__host__ __device__ constexpr int stages(int nt) { return nt == 1 ? 4 : 3; }
 
 // Dynamic shared memory, in bytes from its start.
 struct Smem {
@@ -71,7 +69,7 @@ struct Smem {
 template <int NT, int GPB>
 __host__ __device__ inline Smem smem_of(const W4Args& a) {
   Smem s;
-  s.x = kWarps * stages<NT>() * stage_bytes<GPB>();                       // digits: [entry][2][8 NT][4] pairs of eights
+  s.x = kWarps * stages(NT) * stage_bytes<GPB>();                       // digits: [entry][2][8 NT][4] pairs of eights
   s.unit = s.x + a.entries * NT * 8 * 128;                                // their (unit, - sum of digits): [entry][GPB][8 NT]
   s.sums = s.unit + a.entries * GPB * NT * 8 * 8;                         // parts of the sums: [warp + tile][column][16 rows]
   s.list = s.sums + (kWarps - 1 + a.tiles_per_block) * NT * 8 * kColPitch * 4;
@@ -157,7 +155,7 @@ __device__ __forceinline__ void to_f32(const Raw& r, int kind, float (&v)[8]) {
 // grid: (shares of the row tiles, cluster along K, chunks of tokens)
 template <int NT, int GPB, bool GATEUP, bool ZERO>
 __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__ W4Args a) {
-  constexpr int kStages = stages<NT>(), kStage = stage_bytes<GPB>(), kWords = 4 / GPB;
+  constexpr int kStages = stages(NT), kStage = stage_bytes<GPB>(), kWords = 4 / GPB;
   constexpr int kLanes = 16 / GPB;      // threads that hold one group of a token's activations, eight each
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int s_scan[kWarps];
@@ -173,24 +171,29 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   int* s_off = reinterpret_cast<int*>(smem + L.branch);
   int* s_run = s_off + a.B + 1;
   uint8_t* s_on = reinterpret_cast<uint8_t*>(s_run + a.B + 1);
-  // gate|up waits for everything before it on the stream; by the time all its blocks have passed here only gate|up
-  // itself is outstanding, so the down kernel, which then may start, reads weights and selection without a wait.
-  if (GATEUP) {
-    ptx::griddep_wait();
-  }
-  ptx::griddep_launch_dependents();
-
   // ---- this block's K-blocks and tiles
   const int k_share = (a.kblocks + cluster - 1) / cluster;
   int n_entries = max(0, min(k_share, a.kblocks - rank * k_share));
   int n_tiles = min(a.tiles_per_block, a.tiles - static_cast<int>(blockIdx.x) * a.tiles_per_block);
+  if (GATEUP || a.dense)
+    for (int i = threadIdx.x; i < a.entries; i += kThreads) s_list[i] = rank * k_share + max(0, min(i, n_entries - 1));
+  if (!GATEUP || a.dense)
+    for (int i = threadIdx.x; i < n_tiles; i += kThreads) s_tiles[i] = blockIdx.x * a.tiles_per_block + i;
+  // gate|up waits for everything before it on the stream; by the time all its blocks have passed here only gate|up
+  // itself is outstanding, so the down kernel, which then may start, reads weights and selection without a wait.
+  if (GATEUP) ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
   if (!a.dense) {
     // what the chunk's tokens compute: [token][branch], and the branches of all of them
-    for (int b = threadIdx.x; b <= a.B; b += kThreads) s_off[b] = a.off[b];
-    for (int i = threadIdx.x; i < tokens * a.B; i += kThreads) {
-      const int token = chunk * tokens + i / a.B;
-      s_on[i] = token < a.n && a.alpha[i % a.B] != 0.0f && (a.select == nullptr || a.select[static_cast<int64_t>(token) * a.B + i % a.B] != 0);
+    for (int b = threadIdx.x; b <= a.B; b += kThreads) {
+      s_off[b] = a.off[b];
+      s_run[b] = b < a.B && a.alpha[b] != 0.0f;      // for now: available
     }
+    const uint8_t* select = a.select != nullptr ? a.select + static_cast<int64_t>(chunk) * tokens * a.B : nullptr;
+    const int n_pairs = min(tokens, a.n - chunk * tokens) * a.B;
+    for (int i = threadIdx.x; i < tokens * a.B; i += kThreads) s_on[i] = i < n_pairs && (select == nullptr || select[i] != 0);
+    __syncthreads();
+    for (int i = threadIdx.x; i < tokens * a.B; i += kThreads) s_on[i] &= s_run[i % a.B];
     __syncthreads();
     if (!GATEUP && a.select != nullptr) {
       // c_t: the quotient and the root in double, rounded once, as the routed forward does
@@ -198,7 +201,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
         int k = 0, n_avail = 0;
         for (int b = lane; b < a.B; b += 32) {
           k += s_on[tok * a.B + b];
-          n_avail += a.alpha[b] != 0.0f ? 1 : 0;
+          n_avail += s_run[b];
         }
         k = __reduce_add_sync(0xFFFFFFFFu, k);
         n_avail = __reduce_add_sync(0xFFFFFFFFu, n_avail);
@@ -248,10 +251,6 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
       s_list[threadIdx.x] = s_list[n_entries - 1];
     }
   }
-  if (GATEUP || a.dense)
-    for (int i = threadIdx.x; i < a.entries; i += kThreads) s_list[i] = rank * k_share + max(0, min(i, n_entries - 1));
-  if (!GATEUP || a.dense)
-    for (int i = threadIdx.x; i < n_tiles; i += kThreads) s_tiles[i] = blockIdx.x * a.tiles_per_block + i;
   __syncthreads();
 
   // ---- this warp's run of steps (tile, two K-blocks)
@@ -261,9 +260,13 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   const int count = min(n_tiles * steps, run_begin + per_warp) - run_begin;
   const int tile_begin = steps > 0 ? run_begin / steps : 0, step_begin = run_begin - tile_begin * steps;
 
-  // ---- copies of one stage: 16 bytes of codes per lane, K-block and half; scales and zeros by the first lanes
+  // ---- copies of one stage: of codes, eight lanes take the 64 bytes of a row in both K-blocks (a whole line where they
+  // are neighbours), four rows at a time; scales and zeros by the first lanes
   const uint32_t ring = ptx::smem_u32(smem) + warp * kStages * kStage;
-  const uint32_t q_dst = ring + g * 64 + (t ^ ((g >> 1) & 3)) * 16;
+  const int c_row = lane >> 3, c_block = (lane >> 2) & 1;
+  uint32_t q_dst[2];                    // rows c_row and c_row + 4 of a half
+#pragma unroll
+  for (int r = 0; r < 2; ++r) q_dst[r] = ring + c_block * 1024 + (c_row + 4 * r) * 64 + (t ^ (((c_row + 4 * r) >> 1) & 3)) * 16;
   const int s_block = (lane / (2 * GPB)) & 1, s_half = (lane / GPB) & 1, s_group = lane % GPB;   // lanes below 4 GPB
   const bool s_lane = lane < 4 * GPB;
   const uint8_t* const z_base = ZERO && s_lane ? (s_half ? a.m[1].zero : a.m[0].zero) : nullptr;
@@ -272,7 +275,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   const uint32_t rows16 = static_cast<uint32_t>(a.m[0].rows16);
   // Rows past the last, K-blocks past the last and columns past K are read from the nearest valid place: their results
   // are not used, or their digits and units are 0.
-  const uint8_t* q_src[2];
+  const uint8_t* q_src[2][2];           // [half][row]
   uint32_t s_row = 0;
   int i_tile = tile_begin, i_step = step_begin, i_left = count;
   if (ZERO && s_lane && z_base == nullptr) {         // a half without stored zeros beside one with them: 8 in every slot, for good
@@ -285,20 +288,20 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
       if (open) {                       // the first step of a tile
         const int tile = s_tiles[i_tile];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int row = GATEUP ? tile * 8 + g : min(tile * 16 + 8 * h + g, a.rows - 1);
-          q_src[h] = a.m[h].q + row * a.m[h].pitch;
-        }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const int row = c_row + 4 * r + (GATEUP ? tile * 8 : min(tile * 16 + 8 * h, a.rows - 8));
+            q_src[h][r] = a.m[h].q + row * a.m[h].pitch;
+          }
         s_row = static_cast<uint32_t>(GATEUP ? tile * 8 : min(tile * 16 + 8 * s_half, a.rows - 8));
       }
       const uint2 kb = *reinterpret_cast<const uint2*>(s_list + 2 * i_step);
-      const uint32_t dst = q_dst + slot * kStage;
+      const uint32_t byte = min((c_block == 0 ? kb.x : kb.y) * 64 + t * 16, last_byte);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const uint32_t byte = min((j == 0 ? kb.x : kb.y) * 64 + t * 16, last_byte);
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) cp_async16(dst + (j * 2 + h) * 512, q_src[h] + byte);
-      }
+        for (int r = 0; r < 2; ++r) cp_async16(q_dst[r] + slot * kStage + h * 512, q_src[h][r] + byte);
       if (s_lane) {
         const uint32_t at = min((s_block == 0 ? kb.x : kb.y) * GPB + s_group, last_group) * rows16 + s_row;
         cp_async16(ring + slot * kStage + 2048 + lane * 16, s_base + at);
@@ -320,31 +323,35 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   float2* s_unit = reinterpret_cast<float2*>(smem + L.unit);
   const int even_entries = 2 * steps, units_per_token = even_entries * 16;
   const int kind = GATEUP ? a.x_kind : MLPMOE_FP32;
+  // unit i of token tok; units_per_token is a multiple of 32, so a warp stays inside a token and is whole
+  constexpr int kBatch = NT == 1 ? 4 : 2;          // what the registers hold
+  Raw raw[kBatch];
+  int toks[kBatch], is[kBatch], tok_next = 0, i_next = threadIdx.x;
+  auto load_activations = [&]() {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      while (tok_next < tokens && i_next >= units_per_token) i_next -= units_per_token, ++tok_next;
+      toks[u] = tok_next;
+      is[u] = i_next;
+      i_next += kThreads;
+      raw[u].lo = raw[u].hi = make_uint4(0u, 0u, 0u, 0u);
+      if (toks[u] < tokens) {
+        const int entry = is[u] >> 4, k = s_list[entry] * 128 + (is[u] & 15) * 8, token = chunk * tokens + toks[u];
+        bool in = entry < n_entries && k < a.K && token < a.n;
+        // what the token does not compute is 0, and gate|up may have left it unwritten
+        if (!GATEUP && in && !a.dense) in = s_on[toks[u] * a.B + find_branch(s_off, a.B, k)] != 0;
+        if (in) raw[u] = load_raw(a.x, kind, token * a.x_stride + k);
+      }
+    }
+  };
   auto stage_activations = [&]() {
-    constexpr int kBatch = 4;
     for (int i = threadIdx.x; i < even_entries * GPB * NT * 8; i += kThreads)
       if (i % (NT * 8) >= cols) s_unit[i] = make_float2(0.0f, 0.0f);
-    if (!GATEUP) ptx::griddep_wait();   // h is complete
-    // unit i of token tok; units_per_token is a multiple of 32, so a warp stays inside a token and is whole
-    int tok = 0, i = threadIdx.x;
-    while (tok < tokens) {
-      Raw raw[kBatch];
-      int toks[kBatch], is[kBatch];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        while (tok < tokens && i >= units_per_token) i -= units_per_token, ++tok;
-        toks[u] = tok;
-        is[u] = i;
-        i += kThreads;
-        raw[u].lo = raw[u].hi = make_uint4(0u, 0u, 0u, 0u);
-        if (toks[u] < tokens) {
-          const int entry = is[u] >> 4, k = s_list[entry] * 128 + (is[u] & 15) * 8, token = chunk * tokens + toks[u];
-          bool in = entry < n_entries && k < a.K && token < a.n;
-          // what the token does not compute is 0, and gate|up may have left it unwritten
-          if (!GATEUP && in && !a.dense) in = s_on[toks[u] * a.B + find_branch(s_off, a.B, k)] != 0;
-          if (in) raw[u] = load_raw(a.x, kind, token * a.x_stride + k);
-        }
-      }
+    if (!GATEUP) {
+      ptx::griddep_wait();              // h is complete
+      load_activations();
+    }
+    while (toks[0] < tokens) {
 #pragma unroll
       for (int u = 0; u < kBatch; ++u) {
         if (toks[u] >= tokens) break;
@@ -355,16 +362,22 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
         for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
 #pragma unroll
         for (int o = 1; o < kLanes; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        // the largest becomes 127 in the highest digit and 0 below; a group all below 2^-100 counts as 0 (its unit would
-        // leave the range of fp32)
-        const float most = a.c.pieces == 3 ? 8323072.0f : 32512.0f;
+        // unit: the power of two that puts the largest magnitude between 2^22 / 1.004 and 8355711 (three digits of at most
+        // 127; two: 2^14 / 1.004 and 32639), so that x / unit is exact before it is rounded; a group all below 2^-100
+        // counts as 0 (its unit would leave the range of fp32)
+        const int exponent = (__float_as_int(top * 1.00396f) >> 23) + (a.c.pieces == 3 ? 1 - 23 : 1 - 15);
         const bool some = top >= 7.8886091e-31f;
-        const float inv = some ? most / top : 0.0f;
-        float unit = some ? top / most : 0.0f;
+        const float inv = some ? __int_as_float((254 - exponent) << 23) : 0.0f;
+        float unit = some ? __int_as_float(exponent << 23) : 0.0f;
         // bytes of (m + 0x808080) ^ 0x808080: the digits -128 .. 127 whose sum of powers of 256 is m
         uint32_t m[8];
+        if (a.c.pieces == 3) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m[e] = (static_cast<uint32_t>(__float2int_rn(v[e] * inv)) + 0x00808080u) ^ 0x00808080u;
+          for (int e = 0; e < 8; ++e) m[e] = (static_cast<uint32_t>(__float2int_rn(v[e] * inv)) + 0x00808080u) ^ 0x00808080u;
+        } else {                        // below 2^22: the sum with 1.5 * 2^23 has the rounded number in its low bits
+#pragma unroll
+          for (int e = 0; e < 8; ++e) m[e] = (__float_as_uint(fmaf(v[e], inv, 12582912.0f)) - 0x4B400000u + 0x00808080u) ^ 0x00808080u;
+        }
         const int j = k8 / kLanes, word = unit_word<GPB>(k8);
         if (GATEUP && a.x_scale != nullptr && k8 % kLanes == 0 && some) {
           const int xg = a.x_groups == 1 ? 0 : (s_list[entry] * GPB + j) >> a.x_shift;
@@ -374,27 +387,35 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
         float2* units = s_unit + (entry * GPB + j) * (NT * 8) + toks[u];
         const uint32_t e01 = __byte_perm(m[0], m[2], 0x5140), e23 = __byte_perm(m[4], m[6], 0x5140);   // digits 0 0 1 1 of a pair
         const uint32_t o01 = __byte_perm(m[1], m[3], 0x5140), o23 = __byte_perm(m[5], m[7], 0x5140);
+        auto sum_of_eight = [](uint2 d) { return __dp4a(static_cast<int>(d.x), 0x01010101, __dp4a(static_cast<int>(d.y), 0x01010101, 0)); };
+        const uint2 d0 = make_uint2(__byte_perm(e01, e23, 0x5410), __byte_perm(o01, o23, 0x5410));
+        const uint2 d1 = make_uint2(__byte_perm(e01, e23, 0x7632), __byte_perm(o01, o23, 0x7632));
+        // a sum over 128 digits fits in 16 bits: two digits' sums in one word
+        int sums01 = sum_of_eight(d0) + (sum_of_eight(d1) << 16);
 #pragma unroll
-        for (int p = 0; p < 3; ++p) {
-          if (p == a.c.pieces) break;
-          uint2 digits;
-          if (p < 2) {
-            digits = make_uint2(__byte_perm(e01, e23, p == 0 ? 0x5410 : 0x7632), __byte_perm(o01, o23, p == 0 ? 0x5410 : 0x7632));
-          } else {
-            digits = make_uint2(__byte_perm(__byte_perm(m[0], m[2], 0x0062), __byte_perm(m[4], m[6], 0x0062), 0x5410),
-                                __byte_perm(__byte_perm(m[1], m[3], 0x0062), __byte_perm(m[5], m[7], 0x0062), 0x5410));
-          }
-          int sum = __dp4a(static_cast<int>(digits.x), 0x01010101, __dp4a(static_cast<int>(digits.y), 0x01010101, 0));
+        for (int o = 1; o < kLanes; o *= 2) sums01 += __shfl_xor_sync(0xFFFFFFFFu, sums01, o);
+        const int sum0 = static_cast<int16_t>(sums01), sum1 = (sums01 - sum0) >> 16;
+        out[0] = d0;
+        out[tokens * 8] = d1;
+        if (k8 % kLanes == 0) {
+          units[0] = make_float2(unit, __int_as_float(-sum0));
+          units[tokens] = make_float2(unit * 256.0f, __int_as_float(-sum1));
+        }
+        if (a.c.pieces == 3) {
+          const uint2 d2 = make_uint2(__byte_perm(__byte_perm(m[0], m[2], 0x0062), __byte_perm(m[4], m[6], 0x0062), 0x5410),
+                                      __byte_perm(__byte_perm(m[1], m[3], 0x0062), __byte_perm(m[5], m[7], 0x0062), 0x5410));
+          int sum2 = sum_of_eight(d2);
 #pragma unroll
-          for (int o = 1; o < kLanes; o *= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-          out[p * tokens * 8] = digits;
-          if (k8 % kLanes == 0) units[p * tokens] = make_float2(unit, __int_as_float(-sum));
-          unit *= 256.0f;
+          for (int o = 1; o < kLanes; o *= 2) sum2 += __shfl_xor_sync(0xFFFFFFFFu, sum2, o);
+          out[2 * tokens * 8] = d2;
+          if (k8 % kLanes == 0) units[2 * tokens] = make_float2(unit * 65536.0f, __int_as_float(-sum2));
         }
       }
+      load_activations();
     }
     __syncthreads();
   };
+  if (GATEUP) load_activations();       // on their way before the weights
 
   // columns 8 nt + g: the lanes of a column that stands for no token keep zeros
   bool col_ok[NT];
@@ -539,31 +560,45 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
     const int w0 = steps > 0 ? s_first[tile] : 0, w1 = steps > 0 ? s_last[tile] : -1;
     const int place = s_tiles[tile];
     const int b = GATEUP ? find_branch(a.off, a.B, place * 8) : 0;
-    const int even_tokens = (tokens + 1) & ~1;
-    for (int tok = half; tok < even_tokens; tok += 2) {                     // whole warps: gate|up exchanges its halves below
-      const int token = chunk * tokens + tok;
-      const bool real = tok < tokens && token < a.n;
-      float v = 0.0f;
-      if (real) {
-        if (cluster == 1) {
-          v = sum_of(w0, w1, tile, tok);
-        } else {
-          for (int r = 0; r < cluster; ++r) v += ld_cluster_f32(own + (tile * tokens + tok) * 16 + row, r);
+    for (int tok0 = half; tok0 < tokens + half; tok0 += 8) {                // whole warps; four tokens' loads under way together
+      float v[4], up[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int tok = tok0 + 2 * u;
+        v[u] = 0.0f;
+        if (tok < tokens) {
+          if (cluster == 1) {
+            v[u] = sum_of(w0, w1, tile, tok);
+          } else {
+            float part[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) part[r] = r < cluster ? ld_cluster_f32(own + (tile * tokens + tok) * 16 + row, r) : 0.0f;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v[u] += part[r];
+          }
         }
       }
       if (GATEUP) {
-        const float up = __shfl_down_sync(0xFFFFFFFFu, v, 8);               // rows 8..15 are the up rows of rows 0..7
-        if (!real || row >= 8) continue;
-        const bool on = a.dense || s_on[tok * a.B + b] != 0;
-        a.h[static_cast<int64_t>(token) * a.rows + place * 8 + row] = on ? v / (1.0f + expf(-v)) * up * a.alpha[b] : 0.0f;
-      } else {
-        const int m = place * 16 + row;
-        if (!real || m >= a.rows) continue;
-        if (a.select != nullptr) v *= s_coef[tok];
-        const int64_t at = static_cast<int64_t>(token) * a.rows + m;
-        if (a.residual != nullptr) v += a.residual[at];
-        if (a.y_bf16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
-        else static_cast<float*>(a.y)[at] = v;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) up[u] = __shfl_down_sync(0xFFFFFFFFu, v[u], 8);      // rows 8..15 are the up rows of rows 0..7
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int tok = tok0 + 2 * u, token = chunk * tokens + tok;
+        if (tok >= tokens || token >= a.n) break;
+        if (GATEUP) {
+          if (row >= 8) break;
+          const bool on = a.dense || s_on[tok * a.B + b] != 0;
+          a.h[static_cast<int64_t>(token) * a.rows + place * 8 + row] = on ? v[u] / (1.0f + expf(-v[u])) * up[u] * a.alpha[b] : 0.0f;
+        } else {
+          const int m = place * 16 + row;
+          if (m >= a.rows) break;
+          if (a.select != nullptr) v[u] *= s_coef[tok];
+          const int64_t at = static_cast<int64_t>(token) * a.rows + m;
+          if (a.residual != nullptr) v[u] += a.residual[at];
+          if (a.y_bf16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v[u]);
+          else static_cast<float*>(a.y)[at] = v[u];
+        }
       }
     }
   }

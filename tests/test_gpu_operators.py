@@ -300,12 +300,11 @@ class W4Case:
         return y.t
 
     def tolerance(self, r, xh, yt):
-        """Inside a group of K the activations are whole multiples of unit = max / 8323072 (y fp32) or max / 32512 (y bf16): off
-        by half a unit, and by two roundings of x / unit (each u of at most max / unit, so 1 unit more for the finer one):
-        1.5 / 8323072 or 0.51 / 32512 of the group's largest.  The products are exact.  Sums in fp32: one term per group
-        and digit, up to 16 + 8 parts to join, and six roundings of a term (scale times unit, the product, unit's own, a factor
-        for e4m3's scale); the digits of x add up to at most 3 |x| in magnitude."""
-        q = 1.5 / 8323072 if yt == "fp32" else 0.51 / 32512
+        """Inside a group of K the activations are whole multiples of a unit, a power of two of which the group's largest is at
+        least 2^22 / 1.004 (y fp32) or 2^14 / 1.004 (y bf16): off by half a unit, 1.004 * 2^-23 or 1.004 * 2^-15 of it.  The
+        products are exact.  Sums in fp32: one term per group and digit, up to 16 + 8 parts to join, and six roundings of a
+        term (scale times unit, the product, a factor for e4m3's scale); the digits of x add up to at most 3 |x| in magnitude."""
+        q = 1.004 * (2.0 ** -23 if yt == "fp32" else 2.0 ** -15)
         starts = np.arange(0, self.d, self.group)
         top = np.maximum.reduceat(np.abs(xh), starts, axis=1)
 
@@ -437,7 +436,7 @@ def test_w4_forward_full_size(lib, d, I, n):
     g, u = xd @ deq[0].t(), xd @ deq[1].t()
     h = torch.nn.functional.silu(g) * u
     # as W4Case.tolerance, on the device
-    q = 1.5 / 8323072
+    q = 1.004 * 2.0 ** -23
 
     def product(K, size, v, W):
         tops = v.abs().view(n, -1, group).amax(2)
