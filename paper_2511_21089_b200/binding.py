@@ -126,12 +126,12 @@ def _check(status: int, where: str) -> None:
 
 def _ptr(t) -> Optional[int]:
     """Address of a torch tensor / numpy array / raw int, or None."""
-    if t is None:
-        return None
+    if t is None or type(t) is int:
+        return t
     try:
-        return t.data_ptr()        # torch first: the call's host time is mostly this
+        return t.data_ptr()        # torch first: this is most of a call's host time
     except AttributeError:
-        return t.ctypes.data if isinstance(t, np.ndarray) else t
+        return t.ctypes.data if isinstance(t, np.ndarray) else int(t)
 
 
 def _stream(stream) -> Optional[int]:

@@ -13,10 +13,13 @@ namespace mlpmoe {
 namespace {
 
 constexpr int kMaxB = 256;
-constexpr int kRouteThreads = 256;
-constexpr int kRouteCtas = 296;        // forward: two blocks on each of the 148 SMs, so that the sums to join stay few
+constexpr int kRouteThreads = 1024;    // forward: one block per SM, so that few sums are left to join
+constexpr int kRouteWarps = kRouteThreads / 32;
+constexpr int kRouteCtas = 148;
+constexpr int kRouteRows = 2;          // rows of a segment at a time: two chains of exchanges in flight
+constexpr int kBackwardThreads = 256;
 constexpr int kBackwardCtas = 148 * 8;
-constexpr int kFinishThreads = 1024;
+constexpr int kBackwardRows = 2;
 
 // One block's contribution: B probability sums, then B counts and the number of routed tokens as int32.
 __host__ __device__ inline int64_t partial_words(int B) { return 2 * B + 1; }
@@ -41,9 +44,15 @@ struct RouteArgs {
 
 template <int W>
 __device__ __forceinline__ float seg_max(float v) {
+  if constexpr (W == 32) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xFFFFFFFF;" : "=f"(r) : "f"(v));
+    return r;
+  } else {
 #pragma unroll
-  for (int o = W / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-  return v;
+    for (int o = W / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    return v;
+  }
 }
 template <int W>
 __device__ __forceinline__ float seg_sum(float v) {
@@ -51,17 +60,6 @@ __device__ __forceinline__ float seg_sum(float v) {
   for (int o = W / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
   return v;
 }
-template <int W>
-__device__ __forceinline__ uint32_t seg_max_u32(uint32_t v) {
-  if constexpr (W == 32) {
-    return __reduce_max_sync(0xFFFFFFFFu, v);
-  } else {
-#pragma unroll
-    for (int o = W / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-    return v;
-  }
-}
-
 // The row's values of one lane; places that are not eligible become -infinity, +infinity the largest finite value.
 template <typename T, int VPT, bool VEC>
 __device__ __forceinline__ void load_row(const T* row, int c0, int B, uint32_t avail_mask, bool live, float (&x)[VPT]) {
@@ -102,22 +100,60 @@ __device__ __forceinline__ uint32_t avail_mask_of(const uint8_t* avail, int c0, 
   return m;
 }
 
-// Order-preserving bits of a float; 0 stands for "not eligible" (a float's own image is never 0: -infinity is excluded).
-__device__ __forceinline__ uint32_t key_of(float x) {
-  if (x == -INFINITY) return 0u;
-  const uint32_t u = __float_as_uint(x + 0.0f);    // -0 and +0 are equal: both become +0
-  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+// Descending.
+template <int VPT>
+__device__ __forceinline__ void sort_down(float (&s)[VPT]) {
+  auto order = [&](int i, int j) {
+    const float hi = fmaxf(s[i], s[j]);
+    s[j] = fminf(s[i], s[j]);
+    s[i] = hi;
+  };
+  // odd-even merge networks of 4 and of 8 (Batcher)
+  order(0, 1), order(2, 3), order(0, 2), order(1, 3), order(1, 2);
+  if constexpr (VPT == 8) {
+    order(4, 5), order(6, 7), order(4, 6), order(5, 7), order(5, 6);
+    order(0, 4), order(1, 5), order(2, 6), order(3, 7), order(2, 4), order(3, 5), order(1, 2), order(3, 4), order(5, 6);
+  }
 }
 
-// A block's rows; its column sums go to a.partial, added up in the order of its warps and row segments.
+// What is left once the sums of a column over all tokens are in s_prob[b], s_count[b] and the routed tokens in *s_routed: the outputs.
+__device__ void route_outputs(const RouteArgs& a, const float* s_prob, const int* s_count, const int* s_routed) {
+  const int routed = *s_routed;
+  if (threadIdx.x < 32) {
+    double dot = 0.0;
+    int64_t total = 0;
+    int n_avail = 0;
+    for (int b = threadIdx.x; b < a.B; b += 32) {
+      dot += static_cast<double>(s_count[b]) * static_cast<double>(s_prob[b]);
+      total += s_count[b];
+      n_avail += a.avail == nullptr || a.avail[b] != 0 ? 1 : 0;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
+      total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+      n_avail += __shfl_xor_sync(0xFFFFFFFFu, n_avail, o);
+    }
+    if (threadIdx.x == 0) {
+      a.loss[0] = total > 0 ? static_cast<float>(n_avail * dot / (static_cast<double>(total) * routed)) : 0.0f;
+      a.counts[a.B] = routed;
+    }
+  }
+  for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
+    a.counts[b] = s_count[b];
+    a.prob[b] = routed > 0 ? s_prob[b] / static_cast<float>(routed) : 0.0f;
+  }
+}
+
+// A block's rows.  Of the k largest, each lane offers the largest of its columns that is not taken yet (they are sorted
+// once); every lane that holds the row's largest takes it, until k are taken; that gives the smallest value taken, and
+// the selection is what lies above it and, of equals, the first in index order.
 template <typename T, int LPR, int VPT, bool VEC>
 __global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_constant__ RouteArgs a) {
-  constexpr int kWarps = kRouteThreads / 32, kRows = 32 / LPR;    // kRows: rows of a warp at a time
-  constexpr int kSlots = kWarps * kRows, kCols = LPR * VPT;
-  __shared__ float s_prob[kSlots * kCols];
-  __shared__ int s_count[kSlots * kCols];
-  __shared__ int s_routed[kWarps];
-  ptx::griddep_launch_dependents();
+  constexpr int kSegs = 32 / LPR, kCols = LPR * VPT, R = kRouteRows;
+  __shared__ float s_prob[kRouteWarps * kCols];     // per warp and column: probabilities, then counts
+  __shared__ int s_count[kMaxB];
+  __shared__ int s_routed[kRouteWarps];
   ptx::griddep_wait();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int seg = lane / LPR, l = lane % LPR, c0 = l * VPT;
@@ -129,126 +165,189 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_const
 #pragma unroll
   for (int i = 0; i < VPT; ++i) prob[i] = 0.0f, count[i] = 0;
 
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps * kRows;
-  for (int64_t base = (static_cast<int64_t>(blockIdx.x) * kWarps + warp) * kRows; base < a.n; base += step) {
-    const int64_t t = base + seg;
-    const bool live = t < a.n && (a.valid == nullptr || a.valid[t] != 0);
-    float x[VPT];
-    load_row<T, VPT, VEC>(static_cast<const T*>(a.logits) + (t < a.n ? t : 0) * a.stride, c0, a.B, avail_mask, live, x);
-    // softmax
-    float m = x[0];
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kRouteWarps * kSegs * R;
+  for (int64_t base = (static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp) * kSegs * R; base < a.n; base += step) {
+    float x[R][VPT], s[R][VPT], least[R];
+    int taken[R];
 #pragma unroll
-    for (int i = 1; i < VPT; ++i) m = fmaxf(m, x[i]);
-    m = seg_max<LPR>(m);
-    const bool any = m > -INFINITY;
-    float e[VPT], sum = 0.0f;
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      e[i] = x[i] > -INFINITY ? expf(x[i] - m) : 0.0f;
-      sum += e[i];
+    for (int r = 0; r < R; ++r) {
+      const int64_t t = base + r * kSegs + seg;
+      const bool live = t < a.n && (a.valid == nullptr || a.valid[t] != 0);
+      load_row<T, VPT, VEC>(static_cast<const T*>(a.logits) + (t < a.n ? t : 0) * a.stride, c0, a.B, avail_mask, live, x[r]);
     }
-    sum = seg_sum<LPR>(sum);
-    const float inv = any ? 1.0f / sum : 0.0f;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) prob[i] += e[i] * inv;
-    routed += any && l == 0 ? 1 : 0;
-    // top k: each lane offers the largest of its columns that is not taken yet; the first lane with the row's largest
-    // key takes it (columns ascend with the lane, and inside a lane the lowest index wins a tie)
-    uint32_t key[VPT], taken = 0;
+    for (int r = 0; r < R; ++r) {
+      // softmax; a place that is not eligible holds -infinity and gets exp(-infinity) = 0
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) key[i] = key_of(x[i]);
-    for (int r = 0; r < a.k; ++r) {
-      uint32_t best = key[0];
-      int at = 0;
+      for (int i = 0; i < VPT; ++i) s[r][i] = x[r][i];
+      sort_down(s[r]);
+      const float m = seg_max<LPR>(s[r][0]);
+      const bool any = m > -INFINITY;
+      const float top = any ? m : 0.0f;
+      float e[VPT], sum = 0.0f;
 #pragma unroll
-      for (int i = 1; i < VPT; ++i)
-        if (key[i] > best) best = key[i], at = i;
-      const uint32_t top = seg_max_u32<LPR>(best);
-      const uint32_t who = __ballot_sync(0xFFFFFFFFu, best == top && top != 0u) & seg_lanes;
-      if (who != 0u && lane == __ffs(who) - 1) {
-        taken |= 1u << at;
-#pragma unroll
-        for (int i = 0; i < VPT; ++i)
-          if (i == at) key[i] = 0u;
+      for (int i = 0; i < VPT; ++i) {
+        e[i] = expf(x[r][i] - top);
+        sum += e[i];
       }
-      if (__ballot_sync(0xFFFFFFFFu, who != 0u) == 0u) break;     // no row of the warp has an eligible place left
+      sum = seg_sum<LPR>(sum);
+      const float inv = any ? 1.0f / sum : 0.0f;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) prob[i] += e[i] * inv;
+      routed += any && l == 0 ? 1 : 0;
+      taken[r] = any ? 0 : a.k;
+      least[r] = INFINITY;
+    }
+    for (int turn = 0; turn < a.k; ++turn) {
+      bool more = false;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const float top = seg_max<LPR>(s[r][0]);
+        const bool hit = s[r][0] == top && top > -INFINITY && taken[r] < a.k;
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, hit) & seg_lanes;
+        if (who != 0u) least[r] = top;
+        taken[r] += __popc(who);
+        if (hit) {
+#pragma unroll
+          for (int i = 0; i + 1 < VPT; ++i) s[r][i] = s[r][i + 1];
+          s[r][VPT - 1] = -INFINITY;
+        }
+        more = more || (who != 0u && taken[r] < a.k);
+      }
+      if (!__any_sync(0xFFFFFFFFu, more)) break;
     }
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) count[i] += (taken >> i) & 1u;
-    if (t < a.n) {
-      uint8_t* out = a.select + t * a.B + c0;
-      if (byte_vec) {
+    for (int r = 0; r < R; ++r) {
+      uint32_t above = 0, equal = 0;
 #pragma unroll
-        for (int i = 0; i < VPT; i += 4) {
-          const uint32_t b = taken >> i;
-          if (c0 + i < a.B)
-            *reinterpret_cast<uint32_t*>(out + i) = (b & 1u) | ((b & 2u) << 7) | ((b & 4u) << 14) | ((b & 8u) << 21);
-        }
+      for (int i = 0; i < VPT; ++i) {
+        above |= x[r][i] > least[r] ? 1u << i : 0u;
+        equal |= x[r][i] == least[r] ? 1u << i : 0u;
+      }
+      // equals: as many as are wanted, the first in index order (columns ascend with the lane)
+      int n_above = __popc(above), n_equal = __popc(equal);
+      const int mine = n_equal;
+      if constexpr (LPR == 32) {
+        n_above = __reduce_add_sync(0xFFFFFFFFu, n_above);
+        n_equal = __reduce_add_sync(0xFFFFFFFFu, n_equal);
       } else {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i)
-          if (c0 + i < a.B) out[i] = (taken >> i) & 1u;
+        for (int o = LPR / 2; o > 0; o >>= 1) {
+          n_above += __shfl_xor_sync(0xFFFFFFFFu, n_above, o);
+          n_equal += __shfl_xor_sync(0xFFFFFFFFu, n_equal, o);
+        }
+      }
+      if (__any_sync(0xFFFFFFFFu, n_above + n_equal > a.k)) {
+        int before = mine;
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) {
+          const int u = __shfl_up_sync(0xFFFFFFFFu, before, o, LPR);
+          if (l >= o) before += u;
+        }
+        int room = a.k - n_above - (before - mine);
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+          if ((equal >> i) & 1u) {
+            if (room <= 0) equal &= ~(1u << i);
+            --room;
+          }
+        }
+      }
+      const uint32_t chosen = above | equal;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) count[i] += (chosen >> i) & 1u;
+      const int64_t t = base + r * kSegs + seg;
+      if (t < a.n) {
+        uint8_t* out = a.select + t * a.B + c0;
+        if (byte_vec) {
+#pragma unroll
+          for (int i = 0; i < VPT; i += 4) {
+            const uint32_t b = chosen >> i;
+            if (c0 + i < a.B)
+              *reinterpret_cast<uint32_t*>(out + i) = (b & 1u) | ((b & 2u) << 7) | ((b & 4u) << 14) | ((b & 8u) << 21);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < VPT; ++i)
+            if (c0 + i < a.B) out[i] = (chosen >> i) & 1u;
+        }
       }
     }
   }
 
-  const int slot = warp * kRows + seg;
+  // the warp's rows, then the block's in the order of its warps
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    s_prob[slot * kCols + c0 + i] = prob[i];
-    s_count[slot * kCols + c0 + i] = count[i];
+#pragma unroll
+    for (int o = 16; o >= LPR; o >>= 1) {
+      prob[i] += __shfl_xor_sync(0xFFFFFFFFu, prob[i], o);
+      count[i] += __shfl_xor_sync(0xFFFFFFFFu, count[i], o);
+    }
+    if (seg == 0) s_prob[warp * kCols + c0 + i] = prob[i];
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) routed += __shfl_xor_sync(0xFFFFFFFFu, routed, o);
   if (lane == 0) s_routed[warp] = routed;
   __syncthreads();
-  uint32_t* out = a.partial + static_cast<int64_t>(blockIdx.x) * partial_words(a.B);
-  for (int b = threadIdx.x; b < a.B; b += kRouteThreads) {
-    float p = 0.0f;
-    int c = 0;
-    for (int s = 0; s < kSlots; ++s) {
-      p += s_prob[s * kCols + b];
-      c += s_count[s * kCols + b];
-    }
-    out[b] = __float_as_uint(p);
-    out[a.B + b] = static_cast<uint32_t>(c);
+  float p = 0.0f;
+  const int b = threadIdx.x;
+  if (b < a.B)
+    for (int w = 0; w < kRouteWarps; ++w) p += s_prob[w * kCols + b];
+  __syncthreads();
+  int* s_warp_count = reinterpret_cast<int*>(s_prob);
+  if (seg == 0) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) s_warp_count[warp * kCols + c0 + i] = count[i];
   }
-  if (threadIdx.x == 0) {
-    int c = 0;
-    for (int w = 0; w < kWarps; ++w) c += s_routed[w];
-    out[2 * a.B] = static_cast<uint32_t>(c);
+  __syncthreads();
+  int c = 0;
+  if (b < a.B)
+    for (int w = 0; w < kRouteWarps; ++w) c += s_warp_count[w * kCols + b];
+  if (threadIdx.x == 0)
+    for (int w = 1; w < kRouteWarps; ++w) s_routed[0] += s_routed[w];
+  __syncthreads();
+  if (gridDim.x == 1) {
+    if (b < a.B) s_prob[b] = p, s_count[b] = c;
+    __syncthreads();
+    route_outputs(a, s_prob, s_count, s_routed);
+  } else {
+    uint32_t* out = a.partial + static_cast<int64_t>(blockIdx.x) * partial_words(a.B);
+    if (b < a.B) {
+      out[b] = __float_as_uint(p);
+      out[a.B + b] = static_cast<uint32_t>(c);
+    }
+    if (threadIdx.x == 0) out[2 * a.B] = static_cast<uint32_t>(s_routed[0]);
   }
 }
 
-// Adds the blocks' contributions (in block order), then the loss.  One block.
-__global__ void __launch_bounds__(kFinishThreads) route_finish_kernel(const __grid_constant__ RouteArgs a, int n_partial) {
-  __shared__ float s_prob[kFinishThreads];
-  __shared__ int s_count[kFinishThreads];
-  __shared__ int s_avail;
-  ptx::griddep_launch_dependents();
+// Adds the blocks' contributions in a fixed order: thread (part, b) takes every parts-th block's sums of column b.
+__global__ void __launch_bounds__(kRouteThreads) route_finish_kernel(const __grid_constant__ RouteArgs a, int n_partial) {
+  __shared__ float s_prob[kRouteThreads];
+  __shared__ int s_count[kRouteThreads];
+  __shared__ int s_routed;
   ptx::griddep_wait();
   const int words = static_cast<int>(partial_words(a.B));
-  // thread (part, b): every parts-th block's sums of column b
   int cols = 8;
   while (cols < a.B) cols *= 2;
-  const int parts = kFinishThreads / cols, b = threadIdx.x % cols, part = threadIdx.x / cols;
+  const int parts = kRouteThreads / cols, b = threadIdx.x % cols, part = threadIdx.x / cols;
   float p = 0.0f;
-  int c = 0, routed = 0;
+  int c = 0;
   if (b < a.B) {
+#pragma unroll 8
     for (int i = part; i < n_partial; i += parts) {
-      p += __uint_as_float(a.partial[static_cast<int64_t>(i) * words + b]);
-      c += static_cast<int>(a.partial[static_cast<int64_t>(i) * words + a.B + b]);
+      p += __uint_as_float(a.partial[i * words + b]);
+      c += static_cast<int>(a.partial[i * words + a.B + b]);
     }
   }
   s_prob[threadIdx.x] = p;
   s_count[threadIdx.x] = c;
-  if (threadIdx.x == 0) s_avail = 0;
   __syncthreads();
   if (threadIdx.x < 32) {
-    for (int i = threadIdx.x; i < n_partial; i += 32) routed += static_cast<int>(a.partial[static_cast<int64_t>(i) * words + 2 * a.B]);
+    int routed = 0;
+    for (int i = threadIdx.x; i < n_partial; i += 32) routed += static_cast<int>(a.partial[i * words + 2 * a.B]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) routed += __shfl_xor_sync(0xFFFFFFFFu, routed, o);
-    if (threadIdx.x == 0) a.counts[a.B] = routed;
+    if (threadIdx.x == 0) s_routed = routed;
   }
   if (part == 0 && b < a.B) {
     p = 0.0f;
@@ -257,103 +356,89 @@ __global__ void __launch_bounds__(kFinishThreads) route_finish_kernel(const __gr
       p += s_prob[i * cols + b];
       c += s_count[i * cols + b];
     }
-    a.counts[b] = c;
-    if (a.avail == nullptr || a.avail[b] != 0) atomicAdd(&s_avail, 1);
   }
   __syncthreads();
-  if (part == 0) {
-    s_prob[b] = b < a.B ? p : 0.0f;
-    s_count[b] = b < a.B ? c : 0;
-  }
+  if (part == 0 && b < a.B) s_prob[b] = p, s_count[b] = c;
   __syncthreads();
-  const int total_routed = a.counts[a.B];
-  if (threadIdx.x < 32) {
-    double dot = 0.0;
-    int64_t total = 0;
-    for (int i = threadIdx.x; i < cols; i += 32) {
-      dot += static_cast<double>(s_count[i]) * static_cast<double>(s_prob[i]);
-      total += s_count[i];
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
-      total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
-    }
-    if (threadIdx.x == 0)
-      a.loss[0] = total > 0 ? static_cast<float>(s_avail * dot / (static_cast<double>(total) * total_routed)) : 0.0f;
-  }
-  if (part == 0 && b < a.B) a.prob[b] = total_routed > 0 ? p / static_cast<float>(total_routed) : 0.0f;
+  route_outputs(a, s_prob, s_count, &s_routed);
 }
 
+// f is taken less the mean count, which changes nothing where the probabilities sum to 1 and keeps the difference exact
+// where the load is nearly even (all counts equal: the gradient is 0).
 template <typename T, int LPR, int VPT, bool VEC>
-__global__ void __launch_bounds__(kRouteThreads) route_backward_kernel(const __grid_constant__ RouteArgs a) {
-  constexpr int kWarps = kRouteThreads / 32, kRows = 32 / LPR;
-  ptx::griddep_launch_dependents();
+__global__ void __launch_bounds__(kBackwardThreads) route_backward_kernel(const __grid_constant__ RouteArgs a) {
+  constexpr int kWarps = kBackwardThreads / 32, kSegs = 32 / LPR, R = kBackwardRows;
   ptx::griddep_wait();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int seg = lane / LPR, l = lane % LPR, c0 = l * VPT;
   const uint32_t avail_mask = avail_mask_of<VPT>(a.avail, c0, a.B);
-  // f of the lane's columns, and the factor grad_loss B' / T
-  int total = 0, n_avail = 0;
-  float f[VPT];
+  int total = 0, n_avail = __popc(avail_mask), cnt[VPT];
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
-    const int c = c0 + i < a.B ? a.counts_in[c0 + i] : 0;
-    f[i] = static_cast<float>(c);
-    total += c;
+    cnt[i] = c0 + i < a.B ? a.counts_in[c0 + i] : 0;
+    total += cnt[i];
   }
-  n_avail = __popc(avail_mask);
 #pragma unroll
   for (int o = LPR / 2; o > 0; o >>= 1) {
     total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
     n_avail += __shfl_xor_sync(0xFFFFFFFFu, n_avail, o);
   }
-  const int routed = a.counts_in[a.B];
+  const int routed = a.counts_in[a.B], mean = n_avail > 0 ? total / n_avail : 0;
+  float f[VPT];
 #pragma unroll
-  for (int i = 0; i < VPT; ++i) f[i] = total > 0 ? f[i] / static_cast<float>(total) : 0.0f;
+  for (int i = 0; i < VPT; ++i) f[i] = total > 0 ? static_cast<float>(cnt[i] - mean) / static_cast<float>(total) : 0.0f;
   const float g = a.grad_loss != nullptr ? a.grad_loss[0] : 1.0f;
   const float scale = routed > 0 ? g * static_cast<float>(n_avail) / static_cast<float>(routed) : 0.0f;
 
-  const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps * kRows;
-  for (int64_t base = (static_cast<int64_t>(blockIdx.x) * kWarps + warp) * kRows; base < a.n; base += step) {
-    const int64_t t = base + seg;
-    const bool live = t < a.n && (a.valid == nullptr || a.valid[t] != 0);
-    float x[VPT];
-    load_row<T, VPT, VEC>(static_cast<const T*>(a.logits) + (t < a.n ? t : 0) * a.stride, c0, a.B, avail_mask, live, x);
-    float m = x[0];
+  const int64_t step = static_cast<int64_t>(gridDim.x) * kWarps * kSegs * R;
+  for (int64_t base = (static_cast<int64_t>(blockIdx.x) * kWarps + warp) * kSegs * R; base < a.n; base += step) {
+    float x[R][VPT];
 #pragma unroll
-    for (int i = 1; i < VPT; ++i) m = fmaxf(m, x[i]);
-    m = seg_max<LPR>(m);
-    float sum = 0.0f, dot = 0.0f;
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      x[i] = x[i] > -INFINITY ? expf(x[i] - m) : 0.0f;
-      sum += x[i];
-      dot += x[i] * f[i];
+    for (int r = 0; r < R; ++r) {
+      const int64_t t = base + r * kSegs + seg;
+      const bool live = t < a.n && (a.valid == nullptr || a.valid[t] != 0);
+      load_row<T, VPT, VEC>(static_cast<const T*>(a.logits) + (t < a.n ? t : 0) * a.stride, c0, a.B, avail_mask, live, x[r]);
     }
-    sum = seg_sum<LPR>(sum);
-    dot = seg_sum<LPR>(dot);
-    const float inv = m > -INFINITY ? 1.0f / sum : 0.0f;
-    const float mean_f = dot * inv, c = scale * inv;
-    if (t >= a.n) continue;
-    T* out = static_cast<T*>(a.grad) + t * a.grad_stride + c0;
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) x[i] = c * x[i] * (f[i] - mean_f);
-    if (VEC) {
+    for (int r = 0; r < R; ++r) {
+      float m = x[r][0];
 #pragma unroll
-      for (int i = 0; i < VPT; i += 4) {
-        if (c0 + i >= a.B) continue;
-        if (sizeof(T) == 4) {
-          *reinterpret_cast<float4*>(out + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
-        } else {
-          const __nv_bfloat162 lo = __floats2bfloat162_rn(x[i], x[i + 1]), hi = __floats2bfloat162_rn(x[i + 2], x[i + 3]);
-          *reinterpret_cast<uint2*>(out + i) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-        }
+      for (int i = 1; i < VPT; ++i) m = fmaxf(m, x[r][i]);
+      m = seg_max<LPR>(m);
+      const bool any = m > -INFINITY;
+      const float top = any ? m : 0.0f;
+      float sum = 0.0f, dot = 0.0f;
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        x[r][i] = expf(x[r][i] - top);
+        sum += x[r][i];
+        dot += x[r][i] * f[i];
       }
-    } else {
+      sum = seg_sum<LPR>(sum);
+      dot = seg_sum<LPR>(dot);
+      const float inv = any ? 1.0f / sum : 0.0f;
+      const float mean_f = dot * inv, c = scale * inv;
+      const int64_t t = base + r * kSegs + seg;
+      if (t >= a.n) continue;
+      T* out = static_cast<T*>(a.grad) + t * a.grad_stride + c0;
 #pragma unroll
-      for (int i = 0; i < VPT; ++i)
-        if (c0 + i < a.B) out[i] = static_cast<T>(x[i]);
+      for (int i = 0; i < VPT; ++i) x[r][i] = c * x[r][i] * (f[i] - mean_f);
+      if (VEC) {
+#pragma unroll
+        for (int i = 0; i < VPT; i += 4) {
+          if (c0 + i >= a.B) continue;
+          if (sizeof(T) == 4) {
+            *reinterpret_cast<float4*>(out + i) = make_float4(x[r][i], x[r][i + 1], x[r][i + 2], x[r][i + 3]);
+          } else {
+            const __nv_bfloat162 lo = __floats2bfloat162_rn(x[r][i], x[r][i + 1]), hi = __floats2bfloat162_rn(x[r][i + 2], x[r][i + 3]);
+            *reinterpret_cast<uint2*>(out + i) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+          if (c0 + i < a.B) out[i] = static_cast<T>(x[r][i]);
+      }
     }
   }
 }
@@ -367,18 +452,24 @@ int lanes_per_row(int B) {
   return lanes;
 }
 
-// Blocks for n rows, at most `most`: the rest of the rows in further turns of the same blocks.
-unsigned row_blocks(int64_t n, int B, int most) {
-  const int64_t rows = 32 / lanes_per_row(B) * (kRouteThreads / 32);
+// Blocks of the forward: one as long as its warps have at most four turns each (the sums need no second launch then).
+int forward_blocks(int64_t n, int B) {
+  const int64_t rows = 32 / lanes_per_row(B) * kRouteRows * kRouteWarps;
   const int64_t need = (n + rows - 1) / rows;
-  return static_cast<unsigned>(need < most ? need : most);
+  return need <= 4 ? 1 : static_cast<int>(need < kRouteCtas ? need : kRouteCtas);
+}
+int backward_blocks(int64_t n, int B) {
+  const int64_t rows = 32 / lanes_per_row(B) * kBackwardRows * (kBackwardThreads / 32);
+  const int64_t need = (n + rows - 1) / rows;
+  return static_cast<int>(need < kBackwardCtas ? need : kBackwardCtas);
 }
 
 template <typename T, int LPR, int VPT, bool VEC>
 cudaError_t launch_op(Op op, const RouteArgs& a, cudaStream_t st) {
   if (op == FORWARD)
-    return launch_pdl(route_kernel<T, LPR, VPT, VEC>, dim3(row_blocks(a.n, a.B, kRouteCtas)), dim3(kRouteThreads), 0, st, a);
-  return launch_pdl(route_backward_kernel<T, LPR, VPT, VEC>, dim3(row_blocks(a.n, a.B, kBackwardCtas)), dim3(kRouteThreads), 0, st, a);
+    return launch_pdl(route_kernel<T, LPR, VPT, VEC>, dim3(static_cast<unsigned>(forward_blocks(a.n, a.B))), dim3(kRouteThreads), 0, st, a);
+  return launch_pdl(route_backward_kernel<T, LPR, VPT, VEC>, dim3(static_cast<unsigned>(backward_blocks(a.n, a.B))), dim3(kBackwardThreads),
+                    0, st, a);
 }
 
 template <typename T, bool VEC>
@@ -453,10 +544,11 @@ mlpmoe_status_t mlpmoe_route(const void* logits, mlpmoe_dtype_t dtype, int64_t s
   pdl_overlap_enabled() = true;
   int n_partial = 0;
   if (n_tokens > 0) {
-    n_partial = static_cast<int>(row_blocks(n_tokens, B, kRouteCtas));
+    n_partial = forward_blocks(n_tokens, B);
     if (launch_any(FORWARD, a, dtype, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
   }
-  if (launch_pdl(route_finish_kernel, dim3(1), dim3(kFinishThreads), 0, st, a, n_partial) != cudaSuccess) return MLPMOE_ERR_CUDA;
+  if (n_partial != 1 && launch_pdl(route_finish_kernel, dim3(1), dim3(kRouteThreads), 0, st, a, n_partial) != cudaSuccess)
+    return MLPMOE_ERR_CUDA;
   return MLPMOE_OK;
 }
 

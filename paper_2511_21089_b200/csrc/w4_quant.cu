@@ -1,6 +1,7 @@
 // Weights to 4-bit codes with group scales, and back (mlpmoe_w4_quantize, mlpmoe_w4_dequantize).  Both are bound by
-// the dense matrix they read or write; a block takes a tile of 32 rows x 128 columns, a warp one row of it at a time
-// with four neighbouring columns per lane, so a group of 32, 64 or 128 columns is 8, 16 or 32 lanes.
+// the dense matrix they read or write.  A block takes a tile of 32 rows x 256 columns, a warp four neighbouring rows of
+// it with eight neighbouring columns per lane and row, all loads under way before the first use; a group of 32, 64 or
+// 128 columns is 4, 8 or 16 lanes.
 #include "../../include/mlpmoe.h"
 #include "internal.h"
 #include "w4.h"
@@ -8,7 +9,7 @@
 namespace mlpmoe {
 namespace {
 
-constexpr int kRows = 32, kCols = 128, kThreads = 256;
+constexpr int kRows = 32, kCols = 256, kThreads = 256, kWarpRows = 4;
 constexpr int64_t kMaxDim = int64_t(1) << 20;      // keeps the grid within its limits
 
 struct QuantArgs {
@@ -22,9 +23,42 @@ struct QuantArgs {
 };
 
 template <typename T>
-__device__ __forceinline__ float to_f32(T v) { return static_cast<float>(v); }
+__device__ __forceinline__ void load_eight(const T* p, float (&v)[8]) {
+  if (sizeof(T) == 4) {
+    const float4 lo = reinterpret_cast<const float4*>(p)[0], hi = reinterpret_cast<const float4*>(p)[1];
+    v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w, v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+  } else {
+    const uint4 w = *reinterpret_cast<const uint4*>(p);
+    v[0] = __uint_as_float(w.x << 16), v[1] = __uint_as_float(w.x & 0xFFFF0000u), v[2] = __uint_as_float(w.y << 16),
+    v[3] = __uint_as_float(w.y & 0xFFFF0000u), v[4] = __uint_as_float(w.z << 16), v[5] = __uint_as_float(w.z & 0xFFFF0000u),
+    v[6] = __uint_as_float(w.w << 16), v[7] = __uint_as_float(w.w & 0xFFFF0000u);
+  }
+}
+template <typename T>
+__device__ __forceinline__ void store_eight(T* p, const float (&v)[8]) {
+  if (sizeof(T) == 4) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+  } else {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// rint(v / div), correctly rounded twice as the definition says: from v * (1 / div), off by at most 2^-22 of 16, unless
+// that is within 2^-13 of a half.
+__device__ __forceinline__ float rint_quotient(float v, float div, float inv) {
+  const float r = v * inv, q = rintf(r);
+  return fabsf(r - q) > 0.4998f ? rintf(v / div) : q;
+}
 
 // PAPER: the source is [cols x rows]; the tile goes through shared memory so that both sides are read along memory.
+// VEC: cols % 8 == 0 and rows on 16 bytes.
 template <typename T, bool PAPER, bool VEC>
 __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const __grid_constant__ QuantArgs a) {
   __shared__ float tile[PAPER ? kRows * (kCols + 1) : 1];
@@ -34,52 +68,51 @@ __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const __grid_cons
   if (PAPER) {
     for (int i = threadIdx.x; i < kRows * kCols; i += kThreads) {
       const int64_t r = r0 + i % kRows, c = c0 + i / kRows;
-      tile[(i % kRows) * (kCols + 1) + i / kRows] = r < a.rows && c < a.cols ? to_f32(w[c * a.stride + r]) : 0.0f;
+      tile[(i % kRows) * (kCols + 1) + i / kRows] = r < a.rows && c < a.cols ? static_cast<float>(w[c * a.stride + r]) : 0.0f;
     }
     __syncthreads();
   }
-  const int lanes = a.group / 4;
-  const int64_t col = c0 + 4 * lane;
-  for (int i = warp; i < kRows; i += kThreads / 32) {
-    const int64_t r = r0 + i;
-    if (r >= a.rows) break;
-    float v[4];
+  const int lanes = a.group / 8;
+  const int64_t col = c0 + 8 * lane, row0 = r0 + warp * kWarpRows;
+  float v[kWarpRows][8];
+#pragma unroll
+  for (int i = 0; i < kWarpRows; ++i) {
+    const int64_t r = row0 + i;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
     if (PAPER) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = tile[i * (kCols + 1) + 4 * lane + j];
-    } else if (VEC) {                       // cols % 4 == 0, rows on 16 (fp32) or 8 (bf16) bytes
-      v[0] = v[1] = v[2] = v[3] = 0.0f;
-      if (col < a.cols) {
-        if (sizeof(T) == 4) {
-          const float4 u = *reinterpret_cast<const float4*>(w + r * a.stride + col);
-          v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
-        } else {
-          const uint2 u = *reinterpret_cast<const uint2*>(w + r * a.stride + col);
-          v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xFFFF0000u);
-          v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xFFFF0000u);
-        }
-      }
-    } else {
+      for (int j = 0; j < 8; ++j) v[i][j] = tile[(warp * kWarpRows + i) * (kCols + 1) + 8 * lane + j];
+    } else if (VEC) {
+      if (r < a.rows && col < a.cols) load_eight(w + r * a.stride + col, v[i]);
+    } else if (r < a.rows) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = col + j < a.cols ? to_f32(w[r * a.stride + col + j]) : 0.0f;
+      for (int j = 0; j < 8; ++j)
+        if (col + j < a.cols) v[i][j] = static_cast<float>(w[r * a.stride + col + j]);
     }
-    float lo = fminf(fminf(v[0], v[1]), fminf(v[2], v[3])), hi = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+  }
+#pragma unroll
+  for (int i = 0; i < kWarpRows; ++i) {
+    const int64_t r = row0 + i;
+    float lo = 0.0f, hi = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) lo = fminf(lo, v[i][j]), hi = fmaxf(hi, v[i][j]);
     for (int o = 1; o < lanes; o *= 2) {
       lo = fminf(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, o));
       hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, o));
     }
-    lo = fminf(lo, 0.0f);
-    hi = fmaxf(hi, 0.0f);
     // the scale is rounded to bf16 (2 bytes per group) before the codes are made, so the codes fit the scale that is stored
     const __nv_bfloat16 sb = __float2bfloat16_rn(a.zero != nullptr ? (hi - lo) / 15.0f : fmaxf(-lo, hi) / 7.0f);
     const float s = __bfloat162float(sb);
-    const float div = s > 0.0f ? s : 1.0f;
+    const float div = s > 0.0f ? s : 1.0f, inv = 1.0f / div;
     const float z = a.zero != nullptr ? fminf(fmaxf(rintf(-lo / div), 0.0f), 15.0f) : 8.0f;
     uint32_t code = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (col + j < a.cols) code |= static_cast<uint32_t>(fminf(fmaxf(rintf(v[j] / div) + z, 0.0f), 15.0f)) << (4 * j);
-    if (col / 2 < a.pitch) *reinterpret_cast<uint16_t*>(a.q + r * a.pitch + col / 2) = static_cast<uint16_t>(code);
+    for (int j = 0; j < 8; ++j)
+      if (VEC || col + j < a.cols) code |= static_cast<uint32_t>(fminf(fmaxf(rint_quotient(v[i][j], div, inv) + z, 0.0f), 15.0f)) << (4 * j);
+    if (r >= a.rows) continue;
+    if (VEC && col >= a.cols) code = 0;
+    if (col / 2 < a.pitch) *reinterpret_cast<uint32_t*>(a.q + r * a.pitch + col / 2) = code;
     if (lane % lanes == 0 && col < a.cols) {
       const int64_t at = col / a.group * a.rows16 + r;
       a.scale[at] = sb;
@@ -94,35 +127,32 @@ __global__ void __launch_bounds__(kThreads) w4_dequantize_kernel(const __grid_co
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int64_t r0 = static_cast<int64_t>(blockIdx.y) * kRows, c0 = static_cast<int64_t>(blockIdx.x) * kCols;
   T* w = static_cast<T*>(a.w_out);
-  const int64_t col = c0 + 4 * lane;
-  for (int i = warp; i < kRows; i += kThreads / 32) {
-    const int64_t r = r0 + i;
-    if (r >= a.rows) break;
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (col < a.cols) {
-      const uint32_t code = *reinterpret_cast<const uint16_t*>(a.q + r * a.pitch + col / 2);
-      const int64_t at = col / a.group * a.rows16 + r;
-      const float s = __bfloat162float(a.scale[at]);
-      const int z = a.zero != nullptr ? a.zero[at] : 8;
+  const int64_t col = c0 + 8 * lane, row0 = r0 + warp * kWarpRows;
+  uint32_t code[kWarpRows];
+  float s[kWarpRows];
+  int z[kWarpRows];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[j] = static_cast<float>(static_cast<int>((code >> (4 * j)) & 15u) - z) * s;
-    }
+  for (int i = 0; i < kWarpRows; ++i) {
+    const int64_t r = row0 + i, at = col / a.group * a.rows16 + r;
+    const bool in = r < a.rows && col < a.cols;
+    code[i] = in ? *reinterpret_cast<const uint32_t*>(a.q + r * a.pitch + col / 2) : 0u;
+    s[i] = in ? __bfloat162float(a.scale[at]) : 0.0f;
+    z[i] = in && a.zero != nullptr ? a.zero[at] : 8;
+  }
+#pragma unroll
+  for (int i = 0; i < kWarpRows; ++i) {
+    const int64_t r = row0 + i;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<int>((code[i] >> (4 * j)) & 15u) - z[i]) * s[i];
     if (PAPER) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) tile[i * (kCols + 1) + 4 * lane + j] = v[j];
+      for (int j = 0; j < 8; ++j) tile[(warp * kWarpRows + i) * (kCols + 1) + 8 * lane + j] = v[j];
     } else if (VEC) {
-      if (col < a.cols) {
-        if (sizeof(T) == 4) {
-          *reinterpret_cast<float4*>(w + r * a.stride + col) = make_float4(v[0], v[1], v[2], v[3]);
-        } else {
-          const __nv_bfloat162 x = __floats2bfloat162_rn(v[0], v[1]), y = __floats2bfloat162_rn(v[2], v[3]);
-          *reinterpret_cast<uint2*>(w + r * a.stride + col) =
-              make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-        }
-      }
-    } else {
+      if (r < a.rows && col < a.cols) store_eight(w + r * a.stride + col, v);
+    } else if (r < a.rows) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < 8; ++j)
         if (col + j < a.cols) w[r * a.stride + col + j] = static_cast<T>(v[j]);
     }
   }
@@ -177,7 +207,7 @@ mlpmoe_status_t run(bool back, const void* W, mlpmoe_dtype_t dtype, mlpmoe_layou
   a.rows16 = w4_rows16(rows);
   a.pitch = w4_pitch(cols);
   a.group = group;
-  const bool vec = cols % 4 == 0 && stride % 4 == 0 && on(W, 4 * elem);
+  const bool vec = cols % 8 == 0 && stride % 8 == 0 && on(W, 16);
   const bool paper = layout == MLPMOE_LAYOUT_PAPER;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = dtype == MLPMOE_FP32 ? launch<float>(back, paper, vec, a, st) : launch<__nv_bfloat16>(back, paper, vec, a, st);
