@@ -11,7 +11,7 @@
 namespace mlpmoe {
 namespace {
 
-constexpr int kNone = 2;   // r_kind beside MLPMOE_BF16 (0) and MLPMOE_FP32 (1)
+constexpr int kNone = 2;   // no residual, beside MLPMOE_BF16 (0) and MLPMOE_FP32 (1)
 constexpr float kE4m3Max = 448.0f;
 constexpr float kScaleMin = 1.17549435e-38f;   // 2^-126: keeps 1 / scale finite; a group of zeros gets it too
 
@@ -23,7 +23,7 @@ struct NormArgs {
   void* out;
   float* scales;
   int64_t x_stride, r_stride, x_out_stride, out_stride, n;
-  int d, r_kind, group;   // group: columns per scale, d for one per row
+  int d, group;   // group: columns per scale, d for one per row
   float eps;
 };
 
@@ -34,28 +34,48 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// Eight consecutive elements from column col (VEC: the row starts on 16 bytes and d % 8 == 0, so a chunk is whole).
+// Eight consecutive elements from column col, as they stand in memory (fp32: the whole of a and b; bf16: a), zeros past the
+// row's end.  VEC: the row starts on 16 bytes and d % 8 == 0, so a chunk is whole.
+struct Chunk {
+  uint4 a, b;
+};
 template <bool VEC>
-__device__ __forceinline__ void load8(const void* row, int kind, int col, int d, float (&v)[8]) {
+__device__ __forceinline__ Chunk load_chunk(const void* row, int kind, int col, int d) {
+  Chunk c;
+  c.a = c.b = make_uint4(0u, 0u, 0u, 0u);
+  if (col >= d) return c;
   if (kind == MLPMOE_FP32) {
-    const float* p = static_cast<const float*>(row) + col;
+    const uint32_t* p = static_cast<const uint32_t*>(row) + col;
     if (VEC) {
-      const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+      c.a = reinterpret_cast<const uint4*>(p)[0];
+      c.b = reinterpret_cast<const uint4*>(p)[1];
     } else {
+      uint32_t w[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = col + i < d ? p[i] : 0.0f;
+      for (int i = 0; i < 8; ++i) w[i] = col + i < d ? p[i] : 0u;
+      c.a = make_uint4(w[0], w[1], w[2], w[3]);
+      c.b = make_uint4(w[4], w[5], w[6], w[7]);
     }
   } else {
-    const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(row) + col;
+    const uint16_t* p = static_cast<const uint16_t*>(row) + col;
     if (VEC) {
-      const uint4 a = *reinterpret_cast<const uint4*>(p);
-      v[0] = bf16_lo(a.x), v[1] = bf16_hi(a.x), v[2] = bf16_lo(a.y), v[3] = bf16_hi(a.y);
-      v[4] = bf16_lo(a.z), v[5] = bf16_hi(a.z), v[6] = bf16_lo(a.w), v[7] = bf16_hi(a.w);
+      c.a = *reinterpret_cast<const uint4*>(p);
     } else {
+      uint32_t w[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = col + i < d ? __bfloat162float(p[i]) : 0.0f;
+      for (int i = 0; i < 8; ++i) w[i] = col + i < d ? p[i] : 0u;
+      c.a = make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4] | (w[5] << 16), w[6] | (w[7] << 16));
     }
+  }
+  return c;
+}
+__device__ __forceinline__ void to_f32(const Chunk& c, int kind, float (&v)[8]) {
+  if (kind == MLPMOE_FP32) {
+    v[0] = __uint_as_float(c.a.x), v[1] = __uint_as_float(c.a.y), v[2] = __uint_as_float(c.a.z), v[3] = __uint_as_float(c.a.w);
+    v[4] = __uint_as_float(c.b.x), v[5] = __uint_as_float(c.b.y), v[6] = __uint_as_float(c.b.z), v[7] = __uint_as_float(c.b.w);
+  } else {
+    v[0] = bf16_lo(c.a.x), v[1] = bf16_hi(c.a.x), v[2] = bf16_lo(c.a.y), v[3] = bf16_hi(c.a.y);
+    v[4] = bf16_lo(c.a.z), v[5] = bf16_hi(c.a.z), v[6] = bf16_lo(c.a.w), v[7] = bf16_hi(c.a.w);
   }
 }
 
@@ -116,7 +136,7 @@ __device__ __forceinline__ float row_reduce(float v, float* red) {
 
 // One row per T threads (T = 32: eight rows to a block), NCH chunks of eight consecutive columns per thread.
 // A group of 32, 64 or 128 columns lies in 4, 8 or 16 neighbouring lanes of one warp, so its maximum is a few shuffles.
-template <int XKIND, int OKIND, bool VEC, int T, int NCH>
+template <int XKIND, int RKIND, int OKIND, bool VEC, int T, int NCH>
 __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float red[32];
   ptx::griddep_launch_dependents();
@@ -127,35 +147,27 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
   constexpr int kXBytes = XKIND == MLPMOE_FP32 ? 4 : 2;
   constexpr int kOBytes = OKIND == MLPMOE_FP32 ? 4 : (OKIND == MLPMOE_BF16 ? 2 : 1);
   const char* xrow = static_cast<const char*>(a.x) + t * a.x_stride * kXBytes;
-  const char* rrow = static_cast<const char*>(a.r) + t * a.r_stride * (a.r_kind == MLPMOE_FP32 ? 4 : 2);
+  const char* rrow = static_cast<const char*>(a.r) + t * a.r_stride * (RKIND == MLPMOE_FP32 ? 4 : 2);
   const int d = a.d;
   float s[NCH][8];
+  {
+    Chunk x[NCH], r[NCH];               // all of the row's loads before the first use
 #pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    const int col = (i * T + tid) * 8;
-    if (col < d) {
-      load8<VEC>(xrow, XKIND, col, d, s[i]);
-    } else {
+    for (int i = 0; i < NCH; ++i) x[i] = load_chunk<VEC>(xrow, XKIND, (i * T + tid) * 8, d);
+    if (RKIND != kNone) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s[i][j] = 0.0f;
+      for (int i = 0; i < NCH; ++i) r[i] = load_chunk<VEC>(rrow, RKIND, (i * T + tid) * 8, d);
     }
-  }
-  if (a.r_kind != kNone) {
-    float r[NCH][8];
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      const int col = (i * T + tid) * 8;
-      if (col < d) {
-        load8<VEC>(rrow, a.r_kind, col, d, r[i]);
-      } else {
+      to_f32(x[i], XKIND, s[i]);
+      if (RKIND != kNone) {
+        float v[8];
+        to_f32(r[i], RKIND, v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r[i][j] = 0.0f;
+        for (int j = 0; j < 8; ++j) s[i][j] += v[j];
       }
     }
-#pragma unroll
-    for (int i = 0; i < NCH; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[i][j] += r[i][j];
   }
   float ss = 0.0f;
 #pragma unroll
@@ -177,8 +189,8 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
   for (int i = 0; i < NCH; ++i) {
     const int col = (i * T + tid) * 8;
     float g[8];
-    if (a.gain != nullptr && col < d) {
-      load8<VEC>(a.gain, MLPMOE_FP32, col, d, g);
+    if (a.gain != nullptr) {
+      to_f32(load_chunk<VEC>(a.gain, MLPMOE_FP32, col, d), MLPMOE_FP32, g);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) g[j] = 1.0f;
@@ -228,28 +240,35 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
   }
 }
 
-template <int XKIND, int OKIND, bool VEC>
+template <int XKIND, int RKIND, int OKIND, bool VEC>
 cudaError_t launch_shape(const NormArgs& a, cudaStream_t st) {
   const unsigned n = static_cast<unsigned>(a.n);
   if (a.d <= 1024 && a.n > 296)
-    return launch_pdl(add_norm_kernel<XKIND, OKIND, VEC, 32, 4>, dim3((n + 7) / 8), dim3(256), 0, st, a);
-  if (a.d <= 1024) return launch_pdl(add_norm_kernel<XKIND, OKIND, VEC, 128, 1>, dim3(n), dim3(128), 0, st, a);
-  if (a.d <= 4096 && a.n > 296) return launch_pdl(add_norm_kernel<XKIND, OKIND, VEC, 128, 4>, dim3(n), dim3(128), 0, st, a);
-  if (a.d <= 4096) return launch_pdl(add_norm_kernel<XKIND, OKIND, VEC, 512, 1>, dim3(n), dim3(512), 0, st, a);
-  if (a.d <= 8192) return launch_pdl(add_norm_kernel<XKIND, OKIND, VEC, 512, 2>, dim3(n), dim3(512), 0, st, a);
-  return launch_pdl(add_norm_kernel<XKIND, OKIND, VEC, 1024, 4>, dim3(n), dim3(1024), 0, st, a);
+    return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 32, 4>, dim3((n + 7) / 8), dim3(256), 0, st, a);
+  if (a.d <= 1024) return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 128, 1>, dim3(n), dim3(128), 0, st, a);
+  if (a.d <= 4096 && a.n > 296) return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 128, 4>, dim3(n), dim3(128), 0, st, a);
+  if (a.d <= 4096) return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 512, 1>, dim3(n), dim3(512), 0, st, a);
+  if (a.d <= 8192) return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 512, 2>, dim3(n), dim3(512), 0, st, a);
+  return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 1024, 4>, dim3(n), dim3(1024), 0, st, a);
 }
 
-template <int XKIND, int OKIND>
+template <int XKIND, int RKIND, int OKIND>
 cudaError_t launch_vec(const NormArgs& a, bool vec, cudaStream_t st) {
-  return vec ? launch_shape<XKIND, OKIND, true>(a, st) : launch_shape<XKIND, OKIND, false>(a, st);
+  return vec ? launch_shape<XKIND, RKIND, OKIND, true>(a, st) : launch_shape<XKIND, RKIND, OKIND, false>(a, st);
+}
+
+template <int XKIND, int RKIND>
+cudaError_t launch_out(const NormArgs& a, int out_kind, bool vec, cudaStream_t st) {
+  if (out_kind == MLPMOE_FP32) return launch_vec<XKIND, RKIND, MLPMOE_FP32>(a, vec, st);
+  if (out_kind == MLPMOE_BF16) return launch_vec<XKIND, RKIND, MLPMOE_BF16>(a, vec, st);
+  return launch_vec<XKIND, RKIND, MLPMOE_E4M3>(a, vec, st);
 }
 
 template <int XKIND>
-cudaError_t launch_out(const NormArgs& a, int out_kind, bool vec, cudaStream_t st) {
-  if (out_kind == MLPMOE_FP32) return launch_vec<XKIND, MLPMOE_FP32>(a, vec, st);
-  if (out_kind == MLPMOE_BF16) return launch_vec<XKIND, MLPMOE_BF16>(a, vec, st);
-  return launch_vec<XKIND, MLPMOE_E4M3>(a, vec, st);
+cudaError_t launch_residual(const NormArgs& a, int r_kind, int out_kind, bool vec, cudaStream_t st) {
+  if (r_kind == MLPMOE_FP32) return launch_out<XKIND, MLPMOE_FP32>(a, out_kind, vec, st);
+  if (r_kind == MLPMOE_BF16) return launch_out<XKIND, MLPMOE_BF16>(a, out_kind, vec, st);
+  return launch_out<XKIND, kNone>(a, out_kind, vec, st);
 }
 
 inline bool on(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
@@ -297,11 +316,12 @@ extern "C" mlpmoe_status_t mlpmoe_add_rmsnorm(const void* x, mlpmoe_dtype_t x_dt
   a.out_stride = out_stride;
   a.n = n_tokens;
   a.d = static_cast<int>(d_model);
-  a.r_kind = r ? static_cast<int>(r_dtype) : kNone;
   a.group = group == 0 ? static_cast<int>(d_model) : static_cast<int>(group);
   a.eps = eps;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int r_kind = r ? static_cast<int>(r_dtype) : kNone;
   pdl_overlap_enabled() = true;
-  const cudaError_t e = x_dtype == MLPMOE_FP32 ? launch_out<MLPMOE_FP32>(a, out_dtype, vec, st) : launch_out<MLPMOE_BF16>(a, out_dtype, vec, st);
+  const cudaError_t e = x_dtype == MLPMOE_FP32 ? launch_residual<MLPMOE_FP32>(a, r_kind, out_dtype, vec, st)
+                                               : launch_residual<MLPMOE_BF16>(a, r_kind, out_dtype, vec, st);
   return e == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
 }

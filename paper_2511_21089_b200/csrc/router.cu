@@ -18,7 +18,7 @@ constexpr int kRouteWarps = kRouteThreads / 32;
 constexpr int kRouteCtas = 148;
 constexpr int kRouteRows = 2;          // rows of a segment at a time: two chains of exchanges in flight
 constexpr int kBackwardThreads = 256;
-constexpr int kBackwardCtas = 148 * 8;
+constexpr int kBackwardCtas = 148 * 6;   // all resident
 constexpr int kBackwardRows = 2;
 
 // One block's contribution: B probability sums, then B counts and the number of routed tokens as int32.
@@ -195,26 +195,25 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_const
 #pragma unroll
       for (int i = 0; i < VPT; ++i) prob[i] += e[i] * inv;
       routed += any && l == 0 ? 1 : 0;
-      taken[r] = any ? 0 : a.k;
+      taken[r] = 0;
       least[r] = INFINITY;
     }
+    // k turns always: a row that has its k earlier, or nothing left (every lane then offers -infinity), only goes on
+    // without effect
     for (int turn = 0; turn < a.k; ++turn) {
-      bool more = false;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const float top = seg_max<LPR>(s[r][0]);
-        const bool hit = s[r][0] == top && top > -INFINITY && taken[r] < a.k;
+        const bool hit = s[r][0] == top;
         const uint32_t who = __ballot_sync(0xFFFFFFFFu, hit) & seg_lanes;
-        if (who != 0u) least[r] = top;
+        if (taken[r] < a.k) least[r] = top;
         taken[r] += __popc(who);
         if (hit) {
 #pragma unroll
           for (int i = 0; i + 1 < VPT; ++i) s[r][i] = s[r][i + 1];
           s[r][VPT - 1] = -INFINITY;
         }
-        more = more || (who != 0u && taken[r] < a.k);
       }
-      if (!__any_sync(0xFFFFFFFFu, more)) break;
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -222,7 +221,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const __grid_const
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
         above |= x[r][i] > least[r] ? 1u << i : 0u;
-        equal |= x[r][i] == least[r] ? 1u << i : 0u;
+        equal |= x[r][i] == least[r] && x[r][i] > -INFINITY ? 1u << i : 0u;
       }
       // equals: as many as are wanted, the first in index order (columns ascend with the lane)
       int n_above = __popc(above), n_equal = __popc(equal);
@@ -366,7 +365,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_finish_kernel(const __gri
 // f is taken less the mean count, which changes nothing where the probabilities sum to 1 and keeps the difference exact
 // where the load is nearly even (all counts equal: the gradient is 0).
 template <typename T, int LPR, int VPT, bool VEC>
-__global__ void __launch_bounds__(kBackwardThreads) route_backward_kernel(const __grid_constant__ RouteArgs a) {
+__global__ void __launch_bounds__(kBackwardThreads, VPT == 4 ? 6 : 4) route_backward_kernel(const __grid_constant__ RouteArgs a) {
   constexpr int kWarps = kBackwardThreads / 32, kSegs = 32 / LPR, R = kBackwardRows;
   ptx::griddep_wait();
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;

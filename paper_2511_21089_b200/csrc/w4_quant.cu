@@ -50,11 +50,28 @@ __device__ __forceinline__ void store_eight(T* p, const float (&v)[8]) {
   }
 }
 
-// rint(v / div), correctly rounded twice as the definition says: from v * (1 / div), off by at most 2^-22 of 16, unless
-// that is within 2^-13 of a half.
-__device__ __forceinline__ float rint_quotient(float v, float div, float inv) {
-  const float r = v * inv, q = rintf(r);
-  return fabsf(r - q) > 0.4998f ? rintf(v / div) : q;
+// The codes of eight values, rint(v / div) + z between 0 and 15, four bits each.  The quotient is v * (1 / div), off by at
+// most 2^-22 of 16; only where one of the eight lies within 2^-12 of a half are they divided in full, so that the codes
+// are those of the correctly rounded quotient.  The sum with 1.5 * 2^23 rounds it and has the whole number in its low bits.
+__device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float div, float inv, int z) {
+  constexpr float kMagic = 12582912.0f;
+  float t[8], off = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    t[j] = fmaf(v[j], inv, kMagic);
+    off = fmaxf(off, fabsf(fmaf(v[j], inv, kMagic - t[j])));
+  }
+  if (off > 0.49975f) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = v[j] / div + kMagic;
+  }
+  uint32_t code = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int c = __float_as_int(t[j]) - 0x4B400000 + z;
+    code |= static_cast<uint32_t>(min(max(c, 0), 15)) << (4 * j);
+  }
+  return code;
 }
 
 // PAPER: the source is [cols x rows]; the tile goes through shared memory so that both sides are read along memory.
@@ -106,12 +123,10 @@ __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const __grid_cons
     const float s = __bfloat162float(sb);
     const float div = s > 0.0f ? s : 1.0f, inv = 1.0f / div;
     const float z = a.zero != nullptr ? fminf(fmaxf(rintf(-lo / div), 0.0f), 15.0f) : 8.0f;
-    uint32_t code = 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (VEC || col + j < a.cols) code |= static_cast<uint32_t>(fminf(fmaxf(rint_quotient(v[i][j], div, inv) + z, 0.0f), 15.0f)) << (4 * j);
+    uint32_t code = codes_of(v[i], div, inv, static_cast<int>(z));
     if (r >= a.rows) continue;
-    if (VEC && col >= a.cols) code = 0;
+    const int64_t left = a.cols - col;                 // columns past the last are coded 0
+    if (left < 8) code &= left <= 0 ? 0u : (1u << (4 * left)) - 1u;
     if (col / 2 < a.pitch) *reinterpret_cast<uint32_t*>(a.q + r * a.pitch + col / 2) = code;
     if (lane % lanes == 0 && col < a.cols) {
       const int64_t at = col / a.group * a.rows16 + r;
@@ -130,21 +145,22 @@ __global__ void __launch_bounds__(kThreads) w4_dequantize_kernel(const __grid_co
   const int64_t col = c0 + 8 * lane, row0 = r0 + warp * kWarpRows;
   uint32_t code[kWarpRows];
   float s[kWarpRows];
-  int z[kWarpRows];
+  float z[kWarpRows];
 #pragma unroll
   for (int i = 0; i < kWarpRows; ++i) {
     const int64_t r = row0 + i, at = col / a.group * a.rows16 + r;
     const bool in = r < a.rows && col < a.cols;
     code[i] = in ? *reinterpret_cast<const uint32_t*>(a.q + r * a.pitch + col / 2) : 0u;
     s[i] = in ? __bfloat162float(a.scale[at]) : 0.0f;
-    z[i] = in && a.zero != nullptr ? a.zero[at] : 8;
+    z[i] = 8388608.0f + (in && a.zero != nullptr ? static_cast<float>(a.zero[at]) : 8.0f);
   }
 #pragma unroll
   for (int i = 0; i < kWarpRows; ++i) {
     const int64_t r = row0 + i;
     float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = static_cast<float>(static_cast<int>((code[i] >> (4 * j)) & 15u) - z[i]) * s[i];
+    for (int j = 0; j < 8; ++j)                        // 2^23 + code, less 2^23 + zero: exact
+      v[j] = (__uint_as_float(((code[i] >> (4 * j)) & 15u) | 0x4B000000u) - z[i]) * s[i];
     if (PAPER) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) tile[(warp * kWarpRows + i) * (kCols + 1) + 8 * lane + j] = v[j];
