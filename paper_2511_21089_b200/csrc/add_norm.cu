@@ -84,8 +84,8 @@ __device__ __forceinline__ void store8(void* row, int kind, int col, int d, cons
   if (kind == MLPMOE_FP32) {
     float* p = static_cast<float*>(row) + col;
     if (VEC) {
-      reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+      __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+      __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -246,7 +246,7 @@ cudaError_t launch_shape(const NormArgs& a, cudaStream_t st) {
   if (a.d <= 1024 && a.n > 296)
     return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 32, 4>, dim3((n + 7) / 8), dim3(256), 0, st, a);
   if (a.d <= 1024) return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 128, 1>, dim3(n), dim3(128), 0, st, a);
-  if (a.d <= 4096 && a.n > 296) return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 128, 4>, dim3(n), dim3(128), 0, st, a);
+  if (a.d <= 4096 && a.n > 296) return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 256, 2>, dim3(n), dim3(256), 0, st, a);
   if (a.d <= 4096) return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 512, 1>, dim3(n), dim3(512), 0, st, a);
   if (a.d <= 8192) return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 512, 2>, dim3(n), dim3(512), 0, st, a);
   return launch_pdl(add_norm_kernel<XKIND, RKIND, OKIND, VEC, 1024, 4>, dim3(n), dim3(1024), 0, st, a);

@@ -19,7 +19,7 @@ struct QuantArgs {
   __nv_bfloat16* scale;
   uint8_t* zero;
   int64_t stride, rows, cols, rows16, pitch;
-  int group;
+  int log_group;
 };
 
 template <typename T>
@@ -50,34 +50,35 @@ __device__ __forceinline__ void store_eight(T* p, const float (&v)[8]) {
   }
 }
 
-// The codes of eight values, rint(v / div) + z between 0 and 15, four bits each.  The quotient is v * (1 / div), off by at
-// most 2^-22 of 16; only where one of the eight lies within 2^-12 of a half are they divided in full, so that the codes
-// are those of the correctly rounded quotient.  The sum with 1.5 * 2^23 rounds it and has the whole number in its low bits.
+// The codes of eight values, rint(v / div) + z between 0 and 15, four bits each.  The quotient is v * (1 / div), off by less
+// than 2^-20; only where that lies within 2^-17 of a half is v divided in full, so that the codes are those of the
+// correctly rounded quotient.  The sum with 1.5 * 2^23 rounds it and has the whole number in its low bits.  No code falls
+// below 0: the scale is off by 2^-9 at most, z = rint(-lo / div), and rint(lo / div) = -z.
 __device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float div, float inv, int z) {
   constexpr float kMagic = 12582912.0f;
-  float t[8], off = 0.0f;
+  float t[8], off[8], most = 0.0f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     t[j] = fmaf(v[j], inv, kMagic);
-    off = fmaxf(off, fabsf(fmaf(v[j], inv, kMagic - t[j])));
+    off[j] = fabsf(fmaf(v[j], inv, kMagic - t[j]));
+    most = fmaxf(most, off[j]);
   }
-  if (off > 0.49975f) {
+  if (most > 0.49999f) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t[j] = v[j] / div + kMagic;
+    for (int j = 0; j < 8; ++j)
+      if (off[j] > 0.49999f) t[j] = v[j] / div + kMagic;
   }
   uint32_t code = 0;
+  const int shift = z - 0x4B400000;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const int c = __float_as_int(t[j]) - 0x4B400000 + z;
-    code |= static_cast<uint32_t>(min(max(c, 0), 15)) << (4 * j);
-  }
+  for (int j = 0; j < 8; ++j) code += static_cast<uint32_t>(min(__float_as_int(t[j]) + shift, 15)) << (4 * j);
   return code;
 }
 
 // PAPER: the source is [cols x rows]; the tile goes through shared memory so that both sides are read along memory.
 // VEC: cols % 8 == 0 and rows on 16 bytes.
 template <typename T, bool PAPER, bool VEC>
-__global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const __grid_constant__ QuantArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) w4_quantize_kernel(const __grid_constant__ QuantArgs a) {
   __shared__ float tile[PAPER ? kRows * (kCols + 1) : 1];
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int64_t r0 = static_cast<int64_t>(blockIdx.y) * kRows, c0 = static_cast<int64_t>(blockIdx.x) * kCols;
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const __grid_cons
     }
     __syncthreads();
   }
-  const int lanes = a.group / 8;
+  const int lanes = 1 << (a.log_group - 3);
   const int64_t col = c0 + 8 * lane, row0 = r0 + warp * kWarpRows;
   float v[kWarpRows][8];
 #pragma unroll
@@ -108,31 +109,48 @@ __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const __grid_cons
         if (col + j < a.cols) v[i][j] = static_cast<float>(w[r * a.stride + col + j]);
     }
   }
+  float lo = 0.0f, hi = 0.0f;           // of row lane % 4 in this lane's group
+  {
+    float l[kWarpRows], h[kWarpRows];   // the group's range in each row; l negated
+#pragma unroll
+    for (int i = 0; i < kWarpRows; ++i) {
+      l[i] = h[i] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) l[i] = fmaxf(l[i], -v[i][j]), h[i] = fmaxf(h[i], v[i][j]);
+      if (a.zero == nullptr) h[i] = fmaxf(h[i], l[i]);
+    }
+    for (int o = 1; o < lanes; o *= 2) {
+#pragma unroll
+      for (int i = 0; i < kWarpRows; ++i) {
+        h[i] = fmaxf(h[i], __shfl_xor_sync(0xFFFFFFFFu, h[i], o));
+        if (a.zero != nullptr) l[i] = fmaxf(l[i], __shfl_xor_sync(0xFFFFFFFFu, l[i], o));
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kWarpRows; ++i)
+      if (lane % kWarpRows == i) lo = -l[i], hi = h[i];
+  }
+  // The divisions of a group once, in the lane of its row: the scale is rounded to bf16 (2 bytes per group) before the codes
+  // are made, so the codes fit the scale that is stored.
+  const float s_mine = __bfloat162float(__float2bfloat16_rn(a.zero != nullptr ? (hi - lo) / 15.0f : hi / 7.0f));
+  const float div_mine = s_mine > 0.0f ? s_mine : 1.0f, inv_mine = 1.0f / div_mine;
+  const float z_mine = a.zero != nullptr ? fminf(rintf(-lo / div_mine), 15.0f) : 8.0f;
+  if (lane % lanes < kWarpRows && col - 8 * (lane % lanes) < a.cols && row0 + lane % kWarpRows < a.rows) {
+    const int64_t at = (col >> a.log_group) * a.rows16 + row0 + lane % kWarpRows;
+    a.scale[at] = __float2bfloat16_rn(s_mine);
+    if (a.zero != nullptr) a.zero[at] = static_cast<uint8_t>(z_mine);
+  }
 #pragma unroll
   for (int i = 0; i < kWarpRows; ++i) {
     const int64_t r = row0 + i;
-    float lo = 0.0f, hi = 0.0f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) lo = fminf(lo, v[i][j]), hi = fmaxf(hi, v[i][j]);
-    for (int o = 1; o < lanes; o *= 2) {
-      lo = fminf(lo, __shfl_xor_sync(0xFFFFFFFFu, lo, o));
-      hi = fmaxf(hi, __shfl_xor_sync(0xFFFFFFFFu, hi, o));
-    }
-    // the scale is rounded to bf16 (2 bytes per group) before the codes are made, so the codes fit the scale that is stored
-    const __nv_bfloat16 sb = __float2bfloat16_rn(a.zero != nullptr ? (hi - lo) / 15.0f : fmaxf(-lo, hi) / 7.0f);
-    const float s = __bfloat162float(sb);
-    const float div = s > 0.0f ? s : 1.0f, inv = 1.0f / div;
-    const float z = a.zero != nullptr ? fminf(fmaxf(rintf(-lo / div), 0.0f), 15.0f) : 8.0f;
+    const int from = (lane & ~(kWarpRows - 1)) + i;
+    const float div = __shfl_sync(0xFFFFFFFFu, div_mine, from), inv = __shfl_sync(0xFFFFFFFFu, inv_mine, from);
+    const float z = __shfl_sync(0xFFFFFFFFu, z_mine, from);
     uint32_t code = codes_of(v[i], div, inv, static_cast<int>(z));
     if (r >= a.rows) continue;
     const int64_t left = a.cols - col;                 // columns past the last are coded 0
     if (left < 8) code &= left <= 0 ? 0u : (1u << (4 * left)) - 1u;
     if (col / 2 < a.pitch) *reinterpret_cast<uint32_t*>(a.q + r * a.pitch + col / 2) = code;
-    if (lane % lanes == 0 && col < a.cols) {
-      const int64_t at = col / a.group * a.rows16 + r;
-      a.scale[at] = sb;
-      if (a.zero != nullptr) a.zero[at] = static_cast<uint8_t>(z);
-    }
   }
 }
 
@@ -148,7 +166,7 @@ __global__ void __launch_bounds__(kThreads) w4_dequantize_kernel(const __grid_co
   float z[kWarpRows];
 #pragma unroll
   for (int i = 0; i < kWarpRows; ++i) {
-    const int64_t r = row0 + i, at = col / a.group * a.rows16 + r;
+    const int64_t r = row0 + i, at = (col >> a.log_group) * a.rows16 + r;
     const bool in = r < a.rows && col < a.cols;
     code[i] = in ? *reinterpret_cast<const uint32_t*>(a.q + r * a.pitch + col / 2) : 0u;
     s[i] = in ? __bfloat162float(a.scale[at]) : 0.0f;
@@ -222,7 +240,7 @@ mlpmoe_status_t run(bool back, const void* W, mlpmoe_dtype_t dtype, mlpmoe_layou
   a.cols = cols;
   a.rows16 = w4_rows16(rows);
   a.pitch = w4_pitch(cols);
-  a.group = group;
+  a.log_group = group == 32 ? 5 : (group == 64 ? 6 : 7);
   const bool vec = cols % 8 == 0 && stride % 8 == 0 && on(W, 16);
   const bool paper = layout == MLPMOE_LAYOUT_PAPER;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
