@@ -92,22 +92,25 @@ __global__ void __launch_bounds__(kThreads, 4) w4_quantize_kernel(const __grid_c
   }
   const int lanes = 1 << (a.log_group - 3);
   const int64_t col = c0 + 8 * lane, row0 = r0 + warp * kWarpRows;
+  const int rows_here = static_cast<int>(min(static_cast<int64_t>(kWarpRows), a.rows - row0));
+  const int cols_here = static_cast<int>(min(static_cast<int64_t>(8), a.cols - col));       // of this lane; 0 or less: none
   float v[kWarpRows][8];
+  const T* src = w + row0 * a.stride + col;
 #pragma unroll
   for (int i = 0; i < kWarpRows; ++i) {
-    const int64_t r = row0 + i;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[i][j] = 0.0f;
     if (PAPER) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[i][j] = tile[(warp * kWarpRows + i) * (kCols + 1) + 8 * lane + j];
     } else if (VEC) {
-      if (r < a.rows && col < a.cols) load_eight(w + r * a.stride + col, v[i]);
-    } else if (r < a.rows) {
+      if (i < rows_here && cols_here > 0) load_eight(src, v[i]);
+    } else if (i < rows_here) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (col + j < a.cols) v[i][j] = static_cast<float>(w[r * a.stride + col + j]);
+        if (j < cols_here) v[i][j] = static_cast<float>(src[j]);
     }
+    src += a.stride;
   }
   float lo = 0.0f, hi = 0.0f;           // of row lane % 4 in this lane's group
   {
@@ -135,22 +138,23 @@ __global__ void __launch_bounds__(kThreads, 4) w4_quantize_kernel(const __grid_c
   const float s_mine = __bfloat162float(__float2bfloat16_rn(a.zero != nullptr ? (hi - lo) / 15.0f : hi / 7.0f));
   const float div_mine = s_mine > 0.0f ? s_mine : 1.0f, inv_mine = 1.0f / div_mine;
   const float z_mine = a.zero != nullptr ? fminf(rintf(-lo / div_mine), 15.0f) : 8.0f;
-  if (lane % lanes < kWarpRows && col - 8 * (lane % lanes) < a.cols && row0 + lane % kWarpRows < a.rows) {
-    const int64_t at = (col >> a.log_group) * a.rows16 + row0 + lane % kWarpRows;
+  const int my_row = lane % kWarpRows;
+  if (lane % lanes < kWarpRows && col - 8 * my_row < a.cols && my_row < rows_here) {     // the group's first column is in the matrix
+    const int64_t at = (col >> a.log_group) * a.rows16 + row0 + my_row;
     a.scale[at] = __float2bfloat16_rn(s_mine);
     if (a.zero != nullptr) a.zero[at] = static_cast<uint8_t>(z_mine);
   }
+  const bool store = col / 2 < a.pitch;
+  const uint32_t keep = cols_here >= 8 ? 0xFFFFFFFFu : (cols_here <= 0 ? 0u : (1u << (4 * cols_here)) - 1u);   // columns past the last are coded 0
+  uint8_t* q = a.q + row0 * a.pitch + col / 2;
 #pragma unroll
   for (int i = 0; i < kWarpRows; ++i) {
-    const int64_t r = row0 + i;
     const int from = (lane & ~(kWarpRows - 1)) + i;
     const float div = __shfl_sync(0xFFFFFFFFu, div_mine, from), inv = __shfl_sync(0xFFFFFFFFu, inv_mine, from);
     const float z = __shfl_sync(0xFFFFFFFFu, z_mine, from);
-    uint32_t code = codes_of(v[i], div, inv, static_cast<int>(z));
-    if (r >= a.rows) continue;
-    const int64_t left = a.cols - col;                 // columns past the last are coded 0
-    if (left < 8) code &= left <= 0 ? 0u : (1u << (4 * left)) - 1u;
-    if (col / 2 < a.pitch) *reinterpret_cast<uint32_t*>(a.q + r * a.pitch + col / 2) = code;
+    const uint32_t code = codes_of(v[i], div, inv, static_cast<int>(z));
+    if (i < rows_here && store) *reinterpret_cast<uint32_t*>(q) = code & keep;
+    q += a.pitch;
   }
 }
 
@@ -161,34 +165,41 @@ __global__ void __launch_bounds__(kThreads) w4_dequantize_kernel(const __grid_co
   const int64_t r0 = static_cast<int64_t>(blockIdx.y) * kRows, c0 = static_cast<int64_t>(blockIdx.x) * kCols;
   T* w = static_cast<T*>(a.w_out);
   const int64_t col = c0 + 8 * lane, row0 = r0 + warp * kWarpRows;
+  const int rows_here = static_cast<int>(min(static_cast<int64_t>(kWarpRows), a.rows - row0));
+  const int cols_here = static_cast<int>(min(static_cast<int64_t>(8), a.cols - col));       // of this lane; 0 or less: none
+  const bool in = rows_here > 0 && cols_here > 0;
   uint32_t code[kWarpRows];
-  float s[kWarpRows];
-  float z[kWarpRows];
+  const uint8_t* q = a.q + row0 * a.pitch + col / 2;
 #pragma unroll
   for (int i = 0; i < kWarpRows; ++i) {
-    const int64_t r = row0 + i, at = (col >> a.log_group) * a.rows16 + r;
-    const bool in = r < a.rows && col < a.cols;
-    code[i] = in ? *reinterpret_cast<const uint32_t*>(a.q + r * a.pitch + col / 2) : 0u;
-    s[i] = in ? __bfloat162float(a.scale[at]) : 0.0f;
-    z[i] = 8388608.0f + (in && a.zero != nullptr ? static_cast<float>(a.zero[at]) : 8.0f);
+    code[i] = in && i < rows_here ? *reinterpret_cast<const uint32_t*>(q) : 0u;
+    q += a.pitch;
   }
+  // four rows' scales and zeros at once: rows16 covers a started four
+  const int64_t at = (col >> a.log_group) * a.rows16 + row0;
+  const uint2 sw = in ? *reinterpret_cast<const uint2*>(a.scale + at) : make_uint2(0u, 0u);
+  const uint32_t zw = in && a.zero != nullptr ? *reinterpret_cast<const uint32_t*>(a.zero + at) : 0x08080808u;
+  const float s[kWarpRows] = {__uint_as_float(sw.x << 16), __uint_as_float(sw.x & 0xFFFF0000u), __uint_as_float(sw.y << 16),
+                              __uint_as_float(sw.y & 0xFFFF0000u)};
+  T* dst = w + row0 * a.stride + col;
 #pragma unroll
   for (int i = 0; i < kWarpRows; ++i) {
-    const int64_t r = row0 + i;
     float v[8];
+    // 2^23 + code, less 2^23 + zero: exact
+    const float z = __uint_as_float(((zw >> (8 * i)) & 255u) | 0x4B000000u);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)                        // 2^23 + code, less 2^23 + zero: exact
-      v[j] = (__uint_as_float(((code[i] >> (4 * j)) & 15u) | 0x4B000000u) - z[i]) * s[i];
+    for (int j = 0; j < 8; ++j) v[j] = (__uint_as_float(((code[i] >> (4 * j)) & 15u) | 0x4B000000u) - z) * s[i];
     if (PAPER) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) tile[(warp * kWarpRows + i) * (kCols + 1) + 8 * lane + j] = v[j];
     } else if (VEC) {
-      if (r < a.rows && col < a.cols) store_eight(w + r * a.stride + col, v);
-    } else if (r < a.rows) {
+      if (in && i < rows_here) store_eight(dst, v);
+    } else if (i < rows_here) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (col + j < a.cols) w[r * a.stride + col + j] = static_cast<T>(v[j]);
+        if (j < cols_here) dst[j] = static_cast<T>(v[j]);
     }
+    dst += a.stride;
   }
   if (PAPER) {
     __syncthreads();
