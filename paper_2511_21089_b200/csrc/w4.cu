@@ -7,13 +7,14 @@
 
 namespace mlpmoe {
 
-// How a product is split.  Clusters of 1, 2, 4 or 8 blocks share K (148, 74, 33 or 15 of them are resident at once with
-// this much shared memory, as the occupancy query reports); the row tiles are cut into equal shares, one per cluster,
+// Clusters of 1, 2, 4 and 8 blocks of one SM each that are resident at once (what the occupancy query reports).
+static constexpr int kResident[4] = {148, 74, 33, 15};
+
+// How a product is split.  Clusters of 1, 2, 4 or 8 blocks share K; the row tiles are cut into equal shares, one per cluster,
 // or two or more turns of them where the sums of a share would not fit; and a chunk has as many tokens as fit, up to
 // 24 columns.  Of the splits that fit, the one that moves the fewest bytes through the busiest SM is taken, a
 // cluster's exchange counted like 32 KB: the weights of its steps, the activations, the sums.
 int w4_plan(W4Args* a, int pieces, int group) {
-  static const int kResident[4] = {148, 74, 33, 15};
   const int gpb = 128 / group;
   const int64_t stage = 2048 + 96 * gpb;
   int best = 0;
@@ -62,6 +63,66 @@ int w4_plan(W4Args* a, int pieces, int group) {
 
 namespace {
 
+// From how many tokens on the tiled kernels are used (Llama-shaped layer, bf16 y; the streaming kernels read the weights
+// once per 12 tokens).
+constexpr int kWideFrom = 9;
+
+// How a product of many tokens is split: fills the chunk, the warps of a block and entries; returns the cluster.  Of the
+// splits that fit, the one with the least time by the counts of an SM's cycles per K-block: tensor core, reads of
+// shared memory, instructions, memory.
+int wide_plan(W4WideArgs* a, int pieces, int group, bool may_share_k) {
+  const int gpb = 128 / group;
+  a->slots_per_token = pieces - 1;
+  const int most = kW4WideSlots / a->slots_per_token, chunks = (a->n + most - 1) / most;
+  a->tokens = (a->n + chunks - 1) / chunks;
+  a->slot_tiles = (a->tokens * a->slots_per_token + 3) / 4;
+  const int tiles = a->slot_tiles;
+  int best = 0;
+  int64_t best_cost = INT64_MAX;
+  W4WideArgs pick = *a;
+  for (int i = 0; i < (may_share_k ? 4 : 1); ++i) {
+    const int cluster = 1 << i, entries = (a->kblocks + cluster - 1) / cluster;
+    if (cluster > 1 && a->kblocks < 4 * cluster) break;
+    for (int rg = 1; rg <= 8; ++rg) {
+      const int cg_most = 16 / rg < tiles ? 16 / rg : tiles;
+      const int64_t blocks = static_cast<int64_t>((a->tiles + 2 * rg - 1) / (2 * rg)) * chunks;
+      const int64_t waves = (blocks + kResident[i] - 1) / kResident[i];
+      for (int cg = cg_most; cg >= 1; cg = cg > 1 ? cg / 2 : 0) {
+        const int nt = (tiles + cg - 1) / cg;
+        if (nt > 8) break;
+        const int64_t warps = rg * cg;
+        int64_t cycles = 16 * rg * tiles;                                                        // mma: 4 per tile pair and 16 rows, 2 each
+        const int64_t reads = warps * (9 * nt + 20), issue = warps * (120 + 40 * nt) / 4, memory = 100 * rg + 45 * tiles;
+        if (reads > cycles) cycles = reads;
+        if (issue > cycles) cycles = issue;
+        if (memory > cycles) cycles = memory;
+        const int64_t own = static_cast<int64_t>(a->tokens) * (32 * rg + 4) * 4;
+        if (kW4WideStages * w4_wide_stage_bytes(rg, tiles, gpb) > w4::kSmemMax - 4096 || own > w4::kSmemMax - 4096) continue;
+        const int64_t cost = waves * (entries * (cycles + 200) + 4000 + (cluster > 1 ? 4000 : 0));
+        if (cost < best_cost) {
+          best_cost = cost;
+          best = cluster;
+          pick.row_groups = rg;
+          pick.col_groups = cg;
+          pick.entries = entries;
+        }
+      }
+    }
+  }
+  *a = pick;
+  return best;
+}
+
+inline int chunks_of(const W4WideArgs& a) { return (a.n + a.tokens - 1) / a.tokens; }
+inline int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
+// Digits and units of a product's activations.
+inline int64_t digit_bytes(int64_t n, int pieces, int64_t kblocks, int gpb, int64_t* units) {
+  const int spt = pieces - 1, most = kW4WideSlots / spt;
+  const int64_t chunks = (n + most - 1) / most, tokens = (n + chunks - 1) / chunks, tiles = (tokens * spt + 3) / 4;
+  *units = up256(chunks * kblocks * gpb * tiles * 32);
+  return up256(chunks * kblocks * tiles * 1024);
+}
+
 inline bool on(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 
 mlpmoe_status_t check_layer(const mlpmoe_w4_layer_t* l) {
@@ -90,7 +151,102 @@ W4Mat matrix(const mlpmoe_w4_matrix_t& m, int64_t rows, int64_t cols, int group)
   return r;
 }
 
-inline int64_t h_bytes(const mlpmoe_w4_layer_t* l, int64_t n) { return (n * l->d_inter * 4 + 255) / 256 * 256; }
+// Workspace: the intermediate activations in fp32, then for the tiled kernels the digits and units of x and of h.
+struct Layout {
+  int64_t x_digits, x_units, h_digits, h_units, total;
+};
+Layout layout_of(const mlpmoe_w4_layer_t* l, int64_t n, int pieces) {
+  Layout w;
+  const int gpb = 128 / l->group;
+  w.x_digits = up256(n * l->d_inter * 4);
+  w.x_units = w.h_digits = w.h_units = w.total = w.x_digits;
+  if (n < kWideFrom) return w;
+  int64_t xu = 0, hu = 0;
+  w.x_units = w.x_digits + digit_bytes(n, pieces, (l->d_model + 127) / 128, gpb, &xu);
+  w.h_digits = w.x_units + xu;
+  w.h_units = w.h_digits + digit_bytes(n, pieces, (l->d_inter + 127) / 128, gpb, &hu);
+  w.total = w.h_units + hu;
+  return w;
+}
+
+#define BY_GROUP(call, group, ...) \
+  ((group) == 32 ? launch_w4_##call##_32(__VA_ARGS__) : ((group) == 64 ? launch_w4_##call##_64(__VA_ARGS__) : launch_w4_##call##_128(__VA_ARGS__)))
+
+// Digits of x, gate|up, digits of h, down.
+mlpmoe_status_t forward_wide(const mlpmoe_w4_layer_t* layer, const void* x, mlpmoe_dtype_t x_dtype, int64_t x_stride, const float* x_scale,
+                             int64_t x_group, const uint8_t* select, int32_t compensate, const float* residual, void* y,
+                             mlpmoe_dtype_t y_dtype, int n, void* workspace, void* stream) {
+  const int64_t d = layer->d_model, I = layer->d_inter;
+  const int group = layer->group, pieces = y_dtype == MLPMOE_FP32 ? 3 : 2;
+  const Layout l = layout_of(layer, n, pieces);
+  char* ws = static_cast<char*>(workspace);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+
+  W4WideArgs u = {};
+  u.m[0] = matrix(layer->gate, I, d, group);
+  u.m[1] = matrix(layer->up, I, d, group);
+  u.rows = static_cast<int>(I);
+  u.tiles = u.rows / 8;
+  u.kblocks = static_cast<int>((d + 127) / 128);
+  u.n = n;
+  u.B = layer->B;
+  u.select = select;
+  u.dense = select == nullptr;
+  for (int b = 0; b < layer->B; ++b) {
+    u.off[b + 1] = u.off[b] + static_cast<int32_t>(layer->d_b[b]);
+    u.alpha[b] = layer->alpha ? layer->alpha[b] : 1.0f;
+    if (u.alpha[b] == 0.0f) u.dense = 0;
+  }
+  W4WideArgs w = u;
+  w.m[0] = w.m[1] = matrix(layer->down, d, I, group);
+  w.rows = static_cast<int>(d);
+  w.tiles = (w.rows + 15) / 16;
+  w.kblocks = static_cast<int>((I + 127) / 128);
+  const int u_cluster = wide_plan(&u, pieces, group, false), w_cluster = wide_plan(&w, pieces, group, true);
+  if (u_cluster == 0 || w_cluster == 0) return MLPMOE_ERR_UNSUPPORTED;
+  u.digits = reinterpret_cast<uint8_t*>(ws + l.x_digits);
+  u.units = reinterpret_cast<float2*>(ws + l.x_units);
+  u.h = reinterpret_cast<float*>(ws);
+  w.digits = reinterpret_cast<uint8_t*>(ws + l.h_digits);
+  w.units = reinterpret_cast<float2*>(ws + l.h_units);
+  w.compensate = compensate ? 1 : 0;
+  w.residual = residual;
+  w.y = y;
+  w.y_bf16 = y_dtype == MLPMOE_BF16 ? 1 : 0;
+
+  W4DigitsArgs p = {};
+  p.x = x;
+  p.kind = x_dtype;
+  p.stride = x_stride;
+  if (x_dtype == MLPMOE_E4M3) {
+    p.x_scale = x_scale;
+    p.x_groups = x_group == 0 ? 1 : static_cast<int>((d + x_group - 1) / x_group);
+    for (int64_t g = group; x_group != 0 && g < x_group; g *= 2) ++p.x_shift;
+  }
+  p.K = static_cast<int>(d);
+  p.kblocks = u.kblocks;
+  p.n = n;
+  p.tokens = u.tokens;
+  p.slots_per_token = u.slots_per_token;
+  p.slot_tiles = u.slot_tiles;
+  p.digits = const_cast<uint8_t*>(u.digits);
+  p.units = const_cast<float2*>(u.units);
+  W4DigitsArgs q = p;
+  q.x = ws;
+  q.kind = MLPMOE_FP32;
+  q.stride = I;
+  q.x_scale = nullptr;
+  q.K = static_cast<int>(I);
+  q.kblocks = w.kblocks;
+  q.digits = const_cast<uint8_t*>(w.digits);
+  q.units = const_cast<float2*>(w.units);
+
+  pdl_overlap_enabled() = true;
+  if (BY_GROUP(digits, group, p, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
+  if (BY_GROUP(wide_gateup, group, u, chunks_of(u), st) != cudaSuccess) return MLPMOE_ERR_CUDA;
+  if (BY_GROUP(digits, group, q, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
+  return BY_GROUP(wide_down, group, w, w_cluster, chunks_of(w), st) == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
+}
 
 }  // namespace
 }  // namespace mlpmoe
@@ -105,7 +261,7 @@ mlpmoe_status_t mlpmoe_w4_workspace(const mlpmoe_w4_layer_t* layer, int64_t n_to
   if (rc != MLPMOE_OK) return rc;
   if (n_tokens < 0) return MLPMOE_ERR_INVALID_ARG;
   if (n_tokens > kW4MaxTokens) return MLPMOE_ERR_UNSUPPORTED;
-  *bytes = h_bytes(layer, n_tokens);
+  *bytes = layout_of(layer, n_tokens, 3).total;
   return MLPMOE_OK;
 }
 
@@ -131,9 +287,10 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
   if (!x || !y || !on(x, 16) || !on(y, 16) || !on(residual, 16) || (scaled && (!x_scale || !on(x_scale, 4)))) return MLPMOE_ERR_INVALID_ARG;
   if (residual && residual == y && y_dtype != MLPMOE_FP32) return MLPMOE_ERR_INVALID_ARG;
 
-  if (!workspace || workspace_bytes < h_bytes(layer, n_tokens) || !on(workspace, 256)) return MLPMOE_ERR_INVALID_ARG;
+  if (!workspace || workspace_bytes < layout_of(layer, n_tokens, y_dtype == MLPMOE_FP32 ? 3 : 2).total || !on(workspace, 256)) return MLPMOE_ERR_INVALID_ARG;
 
   const int group = layer->group, n = static_cast<int>(n_tokens), digits = y_dtype == MLPMOE_FP32 ? 3 : 2;
+  if (n >= kWideFrom) return forward_wide(layer, x, x_dtype, x_stride, x_scale, x_group, select, compensate, residual, y, y_dtype, n, workspace, stream);
   W4Args u = {};
   u.m[0] = matrix(layer->gate, I, d, group);
   u.m[1] = matrix(layer->up, I, d, group);
@@ -184,11 +341,8 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
   w.y_bf16 = y_dtype == MLPMOE_BF16 ? 1 : 0;
 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = group == 32 ? launch_w4_gateup_32(u, u_cluster, st)
-                              : (group == 64 ? launch_w4_gateup_64(u, u_cluster, st) : launch_w4_gateup_128(u, u_cluster, st));
-  if (e != cudaSuccess) return MLPMOE_ERR_CUDA;
-  e = group == 32 ? launch_w4_down_32(w, w_cluster, st) : (group == 64 ? launch_w4_down_64(w, w_cluster, st) : launch_w4_down_128(w, w_cluster, st));
-  return e == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
+  if (BY_GROUP(gateup, group, u, u_cluster, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
+  return BY_GROUP(down, group, w, w_cluster, st) == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -55,13 +55,56 @@ struct W4Args {
   float alpha[kW4MaxBranches];
 };
 
+// The same products for more tokens (w4_wide.cuh).
+struct W4WideArgs {
+  W4Mat m[2];
+  int rows, tiles;              // as W4Args; a warp takes two tiles
+  int row_groups, col_groups;   // warps of a block: 32 rows each along the rows, `slot_tiles / col_groups` tiles along the columns
+  int kblocks, entries;         // K-blocks in all, and of a block of the cluster at most
+  int n, tokens, slots_per_token, slot_tiles;   // a chunk: tokens * slots_per_token slots, four to a tile of eight columns
+  const uint8_t* digits;        // [chunk][kblock][slot_tile][2][32 lanes][16 bytes]
+  const float2* units;          // [chunk][kblock][GPB][4 slot_tiles]: (unit, - sum of x in units)
+  int B, dense;
+  const uint8_t* select;
+  float* h;                     // gate|up
+  int compensate;               // down
+  const float* residual;
+  void* y;
+  int y_bf16;
+  int32_t off[kW4MaxBranches + 1];
+  float alpha[kW4MaxBranches];
+};
+
+constexpr int kW4WideStages = 4;
+constexpr int kW4WideSlots = 64;      // of a chunk, at most
+// A stage: codes, scales and zeros of 32 row_groups rows, digits and units of the slots.
+__host__ __device__ inline int w4_wide_stage_bytes(int row_groups, int slot_tiles, int gpb) {
+  return 32 * row_groups * (64 + 3 * gpb) + slot_tiles * (1024 + gpb * 32);
+}
+
+// Activations [n x K] to digits in the order w4_wide_kernel reads them.
+struct W4DigitsArgs {
+  const void* x;
+  int kind;
+  int64_t stride;
+  const float* x_scale;
+  int x_groups, x_shift;
+  int K, kblocks, n, tokens, slots_per_token, slot_tiles;
+  uint8_t* digits;
+  float2* units;
+};
+
 // One launch per group width (w4_g32.cu, w4_g64.cu, w4_g128.cu); `cluster` = blocks that share K.
-cudaError_t launch_w4_gateup_32(const W4Args& a, int cluster, cudaStream_t st);
-cudaError_t launch_w4_gateup_64(const W4Args& a, int cluster, cudaStream_t st);
-cudaError_t launch_w4_gateup_128(const W4Args& a, int cluster, cudaStream_t st);
-cudaError_t launch_w4_down_32(const W4Args& a, int cluster, cudaStream_t st);
-cudaError_t launch_w4_down_64(const W4Args& a, int cluster, cudaStream_t st);
-cudaError_t launch_w4_down_128(const W4Args& a, int cluster, cudaStream_t st);
+#define MLPMOE_W4_LAUNCHES(G)                                                                     \
+  cudaError_t launch_w4_gateup_##G(const W4Args& a, int cluster, cudaStream_t st);                \
+  cudaError_t launch_w4_down_##G(const W4Args& a, int cluster, cudaStream_t st);                  \
+  cudaError_t launch_w4_wide_gateup_##G(const W4WideArgs& a, int chunks, cudaStream_t st);        \
+  cudaError_t launch_w4_wide_down_##G(const W4WideArgs& a, int cluster, int chunks, cudaStream_t st); \
+  cudaError_t launch_w4_digits_##G(const W4DigitsArgs& a, cudaStream_t st);
+MLPMOE_W4_LAUNCHES(32)
+MLPMOE_W4_LAUNCHES(64)
+MLPMOE_W4_LAUNCHES(128)
+#undef MLPMOE_W4_LAUNCHES
 
 // Split of one product: fills a->tiles_per_block, entries and c, returns the cluster.  Host only.
 int w4_plan(W4Args* a, int pieces, int group);

@@ -1,9 +1,16 @@
 // The 4-bit products with one scale per 32 columns.
-#include "w4_kernel.cuh"
+#include "w4_wide.cuh"
 
 namespace mlpmoe {
 
 cudaError_t launch_w4_gateup_32(const W4Args& a, int cluster, cudaStream_t st) { return w4::launch_zero<128 / 32, true>(a, cluster, st); }
 cudaError_t launch_w4_down_32(const W4Args& a, int cluster, cudaStream_t st) { return w4::launch_zero<128 / 32, false>(a, cluster, st); }
+cudaError_t launch_w4_wide_gateup_32(const W4WideArgs& a, int chunks, cudaStream_t st) {
+  return w4::launch_wide_zero<128 / 32, true>(a, 1, chunks, st);
+}
+cudaError_t launch_w4_wide_down_32(const W4WideArgs& a, int cluster, int chunks, cudaStream_t st) {
+  return w4::launch_wide_zero<128 / 32, false>(a, cluster, chunks, st);
+}
+cudaError_t launch_w4_digits_32(const W4DigitsArgs& a, cudaStream_t st) { return w4::launch_digits<128 / 32>(a, st); }
 
 }  // namespace mlpmoe

@@ -152,6 +152,34 @@ __device__ __forceinline__ void to_f32(const Raw& r, int kind, float (&v)[8]) {
   }
 }
 
+// Eight activations as whole numbers of a unit, the power of two that puts the group's largest magnitude `top` between
+// 2^22 / 1.004 and 8355711 (three digits of at most 127; two: 2^14 / 1.004 and 32639), so that x / unit is exact before it
+// is rounded.  m: the number plus 0x808080, exclusive-or 0x808080, whose bytes are its digits -128 .. 127, lowest first.
+// A group all below 2^-100 counts as 0 (its unit would leave the range of fp32) and returns false.
+__device__ __forceinline__ bool to_fixed(const float (&v)[8], float top, int pieces, float* unit, uint32_t (&m)[8]) {
+  const int exponent = (__float_as_int(top * 1.00396f) >> 23) + (pieces == 3 ? 1 - 23 : 1 - 15);
+  const bool some = top >= 7.8886091e-31f;
+  const float inv = some ? __int_as_float((254 - exponent) << 23) : 0.0f;
+  *unit = some ? __int_as_float(exponent << 23) : 0.0f;
+  if (pieces == 3) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m[e] = (static_cast<uint32_t>(__float2int_rn(v[e] * inv)) + 0x00808080u) ^ 0x00808080u;
+  } else {                              // below 2^22: the sum with 1.5 * 2^23 has the rounded number in its low bits
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m[e] = (__float_as_uint(fmaf(v[e], inv, 12582912.0f)) - 0x4B400000u + 0x00808080u) ^ 0x00808080u;
+  }
+  return some;
+}
+// Digits p of the even and of the odd four.
+__device__ __forceinline__ uint2 digit_of(const uint32_t (&m)[8], int p) {
+  const uint32_t pick = p | (p + 4) << 4;
+  return make_uint2(__byte_perm(__byte_perm(m[0], m[2], pick), __byte_perm(m[4], m[6], pick), 0x5410),
+                    __byte_perm(__byte_perm(m[1], m[3], pick), __byte_perm(m[5], m[7], pick), 0x5410));
+}
+__device__ __forceinline__ int sum_of_eight(uint2 d) {
+  return __dp4a(static_cast<int>(d.x), 0x01010101, __dp4a(static_cast<int>(d.y), 0x01010101, 0));
+}
+
 // grid: (shares of the row tiles, cluster along K, chunks of tokens)
 template <int NT, int GPB, bool GATEUP, bool ZERO>
 __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__ W4Args a) {
@@ -362,22 +390,9 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
         for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
 #pragma unroll
         for (int o = 1; o < kLanes; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        // unit: the power of two that puts the largest magnitude between 2^22 / 1.004 and 8355711 (three digits of at most
-        // 127; two: 2^14 / 1.004 and 32639), so that x / unit is exact before it is rounded; a group all below 2^-100
-        // counts as 0 (its unit would leave the range of fp32)
-        const int exponent = (__float_as_int(top * 1.00396f) >> 23) + (a.c.pieces == 3 ? 1 - 23 : 1 - 15);
-        const bool some = top >= 7.8886091e-31f;
-        const float inv = some ? __int_as_float((254 - exponent) << 23) : 0.0f;
-        float unit = some ? __int_as_float(exponent << 23) : 0.0f;
-        // bytes of (m + 0x808080) ^ 0x808080: the digits -128 .. 127 whose sum of powers of 256 is m
+        float unit;
         uint32_t m[8];
-        if (a.c.pieces == 3) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) m[e] = (static_cast<uint32_t>(__float2int_rn(v[e] * inv)) + 0x00808080u) ^ 0x00808080u;
-        } else {                        // below 2^22: the sum with 1.5 * 2^23 has the rounded number in its low bits
-#pragma unroll
-          for (int e = 0; e < 8; ++e) m[e] = (__float_as_uint(fmaf(v[e], inv, 12582912.0f)) - 0x4B400000u + 0x00808080u) ^ 0x00808080u;
-        }
+        const bool some = to_fixed(v, top, a.c.pieces, &unit, m);
         const int j = k8 / kLanes, word = unit_word<GPB>(k8);
         if (GATEUP && a.x_scale != nullptr && k8 % kLanes == 0 && some) {
           const int xg = a.x_groups == 1 ? 0 : (s_list[entry] * GPB + j) >> a.x_shift;
@@ -385,11 +400,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
         }
         uint2* out = s_x + (((entry * 2 + (word >> 1)) * (NT * 8) + toks[u]) * 4 + unit_lane<GPB>(k8)) * 2 + (word & 1);
         float2* units = s_unit + (entry * GPB + j) * (NT * 8) + toks[u];
-        const uint32_t e01 = __byte_perm(m[0], m[2], 0x5140), e23 = __byte_perm(m[4], m[6], 0x5140);   // digits 0 0 1 1 of a pair
-        const uint32_t o01 = __byte_perm(m[1], m[3], 0x5140), o23 = __byte_perm(m[5], m[7], 0x5140);
-        auto sum_of_eight = [](uint2 d) { return __dp4a(static_cast<int>(d.x), 0x01010101, __dp4a(static_cast<int>(d.y), 0x01010101, 0)); };
-        const uint2 d0 = make_uint2(__byte_perm(e01, e23, 0x5410), __byte_perm(o01, o23, 0x5410));
-        const uint2 d1 = make_uint2(__byte_perm(e01, e23, 0x7632), __byte_perm(o01, o23, 0x7632));
+        const uint2 d0 = digit_of(m, 0), d1 = digit_of(m, 1);
         // a sum over 128 digits fits in 16 bits: two digits' sums in one word
         int sums01 = sum_of_eight(d0) + (sum_of_eight(d1) << 16);
 #pragma unroll
@@ -402,8 +413,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
           units[tokens] = make_float2(unit * 256.0f, __int_as_float(-sum1));
         }
         if (a.c.pieces == 3) {
-          const uint2 d2 = make_uint2(__byte_perm(__byte_perm(m[0], m[2], 0x0062), __byte_perm(m[4], m[6], 0x0062), 0x5410),
-                                      __byte_perm(__byte_perm(m[1], m[3], 0x0062), __byte_perm(m[5], m[7], 0x0062), 0x5410));
+          const uint2 d2 = digit_of(m, 2);
           int sum2 = sum_of_eight(d2);
 #pragma unroll
           for (int o = 1; o < kLanes; o *= 2) sum2 += __shfl_xor_sync(0xFFFFFFFFu, sum2, o);
