@@ -67,6 +67,15 @@ namespace {
 // once per 12 tokens).
 constexpr int kWideFrom = 9;
 
+// Tiles of eight columns for `slots` slots: 1, 2, 3, 4, 6, 8, 12 or 16, which divide among the warps of a block.
+int wide_tiles(int slots) {
+  int tiles = (slots + 3) / 4;
+  if (tiles > 12) return 16;
+  if (tiles > 8) return 12;
+  if (tiles > 4) return tiles + (tiles & 1);
+  return tiles;
+}
+
 // How a product of many tokens is split: fills the chunk, the warps of a block and entries; returns the cluster.  Of the
 // splits that fit, the one with the least time by the counts of an SM's cycles per K-block: tensor core, reads of
 // shared memory, instructions, memory.
@@ -75,7 +84,7 @@ int wide_plan(W4WideArgs* a, int pieces, int group, bool may_share_k) {
   a->slots_per_token = pieces - 1;
   const int most = kW4WideSlots / a->slots_per_token, chunks = (a->n + most - 1) / most;
   a->tokens = (a->n + chunks - 1) / chunks;
-  a->slot_tiles = (a->tokens * a->slots_per_token + 3) / 4;
+  a->slot_tiles = wide_tiles(a->tokens * a->slots_per_token);
   const int tiles = a->slot_tiles;
   int best = 0;
   int64_t best_cost = INT64_MAX;
@@ -87,8 +96,10 @@ int wide_plan(W4WideArgs* a, int pieces, int group, bool may_share_k) {
       const int cg_most = 16 / rg < tiles ? 16 / rg : tiles;
       const int64_t blocks = static_cast<int64_t>((a->tiles + 2 * rg - 1) / (2 * rg)) * chunks;
       const int64_t waves = (blocks + kResident[i] - 1) / kResident[i];
-      for (int cg = cg_most; cg >= 1; cg = cg > 1 ? cg / 2 : 0) {
-        const int nt = (tiles + cg - 1) / cg;
+      for (int cg = 4; cg >= 1; cg /= 2) {
+        if (cg > cg_most) continue;
+        if (tiles % cg != 0 || (cg == 1 && tiles % 2 == 0)) continue;
+        const int nt = tiles / cg;
         if (nt > 8) break;
         const int64_t warps = rg * cg;
         int64_t cycles = 16 * rg * tiles;                                                        // mma: 4 per tile pair and 16 rows, 2 each
@@ -118,7 +129,7 @@ inline int64_t up256(int64_t v) { return (v + 255) / 256 * 256; }
 // Digits and units of a product's activations.
 inline int64_t digit_bytes(int64_t n, int pieces, int64_t kblocks, int gpb, int64_t* units) {
   const int spt = pieces - 1, most = kW4WideSlots / spt;
-  const int64_t chunks = (n + most - 1) / most, tokens = (n + chunks - 1) / chunks, tiles = (tokens * spt + 3) / 4;
+  const int64_t chunks = (n + most - 1) / most, tokens = (n + chunks - 1) / chunks, tiles = wide_tiles(static_cast<int>(tokens * spt));
   *units = up256(chunks * kblocks * gpb * tiles * 32);
   return up256(chunks * kblocks * tiles * 1024);
 }

@@ -59,7 +59,7 @@ struct W4Args {
 struct W4WideArgs {
   W4Mat m[2];
   int rows, tiles;              // as W4Args; a warp takes two tiles
-  int row_groups, col_groups;   // warps of a block: 32 rows each along the rows, `slot_tiles / col_groups` tiles along the columns
+  int row_groups, col_groups;   // warps of a block: 32 rows each along the rows, slot_tiles / col_groups tiles (1, 2, 3, 4, 6 or 8) along the columns
   int kblocks, entries;         // K-blocks in all, and of a block of the cluster at most
   int n, tokens, slots_per_token, slot_tiles;   // a chunk: tokens * slots_per_token slots, four to a tile of eight columns
   const uint8_t* digits;        // [chunk][kblock][slot_tile][2][32 lanes][16 bytes]

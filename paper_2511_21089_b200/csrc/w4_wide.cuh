@@ -144,29 +144,43 @@ __global__ void __launch_bounds__(512, 1) w4_wide_kernel(const __grid_constant__
     const int tile = blockIdx.x * a.row_groups * 2 + lt;
     return GATEUP ? min(tile * 8, a.rows - 8) : min(tile * 16 + 8 * half, a.rows - 8);
   };
+  // codes: 128 row_groups pieces of 16 bytes and 32 row_groups col_groups threads, four, two or one each; a thread's rows
+  // never change.  One column group occurs with 1 or 3 tiles only.
+  constexpr int kTurns = NTW == 1 || NTW == 3 ? 4 : 2;
+  const uint8_t* q_src[kTurns];
+  uint32_t q_dst[kTurns];
+#pragma unroll
+  for (int m = 0; m < kTurns; ++m) {
+    const int i = threadIdx.x + m * threads, r = i >> 2, c = i & 3, half = (r >> 3) & 1;
+    const bool in = i < block_rows * 4;
+    q_src[m] = in ? (half == 0 ? a.m[0].q : a.m[1].q) + (half_row(r >> 4, half) + (r & 7)) * a.m[0].pitch : nullptr;
+    q_dst[m] = ring + r * 64 + (c ^ ((r >> 1) & 3)) * 16;
+  }
+  const uint32_t q_col = (threadIdx.x & 3) * 16;
+  // scales and zeros: 4 row_groups GPB pieces (an 8-row half and a group each), one per thread
+  const int s_piece = threadIdx.x / GPB, s_half = s_piece & 1;
+  const bool s_in = threadIdx.x < block_rows / 8 * GPB;
+  const __nv_bfloat16* const s_src = (s_half == 0 ? a.m[0].scale : a.m[1].scale) + (s_in ? half_row(s_piece >> 1, s_half) : 0);
+  const uint8_t* const z_base = s_half == 0 ? a.m[0].zero : a.m[1].zero;
+  const uint8_t* const z_src = ZERO && s_in && z_base != nullptr ? z_base + half_row(s_piece >> 1, s_half) : nullptr;
   auto copy_weights = [&](int entry, int slot) {
-    const int kb = s_list[entry];
-    const uint32_t base = ring + slot * stage;
-    for (int i = threadIdx.x; i < block_rows * 4; i += threads) {        // 16 bytes each; local row i / 4 = tile, half, row
-      const int r = i >> 2, c = i & 3, half = (r >> 3) & 1;
-      const uint32_t byte = min(static_cast<uint32_t>(kb) * 64 + c * 16, last_byte);
-      const uint8_t* q = half == 0 ? a.m[0].q : a.m[1].q;
-      cp_async16(base + r * 64 + (c ^ ((r >> 1) & 3)) * 16, q + (half_row(r >> 4, half) + (r & 7)) * a.m[0].pitch + byte);
-    }
-    for (int i = threadIdx.x; i < block_rows / 8 * GPB; i += threads) {  // scales and zeros of an 8-row half and a group
-      const int piece = i / GPB, half = piece & 1;
-      const uint32_t at = min(static_cast<uint32_t>(kb) * GPB + i % GPB, last_group) * rows16 + half_row(piece >> 1, half);
-      cp_async16(base + o_scale + i * 16, (half == 0 ? a.m[0].scale : a.m[1].scale) + at);
-      const uint8_t* zero = half == 0 ? a.m[0].zero : a.m[1].zero;
-      if (ZERO && zero != nullptr) cp_async8(base + o_zero + i * 8, zero + at);
+    const uint32_t kb = s_list[entry], to = slot * stage, byte = min(kb * 64 + q_col, last_byte);
+#pragma unroll
+    for (int m = 0; m < kTurns; ++m)
+      if (q_src[m] != nullptr) cp_async16(q_dst[m] + to, q_src[m] + byte);
+    if (s_in) {
+      const uint32_t at = min(kb * GPB + threadIdx.x % GPB, last_group) * rows16;
+      cp_async16(ring + to + o_scale + threadIdx.x * 16, s_src + at);
+      if (z_src != nullptr) cp_async8(ring + to + o_zero + threadIdx.x * 8, z_src + at);
     }
   };
   auto copy_digits = [&](int entry, int slot) {
     const int64_t at = static_cast<int64_t>(chunk) * a.kblocks + s_list[entry];
+    const uint32_t to = ring + slot * stage;
     const uint8_t* x = a.digits + at * a.slot_tiles * 1024;
-    for (int i = threadIdx.x; i < a.slot_tiles * 64; i += threads) cp_async16(ring + slot * stage + o_x + i * 16, x + i * 16);
+    for (int i = threadIdx.x * 16; i < a.slot_tiles * 1024; i += threads * 16) cp_async16(to + o_x + i, x + i);
     const uint8_t* u = reinterpret_cast<const uint8_t*>(a.units + at * GPB * 4 * a.slot_tiles);
-    for (int i = threadIdx.x; i < a.slot_tiles * GPB * 2; i += threads) cp_async16(ring + slot * stage + o_unit + i * 16, u + i * 16);
+    for (int i = threadIdx.x * 16; i < a.slot_tiles * GPB * 32; i += threads * 16) cp_async16(to + o_unit + i, u + i);
   };
   for (int i = 0; i < kW4WideStages - 1; ++i)
     if (i < n_entries) copy_weights(i, i);
@@ -229,11 +243,12 @@ __global__ void __launch_bounds__(512, 1) w4_wide_kernel(const __grid_constant__
           op[rt][w][3] = (q[1][w] >> 4) & 0x0F0F0F0Fu;
         }
       }
+      const uint4* xs = reinterpret_cast<const uint4*>(st + o_x + st0 * 1024) + lane;
+      const float2* us = reinterpret_cast<const float2*>(st + o_unit) + (j * 4 * a.slot_tiles + 4 * st0 + t);
 #pragma unroll
       for (int nt = 0; nt < NTW; ++nt) {
-        if (st0 + nt >= a.slot_tiles) break;
-        const uint4* xp = reinterpret_cast<const uint4*>(st + o_x + (st0 + nt) * 1024) + lane;
-        const float2 unit = *reinterpret_cast<const float2*>(st + o_unit + (j * 4 * a.slot_tiles + 4 * (st0 + nt) + t) * 8);
+        const uint4* xp = xs + nt * 64;
+        const float2 unit = us[4 * nt];
         uint4 b[2];
         if (GPB < 4 || j < 2) b[0] = xp[0];
         if (GPB == 1 || (GPB == 2 && j == 1) || (GPB == 4 && j >= 2)) b[1] = xp[32];
@@ -266,7 +281,7 @@ __global__ void __launch_bounds__(512, 1) w4_wide_kernel(const __grid_constant__
   }
   auto token_of = [&](int nt) {                   // of this lane, or -1 where it holds none
     const int s = 4 * (st0 + nt) + t, tok = s / a.slots_per_token, token = chunk * a.tokens + tok;
-    return st0 + nt < a.slot_tiles && tok < a.tokens && token < a.n && (a.slots_per_token == 1 || (t & 1) == 0) ? token : -1;
+    return tok < a.tokens && token < a.n && (a.slots_per_token == 1 || (t & 1) == 0) ? token : -1;
   };
   if (GATEUP) {
 #pragma unroll
@@ -368,14 +383,12 @@ cudaError_t launch_wide(const W4WideArgs& a, int cluster, int chunks, cudaStream
 
 template <int GPB, bool GATEUP, bool ZERO>
 cudaError_t launch_wide_tiles(const W4WideArgs& a, int cluster, int chunks, cudaStream_t st) {
-  switch ((a.slot_tiles + a.col_groups - 1) / a.col_groups) {
+  switch (a.slot_tiles / a.col_groups) {
     case 1: return launch_wide<1, GPB, GATEUP, ZERO>(a, cluster, chunks, st);
     case 2: return launch_wide<2, GPB, GATEUP, ZERO>(a, cluster, chunks, st);
     case 3: return launch_wide<3, GPB, GATEUP, ZERO>(a, cluster, chunks, st);
     case 4: return launch_wide<4, GPB, GATEUP, ZERO>(a, cluster, chunks, st);
-    case 5:
     case 6: return launch_wide<6, GPB, GATEUP, ZERO>(a, cluster, chunks, st);
-    case 7:
     case 8: return launch_wide<8, GPB, GATEUP, ZERO>(a, cluster, chunks, st);
     default: return cudaErrorInvalidValue;
   }
