@@ -386,6 +386,12 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
                                   const float* residual, void* y, mlpmoe_dtype_t y_dtype, int64_t n_tokens, void* workspace,
                                   int64_t workspace_bytes, void* stream);
 mlpmoe_status_t mlpmoe_w4_workspace(const mlpmoe_w4_layer_t* layer, int64_t n_tokens, int64_t* bytes);
+/*
+ * How the last mlpmoe_w4_forward with this workspace ended (copies one word back and synchronises `stream`, the one of the
+ * call): MLPMOE_OK, or MLPMOE_ERR_DEVICE_TIMEOUT if a bounded wait inside its kernels ran out; y is undefined then.  The
+ * next call starts afresh.
+ */
+mlpmoe_status_t mlpmoe_w4_get_status(const void* workspace, void* stream);
 
 /* ------------------------------------------------------------------------- *
  * Queries (host outputs; used by the parity harness)
@@ -467,6 +473,12 @@ mlpmoe_status_t mlpmoe_debug_set_wait(mlpmoe_handle_t h, uint64_t limit_ns, uint
  * each of them on shapes where the rule would pick the other.  MLPMOE_ERR_INVALID_ARG for another value.
  */
 mlpmoe_status_t mlpmoe_debug_set_decode_kernel(mlpmoe_handle_t h, int32_t kernel);
+
+/*
+ * The same for later mlpmoe_w4_forward calls of the process that run on the tensor cores' kernels: the limit of the waits
+ * inside a block (0 = one second), and arrivals that its first stage waits for in vain (0 = normal operation).
+ */
+mlpmoe_status_t mlpmoe_w4_debug_set_wait(uint64_t limit_ns, uint32_t extra_arrivals);
 
 /*
  * The handle's (possibly shared) activation workspace, for guard-band checks and memory

@@ -68,6 +68,8 @@ SIGNATURES = {
     "mlpmoe_w4_dequantize": (c_int32, [c_void_p, c_void_p, c_void_p, c_int64, c_int64, c_int32, c_void_p, c_int32, c_int32, c_int64, c_void_p]),
     "mlpmoe_w4_forward": (c_int32, [POINTER(mlpmoe_w4_layer_t), c_void_p, c_int32, c_int64, c_void_p, c_int64, c_void_p, c_int32, c_void_p,
                                     c_void_p, c_int32, c_int64, c_void_p, c_int64, c_void_p]),
+    "mlpmoe_w4_get_status": (c_int32, [c_void_p, c_void_p]),
+    "mlpmoe_w4_debug_set_wait": (c_int32, [ctypes.c_uint64, ctypes.c_uint32]),
     "mlpmoe_w4_workspace": (c_int32, [POINTER(mlpmoe_w4_layer_t), c_int64, POINTER(c_int64)]),
     "mlpmoe_stack_prepare": (c_int32, [POINTER(c_void_p), c_int32, c_int64, c_void_p]),
     "mlpmoe_debug_set_wait": (c_int32, [c_void_p, ctypes.c_uint64, ctypes.c_uint32]),
@@ -266,6 +268,15 @@ def mlpmoe_w4_workspace(layer: mlpmoe_w4_layer_t, n_tokens: int) -> int:
     v = c_int64()
     _check(lib.mlpmoe_w4_workspace(layer, n_tokens, ctypes.byref(v)), "mlpmoe_w4_workspace")
     return v.value
+
+
+def mlpmoe_w4_get_status(workspace, stream=None) -> int:
+    """MLPMOE_OK or MLPMOE_ERR_DEVICE_TIMEOUT of the last mlpmoe_w4_forward with this workspace."""
+    return lib.mlpmoe_w4_get_status(_ptr(workspace), _stream(stream))
+
+
+def mlpmoe_w4_debug_set_wait(limit_ns: int = 0, extra_arrivals: int = 0) -> None:
+    _check(lib.mlpmoe_w4_debug_set_wait(limit_ns, extra_arrivals), "mlpmoe_w4_debug_set_wait")
 
 
 def mlpmoe_w4_forward(layer: mlpmoe_w4_layer_t, x, y, n_tokens: int, workspace, workspace_bytes: int, x_dtype: int = MLPMOE_BF16,

@@ -2,6 +2,8 @@
 // and down; the second begins with its copies of the weights while the first runs.
 #include <string.h>
 
+#include <atomic>
+
 #include "../../include/mlpmoe.h"
 #include "w4_kernel.cuh"
 
@@ -162,21 +164,61 @@ W4Mat matrix(const mlpmoe_w4_matrix_t& m, int64_t rows, int64_t cols, int group)
   return r;
 }
 
-// Workspace: the intermediate activations in fp32, then for the tiled kernels the digits and units of x and of h.
-struct Layout {
-  int64_t x_digits, x_units, h_digits, h_units, total;
+// From how many tokens on, and from how many codes of the layer on, the tensor cores' kernels are used (y bf16).
+constexpr int kTcFrom = 17;
+constexpr int64_t kTcCodes = int64_t(24) << 20;
+
+// Limits of the bounded waits of the tensor cores' kernels; changed by the test hook only.
+std::atomic<uint64_t> g_wait_limit_ns{1000000000ull};
+std::atomic<uint32_t> g_extra_arrivals{0};
+
+enum Path { STREAM, WIDE, TENSOR };
+Path path_of(const mlpmoe_w4_layer_t* l, int64_t n, mlpmoe_dtype_t y_dtype) {
+  if (n < kWideFrom) return STREAM;
+  return y_dtype == MLPMOE_BF16 && n >= kTcFrom && 3 * l->d_model * l->d_inter >= kTcCodes ? TENSOR : WIDE;
+}
+
+// A chunk of the tensor cores' products: tokens, and the columns of an epilogue warp.  gate|up has 64 columns at most, down
+// 128, two per token.
+struct TcChunk {
+  int tokens, chunks, ne;
 };
-Layout layout_of(const mlpmoe_w4_layer_t* l, int64_t n, int pieces) {
+TcChunk tc_chunk(int64_t n, int pieces) {
+  TcChunk c;
+  const int64_t most = 64 / pieces;
+  c.chunks = static_cast<int>((n + most - 1) / most);
+  c.tokens = static_cast<int>((n + c.chunks - 1) / c.chunks);
+  c.ne = c.tokens * pieces <= 32 ? 32 : 64;
+  return c;
+}
+inline int x_pieces(mlpmoe_dtype_t x_dtype) { return x_dtype == MLPMOE_BF16 ? 1 : 2; }
+// The down product: two pieces, columns 2 ne.
+inline TcChunk tc_down_chunk(int64_t n) { return tc_chunk(n, 1); }
+
+// Workspace: a status word, the intermediate activations in fp32, then the activations of both products as the tiled kernels
+// (digits, units) or the tensor cores' kernels (images) read them.
+struct Layout {
+  int64_t h, x, x_units, y, y_units, total;
+};
+Layout layout_of(const mlpmoe_w4_layer_t* l, int64_t n, Path path, int digits, int pieces) {
   Layout w;
   const int gpb = 128 / l->group;
-  w.x_digits = up256(n * l->d_inter * 4);
-  w.x_units = w.h_digits = w.h_units = w.total = w.x_digits;
-  if (n < kWideFrom) return w;
-  int64_t xu = 0, hu = 0;
-  w.x_units = w.x_digits + digit_bytes(n, pieces, (l->d_model + 127) / 128, gpb, &xu);
-  w.h_digits = w.x_units + xu;
-  w.h_units = w.h_digits + digit_bytes(n, pieces, (l->d_inter + 127) / 128, gpb, &hu);
-  w.total = w.h_units + hu;
+  const int64_t xk = (l->d_model + 127) / 128, hk = (l->d_inter + 127) / 128;
+  int64_t xb = 0, xu = 0, hb = 0, hu = 0;
+  if (path == WIDE) {
+    xb = digit_bytes(n, digits, xk, gpb, &xu);
+    hb = digit_bytes(n, digits, hk, gpb, &hu);
+  } else if (path == TENSOR) {
+    const TcChunk u = tc_chunk(n, pieces), d = tc_down_chunk(n);
+    xb = u.chunks * xk * u.ne * 256;
+    hb = d.chunks * hk * d.ne * 512;
+  }
+  w.h = 256;
+  w.x = w.h + up256(n * l->d_inter * 4);
+  w.x_units = w.x + xb;
+  w.y = w.x_units + xu;
+  w.y_units = w.y + hb;
+  w.total = w.y_units + hu;
   return w;
 }
 
@@ -189,7 +231,7 @@ mlpmoe_status_t forward_wide(const mlpmoe_w4_layer_t* layer, const void* x, mlpm
                              mlpmoe_dtype_t y_dtype, int n, void* workspace, void* stream) {
   const int64_t d = layer->d_model, I = layer->d_inter;
   const int group = layer->group, pieces = y_dtype == MLPMOE_FP32 ? 3 : 2;
-  const Layout l = layout_of(layer, n, pieces);
+  const Layout l = layout_of(layer, n, WIDE, pieces, 1);
   char* ws = static_cast<char*>(workspace);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
 
@@ -215,11 +257,11 @@ mlpmoe_status_t forward_wide(const mlpmoe_w4_layer_t* layer, const void* x, mlpm
   w.kblocks = static_cast<int>((I + 127) / 128);
   const int u_cluster = wide_plan(&u, pieces, group, false), w_cluster = wide_plan(&w, pieces, group, true);
   if (u_cluster == 0 || w_cluster == 0) return MLPMOE_ERR_UNSUPPORTED;
-  u.digits = reinterpret_cast<uint8_t*>(ws + l.x_digits);
+  u.digits = reinterpret_cast<uint8_t*>(ws + l.x);
   u.units = reinterpret_cast<float2*>(ws + l.x_units);
-  u.h = reinterpret_cast<float*>(ws);
-  w.digits = reinterpret_cast<uint8_t*>(ws + l.h_digits);
-  w.units = reinterpret_cast<float2*>(ws + l.h_units);
+  u.h = reinterpret_cast<float*>(ws + l.h);
+  w.digits = reinterpret_cast<uint8_t*>(ws + l.y);
+  w.units = reinterpret_cast<float2*>(ws + l.y_units);
   w.compensate = compensate ? 1 : 0;
   w.residual = residual;
   w.y = y;
@@ -242,8 +284,10 @@ mlpmoe_status_t forward_wide(const mlpmoe_w4_layer_t* layer, const void* x, mlpm
   p.slot_tiles = u.slot_tiles;
   p.digits = const_cast<uint8_t*>(u.digits);
   p.units = const_cast<float2*>(u.units);
+  p.status = reinterpret_cast<uint32_t*>(ws);
   W4DigitsArgs q = p;
-  q.x = ws;
+  q.status = nullptr;
+  q.x = ws + l.h;
   q.kind = MLPMOE_FP32;
   q.stride = I;
   q.x_scale = nullptr;
@@ -259,6 +303,101 @@ mlpmoe_status_t forward_wide(const mlpmoe_w4_layer_t* layer, const void* x, mlpm
   return BY_GROUP(wide_down, group, w, w_cluster, chunks_of(w), st) == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
 }
 
+// The cluster along K of a product: 1, 2, 4 or 8 blocks, whichever takes the fewest turns of K-blocks (a turn is what one
+// block per SM does at a time; six K-blocks' time for the start and the end, six more for the exchange).
+int tc_cluster(int64_t blocks, int64_t kblocks) {
+  int best = 1;
+  int64_t best_cost = INT64_MAX;
+  for (int i = 0; i < 4; ++i) {
+    const int64_t cluster = 1 << i, entries = (kblocks + cluster - 1) / cluster, waves = (blocks + kResident[i] - 1) / kResident[i];
+    if (cluster > 1 && kblocks < 2 * cluster) break;
+    const int64_t cost = waves * (entries + 6 + (cluster > 1 ? 6 : 0));
+    if (cost < best_cost) best_cost = cost, best = static_cast<int>(cluster);
+  }
+  return best;
+}
+
+// Columns of x, gate|up, columns of h, down.
+mlpmoe_status_t forward_tc(const mlpmoe_w4_layer_t* layer, const void* x, mlpmoe_dtype_t x_dtype, int64_t x_stride, const float* x_scale,
+                           int64_t x_group, const uint8_t* select, int32_t compensate, const float* residual, void* y, int n,
+                           void* workspace, void* stream) {
+  const int64_t d = layer->d_model, I = layer->d_inter;
+  const int group = layer->group, pieces = x_pieces(x_dtype);
+  const Layout l = layout_of(layer, n, TENSOR, 2, pieces);
+  const TcChunk uc = tc_chunk(n, pieces), wc = tc_down_chunk(n);
+  char* ws = static_cast<char*>(workspace);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+
+  W4TcArgs u = {};
+  u.m[0] = matrix(layer->gate, I, d, group);
+  u.m[1] = matrix(layer->up, I, d, group);
+  u.rows = static_cast<int>(I);
+  u.kblocks = static_cast<int>((d + 127) / 128);
+  u.n = n;
+  u.tokens = uc.tokens;
+  u.pieces = pieces;
+  u.ne = uc.ne;
+  u.image = reinterpret_cast<uint8_t*>(ws + l.x);
+  u.B = layer->B;
+  u.select = select;
+  u.dense = select == nullptr;
+  for (int b = 0; b < layer->B; ++b) {
+    u.off[b + 1] = u.off[b] + static_cast<int32_t>(layer->d_b[b]);
+    u.alpha[b] = layer->alpha ? layer->alpha[b] : 1.0f;
+    if (u.alpha[b] == 0.0f) u.dense = 0;
+  }
+  u.h = reinterpret_cast<float*>(ws + l.h);
+  u.status = reinterpret_cast<uint32_t*>(ws);
+  u.wait_limit_ns = g_wait_limit_ns.load();
+  u.extra_arrivals = g_extra_arrivals.load();
+  W4TcArgs w = u;
+  w.m[0] = w.m[1] = matrix(layer->down, d, I, group);
+  w.rows = static_cast<int>(d);
+  w.kblocks = static_cast<int>((I + 127) / 128);
+  w.tokens = wc.tokens;
+  w.pieces = 2;
+  w.ne = wc.ne;
+  w.image = reinterpret_cast<uint8_t*>(ws + l.y);
+  w.compensate = compensate ? 1 : 0;
+  w.residual = residual;
+  w.y = static_cast<__nv_bfloat16*>(y);
+
+  W4ColumnsArgs p = {};
+  p.x = x;
+  p.kind = x_dtype;
+  p.stride = x_stride;
+  if (x_dtype == MLPMOE_E4M3) {
+    p.x_scale = x_scale;
+    p.x_group = static_cast<int>(x_group);
+    p.x_groups = x_group == 0 ? 1 : static_cast<int>((d + x_group - 1) / x_group);
+  }
+  p.K = static_cast<int>(d);
+  p.kblocks = u.kblocks;
+  p.n = n;
+  p.tokens = u.tokens;
+  p.pieces = pieces;
+  p.cols = u.ne;
+  p.image = const_cast<uint8_t*>(u.image);
+  p.status = u.status;
+  W4ColumnsArgs q = {};
+  q.x = ws + l.h;
+  q.kind = MLPMOE_FP32;
+  q.stride = I;
+  q.K = static_cast<int>(I);
+  q.kblocks = w.kblocks;
+  q.n = n;
+  q.tokens = w.tokens;
+  q.pieces = 2;
+  q.cols = 2 * w.ne;
+  q.image = const_cast<uint8_t*>(w.image);
+
+  pdl_overlap_enabled() = true;
+  if (launch_w4_columns(p, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
+  if (BY_GROUP(tc_gateup, group, u, tc_cluster((I + 127) / 128 * uc.chunks, u.kblocks), st) != cudaSuccess) return MLPMOE_ERR_CUDA;
+  if (launch_w4_columns(q, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
+  return BY_GROUP(tc_down, group, w, tc_cluster((d + 127) / 128 * wc.chunks, w.kblocks), st) == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
+}
+
 }  // namespace
 }  // namespace mlpmoe
 
@@ -272,7 +411,29 @@ mlpmoe_status_t mlpmoe_w4_workspace(const mlpmoe_w4_layer_t* layer, int64_t n_to
   if (rc != MLPMOE_OK) return rc;
   if (n_tokens < 0) return MLPMOE_ERR_INVALID_ARG;
   if (n_tokens > kW4MaxTokens) return MLPMOE_ERR_UNSUPPORTED;
-  *bytes = layout_of(layer, n_tokens, 3).total;
+  // the most that a call with any types needs
+  *bytes = 0;
+  for (int k = 2; k <= 3; ++k) {
+    const int64_t wide = layout_of(layer, n_tokens, path_of(layer, n_tokens, MLPMOE_FP32), k, 1).total;
+    const int64_t tensor = layout_of(layer, n_tokens, path_of(layer, n_tokens, MLPMOE_BF16), k, k - 1).total;
+    if (wide > *bytes) *bytes = wide;
+    if (tensor > *bytes) *bytes = tensor;
+  }
+  return MLPMOE_OK;
+}
+
+mlpmoe_status_t mlpmoe_w4_get_status(const void* workspace, void* stream) {
+  if (!workspace || !on(workspace, 256)) return MLPMOE_ERR_INVALID_ARG;
+  uint32_t word = 0;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (cudaMemcpyAsync(&word, workspace, sizeof(word), cudaMemcpyDeviceToHost, st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
+    return MLPMOE_ERR_CUDA;
+  return word == kStatusOk ? MLPMOE_OK : MLPMOE_ERR_DEVICE_TIMEOUT;
+}
+
+mlpmoe_status_t mlpmoe_w4_debug_set_wait(uint64_t limit_ns, uint32_t extra_arrivals) {
+  g_wait_limit_ns = limit_ns ? limit_ns : 1000000000ull;
+  g_extra_arrivals = extra_arrivals;
   return MLPMOE_OK;
 }
 
@@ -298,10 +459,14 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
   if (!x || !y || !on(x, 16) || !on(y, 16) || !on(residual, 16) || (scaled && (!x_scale || !on(x_scale, 4)))) return MLPMOE_ERR_INVALID_ARG;
   if (residual && residual == y && y_dtype != MLPMOE_FP32) return MLPMOE_ERR_INVALID_ARG;
 
-  if (!workspace || workspace_bytes < layout_of(layer, n_tokens, y_dtype == MLPMOE_FP32 ? 3 : 2).total || !on(workspace, 256)) return MLPMOE_ERR_INVALID_ARG;
+  const Path path = path_of(layer, n_tokens, y_dtype);
+  const Layout l = layout_of(layer, n_tokens, path, y_dtype == MLPMOE_FP32 ? 3 : 2, x_pieces(x_dtype));
+  if (!workspace || workspace_bytes < l.total || !on(workspace, 256)) return MLPMOE_ERR_INVALID_ARG;
 
   const int group = layer->group, n = static_cast<int>(n_tokens), digits = y_dtype == MLPMOE_FP32 ? 3 : 2;
-  if (n >= kWideFrom) return forward_wide(layer, x, x_dtype, x_stride, x_scale, x_group, select, compensate, residual, y, y_dtype, n, workspace, stream);
+  if (path == TENSOR) return forward_tc(layer, x, x_dtype, x_stride, x_scale, x_group, select, compensate, residual, y, n, workspace, stream);
+  if (path == WIDE)
+    return forward_wide(layer, x, x_dtype, x_stride, x_scale, x_group, select, compensate, residual, y, y_dtype, n, workspace, stream);
   W4Args u = {};
   u.m[0] = matrix(layer->gate, I, d, group);
   u.m[1] = matrix(layer->up, I, d, group);
@@ -327,7 +492,8 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
   u.x = x;
   u.x_kind = x_dtype;
   u.x_stride = x_stride;
-  u.h = static_cast<float*>(workspace);
+  u.h = reinterpret_cast<float*>(static_cast<char*>(workspace) + l.h);
+  u.status = static_cast<uint32_t*>(workspace);
 
   W4Args w = {};
   w.m[0] = w.m[1] = matrix(layer->down, d, I, group);
@@ -340,7 +506,7 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
   w.dense = u.dense;
   const int w_cluster = w4_plan(&w, digits, group);
   if (u_cluster == 0 || w_cluster == 0) return MLPMOE_ERR_UNSUPPORTED;
-  w.x = workspace;
+  w.x = u.h;
   w.x_kind = MLPMOE_FP32;
   w.x_stride = I;
   w.select = select;

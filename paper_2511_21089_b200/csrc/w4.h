@@ -32,6 +32,7 @@ struct W4Args {
   int rows;                 // rows of each
   int tiles;                // 16-row tiles: eight neurons (gate, up), or sixteen rows of W_down
   int tiles_per_block;
+  uint32_t* status;         // cleared where given
   int K, kblocks;           // columns, and ceil(K / 128)
   int entries;              // K-blocks of a block of the cluster at most, rounded up to an even number
   int n;                    // tokens
@@ -92,7 +93,38 @@ struct W4DigitsArgs {
   int K, kblocks, n, tokens, slots_per_token, slot_tiles;
   uint8_t* digits;
   float2* units;
+  uint32_t* status;             // cleared where given
 };
+
+// The same products on the 5th-generation tensor cores (w4_tc.cuh).
+struct W4TcArgs {
+  W4Mat m[2];
+  int rows, kblocks;
+  int n, tokens, pieces, ne;    // a chunk's tokens; bf16 pieces of an activation; columns of an epilogue warp, 32 or 64
+  const uint8_t* image;         // activations as w4_columns_kernel lays them out
+  int B, dense;
+  const uint8_t* select;
+  float* h;                     // gate|up
+  int compensate;               // down
+  const float* residual;
+  __nv_bfloat16* y;
+  uint32_t* status;
+  uint64_t wait_limit_ns;
+  uint32_t extra_arrivals;
+  int32_t off[kW4MaxBranches + 1];
+  float alpha[kW4MaxBranches];
+};
+struct W4ColumnsArgs {
+  const void* x;
+  int kind;
+  int64_t stride;
+  const float* x_scale;
+  int x_groups, x_group;
+  int K, kblocks, n, tokens, pieces, cols;
+  uint8_t* image;
+  uint32_t* status;             // cleared where given
+};
+cudaError_t launch_w4_columns(const W4ColumnsArgs& a, cudaStream_t st);
 
 // One launch per group width (w4_g32.cu, w4_g64.cu, w4_g128.cu); `cluster` = blocks that share K.
 #define MLPMOE_W4_LAUNCHES(G)                                                                     \
@@ -100,7 +132,9 @@ struct W4DigitsArgs {
   cudaError_t launch_w4_down_##G(const W4Args& a, int cluster, cudaStream_t st);                  \
   cudaError_t launch_w4_wide_gateup_##G(const W4WideArgs& a, int chunks, cudaStream_t st);        \
   cudaError_t launch_w4_wide_down_##G(const W4WideArgs& a, int cluster, int chunks, cudaStream_t st); \
-  cudaError_t launch_w4_digits_##G(const W4DigitsArgs& a, cudaStream_t st);
+  cudaError_t launch_w4_digits_##G(const W4DigitsArgs& a, cudaStream_t st);                       \
+  cudaError_t launch_w4_tc_gateup_##G(const W4TcArgs& a, int cluster, cudaStream_t st);           \
+  cudaError_t launch_w4_tc_down_##G(const W4TcArgs& a, int cluster, cudaStream_t st);
 MLPMOE_W4_LAUNCHES(32)
 MLPMOE_W4_LAUNCHES(64)
 MLPMOE_W4_LAUNCHES(128)

@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
   // gate|up waits for everything before it on the stream; by the time all its blocks have passed here only gate|up
   // itself is outstanding, so the down kernel, which then may start, reads weights and selection without a wait.
   if (GATEUP) ptx::griddep_wait();
+  if (GATEUP && a.status != nullptr && threadIdx.x == 0 && blockIdx.x == 0 && rank == 0 && chunk == 0) *a.status = kStatusOk;
   ptx::griddep_launch_dependents();
   if (!a.dense) {
     // what the chunk's tokens compute: [token][branch], and the branches of all of them

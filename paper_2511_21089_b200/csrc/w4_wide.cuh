@@ -15,6 +15,62 @@
 namespace mlpmoe {
 namespace w4 {
 
+// This block's K-blocks into s_list, in order: its share of all of them or, for a product over the intermediate activations
+// with a selection, of those with a neuron that a token of the chunk computes.  Returns how many; ends with a barrier.
+template <bool ALL>
+__device__ __forceinline__ int list_kblocks(int kblocks, int cluster, int rank, int dense, const uint8_t* select, int chunk, int tokens, int n,
+                                            int B, const int32_t* off, const float* alpha, int* s_list, uint8_t* s_live, int* s_n) {
+  const int threads = blockDim.x, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (ALL || dense) {
+    const int share = (kblocks + cluster - 1) / cluster, count = max(0, min(share, kblocks - rank * share));
+    for (int i = threadIdx.x; i < count; i += threads) s_list[i] = rank * share + i;
+    __syncthreads();
+    return count;
+  }
+  const int n_here = min(tokens, n - chunk * tokens);
+  for (int b = threadIdx.x; b < B; b += threads) s_live[b] = select == nullptr && alpha[b] != 0.0f;
+  __syncthreads();
+  if (select != nullptr) {
+    const uint8_t* sel = select + static_cast<int64_t>(chunk) * tokens * B;
+    for (int i = threadIdx.x; i < n_here * B; i += threads)
+      if (sel[i] != 0 && alpha[i % B] != 0.0f) s_live[i % B] = 1;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    int total = 0;
+    for (int pass = 0; pass < 2; ++pass) {        // count, then list this block's share
+      const int per = (total + cluster - 1) / cluster, first = rank * per;
+      int running = 0;
+      for (int base = 0; base < kblocks; base += 32) {
+        const int kb = base + lane;
+        bool live = false;
+        if (kb < kblocks)
+          for (int b = find_branch(off, B, kb * 128); b < B && off[b] < (kb + 1) * 128; ++b) live = live || s_live[b] != 0;
+        const unsigned who = __ballot_sync(0xFFFFFFFFu, live);
+        const int at = running + __popc(who & ((1u << lane) - 1u)) - first;
+        if (pass == 1 && live && at >= 0 && at < per) s_list[at] = kb;
+        running += __popc(who);
+      }
+      if (pass == 0) total = running;
+      else if (lane == 0) *s_n = max(0, min(per, total - first));
+    }
+  }
+  __syncthreads();
+  return *s_n;
+}
+
+// c_t: the quotient and the root in double, rounded once, as the routed forward does.
+__device__ __forceinline__ float token_factor(const uint8_t* select, const float* alpha, int B, int compensate) {
+  int k = 0, n_avail = 0;
+  for (int b = 0; b < B; ++b) {
+    const bool avail = alpha[b] != 0.0f;
+    n_avail += avail ? 1 : 0;
+    k += avail && select[b] != 0 ? 1 : 0;
+  }
+  if (k == 0) return 0.0f;
+  return compensate ? static_cast<float>(sqrt(static_cast<double>(n_avail) / static_cast<double>(k))) : 1.0f;
+}
+
 // A thread takes eight k of one token; the 16 / GPB threads of a group are neighbours.
 template <int GPB>
 __global__ void __launch_bounds__(256) w4_digits_kernel(const __grid_constant__ W4DigitsArgs a) {
@@ -22,6 +78,7 @@ __global__ void __launch_bounds__(256) w4_digits_kernel(const __grid_constant__ 
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (a.status != nullptr && i == 0) *a.status = kStatusOk;
   const int units = a.kblocks * 16, u = static_cast<int>(i % units), k8 = u & 15;
   const int64_t token = i / units;
   Raw raw;
@@ -73,7 +130,7 @@ template <int NTW, int GPB, bool GATEUP, bool ZERO>
 __global__ void __launch_bounds__(512, 1) w4_wide_kernel(const __grid_constant__ W4WideArgs a) {
   constexpr int kWords = 4 / GPB;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ int s_list[kW4MaxDim / 128 + 8];
+  __shared__ int s_list[kW4MaxDim / 128];
   __shared__ int s_n;
   __shared__ uint8_t s_live[kW4MaxBranches];
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
@@ -84,43 +141,8 @@ __global__ void __launch_bounds__(512, 1) w4_wide_kernel(const __grid_constant__
   const int st0 = cg * NTW;                       // first slot tile of the warp
   const int threads = blockDim.x;
 
-  // ---- this block's K-blocks: all of its share, or (down, with a selection) of those with a neuron that a token computes
-  const int share = (a.kblocks + cluster - 1) / cluster;
-  int n_entries = max(0, min(share, a.kblocks - rank * share));
-  if (GATEUP || a.dense) {
-    for (int i = threadIdx.x; i < n_entries; i += threads) s_list[i] = rank * share + i;
-  } else {
-    const int n_here = min(a.tokens, a.n - chunk * a.tokens);
-    for (int b = threadIdx.x; b < a.B; b += threads) s_live[b] = a.select == nullptr && a.alpha[b] != 0.0f;
-    __syncthreads();
-    if (a.select != nullptr) {
-      const uint8_t* sel = a.select + static_cast<int64_t>(chunk) * a.tokens * a.B;
-      for (int i = threadIdx.x; i < n_here * a.B; i += threads)
-        if (sel[i] != 0 && a.alpha[i % a.B] != 0.0f) s_live[i % a.B] = 1;
-    }
-    __syncthreads();
-    if (warp == 0) {                              // one warp lists the live K-blocks in order
-      int total = 0;
-      for (int pass = 0; pass < 2; ++pass) {
-        const int per = (total + cluster - 1) / cluster, first = rank * per;
-        int running = 0;
-        for (int base = 0; base < a.kblocks; base += 32) {
-          const int kb = base + lane;
-          bool live = false;
-          if (kb < a.kblocks)
-            for (int b = find_branch(a.off, a.B, kb * 128); b < a.B && a.off[b] < (kb + 1) * 128; ++b) live = live || s_live[b] != 0;
-          const unsigned who = __ballot_sync(0xFFFFFFFFu, live);
-          const int at = running + __popc(who & ((1u << lane) - 1u)) - first;
-          if (pass == 1 && live && at >= 0 && at < per) s_list[at] = kb;
-          running += __popc(who);
-        }
-        if (pass == 0) total = running;
-        else if (lane == 0) s_n = max(0, min(per, total - first));
-      }
-    }
-    __syncthreads();
-    n_entries = s_n;
-  }
+  const int n_entries = list_kblocks<GATEUP>(a.kblocks, cluster, rank, a.dense, a.select, chunk, a.tokens, a.n, a.B, a.off, a.alpha, s_list,
+                                             s_live, &s_n);
   // the kernel before this one writes the digits, and passed its own wait before this one could start: weights may be read
   ptx::griddep_launch_dependents();
   __syncthreads();
@@ -302,16 +324,7 @@ __global__ void __launch_bounds__(512, 1) w4_wide_kernel(const __grid_constant__
     return;
   }
   auto finish = [&](int token, int m, float v) {
-    if (a.select != nullptr) {
-      // c_t: the quotient and the root in double, rounded once, as the routed forward does
-      int k = 0, n_avail = 0;
-      for (int b = 0; b < a.B; ++b) {
-        const bool avail = a.alpha[b] != 0.0f;
-        n_avail += avail ? 1 : 0;
-        k += avail && a.select[static_cast<int64_t>(token) * a.B + b] != 0 ? 1 : 0;
-      }
-      v *= k == 0 ? 0.0f : (a.compensate ? static_cast<float>(sqrt(static_cast<double>(n_avail) / static_cast<double>(k))) : 1.0f);
-    }
+    if (a.select != nullptr) v *= token_factor(a.select + static_cast<int64_t>(token) * a.B, a.alpha, a.B, a.compensate);
     const int64_t at = static_cast<int64_t>(token) * a.rows + m;
     if (a.residual != nullptr) v += a.residual[at];
     if (a.y_bf16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);

@@ -393,6 +393,58 @@ def test_w4_forward_selection(lib, n, group):
     assert torch.equal(c.run(x, n, "bf16", "fp32", select=none, residual=dev(residual)), dev(residual))
 
 
+@pytest.mark.parametrize("group,asym", [(32, True), (64, False), (128, True)])
+def test_w4_forward_tensor_core_kernels(lib, group, asym):
+    """Layers large enough, with enough tokens and y in bf16, for the kernels of the 5th-generation tensor cores: ragged
+    d_model and d_inter, every type of x, chunks of one token less and more than they hold, selections."""
+    d, d_b = 1032, [1008, 2032, 16, 3008, 2064]
+    c = W4Case(lib, [group, 7], d, d_b, group, asym, alpha=[1.0, 0.7, 1.2, -0.6, 0.9], std=0.05)
+    rng = np.random.default_rng([group, 8])
+    for n, xt, x_group in ((17, "bf16", 0), (33, "fp32", 0), (64, "bf16", 0), (65, "bf16", 0), (40, "e4m3", 128), (130, "e4m3", 0)):
+        xh, x, sc = c.activations([n, 9], n, xt, x_group)
+        residual = rng.normal(size=(n, d)).astype(np.float32)
+        c.check(c.run(x, n, xt, "bf16", sc, x_group, residual=dev(residual)), xh, xt, "bf16", residual=residual)
+        sel = (rng.uniform(size=(n, 5)) < 0.4).astype(np.uint8)
+        sel[:, 3], sel[0] = 0, 0
+        for comp in (True, False):
+            c.check(c.run(x, n, xt, "bf16", sc, x_group, select=torch.from_numpy(sel).cuda(), compensate=comp), xh, xt, "bf16", sel, comp)
+    none = torch.zeros(130, 5, device="cuda", dtype=torch.uint8)
+    assert float(c.run(x, 130, "e4m3", "bf16", sc, 0, select=none).abs().max()) == 0
+    # alpha = 0 drops a branch without a selection; what it holds does not matter
+    c.alpha = [1.0, 0.0, 1.2, -0.6, 0.9]
+    c.layer = lib.mlpmoe_w4_layer(d, c.I, d_b, group, *c.mats, alpha=c.alpha)
+    c.mats[0][1][:, 1008:3040] = float("nan")
+    xh, x, _ = c.activations([64, 9], 64, "bf16")
+    c.check(c.run(x, 64, "bf16", "bf16"), xh, "bf16", "bf16")
+
+
+def test_w4_forward_wait_limit(lib):
+    """A wait inside the tensor cores' kernels that runs out: the call returns, the status says so, and the next call is
+    right again."""
+    d, d_b = 1032, [4064, 4064]
+    c = W4Case(lib, [55], d, d_b, 128, False, std=0.05)
+    xh, x, _ = c.activations([56], 64, "bf16")
+    size = lib.mlpmoe_w4_workspace(c.layer, 64)
+    ws, y = torch.empty(size, device="cuda", dtype=torch.uint8), torch.empty(64, d, device="cuda", dtype=torch.bfloat16)
+
+    def call():
+        lib.mlpmoe_w4_forward(c.layer, x, y, 64, ws, size, x_stride=x.stride(0), y_dtype=lib.MLPMOE_BF16, stream=stream_ptr())
+        return lib.mlpmoe_w4_get_status(ws, stream_ptr())
+    assert call() == lib.MLPMOE_OK
+    c.check(y, xh, "bf16", "bf16")
+    lib.mlpmoe_w4_debug_set_wait(20_000_000, 1)
+    try:
+        assert call() == lib.MLPMOE_ERR_DEVICE_TIMEOUT
+    finally:
+        lib.mlpmoe_w4_debug_set_wait()
+    y.zero_()
+    assert call() == lib.MLPMOE_OK
+    c.check(y, xh, "bf16", "bf16")
+    # the other kernels have no such waits and report so
+    lib.mlpmoe_w4_forward(c.layer, x, y, 3, ws, size, x_stride=x.stride(0), y_dtype=lib.MLPMOE_BF16, stream=stream_ptr())
+    assert lib.mlpmoe_w4_get_status(ws, stream_ptr()) == lib.MLPMOE_OK
+
+
 def test_w4_forward_residual_in_place_and_same_bits(lib):
     c = W4Case(lib, [77], 512, [128] * 8, 64, False)
     xh, x, _ = c.activations([5], 12, "bf16")
@@ -409,8 +461,9 @@ def test_w4_forward_residual_in_place_and_same_bits(lib):
     c.check(ys[0], xh, "bf16", "fp32", residual=r0)
 
 
-@pytest.mark.parametrize("d,I,n", [(896, 4864, 1), (896, 4864, 13), (4096, 14336, 1), (4096, 14336, 64)])
-def test_w4_forward_full_size(lib, d, I, n):
+@pytest.mark.parametrize("d,I,n,yt", [(896, 4864, 1, "fp32"), (896, 4864, 13, "fp32"), (4096, 14336, 1, "fp32"), (4096, 14336, 64, "fp32"),
+                                      (4096, 14336, 64, "bf16")])
+def test_w4_forward_full_size(lib, d, I, n, yt):
     """The Qwen- and Llama-shaped layers against float64 on the device, on weights that the library quantised itself."""
     gen = torch.Generator(device="cuda")
     gen.manual_seed(d + n)
@@ -430,20 +483,20 @@ def test_w4_forward_full_size(lib, d, I, n):
     x = torch.randn(n, d, device="cuda", generator=gen).bfloat16()
     layer = lib.mlpmoe_w4_layer(d, I, [I // 16] * 16, group, *mats)
     size = lib.mlpmoe_w4_workspace(layer, n)
-    ws, y = torch.empty(size, device="cuda", dtype=torch.uint8), torch.empty(n, d, device="cuda")
-    lib.mlpmoe_w4_forward(layer, x, y, n, ws, size, stream=stream_ptr())
+    ws, y = torch.empty(size, device="cuda", dtype=torch.uint8), torch.empty(n, d, device="cuda", dtype=TORCH[yt])
+    lib.mlpmoe_w4_forward(layer, x, y, n, ws, size, y_dtype=kind(lib, yt), stream=stream_ptr())
     xd = x.double()
     g, u = xd @ deq[0].t(), xd @ deq[1].t()
     h = torch.nn.functional.silu(g) * u
     # as W4Case.tolerance, on the device
-    q = 1.004 * 2.0 ** -23
+    q = 1.004 * (2.0 ** -23 if yt == "fp32" else 2.0 ** -15)
 
     def product(K, size, v, W):
         tops = v.abs().view(n, -1, group).amax(2)
         return 3 * U * (K / group + 30) * size + q * (tops @ W.abs().view(W.shape[0], -1, group).sum(2).t())
     eg, eu = (product(d, xd.abs() @ w.abs().t(), xd, w) for w in deq[:2])
     h_err = 1.1 * eg * (u.abs() + eu) + torch.nn.functional.silu(g).abs() * eu + (2.0 ** -20 + g.abs() * 2 * U) * h.abs()
-    tol = h_err @ deq[2].abs().t() + product(I, h.abs() @ deq[2].abs().t(), h.abs() + h_err, deq[2]) + 4 * U * (h @ deq[2].t()).abs() + 1e-30
+    tol = h_err @ deq[2].abs().t() + product(I, h.abs() @ deq[2].abs().t(), h.abs() + h_err, deq[2]) + (4 * U + (2.0 ** -8 if yt == "bf16" else 0)) * (h @ deq[2].t()).abs() + 1e-30
     assert bool(((y.double() - h @ deq[2].t()).abs() <= tol).all())
 
 
