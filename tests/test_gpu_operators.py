@@ -397,7 +397,7 @@ def test_w4_forward_selection(lib, n, group):
 def test_w4_forward_tensor_core_kernels(lib, group, asym):
     """Layers large enough, with enough tokens and y in bf16, for the kernels of the 5th-generation tensor cores: ragged
     d_model and d_inter, every type of x, chunks of one token less and more than they hold, selections."""
-    d, d_b = 1032, [1008, 2032, 16, 3008, 2064]
+    d, d_b = 1032, [1008, 2032, 16, 3008, 2944]
     c = W4Case(lib, [group, 7], d, d_b, group, asym, alpha=[1.0, 0.7, 1.2, -0.6, 0.9], std=0.05)
     rng = np.random.default_rng([group, 8])
     for n, xt, x_group in ((17, "bf16", 0), (33, "fp32", 0), (64, "bf16", 0), (65, "bf16", 0), (40, "e4m3", 128), (130, "e4m3", 0)):
@@ -421,7 +421,7 @@ def test_w4_forward_tensor_core_kernels(lib, group, asym):
 def test_w4_forward_wait_limit(lib):
     """A wait inside the tensor cores' kernels that runs out: the call returns, the status says so, and the next call is
     right again."""
-    d, d_b = 1032, [4064, 4064]
+    d, d_b = 1032, [4512, 4496]
     c = W4Case(lib, [55], d, d_b, 128, False, std=0.05)
     xh, x, _ = c.activations([56], 64, "bf16")
     size = lib.mlpmoe_w4_workspace(c.layer, 64)
