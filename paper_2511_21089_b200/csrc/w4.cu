@@ -178,29 +178,28 @@ Path path_of(const mlpmoe_w4_layer_t* l, int64_t n, mlpmoe_dtype_t y_dtype) {
   return y_dtype == MLPMOE_BF16 && n >= kTcFrom && 3 * l->d_model * l->d_inter >= kTcCodes ? TENSOR : WIDE;
 }
 
-// A chunk of the tensor cores' products: tokens, and the columns of an epilogue warp.  gate|up has 64 columns at most, down
-// 128, two per token.
+// A chunk of the tensor cores' products: tokens, and the columns of an epilogue warp, 32 or 64.  gate|up has one such set of columns
+// for each matrix, down two.
 struct TcChunk {
   int tokens, chunks, ne;
 };
-TcChunk tc_chunk(int64_t n, int pieces) {
+TcChunk tc_chunk(int64_t n, int sets) {
   TcChunk c;
-  const int64_t most = 64 / pieces;
+  const int64_t most = 64 * sets;
   c.chunks = static_cast<int>((n + most - 1) / most);
   c.tokens = static_cast<int>((n + c.chunks - 1) / c.chunks);
-  c.ne = c.tokens * pieces <= 32 ? 32 : 64;
+  c.ne = c.tokens <= 32 * sets ? 32 : 64;
   return c;
 }
-inline int x_pieces(mlpmoe_dtype_t x_dtype) { return x_dtype == MLPMOE_BF16 ? 1 : 2; }
-// The down product: two pieces, columns 2 ne.
-inline TcChunk tc_down_chunk(int64_t n) { return tc_chunk(n, 1); }
+inline TcChunk tc_up_chunk(int64_t n) { return tc_chunk(n, 1); }
+inline TcChunk tc_down_chunk(int64_t n) { return tc_chunk(n, 2); }
 
-// Workspace: a status word, the intermediate activations in fp32, then the activations of both products as the tiled kernels
-// (digits, units) or the tensor cores' kernels (images) read them.
+// Workspace: a status word, the intermediate activations in fp32 (the tensor cores' kernels have them only as an image), then the
+// activations of both products as the tiled kernels (digits, units) or the tensor cores' kernels (images) read them.
 struct Layout {
   int64_t h, x, x_units, y, y_units, total;
 };
-Layout layout_of(const mlpmoe_w4_layer_t* l, int64_t n, Path path, int digits, int pieces) {
+Layout layout_of(const mlpmoe_w4_layer_t* l, int64_t n, Path path, int digits) {
   Layout w;
   const int gpb = 128 / l->group;
   const int64_t xk = (l->d_model + 127) / 128, hk = (l->d_inter + 127) / 128;
@@ -209,12 +208,14 @@ Layout layout_of(const mlpmoe_w4_layer_t* l, int64_t n, Path path, int digits, i
     xb = digit_bytes(n, digits, xk, gpb, &xu);
     hb = digit_bytes(n, digits, hk, gpb, &hu);
   } else if (path == TENSOR) {
-    const TcChunk u = tc_chunk(n, pieces), d = tc_down_chunk(n);
+    const TcChunk u = tc_up_chunk(n), d = tc_down_chunk(n);
     xb = u.chunks * xk * u.ne * 256;
+    xu = up256(n * 4);
     hb = d.chunks * hk * d.ne * 512;
+    hu = d.chunks * hk * d.ne * 8;
   }
   w.h = 256;
-  w.x = w.h + up256(n * l->d_inter * 4);
+  w.x = w.h + (path == TENSOR ? 0 : up256(n * l->d_inter * 4));
   w.x_units = w.x + xb;
   w.y = w.x_units + xu;
   w.y_units = w.y + hb;
@@ -231,7 +232,7 @@ mlpmoe_status_t forward_wide(const mlpmoe_w4_layer_t* layer, const void* x, mlpm
                              mlpmoe_dtype_t y_dtype, int n, void* workspace, void* stream) {
   const int64_t d = layer->d_model, I = layer->d_inter;
   const int group = layer->group, pieces = y_dtype == MLPMOE_FP32 ? 3 : 2;
-  const Layout l = layout_of(layer, n, WIDE, pieces, 1);
+  const Layout l = layout_of(layer, n, WIDE, pieces);
   char* ws = static_cast<char*>(workspace);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
 
@@ -317,14 +318,30 @@ int tc_cluster(int64_t blocks, int64_t kblocks) {
   return best;
 }
 
-// Columns of x, gate|up, columns of h, down.
+// Codes as boxes of 128 rows x 64 bytes.
+bool code_map(CUtensorMap* map, const W4Mat& m, int64_t rows) {
+  using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                              const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static const Encode encode = [] {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool ok = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess;
+    return ok ? reinterpret_cast<Encode>(p) : nullptr;
+  }();
+  const cuuint64_t dim[2] = {static_cast<cuuint64_t>(m.pitch), static_cast<cuuint64_t>(rows)}, stride[1] = {static_cast<cuuint64_t>(m.pitch)};
+  const cuuint32_t box[2] = {64, 128}, one[2] = {1, 1};
+  return encode != nullptr && encode(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(m.q), dim, stride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                     CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Columns of x, gate|up, down.
 mlpmoe_status_t forward_tc(const mlpmoe_w4_layer_t* layer, const void* x, mlpmoe_dtype_t x_dtype, int64_t x_stride, const float* x_scale,
                            int64_t x_group, const uint8_t* select, int32_t compensate, const float* residual, void* y, int n,
                            void* workspace, void* stream) {
   const int64_t d = layer->d_model, I = layer->d_inter;
-  const int group = layer->group, pieces = x_pieces(x_dtype);
-  const Layout l = layout_of(layer, n, TENSOR, 2, pieces);
-  const TcChunk uc = tc_chunk(n, pieces), wc = tc_down_chunk(n);
+  const int group = layer->group;
+  const Layout l = layout_of(layer, n, TENSOR, 2);
+  const TcChunk uc = tc_up_chunk(n), wc = tc_down_chunk(n);
   char* ws = static_cast<char*>(workspace);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
 
@@ -335,9 +352,9 @@ mlpmoe_status_t forward_tc(const mlpmoe_w4_layer_t* layer, const void* x, mlpmoe
   u.kblocks = static_cast<int>((d + 127) / 128);
   u.n = n;
   u.tokens = uc.tokens;
-  u.pieces = pieces;
   u.ne = uc.ne;
   u.image = reinterpret_cast<uint8_t*>(ws + l.x);
+  u.unit = reinterpret_cast<float*>(ws + l.x_units);
   u.B = layer->B;
   u.select = select;
   u.dense = select == nullptr;
@@ -346,7 +363,10 @@ mlpmoe_status_t forward_tc(const mlpmoe_w4_layer_t* layer, const void* x, mlpmoe
     u.alpha[b] = layer->alpha ? layer->alpha[b] : 1.0f;
     if (u.alpha[b] == 0.0f) u.dense = 0;
   }
-  u.h = reinterpret_cast<float*>(ws + l.h);
+  u.h = reinterpret_cast<uint8_t*>(ws + l.y);
+  u.h_unit = reinterpret_cast<float*>(ws + l.y_units);
+  u.h_tokens = wc.tokens;
+  u.h_cols = 2 * wc.ne;
   u.status = reinterpret_cast<uint32_t*>(ws);
   u.wait_limit_ns = g_wait_limit_ns.load();
   u.extra_arrivals = g_extra_arrivals.load();
@@ -355,12 +375,13 @@ mlpmoe_status_t forward_tc(const mlpmoe_w4_layer_t* layer, const void* x, mlpmoe
   w.rows = static_cast<int>(d);
   w.kblocks = static_cast<int>((I + 127) / 128);
   w.tokens = wc.tokens;
-  w.pieces = 2;
   w.ne = wc.ne;
-  w.image = reinterpret_cast<uint8_t*>(ws + l.y);
+  w.image = u.h;
+  w.unit = u.h_unit;
   w.compensate = compensate ? 1 : 0;
   w.residual = residual;
   w.y = static_cast<__nv_bfloat16*>(y);
+  if (!code_map(&u.codes[0], u.m[0], I) || !code_map(&u.codes[1], u.m[1], I) || !code_map(&w.codes[0], w.m[0], d)) return MLPMOE_ERR_CUDA;
 
   W4ColumnsArgs p = {};
   p.x = x;
@@ -375,26 +396,13 @@ mlpmoe_status_t forward_tc(const mlpmoe_w4_layer_t* layer, const void* x, mlpmoe
   p.kblocks = u.kblocks;
   p.n = n;
   p.tokens = u.tokens;
-  p.pieces = pieces;
   p.cols = u.ne;
   p.image = const_cast<uint8_t*>(u.image);
+  p.unit = const_cast<float*>(u.unit);
   p.status = u.status;
-  W4ColumnsArgs q = {};
-  q.x = ws + l.h;
-  q.kind = MLPMOE_FP32;
-  q.stride = I;
-  q.K = static_cast<int>(I);
-  q.kblocks = w.kblocks;
-  q.n = n;
-  q.tokens = w.tokens;
-  q.pieces = 2;
-  q.cols = 2 * w.ne;
-  q.image = const_cast<uint8_t*>(w.image);
-
   pdl_overlap_enabled() = true;
   if (launch_w4_columns(p, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
   if (BY_GROUP(tc_gateup, group, u, tc_cluster((I + 127) / 128 * uc.chunks, u.kblocks), st) != cudaSuccess) return MLPMOE_ERR_CUDA;
-  if (launch_w4_columns(q, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
   return BY_GROUP(tc_down, group, w, tc_cluster((d + 127) / 128 * wc.chunks, w.kblocks), st) == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
 }
 
@@ -414,8 +422,8 @@ mlpmoe_status_t mlpmoe_w4_workspace(const mlpmoe_w4_layer_t* layer, int64_t n_to
   // the most that a call with any types needs
   *bytes = 0;
   for (int k = 2; k <= 3; ++k) {
-    const int64_t wide = layout_of(layer, n_tokens, path_of(layer, n_tokens, MLPMOE_FP32), k, 1).total;
-    const int64_t tensor = layout_of(layer, n_tokens, path_of(layer, n_tokens, MLPMOE_BF16), k, k - 1).total;
+    const int64_t wide = layout_of(layer, n_tokens, path_of(layer, n_tokens, MLPMOE_FP32), k).total;
+    const int64_t tensor = layout_of(layer, n_tokens, path_of(layer, n_tokens, MLPMOE_BF16), k).total;
     if (wide > *bytes) *bytes = wide;
     if (tensor > *bytes) *bytes = tensor;
   }
@@ -460,7 +468,7 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
   if (residual && residual == y && y_dtype != MLPMOE_FP32) return MLPMOE_ERR_INVALID_ARG;
 
   const Path path = path_of(layer, n_tokens, y_dtype);
-  const Layout l = layout_of(layer, n_tokens, path, y_dtype == MLPMOE_FP32 ? 3 : 2, x_pieces(x_dtype));
+  const Layout l = layout_of(layer, n_tokens, path, y_dtype == MLPMOE_FP32 ? 3 : 2);
   if (!workspace || workspace_bytes < l.total || !on(workspace, 256)) return MLPMOE_ERR_INVALID_ARG;
 
   const int group = layer->group, n = static_cast<int>(n_tokens), digits = y_dtype == MLPMOE_FP32 ? 3 : 2;

@@ -98,13 +98,17 @@ struct W4DigitsArgs {
 
 // The same products on the 5th-generation tensor cores (w4_tc.cuh).
 struct W4TcArgs {
+  alignas(64) CUtensorMap codes[2];             // boxes of 128 rows x 64 bytes, 64-byte swizzle
   W4Mat m[2];
   int rows, kblocks;
-  int n, tokens, pieces, ne;    // a chunk's tokens; bf16 pieces of an activation; columns of an epilogue warp, 32 or 64
+  int n, tokens, ne;            // a chunk's tokens; columns of an epilogue warp, 32 or 64
   const uint8_t* image;         // activations as w4_columns_kernel lays them out
+  const float* unit;            // gate|up: [token]; down: [chunk][K-block][column]
   int B, dense;
   const uint8_t* select;
-  float* h;                     // gate|up
+  uint8_t* h;                   // gate|up: the intermediate activations as the down product's image and units, h_tokens a chunk
+  float* h_unit;
+  int h_tokens, h_cols;
   int compensate;               // down
   const float* residual;
   __nv_bfloat16* y;
@@ -120,8 +124,9 @@ struct W4ColumnsArgs {
   int64_t stride;
   const float* x_scale;
   int x_groups, x_group;
-  int K, kblocks, n, tokens, pieces, cols;
+  int K, kblocks, n, tokens, cols;
   uint8_t* image;
+  float* unit;
   uint32_t* status;             // cleared where given
 };
 cudaError_t launch_w4_columns(const W4ColumnsArgs& a, cudaStream_t st);

@@ -103,6 +103,13 @@ __device__ __forceinline__ float ld_cluster_f32(const float* p, uint32_t rank) {
   return v;
 }
 
+__device__ __forceinline__ float4 ld_cluster_f32x4(const float* p, uint32_t rank) {
+  float4 v;
+  const uint32_t addr = ptx::map_to_cta(ptx::smem_u32(p), rank);
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+
 // The last b with first[b] <= value, first ascending.
 __device__ __forceinline__ int find_branch(const int* first, int B, int value) {
   int lo = 0, hi = B;

@@ -1,101 +1,228 @@
 // The layer on 4-bit weights for batches large enough for the 5th-generation tensor cores (y in bf16).
 //
-// The codes become bf16 whole numbers code - zero (exact) in shared memory, in the 128-byte-swizzled K-major form that
-// tcgen05.mma reads, the activations come prepared in the same form (w4_columns_kernel: one bf16 piece of x, or two
-// pieces where x or the intermediate activation has more bits; 2^-16 of the value is left out, y is rounded to 2^-8),
-// and the products of one group of K (32, 64 or 128 columns) accumulate in tensor memory.  Two accumulators alternate:
-// while the tensor core fills one, the epilogue warps read the other back and add it, times the row's scale, to their fp32
-// sums in registers.
-// What it spends per 128 columns of K, 128 neurons and 64 tokens: 64 KB written and 96 KB read in shared memory, about
-// 1300 cycles of an SM, and 660 of issue, where mma.sync (w4_wide.cuh) needs 5000.
+// The codes become fp16 whole numbers code - zero (exact) in tensor memory, where tcgen05.mma takes its first operand
+// from; the activations come as its second, 128-byte-swizzled in shared memory: fp16 times a unit, a power of two of the token
+// (x) or of the token and 128 columns (the intermediate activation, whose row is not known as a whole when it is
+// written) that brings the largest to 2^14..2^15.  What is below 2^-28 of the largest loses bits; of the rest 2^-12 is left
+// out (nothing for x in bf16), where y is rounded to 2^-9.  The products of one group of K (32, 64 or 128 columns)
+// accumulate in tensor memory too.  Two accumulators alternate: while the tensor core fills one, the epilogue warps read
+// the other back and add it, times the row's scale, to their fp32 sums in registers.
 //
 // A block: 128 neurons (128 gate rows and 128 up rows) or 128 rows of W_down.  Warps 0..7 epilogue (tensor memory lanes
-// 32 (warp % 4).., columns NE (warp / 4)..), 8..15 codes to bf16, 16 issues the MMAs, 17 fetches the activations.
+// 32 (warp % 4).., columns NE (warp / 4)..), 8..15 codes to fp16 (the same lanes), 16 issues the MMAs, 17 copies the
+// codes, 18 scales and zeros, 19 the activations.
 #pragma once
 #include "w4_wide.cuh"
 
 namespace mlpmoe {
 namespace w4 {
 
-constexpr int kTcThreads = 18 * 32;
-constexpr int kTcTile = 128 * 128 * 2;            // one matrix's operand of a stage: 128 rows x 128 columns of bf16
+constexpr int kTcThreads = 20 * 32;
 
-template <int NE, bool GATEUP>
+template <int NE, int GPB, bool GATEUP>
 struct TcCfg {
   static constexpr int kMats = GATEUP ? 2 : 1;
   static constexpr int kCols = GATEUP ? NE : 2 * NE;             // columns of an MMA
-  static constexpr int kStages = GATEUP ? 2 : 3;
+  // Tensor memory: two accumulators of 2 NE columns, then the first operand's stages, each 64 columns: half a block of K of both
+  // matrices or a block of W_down's, two values a column.
+  static constexpr int kParts = GATEUP ? 2 : 1, kOperand = 64 / kMats, kOperands = 4 * NE;
+  static constexpr int kFit = (512 - kOperands) / 64;
+  static constexpr int kStages = kFit < 6 ? kFit : 6;
+  // Shared memory: stages of one block of K, each the activations, the codes, scales and zeros of 128 rows and the units.
   static constexpr int kB = kCols * 256;
-  static constexpr int kStage = kMats * kTcTile + kB;
-  static constexpr int kBars = kStages * kStage;
-  static constexpr int kSmem = kBars + 256 + 1024;               // barriers, slack for 1024-byte alignment
-  static constexpr int kTmem = 4 * NE;                           // two accumulators of 2 NE columns
+  static constexpr int kCodes = kB, kScales = kCodes + kMats * 8192, kZeros = kScales + kMats * GPB * 256, kUnits = kZeros + kMats * GPB * 128;
+  static constexpr int kStage = (kUnits + (GATEUP ? 0 : kCols * 4) + 1023) / 1024 * 1024;
+  static constexpr int kMost = (232448 - 6144) / kStage, kRing = kMost < 8 ? kMost : 8;
+  static constexpr int kSums = 2 * NE * 128 * 4;                 // [column][row], over the stages at the end
+  static constexpr int kBars = kRing * kStage > kSums ? kRing * kStage : kSums;
+  static constexpr int kSmem = kBars + 512 + 1024;               // barriers, slack for 1024-byte alignment
 };
 
-// Eight codes -> four bf16 pairs code - zero, pairs (e, e + 4) of eight consecutive columns; bias = (128 + zero) twice.  The
-// code slides into the mantissa of 128.0; the difference is exact.
-__device__ __forceinline__ uint4 unpack_bf16(uint32_t w, uint32_t bias) {
-  uint32_t p[4];
+// Eight codes -> four fp16 pairs code - zero, pairs (e, e + 4) of eight consecutive columns.  The code slides into the mantissa of
+// 1024.0, as it is or times 16, which a multiplication by 1/16 takes back: one shift for two pairs.  All of it is exact.
+// bias = -(1024 + zero) and -(64 + zero), twice each.
+struct Bias {
+  __half2 one, sixteen;
+};
+__device__ __forceinline__ Bias bias_of(uint32_t zero) {
+  const uint32_t bits = 0xE400E400u + zero * 0x00010001u;
+  const __half2 one = *reinterpret_cast<const __half2*>(&bits);
+  return {one, __hadd2(one, __floats2half2_rn(960.0f, 960.0f))};
+}
+__device__ __forceinline__ void unpack_f16(uint32_t w, const Bias& bias, uint32_t* p) {
+  const __half2 sixteenth = __floats2half2_rn(0.0625f, 0.0625f);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
+    const uint32_t from = i < 2 ? w : w >> 8;
     uint32_t u;
-    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(u) : "r"(w >> (4 * i)), "r"(0x000F000Fu), "r"(0x43004300u));
-    const __nv_bfloat162 v = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u), *reinterpret_cast<const __nv_bfloat162*>(&bias));
-    p[i] = *reinterpret_cast<const uint32_t*>(&v);
+    asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(u) : "r"(from), "r"(i % 2 ? 0x00F000F0u : 0x000F000Fu), "r"(0x64006400u));
+    const __half2 v = *reinterpret_cast<const __half2*>(&u), o = i % 2 ? __hfma2(v, sixteenth, bias.sixteen) : __hadd2(v, bias.one);
+    p[i] = *reinterpret_cast<const uint32_t*>(&o);
   }
-  return make_uint4(p[0], p[1], p[2], p[3]);
 }
 
-// Activations as the MMAs' second operand: per chunk and K-block, two halves of 64 columns of K, each `cols` rows of 128 bytes
-// under the 128-byte swizzle; row p tokens + tok holds piece p of token tok.  A thread takes eight k of one token.
+// The unit for values of at most `top`, and its reciprocal.  Infinities and NaN pass through.
+__device__ __forceinline__ float unit_of(float top, float* inverse) {
+  const int e = min(max(static_cast<int>(__float_as_uint(top) >> 23), 32), 255);      // biased exponent; 2^-95 and below share a unit
+  const bool one = e == 255;
+  *inverse = one ? 1.0f : __uint_as_float(static_cast<uint32_t>(268 - e) << 23);        // 2^(14 - (e - 127))
+  return one ? 1.0f : __uint_as_float(static_cast<uint32_t>(e - 14) << 23);
+}
+
+// Eight k's as part of row c of an image's half.
+__device__ __forceinline__ void store_column(uint8_t* half, int c, int k8, const float* v, float inverse) {
+  uint32_t o[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const __half2 pair = __floats2half2_rn(v[e] * inverse, v[e + 4] * inverse);
+    o[e] = *reinterpret_cast<const uint32_t*>(&pair);
+  }
+  *reinterpret_cast<uint4*>(half + c * 128 + (((k8 & 7) ^ (c & 7)) * 16)) = make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// x as the MMAs' second operand: per chunk and K-block, two halves of 64 columns of K, each `cols` rows of 128 bytes under the
+// 128-byte swizzle; a row is a token.  A block takes one token, a thread eight k at a time; the second reading is from the
+// caches.
 static __global__ void __launch_bounds__(256) w4_columns_kernel(const __grid_constant__ W4ColumnsArgs a) {
+  __shared__ float s_top[8];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (a.status != nullptr && i == 0) *a.status = kStatusOk;
-  const int units = a.kblocks * 16, u = static_cast<int>(i % units), k8 = u & 15;
-  const int64_t token = i / units;
-  if (token >= a.n) return;
-  float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-  if (u * 8 < a.K) {
-    to_f32(load_raw(a.x, a.kind, token * a.stride + u * 8), a.kind, v);
-    if (a.x_scale != nullptr) {
-      const float s = a.x_scale[token * a.x_groups + (a.x_groups == 1 ? 0 : u * 8 / a.x_group)];
+  const int64_t token = blockIdx.x;
+  if (a.status != nullptr && token == 0 && threadIdx.x == 0) *a.status = kStatusOk;
+  auto load = [&](int u, float (&v)[8]) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= s;
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    if (u * 8 < a.K) {
+      to_f32(load_raw(a.x, a.kind, token * a.stride + u * 8), a.kind, v);
+      if (a.x_scale != nullptr) {
+        const float s = a.x_scale[token * a.x_groups + (a.x_groups == 1 ? 0 : u * 8 / a.x_group)];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= s;
+      }
     }
+  };
+  float top = 0.0f;
+  for (int u = threadIdx.x; u * 8 < a.K; u += 256) {
+    float v[8];
+    load(u, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
   }
-  const int chunk = static_cast<int>(token / a.tokens);
-  uint8_t* half = a.image + ((static_cast<int64_t>(chunk) * a.kblocks + u / 16) * 2 + (k8 >> 3)) * (a.cols * 128);
-  for (int p = 0; p < a.pieces; ++p) {
-    const int c = p * a.tokens + static_cast<int>(token % a.tokens);
-    uint32_t o[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const __nv_bfloat162 pair = __floats2bfloat162_rn(v[e], v[e + 4]);
-      v[e] -= __low2float(pair);
-      v[e + 4] -= __high2float(pair);
-      o[e] = *reinterpret_cast<const uint32_t*>(&pair);
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+  if (threadIdx.x % 32 == 0) s_top[threadIdx.x / 32] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 8; ++w) top = fmaxf(top, s_top[w]);
+  float inverse;
+  const float unit = unit_of(top, &inverse);
+  if (threadIdx.x == 0) a.unit[token] = unit;
+  const int chunk = static_cast<int>(token / a.tokens), c = static_cast<int>(token % a.tokens);
+  for (int u = threadIdx.x; u < a.kblocks * 16; u += 256) {
+    float v[8];
+    load(u, v);
+    store_column(a.image + ((static_cast<int64_t>(chunk) * a.kblocks + u / 16) * 2 + (u >> 3 & 1)) * (a.cols * 128), c, u & 15, v, inverse);
+  }
+}
+
+// What a block writes, from the [column][row] sums of all CL blocks of its cluster.  A thread takes eight rows of one token.
+template <int CL, int NE, bool GATEUP>
+__device__ __forceinline__ void tc_outputs(const W4TcArgs& a, const float* sums, const float* factor) {
+  const int chunk = blockIdx.z, rank = blockIdx.y, n_here = min(a.tokens, a.n - chunk * a.tokens);
+  auto total_of = [&](int col, int r, float* v) {
+    const float* at = sums + col * 128 + r;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+    constexpr int kAtOnce = CL < 4 ? CL : 4;
+#pragma unroll
+    for (int k0 = 0; k0 < CL; k0 += kAtOnce) {
+      float4 part[kAtOnce][2];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) part[k][q] = CL == 1 ? reinterpret_cast<const float4*>(at)[q] : ld_cluster_f32x4(at + 4 * q, k0 + k);
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          v[4 * q] += part[k][q].x;
+          v[4 * q + 1] += part[k][q].y;
+          v[4 * q + 2] += part[k][q].z;
+          v[4 * q + 3] += part[k][q].w;
+        }
     }
-    *reinterpret_cast<uint4*>(half + c * 128 + (((k8 & 7) ^ (c & 7)) * 16)) = make_uint4(o[0], o[1], o[2], o[3]);
+  };
+  for (int i = rank * kTcThreads + threadIdx.x; i < n_here * 16; i += CL * kTcThreads) {
+    const int tok = i >> 4, k8 = i & 15, row = blockIdx.x * 128 + 8 * k8, token = chunk * a.tokens + tok;
+    float v[8];
+    if (GATEUP) {
+      bool on = row < a.rows;
+      const int b = find_branch(a.off, a.B, row);             // the eight rows are one branch's: its width is a multiple of 16
+      const float alpha = a.alpha[b];
+      on = on && alpha != 0.0f && (a.select == nullptr || a.select[static_cast<int64_t>(token) * a.B + b] != 0);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+      if (on) {
+        float up[8];
+        const float unit = factor[tok];
+        total_of(tok, 8 * k8, v);
+        total_of(NE + tok, 8 * k8, up);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float gate = v[e] * unit;
+          // __expf is off by 2 + 1.2 |gate| units in the last place, the quotient by 2; with expf and the exact quotient these
+          // lines took a quarter of what the block spends behind its last product
+          v[e] = __fdividef(gate, 1.0f + __expf(-gate)) * (up[e] * unit) * alpha;
+        }
+      }
+      // these 128 rows are one block of the down product's K; a token's 16 threads are one half of a warp
+      float top = 0.0f, inverse;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFu << (threadIdx.x & 16), top, o));
+      const float unit = unit_of(top, &inverse);
+      const int64_t block = static_cast<int64_t>(token / a.h_tokens) * gridDim.x + blockIdx.x;
+      const int c = token % a.h_tokens;
+      store_column(a.h + (block * 2 + (k8 >> 3)) * (a.h_cols * 128), c, k8, v, inverse);
+      if (k8 == 0) a.h_unit[block * a.h_cols + c] = unit;
+    } else if (row < a.rows) {
+      total_of(tok, 8 * k8, v);
+      const int64_t at = static_cast<int64_t>(token) * a.rows + row;
+      uint32_t o[4];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (a.select != nullptr) v[e] *= factor[tok];
+        if (a.residual != nullptr) v[e] += a.residual[at + e];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const __nv_bfloat162 pair = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+        o[e] = *reinterpret_cast<const uint32_t*>(&pair);
+      }
+      *reinterpret_cast<uint4*>(a.y + at) = make_uint4(o[0], o[1], o[2], o[3]);
+    }
   }
 }
 
 // grid: (blocks of 128 rows, cluster along K, chunks)
 template <int NE, int GPB, bool GATEUP, bool ZERO>
 __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_constant__ W4TcArgs a) {
-  using C = TcCfg<NE, GATEUP>;
+  using C = TcCfg<NE, GPB, GATEUP>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ int s_list[kW4MaxDim / 128];
   __shared__ int s_n;
+  __shared__ float s_factor[128];                 // per token: gate|up x's unit, down the selection's factor
   __shared__ uint8_t s_live[kW4MaxBranches];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint64_t* full_a = reinterpret_cast<uint64_t*>(smem + C::kBars);
-  uint64_t* full_b = full_a + C::kStages;
-  uint64_t* empty = full_b + C::kStages;
-  uint64_t* d_full = empty + C::kStages;
+  uint64_t* empty_a = full_a + C::kStages;
+  uint64_t* full = empty_a + C::kStages;
+  uint64_t* empty = full + C::kRing;
+  uint64_t* d_full = empty + C::kRing;
   uint64_t* d_empty = d_full + 2;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(d_empty + 2);
+  uint64_t* drained = d_empty + 2;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
   volatile uint32_t* abort_flag = tmem_slot + 1;
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int chunk = blockIdx.z, rank = blockIdx.y, cluster = gridDim.y;
@@ -103,19 +230,25 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
-      ptx::mbar_init(&full_a[s], 256 + a.extra_arrivals);
-      ptx::mbar_init(&full_b[s], 1);
-      ptx::mbar_init(&empty[s], 1);
+      ptx::mbar_init(&full_a[s], 8 + a.extra_arrivals);
+      ptx::mbar_init(&empty_a[s], 1);
+    }
+    for (int s = 0; s < C::kRing; ++s) {
+      ptx::mbar_init(&full[s], 3);
+      ptx::mbar_init(&empty[s], 17);              // eight warps of either kind, and the MMAs
     }
     for (int b = 0; b < 2; ++b) {
       ptx::mbar_init(&d_full[b], 1);
       ptx::mbar_init(&d_empty[b], 8);
     }
+    ptx::mbar_init(drained, 1);
     *abort_flag = 0;
     ptx::fence_barrier_init();
   }
+  // 61,440 of an SM's 65,536 registers are this block's: no second block that takes tensor memory fits beside it, so the
+  // allocation waits for nobody who waits for this cluster.
   if (warp == 16) {
-    ptx::tmem_alloc(tmem_slot, C::kTmem);
+    ptx::tmem_alloc(tmem_slot, 512);
     ptx::tmem_relinquish();
   }
   const int n_entries = list_kblocks<GATEUP>(a.kblocks, cluster, rank, a.dense, a.select, chunk, a.tokens, a.n, a.B, a.off, a.alpha, s_list,
@@ -129,165 +262,222 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
 
   if (warp < 8) {
     // ------------------------------------------------------------- sums of the groups
-    const int quad = warp % 4, half = warp / 4, row = row0 + quad * 32 + lane;
-    const W4Mat& m = a.m[GATEUP ? half : 0];
-    const __nv_bfloat16* scale = m.scale + min(row, a.rows - 1);
-    const int64_t rows16 = m.rows16;
-    const int last_group = static_cast<int>(m.n_groups) - 1, steps = n_entries * GPB;
-    auto load_scale = [&](int step) {
-      return step < steps ? __bfloat162float(scale[min(s_list[step / GPB] * GPB + step % GPB, last_group) * rows16]) : 0.0f;
-    };
+    if (!GATEUP && a.select != nullptr && threadIdx.x < 128 && chunk * a.tokens + static_cast<int>(threadIdx.x) < min(a.n, (chunk + 1) * a.tokens))
+      s_factor[threadIdx.x] = token_factor(a.select + (static_cast<int64_t>(chunk) * a.tokens + threadIdx.x) * a.B, a.alpha, a.B, a.compensate);
+    const int quad = warp % 4, half = warp / 4;
+    const int steps = n_entries * GPB;
+    const int at_scale = C::kScales + (GATEUP ? half * GPB * 256 : 0) + (quad * 32 + lane) * 2, at_unit = C::kUnits + half * NE * 4;
+    int stage = 0;
+    uint32_t phase = 0;
     float acc[NE];
 #pragma unroll
     for (int i = 0; i < NE; ++i) acc[i] = 0.0f;
-    float s_next = load_scale(0);
     const uint32_t taddr = tmem + static_cast<uint32_t>(half * NE) + (static_cast<uint32_t>(quad * 32) << 16);
     for (int step = 0; step < steps; ++step) {
-      const float s = s_next;
-      s_next = load_scale(step + 1);
+      bool ok = step % GPB != 0 || ptx::mbar_wait_bounded(&full[stage], phase, abort_flag, a.wait_limit_ns);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      const uint8_t* in = smem + stage * C::kStage;
+      const float s = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(in + at_scale + step % GPB * 256));
       const int b = step & 1;
-      bool ok = ptx::mbar_wait_bounded(&d_full[b], (step >> 1) & 1, abort_flag, a.wait_limit_ns);
+      ok = ptx::mbar_wait_bounded(&d_full[b], (step >> 1) & 1, abort_flag, a.wait_limit_ns);
       ok = __all_sync(0xFFFFFFFFu, ok);
       if (!ok) break;
       ptx::tc_fence_after();
-      constexpr int kPart = NE == 64 ? 16 : 32;   // what the registers hold beside the sums
+      constexpr int kPart = NE == 64 ? (GATEUP ? 16 : 8) : 32;   // what the registers hold beside the sums
 #pragma unroll
       for (int i = 0; i < NE; i += kPart) {
         uint32_t r[kPart];
         if constexpr (kPart == 32) ptx::tmem_ld_32x32(taddr + b * 2 * NE + i, r);
-        else ptx::tmem_ld_32x16(taddr + b * 2 * NE + i, r);
+        else if constexpr (kPart == 16) ptx::tmem_ld_32x16(taddr + b * 2 * NE + i, r);
+        else ptx::tmem_ld_32x8(taddr + b * 2 * NE + i, r);
         ptx::tmem_ld_wait();
 #pragma unroll
-        for (int k = 0; k < kPart; ++k) acc[i + k] += __uint_as_float(r[k]) * s;
+        for (int k = 0; k < kPart; k += 4) {
+          if constexpr (GATEUP) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[i + k + q] += __uint_as_float(r[k + q]) * s;
+          } else {                                // a scale (8 bits) times a power of two is exact
+            const float4 u = *reinterpret_cast<const float4*>(in + at_unit + (i + k) * 4);
+            acc[i + k] += __uint_as_float(r[k]) * (s * u.x);
+            acc[i + k + 1] += __uint_as_float(r[k + 1]) * (s * u.y);
+            acc[i + k + 2] += __uint_as_float(r[k + 2]) * (s * u.z);
+            acc[i + k + 3] += __uint_as_float(r[k + 3]) * (s * u.w);
+          }
+        }
       }
       ptx::tc_fence_before();
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&d_empty[b]);
+      if (step % GPB == GPB - 1) {
+        if (lane == 0) ptx::mbar_arrive(&empty[stage]);
+        if (++stage == C::kRing) stage = 0, phase ^= 1u;
+      }
     }
     __syncwarp();
-    // every MMA of the block is complete once the last accumulator was: the stages are free
+    // every MMA of the block is complete once the last accumulator was, and no copy is under way: once the eight warps have
+    // read the last scales the stages are free
+    asm volatile("bar.sync 1, 256;" ::: "memory");
     float* sums = reinterpret_cast<float*>(smem) + half * NE * 128 + quad * 32 + lane;      // [column][row]
 #pragma unroll
     for (int i = 0; i < NE; ++i) sums[i * 128] = acc[i];
   } else if (warp < 16) {
     // ------------------------------------------------------------- codes to bf16
-    constexpr int kItems = 2 * C::kMats;          // 16 bytes of codes each: rows t / 4 + 64 i, columns 32 (t % 4)..
-    const int t = threadIdx.x - 256, c = t & 3;
-    const uint8_t* src[kItems];
-    const uint8_t* zsrc[kItems];
-#pragma unroll
-    for (int i = 0; i < kItems; ++i) {
-      const W4Mat& m = i < 2 ? a.m[0] : a.m[1];
-      const int row = min(row0 + (((t >> 2) + 64 * i) & 127), a.rows - 1);
-      src[i] = m.q + row * m.pitch;
-      zsrc[i] = ZERO && m.zero != nullptr ? m.zero + row : nullptr;
-    }
-    const uint32_t last_byte = static_cast<uint32_t>(a.m[0].pitch) - 16;
-    const int last_group = static_cast<int>(a.m[0].n_groups) - 1, group = c * GPB / 4;
-    const int64_t rows16 = a.m[0].rows16;
-    uint4 code[2][kItems];
-    uint32_t zero[2][kItems];
-    auto fetch = [&](int e, int u) {
-      if (e >= n_entries) return;
-      const int kb = s_list[e];
-#pragma unroll
-      for (int i = 0; i < kItems; ++i) {
-        code[u][i] = *reinterpret_cast<const uint4*>(src[i] + min(static_cast<uint32_t>(kb) * 64 + c * 16, last_byte));
-        if (ZERO) zero[u][i] = zsrc[i] != nullptr ? zsrc[i][min(kb * GPB + group, last_group) * rows16] : 8u;
-      }
-    };
-    fetch(0, 0);
-    fetch(1, 1);
-    int stage = 0;
-    uint32_t phase = 0;
+    // gate|up: a warp takes 32 rows of one matrix; down: of half of the columns.  32 columns (16 bytes) at a time, 64 to a
+    // stage of the operand.
+    constexpr int kChunks = 2 * C::kParts, kZeros = GPB * kChunks > 4 ? GPB * kChunks / 4 : 1;      // groups that the warp's columns touch
+    const int quad = warp % 4, part = (warp - 8) / 4, chunk0 = GATEUP ? 0 : 2 * part, r = quad * 32 + lane;
+    const bool has_zero = ZERO && a.m[GATEUP ? part : 0].zero != nullptr;
+    const int at_codes = C::kCodes + (GATEUP ? part * 8192 : 0) + r * 64;
+    const int at_zero = C::kZeros + (GATEUP ? part * GPB * 128 : chunk0 * GPB / 4 * 128) + r;
+    const uint32_t to = tmem + C::kOperands + (GATEUP ? part * C::kOperand : chunk0 * 16) + (static_cast<uint32_t>(quad * 32) << 16);
+    int stage = 0, slot = 0;
+    uint32_t phase = 0, slot_phase = 0;
     bool ok = true;
-    for (int e = 0; ok && e < n_entries; e += 2) {
+    for (int e = 0; ok && e < n_entries; ++e) {
+      ok = ptx::mbar_wait_bounded(&full[slot], slot_phase, abort_flag, a.wait_limit_ns);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      const uint8_t* in = smem + slot * C::kStage;
+      uint4 c[kChunks];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        if (e + u >= n_entries) break;
-        ok = ptx::mbar_wait_bounded(&empty[stage], phase ^ 1u, abort_flag, a.wait_limit_ns);
+      for (int i = 0; i < kChunks; ++i) c[i] = *reinterpret_cast<const uint4*>(in + at_codes + (((chunk0 + i) ^ (r >> 1 & 3)) * 16));
+      Bias bias[kZeros];
+#pragma unroll
+      for (int j = 0; j < kZeros; ++j) bias[j] = bias_of(has_zero ? in[at_zero + j * 128] : 8u);
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&empty[slot]);
+      if (++slot == C::kRing) slot = 0, slot_phase ^= 1u;
+#pragma unroll
+      for (int h = 0; h < C::kParts; ++h) {
+        uint32_t p[2][16];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int i = 2 * h + j;
+          const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) unpack_f16(w[k], bias[i * kZeros / kChunks], p[j] + 4 * k);
+        }
+        ok = ptx::mbar_wait_bounded(&empty_a[stage], phase ^ 1u, abort_flag, a.wait_limit_ns);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
+        ptx::tc_fence_after();
 #pragma unroll
-        for (int i = 0; i < kItems; ++i) {
-          const int r = (t >> 2) + 64 * (i & 1);  // row of its matrix's operand
-          uint8_t* to = smem + stage * C::kStage + (i >> 1) * kTcTile + (c >> 1) * (kTcTile / 2) + r * 128;
-          const uint32_t bias = ZERO ? 0x43004300u + zero[u][i] * 0x00010001u : 0x43084308u;
-          // the lanes of the second half of K store their words in another order, so that eight lanes meet eight banks
-          const uint4 q = code[u][i];
-          const uint32_t w[4] = {c & 2 ? q.z : q.x, c & 2 ? q.w : q.y, c & 2 ? q.x : q.z, c & 2 ? q.y : q.w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int j = (c & 1) * 4 + (k ^ (c & 2));          // 16-byte unit of the 128-byte row
-            *reinterpret_cast<uint4*>(to + ((j ^ (r & 7)) * 16)) = unpack_bf16(w[k], bias);
-          }
-        }
-        ptx::fence_proxy_async_smem();
-        ptx::mbar_arrive(&full_a[stage]);
-        fetch(e + u + 2, u);
+        for (int j = 0; j < 2; ++j) ptx::tmem_st_32x16(to + stage * 64 + j * 16, p[j]);
+        ptx::tmem_st_wait();
+        ptx::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(&full_a[stage]);
         if (++stage == C::kStages) stage = 0, phase ^= 1u;
       }
     }
   } else if (warp == 16) {
     // ------------------------------------------------------------- MMAs
-    if (lane == 0) {
-      constexpr uint32_t idesc = ptx::make_idesc_bf16_f32(128, C::kCols);
-      constexpr int kSteps = 8 / GPB;             // of 16 columns, in a group
-      int stage = 0, d = 0;
+    if (ptx::elect_one()) {
+      constexpr uint32_t idesc = ptx::make_idesc_f16_f32(128, C::kCols);
+      constexpr int kSteps = 8 / GPB, kPart = 8 / C::kParts;      // of 16 columns, in a group and in a stage
+      int stage = 0, slot = 0, d = 0;
       uint32_t phase = 0, d_phase = 0;
       bool ok = true;
       for (int e = 0; ok && e < n_entries; ++e) {
-        ok = ptx::mbar_wait_bounded(&full_a[stage], phase, abort_flag, a.wait_limit_ns) &&
-             ptx::mbar_wait_bounded(&full_b[stage], phase, abort_flag, a.wait_limit_ns);
-        if (!ok) break;
-        const uint32_t sa = ptx::smem_u32(smem + stage * C::kStage), sb = sa + C::kMats * kTcTile;
-        for (int j = 0; j < GPB; ++j) {
-          ok = ptx::mbar_wait_bounded(&d_empty[d], d_phase ^ 1u, abort_flag, a.wait_limit_ns);
+        const uint32_t sb = ptx::smem_u32(smem + slot * C::kStage);
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+          // the warps that made the operand have seen the stage's copies complete
+          if (ks % kPart == 0) ok = ok && ptx::mbar_wait_bounded(&full_a[stage], phase, abort_flag, a.wait_limit_ns);
+          if (ks % kSteps == 0) ok = ok && ptx::mbar_wait_bounded(&d_empty[d], d_phase ^ 1u, abort_flag, a.wait_limit_ns);
           if (!ok) break;
-          ptx::tc_fence_after();
+          if (ks % kPart == 0 || ks % kSteps == 0) ptx::tc_fence_after();
 #pragma unroll
           for (int mat = 0; mat < C::kMats; ++mat) {
-#pragma unroll
-            for (int k = 0; k < kSteps; ++k) {
-              // 16 columns further inside the swizzled 128-byte row = +32 bytes = +2 in the descriptor's address field
-              const int ks = j * kSteps + k;
-              const uint64_t da = ptx::make_desc_sw128_kmajor(sa + mat * kTcTile + (ks >> 2) * (kTcTile / 2)) + 2 * (ks & 3);
-              const uint64_t db = ptx::make_desc_sw128_kmajor(sb + (ks >> 2) * (C::kCols * 128)) + 2 * (ks & 3);
-              ptx::umma_bf16(tmem + d * 2 * NE + mat * C::kCols, da, db, idesc, k != 0 ? 1u : 0u);
-            }
+            // 16 columns of K: eight columns of tensor memory; in the swizzled 128-byte row +32 bytes = +2 in the descriptor's
+            // address field
+            const uint64_t db = ptx::make_desc_sw128_kmajor(sb + (ks >> 2) * (C::kCols * 128)) + 2 * (ks & 3);
+            ptx::umma_f16_ts(tmem + d * 2 * NE + mat * C::kCols, tmem + C::kOperands + stage * 64 + mat * C::kOperand + ks % kPart * 8, db, idesc,
+                             ks % kSteps != 0 ? 1u : 0u);
           }
-          ptx::umma_commit(&d_full[d]);
-          if (++d == 2) d = 0, d_phase ^= 1u;
+          if (ks % kSteps == kSteps - 1) {
+            ptx::umma_commit(&d_full[d]);
+            if (++d == 2) d = 0, d_phase ^= 1u;
+          }
+          if (ks % kPart == kPart - 1) {
+            ptx::umma_commit(&empty_a[stage]);
+            if (++stage == C::kStages) stage = 0, phase ^= 1u;
+          }
         }
         if (!ok) break;
-        ptx::umma_commit(&empty[stage]);
-        if (++stage == C::kStages) stage = 0, phase ^= 1u;
+        ptx::umma_commit(&empty[slot]);
+        if (++slot == C::kRing) slot = 0;
+      }
+      if (!ok) {                                  // gave up: the MMAs under way still use tensor and shared memory
+        ptx::umma_commit(drained);
+        uint32_t polls = 0;
+        while (!ptx::mbar_try_wait(drained, 0) && ++polls < 1000000u) {}
       }
     }
-  } else if (lane == 0) {
-    // ------------------------------------------------------------- activations
-    ptx::griddep_wait();                          // they are complete
+  } else {
+    // ------------------------------------------------------------- copies
+    // Warp 17 the codes, a lane for each matrix; 18 the scales, then the zeros, a lane for each matrix and group; 19 the
+    // activations and (down) their units.
+    const uint8_t* src = nullptr;
+    int64_t pitch = 0;
+    int mul = 1, add = 0, last = 1 << 30, to = 0;
+    uint32_t bytes = 0;
+    if (warp == 17) {
+      bytes = lane < C::kMats ? 8192 : 0;
+      to = C::kCodes + lane * 8192;
+    } else if (warp == 18) {
+      const bool is_zero = lane >= C::kMats * GPB;
+      const int at = lane - (is_zero ? C::kMats * GPB : 0), mat = at / GPB % C::kMats, size = is_zero ? 1 : 2;
+      const W4Mat& m = a.m[mat];
+      if (at < C::kMats * GPB && (!is_zero || (ZERO && m.zero != nullptr))) {
+        src = (is_zero ? m.zero : reinterpret_cast<const uint8_t*>(m.scale)) + row0 * size;
+        bytes = static_cast<uint32_t>(min(m.rows16 - row0, static_cast<int64_t>(128))) * size;
+      }
+      pitch = m.rows16 * size;
+      mul = GPB;
+      add = at % GPB;
+      last = static_cast<int>(m.n_groups) - 1;
+      to = (is_zero ? C::kZeros : C::kScales) + at * 128 * size;
+    } else if (lane == 0) {
+      src = a.image;
+      pitch = bytes = C::kB;
+      add = chunk * a.kblocks;
+    } else if (!GATEUP && lane == 1) {
+      src = reinterpret_cast<const uint8_t*>(a.unit);
+      pitch = bytes = C::kCols * 4;
+      add = chunk * a.kblocks;
+      to = C::kUnits;
+    }
+    const uint32_t all = __reduce_add_sync(0xFFFFFFFFu, bytes);
+    if (warp == 19) {
+      ptx::griddep_wait();                        // the activations are complete
+      if (GATEUP)
+        for (int t = lane; t < 64 && chunk * a.tokens + t < min(a.n, (chunk + 1) * a.tokens); t += 32)
+          s_factor[t] = a.unit[chunk * a.tokens + t];
+    }
     int stage = 0, issued = 0;
-    uint32_t phase = 0;
+    uint32_t phase = 1;
     bool ok = true;
-    for (int e = 0; ok && e < n_entries; ++e) {
-      ok = ptx::mbar_wait_bounded(&empty[stage], phase ^ 1u, abort_flag, a.wait_limit_ns);
+    for (int e = 0; e < n_entries; ++e) {
+      ok = ptx::mbar_wait_bounded(&empty[stage], phase, abort_flag, a.wait_limit_ns);
+      ok = __all_sync(0xFFFFFFFFu, ok);
       if (!ok) break;
+      if (lane == 0) ptx::mbar_expect_tx(&full[stage], all);
+      __syncwarp();
+      if (bytes != 0) {
+        uint8_t* dst = smem + stage * C::kStage + to;
+        if (warp == 17) ptx::tma_load_2d(dst, &a.codes[lane], s_list[e] * 64, row0, &full[stage]);
+        else ptx::bulk_load_1d(dst, src + min(s_list[e] * mul + add, last) * pitch, bytes, &full[stage]);
+      }
       ++issued;
-      ptx::mbar_expect_tx(&full_b[stage], C::kB);
-      ptx::bulk_load_1d(smem + stage * C::kStage + C::kMats * kTcTile,
-                        a.image + (static_cast<int64_t>(chunk) * a.kblocks + s_list[e]) * C::kB, C::kB, &full_b[stage]);
-      if (++stage == C::kStages) stage = 0, phase ^= 1u;
+      if (++stage == C::kRing) stage = 0, phase ^= 1u;
     }
-    // leave only when the MMAs have released every stage and no copy is under way
-    for (int i = 0; ok && i < C::kStages; ++i) {
-      ok = ptx::mbar_wait_bounded(&empty[stage], phase ^ 1u, abort_flag, a.wait_limit_ns);
-      if (++stage == C::kStages) stage = 0, phase ^= 1u;
-    }
-    // gave up: the copies still on their way into this block's shared memory need nobody else to arrive
-    for (int e = issued > C::kStages ? issued - C::kStages : 0; !ok && e < issued; ++e) {
+    // No copy of this warp's is under way when the block goes on.  Where another warp gave up earlier a stage stays
+    // incomplete, and a copy of its own has landed long before the polls are used up.
+    for (int e = max(issued - C::kRing, 0); e < issued; ++e) {
       uint32_t polls = 0;
-      while (!ptx::mbar_try_wait(&full_b[e % C::kStages], (e / C::kStages) & 1) && ++polls < 1000000u) {}
+      while (!ptx::mbar_try_wait(&full[e % C::kRing], (e / C::kRing) & 1) && ++polls < 20000u) {}
     }
   }
 
@@ -296,50 +486,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
   __syncthreads();
   if (warp == 16) {
     ptx::tc_fence_after();
-    ptx::tmem_dealloc(tmem, C::kTmem);
+    ptx::tmem_dealloc(tmem, 512);
   }
   if (threadIdx.x == 0 && *abort_flag) atomicExch(a.status, kStatusTimeout);
   if (cluster > 1) ptx::cluster_sync_all();
 
-  // ---- [column][row] sums of all blocks of the cluster; a token's pieces are columns tok, tokens + tok
-  const float* sums = reinterpret_cast<const float*>(smem);
-  auto total_of = [&](int col0, int tok, int r) {
-    float part[2][8], v = 0.0f;
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        part[p][k] = 0.0f;
-        if (p < a.pieces && k < cluster) {
-          const float* at = sums + (col0 + p * a.tokens + tok) * 128 + r;
-          part[p][k] = cluster == 1 ? *at : ld_cluster_f32(at, k);
-        }
-      }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v += part[0][k] + part[1][k];
-    return v;
-  };
-  const int n_here = min(a.tokens, a.n - chunk * a.tokens);
-  for (int i = rank * kTcThreads + threadIdx.x; i < n_here * 128; i += cluster * kTcThreads) {
-    const int tok = i >> 7, r = i & 127, row = row0 + r, token = chunk * a.tokens + tok;
-    if (row >= a.rows) continue;
-    if (GATEUP) {
-      const int b = find_branch(a.off, a.B, row);
-      const bool on = a.alpha[b] != 0.0f && (a.select == nullptr || a.select[static_cast<int64_t>(token) * a.B + b] != 0);
-      float h = 0.0f;
-      if (on) {
-        const float gate = total_of(0, tok, r), up = total_of(NE, tok, r);
-        h = gate / (1.0f + expf(-gate)) * up * a.alpha[b];
-      }
-      a.h[static_cast<int64_t>(token) * a.rows + row] = h;
-    } else {
-      float v = total_of(0, tok, r);
-      if (a.select != nullptr) v *= token_factor(a.select + static_cast<int64_t>(token) * a.B, a.alpha, a.B, a.compensate);
-      const int64_t at = static_cast<int64_t>(token) * a.rows + row;
-      if (a.residual != nullptr) v += a.residual[at];
-      a.y[at] = __float2bfloat16_rn(v);
-    }
-  }
+  if (cluster == 1) tc_outputs<1, NE, GATEUP>(a, reinterpret_cast<const float*>(smem), s_factor);
+  else if (cluster == 2) tc_outputs<2, NE, GATEUP>(a, reinterpret_cast<const float*>(smem), s_factor);
+  else if (cluster == 4) tc_outputs<4, NE, GATEUP>(a, reinterpret_cast<const float*>(smem), s_factor);
+  else tc_outputs<8, NE, GATEUP>(a, reinterpret_cast<const float*>(smem), s_factor);
   if (cluster > 1) {
     __syncthreads();
     ptx::cluster_sync_all();                      // no block leaves while another reads its sums
@@ -349,7 +504,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
 template <int NE, int GPB, bool GATEUP, bool ZERO>
 cudaError_t launch_tc(const W4TcArgs& a, int cluster, cudaStream_t st) {
   auto kernel = w4_tc_kernel<NE, GPB, GATEUP, ZERO>;
-  const int smem = TcCfg<NE, GATEUP>::kSmem;
+  const int smem = TcCfg<NE, GPB, GATEUP>::kSmem;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};

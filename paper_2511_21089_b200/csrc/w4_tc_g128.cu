@@ -7,8 +7,7 @@ cudaError_t launch_w4_tc_gateup_128(const W4TcArgs& a, int cluster, cudaStream_t
 cudaError_t launch_w4_tc_down_128(const W4TcArgs& a, int cluster, cudaStream_t st) { return w4::launch_tc_any<128 / 128, false>(a, cluster, st); }
 
 cudaError_t launch_w4_columns(const W4ColumnsArgs& a, cudaStream_t st) {
-  const int64_t threads = static_cast<int64_t>(a.n) * a.kblocks * 16;
-  return launch_pdl(w4::w4_columns_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, st, a);
+  return launch_pdl(w4::w4_columns_kernel, dim3(static_cast<unsigned>(a.n)), dim3(256), 0, st, a);
 }
 
 }  // namespace mlpmoe
