@@ -23,13 +23,11 @@ template <int NE, int GPB, bool GATEUP>
 struct TcCfg {
   static constexpr int kMats = GATEUP ? 2 : 1;
   static constexpr int kCols = GATEUP ? NE : 2 * NE;             // columns of an MMA
-  // Tensor memory: two accumulators of 2 NE columns, then the first operand's stages, each 64 columns: half a block of K of both
-  // matrices or a block of W_down's, two values a column.
-  static constexpr int kParts = GATEUP ? 2 : 1, kOperand = 64 / kMats, kOperands = 4 * NE;
-  static constexpr int kFit = (512 - kOperands) / 64;
-  static constexpr int kStages = kFit < 6 ? kFit : 6;
-  // Shared memory: stages of one block of K, each the activations, the codes, scales and zeros of 128 rows and the units.
+  // Tensor memory: two accumulators of 2 NE columns, then the first operand's stages, each 64 columns: a block of K of one
+  // matrix, two values a column.
+  static constexpr int kOperands = 4 * NE, kFit = (512 - kOperands) / 64 / kMats, kStages = kFit < 4 ? kFit : 4;      // of each matrix
   static constexpr int kB = kCols * 256;
+  // Shared memory: stages of one block of K, each the activations, the codes, scales and zeros of 128 rows and the units.
   static constexpr int kCodes = kB, kScales = kCodes + kMats * 8192, kZeros = kScales + kMats * GPB * 256, kUnits = kZeros + kMats * GPB * 128;
   static constexpr int kStage = (kUnits + (GATEUP ? 0 : kCols * 4) + 1023) / 1024 * 1024;
   static constexpr int kMost = (232448 - 6144) / kStage, kRing = kMost < 8 ? kMost : 8;
@@ -59,6 +57,23 @@ __device__ __forceinline__ void unpack_f16(uint32_t w, const Bias& bias, uint32_
     const __half2 v = *reinterpret_cast<const __half2*>(&u), o = i % 2 ? __hfma2(v, sixteenth, bias.sixteen) : __hadd2(v, bias.one);
     p[i] = *reinterpret_cast<const uint32_t*>(&o);
   }
+}
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t pair(float lo, float hi) {
+  uint64_t v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+  return v;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t x, uint64_t y) {
+  uint64_t v;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(x), "l"(y));
+  return v;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t z) {
+  uint64_t v;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(x), "l"(y), "l"(z));
+  return v;
 }
 
 // The unit for values of at most `top`, and its reciprocal.  Infinities and NaN pass through.
@@ -216,8 +231,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
   __shared__ uint8_t s_live[kW4MaxBranches];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint64_t* full_a = reinterpret_cast<uint64_t*>(smem + C::kBars);
-  uint64_t* empty_a = full_a + C::kStages;
-  uint64_t* full = empty_a + C::kStages;
+  uint64_t* empty_a = full_a + C::kMats * C::kStages;
+  uint64_t* full = empty_a + C::kMats * C::kStages;
   uint64_t* empty = full + C::kRing;
   uint64_t* d_full = empty + C::kRing;
   uint64_t* d_empty = d_full + 2;
@@ -229,8 +244,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
   const int row0 = blockIdx.x * 128;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < C::kStages; ++s) {
-      ptx::mbar_init(&full_a[s], 8 + a.extra_arrivals);
+    for (int s = 0; s < C::kMats * C::kStages; ++s) {
+      ptx::mbar_init(&full_a[s], 8 / C::kMats + a.extra_arrivals);
       ptx::mbar_init(&empty_a[s], 1);
     }
     for (int s = 0; s < C::kRing; ++s) {
@@ -269,9 +284,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
     const int at_scale = C::kScales + (GATEUP ? half * GPB * 256 : 0) + (quad * 32 + lane) * 2, at_unit = C::kUnits + half * NE * 4;
     int stage = 0;
     uint32_t phase = 0;
-    float acc[NE];
+    uint64_t acc[NE / 2];                         // pairs of fp32
 #pragma unroll
-    for (int i = 0; i < NE; ++i) acc[i] = 0.0f;
+    for (int i = 0; i < NE / 2; ++i) acc[i] = 0;
     const uint32_t taddr = tmem + static_cast<uint32_t>(half * NE) + (static_cast<uint32_t>(quad * 32) << 16);
     for (int step = 0; step < steps; ++step) {
       bool ok = step % GPB != 0 || ptx::mbar_wait_bounded(&full[stage], phase, abort_flag, a.wait_limit_ns);
@@ -294,16 +309,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
         ptx::tmem_ld_wait();
 #pragma unroll
         for (int k = 0; k < kPart; k += 4) {
-          if constexpr (GATEUP) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) acc[i + k + q] += __uint_as_float(r[k + q]) * s;
-          } else {                                // a scale (8 bits) times a power of two is exact
+          uint64_t s0 = pair(s, s), s1 = s0;
+          if constexpr (!GATEUP) {                // a scale (8 bits) times a power of two is exact
             const float4 u = *reinterpret_cast<const float4*>(in + at_unit + (i + k) * 4);
-            acc[i + k] += __uint_as_float(r[k]) * (s * u.x);
-            acc[i + k + 1] += __uint_as_float(r[k + 1]) * (s * u.y);
-            acc[i + k + 2] += __uint_as_float(r[k + 2]) * (s * u.z);
-            acc[i + k + 3] += __uint_as_float(r[k + 3]) * (s * u.w);
+            s0 = mul2(s0, pair(u.x, u.y));
+            s1 = mul2(s1, pair(u.z, u.w));
           }
+          acc[(i + k) / 2] = fma2(pair(__uint_as_float(r[k]), __uint_as_float(r[k + 1])), s0, acc[(i + k) / 2]);
+          acc[(i + k) / 2 + 1] = fma2(pair(__uint_as_float(r[k + 2]), __uint_as_float(r[k + 3])), s1, acc[(i + k) / 2 + 1]);
         }
       }
       ptx::tc_fence_before();
@@ -320,17 +333,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
     asm volatile("bar.sync 1, 256;" ::: "memory");
     float* sums = reinterpret_cast<float*>(smem) + half * NE * 128 + quad * 32 + lane;      // [column][row]
 #pragma unroll
-    for (int i = 0; i < NE; ++i) sums[i * 128] = acc[i];
+    for (int i = 0; i < NE; i += 2) {
+      sums[i * 128] = __uint_as_float(static_cast<uint32_t>(acc[i / 2]));
+      sums[(i + 1) * 128] = __uint_as_float(static_cast<uint32_t>(acc[i / 2] >> 32));
+    }
   } else if (warp < 16) {
     // ------------------------------------------------------------- codes to bf16
-    // gate|up: a warp takes 32 rows of one matrix; down: of half of the columns.  32 columns (16 bytes) at a time, 64 to a
-    // stage of the operand.
-    constexpr int kChunks = 2 * C::kParts, kZeros = GPB * kChunks > 4 ? GPB * kChunks / 4 : 1;      // groups that the warp's columns touch
+    // gate|up: a warp takes 32 rows of one matrix; down: of half of the columns.  32 columns (16 bytes) at a time.
+    constexpr int kChunks = 4 / (3 - C::kMats), kZeros = GPB * kChunks > 4 ? GPB * kChunks / 4 : 1;      // groups that the warp's columns touch
     const int quad = warp % 4, part = (warp - 8) / 4, chunk0 = GATEUP ? 0 : 2 * part, r = quad * 32 + lane;
     const bool has_zero = ZERO && a.m[GATEUP ? part : 0].zero != nullptr;
     const int at_codes = C::kCodes + (GATEUP ? part * 8192 : 0) + r * 64;
     const int at_zero = C::kZeros + (GATEUP ? part * GPB * 128 : chunk0 * GPB / 4 * 128) + r;
-    const uint32_t to = tmem + C::kOperands + (GATEUP ? part * C::kOperand : chunk0 * 16) + (static_cast<uint32_t>(quad * 32) << 16);
+    const uint32_t to = tmem + C::kOperands + (GATEUP ? part * C::kStages * 64 : part * 32) + (static_cast<uint32_t>(quad * 32) << 16);
+    uint64_t* full_mine = full_a + (GATEUP ? part * C::kStages : 0);
+    uint64_t* empty_mine = empty_a + (GATEUP ? part * C::kStages : 0);
     int stage = 0, slot = 0;
     uint32_t phase = 0, slot_phase = 0;
     bool ok = true;
@@ -348,66 +365,62 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
       __syncwarp();
       if (lane == 0) ptx::mbar_arrive(&empty[slot]);
       if (++slot == C::kRing) slot = 0, slot_phase ^= 1u;
+      ok = ptx::mbar_wait_bounded(&empty_mine[stage], phase ^ 1u, abort_flag, a.wait_limit_ns);
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      ptx::tc_fence_after();
 #pragma unroll
-      for (int h = 0; h < C::kParts; ++h) {
-        uint32_t p[2][16];
+      for (int i = 0; i < kChunks; ++i) {
+        const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+        uint32_t p[16];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int i = 2 * h + j;
-          const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) unpack_f16(w[k], bias[i * kZeros / kChunks], p[j] + 4 * k);
-        }
-        ok = ptx::mbar_wait_bounded(&empty_a[stage], phase ^ 1u, abort_flag, a.wait_limit_ns);
-        ok = __all_sync(0xFFFFFFFFu, ok);
-        if (!ok) break;
-        ptx::tc_fence_after();
-#pragma unroll
-        for (int j = 0; j < 2; ++j) ptx::tmem_st_32x16(to + stage * 64 + j * 16, p[j]);
-        ptx::tmem_st_wait();
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(&full_a[stage]);
-        if (++stage == C::kStages) stage = 0, phase ^= 1u;
+        for (int k = 0; k < 4; ++k) unpack_f16(w[k], bias[i * kZeros / kChunks], p + 4 * k);
+        ptx::tmem_st_32x16(to + stage * 64 + i * 16, p);
       }
+      ptx::tmem_st_wait();
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(&full_mine[stage]);
+      if (++stage == C::kStages) stage = 0, phase ^= 1u;
     }
   } else if (warp == 16) {
     // ------------------------------------------------------------- MMAs
     if (ptx::elect_one()) {
       constexpr uint32_t idesc = ptx::make_idesc_f16_f32(128, C::kCols);
-      constexpr int kSteps = 8 / GPB, kPart = 8 / C::kParts;      // of 16 columns, in a group and in a stage
+      constexpr int kSteps = 8 / GPB;             // of 16 columns, in a group
       int stage = 0, slot = 0, d = 0;
       uint32_t phase = 0, d_phase = 0;
       bool ok = true;
       for (int e = 0; ok && e < n_entries; ++e) {
         const uint32_t sb = ptx::smem_u32(smem + slot * C::kStage);
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-          // the warps that made the operand have seen the stage's copies complete
-          if (ks % kPart == 0) ok = ok && ptx::mbar_wait_bounded(&full_a[stage], phase, abort_flag, a.wait_limit_ns);
-          if (ks % kSteps == 0) ok = ok && ptx::mbar_wait_bounded(&d_empty[d], d_phase ^ 1u, abort_flag, a.wait_limit_ns);
-          if (!ok) break;
-          if (ks % kPart == 0 || ks % kSteps == 0) ptx::tc_fence_after();
+        for (int j = 0; j < GPB; ++j) {
+          ok = ptx::mbar_wait_bounded(&d_empty[d], d_phase ^ 1u, abort_flag, a.wait_limit_ns);
 #pragma unroll
           for (int mat = 0; mat < C::kMats; ++mat) {
-            // 16 columns of K: eight columns of tensor memory; in the swizzled 128-byte row +32 bytes = +2 in the descriptor's
-            // address field
-            const uint64_t db = ptx::make_desc_sw128_kmajor(sb + (ks >> 2) * (C::kCols * 128)) + 2 * (ks & 3);
-            ptx::umma_f16_ts(tmem + d * 2 * NE + mat * C::kCols, tmem + C::kOperands + stage * 64 + mat * C::kOperand + ks % kPart * 8, db, idesc,
-                             ks % kSteps != 0 ? 1u : 0u);
+            // the warps that made the operand have seen the stage's copies complete
+            if (j == 0) ok = ok && ptx::mbar_wait_bounded(&full_a[mat * C::kStages + stage], phase, abort_flag, a.wait_limit_ns);
+            if (!ok) break;
+            ptx::tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+              // 16 columns of K: eight columns of tensor memory; in the swizzled 128-byte row +32 bytes = +2 in the descriptor's
+              // address field
+              const int ks = j * kSteps + k;
+              const uint64_t db = ptx::make_desc_sw128_kmajor(sb + (ks >> 2) * (C::kCols * 128)) + 2 * (ks & 3);
+              ptx::umma_f16_ts(tmem + d * 2 * NE + mat * C::kCols, tmem + C::kOperands + (mat * C::kStages + stage) * 64 + ks * 8, db, idesc,
+                               k != 0 ? 1u : 0u);
+            }
+            if (j == GPB - 1) ptx::umma_commit(&empty_a[mat * C::kStages + stage]);
           }
-          if (ks % kSteps == kSteps - 1) {
-            ptx::umma_commit(&d_full[d]);
-            if (++d == 2) d = 0, d_phase ^= 1u;
-          }
-          if (ks % kPart == kPart - 1) {
-            ptx::umma_commit(&empty_a[stage]);
-            if (++stage == C::kStages) stage = 0, phase ^= 1u;
-          }
+          if (!ok) break;
+          ptx::umma_commit(&d_full[d]);
+          if (++d == 2) d = 0, d_phase ^= 1u;
         }
         if (!ok) break;
         ptx::umma_commit(&empty[slot]);
         if (++slot == C::kRing) slot = 0;
+        if (++stage == C::kStages) stage = 0, phase ^= 1u;
       }
       if (!ok) {                                  // gave up: the MMAs under way still use tensor and shared memory
         ptx::umma_commit(drained);
@@ -450,12 +463,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
       to = C::kUnits;
     }
     const uint32_t all = __reduce_add_sync(0xFFFFFFFFu, bytes);
-    if (warp == 19) {
-      ptx::griddep_wait();                        // the activations are complete
-      if (GATEUP)
-        for (int t = lane; t < 64 && chunk * a.tokens + t < min(a.n, (chunk + 1) * a.tokens); t += 32)
-          s_factor[t] = a.unit[chunk * a.tokens + t];
-    }
+    if (warp == 19) ptx::griddep_wait();          // the activations are complete
     int stage = 0, issued = 0;
     uint32_t phase = 1;
     bool ok = true;
@@ -473,6 +481,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
       ++issued;
       if (++stage == C::kRing) stage = 0, phase ^= 1u;
     }
+    if (GATEUP && warp == 19)
+      for (int t = lane; t < 64 && chunk * a.tokens + t < min(a.n, (chunk + 1) * a.tokens); t += 32) s_factor[t] = a.unit[chunk * a.tokens + t];
     // No copy of this warp's is under way when the block goes on.  Where another warp gave up earlier a stage stays
     // incomplete, and a copy of its own has landed long before the polls are used up.
     for (int e = max(issued - C::kRing, 0); e < issued; ++e) {
