@@ -164,9 +164,11 @@ W4Mat matrix(const mlpmoe_w4_matrix_t& m, int64_t rows, int64_t cols, int group)
   return r;
 }
 
-// From how many tokens on, and from how many codes of the layer on, the tensor cores' kernels are used (y bf16).
-constexpr int kTcFrom = 17;
-constexpr int64_t kTcCodes = int64_t(24) << 20;
+// From how many codes times tokens on the kernels of the 5th-generation tensor cores are used (y bf16, which is what their fp16
+// operand is precise enough for), instead of the tiled kernels.  Measured, tiled / tensor, in us: 4096 x 14336, 9 tokens 52 / 47,
+// 16 tokens 66 / 48, 64 tokens 129 / 53; 2048 x 8192, 16 tokens 26.5 / 27.0, 24 tokens 36 / 28; 896 x 4864, 32 tokens
+// 20.5 / 21.1, 64 tokens 27.6 / 24.3; 512 x 2048, 64 tokens 17 / 22.  With fewer rows than their tile's 128 most of it is padding.
+constexpr int64_t kTcWork = int64_t(768) << 20;
 
 // Limits of the bounded waits of the tensor cores' kernels; changed by the test hook only.
 std::atomic<uint64_t> g_wait_limit_ns{1000000000ull};
@@ -175,7 +177,8 @@ std::atomic<uint32_t> g_extra_arrivals{0};
 enum Path { STREAM, WIDE, TENSOR };
 Path path_of(const mlpmoe_w4_layer_t* l, int64_t n, mlpmoe_dtype_t y_dtype) {
   if (n < kWideFrom) return STREAM;
-  return y_dtype == MLPMOE_BF16 && n >= kTcFrom && 3 * l->d_model * l->d_inter >= kTcCodes ? TENSOR : WIDE;
+  if (y_dtype != MLPMOE_BF16 || l->d_model < 128 || l->d_inter < 128) return WIDE;
+  return n * (3 * l->d_model * l->d_inter) >= kTcWork ? TENSOR : WIDE;
 }
 
 // A chunk of the tensor cores' products: tokens, and the columns of an epilogue warp, 32 or 64.  gate|up has one such set of columns

@@ -3,8 +3,8 @@
 // The codes become fp16 whole numbers code - zero (exact) in tensor memory, where tcgen05.mma takes its first operand
 // from; the activations come as its second, 128-byte-swizzled in shared memory: fp16 times a unit, a power of two of the token
 // (x) or of the token and 128 columns (the intermediate activation, whose row is not known as a whole when it is
-// written) that brings the largest to 2^14..2^15.  What is below 2^-28 of the largest loses bits; of the rest 2^-12 is left
-// out (nothing for x in bf16), where y is rounded to 2^-9.  The products of one group of K (32, 64 or 128 columns)
+// written) that brings the largest to 2^14..2^15.  What is below 2^-28 of the largest loses bits; the rest is rounded to
+// 2^-11 (not at all for x in bf16), where y is rounded to 2^-8.  The products of one group of K (32, 64 or 128 columns)
 // accumulate in tensor memory too.  Two accumulators alternate: while the tensor core fills one, the epilogue warps read
 // the other back and add it, times the row's scale, to their fp32 sums in registers.
 //

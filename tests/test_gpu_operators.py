@@ -397,7 +397,7 @@ def test_w4_forward_selection(lib, n, group):
 def test_w4_forward_tensor_core_kernels(lib, group, asym):
     """Layers large enough, with enough tokens and y in bf16, for the kernels of the 5th-generation tensor cores: ragged
     d_model and d_inter, every type of x, chunks of one token less and more than they hold, selections."""
-    d, d_b = 1032, [1008, 2032, 16, 3008, 2944]
+    d, d_b = 1032, [1008, 7040, 16, 3008, 4944]
     c = W4Case(lib, [group, 7], d, d_b, group, asym, alpha=[1.0, 0.7, 1.2, -0.6, 0.9], std=0.05)
     rng = np.random.default_rng([group, 8])
     for n, xt, x_group in ((17, "bf16", 0), (33, "fp32", 0), (64, "bf16", 0), (65, "bf16", 0), (40, "e4m3", 128), (130, "e4m3", 0)):
@@ -413,7 +413,7 @@ def test_w4_forward_tensor_core_kernels(lib, group, asym):
     # alpha = 0 drops a branch without a selection; what it holds does not matter
     c.alpha = [1.0, 0.0, 1.2, -0.6, 0.9]
     c.layer = lib.mlpmoe_w4_layer(d, c.I, d_b, group, *c.mats, alpha=c.alpha)
-    c.mats[0][1][:, 1008:3040] = float("nan")
+    c.mats[0][1][:, 1008:8048] = float("nan")
     xh, x, _ = c.activations([64, 9], 64, "bf16")
     c.check(c.run(x, 64, "bf16", "bf16"), xh, "bf16", "bf16")
 
