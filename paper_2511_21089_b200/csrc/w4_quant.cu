@@ -51,22 +51,33 @@ __device__ __forceinline__ void store_eight(T* p, const float (&v)[8]) {
 }
 
 // The codes of eight values, rint(v / div) + z between 0 and 15, four bits each.  The quotient is v * (1 / div), off by less
-// than 2^-20; only where that lies within 2^-17 of a half is v divided in full, so that the codes are those of the
-// correctly rounded quotient.  The sum with 1.5 * 2^23 rounds it and has the whole number in its low bits.  No code falls
-// below 0: the scale is off by 2^-9 at most, z = rint(-lo / div), and rint(lo / div) = -z.
+// than 2^-20; only what lies within 2^-17 of a half needs more, so that the codes are those of the correctly rounded
+// quotient.  An fp32 value is divided in full.  A bf16 value is there exactly half way between two whole numbers, and commonly
+// (8 bits over 8 bits): with a and b the significands of v and div, both below 256, and v at least div / 2, the distance
+// from a half is a multiple of 1 / (4 b).  So the sum with 1.5 * 2^12 first takes the quotient to multiples of 2^-11, which
+// makes such a half exact and moves nothing else onto or over one (with the division these values cost a third of the time).
+// The sum with 1.5 * 2^23 rounds to even and has the whole number in its low bits.  No code falls below 0: the scale is off by
+// 2^-9 at most, z = rint(-lo / div), and rint(lo / div) = -z.
+template <bool BF16>
 __device__ __forceinline__ uint32_t codes_of(const float (&v)[8], float div, float inv, int z) {
-  constexpr float kMagic = 12582912.0f;
-  float t[8], off[8], most = 0.0f;
+  constexpr float kMagic = 12582912.0f, kFine = 6144.0f;
+  float t[8];
+  if constexpr (BF16) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    t[j] = fmaf(v[j], inv, kMagic);
-    off[j] = fabsf(fmaf(v[j], inv, kMagic - t[j]));
-    most = fmaxf(most, off[j]);
-  }
-  if (most > 0.49999f) {
+    for (int j = 0; j < 8; ++j) t[j] = fmaf(v[j], inv, kFine) + (kMagic - kFine);
+  } else {
+    float off[8], most = 0.0f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (off[j] > 0.49999f) t[j] = v[j] / div + kMagic;
+    for (int j = 0; j < 8; ++j) {
+      t[j] = fmaf(v[j], inv, kMagic);
+      off[j] = fabsf(fmaf(v[j], inv, kMagic - t[j]));
+      most = fmaxf(most, off[j]);
+    }
+    if (most > 0.49999f) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (off[j] > 0.49999f) t[j] = v[j] / div + kMagic;
+    }
   }
   uint32_t code = 0;
   const int shift = z - 0x4B400000;
@@ -115,19 +126,46 @@ __global__ void __launch_bounds__(kThreads, 4) w4_quantize_kernel(const __grid_c
   float lo = 0.0f, hi = 0.0f;           // of row lane % 4 in this lane's group
   {
     float l[kWarpRows], h[kWarpRows];   // the group's range in each row; l negated
-#pragma unroll
-    for (int i = 0; i < kWarpRows; ++i) {
-      l[i] = h[i] = 0.0f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) l[i] = fmaxf(l[i], -v[i][j]), h[i] = fmaxf(h[i], v[i][j]);
-      if (a.zero == nullptr) h[i] = fmaxf(h[i], l[i]);
-    }
-    for (int o = 1; o < lanes; o *= 2) {
+    if constexpr (sizeof(T) == 2) {     // two bf16 at a time: a comparison keeps either of its operands as it is
+      uint32_t range[kWarpRows];        // (l, h)
 #pragma unroll
       for (int i = 0; i < kWarpRows; ++i) {
-        h[i] = fmaxf(h[i], __shfl_xor_sync(0xFFFFFFFFu, h[i], o));
-        if (a.zero != nullptr) l[i] = fmaxf(l[i], __shfl_xor_sync(0xFFFFFFFFu, l[i], o));
+        __nv_bfloat162 p[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[j] = __floats2bfloat162_rn(v[i][2 * j], v[i][2 * j + 1]);
+        const __nv_bfloat162 most = __hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3])), least = __hmin2(__hmin2(p[0], p[1]), __hmin2(p[2], p[3]));
+        const __nv_bfloat162 both = __halves2bfloat162(__hneg(__hmin(least.x, least.y)), __hmax(most.x, most.y));
+        const __nv_bfloat162 from_zero = __hmax2(both, __floats2bfloat162_rn(0.0f, 0.0f));
+        range[i] = *reinterpret_cast<const uint32_t*>(&from_zero);
       }
+      for (int o = 1; o < lanes; o *= 2) {
+#pragma unroll
+        for (int i = 0; i < kWarpRows; ++i) {
+          const uint32_t other = __shfl_xor_sync(0xFFFFFFFFu, range[i], o);
+          const __nv_bfloat162 wide = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&range[i]), *reinterpret_cast<const __nv_bfloat162*>(&other));
+          range[i] = *reinterpret_cast<const uint32_t*>(&wide);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kWarpRows; ++i) l[i] = __uint_as_float(range[i] << 16), h[i] = __uint_as_float(range[i] & 0xFFFF0000u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kWarpRows; ++i) {
+        l[i] = h[i] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) l[i] = fmaxf(l[i], -v[i][j]), h[i] = fmaxf(h[i], v[i][j]);
+      }
+      for (int o = 1; o < lanes; o *= 2) {
+#pragma unroll
+        for (int i = 0; i < kWarpRows; ++i) {
+          h[i] = fmaxf(h[i], __shfl_xor_sync(0xFFFFFFFFu, h[i], o));
+          l[i] = fmaxf(l[i], __shfl_xor_sync(0xFFFFFFFFu, l[i], o));
+        }
+      }
+    }
+    if (a.zero == nullptr) {
+#pragma unroll
+      for (int i = 0; i < kWarpRows; ++i) h[i] = fmaxf(h[i], l[i]);
     }
 #pragma unroll
     for (int i = 0; i < kWarpRows; ++i)
@@ -152,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, 4) w4_quantize_kernel(const __grid_c
     const int from = (lane & ~(kWarpRows - 1)) + i;
     const float div = __shfl_sync(0xFFFFFFFFu, div_mine, from), inv = __shfl_sync(0xFFFFFFFFu, inv_mine, from);
     const float z = __shfl_sync(0xFFFFFFFFu, z_mine, from);
-    const uint32_t code = codes_of(v[i], div, inv, static_cast<int>(z));
+    const uint32_t code = codes_of<sizeof(T) == 2>(v[i], div, inv, static_cast<int>(z));
     if (i < rows_here && store) *reinterpret_cast<uint32_t*>(q) = code & keep;
     q += a.pitch;
   }
