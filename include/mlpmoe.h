@@ -260,7 +260,7 @@ mlpmoe_status_t mlpmoe_stack_forward_host(const mlpmoe_handle_t* layers, int32_t
 /* ------------------------------------------------------------------------- *
  * Operators around a routed layer step (not in the paper): the norm before the
  * layer, the router that makes the selection, and the layer on 4-bit weights for
- * a few tokens.  They need no handle: every buffer is the caller's, the calls only
+ * decode.  They need no handle: every buffer is the caller's, the calls only
  * enqueue on `stream`, allocate nothing, never synchronise and can be captured into
  * a graph.  A workspace is scratch of one call: two calls that may overlap (other
  * streams, replays of two graphs at the same time) need one each.
@@ -341,7 +341,8 @@ typedef struct {
  *     zero == NULL:  s = bf16(max |w| / 7),                          code = clamp(rint(w / s) + 8, 0, 15)
  *     otherwise:     s = bf16((max(w, 0) - min(w, 0)) / 15),  z = clamp(rint(-min(w, 0) / s), 0, 15),
  *                    code = clamp(rint(w / s) + z, 0, 15)
- * (s = 0: code = z, z = 0 where it is stored).  Columns past cols are coded 0 up to the row's end.
+ * (s below 2^-126 counts as 0; s = 0: code = z, z = 0 where it is stored; s infinite, from a range past fp32's: the same
+ * codes).  Columns past cols are coded 0 up to the row's end.
  *   W       device, fp32 or bf16: [rows x cols] with rows `stride` apart (MLPMOE_LAYOUT_LINEAR), or its transpose
  *           [cols x rows] (MLPMOE_LAYOUT_PAPER); stride 0 = contiguous
  * mlpmoe_w4_dequantize writes (code - zero) * scale back, rounded to dtype: for a prefill layer made of the same weights
@@ -363,13 +364,16 @@ typedef struct {
 } mlpmoe_w4_layer_t;
 
 /*
- * The layer equation of Section 3.1 on 4-bit weights, for decode (any token count is computed, but the weights are read
- * once per a few tokens, so a layer of mlpmoe_create is faster for long inputs):
+ * The layer equation of Section 3.1 on 4-bit weights, for decode (any token count is computed, but the weights are read and
+ * unpacked once per 64 tokens or fewer, so a layer of mlpmoe_create is faster for long inputs):
  *     y_t = residual_t + c_t * sum_{b in S_t} alpha_b W_down^(b) [ silu(W_gate^(b) x_t) (.) W_up^(b) x_t ]
- * with S_t and c_t as in mlpmoe_forward_routed (select NULL: every branch with alpha_b != 0, c_t = 1).  Branches that
- * no token selects are not read.  Inside each group of columns x and the intermediate activation are held as fixed
- * point, off by at most 2^-23 (y fp32) or 2^-15 (y bf16) of the group's largest magnitude (a group all below 2^-100
- * counts as 0); their products with the codes are exact, scales and sums are fp32.
+ * with S_t and c_t as in mlpmoe_forward_routed (select NULL: every branch with alpha_b != 0, c_t = 1).  What a branch holds
+ * that no token selects does not enter y; with up to eight tokens it is not read either.  Inside each group of columns
+ * x and the intermediate activation are held as fixed point, off by at most 2^-23 (y fp32) or 2^-15 (y bf16) of the
+ * group's largest magnitude (a group all below 2^-100 counts as 0); or, for y in bf16 on a batch large enough for the
+ * kernels of the 5th-generation tensor cores, as fp16 times a power of two of the token (x) or of the token and 128
+ * columns (intermediate activation), off by at most 2^-11 of each value or 2^-39 of the largest (x in bf16: only the
+ * latter).  Their products with the codes are exact, scales and sums are fp32.
  *   x        device, [n_tokens x d_model] of x_dtype (bf16, fp32, or e4m3 with scales), rows x_stride elements apart
  *            (0 = d_model), 16-byte aligned, x_stride a multiple of 8
  *   x_scale  device fp32 [n_tokens x ceil(d_model / x_group)] for e4m3 (x_group = 0: one per token), else ignored;

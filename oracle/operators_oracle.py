@@ -89,15 +89,18 @@ def w4_quantize(W, group, asymmetric):
     W = np.asarray(W, dtype=np.float32)
     rows, cols = W.shape
     codes, scales, zeros = np.zeros((rows, cols), np.uint8), [], []
+
+    def flushed(s):
+        return np.where(s < np.float32(2.0 ** -126), np.float32(0), s)
     for lo in range(0, cols, group):
         w = W[:, lo:lo + group]
         if asymmetric:
             mn, mx = np.minimum(w.min(axis=1), np.float32(0)), np.maximum(w.max(axis=1), np.float32(0))
-            s = round_to_bf16((mx - mn) / np.float32(15)).astype(np.float32)
+            s = flushed(round_to_bf16((mx - mn) / np.float32(15)).astype(np.float32))
             div = np.where(s > 0, s, np.float32(1))
             z = np.clip(np.rint(-mn / div), 0, 15)
         else:
-            s = round_to_bf16(np.abs(w).max(axis=1) / np.float32(7)).astype(np.float32)
+            s = flushed(round_to_bf16(np.abs(w).max(axis=1) / np.float32(7)).astype(np.float32))
             div = np.where(s > 0, s, np.float32(1))
             z = np.full(rows, 8.0, np.float32)
         codes[:, lo:lo + group] = np.clip(np.rint(w / div[:, None]) + z[:, None], 0, 15)

@@ -173,7 +173,8 @@ __global__ void __launch_bounds__(kThreads, 4) w4_quantize_kernel(const __grid_c
   }
   // The divisions of a group once, in the lane of its row: the scale is rounded to bf16 (2 bytes per group) before the codes
   // are made, so the codes fit the scale that is stored.
-  const float s_mine = __bfloat162float(__float2bfloat16_rn(a.zero != nullptr ? (hi - lo) / 15.0f : hi / 7.0f));
+  float s_mine = __bfloat162float(__float2bfloat16_rn(a.zero != nullptr ? (hi - lo) / 15.0f : hi / 7.0f));
+  if (s_mine < 1.17549435e-38f) s_mine = 0.0f;             // below 2^-126 its reciprocal may be infinite
   const float div_mine = s_mine > 0.0f ? s_mine : 1.0f, inv_mine = 1.0f / div_mine;
   const float z_mine = a.zero != nullptr ? fminf(rintf(-lo / div_mine), 15.0f) : 8.0f;
   const int my_row = lane % kWarpRows;
