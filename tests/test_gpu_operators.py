@@ -44,6 +44,8 @@ NORM_CASES = [
     (301, 1001, "bf16", "fp32", "fp32", 0, 3), (298, 1032, "fp32", "none", "bf16", 0, 0), (299, 4095, "fp32", "bf16", "e4m3", 128, 0),
     (310, 4096, "bf16", "bf16", "e4m3", 0, 16), (2, 4104, "fp32", "bf16", "e4m3", 128, 0), (1, 8192, "fp32", "fp32", "bf16", 0, 0),
     (2, 8200, "bf16", "fp32", "e4m3", 128, 0), (2, 20001, "fp32", "bf16", "fp32", 0, 0), (1, 32768, "fp32", "bf16", "e4m3", 0, 0), (4, 100, "fp32", "fp32", "e4m3", 128, 28),
+    (4100, 512, "fp32", "bf16", "e4m3", 128, 0), (4099, 100, "bf16", "fp32", "bf16", 0, 3), (4098, 264, "fp32", "bf16", "e4m3", 64, 8),
+    (1030, 4096, "fp32", "bf16", "e4m3", 128, 0), (1029, 2057, "bf16", "fp32", "e4m3", 64, 3), (300, 2048, "fp32", "bf16", "e4m3", 32, 0),
 ]
 
 
