@@ -2,6 +2,8 @@
 // the dense matrix they read or write.  A block takes a tile of 32 rows x 256 columns, a warp four neighbouring rows of
 // it with eight neighbouring columns per lane and row, all loads under way before the first use; a group of 32, 64 or
 // 128 columns is 4, 8 or 16 lanes.
+// 14336 x 4096 bf16, group 128 with zeros: codes 45 us of 147 MB (23 for a copy; 76 % of the issue slots are taken: a range, a
+// product, a sum, a clamp and a place for each value), back 24 us, where the copy takes 23.
 #include "../../include/mlpmoe.h"
 #include "internal.h"
 #include "w4.h"
