@@ -596,6 +596,18 @@ def test_w4_forward_magnitudes(lib, path):
         c.check(c.run(x, n, xt, yt), host(x), xt, yt, fp16=path == "tensor")
 
 
+@pytest.mark.parametrize("d,d_b", [(65536, [64, 80]), (128, [65520, 16])])
+def test_w4_forward_longest_rows(lib, d, d_b):
+    """The largest d_model and d_inter, on every path, all branches and a selection."""
+    c = W4Case(lib, [73, d], d, d_b, 128, True, std=0.02)
+    for n, yt, fp16 in ((1, "fp32", False), (8, "bf16", False), (11, "fp32", False), (40, "bf16", True)):
+        xh, x, _ = c.activations([74, n], n, "bf16")
+        c.check(c.run(x, n, "bf16", yt), xh, "bf16", yt, fp16=fp16)
+        sel = np.zeros((n, 2), np.uint8)
+        sel[:, 1] = 1
+        c.check(c.run(x, n, "bf16", yt, select=torch.from_numpy(sel).cuda()), xh, "bf16", yt, sel, fp16=fp16)
+
+
 def test_w4_forward_most_branches(lib):
     """256 branches of 16 neurons on every path, a selection of 8 per token."""
     d_b = [16] * 256
