@@ -8,16 +8,15 @@
 // accumulate in tensor memory too.  Two accumulators alternate: while the tensor core fills one, the epilogue warps read
 // the other back and add it, times the row's scale, to their fp32 sums in registers.
 //
-// Per code the conversion costs a block about 1.3 instructions (a mask, an addition or a multiplication-addition, a share of
-// the waits), and that is what bounds these kernels up to 64 tokens, not the copy (floor of the Llama-shaped layer 14.5 us) nor
-// the MMAs: before the last step below 128 columns of K took 1450 cycles of which the MMAs run 580 (gate|up), 1100 and 290
-// (down).  Measured there, 64 tokens, group 128 with zeros: 53 us (each alone, with cold caches: columns 6, gate|up 33,
-// down 28).  On the way: the operand
-// in shared memory (64 KB written and read for each 128 columns of K), waits that read the timer at once, and MMAs
-// issued under `lane == 0` 99 us; the operand in tensor memory, the rest as it was 94; codes through a ring of copies instead of
-// registers 82; scales through a ring too 70; waits that read the timer late 58; copies issued by three warps 56; an operand
-// stage for each matrix and paired sums 53.  Tried without gain: stages of half a block of K, reading the next codes while
-// tensor memory takes the last.
+// What bounds these kernels up to 64 tokens is the conversion of the codes (1.1 instructions a code of the 3.5 that a block's
+// warps issue, at 2.2 a cycle), not the copy (floor of the Llama-shaped layer 14.5 us) nor the MMAs: before the last step below
+// 128 columns of K took 1450 cycles of which the MMAs run 580 (gate|up), 1100 and 290 (down).  Measured there, 64 tokens,
+// group 128 with zeros: 53 us (each alone, with cold caches: columns 6, gate|up 33, down 28).  On the way: the operand in shared
+// memory (64 KB written and read for each 128 columns of K), waits that read the timer at once, and MMAs issued under
+// `lane == 0` 99 us; the operand in tensor memory, the rest as it was 94; codes through a ring of copies instead of registers
+// 82; scales through a ring too 70; waits that read the timer late 58; copies issued by three warps 56; an operand stage for
+// each matrix and paired sums 53.  Tried without gain: stages of half a block of K, reading the next codes while tensor
+// memory takes the last.
 //
 // A block: 128 neurons (128 gate rows and 128 up rows) or 128 rows of W_down.  Warps 0..7 epilogue (tensor memory lanes
 // 32 (warp % 4).., columns NE (warp / 4)..), 8..15 codes to fp16 (the same lanes), 16 issues the MMAs, 17 copies the
