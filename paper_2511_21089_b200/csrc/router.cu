@@ -373,7 +373,8 @@ __global__ void __launch_bounds__(kBackwardThreads, VPT == 4 ? 6 : 4) route_back
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int seg = lane / LPR, l = lane % LPR, c0 = l * VPT;
   const uint32_t avail_mask = avail_mask_of<VPT>(a.avail, c0, a.B);
-  int total = 0, n_avail = __popc(avail_mask), cnt[VPT];
+  int64_t total = 0;                    // up to n_tokens * top_k: past 32 bits
+  int n_avail = __popc(avail_mask), cnt[VPT];
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     cnt[i] = c0 + i < a.B ? a.counts_in[c0 + i] : 0;
@@ -384,7 +385,7 @@ __global__ void __launch_bounds__(kBackwardThreads, VPT == 4 ? 6 : 4) route_back
     total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
     n_avail += __shfl_xor_sync(0xFFFFFFFFu, n_avail, o);
   }
-  const int routed = a.counts_in[a.B], mean = n_avail > 0 ? total / n_avail : 0;
+  const int routed = a.counts_in[a.B], mean = n_avail > 0 ? static_cast<int>(total / n_avail) : 0;
   float f[VPT];
 #pragma unroll
   for (int i = 0; i < VPT; ++i) f[i] = total > 0 ? static_cast<float>(cnt[i] - mean) / static_cast<float>(total) : 0.0f;

@@ -1,0 +1,33 @@
+"""GPU tests of the operators around a routed layer step where a call is allowed but unusual: sums of counts past 32 bits."""
+import numpy as np
+import pytest
+import torch
+
+import oracle
+from tests.helpers import stream_ptr
+from tests.test_gpu_operators import TORCH, U, dev, host, kind
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ router
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,B", [(5, 3), (9, 32), (3, 256)])
+def test_route_gradient_of_counts_past_32_bits(lib, n, B, dtype):
+    """The counts of all branches may add up to more than 2^31 (2^24 tokens on 128 of 256 branches)."""
+    rng = np.random.default_rng([91, B])
+    logits = dev(rng.normal(size=(n, B)), dtype)
+    routed = (1 << 31) - 5
+    counts = np.append(rng.integers(int(0.6 * routed), routed, size=B), routed)
+    assert counts[:-1].sum() > 1 << 31
+    grad = torch.empty(n, B, device="cuda", dtype=TORCH[dtype])
+    scale = 2.0 ** 31                                    # the gradient's 1 / T, so that bf16's smallest values play no part
+    lib.mlpmoe_route_backward(logits, torch.from_numpy(counts.astype(np.int32)).cuda(), grad, n, B, grad_loss=dev([scale]), dtype=kind(lib, dtype),
+                              stream=stream_ptr())
+    lh = host(logits)
+    want, size = oracle.route_grad(lh, counts, grad_loss=scale)
+    # as check_route of the other file: x - max (span u), expf, the row's sum, a reciprocal and a product, twice; a dot product of B terms
+    rel = (float(lh.max() - lh.min()) + 20) * U
+    assert np.all(np.abs(host(grad) - want) <= (2 * rel + (B + 20) * U) * size + (2.0 ** -8 if dtype == "bf16" else 0.0) * np.abs(want) + 1e-38)
+    assert np.abs(want).max() > 0
