@@ -175,9 +175,45 @@ constexpr int64_t kTcWork = int64_t(768) << 20;
 std::atomic<uint64_t> g_wait_limit_ns{1000000000ull};
 std::atomic<uint32_t> g_extra_arrivals{0};
 
+// The streaming kernels' split of both products.
+struct StreamPlan {
+  W4Args u, w;                  // gate|up, down
+  int u_cluster, w_cluster;     // 0: no split
+};
+void plan_stream(const mlpmoe_w4_layer_t* l, int n, int digits, bool dense, StreamPlan* p) {
+  const int64_t d = l->d_model, I = l->d_inter;
+  p->u = W4Args{};
+  p->u.rows = static_cast<int>(I);
+  p->u.tiles = static_cast<int>(I / 8);
+  p->u.K = static_cast<int>(d);
+  p->u.kblocks = static_cast<int>((d + 127) / 128);
+  p->u.n = n;
+  p->u.B = l->B;
+  p->u.dense = dense;
+  p->w = W4Args{};
+  p->w.rows = static_cast<int>(d);
+  p->w.tiles = static_cast<int>((d + 15) / 16);
+  p->w.K = static_cast<int>(I);
+  p->w.kblocks = static_cast<int>((I + 127) / 128);
+  p->w.n = n;
+  p->w.B = l->B;
+  p->w.dense = dense;
+  p->u_cluster = w4_plan(&p->u, digits, l->group);
+  p->w_cluster = p->u_cluster == 0 ? 0 : w4_plan(&p->w, digits, l->group);
+}
+
+inline int digits_of(mlpmoe_dtype_t y_dtype) { return y_dtype == MLPMOE_FP32 ? 3 : 2; }
+
+// A few tokens stream, unless a block's share of a row's activations does not fit beside the rings even where eight blocks share K
+// (group 32: from about 49,000 columns on; group 64: both dimensions near 65,536); the tiled kernels stream K.  Fills the plan where
+// the answer is STREAM.
 enum Path { STREAM, WIDE, TENSOR };
-Path path_of(const mlpmoe_w4_layer_t* l, int64_t n, mlpmoe_dtype_t y_dtype) {
-  if (n < kWideFrom) return STREAM;
+Path path_of(const mlpmoe_w4_layer_t* l, int64_t n, mlpmoe_dtype_t y_dtype, bool dense, StreamPlan* plan) {
+  if (n < kWideFrom) {
+    if (n == 0) return STREAM;
+    plan_stream(l, static_cast<int>(n), digits_of(y_dtype), dense, plan);
+    return plan->w_cluster != 0 ? STREAM : WIDE;
+  }
   if (y_dtype != MLPMOE_BF16 || l->d_model < 128 || l->d_inter < 128) return WIDE;
   return n * (3 * l->d_model * l->d_inter) >= kTcWork ? TENSOR : WIDE;
 }
@@ -424,13 +460,14 @@ mlpmoe_status_t mlpmoe_w4_workspace(const mlpmoe_w4_layer_t* layer, int64_t n_to
   if (rc != MLPMOE_OK) return rc;
   if (n_tokens < 0) return MLPMOE_ERR_INVALID_ARG;
   if (n_tokens > kW4MaxTokens) return MLPMOE_ERR_UNSUPPORTED;
-  // the most that a call with any types needs
+  // the most that a call with any types, with or without a selection, needs
   *bytes = 0;
-  for (int k = 2; k <= 3; ++k) {
-    const int64_t wide = layout_of(layer, n_tokens, path_of(layer, n_tokens, MLPMOE_FP32), k).total;
-    const int64_t tensor = layout_of(layer, n_tokens, path_of(layer, n_tokens, MLPMOE_BF16), k).total;
-    if (wide > *bytes) *bytes = wide;
-    if (tensor > *bytes) *bytes = tensor;
+  for (const mlpmoe_dtype_t y_dtype : {MLPMOE_FP32, MLPMOE_BF16}) {
+    for (const bool dense : {false, true}) {
+      StreamPlan plan;
+      const int64_t total = layout_of(layer, n_tokens, path_of(layer, n_tokens, y_dtype, dense, &plan), digits_of(y_dtype)).total;
+      if (total > *bytes) *bytes = total;
+    }
   }
   return MLPMOE_OK;
 }
@@ -472,53 +509,38 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
   if (!x || !y || !on(x, 16) || !on(y, 16) || !on(residual, 16) || (scaled && (!x_scale || !on(x_scale, 4)))) return MLPMOE_ERR_INVALID_ARG;
   if (residual && residual == y && y_dtype != MLPMOE_FP32) return MLPMOE_ERR_INVALID_ARG;
 
-  const Path path = path_of(layer, n_tokens, y_dtype);
-  const Layout l = layout_of(layer, n_tokens, path, y_dtype == MLPMOE_FP32 ? 3 : 2);
+  bool dense = select == nullptr;
+  for (int b = 0; b < layer->B && layer->alpha != nullptr; ++b) dense = dense && layer->alpha[b] != 0.0f;
+  StreamPlan plan;
+  const Path path = path_of(layer, n_tokens, y_dtype, dense, &plan);
+  const Layout l = layout_of(layer, n_tokens, path, digits_of(y_dtype));
   if (!workspace || workspace_bytes < l.total || !on(workspace, 256)) return MLPMOE_ERR_INVALID_ARG;
 
-  const int group = layer->group, n = static_cast<int>(n_tokens), digits = y_dtype == MLPMOE_FP32 ? 3 : 2;
+  const int group = layer->group, n = static_cast<int>(n_tokens);
   if (path == TENSOR) return forward_tc(layer, x, x_dtype, x_stride, x_scale, x_group, select, compensate, residual, y, n, workspace, stream);
   if (path == WIDE)
     return forward_wide(layer, x, x_dtype, x_stride, x_scale, x_group, select, compensate, residual, y, y_dtype, n, workspace, stream);
-  W4Args u = {};
+  W4Args& u = plan.u;
   u.m[0] = matrix(layer->gate, I, d, group);
   u.m[1] = matrix(layer->up, I, d, group);
-  u.rows = static_cast<int>(I);
-  u.tiles = static_cast<int>(I / 8);
-  u.K = static_cast<int>(d);
-  u.kblocks = static_cast<int>((d + 127) / 128);
-  u.n = n;
   if (scaled) {
     u.x_scale = x_scale;
     u.x_groups = x_group == 0 ? 1 : static_cast<int>((d + x_group - 1) / x_group);
     for (int64_t g = group; x_group != 0 && g < x_group; g *= 2) ++u.x_shift;
   }
-  u.B = layer->B;
   u.select = select;
-  u.dense = select == nullptr;
   for (int b = 0; b < layer->B; ++b) {
     u.off[b + 1] = u.off[b] + static_cast<int32_t>(layer->d_b[b]);
     u.alpha[b] = layer->alpha ? layer->alpha[b] : 1.0f;
-    if (u.alpha[b] == 0.0f) u.dense = 0;
   }
-  const int u_cluster = w4_plan(&u, digits, group);
   u.x = x;
   u.x_kind = x_dtype;
   u.x_stride = x_stride;
   u.h = reinterpret_cast<float*>(static_cast<char*>(workspace) + l.h);
   u.status = static_cast<uint32_t*>(workspace);
 
-  W4Args w = {};
+  W4Args& w = plan.w;
   w.m[0] = w.m[1] = matrix(layer->down, d, I, group);
-  w.rows = static_cast<int>(d);
-  w.tiles = static_cast<int>((d + 15) / 16);
-  w.K = static_cast<int>(I);
-  w.kblocks = static_cast<int>((I + 127) / 128);
-  w.n = n;
-  w.B = u.B;
-  w.dense = u.dense;
-  const int w_cluster = w4_plan(&w, digits, group);
-  if (u_cluster == 0 || w_cluster == 0) return MLPMOE_ERR_UNSUPPORTED;
   w.x = u.h;
   w.x_kind = MLPMOE_FP32;
   w.x_stride = I;
@@ -531,8 +553,8 @@ mlpmoe_status_t mlpmoe_w4_forward(const mlpmoe_w4_layer_t* layer, const void* x,
   w.y_bf16 = y_dtype == MLPMOE_BF16 ? 1 : 0;
 
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (BY_GROUP(gateup, group, u, u_cluster, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
-  return BY_GROUP(down, group, w, w_cluster, st) == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
+  if (BY_GROUP(gateup, group, u, plan.u_cluster, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
+  return BY_GROUP(down, group, w, plan.w_cluster, st) == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
 }
 
 }  // extern "C"

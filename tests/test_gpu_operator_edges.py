@@ -1,13 +1,30 @@
-"""GPU tests of the operators around a routed layer step where a call is allowed but unusual: sums of counts past 32 bits."""
+"""GPU tests of the operators around a routed layer step where a call is allowed but unusual: long rows on small groups, sums of
+counts past 32 bits."""
 import numpy as np
 import pytest
 import torch
 
 import oracle
 from tests.helpers import stream_ptr
-from tests.test_gpu_operators import TORCH, U, dev, host, kind
+from tests.test_gpu_operators import TORCH, U, W4Case, dev, host, kind
 
 pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------ 4-bit layer
+
+@pytest.mark.parametrize("group", [32, 64])
+@pytest.mark.parametrize("d,d_b", [(51328, [64, 80]), (53248, [96, 48]), (65536, [64, 80]), (136, [51312, 16]), (128, [53232, 16]), (128, [65520, 16])])
+def test_w4_forward_long_rows_on_small_groups(lib, d, d_b, group):
+    """Rows whose digits, units and rings do not fit in shared memory together: few tokens take the tiled kernels then."""
+    c = W4Case(lib, [81, d, group], d, d_b, group, True, std=0.02)
+    for n, yt in ((1, "fp32"), (1, "bf16"), (5, "fp32"), (8, "bf16"), (8, "fp32"), (11, "fp32")):
+        xh, x, _ = c.activations([82, n], n, "bf16")
+        c.check(c.run(x, n, "bf16", yt), xh, "bf16", yt)
+        sel = np.zeros((n, 2), np.uint8)
+        sel[:, 0] = 1
+        sel[0, 1] = 1
+        c.check(c.run(x, n, "bf16", yt, select=torch.from_numpy(sel).cuda()), xh, "bf16", yt, sel)
 
 
 # ------------------------------------------------------------------------------------------------ router

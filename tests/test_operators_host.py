@@ -199,3 +199,28 @@ def test_w4_workspace_grows_with_the_tokens(lib):
     assert all(a <= b for a, b in zip(sizes, sizes[1:]))
     # the intermediate activations in fp32
     assert sizes[4] >= 64 * 4 * 4864
+
+
+def test_w4_forward_has_kernels_for_every_documented_size(lib):
+    """Every size is accepted with the workspace that is asked for: without a device a call gets as far as its first launch."""
+    if torch.cuda.is_available():
+        pytest.skip("the addresses here are not a device's")
+    m = (FAKE, FAKE, FAKE)
+    sizes = (8, 128, 1032, 14336, 48, 51328, 53248, 65520, 65536)
+    for group in (32, 64, 128):
+        for d in sizes:
+            for I in sizes:
+                for B in (1, 64, 256):
+                    if I % 16 or I < 16 * B:
+                        continue
+                    layer = lib.mlpmoe_w4_layer(d, I, [16] * (B - 1) + [I - 16 * (B - 1)], group, m, m, m)
+                    most = lib.mlpmoe_w4_workspace(layer, 64)
+                    last = 0
+                    for n in (1, 2, 3, 8, 9, 64):
+                        size = lib.mlpmoe_w4_workspace(layer, n)
+                        assert last <= size <= most              # a workspace serves any call of fewer tokens
+                        last = size
+                        for yt in (lib.MLPMOE_BF16, lib.MLPMOE_FP32):
+                            for select in (None, FAKE):
+                                rc = lib.lib.mlpmoe_w4_forward(layer, FAKE, 0, 0, None, 0, select, 1, None, FAKE, yt, n, FAKE, size, None)
+                                assert rc == lib.MLPMOE_ERR_CUDA, (group, d, I, B, n, yt, select)
