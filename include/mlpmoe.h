@@ -373,7 +373,8 @@ typedef struct {
  * group's largest magnitude (a group all below 2^-100 counts as 0); or, for y in bf16 on a batch large enough for the
  * kernels of the 5th-generation tensor cores, as fp16 times a power of two of the token (x) or of the token and 128
  * columns (intermediate activation), off by at most 2^-11 of each value or 2^-39 of the largest (x in bf16: only the
- * latter).  Their products with the codes are exact, scales and sums are fp32.
+ * latter).  Their products with the codes are exact, scales and sums are fp32.  An infinity or a NaN in x, or an intermediate
+ * activation past fp32's range, makes the y of its token infinite or NaN, where the token computes a branch; other tokens keep their values.
  *   x        device, [n_tokens x d_model] of x_dtype (bf16, fp32, or e4m3 with scales), rows x_stride elements apart
  *            (0 = d_model), 16-byte aligned, x_stride a multiple of 8
  *   x_scale  device fp32 [n_tokens x ceil(d_model / x_group)] for e4m3 (x_group = 0: one per token), else ignored;

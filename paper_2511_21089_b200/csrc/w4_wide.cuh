@@ -89,9 +89,9 @@ __global__ void __launch_bounds__(256) w4_digits_kernel(const __grid_constant__ 
   float v[8], top = 0.0f, unit;
   to_f32(raw, a.kind, v);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+  for (int e = 0; e < 8; ++e) top = larger(top, v[e]);
 #pragma unroll
-  for (int o = 1; o < kLanes; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+  for (int o = 1; o < kLanes; o *= 2) top = larger(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
   const int pieces = a.slots_per_token + 1;
   uint32_t m[8];
   const bool some = to_fixed(v, top, pieces, &unit, m);

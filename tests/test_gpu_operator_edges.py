@@ -1,12 +1,12 @@
-"""GPU tests of the operators around a routed layer step where a call is allowed but unusual: long rows on small groups, sums of
-counts past 32 bits."""
+"""GPU tests of the operators around a routed layer step where a call is allowed but unusual: long rows on small groups, values
+that are not finite, sums of counts past 32 bits."""
 import numpy as np
 import pytest
 import torch
 
 import oracle
 from tests.helpers import stream_ptr
-from tests.test_gpu_operators import TORCH, U, W4Case, dev, host, kind
+from tests.test_gpu_operators import PATHS, TORCH, U, W4Case, dev, host, kind
 
 pytestmark = pytest.mark.gpu
 
@@ -25,6 +25,35 @@ def test_w4_forward_long_rows_on_small_groups(lib, d, d_b, group):
         sel[:, 0] = 1
         sel[0, 1] = 1
         c.check(c.run(x, n, "bf16", yt, select=torch.from_numpy(sel).cuda()), xh, "bf16", yt, sel)
+
+
+# every path with every type of y that it takes: (d_model, branch widths, tokens, type of y)
+EVERY = {"stream fp32": (520, [96, 160, 256], 5, "fp32"), "stream bf16": (520, [96, 160, 256], 7, "bf16"), "tiled fp32": (520, [96, 160, 256], 40, "fp32"),
+         "tiled bf16": (520, [96, 160, 256], 40, "bf16"), "tensor": PATHS["tensor"]}
+
+
+@pytest.mark.parametrize("path", list(EVERY))
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_w4_forward_values_that_are_not_finite(lib, path, group):
+    """A NaN or an infinity in a live token's x, or an intermediate activation past fp32's range, shows in all of the token's y; the
+    other tokens keep their bits."""
+    d, d_b, n, yt = EVERY[path]
+    c = W4Case(lib, [83, group], d, d_b, group, False, std=0.05)
+    for xt, bad in (("bf16", (float("nan"), float("inf"), float("-inf"))), ("fp32", (float("nan"), float("inf"), 1e30)), ("e4m3", (float("nan"),))):
+        _, x, sc = c.activations([84], n, xt)
+        want = c.run(x, n, xt, yt, sc).clone()
+        for k, value in enumerate(bad):
+            row, wide = (0, n - 1, 2)[k], x.float().clone()
+            if value == 1e30:
+                wide[row] *= value                      # finite x and gates, but their product is not
+            else:
+                wide[row, (d - 1, 37, 0)[k]] = value
+            broken = torch.empty_like(x)
+            broken.copy_(wide)
+            got = c.run(broken, n, xt, yt, sc)
+            rest = torch.arange(n, device="cuda") != row
+            assert not bool(torch.isfinite(got[row].float()).any()), (xt, value)
+            assert torch.equal(got[rest], want[rest]), (xt, value)
 
 
 # ------------------------------------------------------------------------------------------------ router
