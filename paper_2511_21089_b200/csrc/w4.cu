@@ -111,7 +111,7 @@ int wide_plan(W4WideArgs* a, int pieces, int group, bool may_share_k) {
         if (issue > cycles) cycles = issue;
         if (memory > cycles) cycles = memory;
         const int64_t own = static_cast<int64_t>(a->tokens) * (32 * rg + 4) * 4;
-        if (kW4WideStages * w4_wide_stage_bytes(rg, tiles, gpb) > w4::kSmemMax - 4096 || own > w4::kSmemMax - 4096) continue;
+        if (kW4WideStages * w4_wide_stage_bytes(rg, tiles, gpb) > w4::kWideSmemMax || own > w4::kWideSmemMax) continue;
         const int64_t cost = waves * (entries * (cycles + 200) + 4000 + (cluster > 1 ? 4000 : 0));
         if (cost < best_cost) {
           best_cost = cost;

@@ -41,6 +41,7 @@ constexpr int kWarps = 16;
 constexpr int kThreads = kWarps * 32;
 constexpr int kColPitch = 20;          // floats between the 16-row columns of a sum tile: keeps a warp's stores on 32 banks
 constexpr int kSmemMax = 226 * 1024;  // dynamic; the rest of the 227 KB is for the small static arrays
+constexpr int kWideSmemMax = kSmemMax - 4096;   // the tiled kernels have more of those
 
 // Where the unit of k8 (eight consecutive k, 0..15 in a block of 128) stands: word w of lane t of the row's four lanes.
 // A group's k have to meet in one mma, so the four lanes together cover one group (GPB groups to a block).
@@ -640,7 +641,8 @@ cudaError_t launch(const W4Args& a, int cluster, cudaStream_t st) {
   auto kernel = w4_kernel<NT, GPB, GATEUP, ZERO>;
   const int smem = smem_of<NT, GPB>(a).total;
   if (smem > kSmemMax) return cudaErrorInvalidValue;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  // the same for every call: the limit is the kernel's, and another thread's call may come between here and the launch
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemMax);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>((a.tiles + a.tiles_per_block - 1) / a.tiles_per_block), static_cast<unsigned>(cluster),

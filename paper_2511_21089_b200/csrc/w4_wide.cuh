@@ -376,7 +376,9 @@ cudaError_t launch_wide(const W4WideArgs& a, int cluster, int chunks, cudaStream
   int smem = kW4WideStages * w4_wide_stage_bytes(a.row_groups, a.slot_tiles, GPB);
   const int own = GATEUP ? 0 : a.tokens * (32 * a.row_groups + 4) * 4;
   if (own > smem) smem = own;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (smem > kWideSmemMax) return cudaErrorInvalidValue;
+  // the same for every call: the limit is the kernel's, and another thread's call may come between here and the launch
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kWideSmemMax);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>((a.tiles + 2 * a.row_groups - 1) / (2 * a.row_groups)), static_cast<unsigned>(cluster),

@@ -1,5 +1,7 @@
 """GPU tests of the operators around a routed layer step where a call is allowed but unusual: long rows on small groups, values
-that are not finite, sums of counts past 32 bits."""
+that are not finite, sums of counts past 32 bits, calls from two host threads."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -54,6 +56,37 @@ def test_w4_forward_values_that_are_not_finite(lib, path, group):
             rest = torch.arange(n, device="cuda") != row
             assert not bool(torch.isfinite(got[row].float()).any()), (xt, value)
             assert torch.equal(got[rest], want[rest]), (xt, value)
+
+
+@pytest.mark.parametrize("n,yt", [(1, "bf16"), (2, "fp32"), (12, "bf16"), (12, "fp32")])
+def test_w4_forward_from_two_threads(lib, n, yt):
+    """Layers of two sizes that run the same kernels, called from two host threads at once, on a stream and a workspace each."""
+    cases = [W4Case(lib, [88], 2048, [4096], 64, False, std=0.05), W4Case(lib, [89], 264, [64, 64], 64, False, std=0.05)]
+    jobs = []
+    for c in cases:
+        size = lib.mlpmoe_w4_workspace(c.layer, n)
+        x = c.activations([90], n, "bf16")[1].contiguous()
+        y, ws = torch.empty(n, c.d, device="cuda", dtype=TORCH[yt]), torch.empty(size, device="cuda", dtype=torch.uint8)
+        jobs.append((c, x, y, ws, size, torch.cuda.Stream(), c.run(x, n, "bf16", yt).clone()))
+    torch.cuda.synchronize()
+    failures, start = [], threading.Barrier(2)
+
+    def work(c, x, y, ws, size, stream, want):
+        try:
+            start.wait()
+            for _ in range(4000):
+                lib.mlpmoe_w4_forward(c.layer, x, y, n, ws, size, y_dtype=kind(lib, yt), stream=stream.cuda_stream)
+        except Exception as e:
+            failures.append(e)
+    threads = [threading.Thread(target=work, args=j) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failures
+    for c, x, y, ws, size, stream, want in jobs:
+        assert torch.equal(y, want)
 
 
 # ------------------------------------------------------------------------------------------------ router
