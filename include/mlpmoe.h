@@ -368,7 +368,7 @@ typedef struct {
  * unpacked once per 64 tokens or fewer, so a layer of mlpmoe_create is faster for long inputs):
  *     y_t = residual_t + c_t * sum_{b in S_t} alpha_b W_down^(b) [ silu(W_gate^(b) x_t) (.) W_up^(b) x_t ]
  * with S_t and c_t as in mlpmoe_forward_routed (select NULL: every branch with alpha_b != 0, c_t = 1).  What a branch holds
- * that no token selects does not enter y; with up to eight tokens it is not read either.  Inside each group of columns
+ * that a token does not select does not enter its y, finite or not; what no token selects is with up to eight tokens not read either.  Inside each group of columns
  * x and the intermediate activation are held as fixed point, off by at most 2^-23 (y fp32) or 2^-15 (y bf16) of the
  * group's largest magnitude (a group all below 2^-100 counts as 0); or, for y in bf16 on a batch large enough for the
  * kernels of the 5th-generation tensor cores, as fp16 times a power of two of the token (x) or of the token and 128

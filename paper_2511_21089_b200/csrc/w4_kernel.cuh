@@ -163,6 +163,8 @@ __device__ __forceinline__ void to_f32(const Raw& r, int kind, float (&v)[8]) {
   }
 }
 
+__device__ __forceinline__ bool is_finite(float v) { return fabsf(v) <= 3.402823466e38f; }
+
 // The larger magnitude; a NaN wins.
 __device__ __forceinline__ float larger(float top, float v) {
   asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(v)));
@@ -175,7 +177,7 @@ __device__ __forceinline__ float larger(float top, float v) {
 // infinity or a NaN; its unit is NaN and makes the token's sums NaN, whatever its digits are.
 __device__ __forceinline__ bool to_fixed(const float (&v)[8], float top, int pieces, float* unit, uint32_t (&m)[8]) {
   const int exponent = (__float_as_int(top * 1.00396f) >> 23) + (pieces == 3 ? 1 - 23 : 1 - 15);
-  const bool some = top >= 7.8886091e-31f && top <= 3.402823466e38f;
+  const bool some = top >= 7.8886091e-31f && is_finite(top);
   const float inv = some ? __int_as_float((254 - exponent) << 23) : 0.0f;
   *unit = some ? __int_as_float(exponent << 23) : top * 0.0f;
   if (pieces == 3) {
@@ -533,12 +535,23 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
           mma(part[nt], a0, a1, a2, a3, at & 1 ? b.z : b.x, at & 1 ? b.w : b.y);
         }
       }
+      if (!GATEUP && !a.dense && !(is_finite(s[0]) && is_finite(s[1]))) {
+        // perhaps a branch's that some token does not compute: nothing of it enters where the activations are 0
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        acc[nt][0] += (__int_as_float(part[nt][0]) - 12582912.0f) * (s[0] * unit[nt].x);
-        acc[nt][1] += (__int_as_float(part[nt][1]) - 12582912.0f) * (s[0] * unit[nt].y);
-        acc[nt][2] += (__int_as_float(part[nt][2]) - 12582912.0f) * (s[1] * unit[nt].x);
-        acc[nt][3] += (__int_as_float(part[nt][3]) - 12582912.0f) * (s[1] * unit[nt].y);
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float u = i & 1 ? unit[nt].y : unit[nt].x;
+            if (u != 0.0f) acc[nt][i] += (__int_as_float(part[nt][i]) - 12582912.0f) * (s[i / 2] * u);
+          }
+      } else {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          acc[nt][0] += (__int_as_float(part[nt][0]) - 12582912.0f) * (s[0] * unit[nt].x);
+          acc[nt][1] += (__int_as_float(part[nt][1]) - 12582912.0f) * (s[0] * unit[nt].y);
+          acc[nt][2] += (__int_as_float(part[nt][2]) - 12582912.0f) * (s[1] * unit[nt].x);
+          acc[nt][3] += (__int_as_float(part[nt][3]) - 12582912.0f) * (s[1] * unit[nt].y);
+        }
       }
     }
     slot = slot + 1 == kStages ? 0 : slot + 1;

@@ -86,6 +86,18 @@ __device__ __forceinline__ uint64_t fma2(uint64_t x, uint64_t y, uint64_t z) {
   return v;
 }
 
+// Sums of a row whose scale is not finite, perhaps of a branch that some tokens do not compute: nothing of it enters those whose
+// product with the activations is 0.
+template <int N>
+__device__ __forceinline__ void add_where_not_zero(uint64_t* acc, const uint32_t (&r)[N], float s, const float* unit) {
+#pragma unroll
+  for (int k = 0; k < N; k += 2) {
+    const float2 u = *reinterpret_cast<const float2*>(unit + k);
+    const float v0 = __uint_as_float(r[k]), v1 = __uint_as_float(r[k + 1]);
+    acc[k / 2] = fma2(pair(v0, v1), pair(v0 != 0.0f ? s * u.x : 0.0f, v1 != 0.0f ? s * u.y : 0.0f), acc[k / 2]);
+  }
+}
+
 // The unit for values of at most `top`, and its reciprocal.  Infinities and NaN pass through.
 __device__ __forceinline__ float unit_of(float top, float* inverse) {
   const int e = min(max(static_cast<int>(__float_as_uint(top) >> 23), 32), 255);      // biased exponent; 2^-95 and below share a unit
@@ -231,7 +243,8 @@ __device__ __forceinline__ void tc_outputs(const W4TcArgs& a, const float* sums,
 }
 
 // grid: (blocks of 128 rows, cluster along K, chunks)
-template <int NE, int GPB, bool GATEUP, bool ZERO>
+// MASKED: down where a token may leave out branches; their scales need not be finite.
+template <int NE, int GPB, bool GATEUP, bool ZERO, bool MASKED>
 __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_constant__ W4TcArgs a) {
   using C = TcCfg<NE, GPB, GATEUP>;
   extern __shared__ uint8_t smem_raw[];
@@ -304,19 +317,34 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
       if (!ok) break;
       const uint8_t* in = smem + stage * C::kStage;
       const float s = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(in + at_scale + step % GPB * 256));
+      const bool odd = MASKED && !is_finite(s), some_odd = MASKED && NE == 64 && __any_sync(0xFFFFFFFFu, odd);
       const int b = step & 1;
       ok = ptx::mbar_wait_bounded(&d_full[b], (step >> 1) & 1, abort_flag, a.wait_limit_ns);
       ok = __all_sync(0xFFFFFFFFu, ok);
       if (!ok) break;
       ptx::tc_fence_after();
+      if (some_odd) {                             // for the warp, before the loop: 64 columns leave no registers for a branch in it
+#pragma unroll
+        for (int i = 0; i < NE; i += 8) {
+          uint32_t r[8];
+          ptx::tmem_ld_32x8(taddr + b * 2 * NE + i, r);
+          ptx::tmem_ld_wait();
+          add_where_not_zero(acc + i / 2, r, s, reinterpret_cast<const float*>(in + at_unit) + i);
+        }
+      }
       constexpr int kPart = NE == 64 ? (GATEUP ? 16 : 8) : 32;   // what the registers hold beside the sums
 #pragma unroll
       for (int i = 0; i < NE; i += kPart) {
+        if (some_odd) break;
         uint32_t r[kPart];
         if constexpr (kPart == 32) ptx::tmem_ld_32x32(taddr + b * 2 * NE + i, r);
         else if constexpr (kPart == 16) ptx::tmem_ld_32x16(taddr + b * 2 * NE + i, r);
         else ptx::tmem_ld_32x8(taddr + b * 2 * NE + i, r);
         ptx::tmem_ld_wait();
+        if (NE == 32 && odd) {
+          add_where_not_zero(acc + i / 2, r, s, reinterpret_cast<const float*>(in + at_unit) + i);
+          continue;
+        }
 #pragma unroll
         for (int k = 0; k < kPart; k += 4) {
           uint64_t s0 = pair(s, s), s1 = s0;
@@ -521,9 +549,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
   }
 }
 
-template <int NE, int GPB, bool GATEUP, bool ZERO>
+template <int NE, int GPB, bool GATEUP, bool ZERO, bool MASKED>
 cudaError_t launch_tc(const W4TcArgs& a, int cluster, cudaStream_t st) {
-  auto kernel = w4_tc_kernel<NE, GPB, GATEUP, ZERO>;
+  auto kernel = w4_tc_kernel<NE, GPB, GATEUP, ZERO, MASKED>;
   const int smem = TcCfg<NE, GPB, GATEUP>::kSmem;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
@@ -545,11 +573,17 @@ cudaError_t launch_tc(const W4TcArgs& a, int cluster, cudaStream_t st) {
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
+template <int NE, int GPB, bool GATEUP, bool ZERO>
+cudaError_t launch_tc_masked(const W4TcArgs& a, int cluster, cudaStream_t st) {
+  // the test of every scale costs up to 3 us of 98 (4096 x 14336, 128 tokens), so calls without a selection go without it
+  return GATEUP || a.dense ? launch_tc<NE, GPB, GATEUP, ZERO, false>(a, cluster, st) : launch_tc<NE, GPB, GATEUP, ZERO, !GATEUP>(a, cluster, st);
+}
+
 template <int GPB, bool GATEUP>
 cudaError_t launch_tc_any(const W4TcArgs& a, int cluster, cudaStream_t st) {
   const bool zero = a.m[0].zero != nullptr || a.m[1].zero != nullptr;
-  if (a.ne == 32) return zero ? launch_tc<32, GPB, GATEUP, true>(a, cluster, st) : launch_tc<32, GPB, GATEUP, false>(a, cluster, st);
-  return zero ? launch_tc<64, GPB, GATEUP, true>(a, cluster, st) : launch_tc<64, GPB, GATEUP, false>(a, cluster, st);
+  if (a.ne == 32) return zero ? launch_tc_masked<32, GPB, GATEUP, true>(a, cluster, st) : launch_tc_masked<32, GPB, GATEUP, false>(a, cluster, st);
+  return zero ? launch_tc_masked<64, GPB, GATEUP, true>(a, cluster, st) : launch_tc_masked<64, GPB, GATEUP, false>(a, cluster, st);
 }
 
 }  // namespace w4

@@ -286,8 +286,11 @@ __global__ void __launch_bounds__(512, 1) w4_wide_kernel(const __grid_constant__
             mma(part, op[rt][w][0], op[rt][w][1], op[rt][w][2], op[rt][w][3], at & 1 ? v.z : v.x, at & 1 ? v.w : v.y);
           }
           // at most 15 * 128 * (128 + 256 * 127): exact in 32 bits, rounded once to fp32
-          acc[rt][nt][0] += __int2float_rn(part[0] + 256 * part[1]) * (s[rt][0] * unit.x);
-          acc[rt][nt][1] += __int2float_rn(part[2] + 256 * part[3]) * (s[rt][1] * unit.x);
+          // a branch that the token does not compute: its activations are 0, its scales may be anything
+          if (GATEUP || a.dense || unit.x != 0.0f) {
+            acc[rt][nt][0] += __int2float_rn(part[0] + 256 * part[1]) * (s[rt][0] * unit.x);
+            acc[rt][nt][1] += __int2float_rn(part[2] + 256 * part[3]) * (s[rt][1] * unit.x);
+          }
         }
       }
     }

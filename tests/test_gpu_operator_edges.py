@@ -1,5 +1,5 @@
 """GPU tests of the operators around a routed layer step where a call is allowed but unusual: long rows on small groups, values
-that are not finite, sums of counts past 32 bits, calls from two host threads."""
+that are not finite, sums of counts past 32 bits, calls from two host threads, weights that no token uses."""
 import threading
 
 import numpy as np
@@ -56,6 +56,38 @@ def test_w4_forward_values_that_are_not_finite(lib, path, group):
             rest = torch.arange(n, device="cuda") != row
             assert not bool(torch.isfinite(got[row].float()).any()), (xt, value)
             assert torch.equal(got[rest], want[rest]), (xt, value)
+
+
+@pytest.mark.parametrize("path", list(EVERY))
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("group", [32, 128])
+def test_w4_forward_down_weights_that_a_token_does_not_use(lib, path, value, group):
+    """W_down's scales of a branch are not finite: tokens without the branch are as if it were not there, tokens with it are not
+    finite; and a branch with alpha = 0 stays out without a selection."""
+    d, d_b, n, yt = {"stream": (200, [96, 32, 128, 256], 6, path[7:]), "tiled": (200, [96, 32, 128, 256], 40, path[6:]),
+                     "tensor": (1032, [4448, 160, 4352, 128], 66, "bf16")}[path.split()[0]]
+    off = oracle.branch_offsets(d_b)
+    assert off[1] % 32 == 0 and off[2] % 128 == 0
+    c = W4Case(lib, [85, group], d, d_b, group, True, std=0.05)
+    dead = 1 if group == 32 else 3                       # one inside blocks of 128 columns that others use too; one of its own
+    xh, x, _ = c.activations([86], n, "bf16")
+    sel = (np.random.default_rng(87).uniform(size=(n, 4)) < 0.5).astype(np.uint8)
+    sel[:, 0] |= 1                                       # every token uses the blocks around the branch
+    sel[:, 2] |= 1
+    none = sel.copy()
+    none[:, dead] = 0
+    sel[:, dead] = np.arange(n) % 2
+    c.mats[2][1][off[dead] // group:off[dead + 1] // group] = value
+    c.check(c.run(x, n, "bf16", yt, select=torch.from_numpy(none).cuda()), xh, "bf16", yt, none, fp16=path == "tensor")
+    got = c.run(x, n, "bf16", yt, select=torch.from_numpy(sel).cuda())
+    assert not bool(torch.isfinite(got[1::2].float()).any())
+    r = oracle.w4_layer_forward(xh[0::2], *c.W, d_b, None, sel[0::2])
+    tol = c.tolerance(r, xh[0::2], yt, "bf16" if path == "tensor" else None) + (2.0 ** -8 if yt == "bf16" else 0.0) * np.abs(r["y"])
+    assert np.all(np.abs(host(got)[0::2] - r["y"]) <= tol + 1e-30)
+    c.alpha = [1.0, 1.0, 0.7, 1.0]
+    c.alpha[dead] = 0.0
+    c.layer = lib.mlpmoe_w4_layer(d, c.I, d_b, group, *c.mats, alpha=c.alpha)
+    c.check(c.run(x, n, "bf16", yt), xh, "bf16", yt, fp16=path == "tensor")
 
 
 @pytest.mark.parametrize("n,yt", [(1, "bf16"), (2, "fp32"), (12, "bf16"), (12, "fp32")])
