@@ -165,21 +165,31 @@ __device__ __forceinline__ void to_f32(const Raw& r, int kind, float (&v)[8]) {
 
 __device__ __forceinline__ bool is_finite(float v) { return fabsf(v) <= 3.402823466e38f; }
 
-// The larger magnitude; a NaN wins.
-__device__ __forceinline__ float larger(float top, float v) {
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(top) : "f"(fabsf(v)));
+// The largest magnitude; a NaN wins.
+__device__ __forceinline__ float larger(float a, float b) {
+  float top;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(top) : "f"(fabsf(a)), "f"(fabsf(b)));
+  return top;
+}
+__device__ __forceinline__ float largest(const float (&v)[8]) {
+  float top = larger(v[0], v[1]);
+#pragma unroll
+  for (int e = 2; e < 8; e += 2) {
+    const float next = top;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(top) : "f"(next), "f"(fabsf(v[e])), "f"(fabsf(v[e + 1])));
+  }
   return top;
 }
 // Eight activations as whole numbers of a unit, the power of two that puts the group's largest magnitude `top` between
 // 2^22 / 1.004 and 8355711 (three digits of at most 127; two: 2^14 / 1.004 and 32639), so that x / unit is exact before it
 // is rounded.  m: the number plus 0x808080, exclusive-or 0x808080, whose bytes are its digits -128 .. 127, lowest first.
-// A group all below 2^-100 counts as 0 (its unit would leave the range of fp32) and returns false.  So does a group with an
-// infinity or a NaN; its unit is NaN and makes the token's sums NaN, whatever its digits are.
+// A group all below 2^-100 counts as 0 (its unit would leave the range of fp32) and returns false.  The unit of a group with an
+// infinity or a NaN is NaN and makes the token's sums NaN, whatever the digits are.
 __device__ __forceinline__ bool to_fixed(const float (&v)[8], float top, int pieces, float* unit, uint32_t (&m)[8]) {
   const int exponent = (__float_as_int(top * 1.00396f) >> 23) + (pieces == 3 ? 1 - 23 : 1 - 15);
-  const bool some = top >= 7.8886091e-31f && is_finite(top);
+  const bool some = top >= 7.8886091e-31f;
   const float inv = some ? __int_as_float((254 - exponent) << 23) : 0.0f;
-  *unit = some ? __int_as_float(exponent << 23) : top * 0.0f;
+  *unit = fmaf(top, 0.0f, some ? __int_as_float(exponent << 23) : 0.0f);
   if (pieces == 3) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) m[e] = (static_cast<uint32_t>(__float2int_rn(v[e] * inv)) + 0x00808080u) ^ 0x00808080u;
@@ -404,10 +414,9 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
       for (int u = 0; u < kBatch; ++u) {
         if (toks[u] >= tokens) break;
         const int k8 = is[u] & 15, entry = is[u] >> 4;
-        float v[8], top = 0.0f;
+        float v[8];
         to_f32(raw[u], kind, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) top = larger(top, v[e]);
+        float top = largest(v);
 #pragma unroll
         for (int o = 1; o < kLanes; o *= 2) top = larger(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         float unit;

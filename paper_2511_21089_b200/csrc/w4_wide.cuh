@@ -86,10 +86,9 @@ __global__ void __launch_bounds__(256) w4_digits_kernel(const __grid_constant__ 
   Raw raw;
   raw.lo = raw.hi = make_uint4(0u, 0u, 0u, 0u);
   if (token < a.n && u * 8 < a.K) raw = load_raw(a.x, a.kind, token * a.stride + u * 8);
-  float v[8], top = 0.0f, unit;
+  float v[8], unit;
   to_f32(raw, a.kind, v);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) top = larger(top, v[e]);
+  float top = largest(v);
 #pragma unroll
   for (int o = 1; o < kLanes; o *= 2) top = larger(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
   const int pieces = a.slots_per_token + 1;
