@@ -133,11 +133,15 @@ def _ptr(t) -> Optional[int]:
     try:
         return t.data_ptr()        # torch first: this is most of a call's host time
     except AttributeError:
-        return t.ctypes.data if isinstance(t, np.ndarray) else int(t)
+        if isinstance(t, np.ndarray):
+            return t.ctypes.data
+        if isinstance(t, int):
+            return t
+        raise                      # anything else is no buffer
 
 
 def _stream(stream) -> Optional[int]:
-    if stream is None or type(stream) is int:
+    if stream is None or isinstance(stream, int):
         return stream
     return stream.cuda_stream
 

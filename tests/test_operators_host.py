@@ -224,3 +224,22 @@ def test_w4_forward_has_kernels_for_every_documented_size(lib):
                             for select in (None, FAKE):
                                 rc = lib.lib.mlpmoe_w4_forward(layer, FAKE, 0, 0, None, 0, select, 1, None, FAKE, yt, n, FAKE, size, None)
                                 assert rc == lib.MLPMOE_ERR_CUDA, (group, d, I, B, n, yt, select)
+
+
+def test_binding_takes_buffers_and_streams_only(lib):
+    """What is no buffer raises before the library is called; addresses and streams may be subclasses of int."""
+    class Address(int):
+        pass
+
+    array, tensor = np.zeros(4, np.float32), torch.zeros(4)
+    assert lib._ptr(None) is None and lib._ptr(Address(FAKE)) == FAKE
+    assert lib._ptr(array) == array.ctypes.data and lib._ptr(tensor) == tensor.data_ptr()
+    for wrong in (1.5, "4096", b"4096", [1, 2], np.float32(3.0), object()):
+        with pytest.raises(AttributeError):
+            lib._ptr(wrong)
+        with pytest.raises(AttributeError):
+            lib.mlpmoe_add_rmsnorm(wrong, None, None, None, 0, 64)
+    assert lib._stream(None) is None and lib._stream(Address(7)) == 7
+    for wrong in (1.5, "0"):
+        with pytest.raises(AttributeError):
+            lib._stream(wrong)
