@@ -183,9 +183,9 @@ __device__ __forceinline__ float largest(const float (&v)[8]) {
 // Eight activations as whole numbers of a unit, the power of two that puts the group's largest magnitude `top` between
 // 2^22 / 1.004 and 8355711 (three digits of at most 127; two: 2^14 / 1.004 and 32639), so that x / unit is exact before it
 // is rounded.  m: the number plus 0x808080, exclusive-or 0x808080, whose bytes are its digits -128 .. 127, lowest first.
-// A group all below 2^-100 counts as 0 (its unit would leave the range of fp32) and returns false.  The unit of a group with an
-// infinity or a NaN is NaN and makes the token's sums NaN, whatever the digits are.
-__device__ __forceinline__ bool to_fixed(const float (&v)[8], float top, int pieces, float* unit, uint32_t (&m)[8]) {
+// A group all below 2^-100 counts as 0 (its unit would leave the range of fp32).  The unit of a group with an infinity or a NaN is
+// NaN and makes the token's sums NaN, whatever the digits are.
+__device__ __forceinline__ void to_fixed(const float (&v)[8], float top, int pieces, float* unit, uint32_t (&m)[8]) {
   const int exponent = (__float_as_int(top * 1.00396f) >> 23) + (pieces == 3 ? 1 - 23 : 1 - 15);
   const bool some = top >= 7.8886091e-31f;
   const float inv = some ? __int_as_float((254 - exponent) << 23) : 0.0f;
@@ -197,7 +197,6 @@ __device__ __forceinline__ bool to_fixed(const float (&v)[8], float top, int pie
 #pragma unroll
     for (int e = 0; e < 8; ++e) m[e] = (__float_as_uint(fmaf(v[e], inv, 12582912.0f)) - 0x4B400000u + 0x00808080u) ^ 0x00808080u;
   }
-  return some;
 }
 // Digits p of the even and of the odd four.
 __device__ __forceinline__ uint2 digit_of(const uint32_t (&m)[8], int p) {
@@ -421,9 +420,9 @@ __global__ void __launch_bounds__(kThreads, 1) w4_kernel(const __grid_constant__
         for (int o = 1; o < kLanes; o *= 2) top = larger(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
         float unit;
         uint32_t m[8];
-        const bool some = to_fixed(v, top, a.c.pieces, &unit, m);
+        to_fixed(v, top, a.c.pieces, &unit, m);
         const int j = k8 / kLanes, word = unit_word<GPB>(k8);
-        if (GATEUP && a.x_scale != nullptr && k8 % kLanes == 0 && some) {
+        if (GATEUP && a.x_scale != nullptr && k8 % kLanes == 0 && s_list[entry] * 128 + k8 * 8 < a.K && chunk * tokens + toks[u] < a.n) {
           const int xg = a.x_groups == 1 ? 0 : (s_list[entry] * GPB + j) >> a.x_shift;
           unit *= a.x_scale[static_cast<int64_t>(chunk * tokens + toks[u]) * a.x_groups + xg];
         }

@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(256) w4_digits_kernel(const __grid_constant__ 
   for (int o = 1; o < kLanes; o *= 2) top = larger(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
   const int pieces = a.slots_per_token + 1;
   uint32_t m[8];
-  const bool some = to_fixed(v, top, pieces, &unit, m);
+  to_fixed(v, top, pieces, &unit, m);
   const uint2 d0 = digit_of(m, 0), d1 = digit_of(m, 1), d2 = digit_of(m, 2);
   int sum01 = sum_of_eight(d0) + 256 * sum_of_eight(d1), sum2 = sum_of_eight(d2);
 #pragma unroll
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(256) w4_digits_kernel(const __grid_constant__ 
     *place(slot + 1, 1) = make_uint2(0u, 0u);
   }
   if (k8 % kLanes == 0) {
-    if (a.x_scale != nullptr && some) {
+    if (a.x_scale != nullptr && u * 8 < a.K) {
       const int xg = a.x_groups == 1 ? 0 : (u / 16 * GPB + j) >> a.x_shift;
       unit *= a.x_scale[token * a.x_groups + xg];
     }

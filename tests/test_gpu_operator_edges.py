@@ -59,6 +59,26 @@ def test_w4_forward_values_that_are_not_finite(lib, path, group):
 
 
 @pytest.mark.parametrize("path", list(EVERY))
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("group,x_group", [(32, 0), (32, 64), (128, 128)])
+def test_w4_forward_scales_of_x_that_are_not_finite(lib, path, value, group, x_group):
+    """A scale of 8-bit activations that is NaN or infinite shows in all of the token's y, also over codes that are all 0."""
+    d, d_b, n, yt = EVERY[path]
+    c = W4Case(lib, [92, group], d, d_b, group, True, std=0.05)
+    _, x, sc = c.activations([93], n, "e4m3", x_group)
+    want = c.run(x, n, "e4m3", yt, sc, x_group).clone()
+    zeros, broken = x.view(torch.uint8).clone().view(x.dtype), sc.clone()
+    last = broken.shape[1] - 1
+    broken[1, last], broken[n - 1, 0] = value, value
+    zeros.view(torch.uint8)[n - 1, :x_group or d] = 0
+    zeros.view(torch.uint8)[1, last * x_group:] = 0
+    got = c.run(zeros, n, "e4m3", yt, broken, x_group)
+    rest = torch.ones(n, dtype=torch.bool, device="cuda")
+    rest[1] = rest[n - 1] = False
+    assert not bool(torch.isfinite(got[~rest].float()).any()) and torch.equal(got[rest], want[rest])
+
+
+@pytest.mark.parametrize("path", list(EVERY))
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
 @pytest.mark.parametrize("group", [32, 128])
 def test_w4_forward_down_weights_that_a_token_does_not_use(lib, path, value, group):
