@@ -368,13 +368,16 @@ typedef struct {
  * unpacked once per 64 tokens or fewer, so a layer of mlpmoe_create is faster for long inputs):
  *     y_t = residual_t + c_t * sum_{b in S_t} alpha_b W_down^(b) [ silu(W_gate^(b) x_t) (.) W_up^(b) x_t ]
  * with S_t and c_t as in mlpmoe_forward_routed (select NULL: every branch with alpha_b != 0, c_t = 1).  What a branch holds
- * that a token does not select does not enter its y, finite or not; what no token selects is with up to eight tokens not read either.  Inside each group of columns
- * x and the intermediate activation are held as fixed point, off by at most 2^-23 (y fp32) or 2^-15 (y bf16) of the
- * group's largest magnitude (a group all below 2^-100 counts as 0); or, for y in bf16 on a batch large enough for the
- * kernels of the 5th-generation tensor cores, as fp16 times a power of two of the token (x) or of the token and 128
- * columns (intermediate activation), off by at most 2^-11 of each value or 2^-39 of the largest (x in bf16: only the
- * latter).  Their products with the codes are exact, scales and sums are fp32.  An infinity or a NaN in x, or an intermediate
- * activation past fp32's range, makes the y of its token infinite or NaN, where the token computes a branch; other tokens keep their values.
+ * that a token does not select does not enter its y, finite or not; what no token selects is with up to eight tokens not
+ * read either.
+ * Inside each group of columns x and the intermediate activation are held as fixed point, off by at most 2^-23 (y fp32) or
+ * 2^-15 (y bf16) of the group's largest magnitude (a group all below 2^-100 counts as 0); or, for y in bf16 on a batch large
+ * enough for the kernels of the 5th-generation tensor cores, as fp16 times a power of two of the token (x) or of the token
+ * and 128 columns (intermediate activation), off by at most 2^-11 of each value or 2^-39 of the largest (x in bf16: only the
+ * latter), with silu by the fast exponential (off by (4 + 1.2 |gate|) 2^-23 of its value).  Their products with the codes are
+ * exact, scales and sums are fp32.  Which kernels run, and with them the last bits of a token's y, depends on n_tokens, y_dtype
+ * and the layer's sizes.  An infinity or a NaN in x or its scale, or an intermediate activation past fp32's range, makes the y of
+ * its token infinite or NaN, where the token computes a branch; other tokens keep their values.
  *   x        device, [n_tokens x d_model] of x_dtype (bf16, fp32, or e4m3 with scales), rows x_stride elements apart
  *            (0 = d_model), 16-byte aligned, x_stride a multiple of 8
  *   x_scale  device fp32 [n_tokens x ceil(d_model / x_group)] for e4m3 (x_group = 0: one per token), else ignored;
@@ -382,7 +385,7 @@ typedef struct {
  *   select   device uint8 [n_tokens x B] or NULL
  *   residual device fp32 [n_tokens x d_model] or NULL; may be y when y_dtype is fp32
  *   y        device, [n_tokens x d_model] of y_dtype (fp32 or bf16), 16-byte aligned
- *   workspace device, 256-byte aligned, of the size that mlpmoe_w4_workspace gives
+ *   workspace device, 256-byte aligned, of the size that mlpmoe_w4_workspace gives for n_tokens or more
  * d_model a multiple of 8, d_b multiples of 16, B <= 256, d_model and d_inter up to 65536, n_tokens up to 65536.
  * The same call gives the same bits every time.  Errors as mlpmoe_create and mlpmoe_forward_ex.
  */

@@ -2,7 +2,8 @@
 //     s = x + r,  x_out = s,  v = s / sqrt(mean(s^2) + eps) * gain,  out = v | e4m3(v / scale).
 // HBM-bound (a few operations per element): every element of x and r is read once and stays in registers
 // between the sum of squares and the output, so a row costs one trip through memory.  16384 x 4096 fp32 + bf16 to fp32 and
-// e4m3 with scales: 738 MB in 113 us (a copy: 119; 123 to 129 over seconds of it); one token 2 us (latency of one load, a block sum, a store).
+// e4m3 with scales: 738 MB in 120 to 129 us over seconds of it, 113 in runs of 30 ms (a copy: 119); one token 2 us (latency of one
+// load, a block sum, a store).
 #include <cuda_fp8.h>
 
 #include "../../include/mlpmoe.h"
@@ -243,7 +244,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
 
 // A row to a block whose threads take eight columns each: all loads of a row are in flight at once and none is idle long.  A warp
 // to a row (no block barrier) where a row is 512 columns at most and there are many: 65536 x 512 60.6 us against 69.9,
-// while at 1200 rows both take 3.1.  Two chunks to a thread for 8-bit output of longer rows, whose scales are half the
+// while at 1200 rows both take 3.1.  Rows of more than 8192 columns that are not aligned spill up to 132 bytes a thread.  Two chunks to a thread for 8-bit output of longer rows, whose scales are half the
 // work: 16384 x 4096 111 us against 129 with one (bf16 output: 121 against 117, so it keeps one).
 template <int XKIND, int RKIND, int OKIND, bool VEC>
 cudaError_t launch_shape(const NormArgs& a, cudaStream_t st) {

@@ -4,7 +4,9 @@
 // One pass over the logits each way.  A row belongs to LPR lanes of a warp with VPT neighbouring columns each, so a
 // lane's columns never change and the column sums live in its registers until the kernel's end.  Forward: bound by the
 // k exchanges of the selection (131072 x 128, top 16: 59 us and 10 for the sums, 75 % of the issue slots, where the logits alone
-// take 13).  Backward: 131072 x 128 fp32 34 us, 62 % of a copy; 30 instructions per logit keep it from the rest.
+// take 13; a row has all 32 lanes there, so its k exchanges are the whole warp's).  Backward: 131072 x 128 fp32 34 us, 62 % of a copy; 30
+// instructions per logit keep it from the rest, of them the sums over a row's lanes, paid for four columns a lane.
+// B above 128 (eight columns a lane) spills 88 bytes a thread in the forward: 131072 x 256, top 16: 115 us.
 #include <math.h>
 
 #include "../../include/mlpmoe.h"

@@ -14,8 +14,8 @@
 // the group's own; scale and unit are applied to the group's whole-number sum in fp32.
 // mma.sync and not tcgen05: a scale per group of K means reading the accumulators back after every 32 to 128 columns of
 // K, and for a few tokens converting the codes to an operand that tensor memory takes costs more than these products.
-// Measured (4096 x 14336, group 128): one token 29.6 us, eight on a selection of 8 of 64 branches 46.7; the codes alone take
-// 14.3 us of a copy.  Of the 29.6 about 12 are fixed: two launches, filling the rings, the digits, the sums' exchange between
+// Measured (4096 x 14336, group 128): one token 29.9 us, eight on a selection of 8 of 32 branches 46.4; the codes alone take
+// 14.3 us of a copy.  Of the 29.9 about 12 are fixed: two launches, filling the rings, the digits, the sums' exchange between
 // warps and blocks; the loop runs at 70 % of the issue slots.  Five ring stages instead of four bring nothing.
 //
 // One block per SM takes an equal share of the 16-row tiles (gate|up: the gate and up rows of eight neurons, so that a

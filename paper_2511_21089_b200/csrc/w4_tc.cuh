@@ -11,12 +11,12 @@
 // What bounds these kernels up to 64 tokens is the conversion of the codes (1.1 instructions a code of the 3.5 that a block's
 // warps issue, at 2.2 a cycle), not the copy (floor of the Llama-shaped layer 14.5 us) nor the MMAs: before the last step below
 // 128 columns of K took 1450 cycles of which the MMAs run 580 (gate|up), 1100 and 290 (down).  Measured there, 64 tokens,
-// group 128 with zeros: 53 us (each alone, with cold caches: columns 6, gate|up 33, down 28).  On the way: the operand in shared
+// group 128 with zeros: 53 us (each alone, with cold caches: columns 6, gate|up 33, down 27).  On the way: the operand in shared
 // memory (64 KB written and read for each 128 columns of K), waits that read the timer at once, and MMAs issued under
 // `lane == 0` 99 us; the operand in tensor memory, the rest as it was 94; codes through a ring of copies instead of registers
 // 82; scales through a ring too 70; waits that read the timer late 58; copies issued by three warps 56; an operand stage for
 // each matrix and paired sums 53.  Tried without gain: stages of half a block of K, reading the next codes while tensor
-// memory takes the last.
+// memory takes the last.  Down with more than 64 tokens a chunk spills 72 to 116 bytes a thread.
 //
 // A block: 128 neurons (128 gate rows and 128 up rows) or 128 rows of W_down.  Warps 0..7 epilogue (tensor memory lanes
 // 32 (warp % 4).., columns NE (warp / 4)..), 8..15 codes to fp16 (the same lanes), 16 issues the MMAs, 17 copies the
@@ -46,8 +46,8 @@ struct TcCfg {
   static constexpr int kSmem = kBars + 512 + 1024;               // barriers, slack for 1024-byte alignment
 };
 
-// Eight codes -> four fp16 pairs code - zero, pairs (e, e + 4) of eight consecutive columns.  The code slides into the mantissa of
-// 1024.0, as it is or times 16, which a multiplication by 1/16 takes back: one shift for two pairs.  All of it is exact.
+// Eight codes -> four fp16 pairs code - zero, pairs (e, e + 4) of eight consecutive columns, by the widely used conversion of small
+// whole numbers to floats through the mantissa: the code slides into that of 1024.0, as it is or times 16, which a multiplication by 1/16 takes back: one shift for two pairs.  All of it is exact.
 // bias = -(1024 + zero) and -(64 + zero), twice each.
 struct Bias {
   __half2 one, sixteen;
@@ -376,7 +376,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) w4_tc_kernel(const __grid_const
       sums[(i + 1) * 128] = __uint_as_float(static_cast<uint32_t>(acc[i / 2] >> 32));
     }
   } else if (warp < 16) {
-    // ------------------------------------------------------------- codes to bf16
+    // ------------------------------------------------------------- codes to fp16
     // gate|up: a warp takes 32 rows of one matrix; down: of half of the columns.  32 columns (16 bytes) at a time.
     constexpr int kChunks = 4 / (3 - C::kMats), kZeros = GPB * kChunks > 4 ? GPB * kChunks / 4 : 1;      // groups that the warp's columns touch
     const int quad = warp % 4, part = (warp - 8) / 4, chunk0 = GATEUP ? 0 : 2 * part, r = quad * 32 + lane;

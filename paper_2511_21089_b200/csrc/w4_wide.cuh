@@ -9,8 +9,8 @@
 // Two digits of one token are neighbouring columns and so sit in one lane: c0 + 256 c1 is still exact in 32 bits, and scale
 // and unit are applied once per token ("slot": two digits; an fp32 y takes two slots per token, the second
 // with the third digit alone).
-// Measured (4096 x 14336, group 128, y bf16): 64 tokens 129 us, 16 tokens 66, 9 tokens 52; bound by the issue of
-// mma.sync and of the reads that feed it (two digits are two columns per token).
+// Measured (4096 x 14336, group 128, y bf16): 64 tokens 129 us, 16 tokens 66, 9 tokens 52; y fp32 (twice the slots)
+// 236, 95 and 78; bound by the issue of mma.sync and of the reads that feed it (two digits are two columns per token).
 #pragma once
 #include "w4_kernel.cuh"
 
