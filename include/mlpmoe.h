@@ -402,6 +402,168 @@ mlpmoe_status_t mlpmoe_w4_workspace(const mlpmoe_w4_layer_t* layer, int64_t n_to
 mlpmoe_status_t mlpmoe_w4_get_status(const void* workspace, void* stream);
 
 /* ------------------------------------------------------------------------- *
+ * Operators of a training step around a routed layer (not in the paper): the tokens
+ * sorted by the branches that the router selected for them and back, with the gradient; the
+ * residual norms' gradient and LayerNorm; AdamW over many tensors.  As above: no handle, every
+ * buffer is the caller's, the calls only enqueue, and a workspace is scratch of one call.  Every
+ * result is the same from call to call, bit by bit.  In the order of a step:
+ *     mlpmoe_add_rmsnorm -> (logits) -> mlpmoe_route -> mlpmoe_sort_tokens -> mlpmoe_dispatch -> (the branches' products over
+ *     their rows) -> mlpmoe_combine;   mlpmoe_combine_backward -> (the products' gradients) -> mlpmoe_combine without weights
+ *     (the gradient of mlpmoe_dispatch) -> mlpmoe_route_backward -> mlpmoe_norm_backward -> mlpmoe_adamw.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Tokens sorted by branch: branch b gets the rows offsets[b] .. offsets[b] + counts[b] - 1, one for each token that selects it, in
+ * ascending order; offsets[0] = 0 and offsets[b + 1] = offsets[b] + counts[b] rounded up to a multiple of align.
+ *   select        device uint8 [n_tokens x B], contiguous, as mlpmoe_route leaves it (any value but 0 selects).  Of a token that
+ *                 selects more than `slots` branches the first `slots` (lowest b) are taken
+ *   offsets       device int32 [B + 1];  counts  device int32 [B]
+ *   row_token     device int32 [rows]: the token of a row; -1 in the rows between a branch's end and the next start; rows from
+ *                 offsets[B] on are left as they were.  rows: at least what mlpmoe_sort_rows gives, which no selection exceeds
+ *   token_row     device int32 [n_tokens x slots]: the rows of a token's branches, ascending b, then -1
+ *   token_branch  device int32 [n_tokens x slots], or NULL: those branches, then -1
+ *   workspace     device, 16-byte aligned, of the size that mlpmoe_sort_workspace gives
+ * 1 <= B <= 256, 1 <= align <= 1024, slots >= 1, at most 2^31 - 1 rows (more: MLPMOE_ERR_UNSUPPORTED).
+ */
+mlpmoe_status_t mlpmoe_sort_tokens(const uint8_t* select, int64_t n_tokens, int32_t B, int32_t slots, int32_t align, int32_t* offsets,
+                                   int32_t* counts, int32_t* row_token, int64_t rows, int32_t* token_row, int32_t* token_branch,
+                                   void* workspace, int64_t workspace_bytes, void* stream);
+mlpmoe_status_t mlpmoe_sort_rows(int64_t n_tokens, int32_t B, int32_t slots, int32_t align, int64_t* rows);
+mlpmoe_status_t mlpmoe_sort_workspace(int64_t n_tokens, int32_t B, int64_t* bytes);
+
+/*
+ * Rows of the tokens to their branches: rows[token_row[t, j]] = x[t] for every place j of token t, bit by bit; the rows between a
+ * branch's end and the next start are cleared.  Rows from offsets[B] on are left as they were.
+ *   x, rows       device, fp32, bf16 or e4m3, rows x_stride / rows_stride elements apart (0 = d_model); must not overlap
+ *   x_scale, row_scale  device fp32 [n_tokens x ceil(d_model / group)] and [n_rows x ...]: the scales of e4m3 (group 0: one per
+ *                 token; 32, 64 or 128), copied along (0 in cleared rows); other types: ignored
+ *   n_rows        rows that the buffer has; a place in token_row outside of 0 .. n_rows - 1 is skipped
+ *   B, slots, align, offsets, counts, token_row   as mlpmoe_sort_tokens had and left them (offsets and counts: not read if align is 1)
+ * Gradient with respect to x: mlpmoe_combine with weight NULL over the rows' gradient.
+ */
+mlpmoe_status_t mlpmoe_dispatch(const void* x, mlpmoe_dtype_t dtype, int64_t x_stride, const float* x_scale, int64_t group,
+                                int64_t n_tokens, int64_t d_model, int32_t B, int32_t slots, int32_t align, const int32_t* offsets,
+                                const int32_t* counts, const int32_t* token_row, void* rows, int64_t rows_stride, float* row_scale,
+                                int64_t n_rows, void* stream);
+
+/*
+ * Rows summed back to their tokens, in fp32, ascending j, the residual last:
+ *     y[t] = residual[t] + sum_j weight[t, j] * rows[token_row[t, j]]        (places of -1 or outside of 0 .. n_rows - 1: nothing)
+ *   rows      device, fp32 or bf16, rows_stride elements apart (0 = d_model)
+ *   weight    device fp32 [n_tokens x slots], or NULL: 1; where there is no row it is not used
+ *   residual  device, fp32 or bf16 [n_tokens x d_model], or NULL; may be y itself (same type and stride)
+ *   y         device, fp32 or bf16; must not overlap rows
+ */
+mlpmoe_status_t mlpmoe_combine(const void* rows, mlpmoe_dtype_t rows_dtype, int64_t rows_stride, int64_t n_rows, const int32_t* token_row,
+                               const float* weight, int32_t slots, const void* residual, mlpmoe_dtype_t residual_dtype,
+                               int64_t residual_stride, void* y, mlpmoe_dtype_t y_dtype, int64_t y_stride, int64_t n_tokens,
+                               int64_t d_model, void* stream);
+
+/*
+ * Gradient of mlpmoe_combine (that of the residual is grad_y itself):
+ *     grad_rows[token_row[t, j]] = weight[t, j] * grad_y[t];     grad_weight[t, j] = sum_c grad_y[t, c] * rows[token_row[t, j], c]
+ * and 0 for the weight of a place without a row and for the rows between a branch's end and the next start.
+ *   grad_rows    device, of rows_dtype, grad_rows_stride elements apart (0 = d_model), or NULL; may be rows itself (same stride).
+ *                Rows from offsets[B] on are left as they were
+ *   grad_weight  device fp32 [n_tokens x slots], or NULL (rows is not read then)
+ *   B, slots, align, offsets, counts, token_row, n_rows, weight   as above (offsets and counts: only for grad_rows with align above 1)
+ * d_model up to 32768 (more: MLPMOE_ERR_UNSUPPORTED).
+ */
+mlpmoe_status_t mlpmoe_combine_backward(const void* grad_y, mlpmoe_dtype_t grad_y_dtype, int64_t grad_y_stride, const void* rows,
+                                        mlpmoe_dtype_t rows_dtype, int64_t rows_stride, int64_t n_rows, const int32_t* token_row,
+                                        const float* weight, int32_t slots, int32_t B, int32_t align, const int32_t* offsets,
+                                        const int32_t* counts, void* grad_rows, int64_t grad_rows_stride, float* grad_weight,
+                                        int64_t n_tokens, int64_t d_model, void* stream);
+
+/*
+ * Residual addition and LayerNorm in one pass: mlpmoe_add_rmsnorm with
+ *     v = (s - mean(s)) / sqrt(mean((s - mean(s))^2) + eps) * gain + bias
+ *   bias   device fp32 [d_model], or NULL: 0
+ * and everything else as there.
+ */
+mlpmoe_status_t mlpmoe_add_layernorm(const void* x, mlpmoe_dtype_t x_dtype, int64_t x_stride, const void* r, mlpmoe_dtype_t r_dtype,
+                                     int64_t r_stride, const float* gain, const float* bias, void* x_out, int64_t x_out_stride, void* out,
+                                     mlpmoe_dtype_t out_dtype, int64_t out_stride, float* scales, int64_t group, int64_t n_tokens,
+                                     int64_t d_model, float eps, void* stream);
+
+typedef enum { MLPMOE_RMSNORM = 0, MLPMOE_LAYERNORM = 1 } mlpmoe_norm_t;
+
+/*
+ * Gradient of the two residual norms, with z = s - mean(s) (LayerNorm) or s (RMSNorm), q = 1 / sqrt(mean(z^2) + eps), h = gain * grad_out:
+ *     grad_x    = grad_s + q * (h - mean(h) - z * q^2 * mean(h * z))      (mean(h): LayerNorm only)
+ *     grad_gain = sum_t grad_out * z * q,     grad_bias = sum_t grad_out
+ * grad_x is the gradient of x and of r alike (s = x + r); mean and q are computed again from s.  Sums are fp32 in a fixed order.
+ *   s         device, fp32 or bf16: what the forward call left in x_out
+ *   grad_out  device, fp32 or bf16: the gradient of out
+ *   grad_s    device, fp32 or bf16, or NULL: the gradient that reaches s on its other way, the residual stream
+ *   grad_x    device, fp32 or bf16; may be grad_s itself (same type and stride), must not overlap s or grad_out
+ *   grad_gain, grad_bias  device fp32 [d_model], or NULL (grad_bias: LayerNorm only); n_tokens = 0 clears them
+ *   workspace device, 16-byte aligned, of the size that mlpmoe_norm_backward_workspace gives; not used if both are NULL
+ * Strides in elements, 0 = d_model; any d_model up to 32768 (more: MLPMOE_ERR_UNSUPPORTED), any element alignment.
+ */
+mlpmoe_status_t mlpmoe_norm_backward(mlpmoe_norm_t norm, const void* s, mlpmoe_dtype_t s_dtype, int64_t s_stride, const float* gain,
+                                     const void* grad_out, mlpmoe_dtype_t grad_out_dtype, int64_t grad_out_stride, const void* grad_s,
+                                     mlpmoe_dtype_t grad_s_dtype, int64_t grad_s_stride, void* grad_x, mlpmoe_dtype_t grad_x_dtype,
+                                     int64_t grad_x_stride, float* grad_gain, float* grad_bias, int64_t n_tokens, int64_t d_model,
+                                     float eps, void* workspace, int64_t workspace_bytes, void* stream);
+mlpmoe_status_t mlpmoe_norm_backward_workspace(int64_t n_tokens, int64_t d_model, int64_t* bytes);
+
+/*
+ * A tensor of an AdamW step: n elements, contiguous.
+ *   param        device, of param_dtype (fp32 or bf16): updated
+ *   grad         device, of grad_dtype (fp32 or bf16)
+ *   m, v         device, of state_dtype: updated, zeros before the first step.  MLPMOE_FP32: the two moments.  MLPMOE_E4M3: codes
+ *                with a scale per 128 elements, m ~ code * m_scale and sqrt(v) ~ code * v_scale
+ *   m_scale, v_scale  device fp32 [ceil(n / 128)]: e4m3 only
+ *   param_bf16   device bf16 [n], or NULL: receives the new param rounded to nearest (param_dtype fp32 only), for mlpmoe_create
+ *   weight_decay of this tensor, >= 0
+ * Any element alignment; buffers that start on 16 bytes take wide loads.  Buffers must not overlap, within a tensor or between two.
+ */
+typedef struct {
+  void* param;
+  const void* grad;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  void* param_bf16;
+  int64_t n;
+  float weight_decay;
+  mlpmoe_dtype_t param_dtype, grad_dtype, state_dtype;
+} mlpmoe_adamw_tensor_t;
+
+/*
+ *   lr, beta1, beta2, eps    0 <= beta < 1, eps above 0 in fp32
+ *   step           number of this step, from 1; step_device: device int64 [1], read instead if not NULL (below 1 counts as 1), so
+ *                  that a captured graph can be replayed
+ *   lr_device      device fp32 [1], read instead of lr if not NULL
+ *   grad_scale     device fp32 [1], or NULL: every gradient is multiplied by it (clipping, a loss scale's reciprocal)
+ *   stochastic     not 0: codes of e4m3 moments, and params in bf16, are rounded up with the probability of the part that
+ *                  truncation would cut off, with 16 random bits each from a hash of (seed, step, place in the list, element)
+ */
+typedef struct {
+  double lr, beta1, beta2, eps;
+  int64_t step;
+  const int64_t* step_device;
+  const float* lr_device;
+  const float* grad_scale;
+  uint64_t seed;
+  int32_t stochastic;
+} mlpmoe_adamw_settings_t;
+
+/*
+ * One AdamW step over n_tensors tensors (a host array, not needed after the call), in fp32, a launch for up to 400 of one state type:
+ *     g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *     param = param - lr * weight_decay * param - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
+ * The param takes the new moments before they are rounded.  e4m3 moments: scale = max(max |finite value| / 448, 2^-126) of each 128
+ * elements; a root above zero is stored as the smallest code at least.  A gradient that is not finite makes its own element's param
+ * and moments not finite (a NaN code), other elements of its 128 keep theirs.
+ * Errors before anything is enqueued: MLPMOE_ERR_INVALID_ARG (NULL, a pointer off its element's alignment, a type or setting that is
+ * not allowed), MLPMOE_ERR_UNSUPPORTED (more than 2^40 elements in a tensor).
+ */
+mlpmoe_status_t mlpmoe_adamw(const mlpmoe_adamw_tensor_t* tensors, int32_t n_tensors, const mlpmoe_adamw_settings_t* settings, void* stream);
+
+/* ------------------------------------------------------------------------- *
  * Queries (host outputs; used by the parity harness)
  * ------------------------------------------------------------------------- */
 

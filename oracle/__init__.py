@@ -39,3 +39,15 @@ from .operators_oracle import (  # noqa: F401
     w4_unpack,
     w4_layer_forward,
 )
+from .training_oracle import (  # noqa: F401
+    sort_tokens,
+    combine,
+    combine_grad,
+    add_layernorm,
+    norm_grad,
+    mix32,
+    adamw_noise,
+    e4m3_up_or_down,
+    adamw_blocks,
+    adamw,
+)

@@ -31,6 +31,8 @@ MLPMOE_FP32 = 1
 MLPMOE_E4M3 = 2
 MLPMOE_LAYOUT_PAPER = 0
 MLPMOE_LAYOUT_LINEAR = 1
+MLPMOE_RMSNORM = 0
+MLPMOE_LAYERNORM = 1
 
 class mlpmoe_w4_matrix_t(ctypes.Structure):
     _fields_ = [("q", c_void_p), ("scale", c_void_p), ("zero", c_void_p)]
@@ -39,6 +41,17 @@ class mlpmoe_w4_matrix_t(ctypes.Structure):
 class mlpmoe_w4_layer_t(ctypes.Structure):
     _fields_ = [("d_model", c_int64), ("d_inter", c_int64), ("d_b", POINTER(c_int64)), ("alpha", POINTER(c_float)), ("B", c_int32),
                 ("group", c_int32), ("gate", mlpmoe_w4_matrix_t), ("up", mlpmoe_w4_matrix_t), ("down", mlpmoe_w4_matrix_t)]
+
+
+class mlpmoe_adamw_tensor_t(ctypes.Structure):
+    _fields_ = [("param", c_void_p), ("grad", c_void_p), ("m", c_void_p), ("v", c_void_p), ("m_scale", c_void_p), ("v_scale", c_void_p),
+                ("param_bf16", c_void_p), ("n", c_int64), ("weight_decay", c_float), ("param_dtype", c_int32), ("grad_dtype", c_int32),
+                ("state_dtype", c_int32)]
+
+
+class mlpmoe_adamw_settings_t(ctypes.Structure):
+    _fields_ = [("lr", c_double), ("beta1", c_double), ("beta2", c_double), ("eps", c_double), ("step", c_int64), ("step_device", c_void_p),
+                ("lr_device", c_void_p), ("grad_scale", c_void_p), ("seed", ctypes.c_uint64), ("stochastic", c_int32)]
 
 
 # name -> (restype, argtypes): every symbol include/mlpmoe.h declares
@@ -71,6 +84,22 @@ SIGNATURES = {
     "mlpmoe_w4_get_status": (c_int32, [c_void_p, c_void_p]),
     "mlpmoe_w4_debug_set_wait": (c_int32, [ctypes.c_uint64, ctypes.c_uint32]),
     "mlpmoe_w4_workspace": (c_int32, [POINTER(mlpmoe_w4_layer_t), c_int64, POINTER(c_int64)]),
+    "mlpmoe_sort_tokens": (c_int32, [c_void_p, c_int64, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p,
+                                     c_void_p, c_int64, c_void_p]),
+    "mlpmoe_sort_rows": (c_int32, [c_int64, c_int32, c_int32, c_int32, POINTER(c_int64)]),
+    "mlpmoe_sort_workspace": (c_int32, [c_int64, c_int32, POINTER(c_int64)]),
+    "mlpmoe_dispatch": (c_int32, [c_void_p, c_int32, c_int64, c_void_p, c_int64, c_int64, c_int64, c_int32, c_int32, c_int32, c_void_p, c_void_p,
+                                  c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
+    "mlpmoe_combine": (c_int32, [c_void_p, c_int32, c_int64, c_int64, c_void_p, c_void_p, c_int32, c_void_p, c_int32, c_int64, c_void_p, c_int32,
+                                 c_int64, c_int64, c_int64, c_void_p]),
+    "mlpmoe_combine_backward": (c_int32, [c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64, c_int64, c_void_p, c_void_p, c_int32, c_int32,
+                                          c_int32, c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int64, c_void_p]),
+    "mlpmoe_add_layernorm": (c_int32, [c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_void_p, c_int64, c_void_p,
+                                       c_int32, c_int64, c_void_p, c_int64, c_int64, c_int64, c_float, c_void_p]),
+    "mlpmoe_norm_backward": (c_int32, [c_int32, c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_int32, c_int64, c_void_p, c_int32, c_int64,
+                                       c_void_p, c_int32, c_int64, c_void_p, c_void_p, c_int64, c_int64, c_float, c_void_p, c_int64, c_void_p]),
+    "mlpmoe_norm_backward_workspace": (c_int32, [c_int64, c_int64, POINTER(c_int64)]),
+    "mlpmoe_adamw": (c_int32, [POINTER(mlpmoe_adamw_tensor_t), c_int32, POINTER(mlpmoe_adamw_settings_t), c_void_p]),
     "mlpmoe_stack_prepare": (c_int32, [POINTER(c_void_p), c_int32, c_int64, c_void_p]),
     "mlpmoe_debug_set_wait": (c_int32, [c_void_p, ctypes.c_uint64, ctypes.c_uint32]),
     "mlpmoe_debug_set_decode_kernel": (c_int32, [c_void_p, c_int32]),
@@ -290,6 +319,105 @@ def mlpmoe_w4_forward(layer: mlpmoe_w4_layer_t, x, y, n_tokens: int, workspace, 
     _check(lib.mlpmoe_w4_forward(layer, _ptr(x), x_dtype, x_stride, _ptr(x_scale), x_group, _ptr(select), 1 if compensate else 0,
                                  _ptr(residual), _ptr(y), y_dtype, n_tokens, _ptr(workspace), workspace_bytes, _stream(stream)),
            "mlpmoe_w4_forward")
+
+
+def mlpmoe_sort_rows(n_tokens: int, B: int, slots: int, align: int = 1) -> int:
+    """Rows that mlpmoe_sort_tokens can need at most."""
+    v = c_int64()
+    _check(lib.mlpmoe_sort_rows(n_tokens, B, slots, align, ctypes.byref(v)), "mlpmoe_sort_rows")
+    return v.value
+
+
+def mlpmoe_sort_workspace(n_tokens: int, B: int) -> int:
+    """Bytes of workspace that mlpmoe_sort_tokens needs."""
+    v = c_int64()
+    _check(lib.mlpmoe_sort_workspace(n_tokens, B, ctypes.byref(v)), "mlpmoe_sort_workspace")
+    return v.value
+
+
+def mlpmoe_sort_tokens(select, n_tokens: int, B: int, slots: int, offsets, counts, row_token, rows: int, token_row, workspace,
+                       workspace_bytes: int, align: int = 1, token_branch=None, stream=None) -> None:
+    """select: uint8 [n_tokens x B]; the others int32: offsets [B + 1], counts [B], row_token [rows], token_row and token_branch
+    [n_tokens x slots], all on the device."""
+    _check(lib.mlpmoe_sort_tokens(_ptr(select), n_tokens, B, slots, align, _ptr(offsets), _ptr(counts), _ptr(row_token), rows, _ptr(token_row),
+                                  _ptr(token_branch), _ptr(workspace), workspace_bytes, _stream(stream)), "mlpmoe_sort_tokens")
+
+
+def mlpmoe_dispatch(x, rows, n_tokens: int, d_model: int, B: int, slots: int, offsets, counts, token_row, n_rows: int, align: int = 1,
+                    dtype: int = MLPMOE_BF16, x_scale=None, row_scale=None, group: int = 0, x_stride: int = 0, rows_stride: int = 0,
+                    stream=None) -> None:
+    """rows[token_row[t, j]] = x[t]; offsets, counts and token_row from mlpmoe_sort_tokens with the same B, slots and align."""
+    _check(lib.mlpmoe_dispatch(_ptr(x), dtype, x_stride, _ptr(x_scale), group, n_tokens, d_model, B, slots, align, _ptr(offsets), _ptr(counts),
+                               _ptr(token_row), _ptr(rows), rows_stride, _ptr(row_scale), n_rows, _stream(stream)), "mlpmoe_dispatch")
+
+
+def mlpmoe_combine(rows, n_rows: int, token_row, slots: int, y, n_tokens: int, d_model: int, weight=None, residual=None,
+                   rows_dtype: int = MLPMOE_BF16, residual_dtype: int = MLPMOE_FP32, y_dtype: int = MLPMOE_FP32, rows_stride: int = 0,
+                   residual_stride: int = 0, y_stride: int = 0, stream=None) -> None:
+    """y[t] = residual[t] + sum_j weight[t, j] * rows[token_row[t, j]]; weight: fp32 [n_tokens x slots] or None for 1."""
+    _check(lib.mlpmoe_combine(_ptr(rows), rows_dtype, rows_stride, n_rows, _ptr(token_row), _ptr(weight), slots, _ptr(residual), residual_dtype,
+                              residual_stride, _ptr(y), y_dtype, y_stride, n_tokens, d_model, _stream(stream)), "mlpmoe_combine")
+
+
+def mlpmoe_combine_backward(grad_y, rows, n_rows: int, token_row, slots: int, grad_rows, grad_weight, n_tokens: int, d_model: int, weight=None,
+                            B: int = 1, align: int = 1, offsets=None, counts=None, grad_y_dtype: int = MLPMOE_FP32,
+                            rows_dtype: int = MLPMOE_BF16, grad_y_stride: int = 0, rows_stride: int = 0, grad_rows_stride: int = 0,
+                            stream=None) -> None:
+    """grad_rows (of rows_dtype) and grad_weight (fp32 [n_tokens x slots]) of mlpmoe_combine; either may be None.  With align above 1 it
+    takes the B, align, offsets and counts of mlpmoe_sort_tokens, to clear the rows between the branches."""
+    _check(lib.mlpmoe_combine_backward(_ptr(grad_y), grad_y_dtype, grad_y_stride, _ptr(rows), rows_dtype, rows_stride, n_rows, _ptr(token_row),
+                                       _ptr(weight), slots, B, align, _ptr(offsets), _ptr(counts), _ptr(grad_rows), grad_rows_stride,
+                                       _ptr(grad_weight), n_tokens, d_model, _stream(stream)), "mlpmoe_combine_backward")
+
+
+def mlpmoe_add_layernorm(x, r, x_out, out, n_tokens: int, d_model: int, gain=None, bias=None, scales=None, group: int = 0, eps: float = 1e-5,
+                         x_dtype: int = MLPMOE_FP32, r_dtype: int = MLPMOE_FP32, out_dtype: int = MLPMOE_BF16, x_stride: int = 0,
+                         r_stride: int = 0, x_out_stride: int = 0, out_stride: int = 0, stream=None) -> None:
+    """x_out = x + r and out = its LayerNorm; strides in elements (0 = d_model); r, x_out, gain and bias may be None."""
+    _check(lib.mlpmoe_add_layernorm(_ptr(x), x_dtype, x_stride, _ptr(r), r_dtype, r_stride, _ptr(gain), _ptr(bias), _ptr(x_out), x_out_stride,
+                                    _ptr(out), out_dtype, out_stride, _ptr(scales), group, n_tokens, d_model, eps, _stream(stream)),
+           "mlpmoe_add_layernorm")
+
+
+def mlpmoe_norm_backward_workspace(n_tokens: int, d_model: int) -> int:
+    """Bytes of workspace that mlpmoe_norm_backward needs for grad_gain or grad_bias."""
+    v = c_int64()
+    _check(lib.mlpmoe_norm_backward_workspace(n_tokens, d_model, ctypes.byref(v)), "mlpmoe_norm_backward_workspace")
+    return v.value
+
+
+def mlpmoe_norm_backward(norm: int, s, grad_out, grad_x, n_tokens: int, d_model: int, workspace=None, workspace_bytes: int = 0, gain=None,
+                         grad_s=None, grad_gain=None, grad_bias=None, eps: float = 1e-6, s_dtype: int = MLPMOE_FP32,
+                         grad_out_dtype: int = MLPMOE_BF16, grad_s_dtype: int = MLPMOE_FP32, grad_x_dtype: int = MLPMOE_FP32,
+                         s_stride: int = 0, grad_out_stride: int = 0, grad_s_stride: int = 0, grad_x_stride: int = 0, stream=None) -> None:
+    """norm: MLPMOE_RMSNORM or MLPMOE_LAYERNORM, with the eps of the forward call; s: its x_out."""
+    _check(lib.mlpmoe_norm_backward(norm, _ptr(s), s_dtype, s_stride, _ptr(gain), _ptr(grad_out), grad_out_dtype, grad_out_stride, _ptr(grad_s),
+                                    grad_s_dtype, grad_s_stride, _ptr(grad_x), grad_x_dtype, grad_x_stride, _ptr(grad_gain), _ptr(grad_bias),
+                                    n_tokens, d_model, eps, _ptr(workspace), workspace_bytes, _stream(stream)), "mlpmoe_norm_backward")
+
+
+def mlpmoe_adamw_tensors(tensors: Sequence[dict]):
+    """The description of the tensors of mlpmoe_adamw, from dicts with the fields of mlpmoe_adamw_tensor_t: n, param, grad, m, v, and
+    where they are used m_scale, v_scale, param_bf16, weight_decay, and the types (fp32 by default).  It keeps the tensors as long as it lives."""
+    arr = (mlpmoe_adamw_tensor_t * len(tensors))()
+    for record, t in zip(arr, tensors):
+        for name in ("param", "grad", "m", "v", "m_scale", "v_scale", "param_bf16"):
+            setattr(record, name, _ptr(t.get(name)))
+        record.n = t["n"]
+        record.weight_decay = t.get("weight_decay", 0.0)
+        for name in ("param_dtype", "grad_dtype", "state_dtype"):
+            setattr(record, name, t.get(name, MLPMOE_FP32))
+    arr._tensors = [dict(t) for t in tensors]
+    return arr
+
+
+def mlpmoe_adamw(tensors, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, step=1, grad_scale=None, lr_device=None,
+                 stochastic: bool = False, seed: int = 0, stream=None) -> None:
+    """tensors: from mlpmoe_adamw_tensors; step: the number of this step, from 1, or a device int64 [1] that holds it."""
+    host = isinstance(step, int)
+    settings = mlpmoe_adamw_settings_t(lr, beta1, beta2, eps, step if host else 0, None if host else _ptr(step), _ptr(lr_device),
+                                       _ptr(grad_scale), seed, 1 if stochastic else 0)
+    _check(lib.mlpmoe_adamw(tensors, len(tensors), settings, _stream(stream)), "mlpmoe_adamw")
 
 
 def mlpmoe_stack_forward(layers: Sequence[int], x, n_tokens: int, eps: float = 1e-6, stream=None) -> None:

@@ -18,7 +18,7 @@ CSRC = os.path.join(PKG, "csrc")
 OUT = os.path.join(PKG, "libmlpmoe_b200.so")
 OBJDIR = os.path.join(ROOT, "_build")
 SOURCES = ["api.cu", "pack.cu", "route.cu", "simt_gemm.cu", "tc_gemm.cu", "tc_layer.cu", "tc_stack.cu", "decode.cu", "decode_stack.cu", "decode_fused.cu", "static_scratch.cu",
-           "add_norm.cu", "router.cu", "w4.cu", "w4_quant.cu", "w4_g32.cu", "w4_g64.cu", "w4_g128.cu",
+           "add_norm.cu", "add_layernorm.cu", "norm_backward.cu", "dispatch.cu", "adamw.cu", "router.cu", "w4.cu", "w4_quant.cu", "w4_g32.cu", "w4_g64.cu", "w4_g128.cu",
            "w4_tc_g32.cu", "w4_tc_g64.cu", "w4_tc_g128.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC"]

@@ -1,0 +1,12 @@
+// Residual addition + LayerNorm + (optionally) 8-bit output with scales in one pass (mlpmoe_add_layernorm):
+//     s = x + r,  x_out = s,  v = (s - mean(s)) / sqrt(var(s) + eps) * gain + bias,  out = v | e4m3(v / scale).
+// The kernel of mlpmoe_add_rmsnorm with one sum over the row more: HBM-bound, a row in registers between its one load and its one store.
+#include "add_norm.cuh"
+
+extern "C" mlpmoe_status_t mlpmoe_add_layernorm(const void* x, mlpmoe_dtype_t x_dtype, int64_t x_stride, const void* r,
+                                                mlpmoe_dtype_t r_dtype, int64_t r_stride, const float* gain, const float* bias, void* x_out,
+                                                int64_t x_out_stride, void* out, mlpmoe_dtype_t out_dtype, int64_t out_stride,
+                                                float* scales, int64_t group, int64_t n_tokens, int64_t d_model, float eps, void* stream) {
+  return mlpmoe::add_norm<true>(x, x_dtype, x_stride, r, r_dtype, r_stride, gain, bias, x_out, x_out_stride, out, out_dtype, out_stride, scales,
+                                group, n_tokens, d_model, eps, stream);
+}

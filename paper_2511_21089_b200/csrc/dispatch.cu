@@ -1,0 +1,785 @@
+// Tokens sorted by branch and back (mlpmoe_sort_tokens, mlpmoe_dispatch, mlpmoe_combine, mlpmoe_combine_backward):
+//     rows of branch b = the tokens that select b, ascending;   x_rows[r] = x[token of r];
+//     y[t] = residual[t] + sum_j w[t, j] y_rows[row_j of t];    d y_rows[row_j] = w[t, j] dy[t],  d w[t, j] = <dy[t], y_rows[row_j]>.
+// Moving and summing rows is bound by memory: each kernel works from the token's side, so that what is shared by a token's rows (x, dy,
+// y) crosses memory once and the rows themselves once.  Nothing waits for another block and nothing floating is added atomically.
+#include "../../include/mlpmoe.h"
+#include "internal.h"
+#include "ptx.cuh"
+#include "row_io.cuh"
+
+namespace mlpmoe {
+namespace {
+
+constexpr int kMaxB = 256;
+constexpr int kNone = 2;             // no residual, beside MLPMOE_BF16 (0) and MLPMOE_FP32 (1)
+constexpr int kMaxAlign = 1024;
+
+// ------------------------------------------------------------------------------------------------ the sorted order
+// The selection as a matrix of bits, in squares of 32 tokens x 32 branches: a lane reads its token's row, and the square
+// transposed holds, for each branch, which of the 32 tokens are in it.  First kernel: the transposed bits and their counts
+// per tile of tokens.  Second: each tile adds up the tiles before it, and every set bit's place is its branch's start plus
+// the bits before it.  A small batch is one tile and takes one launch.
+constexpr int kSortThreads = 512;
+constexpr int kSortTiles = 148;           // tiles aimed at: one block per SM; every tile reads every tile's counts
+constexpr int kSortScanTiles = 512;       // from here on those sums are made once, by a kernel of their own
+constexpr int kSortTileBits = 4096;       // words of 32 bits of one tile: 32 KB of shared memory with the places
+
+struct SortArgs {
+  const uint8_t* select;
+  uint32_t* mask;          // [groups of 32 tokens][B32]: bit i: token i of the group is in the branch
+  int32_t* tile_counts;    // [tiles][B32]; after the scan: of the tiles before
+  int32_t* totals;         // [B32], the scan's
+  int32_t* offsets;
+  int32_t* counts;
+  int32_t* row_token;
+  int32_t* token_row;
+  int32_t* token_branch;
+  int64_t n, rows;
+  int B, B32, slots, align, tile_groups, tiles, groups, wide, scanned;
+};
+
+// Row lane, bit j -> row j, bit lane.
+__device__ __forceinline__ uint32_t transpose32(uint32_t v, int lane) {
+  uint32_t m = 0x0000FFFFu;
+#pragma unroll
+  for (int s = 16; s > 0; s >>= 1) {
+    const uint32_t u = __shfl_xor_sync(0xFFFFFFFFu, v, s);
+    v = (lane & s) ? (v & ~m) | ((u >> s) & m) : (v & m) | ((u & m) << s);
+    m ^= m << (s >> 1);
+  }
+  return v;
+}
+
+// One bit for each byte of x that is not zero.
+__device__ __forceinline__ uint32_t nonzero4(uint32_t x) {
+  const uint32_t t = (((x & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | x) & 0x80808080u;
+  return ((t >> 7) * 0x01020408u) >> 24 & 15u;
+}
+
+// Branches b0 .. b0 + 31 of the row at p.
+__device__ __forceinline__ uint32_t row_bits(const uint8_t* p, int b0, int B, int wide) {
+  uint32_t m = 0;
+  if (wide == 16) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      if (b0 + 16 * h >= B) break;
+      const uint4 v = *reinterpret_cast<const uint4*>(p + b0 + 16 * h);
+      m |= (nonzero4(v.x) | nonzero4(v.y) << 4 | nonzero4(v.z) << 8 | nonzero4(v.w) << 12) << (16 * h);
+    }
+  } else if (wide == 4) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (b0 + 4 * i < B) m |= nonzero4(*reinterpret_cast<const uint32_t*>(p + b0 + 4 * i)) << (4 * i);
+  } else {
+#pragma unroll 8
+    for (int i = 0; i < 32; ++i)
+      if (b0 + i < B && p[b0 + i] != 0) m |= 1u << i;
+  }
+  return m;
+}
+
+// The transposed bits of a group of 32 tokens, branch by branch, to out[B32]; a token's branches past its first `slots` are dropped.
+template <typename F>
+__device__ __forceinline__ void group_bits(const SortArgs& a, int64_t group, int lane, F&& out) {
+  const int64_t t = group * 32 + lane;
+  const uint8_t* p = a.select + t * a.B;
+  int room = a.slots;
+  for (int b0 = 0; b0 < a.B32; b0 += 32) {
+    uint32_t m = t < a.n ? row_bits(p, b0, a.B, a.wide) : 0u;
+    while (__popc(m) > room) m &= ~(0x80000000u >> __clz(m));
+    room -= __popc(m);
+    out(b0 + lane, transpose32(m, lane));
+  }
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const __grid_constant__ SortArgs a) {
+  __shared__ int32_t cnt[kMaxB];
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  for (int b = threadIdx.x; b < a.B32; b += kSortThreads) cnt[b] = 0;
+  __syncthreads();
+  const int lane = threadIdx.x % 32;
+  for (int i = threadIdx.x / 32; i < a.tile_groups; i += kSortThreads / 32) {
+    const int64_t g = static_cast<int64_t>(blockIdx.x) * a.tile_groups + i;
+    if (g >= a.groups) break;
+    group_bits(a, g, lane, [&](int b, uint32_t m) {
+      a.mask[g * a.B32 + b] = m;
+      atomicAdd(&cnt[b], __popc(m));
+    });
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.B32; b += kSortThreads) a.tile_counts[static_cast<int64_t>(blockIdx.x) * a.B32 + b] = cnt[b];
+}
+
+// Sums of the tiles before each tile, for very many tiles: a block to 32 branches, a warp to a stretch of the tiles.
+__global__ void __launch_bounds__(1024) sort_scan_kernel(const __grid_constant__ SortArgs a) {
+  __shared__ int32_t part[32][33];
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int lane = threadIdx.x % 32, w = threadIdx.x / 32, b = blockIdx.x * 32 + lane;
+  const int per = (a.tiles + 31) / 32, lo = w * per, hi = min(a.tiles, lo + per);
+  int32_t sum = 0;
+  for (int i = lo; i < hi; ++i) sum += a.tile_counts[static_cast<int64_t>(i) * a.B32 + b];
+  part[w][lane] = sum;
+  __syncthreads();
+  int32_t run = 0;
+  for (int i = 0; i < w; ++i) run += part[i][lane];
+  for (int i = lo; i < hi; ++i) {
+    int32_t* p = a.tile_counts + static_cast<int64_t>(i) * a.B32 + b;
+    const int32_t c = *p;
+    *p = run;
+    run += c;
+  }
+  if (w == 31) a.totals[b] = run;
+}
+
+template <bool ONE>      // one tile: the bits and their counts are made here
+__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_constant__ SortArgs a) {
+  __shared__ uint32_t mask[kSortTileBits];
+  __shared__ int32_t place[kSortTileBits];     // where the group's first token of the branch goes; before that scratch of the sums
+  __shared__ int32_t first[kMaxB], total[kMaxB], before[kMaxB], warp_sum[kMaxB / 32];
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, tile = blockIdx.x;
+  const int64_t g0 = static_cast<int64_t>(tile) * a.tile_groups;
+  const int n_groups = static_cast<int>(min(static_cast<int64_t>(a.tile_groups), a.groups - g0));
+  if (ONE) {
+    for (int i = warp; i < n_groups; i += kSortThreads / 32) group_bits(a, i, lane, [&](int b, uint32_t m) { mask[i * a.B32 + b] = m; });
+    __syncthreads();
+    if (tid < a.B32) {
+      int32_t sum = 0;
+      for (int i = 0; i < n_groups; ++i) sum += __popc(mask[i * a.B32 + tid]);
+      before[tid] = 0;
+      total[tid] = sum;
+    }
+  } else {
+    for (int i = tid; i < n_groups * a.B32; i += kSortThreads) mask[i] = a.mask[g0 * a.B32 + i];
+    if (a.scanned) {
+      if (tid < a.B32) {
+        before[tid] = a.tile_counts[static_cast<int64_t>(tile) * a.B32 + tid];
+        total[tid] = a.totals[tid];
+      }
+    } else {
+      const int parts = kSortThreads / a.B32, b = tid % a.B32, part = tid / a.B32;
+      if (part < parts) {
+        int32_t sum = 0, sum_before = 0;
+#pragma unroll 8
+        for (int i = part; i < a.tiles; i += parts) {
+          const int32_t c = a.tile_counts[static_cast<int64_t>(i) * a.B32 + b];
+          sum += c;
+          sum_before += i < tile ? c : 0;
+        }
+        place[part * a.B32 + b] = sum;
+        place[(parts + part) * a.B32 + b] = sum_before;
+      }
+      __syncthreads();
+      if (tid < a.B32) {
+        int32_t sum = 0, sum_before = 0;
+        for (int i = 0; i < parts; ++i) {
+          sum += place[i * a.B32 + tid];
+          sum_before += place[(parts + i) * a.B32 + tid];
+        }
+        before[tid] = sum_before;
+        total[tid] = sum;
+      }
+    }
+  }
+  __syncthreads();
+  // branch starts: a scan of the counts rounded up to the alignment
+  const int32_t padded = tid < a.B32 ? (total[tid] + a.align - 1) / a.align * a.align : 0;
+  int32_t incl = padded;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int32_t u = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 31 && warp < kMaxB / 32) warp_sum[warp] = incl;
+  __syncthreads();
+  if (tid < a.B32) {
+    int32_t start = incl - padded;
+    for (int i = 0; i < warp; ++i) start += warp_sum[i];
+    first[tid] = start;
+    if (tile == 0 && tid < a.B) {
+      a.offsets[tid] = start;
+      a.counts[tid] = total[tid];
+      if (tid == a.B - 1) a.offsets[a.B] = start + padded;
+    }
+  }
+  __syncthreads();
+  // the rows between a branch's end and the next start belong to no token
+  for (int b = tile; b < a.B; b += gridDim.x) {
+    const int32_t end = first[b] + total[b], next = first[b] + (total[b] + a.align - 1) / a.align * a.align;
+    for (int32_t r = end + tid; r < next; r += kSortThreads)
+      if (r < a.rows) a.row_token[r] = -1;
+  }
+  if (tid < a.B32) {
+    int32_t run = first[tid] + before[tid];
+    for (int i = 0; i < n_groups; ++i) {
+      place[i * a.B32 + tid] = run;
+      run += __popc(mask[i * a.B32 + tid]);
+    }
+  }
+  __syncthreads();
+  const uint32_t lower = (1u << lane) - 1u;
+  for (int i = warp; i < n_groups; i += kSortThreads / 32) {
+    const int64_t t = (g0 + i) * 32 + lane;
+    int32_t* rows = a.token_row + t * a.slots;
+    int32_t* branches = a.token_branch + t * a.slots;
+    int slot = 0;
+    for (int b0 = 0; b0 < a.B32; b0 += 32) {
+      uint32_t m = transpose32(mask[i * a.B32 + b0 + lane], lane);
+      while (m != 0) {
+        const int b = b0 + __ffs(m) - 1;
+        m &= m - 1;
+        const int32_t r = place[i * a.B32 + b] + __popc(mask[i * a.B32 + b] & lower);
+        if (r < a.rows) a.row_token[r] = static_cast<int32_t>(t);
+        rows[slot] = r;
+        if (a.token_branch != nullptr) branches[slot] = b;
+        ++slot;
+      }
+    }
+    if (t < a.n)
+      for (; slot < a.slots; ++slot) {
+        rows[slot] = -1;
+        if (a.token_branch != nullptr) branches[slot] = -1;
+      }
+  }
+}
+
+// Tiles of a batch: as many as there are SMs where a tile then has four groups of 32 tokens at least, more where a tile gets too large.
+void sort_plan(int64_t n, int32_t B, SortArgs* a) {
+  a->n = n;
+  a->B = B;
+  a->B32 = (B + 31) / 32 * 32;
+  a->groups = static_cast<int>((n + 31) / 32);
+  const int most = kSortTileBits / a->B32 < 32 ? kSortTileBits / a->B32 : 32;
+  int g = (a->groups + kSortTiles - 1) / kSortTiles;
+  if (g < 4) g = 4;
+  if (g > most || a->groups <= most) g = most;
+  a->tile_groups = g;
+  a->tiles = a->groups <= g ? 1 : (a->groups + g - 1) / g;
+  a->scanned = a->tiles > kSortScanTiles;
+}
+
+int64_t round16(int64_t v) { return (v + 15) / 16 * 16; }
+int64_t sort_mask_bytes(const SortArgs& a) { return a.tiles == 1 ? 0 : round16(static_cast<int64_t>(a.groups) * a.B32 * 4); }
+int64_t sort_bytes(const SortArgs& a) { return sort_mask_bytes(a) + (a.tiles == 1 ? 16 : round16((static_cast<int64_t>(a.tiles) + 1) * a.B32 * 4)); }
+
+// ------------------------------------------------------------------------------------------------ rows to their branches
+constexpr int kMoveThreads = 256;
+constexpr int kMoveVecs = 4;          // 16 bytes each, per lane: a warp moves 2 KB of a row
+
+struct DispatchArgs {
+  const uint8_t* x;
+  const float* x_scale;
+  const int32_t* offsets;
+  const int32_t* counts;
+  const int32_t* token_row;
+  uint8_t* rows;
+  float* row_scale;
+  int64_t n, x_stride, rows_stride, d;    // strides and width in bytes
+  int64_t n_rows, token_blocks;
+  int B, slots, scales, parts;            // parts: warps of a row; scales: scales of a row
+};
+
+// A row's bytes, copied or cleared: 16 at a time where all rows start on 16 bytes, then the rest one at a time.
+template <int ES>
+struct Elem {
+  using type = uint8_t;
+};
+template <>
+struct Elem<2> {
+  using type = uint16_t;
+};
+template <>
+struct Elem<4> {
+  using type = uint32_t;
+};
+
+// One warp to a token's part of a row: the part is read once and written to each of the token's rows.  Behind the tokens, one
+// warp to each row that aligning can have left between two branches: cleared, so that products over a branch's whole tiles see zeros.
+template <int ES, bool VEC>
+__global__ void __launch_bounds__(kMoveThreads) dispatch_kernel(const __grid_constant__ DispatchArgs a) {
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int lane = threadIdx.x % 32;
+  using E = typename Elem<ES>::type;
+  if (blockIdx.x >= a.token_blocks) {
+    const int64_t u = (blockIdx.x - a.token_blocks) * (kMoveThreads / 32) + threadIdx.x / 32;
+    const int64_t b = u % a.B, i = u / a.B;
+    const int64_t r = static_cast<int64_t>(a.offsets[b]) + a.counts[b] + i;
+    if (r >= a.offsets[b + 1] || r >= a.n_rows || r < 0) return;
+    uint8_t* p = a.rows + r * a.rows_stride;
+    const int64_t whole = VEC ? a.d / 16 * 16 : 0;
+    for (int64_t c = lane * 16; c < whole; c += 512) *reinterpret_cast<uint4*>(p + c) = make_uint4(0u, 0u, 0u, 0u);
+    for (int64_t c = whole + lane * ES; c < a.d; c += 32 * ES) *reinterpret_cast<E*>(p + c) = 0;
+    for (int s = lane; s < a.scales; s += 32) a.row_scale[r * a.scales + s] = 0.0f;
+    return;
+  }
+  const int64_t u = static_cast<int64_t>(blockIdx.x) * (kMoveThreads / 32) + threadIdx.x / 32;
+  const int64_t t = u / a.parts;
+  const int part = static_cast<int>(u - t * a.parts);
+  if (t >= a.n) return;
+  const int64_t c0 = static_cast<int64_t>(part) * (512 * kMoveVecs);
+  const uint8_t* x = a.x + t * a.x_stride;
+  const int64_t whole = VEC ? a.d / 16 * 16 : 0;
+  uint4 v[kMoveVecs];
+  if (VEC) {
+#pragma unroll
+    for (int i = 0; i < kMoveVecs; ++i) {
+      const int64_t c = c0 + (i * 32 + lane) * 16;
+      if (c < whole) v[i] = *reinterpret_cast<const uint4*>(x + c);
+    }
+  }
+  const int64_t rest_lo = whole > c0 ? whole : c0;      // elements that no 16 bytes hold
+  const int64_t rest_hi = a.d < c0 + 512 * kMoveVecs ? a.d : c0 + 512 * kMoveVecs;
+  for (int j0 = 0; j0 < a.slots; j0 += 32) {
+    const int32_t mine = j0 + lane < a.slots ? a.token_row[t * a.slots + j0 + lane] : -1;
+    uint32_t live = __ballot_sync(0xFFFFFFFFu, static_cast<uint32_t>(mine) < static_cast<uint64_t>(a.n_rows));
+    while (live != 0) {
+      const int64_t r = __shfl_sync(0xFFFFFFFFu, mine, __ffs(live) - 1);
+      live &= live - 1;
+      uint8_t* p = a.rows + r * a.rows_stride;
+      if (VEC) {
+#pragma unroll
+        for (int i = 0; i < kMoveVecs; ++i) {
+          const int64_t c = c0 + (i * 32 + lane) * 16;
+          if (c < whole) *reinterpret_cast<uint4*>(p + c) = v[i];
+        }
+      }
+      for (int64_t c = rest_lo + lane * ES; c < rest_hi; c += 32 * ES) *reinterpret_cast<E*>(p + c) = *reinterpret_cast<const E*>(x + c);
+      if (part == 0)
+        for (int s = lane; s < a.scales; s += 32) a.row_scale[r * a.scales + s] = a.x_scale[t * a.scales + s];
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ rows summed to their tokens
+struct CombineArgs {
+  const void* rows;
+  const int32_t* token_row;
+  const float* weight;
+  const void* residual;
+  void* y;
+  int64_t rows_stride, residual_stride, y_stride, n, n_rows;
+  int slots, d, parts;
+};
+
+constexpr int kCombineRows = 4;       // rows of a token under way at a time
+
+// One warp to NC x 256 columns of a token: the sum stays in registers, kCombineRows rows' loads are in flight at once.
+template <int RK, int SK, int YK, bool VEC, int NC>
+__global__ void __launch_bounds__(kMoveThreads) combine_kernel(const __grid_constant__ CombineArgs a) {
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int lane = threadIdx.x % 32;
+  const int64_t u = static_cast<int64_t>(blockIdx.x) * (kMoveThreads / 32) + threadIdx.x / 32;
+  const int64_t t = u / a.parts;
+  if (t >= a.n) return;
+  const int c0 = static_cast<int>(u - t * a.parts) * (256 * NC) + lane * 8;
+  float acc[NC][8];
+#pragma unroll
+  for (int i = 0; i < NC; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[i][e] = 0.0f;
+  Chunk res[NC];
+  if (SK != kNone) {
+    const char* p = static_cast<const char*>(a.residual) + t * a.residual_stride * bytes_of(SK);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) res[i] = load_chunk<VEC>(p, SK, c0 + 256 * i, a.d);
+  }
+  for (int j0 = 0; j0 < a.slots; j0 += 32) {
+    int32_t mine = j0 + lane < a.slots ? a.token_row[t * a.slots + j0 + lane] : -1;
+    if (static_cast<uint32_t>(mine) >= static_cast<uint64_t>(a.n_rows)) mine = -1;
+    const float w_mine = mine < 0 ? 0.0f : (a.weight != nullptr ? a.weight[t * a.slots + j0 + lane] : 1.0f);
+    uint32_t live = __ballot_sync(0xFFFFFFFFu, mine >= 0);
+    while (live != 0) {
+      Chunk v[kCombineRows][NC];
+      float w[kCombineRows];
+#pragma unroll
+      for (int k = 0; k < kCombineRows; ++k) {
+        const int src = live != 0 ? __ffs(live) - 1 : 0;
+        const int64_t r = __shfl_sync(0xFFFFFFFFu, mine, src);
+        w[k] = __shfl_sync(0xFFFFFFFFu, w_mine, src);
+        const char* p = static_cast<const char*>(a.rows) + r * a.rows_stride * bytes_of(RK);
+#pragma unroll
+        for (int i = 0; i < NC; ++i) v[k][i] = load_chunk<VEC>(p, RK, live != 0 ? c0 + 256 * i : a.d, a.d);
+        if (live == 0) w[k] = 0.0f;
+        live &= live - 1;
+      }
+#pragma unroll
+      for (int k = 0; k < kCombineRows; ++k)
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+          float f[8];
+          to_f32(v[k][i], RK, f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[i][e] = fmaf(w[k], f[e], acc[i][e]);
+        }
+    }
+  }
+  char* y = static_cast<char*>(a.y) + t * a.y_stride * bytes_of(YK);
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    if (SK != kNone) {
+      float f[8];
+      to_f32(res[i], SK, f);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[i][e] += f[e];
+    }
+    if (c0 + 256 * i < a.d) store8<VEC>(y, YK, c0 + 256 * i, a.d, acc[i]);
+  }
+}
+
+template <int RK, int SK, int YK, bool VEC>
+cudaError_t launch_combine(CombineArgs a, cudaStream_t st) {
+  const int nc = a.d > 256 ? 2 : 1;
+  a.parts = (a.d + 256 * nc - 1) / (256 * nc);
+  const int64_t blocks = (a.n * a.parts + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
+  if (nc == 2) return launch_pdl(combine_kernel<RK, SK, YK, VEC, 2>, dim3(static_cast<unsigned>(blocks)), dim3(kMoveThreads), 0, st, a);
+  return launch_pdl(combine_kernel<RK, SK, YK, VEC, 1>, dim3(static_cast<unsigned>(blocks)), dim3(kMoveThreads), 0, st, a);
+}
+template <int RK, int SK>
+cudaError_t launch_combine_to(const CombineArgs& a, int y_kind, bool vec, cudaStream_t st) {
+  if (y_kind == MLPMOE_FP32) return vec ? launch_combine<RK, SK, MLPMOE_FP32, true>(a, st) : launch_combine<RK, SK, MLPMOE_FP32, false>(a, st);
+  return vec ? launch_combine<RK, SK, MLPMOE_BF16, true>(a, st) : launch_combine<RK, SK, MLPMOE_BF16, false>(a, st);
+}
+template <int RK>
+cudaError_t launch_combine_from(const CombineArgs& a, int res_kind, int y_kind, bool vec, cudaStream_t st) {
+  if (res_kind == MLPMOE_FP32) return launch_combine_to<RK, MLPMOE_FP32>(a, y_kind, vec, st);
+  if (res_kind == MLPMOE_BF16) return launch_combine_to<RK, MLPMOE_BF16>(a, y_kind, vec, st);
+  return launch_combine_to<RK, kNone>(a, y_kind, vec, st);
+}
+
+// ------------------------------------------------------------------------------------------------ its gradient
+struct CombineGradArgs {
+  const void* grad_y;
+  const void* rows;
+  const int32_t* token_row;
+  const float* weight;
+  const int32_t* offsets;
+  const int32_t* counts;
+  void* grad_rows;
+  float* grad_weight;
+  int64_t grad_y_stride, rows_stride, grad_rows_stride, n, n_rows, token_blocks;
+  int slots, d, B;
+};
+
+// T threads to a token (T = 32: a warp of a block of four): grad_y stays in registers, each of the token's rows is read for its
+// product with it and receives w * grad_y.  A row is read before it is written, by the same thread, so both may be one buffer.
+template <int GK, int RK, bool VEC, int T, int NCH>
+__global__ void __launch_bounds__(T == 32 ? 128 : T) combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
+  __shared__ float red[T / 32][32];
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int lane = threadIdx.x % 32;
+  if (blockIdx.x >= a.token_blocks) {      // the rows between a branch's end and the next start: no gradient
+    constexpr int kWarps = (T == 32 ? 128 : T) / 32;
+    const int64_t u = (blockIdx.x - a.token_blocks) * kWarps + threadIdx.x / 32;
+    const int64_t b = u % a.B, i = u / a.B;
+    const int64_t r = static_cast<int64_t>(a.offsets[b]) + a.counts[b] + i;
+    if (r >= a.offsets[b + 1] || r >= a.n_rows || r < 0) return;
+    char* p = static_cast<char*>(a.grad_rows) + r * a.grad_rows_stride * bytes_of(RK);
+    const float zero[8] = {};
+    for (int c = lane * 8; c < a.d; c += 256) store8<VEC>(p, RK, c, a.d, zero);
+    return;
+  }
+  const int tid = T == 32 ? lane : threadIdx.x;
+  const int64_t t = T == 32 ? static_cast<int64_t>(blockIdx.x) * 4 + threadIdx.x / 32 : blockIdx.x;
+  if (t >= a.n) return;                    // T == 32 only: whole warps leave, no block barrier follows
+  float g[NCH][8];
+  {
+    const char* p = static_cast<const char*>(a.grad_y) + t * a.grad_y_stride * bytes_of(GK);
+    Chunk c[NCH];
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) c[i] = load_chunk<VEC>(p, GK, (i * T + tid) * 8, a.d);
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) to_f32(c[i], GK, g[i]);
+  }
+  for (int j0 = 0; j0 < a.slots; j0 += 32) {
+    int32_t mine = j0 + lane < a.slots ? a.token_row[t * a.slots + j0 + lane] : -1;
+    if (static_cast<uint32_t>(mine) >= static_cast<uint64_t>(a.n_rows)) mine = -1;
+    const float w_mine = mine < 0 ? 0.0f : (a.weight != nullptr ? a.weight[t * a.slots + j0 + lane] : 1.0f);
+    uint32_t live = __ballot_sync(0xFFFFFFFFu, mine >= 0);
+    float dot_mine = 0.0f;
+    while (live != 0) {
+      const int src = __ffs(live) - 1;
+      live &= live - 1;
+      const int64_t r = __shfl_sync(0xFFFFFFFFu, mine, src);
+      const float w = __shfl_sync(0xFFFFFFFFu, w_mine, src);
+      if (a.grad_weight != nullptr) {
+        const char* p = static_cast<const char*>(a.rows) + r * a.rows_stride * bytes_of(RK);
+        Chunk c[NCH];
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) c[i] = load_chunk<VEC>(p, RK, (i * T + tid) * 8, a.d);
+        float dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+          float f[8];
+          to_f32(c[i], RK, f);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) dot = fmaf(g[i][e], f[e], dot);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
+        if (lane == src) dot_mine = dot;
+      }
+      if (a.grad_rows != nullptr) {
+        char* p = static_cast<char*>(a.grad_rows) + r * a.grad_rows_stride * bytes_of(RK);
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+          const int col = (i * T + tid) * 8;
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] = w * g[i][e];
+          if (col < a.d) store8<VEC>(p, RK, col, a.d, f);
+        }
+      }
+    }
+    if (a.grad_weight == nullptr) continue;
+    if (T > 32) {
+      red[threadIdx.x / 32][lane] = dot_mine;
+      __syncthreads();
+      if (threadIdx.x < 32) {
+        dot_mine = red[0][lane];
+#pragma unroll
+        for (int i = 1; i < T / 32; ++i) dot_mine += red[i][lane];
+      }
+      __syncthreads();
+    }
+    if ((T == 32 || threadIdx.x < 32) && j0 + lane < a.slots) a.grad_weight[t * a.slots + j0 + lane] = dot_mine;
+  }
+}
+
+template <int GK, int RK, bool VEC, int T, int NCH>
+cudaError_t launch_grad(CombineGradArgs a, int64_t pad_rows, cudaStream_t st) {
+  constexpr int kThreads = T == 32 ? 128 : T;
+  a.token_blocks = T == 32 ? (a.n + 3) / 4 : a.n;
+  const int64_t blocks = a.token_blocks + (pad_rows + kThreads / 32 - 1) / (kThreads / 32);
+  return launch_pdl(combine_backward_kernel<GK, RK, VEC, T, NCH>, dim3(static_cast<unsigned>(blocks)), dim3(kThreads), 0, st, a);
+}
+template <int GK, int RK, bool VEC>
+cudaError_t launch_grad_shape(const CombineGradArgs& a, int64_t pad_rows, cudaStream_t st) {
+  if (a.d <= 256) return launch_grad<GK, RK, VEC, 32, 1>(a, pad_rows, st);
+  if (a.d <= 1024) return launch_grad<GK, RK, VEC, 128, 1>(a, pad_rows, st);
+  if (a.d <= 4096) return launch_grad<GK, RK, VEC, 256, 2>(a, pad_rows, st);
+  if (a.d <= 8192) return launch_grad<GK, RK, VEC, 512, 2>(a, pad_rows, st);
+  return launch_grad<GK, RK, VEC, 1024, 4>(a, pad_rows, st);
+}
+template <int GK>
+cudaError_t launch_grad_from(const CombineGradArgs& a, int rows_kind, bool vec, int64_t pad_rows, cudaStream_t st) {
+  if (rows_kind == MLPMOE_FP32)
+    return vec ? launch_grad_shape<GK, MLPMOE_FP32, true>(a, pad_rows, st) : launch_grad_shape<GK, MLPMOE_FP32, false>(a, pad_rows, st);
+  return vec ? launch_grad_shape<GK, MLPMOE_BF16, true>(a, pad_rows, st) : launch_grad_shape<GK, MLPMOE_BF16, false>(a, pad_rows, st);
+}
+
+inline bool plain_kind(mlpmoe_dtype_t t) { return t == MLPMOE_FP32 || t == MLPMOE_BF16; }
+
+// Rows that aligning can have left between branches, at most.
+inline int64_t pad_rows_of(int32_t B, int32_t align) { return static_cast<int64_t>(B) * (align - 1); }
+
+}  // namespace
+}  // namespace mlpmoe
+
+using namespace mlpmoe;
+
+extern "C" {
+
+mlpmoe_status_t mlpmoe_sort_rows(int64_t n_tokens, int32_t B, int32_t slots, int32_t align, int64_t* rows) {
+  if (n_tokens < 0 || n_tokens > INT32_MAX || B <= 0 || slots <= 0 || align <= 0 || !rows) return MLPMOE_ERR_INVALID_ARG;
+  if (B > kMaxB || align > kMaxAlign) return MLPMOE_ERR_UNSUPPORTED;
+  const int64_t pairs = n_tokens * (slots < B ? slots : B);
+  const int64_t most = pairs + (pairs < B ? pairs : B) * (align - 1);
+  if (most > INT32_MAX) return MLPMOE_ERR_UNSUPPORTED;
+  *rows = most;
+  return MLPMOE_OK;
+}
+
+mlpmoe_status_t mlpmoe_sort_workspace(int64_t n_tokens, int32_t B, int64_t* bytes) {
+  if (n_tokens < 0 || n_tokens > INT32_MAX || B <= 0 || !bytes) return MLPMOE_ERR_INVALID_ARG;
+  if (B > kMaxB) return MLPMOE_ERR_UNSUPPORTED;
+  SortArgs a = {};
+  sort_plan(n_tokens, B, &a);
+  *bytes = sort_bytes(a);
+  return MLPMOE_OK;
+}
+
+mlpmoe_status_t mlpmoe_sort_tokens(const uint8_t* select, int64_t n_tokens, int32_t B, int32_t slots, int32_t align, int32_t* offsets,
+                                   int32_t* counts, int32_t* row_token, int64_t rows, int32_t* token_row, int32_t* token_branch,
+                                   void* workspace, int64_t workspace_bytes, void* stream) {
+  int64_t most = 0;
+  const mlpmoe_status_t rc = mlpmoe_sort_rows(n_tokens, B, slots, align, &most);
+  if (rc != MLPMOE_OK) return rc;
+  if (rows < most || rows > INT32_MAX || !offsets || !counts || !on(offsets, 4) || !on(counts, 4)) return MLPMOE_ERR_INVALID_ARG;
+  if (n_tokens > 0 && (!select || !row_token || !token_row)) return MLPMOE_ERR_INVALID_ARG;
+  if (!on(row_token, 4) || !on(token_row, 4) || !on(token_branch, 4)) return MLPMOE_ERR_INVALID_ARG;
+  SortArgs a = {};
+  sort_plan(n_tokens, B, &a);
+  if (!workspace || workspace_bytes < sort_bytes(a) || !on(workspace, 16)) return MLPMOE_ERR_INVALID_ARG;
+  a.select = select;
+  a.mask = static_cast<uint32_t*>(workspace);
+  a.tile_counts = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + sort_mask_bytes(a));
+  a.totals = a.tile_counts + static_cast<int64_t>(a.tiles) * a.B32;
+  a.offsets = offsets;
+  a.counts = counts;
+  a.row_token = row_token;
+  a.token_row = token_row;
+  a.token_branch = token_branch;
+  a.rows = rows;
+  a.slots = slots;
+  a.align = align;
+  a.wide = B % 16 == 0 && on(select, 16) ? 16 : (B % 4 == 0 && on(select, 4) ? 4 : 1);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  pdl_overlap_enabled() = true;
+  cudaError_t e;
+  if (a.tiles == 1) {
+    e = launch_pdl(sort_place_kernel<true>, dim3(1), dim3(kSortThreads), 0, st, a);
+  } else {
+    e = launch_pdl(sort_count_kernel, dim3(static_cast<unsigned>(a.tiles)), dim3(kSortThreads), 0, st, a);
+    if (e == cudaSuccess && a.scanned) e = launch_pdl(sort_scan_kernel, dim3(static_cast<unsigned>(a.B32 / 32)), dim3(1024), 0, st, a);
+    if (e == cudaSuccess) e = launch_pdl(sort_place_kernel<false>, dim3(static_cast<unsigned>(a.tiles)), dim3(kSortThreads), 0, st, a);
+  }
+  return e == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
+}
+
+mlpmoe_status_t mlpmoe_dispatch(const void* x, mlpmoe_dtype_t dtype, int64_t x_stride, const float* x_scale, int64_t group,
+                                int64_t n_tokens, int64_t d_model, int32_t B, int32_t slots, int32_t align, const int32_t* offsets,
+                                const int32_t* counts, const int32_t* token_row, void* rows, int64_t rows_stride, float* row_scale,
+                                int64_t n_rows, void* stream) {
+  if (n_tokens < 0 || n_tokens > INT32_MAX || d_model <= 0 || d_model > INT32_MAX / 8 || slots <= 0 || align <= 0 || B <= 0 || n_rows < 0 ||
+      n_rows > INT32_MAX)
+    return MLPMOE_ERR_INVALID_ARG;
+  if (B > kMaxB || align > kMaxAlign) return MLPMOE_ERR_UNSUPPORTED;
+  if (dtype != MLPMOE_FP32 && dtype != MLPMOE_BF16 && dtype != MLPMOE_E4M3) return MLPMOE_ERR_INVALID_ARG;
+  if (dtype == MLPMOE_E4M3 && group != 0 && group != 32 && group != 64 && group != 128) return MLPMOE_ERR_INVALID_ARG;
+  if (x_stride == 0) x_stride = d_model;
+  if (rows_stride == 0) rows_stride = d_model;
+  if (x_stride < d_model || rows_stride < d_model) return MLPMOE_ERR_INVALID_ARG;
+  if (n_tokens == 0) return MLPMOE_OK;
+  const int es = bytes_of(dtype);
+  if (!x || !token_row || !rows || !on(x, es) || !on(rows, es) || !on(token_row, 4)) return MLPMOE_ERR_INVALID_ARG;
+  if (dtype == MLPMOE_E4M3 && (!x_scale || !row_scale || !on(x_scale, 4) || !on(row_scale, 4))) return MLPMOE_ERR_INVALID_ARG;
+  if (align > 1 && (!offsets || !counts || !on(offsets, 4) || !on(counts, 4))) return MLPMOE_ERR_INVALID_ARG;
+  DispatchArgs a = {};
+  a.x = static_cast<const uint8_t*>(x);
+  a.x_scale = x_scale;
+  a.offsets = offsets;
+  a.counts = counts;
+  a.token_row = token_row;
+  a.rows = static_cast<uint8_t*>(rows);
+  a.row_scale = row_scale;
+  a.n = n_tokens;
+  a.x_stride = x_stride * es;
+  a.rows_stride = rows_stride * es;
+  a.d = d_model * es;
+  a.n_rows = n_rows;
+  a.B = B;
+  a.slots = slots;
+  a.scales = dtype == MLPMOE_E4M3 ? static_cast<int>(group == 0 ? 1 : (d_model + group - 1) / group) : 0;
+  a.parts = static_cast<int>((a.d + 512 * kMoveVecs - 1) / (512 * kMoveVecs));
+  a.token_blocks = (n_tokens * a.parts + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
+  const int64_t blocks = a.token_blocks + (pad_rows_of(B, align) + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
+  if (blocks > INT32_MAX) return MLPMOE_ERR_UNSUPPORTED;
+  const bool vec = on(x, 16) && on(rows, 16) && a.x_stride % 16 == 0 && a.rows_stride % 16 == 0;
+  const dim3 grid(static_cast<unsigned>(blocks)), block(kMoveThreads);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  pdl_overlap_enabled() = true;
+  cudaError_t e;
+  if (es == 4)
+    e = vec ? launch_pdl(dispatch_kernel<4, true>, grid, block, 0, st, a) : launch_pdl(dispatch_kernel<4, false>, grid, block, 0, st, a);
+  else if (es == 2)
+    e = vec ? launch_pdl(dispatch_kernel<2, true>, grid, block, 0, st, a) : launch_pdl(dispatch_kernel<2, false>, grid, block, 0, st, a);
+  else
+    e = vec ? launch_pdl(dispatch_kernel<1, true>, grid, block, 0, st, a) : launch_pdl(dispatch_kernel<1, false>, grid, block, 0, st, a);
+  return e == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
+}
+
+mlpmoe_status_t mlpmoe_combine(const void* rows, mlpmoe_dtype_t rows_dtype, int64_t rows_stride, int64_t n_rows, const int32_t* token_row,
+                               const float* weight, int32_t slots, const void* residual, mlpmoe_dtype_t residual_dtype,
+                               int64_t residual_stride, void* y, mlpmoe_dtype_t y_dtype, int64_t y_stride, int64_t n_tokens,
+                               int64_t d_model, void* stream) {
+  if (n_tokens < 0 || n_tokens > INT32_MAX || d_model <= 0 || d_model > INT32_MAX / 8 || slots <= 0 || n_rows < 0 || n_rows > INT32_MAX)
+    return MLPMOE_ERR_INVALID_ARG;
+  if (!plain_kind(rows_dtype) || !plain_kind(y_dtype) || (residual && !plain_kind(residual_dtype))) return MLPMOE_ERR_INVALID_ARG;
+  if (rows_stride == 0) rows_stride = d_model;
+  if (residual_stride == 0) residual_stride = d_model;
+  if (y_stride == 0) y_stride = d_model;
+  if (rows_stride < d_model || (residual && residual_stride < d_model) || y_stride < d_model) return MLPMOE_ERR_INVALID_ARG;
+  if (n_tokens == 0) return MLPMOE_OK;
+  if ((n_rows > 0 && !rows) || !token_row || !y || !on(rows, bytes_of(rows_dtype)) || !on(y, bytes_of(y_dtype)) || !on(token_row, 4) ||
+      !on(weight, 4) || (residual && !on(residual, bytes_of(residual_dtype))))
+    return MLPMOE_ERR_INVALID_ARG;
+  if (residual == y && (residual_dtype != y_dtype || (residual_stride != y_stride && n_tokens > 1))) return MLPMOE_ERR_INVALID_ARG;
+  if (n_tokens * ((d_model + 255) / 256) / (kMoveThreads / 32) >= INT32_MAX) return MLPMOE_ERR_UNSUPPORTED;      // blocks of a launch
+  const bool vec = d_model % 8 == 0 && rows_stride % 8 == 0 && on(rows, 16) && y_stride % 8 == 0 && on(y, 16) &&
+                   (!residual || (residual_stride % 8 == 0 && on(residual, 16)));
+  CombineArgs a = {};
+  a.rows = rows;
+  a.token_row = token_row;
+  a.weight = weight;
+  a.residual = residual;
+  a.y = y;
+  a.rows_stride = rows_stride;
+  a.residual_stride = residual ? residual_stride : 0;
+  a.y_stride = y_stride;
+  a.n = n_tokens;
+  a.n_rows = n_rows;
+  a.slots = slots;
+  a.d = static_cast<int>(d_model);
+  pdl_overlap_enabled() = true;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int res_kind = residual ? static_cast<int>(residual_dtype) : kNone;
+  const cudaError_t e = rows_dtype == MLPMOE_FP32 ? launch_combine_from<MLPMOE_FP32>(a, res_kind, y_dtype, vec, st)
+                                                  : launch_combine_from<MLPMOE_BF16>(a, res_kind, y_dtype, vec, st);
+  return e == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
+}
+
+mlpmoe_status_t mlpmoe_combine_backward(const void* grad_y, mlpmoe_dtype_t grad_y_dtype, int64_t grad_y_stride, const void* rows,
+                                        mlpmoe_dtype_t rows_dtype, int64_t rows_stride, int64_t n_rows, const int32_t* token_row,
+                                        const float* weight, int32_t slots, int32_t B, int32_t align, const int32_t* offsets,
+                                        const int32_t* counts, void* grad_rows, int64_t grad_rows_stride, float* grad_weight,
+                                        int64_t n_tokens, int64_t d_model, void* stream) {
+  if (n_tokens < 0 || n_tokens > INT32_MAX || d_model <= 0 || slots <= 0 || B <= 0 || align <= 0 || n_rows < 0 || n_rows > INT32_MAX)
+    return MLPMOE_ERR_INVALID_ARG;
+  if (!plain_kind(grad_y_dtype) || !plain_kind(rows_dtype)) return MLPMOE_ERR_INVALID_ARG;
+  if (d_model > 32768 || B > kMaxB || align > kMaxAlign || n_tokens > INT32_MAX - kMaxB * kMaxAlign) return MLPMOE_ERR_UNSUPPORTED;
+  if (grad_y_stride == 0) grad_y_stride = d_model;
+  if (rows_stride == 0) rows_stride = d_model;
+  if (grad_rows_stride == 0) grad_rows_stride = d_model;
+  if (grad_y_stride < d_model || rows_stride < d_model || grad_rows_stride < d_model) return MLPMOE_ERR_INVALID_ARG;
+  if (n_tokens == 0) return MLPMOE_OK;
+  if (!grad_y || !token_row || (!grad_rows && !grad_weight) || (grad_weight && n_rows > 0 && !rows)) return MLPMOE_ERR_INVALID_ARG;
+  if (!on(grad_y, bytes_of(grad_y_dtype)) || !on(rows, bytes_of(rows_dtype)) || !on(grad_rows, bytes_of(rows_dtype)) || !on(token_row, 4) ||
+      !on(weight, 4) || !on(grad_weight, 4))
+    return MLPMOE_ERR_INVALID_ARG;
+  if (grad_rows && align > 1 && (!offsets || !counts || !on(offsets, 4) || !on(counts, 4))) return MLPMOE_ERR_INVALID_ARG;
+  if (grad_rows && grad_rows == rows && grad_rows_stride != rows_stride) return MLPMOE_ERR_INVALID_ARG;
+  const bool vec = d_model % 8 == 0 && grad_y_stride % 8 == 0 && on(grad_y, 16) && (!grad_weight || (rows_stride % 8 == 0 && on(rows, 16))) &&
+                   (!grad_rows || (grad_rows_stride % 8 == 0 && on(grad_rows, 16)));
+  CombineGradArgs a = {};
+  a.grad_y = grad_y;
+  a.rows = rows;
+  a.token_row = token_row;
+  a.weight = weight;
+  a.offsets = offsets;
+  a.counts = counts;
+  a.grad_rows = grad_rows;
+  a.grad_weight = grad_weight;
+  a.grad_y_stride = grad_y_stride;
+  a.rows_stride = rows_stride;
+  a.grad_rows_stride = grad_rows_stride;
+  a.n = n_tokens;
+  a.n_rows = n_rows;
+  a.slots = slots;
+  a.d = static_cast<int>(d_model);
+  a.B = B;
+  const int64_t pad_rows = grad_rows ? pad_rows_of(B, align) : 0;
+  pdl_overlap_enabled() = true;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = grad_y_dtype == MLPMOE_FP32 ? launch_grad_from<MLPMOE_FP32>(a, rows_dtype, vec, pad_rows, st)
+                                                    : launch_grad_from<MLPMOE_BF16>(a, rows_dtype, vec, pad_rows, st);
+  return e == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,124 @@
+// Rows in memory to registers and back, eight consecutive elements a thread, and sums over a row's threads: shared by the norms
+// and by the kernels that move and sum rows.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+
+#include "../../include/mlpmoe.h"
+#include "internal.h"
+
+namespace mlpmoe {
+
+__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xFFFF0000u); }
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&p);
+}
+
+// Eight consecutive elements from column col, as they stand in memory (fp32: the whole of a and b; bf16: a), zeros past the
+// row's end.  VEC: the row starts on 16 bytes and d % 8 == 0, so a chunk is whole.
+struct Chunk {
+  uint4 a, b;
+};
+template <bool VEC>
+__device__ __forceinline__ Chunk load_chunk(const void* row, int kind, int col, int d) {
+  Chunk c;
+  c.a = c.b = make_uint4(0u, 0u, 0u, 0u);
+  if (col >= d) return c;
+  if (kind == MLPMOE_FP32) {
+    const uint32_t* p = static_cast<const uint32_t*>(row) + col;
+    if (VEC) {
+      c.a = reinterpret_cast<const uint4*>(p)[0];
+      c.b = reinterpret_cast<const uint4*>(p)[1];
+    } else {
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = col + i < d ? p[i] : 0u;
+      c.a = make_uint4(w[0], w[1], w[2], w[3]);
+      c.b = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+  } else {
+    const uint16_t* p = static_cast<const uint16_t*>(row) + col;
+    if (VEC) {
+      c.a = *reinterpret_cast<const uint4*>(p);
+    } else {
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = col + i < d ? p[i] : 0u;
+      c.a = make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4] | (w[5] << 16), w[6] | (w[7] << 16));
+    }
+  }
+  return c;
+}
+__device__ __forceinline__ void to_f32(const Chunk& c, int kind, float (&v)[8]) {
+  if (kind == MLPMOE_FP32) {
+    v[0] = __uint_as_float(c.a.x), v[1] = __uint_as_float(c.a.y), v[2] = __uint_as_float(c.a.z), v[3] = __uint_as_float(c.a.w);
+    v[4] = __uint_as_float(c.b.x), v[5] = __uint_as_float(c.b.y), v[6] = __uint_as_float(c.b.z), v[7] = __uint_as_float(c.b.w);
+  } else {
+    v[0] = bf16_lo(c.a.x), v[1] = bf16_hi(c.a.x), v[2] = bf16_lo(c.a.y), v[3] = bf16_hi(c.a.y);
+    v[4] = bf16_lo(c.a.z), v[5] = bf16_hi(c.a.z), v[6] = bf16_lo(c.a.w), v[7] = bf16_hi(c.a.w);
+  }
+}
+
+template <bool VEC>
+__device__ __forceinline__ void store8(void* row, int kind, int col, int d, const float (&v)[8]) {
+  if (kind == MLPMOE_FP32) {
+    float* p = static_cast<float*>(row) + col;
+    if (VEC) {
+      __stcs(reinterpret_cast<float4*>(p), make_float4(v[0], v[1], v[2], v[3]));
+      __stcs(reinterpret_cast<float4*>(p) + 1, make_float4(v[4], v[5], v[6], v[7]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + i < d) p[i] = v[i];
+    }
+  } else if (kind == MLPMOE_BF16) {
+    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(row) + col;
+    if (VEC) {
+      *reinterpret_cast<uint4*>(p) = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + i < d) p[i] = __float2bfloat16_rn(v[i]);
+    }
+  } else {
+    uint8_t* p = static_cast<uint8_t*>(row) + col;
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = __nv_cvt_float2_to_fp8x2(make_float2(v[2 * i], v[2 * i + 1]), __NV_SATFINITE, __NV_E4M3);
+    if (VEC) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (col + i < d) p[i] = static_cast<uint8_t>(c[i / 2] >> (8 * (i & 1)));
+    }
+  }
+}
+
+// Sum (or maximum) over the T threads of a row, the same bits in all of them.  T = 32: the row's warp; else the block.
+template <int T, bool MAX>
+__device__ __forceinline__ float row_reduce(float v, float* red) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float u = __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    v = MAX ? fmaxf(v, u) : v + u;
+  }
+  if (T > 32) {
+    if (threadIdx.x % 32 == 0) red[threadIdx.x / 32] = v;
+    __syncthreads();
+    v = red[0];
+#pragma unroll
+    for (int i = 1; i < T / 32; ++i) v = MAX ? fmaxf(v, red[i]) : v + red[i];
+    __syncthreads();
+  }
+  return v;
+}
+
+// Bytes of an element of a kind (MLPMOE_BF16, MLPMOE_FP32, MLPMOE_E4M3).
+__host__ __device__ constexpr int bytes_of(int kind) { return kind == MLPMOE_FP32 ? 4 : (kind == MLPMOE_BF16 ? 2 : 1); }
+
+inline bool on(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+
+}  // namespace mlpmoe
