@@ -533,7 +533,7 @@ typedef struct {
 } mlpmoe_adamw_tensor_t;
 
 /*
- *   lr, beta1, beta2, eps    0 <= beta < 1, eps above 0 in fp32
+ *   lr, beta1, beta2, eps    0 <= beta < 1, eps at least 2^-126
  *   step           number of this step, from 1; step_device: device int64 [1], read instead if not NULL (below 1 counts as 1), so
  *                  that a captured graph can be replayed
  *   lr_device      device fp32 [1], read instead of lr if not NULL
@@ -552,7 +552,7 @@ typedef struct {
 } mlpmoe_adamw_settings_t;
 
 /*
- * One AdamW step over n_tensors tensors (a host array, not needed after the call), in fp32, a launch for up to 400 of one state type:
+ * One AdamW step over n_tensors tensors (a host array, not needed after the call), in fp32, a launch for up to 400 of the same types:
  *     g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *     param = param - lr * weight_decay * param - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
  * The param takes the new moments before they are rounded.  e4m3 moments: scale = max(max |finite value| / 448, 2^-126) of each 128

@@ -399,14 +399,10 @@ def mlpmoe_norm_backward(norm: int, s, grad_out, grad_x, n_tokens: int, d_model:
 def mlpmoe_adamw_tensors(tensors: Sequence[dict]):
     """The description of the tensors of mlpmoe_adamw, from dicts with the fields of mlpmoe_adamw_tensor_t: n, param, grad, m, v, and
     where they are used m_scale, v_scale, param_bf16, weight_decay, and the types (fp32 by default).  It keeps the tensors as long as it lives."""
-    arr = (mlpmoe_adamw_tensor_t * len(tensors))()
-    for record, t in zip(arr, tensors):
-        for name in ("param", "grad", "m", "v", "m_scale", "v_scale", "param_bf16"):
-            setattr(record, name, _ptr(t.get(name)))
-        record.n = t["n"]
-        record.weight_decay = t.get("weight_decay", 0.0)
-        for name in ("param_dtype", "grad_dtype", "state_dtype"):
-            setattr(record, name, t.get(name, MLPMOE_FP32))
+    arr = (mlpmoe_adamw_tensor_t * len(tensors))(*(
+        (_ptr(t["param"]), _ptr(t["grad"]), _ptr(t["m"]), _ptr(t["v"]), _ptr(t.get("m_scale")), _ptr(t.get("v_scale")), _ptr(t.get("param_bf16")), t["n"],
+         t.get("weight_decay", 0.0), t.get("param_dtype", MLPMOE_FP32), t.get("grad_dtype", MLPMOE_FP32), t.get("state_dtype", MLPMOE_FP32))
+        for t in tensors))
     arr._tensors = [dict(t) for t in tensors]
     return arr
 

@@ -21,8 +21,9 @@ namespace mlpmoe {
 namespace {
 
 constexpr int kAdamThreads = 256;
-constexpr int kAdamTurns = 2;                                  // chunks of eight elements of a thread
-constexpr int kAdamBlock = kAdamThreads * 8 * kAdamTurns;      // elements of a block
+// Chunks of eight elements a thread: all of a block's loads are issued before its first use (two chunks: 36 registers of 8-bit states; one: 32 of fp32 ones).
+__host__ __device__ constexpr int turns_of(bool eight) { return eight ? 2 : 1; }
+__host__ __device__ constexpr int block_of(bool eight) { return kAdamThreads * 8 * turns_of(eight); }      // elements of a block
 constexpr int kStateBlock = 128;                               // elements of a scale
 constexpr float kE4m3Max = 448.0f;
 constexpr float kScaleMin = 1.17549435e-38f;                   // 2^-126
@@ -40,12 +41,11 @@ struct AdamTensor {
   float decay;
   uint32_t first;       // the tensor's first block
   uint32_t index;       // its place in the caller's list
-  uint32_t flags;
+  uint32_t wide;        // all buffers start on 16 bytes
 };
-constexpr uint32_t kParamBf16 = 1, kGradBf16 = 2, kWide = 4;
 
 struct AdamSettings {
-  float lr, b1, b2, one_b1, one_b2, eps, log_b1, log_b2;
+  float lr, b1, b2, one_b1, root_b2, eps, log_b1, log_b2;
   const float* lr_device;
   const int64_t* step_device;
   const float* grad_scale;
@@ -69,38 +69,34 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t h) {
   return h ^ (h >> 16);
 }
 
-__device__ __forceinline__ void load8(const void* base, bool bf16, int64_t i, int64_t n, bool wide, float (&v)[8]) {
-  const int kind = bf16 ? MLPMOE_BF16 : MLPMOE_FP32;
-  const char* p = static_cast<const char*>(base) + i * bytes_of(kind);
-  if (wide && i + 8 <= n) {
-    to_f32(load_chunk<true>(p, kind, 0, 8), kind, v);
-  } else {
-    to_f32(load_chunk<false>(p, kind, 0, static_cast<int>(n - i < 8 ? n - i : 8)), kind, v);
-  }
+// Eight elements from i on, as they stand in memory, zeros past the end.
+template <int KIND>
+__device__ __forceinline__ Chunk fetch(const void* base, int64_t i, int64_t n, bool wide) {
+  const char* p = static_cast<const char*>(base) + i * bytes_of(KIND);
+  if (wide && i + 8 <= n) return load_chunk<true>(p, KIND, 0, 8);
+  return load_chunk<false>(p, KIND, 0, i >= n ? 0 : static_cast<int>(n - i < 8 ? n - i : 8));
 }
-__device__ __forceinline__ void store_to(void* base, bool bf16, int64_t i, int64_t n, bool wide, const float (&v)[8]) {
-  const int kind = bf16 ? MLPMOE_BF16 : MLPMOE_FP32;
-  char* p = static_cast<char*>(base) + i * bytes_of(kind);
+__device__ __forceinline__ uint2 fetch_codes(const void* base, int64_t i, int64_t n, bool wide) {
+  const uint8_t* p = static_cast<const uint8_t*>(base) + i;
+  if (wide && i + 8 <= n) return *reinterpret_cast<const uint2*>(p);
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (i + e < n) w[e / 4] |= static_cast<uint32_t>(p[e]) << (8 * (e % 4));
+  return make_uint2(w[0], w[1]);
+}
+template <int KIND>
+__device__ __forceinline__ void put(void* base, int64_t i, int64_t n, bool wide, const float (&v)[8]) {
+  char* p = static_cast<char*>(base) + i * bytes_of(KIND);
   if (wide && i + 8 <= n) {
-    store8<true>(p, kind, 0, 8, v);
+    store8<true>(p, KIND, 0, 8, v);
   } else {
-    store8<false>(p, kind, 0, static_cast<int>(n - i < 8 ? n - i : 8), v);
+    store8<false>(p, KIND, 0, static_cast<int>(n - i < 8 ? n - i : 8), v);
   }
 }
 
-// Eight e4m3 codes as their values.
-__device__ __forceinline__ void load_codes(const void* base, int64_t i, int64_t n, bool wide, float (&v)[8]) {
-  const uint8_t* p = static_cast<const uint8_t*>(base) + i;
-  uint32_t w[2] = {0u, 0u};
-  if (wide && i + 8 <= n) {
-    const uint2 u = *reinterpret_cast<const uint2*>(p);
-    w[0] = u.x;
-    w[1] = u.y;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (i + e < n) w[e / 4] |= static_cast<uint32_t>(p[e]) << (8 * (e % 4));
-  }
+__device__ __forceinline__ void values_of(uint2 codes, float (&v)[8]) {
+  const uint32_t w[2] = {codes.x, codes.y};
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w[e / 4] >> (8 * (e % 4))), __NV_E4M3);
@@ -111,47 +107,91 @@ __device__ __forceinline__ void load_codes(const void* base, int64_t i, int64_t 
 }
 
 __device__ __forceinline__ bool finite(float x) { return fabsf(x) <= FLT_MAX; }
+__device__ __forceinline__ float max_nan(float a, float b) {      // a NaN wins
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float sqrt_fast(float x) {             // off by 2^-23 at most
+  float r;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
 
-// Eight values of a block of 128 (16 lanes) to codes and the block's scale.  What is not finite becomes a NaN code and stays out of the scale.
+// Eight values of a block of 128 (16 neighbouring lanes) as codes, and the block's scale.  What is not finite becomes a NaN code and
+// stays out of the scale.  Stochastic: up with the probability of what truncation cuts off, by adding 16 random bits and a half
+// below the third bit of the fraction (the half also keeps the block's largest at 448); below 2^-6, where the steps of e4m3 no
+// longer shrink, to the value plus 2^-6.  Few elements lie there, so a thread without any skips that.
 template <bool NOISE, bool ROOT>
-__device__ __forceinline__ void store_codes(void* base, float* scales, int64_t i, int64_t n, bool wide, const float (&x)[8], const uint32_t (&noise)[8]) {
-  float top = 0.0f;
+__device__ __forceinline__ uint2 codes_of(const float (&x)[8], const uint32_t (&noise)[8], float& scale) {
+  float top = fabsf(x[0]), low = fabsf(x[0]);
 #pragma unroll
-  for (int e = 0; e < 8; ++e) top = fmaxf(top, finite(x[e]) ? fabsf(x[e]) : 0.0f);
+  for (int e = 1; e < 8; ++e) {
+    top = max_nan(top, fabsf(x[e]));
+    if (NOISE || ROOT) low = fminf(low, fabsf(x[e]));
+  }
 #pragma unroll
-  for (int o = 1; o < kStateBlock / 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-  const float scale = fmaxf(top / kE4m3Max, kScaleMin), inv = 1.0f / scale;
-  if (i >= n) return;
-  if (i % kStateBlock == 0) scales[i / kStateBlock] = scale;
+  for (int o = 1; o < kStateBlock / 8; o <<= 1) top = max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+  const bool fine = top <= FLT_MAX;
+  if (!fine) {                             // the same for all lanes of the block
+    top = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = fmaxf(top, finite(x[e]) ? fabsf(x[e]) : 0.0f);
+    const uint32_t half = 0xFFFFu << (threadIdx.x & 16);
+#pragma unroll
+    for (int o = 1; o < kStateBlock / 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(half, top, o));
+  }
+  scale = fmaxf(top * (1.0f / kE4m3Max), kScaleMin);
+  const float inv = __fdividef(1.0f, scale);
   float y[8];
+  if (fine && (!(NOISE || ROOT) || low >= scale * (NOISE ? 0.0157f : 0.002f))) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float a = fminf(fabsf(x[e]) * inv, kE4m3Max);
-    if (NOISE) {
-      // up with the probability of what truncation would cut: 16 random bits (and a half) added below the third bit of the fraction;
-      // below 2^-6, where the steps no longer shrink, on the value plus 2^-6
-      const float base_of = a < 0.015625f ? 0.015625f : 0.0f;
-      const uint32_t bits = __float_as_uint(a + base_of) + (((ROOT ? noise[e] >> 16 : noise[e] & 0xFFFFu) << 4) | 8u);
-      a = fminf(__uint_as_float(bits & 0xFFF00000u) - base_of, kE4m3Max);
+    for (int e = 0; e < 8; ++e) {
+      y[e] = x[e] * inv;
+      if (NOISE) {
+        const uint32_t bits = (((ROOT ? noise[e] >> 12 : noise[e] << 4) & 0x000FFFF0u) | 8u) + __float_as_uint(y[e]);
+        y[e] = __uint_as_float(bits & 0xFFF00000u);
+      }
     }
-    if (ROOT && x[e] > 0.0f) a = fmaxf(a, kRootMin);
-    y[e] = finite(x[e]) ? copysignf(a, x[e]) : __uint_as_float(0x7FC00000u);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float a = fabsf(x[e]) * inv;
+      if (NOISE) {
+        const float base = a < 0.015625f ? 0.015625f : 0.0f;
+        const uint32_t bits = (((ROOT ? noise[e] >> 12 : noise[e] << 4) & 0x000FFFF0u) | 8u) + __float_as_uint(a + base);
+        a = __uint_as_float(bits & 0xFFF00000u) - base;
+      }
+      if (ROOT && x[e] > 0.0f) a = fmaxf(a, kRootMin);
+      y[e] = finite(x[e]) ? copysignf(a, x[e]) : __uint_as_float(0x7FC00000u);
+    }
   }
   uint32_t c[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) c[e] = __nv_cvt_float2_to_fp8x2(make_float2(y[2 * e], y[2 * e + 1]), __NV_SATFINITE, __NV_E4M3);
+  return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+}
+__device__ __forceinline__ void put_codes(void* base, float* scales, int64_t i, int64_t n, bool wide, uint2 c, float scale) {
+  if (i % kStateBlock == 0) scales[i / kStateBlock] = scale;
   uint8_t* p = static_cast<uint8_t*>(base) + i;
   if (wide && i + 8 <= n) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+    *reinterpret_cast<uint2*>(p) = c;
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (i + e < n) p[e] = static_cast<uint8_t>(c[e / 2] >> (8 * (e & 1)));
+      if (i + e < n) p[e] = static_cast<uint8_t>((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
   }
 }
 
-template <int K, bool EIGHT, bool NOISE>
+struct Rates {
+  float keep, rate, inv_root, one_b1, root_b2;     // lr wd; lr / (1 - b1^i); 1 / sqrt(1 - b2^i); (1 - b1) gs; sqrt(1 - b2) gs
+  uint32_t key;
+};
+
+template <int K, int PK, int GK, bool EIGHT, bool NOISE>
 __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamArgs<K> a) {
+  constexpr int kTurns = turns_of(EIGHT);
+  __shared__ Rates shared_rates;
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   int lo = 0, hi = a.count - 1;
@@ -165,71 +205,94 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
   }
   const AdamTensor& t = a.t[lo];
   const AdamSettings& s = a.s;
-  int64_t step = s.step_device != nullptr ? *s.step_device : s.step;
-  if (step < 1) step = 1;
-  const float lr = s.lr_device != nullptr ? *s.lr_device : s.lr;
-  const float gs = s.grad_scale != nullptr ? *s.grad_scale : 1.0f;
-  const float fstep = static_cast<float>(step);
-  const float rate = lr / -expm1f(fstep * s.log_b1);
-  const float inv_root = 1.0f / sqrtf(-expm1f(fstep * s.log_b2));
-  const float keep = lr * t.decay;
-  const bool p16 = t.flags & kParamBf16, g16 = t.flags & kGradBf16, wide = t.flags & kWide;
-  const int64_t start = static_cast<int64_t>(blockIdx.x - t.first) * kAdamBlock;
-  uint32_t key = 0;
-  if (NOISE) {
-    key = mix(t.index ^ mix(s.key ^ static_cast<uint32_t>(step)));
-    if (start >> 32) key = mix(key ^ static_cast<uint32_t>(start >> 32));
-  }
+  const bool wide = t.wide != 0;
+  const int64_t n = t.n, start = static_cast<int64_t>(blockIdx.x - t.first) * block_of(EIGHT);
+  Chunk cp[kTurns], cg[kTurns], cm[kTurns], cv[kTurns];
+  uint2 em[kTurns], ev[kTurns];
+  float ms[kTurns], vs[kTurns];
 #pragma unroll
-  for (int turn = 0; turn < kAdamTurns; ++turn) {
+  for (int turn = 0; turn < kTurns; ++turn) {
     const int64_t i = start + (turn * kAdamThreads + threadIdx.x) * 8;
-    float p[8] = {}, g[8] = {}, m[8] = {}, v[8] = {};
-    if (i < t.n) {
-      load8(t.p, p16, i, t.n, wide, p);
-      load8(t.g, g16, i, t.n, wide, g);
-      if (EIGHT) {
-        load_codes(t.m, i, t.n, wide, m);
-        load_codes(t.v, i, t.n, wide, v);
-        const float ms = t.m_scale[i / kStateBlock], vs = t.v_scale[i / kStateBlock];
+    cp[turn] = fetch<PK>(t.p, i, n, wide);
+    cg[turn] = fetch<GK>(t.g, i, n, wide);
+    if (EIGHT) {
+      em[turn] = fetch_codes(t.m, i, n, wide);
+      ev[turn] = fetch_codes(t.v, i, n, wide);
+      ms[turn] = i < n ? t.m_scale[i / kStateBlock] : 0.0f;
+      vs[turn] = i < n ? t.v_scale[i / kStateBlock] : 0.0f;
+    } else {
+      cm[turn] = fetch<MLPMOE_FP32>(t.m, i, n, wide);
+      cv[turn] = fetch<MLPMOE_FP32>(t.v, i, n, wide);
+    }
+  }
+  if (threadIdx.x == 0) {                  // while the loads are under way
+    int64_t step = s.step_device != nullptr ? *s.step_device : s.step;
+    if (step < 1) step = 1;
+    const float lr = s.lr_device != nullptr ? *s.lr_device : s.lr;
+    const float gs = s.grad_scale != nullptr ? *s.grad_scale : 1.0f;
+    Rates r;
+    r.keep = lr * t.decay;
+    r.rate = lr / -expm1f(static_cast<float>(step) * s.log_b1);
+    r.inv_root = 1.0f / sqrtf(-expm1f(static_cast<float>(step) * s.log_b2));
+    r.one_b1 = s.one_b1 * gs;
+    r.root_b2 = s.root_b2 * gs;
+    r.key = mix(t.index ^ mix(s.key ^ static_cast<uint32_t>(step)));
+    if (start >> 32) r.key = mix(r.key ^ static_cast<uint32_t>(start >> 32));
+    shared_rates = r;
+  }
+  __syncthreads();
+  const Rates r = shared_rates;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          m[e] *= ms;
-          v[e] *= vs;
-          v[e] *= v[e];
-        }
-      } else {
-        load8(t.m, false, i, t.n, wide, m);
-        load8(t.v, false, i, t.n, wide, v);
+  for (int turn = 0; turn < kTurns; ++turn) {
+    const int64_t i = start + (turn * kAdamThreads + threadIdx.x) * 8;
+    float p[8], g[8], m[8], v[8];
+    to_f32(cp[turn], PK, p);
+    to_f32(cg[turn], GK, g);
+    if (EIGHT) {
+      values_of(em[turn], m);
+      values_of(ev[turn], v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        m[e] *= ms[turn];
+        v[e] *= vs[turn];
+        v[e] *= v[e];
       }
+    } else {
+      to_f32(cm[turn], MLPMOE_FP32, m);
+      to_f32(cv[turn], MLPMOE_FP32, v);
     }
     float root[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float x = g[e] * gs;
-      m[e] = fmaf(s.b1, m[e], s.one_b1 * x);
-      v[e] = fmaf(s.b2, v[e], s.one_b2 * x * x);
-      root[e] = sqrtf(v[e]);
-      p[e] = p[e] - keep * p[e] - rate * (m[e] / fmaf(root[e], inv_root, s.eps));
-    }
     uint32_t noise[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) noise[e] = NOISE ? mix(key + (static_cast<uint32_t>(i) + e) * 0x9E3779B1u) : 0u;
-    if (i < t.n) {
-      if (t.copy != nullptr) store_to(t.copy, true, i, t.n, wide, p);
-      if (NOISE && p16) {
+    for (int e = 0; e < 8; ++e) {
+      const float y = g[e] * r.root_b2;
+      m[e] = fmaf(s.b1, m[e], g[e] * r.one_b1);
+      v[e] = fmaf(y, y, s.b2 * v[e]);
+      root[e] = sqrt_fast(v[e]);
+      p[e] = fmaf(-r.keep, p[e], p[e]);
+      p[e] = fmaf(-r.rate, __fdividef(m[e], fmaf(root[e], r.inv_root, s.eps)), p[e]);
+      noise[e] = NOISE ? mix(r.key + static_cast<uint32_t>(i) * 0x9E3779B1u + e * 0x9E3779B1u) : 0u;
+    }
+    if (i < n) {
+      if (PK == MLPMOE_FP32 && t.copy != nullptr) put<MLPMOE_BF16>(t.copy, i, n, wide, p);
+      if (NOISE && PK == MLPMOE_BF16) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (finite(p[e])) p[e] = __uint_as_float((__float_as_uint(p[e]) + (mix(noise[e] ^ 0x9E3779B1u) & 0xFFFFu)) & 0xFFFF0000u);
       }
-      store_to(t.p, p16, i, t.n, wide, p);
+      put<PK>(t.p, i, n, wide, p);
       if (!EIGHT) {
-        store_to(t.m, false, i, t.n, wide, m);
-        store_to(t.v, false, i, t.n, wide, v);
+        put<MLPMOE_FP32>(t.m, i, n, wide, m);
+        put<MLPMOE_FP32>(t.v, i, n, wide, v);
       }
     }
     if (EIGHT) {
-      store_codes<NOISE, false>(t.m, t.m_scale, i, t.n, wide, m, noise);
-      store_codes<NOISE, true>(t.v, t.v_scale, i, t.n, wide, root, noise);
+      float scale_m, scale_v;
+      const uint2 code_m = codes_of<NOISE, false>(m, noise, scale_m), code_v = codes_of<NOISE, true>(root, noise, scale_v);
+      if (i < n) {
+        put_codes(t.m, t.m_scale, i, n, wide, code_m, scale_m);
+        put_codes(t.v, t.v_scale, i, n, wide, code_v, scale_v);
+      }
     }
   }
 }
@@ -238,8 +301,23 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
 constexpr int kAdamFew = 44, kAdamMany = 400;
 static_assert(sizeof(AdamArgs<kAdamFew>) <= 4096 && sizeof(AdamArgs<kAdamMany>) <= 32764, "kernel parameters");
 
+// A launch takes tensors of one set of types.
+struct Kinds {
+  bool p16, g16, eight, noise;
+};
+
+template <int K, int PK, int GK>
+cudaError_t launch_kinds(const Kinds& k, unsigned blocks, const AdamArgs<K>& a, cudaStream_t st) {
+  const dim3 grid(blocks), block(kAdamThreads);
+  if (k.eight)
+    return k.noise ? launch_pdl(adamw_kernel<K, PK, GK, true, true>, grid, block, 0, st, a) : launch_pdl(adamw_kernel<K, PK, GK, true, false>, grid, block, 0, st, a);
+  // moments in fp32: nothing to round but a bf16 param
+  return k.noise && PK == MLPMOE_BF16 ? launch_pdl(adamw_kernel<K, PK, GK, false, PK == MLPMOE_BF16>, grid, block, 0, st, a)
+                                      : launch_pdl(adamw_kernel<K, PK, GK, false, false>, grid, block, 0, st, a);
+}
+
 template <int K>
-cudaError_t launch_adamw(const AdamSettings& s, const AdamTensor* t, int count, bool eight, bool noise, cudaStream_t st) {
+cudaError_t launch_adamw(const AdamSettings& s, const AdamTensor* t, int count, const Kinds& k, cudaStream_t st) {
   AdamArgs<K> a;
   a.s = s;
   a.count = count;
@@ -247,12 +325,12 @@ cudaError_t launch_adamw(const AdamSettings& s, const AdamTensor* t, int count, 
   for (int i = 0; i < count; ++i) {
     a.t[i] = t[i];
     a.t[i].first = static_cast<uint32_t>(blocks);
-    blocks += (t[i].n + kAdamBlock - 1) / kAdamBlock;
+    blocks += (t[i].n + block_of(k.eight) - 1) / block_of(k.eight);
   }
-  const dim3 grid(static_cast<unsigned>(blocks)), block(kAdamThreads);
-  if (eight)
-    return noise ? launch_pdl(adamw_kernel<K, true, true>, grid, block, 0, st, a) : launch_pdl(adamw_kernel<K, true, false>, grid, block, 0, st, a);
-  return noise ? launch_pdl(adamw_kernel<K, false, true>, grid, block, 0, st, a) : launch_pdl(adamw_kernel<K, false, false>, grid, block, 0, st, a);
+  const unsigned grid = static_cast<unsigned>(blocks);
+  if (k.p16)
+    return k.g16 ? launch_kinds<K, MLPMOE_BF16, MLPMOE_BF16>(k, grid, a, st) : launch_kinds<K, MLPMOE_BF16, MLPMOE_FP32>(k, grid, a, st);
+  return k.g16 ? launch_kinds<K, MLPMOE_FP32, MLPMOE_BF16>(k, grid, a, st) : launch_kinds<K, MLPMOE_FP32, MLPMOE_FP32>(k, grid, a, st);
 }
 
 mlpmoe_status_t check_tensor(const mlpmoe_adamw_tensor_t& t) {
@@ -280,7 +358,7 @@ extern "C" mlpmoe_status_t mlpmoe_adamw(const mlpmoe_adamw_tensor_t* tensors, in
                                         void* stream) {
   if (n_tensors < 0 || (n_tensors > 0 && !tensors) || !settings) return MLPMOE_ERR_INVALID_ARG;
   const mlpmoe_adamw_settings_t& o = *settings;
-  if (!(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0) || !(o.eps <= FLT_MAX) || !(static_cast<float>(o.eps) > 0.0f))
+  if (!(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0) || !(o.eps <= FLT_MAX) || !(static_cast<float>(o.eps) >= FLT_MIN))
     return MLPMOE_ERR_INVALID_ARG;
   if (!(fabs(o.lr) <= FLT_MAX) || (!o.step_device && o.step < 1)) return MLPMOE_ERR_INVALID_ARG;
   if (!on(o.lr_device, 4) || !on(o.grad_scale, 4) || !on(o.step_device, 8)) return MLPMOE_ERR_INVALID_ARG;
@@ -293,7 +371,7 @@ extern "C" mlpmoe_status_t mlpmoe_adamw(const mlpmoe_adamw_tensor_t* tensors, in
   s.b1 = static_cast<float>(o.beta1);
   s.b2 = static_cast<float>(o.beta2);
   s.one_b1 = static_cast<float>(1.0 - o.beta1);
-  s.one_b2 = static_cast<float>(1.0 - o.beta2);
+  s.root_b2 = static_cast<float>(sqrt(1.0 - o.beta2));
   s.eps = static_cast<float>(o.eps);
   s.log_b1 = static_cast<float>(log(o.beta1));
   s.log_b2 = static_cast<float>(log(o.beta2));
@@ -304,22 +382,22 @@ extern "C" mlpmoe_status_t mlpmoe_adamw(const mlpmoe_adamw_tensor_t* tensors, in
   s.key = mix(mix(static_cast<uint32_t>(o.seed)) ^ static_cast<uint32_t>(o.seed >> 32));
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   pdl_overlap_enabled() = true;
-  for (const bool eight : {false, true}) {
+  for (int kind = 0; kind < 8; ++kind) {
+    const Kinds k = {(kind & 1) != 0, (kind & 2) != 0, (kind & 4) != 0, o.stochastic != 0};
     AdamTensor batch[kAdamMany];
     int count = 0;
     int64_t blocks = 0;
     auto flush = [&]() {
       if (count == 0) return cudaSuccess;
-      const cudaError_t e = count <= kAdamFew ? launch_adamw<kAdamFew>(s, batch, count, eight, o.stochastic != 0, st)
-                                              : launch_adamw<kAdamMany>(s, batch, count, eight, o.stochastic != 0, st);
+      const cudaError_t e = count <= kAdamFew ? launch_adamw<kAdamFew>(s, batch, count, k, st) : launch_adamw<kAdamMany>(s, batch, count, k, st);
       count = 0;
       blocks = 0;
       return e;
     };
     for (int32_t i = 0; i < n_tensors; ++i) {
       const mlpmoe_adamw_tensor_t& t = tensors[i];
-      if (t.n == 0 || (t.state_dtype == MLPMOE_E4M3) != eight) continue;
-      const int64_t need = (t.n + kAdamBlock - 1) / kAdamBlock;
+      if (t.n == 0 || (t.param_dtype == MLPMOE_BF16) != k.p16 || (t.grad_dtype == MLPMOE_BF16) != k.g16 || (t.state_dtype == MLPMOE_E4M3) != k.eight) continue;
+      const int64_t need = (t.n + block_of(k.eight) - 1) / block_of(k.eight);
       if ((count == kAdamMany || blocks + need > INT32_MAX) && flush() != cudaSuccess) return MLPMOE_ERR_CUDA;
       AdamTensor& r = batch[count++];
       blocks += need;
@@ -333,8 +411,7 @@ extern "C" mlpmoe_status_t mlpmoe_adamw(const mlpmoe_adamw_tensor_t* tensors, in
       r.n = t.n;
       r.decay = t.weight_decay;
       r.index = static_cast<uint32_t>(i);
-      const bool wide = on(t.param, 16) && on(t.grad, 16) && on(t.m, 16) && on(t.v, 16) && on(t.param_bf16, 16);
-      r.flags = (t.param_dtype == MLPMOE_BF16 ? kParamBf16 : 0u) | (t.grad_dtype == MLPMOE_BF16 ? kGradBf16 : 0u) | (wide ? kWide : 0u);
+      r.wide = on(t.param, 16) && on(t.grad, 16) && on(t.m, 16) && on(t.v, 16) && on(t.param_bf16, 16);
     }
     if (flush() != cudaSuccess) return MLPMOE_ERR_CUDA;
   }

@@ -33,6 +33,7 @@ struct NormArgs {
 template <bool LAYER, int XKIND, int RKIND, int OKIND, bool VEC, int T, int NCH>
 __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __grid_constant__ NormArgs a) {
   __shared__ float red[32];
+  __shared__ float sums[LAYER ? 2 : 1][T / 32][4];
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   const int tid = T == 32 ? threadIdx.x % 32 : threadIdx.x;
@@ -76,9 +77,11 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
       if (col < d) store8<VEC>(xo, XKIND, col, d, s[i]);
     }
   }
-  ss = row_reduce<T, false>(ss, red);
   if (LAYER) {                               // the mean first, then the squares of what is left: no cancellation
-    const float mean = ss / static_cast<float>(d);
+    int turn = 0;
+    float sum[1] = {ss};
+    row_sums<T, 1>(sum, sums, turn);
+    const float mean = sum[0] / static_cast<float>(d);
     ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < NCH; ++i)
@@ -87,6 +90,10 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
         s[i][j] = (VEC ? (i * T + tid) * 8 : (i * T + tid) * 8 + j) < d ? s[i][j] - mean : 0.0f;
         ss += s[i][j] * s[i][j];
       }
+    sum[0] = ss;
+    row_sums<T, 1>(sum, sums, turn);
+    ss = sum[0];
+  } else {
     ss = row_reduce<T, false>(ss, red);
   }
   const float inv = 1.0f / sqrtf(ss / static_cast<float>(d) + a.eps);

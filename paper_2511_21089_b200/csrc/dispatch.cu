@@ -469,7 +469,8 @@ struct CombineGradArgs {
 // T threads to a token (T = 32: a warp of a block of four): grad_y stays in registers, each of the token's rows is read for its
 // product with it and receives w * grad_y.  A row is read before it is written, by the same thread, so both may be one buffer.
 template <int GK, int RK, bool VEC, int T, int NCH>
-__global__ void __launch_bounds__(T == 32 ? 128 : T) combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
+__global__ void __launch_bounds__(T == 32 ? 128 : T, T == 32 ? 8 : (T < 1024 ? 1024 / T : 1)) combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
+  constexpr int kGradRows = NCH == 4 ? 1 : 4;       // rows of a token under way at a time: as many as there are registers for
   __shared__ float red[T / 32][32];
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
@@ -504,36 +505,58 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T) combine_backward_kernel(con
     uint32_t live = __ballot_sync(0xFFFFFFFFu, mine >= 0);
     float dot_mine = 0.0f;
     while (live != 0) {
-      const int src = __ffs(live) - 1;
-      live &= live - 1;
-      const int64_t r = __shfl_sync(0xFFFFFFFFu, mine, src);
-      const float w = __shfl_sync(0xFFFFFFFFu, w_mine, src);
+      int src[kGradRows];
+      int64_t r[kGradRows];
+      float w[kGradRows];
+      uint32_t next = live;
+#pragma unroll
+      for (int k = 0; k < kGradRows; ++k) {
+        src[k] = next != 0 ? __ffs(next) - 1 : -1;
+        next &= next - 1;
+        r[k] = __shfl_sync(0xFFFFFFFFu, mine, src[k] & 31);
+        w[k] = __shfl_sync(0xFFFFFFFFu, w_mine, src[k] & 31);
+      }
+      live = next;
       if (a.grad_weight != nullptr) {
-        const char* p = static_cast<const char*>(a.rows) + r * a.rows_stride * bytes_of(RK);
-        Chunk c[NCH];
+        Chunk c[kGradRows][NCH];
 #pragma unroll
-        for (int i = 0; i < NCH; ++i) c[i] = load_chunk<VEC>(p, RK, (i * T + tid) * 8, a.d);
-        float dot = 0.0f;
+        for (int k = 0; k < kGradRows; ++k) {
+          const char* p = static_cast<const char*>(a.rows) + r[k] * a.rows_stride * bytes_of(RK);
 #pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-          float f[8];
-          to_f32(c[i], RK, f);
-#pragma unroll
-          for (int e = 0; e < 8; ++e) dot = fmaf(g[i][e], f[e], dot);
+          for (int i = 0; i < NCH; ++i) c[k][i] = load_chunk<VEC>(p, RK, src[k] >= 0 ? (i * T + tid) * 8 : a.d, a.d);
         }
+        float dot[kGradRows];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, o);
-        if (lane == src) dot_mine = dot;
+        for (int k = 0; k < kGradRows; ++k) {
+          dot[k] = 0.0f;
+#pragma unroll
+          for (int i = 0; i < NCH; ++i) {
+            float f[8];
+            to_f32(c[k][i], RK, f);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot[k] = fmaf(g[i][e], f[e], dot[k]);
+          }
+        }
+        const float sum = warp_sums<kGradRows>(dot);
+#pragma unroll
+        for (int k = 0; k < kGradRows; ++k) {
+          const float of_k = __shfl_sync(0xFFFFFFFFu, sum, k * lanes_of(kGradRows));
+          if (lane == src[k]) dot_mine = of_k;
+        }
       }
       if (a.grad_rows != nullptr) {
-        char* p = static_cast<char*>(a.grad_rows) + r * a.grad_rows_stride * bytes_of(RK);
 #pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-          const int col = (i * T + tid) * 8;
-          float f[8];
+        for (int k = 0; k < kGradRows; ++k) {
+          if (src[k] < 0) continue;
+          char* p = static_cast<char*>(a.grad_rows) + r[k] * a.grad_rows_stride * bytes_of(RK);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = w * g[i][e];
-          if (col < a.d) store8<VEC>(p, RK, col, a.d, f);
+          for (int i = 0; i < NCH; ++i) {
+            const int col = (i * T + tid) * 8;
+            float f[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[e] = w[k] * g[i][e];
+            if (col < a.d) store8<VEC>(p, RK, col, a.d, f);
+          }
         }
       }
     }

@@ -2,8 +2,8 @@
 //     z = s - mean(s) (LayerNorm) or s (RMSNorm);  inv = 1 / sqrt(mean(z^2) + eps);  h = gain * dv;
 //     dx = ds + inv * (h - mean(h) - z * inv^2 * mean(h z))   (mean(h): LayerNorm only);
 //     dgain = sum_t dv * z * inv;   dbias = sum_t dv.
-// HBM-bound: s, dv and ds are read once, a block keeps its columns' sums over all of its rows in registers, the next row's loads are
-// under way while a row is reduced, and the blocks' sums are joined by a second launch in a fixed order.
+// HBM-bound: s, dv and ds are read once, a block keeps its columns' sums over all of its rows in registers, the next rows are on
+// their way while a row is reduced, and the blocks' sums are joined by a second launch in a fixed order.
 #include "../../include/mlpmoe.h"
 #include "internal.h"
 #include "ptx.cuh"
@@ -33,89 +33,95 @@ struct NormGradArgs {
   float eps;
 };
 
-// Sums of V values over the T threads of a row, the same bits in all of them.  `red`: two sets, used in turn, so that one barrier will do.
-template <int T, int V>
-__device__ __forceinline__ void row_sums(float (&v)[V], float (*red)[T / 32][4], int& turn) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
-#pragma unroll
-    for (int k = 0; k < V; ++k) v[k] += __shfl_xor_sync(0xFFFFFFFFu, v[k], o);
-  if (T > 32) {
-    float(*r)[4] = red[turn];
-    turn ^= 1;
-    if (threadIdx.x % 32 == 0)
-#pragma unroll
-      for (int k = 0; k < V; ++k) r[threadIdx.x / 32][k] = v[k];
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = r[0][k];
-#pragma unroll
-    for (int i = 1; i < T / 32; ++i)
-#pragma unroll
-      for (int k = 0; k < V; ++k) v[k] += r[i][k];
-  }
+__device__ __forceinline__ void copy_async16(uint4* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// T threads to a row (T = 32: eight rows to a block), NCH chunks of eight columns a thread.  SUMS: the columns' sums are kept here;
-// else the row's mean and inv go to memory for a kernel of their own.
-template <bool LAYER, bool VEC, int T, int NCH, bool SUMS>
-__global__ void __launch_bounds__(T == 32 ? 256 : T) norm_backward_kernel(const __grid_constant__ NormGradArgs a) {
-  constexpr int R = T == 32 ? 8 : 1;
+// Pieces of 16 bytes that eight elements of a kind take.
+__host__ __device__ constexpr int pieces_of(int kind) { return kind == MLPMOE_FP32 ? 2 : (kind == MLPMOE_BF16 ? 1 : 0); }
+
+// T threads to a row (T = 32: eight rows to a block), NCH chunks of eight columns a thread, whose sums over the block's rows stay in
+// registers.  The next STAGES - 1 rows are on their way to shared memory meanwhile; a thread reads only what it copied itself, so that
+// takes no barrier.  (The rows ahead in registers: 98 of them a thread, one block of 512 per SM, 258 us at 16384 x 4096.)
+template <bool LAYER, bool VEC, int T, int NCH, int STAGES, int CTAS>
+__global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(const __grid_constant__ NormGradArgs a) {
+  constexpr int R = T == 32 ? 8 : 1, THREADS = T == 32 ? 256 : T;
+  extern __shared__ uint4 staged[];
   __shared__ float red[2][T / 32][4];
-  __shared__ float join[T == 32 ? 8 : 1][T == 32 ? 256 : 1];
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   const int tid = T == 32 ? threadIdx.x % 32 : threadIdx.x, d = a.d;
+  const int ps = pieces_of(a.s_kind), pv = pieces_of(a.dv_kind), pr = pieces_of(a.ds_kind), pieces = ps + pv + pr;
   const int64_t step = static_cast<int64_t>(gridDim.x) * R;
   int64_t t = static_cast<int64_t>(blockIdx.x) * R + (T == 32 ? threadIdx.x / 32 : 0);
-  float gain[NCH][8], sum_g[SUMS ? NCH : 1][8], sum_b[SUMS && LAYER ? NCH : 1][8];
+  float sum_g[NCH][8], sum_b[LAYER ? NCH : 1][8];
 #pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    if (a.gain != nullptr) {
-      to_f32(load_chunk<VEC>(a.gain, MLPMOE_FP32, (i * T + tid) * 8, d), MLPMOE_FP32, gain[i]);
-    } else {
+  for (int i = 0; i < NCH; ++i)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) gain[i][e] = 1.0f;
+    for (int e = 0; e < 8; ++e) {
+      sum_g[i][e] = 0.0f;
+      if (LAYER) sum_b[i][e] = 0.0f;
     }
-    if (SUMS)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sum_g[i][e] = 0.0f;
-        if (LAYER) sum_b[i][e] = 0.0f;
-      }
-  }
-  Chunk cs[NCH], cv[NCH], cr[NCH];
-  auto fetch = [&](int64_t row) {
-    const char* ps = static_cast<const char*>(a.s) + row * a.s_stride * bytes_of(a.s_kind);
-    const char* pv = static_cast<const char*>(a.dv) + row * a.dv_stride * bytes_of(a.dv_kind);
-    const char* pr = static_cast<const char*>(a.ds) + row * a.ds_stride * bytes_of(a.ds_kind);
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) cs[i] = load_chunk<VEC>(ps, a.s_kind, (i * T + tid) * 8, d);
-#pragma unroll
-    for (int i = 0; i < NCH; ++i) cv[i] = load_chunk<VEC>(pv, a.dv_kind, (i * T + tid) * 8, d);
-    if (a.ds_kind != kNone) {
-#pragma unroll
-      for (int i = 0; i < NCH; ++i) cr[i] = load_chunk<VEC>(pr, a.ds_kind, (i * T + tid) * 8, d);
+  auto slot = [&](int stage, int i, int piece) { return staged + ((stage * NCH + i) * pieces + piece) * THREADS + threadIdx.x; };
+  auto fetch_one = [&](const void* base, int kind, int64_t offset, int stage, int i, int first) {
+    const int col = (i * T + tid) * 8;
+    const char* p = static_cast<const char*>(base) + offset * bytes_of(kind);
+    if (VEC) {
+      if (col >= d) return;
+      copy_async16(slot(stage, i, first), p + col * bytes_of(kind));
+      if (kind == MLPMOE_FP32) copy_async16(slot(stage, i, first + 1), p + col * 4 + 16);
+    } else {
+      const Chunk c = load_chunk<false>(p, kind, col, d);
+      *slot(stage, i, first) = c.a;
+      if (kind == MLPMOE_FP32) *slot(stage, i, first + 1) = c.b;
     }
   };
-  if (t < a.n) fetch(t);
-  int turn = 0;
-  const float inv_d = 1.0f / static_cast<float>(d);
-  for (; t < a.n; t += step) {
-    float z[NCH][8], v[NCH][8], r[NCH][8];
+  auto fetch = [&](int64_t row, int stage) {
+    if (row < a.n) {
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      to_f32(cs[i], a.s_kind, z[i]);
-      to_f32(cv[i], a.dv_kind, v[i]);
-      if (a.ds_kind != kNone) {
-        to_f32(cr[i], a.ds_kind, r[i]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[i][e] = 0.0f;
+      for (int i = 0; i < NCH; ++i) {
+        fetch_one(a.s, a.s_kind, row * a.s_stride, stage, i, 0);
+        fetch_one(a.dv, a.dv_kind, row * a.dv_stride, stage, i, ps);
+        if (pr != 0) fetch_one(a.ds, a.ds_kind, row * a.ds_stride, stage, i, ps + pv);
       }
     }
-    if (SUMS && t + step < a.n) fetch(t + step);
-    float mean = 0.0f, mean_h = 0.0f, ss, hz;
+    copy_commit();
+  };
+  auto value = [&](int stage, int i, int first, int kind, float (&v)[8]) {
+    Chunk c;
+    c.a = c.b = make_uint4(0u, 0u, 0u, 0u);
+    if (!VEC || (i * T + tid) * 8 < d) {
+      c.a = *slot(stage, i, first);
+      if (kind == MLPMOE_FP32) c.b = *slot(stage, i, first + 1);
+    }
+    to_f32(c, kind, v);
+  };
+  auto gain_of = [&](int i, float (&g)[8]) {      // from the L1 cache: eight registers a chunk are worth more
+    if (a.gain != nullptr) {
+      to_f32(load_chunk<VEC>(a.gain, MLPMOE_FP32, (i * T + tid) * 8, d), MLPMOE_FP32, g);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g[e] = 1.0f;
+    }
+  };
+#pragma unroll
+  for (int k = 0; k < STAGES; ++k) fetch(t + k * step, k);
+  int turn = 0, stage = 0;
+  const float inv_d = 1.0f / static_cast<float>(d);
+  for (; t < a.n; t += step) {
+    copy_wait<STAGES - 1>();
+    float z[NCH][8], v[NCH][8];
+#pragma unroll
+    for (int i = 0; i < NCH; ++i) {
+      value(stage, i, 0, a.s_kind, z[i]);
+      value(stage, i, ps, a.dv_kind, v[i]);
+    }
+    float mean_h = 0.0f, ss, hz;
     if (LAYER) {
       float sum[1] = {0.0f};
 #pragma unroll
@@ -123,19 +129,22 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) norm_backward_kernel(const 
 #pragma unroll
         for (int e = 0; e < 8; ++e) sum[0] += z[i][e];
       row_sums<T, 1>(sum, red, turn);
-      mean = sum[0] * inv_d;
+      const float mean = sum[0] * inv_d;
       float q[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int i = 0; i < NCH; ++i)
+      for (int i = 0; i < NCH; ++i) {
+        float gain[8];
+        gain_of(i, gain);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int col = (i * T + tid) * 8 + (VEC ? 0 : e);
           z[i][e] = col < d ? z[i][e] - mean : 0.0f;
-          const float h = gain[i][e] * v[i][e];
+          const float h = gain[e] * v[i][e];
           q[0] += z[i][e] * z[i][e];
           q[1] += h * z[i][e];
           q[2] += h;
         }
+      }
       row_sums<T, 3>(q, red, turn);
       ss = q[0];
       hz = q[1];
@@ -143,68 +152,147 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) norm_backward_kernel(const 
     } else {
       float q[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (int i = 0; i < NCH; ++i)
+      for (int i = 0; i < NCH; ++i) {
+        float gain[8];
+        gain_of(i, gain);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           q[0] += z[i][e] * z[i][e];
-          q[1] += gain[i][e] * v[i][e] * z[i][e];
+          q[1] += gain[e] * v[i][e] * z[i][e];
         }
+      }
       row_sums<T, 2>(q, red, turn);
       ss = q[0];
       hz = q[1];
     }
     const float inv = 1.0f / sqrtf(ss * inv_d + a.eps);
     const float along = hz * inv * inv * inv_d;
-    if (!SUMS && tid == 0 && a.stats != nullptr) {
-      a.stats[2 * t] = mean;
-      a.stats[2 * t + 1] = inv;
-    }
     char* px = static_cast<char*>(a.dx) + t * a.dx_stride * bytes_of(a.dx_kind);
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
+      float gain[8], r[8];
+      gain_of(i, gain);
+      if (pr != 0) {
+        value(stage, i, ps + pv, a.ds_kind, r);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = 0.0f;
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if (SUMS) {
-          sum_g[i][e] += v[i][e] * (z[i][e] * inv);
-          if (LAYER) sum_b[i][e] += v[i][e];
-        }
-        r[i][e] += inv * (gain[i][e] * v[i][e] - mean_h - z[i][e] * along);
+        sum_g[i][e] += v[i][e] * (z[i][e] * inv);
+        if (LAYER) sum_b[i][e] += v[i][e];
+        r[e] += inv * (gain[e] * v[i][e] - mean_h - z[i][e] * along);
       }
       const int col = (i * T + tid) * 8;
-      if (col < d) store8<VEC>(px, a.dx_kind, col, d, r[i]);
+      if (col < d) store8<VEC>(px, a.dx_kind, col, d, r);
     }
+    fetch(t + STAGES * step, stage);
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
   }
-  if (!SUMS || (a.dgain == nullptr && a.dbias == nullptr)) return;
+  if (a.dgain == nullptr && a.dbias == nullptr) return;
   // the block's sums: to the result where it is the only block
   float* out_g = gridDim.x == 1 ? a.dgain : a.partial + static_cast<int64_t>(blockIdx.x) * 2 * d;
   float* out_b = gridDim.x == 1 ? a.dbias : a.partial + (static_cast<int64_t>(blockIdx.x) * 2 + 1) * d;
-  if (T == 32) {
+  if (T == 32) {                           // the eight rows' sums first; the copies are done with shared memory
+    float* join = reinterpret_cast<float*>(staged);
 #pragma unroll
     for (int which = 0; which < (LAYER ? 2 : 1); ++which) {
+      copy_wait<0>();
       __syncthreads();
 #pragma unroll
-      for (int e = 0; e < 8; ++e) join[threadIdx.x / 32 % (T == 32 ? 8 : 1)][(tid * 8 + e) % (T == 32 ? 256 : 1)] = which == 0 ? sum_g[0][e] : sum_b[0][e];
+      for (int e = 0; e < 8; ++e) join[threadIdx.x * 8 + e] = which == 0 ? sum_g[0][e] : sum_b[0][e];
       __syncthreads();
       float* out = which == 0 ? out_g : out_b;
-      const int col = threadIdx.x;
-      if (col < d && out != nullptr) {
-        float sum = 0.0f;
+      if (threadIdx.x < d && out != nullptr) {
+        float sum = join[threadIdx.x];
 #pragma unroll
-        for (int w = 0; w < (T == 32 ? 8 : 1); ++w) sum += join[w][col % (T == 32 ? 256 : 1)];
-        out[col] = sum;
+        for (int w = 1; w < 8; ++w) sum += join[w * 256 + threadIdx.x];
+        out[threadIdx.x] = sum;
       }
     }
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int i = 0; i < (SUMS ? NCH : 1); ++i) {
-    const int col = (i * T + tid) * 8;
+    for (int i = 0; i < NCH; ++i) {
+      const int col = (i * T + tid) * 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (col + e >= d) continue;
+        if (out_g != nullptr) out_g[col + e] = sum_g[i][e];
+        if (LAYER && out_b != nullptr) out_b[col + e] = sum_b[LAYER ? i : 0][e];
+      }
+    }
+  }
+}
+
+// Rows above 8192 columns, a block to a row: no room for the columns' sums, so the row's mean and inv go to memory for a kernel of
+// their own, and grad_out is read a second time (from the L2 cache) instead of being held.
+template <bool LAYER, bool VEC>
+__global__ void __launch_bounds__(1024, 1) norm_backward_long_kernel(const __grid_constant__ NormGradArgs a) {
+  constexpr int T = 1024, NCH = 4;
+  __shared__ float red[2][T / 32][4];
+  ptx::griddep_launch_dependents();
+  ptx::griddep_wait();
+  const int d = a.d;
+  const int64_t t = blockIdx.x;
+  const char* ps = static_cast<const char*>(a.s) + t * a.s_stride * bytes_of(a.s_kind);
+  const char* pv = static_cast<const char*>(a.dv) + t * a.dv_stride * bytes_of(a.dv_kind);
+  const char* pr = static_cast<const char*>(a.ds) + t * a.ds_stride * bytes_of(a.ds_kind);
+  char* px = static_cast<char*>(a.dx) + t * a.dx_stride * bytes_of(a.dx_kind);
+  const float inv_d = 1.0f / static_cast<float>(d);
+  int turn = 0;
+  float z[NCH][8], mean = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) to_f32(load_chunk<VEC>(ps, a.s_kind, (i * T + threadIdx.x) * 8, d), a.s_kind, z[i]);
+  if (LAYER) {
+    float sum[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < NCH; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[0] += z[i][e];
+    row_sums<T, 1>(sum, red, turn);
+    mean = sum[0] * inv_d;
+  }
+  auto h_of = [&](int i, float (&h)[8]) {
+    const int col = (i * T + threadIdx.x) * 8;
+    to_f32(load_chunk<VEC>(pv, a.dv_kind, col, d), a.dv_kind, h);
+    if (a.gain != nullptr) {
+      float g[8];
+      to_f32(load_chunk<VEC>(a.gain, MLPMOE_FP32, col, d), MLPMOE_FP32, g);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[e] *= g[e];
+    }
+  };
+  float q[3] = {0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    float h[8];
+    h_of(i, h);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      if (col + e >= d) continue;
-      if (out_g != nullptr) out_g[col + e] = sum_g[i][e];
-      if (LAYER && out_b != nullptr) out_b[col + e] = sum_b[LAYER ? i : 0][e];
+      if (LAYER) z[i][e] = (i * T + threadIdx.x) * 8 + e < d ? z[i][e] - mean : 0.0f;
+      q[0] += z[i][e] * z[i][e];
+      q[1] += h[e] * z[i][e];
+      q[2] += h[e];
     }
+  }
+  row_sums<T, 3>(q, red, turn);
+  const float inv = 1.0f / sqrtf(q[0] * inv_d + a.eps);
+  const float along = q[1] * inv * inv * inv_d, mean_h = LAYER ? q[2] * inv_d : 0.0f;
+  if (threadIdx.x == 0 && a.stats != nullptr) {
+    a.stats[2 * t] = mean;
+    a.stats[2 * t + 1] = inv;
+  }
+#pragma unroll
+  for (int i = 0; i < NCH; ++i) {
+    const int col = (i * T + threadIdx.x) * 8;
+    if (col >= d) continue;
+    float h[8], r[8] = {};
+    h_of(i, h);
+    if (a.ds_kind != kNone) to_f32(load_chunk<VEC>(pr, a.ds_kind, col, d), a.ds_kind, r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] += inv * (h[e] - mean_h - z[i][e] * along);
+    store8<VEC>(px, a.dx_kind, col, d, r);
   }
 }
 
@@ -248,34 +336,43 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const __grid_constant__
   }
 }
 
-// Blocks of a call, and the threads of a row: about 1024 threads on every SM, so that few sums are left to join.
+// How a row of d columns is dealt: threads of a row and chunks of a thread, stages of rows on their way, blocks per SM.  Registers and
+// shared memory (40 bytes a chunk of fp32 s, bf16 grad_out, fp32 grad_s, up to 96) allow that many, and few blocks leave few sums to join.
 struct Shape {
-  int threads, rows, blocks;
+  int threads, rows, chunks, stages, ctas;
 };
-Shape shape_of(int64_t n, int64_t d) {
-  Shape s;
-  s.rows = d <= 256 ? 8 : 1;
-  s.threads = d <= 256 ? 256 : (d <= 1024 ? 128 : (d <= 2048 ? 256 : (d <= 4096 ? 512 : 1024)));
-  const int64_t need = (n + s.rows - 1) / s.rows, most = static_cast<int64_t>(kSms) * (1024 / s.threads);
-  s.blocks = static_cast<int>(need < most ? need : most);
-  return s;
+constexpr Shape kShapes[] = {{256, 8, 1, 3, 3}, {128, 1, 1, 3, 6}, {256, 1, 1, 3, 3}, {512, 1, 1, 2, 2}, {1024, 1, 1, 2, 1}};
+int shape_of(int64_t d) { return d <= 256 ? 0 : (d <= 1024 ? 1 : (d <= 2048 ? 2 : (d <= 4096 ? 3 : 4))); }
+int blocks_of(int64_t n, int64_t d) {
+  const Shape s = kShapes[shape_of(d)];
+  const int64_t need = (n + s.rows - 1) / s.rows, most = static_cast<int64_t>(kSms) * s.ctas;
+  return static_cast<int>(need < most ? need : most);
 }
 
+template <bool LAYER, bool VEC, int SHAPE>
+cudaError_t launch_shape(const NormGradArgs& a, cudaStream_t st) {
+  constexpr Shape s = kShapes[SHAPE];
+  auto kernel = norm_backward_kernel<LAYER, VEC, s.rows == 8 ? 32 : s.threads, s.chunks, s.stages, s.ctas>;
+  const int bytes = s.stages * s.chunks * s.threads * 16, pieces = pieces_of(a.s_kind) + pieces_of(a.dv_kind) + pieces_of(a.ds_kind);
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 6 * bytes);      // the same for every call
+  if (e != cudaSuccess) return e;
+  return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks_of(a.n, a.d))), dim3(s.threads), static_cast<size_t>(pieces) * bytes, st, a);
+}
 template <bool LAYER, bool VEC>
 cudaError_t launch_rows(const NormGradArgs& a, cudaStream_t st) {
-  if (a.d > kOnePassD) return launch_pdl(norm_backward_kernel<LAYER, VEC, 1024, 4, false>, dim3(static_cast<unsigned>(a.n)), dim3(1024), 0, st, a);
-  const Shape s = shape_of(a.n, a.d);
-  const dim3 grid(static_cast<unsigned>(s.blocks)), block(static_cast<unsigned>(s.threads));
-  if (a.d <= 256) return launch_pdl(norm_backward_kernel<LAYER, VEC, 32, 1, true>, grid, block, 0, st, a);
-  if (a.d <= 1024) return launch_pdl(norm_backward_kernel<LAYER, VEC, 128, 1, true>, grid, block, 0, st, a);
-  if (a.d <= 2048) return launch_pdl(norm_backward_kernel<LAYER, VEC, 256, 1, true>, grid, block, 0, st, a);
-  if (a.d <= 4096) return launch_pdl(norm_backward_kernel<LAYER, VEC, 512, 1, true>, grid, block, 0, st, a);
-  return launch_pdl(norm_backward_kernel<LAYER, VEC, 1024, 1, true>, grid, block, 0, st, a);
+  if (a.d > kOnePassD) return launch_pdl(norm_backward_long_kernel<LAYER, VEC>, dim3(static_cast<unsigned>(a.n)), dim3(1024), 0, st, a);
+  switch (shape_of(a.d)) {
+    case 0: return launch_shape<LAYER, VEC, 0>(a, st);
+    case 1: return launch_shape<LAYER, VEC, 1>(a, st);
+    case 2: return launch_shape<LAYER, VEC, 2>(a, st);
+    case 3: return launch_shape<LAYER, VEC, 3>(a, st);
+    default: return launch_shape<LAYER, VEC, 4>(a, st);
+  }
 }
 
 int64_t stats_bytes(int64_t n, int64_t d) { return d > kOnePassD ? (n * 8 + 15) / 16 * 16 : 0; }
 int64_t grad_bytes(int64_t n, int64_t d) {
-  const int64_t blocks = d > kOnePassD ? kSplitRows : shape_of(n, d).blocks;
+  const int64_t blocks = d > kOnePassD ? kSplitRows : blocks_of(n, d);
   return stats_bytes(n, d) + (blocks > 0 ? blocks : 1) * 2 * d * 4;
 }
 
@@ -356,7 +453,7 @@ mlpmoe_status_t mlpmoe_norm_backward(mlpmoe_norm_t norm, const void* s, mlpmoe_d
     e = vec ? launch_rows<false, true>(a, st) : launch_rows<false, false>(a, st);
   if (e != cudaSuccess) return MLPMOE_ERR_CUDA;
   if (!sums) return MLPMOE_OK;
-  int blocks = shape_of(n_tokens, d_model).blocks;
+  int blocks = blocks_of(n_tokens, d_model);
   if (d_model > kOnePassD) {
     blocks = static_cast<int>(n_tokens < kSplitRows ? n_tokens : kSplitRows);
     e = launch_pdl(norm_column_sums_kernel, dim3(static_cast<unsigned>((d_model + 255) / 256), static_cast<unsigned>(blocks)), dim3(256), 0, st, a,

@@ -116,6 +116,54 @@ __device__ __forceinline__ float row_reduce(float v, float* red) {
   return v;
 }
 
+// Sums of V values (V <= 4) over the 32 lanes of a warp: V == 1 in every lane, else value k in the lanes of the k-th half (V == 2) or
+// quarter.  The first steps exchange values, so that four sums cost 6 exchanges and not 20.
+template <int V>
+__device__ __forceinline__ float warp_sums(const float (&v)[V]) {
+  const int lane = threadIdx.x % 32;
+  float x;
+  if (V == 1) {
+    x = v[0];
+    x += __shfl_xor_sync(0xFFFFFFFFu, x, 16);
+    x += __shfl_xor_sync(0xFFFFFFFFu, x, 8);
+  } else if (V == 2) {
+    x = (lane & 16 ? v[V - 1] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, lane & 16 ? v[0] : v[V - 1], 16);
+    x += __shfl_xor_sync(0xFFFFFFFFu, x, 8);
+  } else {
+    const float v3 = V == 4 ? v[V - 1] : 0.0f;
+    const float a = (lane & 16 ? v[2 % V] : v[0]) + __shfl_xor_sync(0xFFFFFFFFu, lane & 16 ? v[0] : v[2 % V], 16);
+    const float b = (lane & 16 ? v3 : v[1 % V]) + __shfl_xor_sync(0xFFFFFFFFu, lane & 16 ? v[1 % V] : v3, 16);
+    x = (lane & 8 ? b : a) + __shfl_xor_sync(0xFFFFFFFFu, lane & 8 ? a : b, 8);
+  }
+#pragma unroll
+  for (int o = 4; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+  return x;
+}
+constexpr int __host__ __device__ lanes_of(int values) { return values == 1 ? 32 : (values == 2 ? 16 : 8); }      // lanes of a value there
+
+// Sums of V values over the T threads of a row (T = 32: a warp, else the block), the same bits in all of them.  `red`: two sets, used
+// in turn, so that one barrier a call will do.
+template <int T, int V>
+__device__ __forceinline__ void row_sums(float (&v)[V], float (*red)[T / 32][4], int& turn) {
+  constexpr int L = lanes_of(V);
+  const int lane = threadIdx.x % 32;
+  float x = warp_sums<V>(v);
+  if (T > 32) {
+    float(*r)[4] = red[turn];
+    turn ^= 1;
+    if (lane % L == 0 && lane / L < V) r[threadIdx.x / 32][lane / L] = x;
+    __syncthreads();
+    x = 0.0f;
+#pragma unroll
+    for (int i = 0; i < T / 32; i += L)
+      if (i + lane % L < T / 32) x += r[i + lane % L][lane / L];
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = V == 1 ? x : __shfl_sync(0xFFFFFFFFu, x, k * L);
+}
+
 // Bytes of an element of a kind (MLPMOE_BF16, MLPMOE_FP32, MLPMOE_E4M3).
 __host__ __device__ constexpr int bytes_of(int kind) { return kind == MLPMOE_FP32 ? 4 : (kind == MLPMOE_BF16 ? 2 : 1); }
 
