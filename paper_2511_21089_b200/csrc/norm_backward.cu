@@ -33,194 +33,215 @@ struct NormGradArgs {
   float eps;
 };
 
-__device__ __forceinline__ void copy_async16(uint4* to, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
+// Four consecutive values of a kind as they stand in shared memory (fp32: 16 bytes, bf16: 8).
+template <int KIND>
+__device__ __forceinline__ void quad_of(const char* p, float (&v)[4]) {
+  if (KIND == MLPMOE_FP32) {
+    const float4 f = *reinterpret_cast<const float4*>(p);
+    v[0] = f.x, v[1] = f.y, v[2] = f.z, v[3] = f.w;
+  } else {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    v[0] = bf16_lo(u.x), v[1] = bf16_hi(u.x), v[2] = bf16_lo(u.y), v[3] = bf16_hi(u.y);
+  }
 }
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+// Four values, 4 KIND bytes each, on their way to shared memory; WIDE: in one copy, else one at a time and at once.
+template <bool WIDE>
+__device__ __forceinline__ void copy_quad(char* to, const char* from, int kind, int left) {
+  if (WIDE) {
+    if (kind == MLPMOE_FP32) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
+    } else {
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
+    }
+  } else if (kind == MLPMOE_FP32) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) reinterpret_cast<float*>(to)[e] = e < left ? reinterpret_cast<const float*>(from)[e] : 0.0f;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) reinterpret_cast<uint16_t*>(to)[e] = e < left ? reinterpret_cast<const uint16_t*>(from)[e] : uint16_t{0};
+  }
 }
 
-// Pieces of 16 bytes that eight elements of a kind take.
-__host__ __device__ constexpr int pieces_of(int kind) { return kind == MLPMOE_FP32 ? 2 : (kind == MLPMOE_BF16 ? 1 : 0); }
+// Sums of V values over the threads of a row, the same bits in all of them: a warp (WARP), or the block's `warps` warps by way of
+// `red`, two sets used in turn, so that one barrier a call will do.
+template <bool WARP, int V>
+__device__ __forceinline__ void block_sums(float (&v)[V], float (*red)[32][4], int& turn, int warps) {
+  constexpr int L = lanes_of(V);
+  const int lane = threadIdx.x % 32;
+  float x = warp_sums<V>(v);
+  if (!WARP) {
+    float(*r)[4] = red[turn];
+    turn ^= 1;
+    if (lane % L == 0 && lane / L < V) r[threadIdx.x / 32][lane / L] = x;
+    __syncthreads();
+    x = 0.0f;
+    for (int i = lane % L; i < warps; i += L) x += r[i][lane / L];
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
+  }
+#pragma unroll
+  for (int k = 0; k < V; ++k) v[k] = V == 1 ? x : __shfl_sync(0xFFFFFFFFu, x, k * L);
+}
 
-// T threads to a row (T = 32: eight rows to a block), NCH chunks of eight columns a thread, whose sums over the block's rows stay in
-// registers.  The next STAGES - 1 rows are on their way to shared memory meanwhile; a thread reads only what it copied itself, so that
-// takes no barrier.  (The rows ahead in registers: 98 of them a thread, one block of 512 per SM, 258 us at 16384 x 4096.)
-template <bool LAYER, bool VEC, int T, int NCH, int STAGES, int CTAS>
-__global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(const __grid_constant__ NormGradArgs a) {
-  constexpr int R = T == 32 ? 8 : 1, THREADS = T == 32 ? 256 : T;
-  extern __shared__ uint4 staged[];
-  __shared__ float red[2][T / 32][4];
+constexpr int kStages = 2;
+
+// A row to the block's threads (WARP: to each of its eight warps), two times four neighbouring columns a thread, whose sums over
+// the block's rows stay in registers.  The next row is on its way to shared memory meanwhile; a thread reads only what it
+// copied itself, so that takes no barrier.  (The row ahead in registers, types told apart as it runs: 98 registers, 512 threads per SM, 258 us
+// at 16384 x 4096.)
+template <bool LAYER, bool WARP, bool WIDE, int SK, int VK>
+__global__ void __launch_bounds__(WARP ? 256 : 1024, WARP ? 4 : 1) norm_backward_kernel(const __grid_constant__ NormGradArgs a) {
+  extern __shared__ char staged[];
+  __shared__ float red[2][32][4];
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
-  const int tid = T == 32 ? threadIdx.x % 32 : threadIdx.x, d = a.d;
-  const int ps = pieces_of(a.s_kind), pv = pieces_of(a.dv_kind), pr = pieces_of(a.ds_kind), pieces = ps + pv + pr;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * R;
-  int64_t t = static_cast<int64_t>(blockIdx.x) * R + (T == 32 ? threadIdx.x / 32 : 0);
-  float sum_g[NCH][8], sum_b[LAYER ? NCH : 1][8];
-#pragma unroll
-  for (int i = 0; i < NCH; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      sum_g[i][e] = 0.0f;
-      if (LAYER) sum_b[i][e] = 0.0f;
-    }
-  auto slot = [&](int stage, int i, int piece) { return staged + ((stage * NCH + i) * pieces + piece) * THREADS + threadIdx.x; };
-  auto fetch_one = [&](const void* base, int kind, int64_t offset, int stage, int i, int first) {
-    const int col = (i * T + tid) * 8;
-    const char* p = static_cast<const char*>(base) + offset * bytes_of(kind);
-    if (VEC) {
-      if (col >= d) return;
-      copy_async16(slot(stage, i, first), p + col * bytes_of(kind));
-      if (kind == MLPMOE_FP32) copy_async16(slot(stage, i, first + 1), p + col * 4 + 16);
-    } else {
-      const Chunk c = load_chunk<false>(p, kind, col, d);
-      *slot(stage, i, first) = c.a;
-      if (kind == MLPMOE_FP32) *slot(stage, i, first + 1) = c.b;
-    }
-  };
+  const int d = a.d, tid = WARP ? threadIdx.x % 32 : threadIdx.x, T = WARP ? 32 : blockDim.x;
+  const int dk_bytes = bytes_of(a.ds_kind), row_warps = blockDim.x / 32;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * (WARP ? 8 : 1);
+  int64_t t = static_cast<int64_t>(blockIdx.x) * (WARP ? 8 : 1) + (WARP ? threadIdx.x / 32 : 0);
+  const int cols[2] = {tid * 4, (tid + T) * 4};
+  // in shared memory: [stage][quad][thread] of s, then of dv, then of ds
+  constexpr int kSBytes = 4 * bytes_of(SK), kVBytes = 4 * bytes_of(VK);
+  const int threads = blockDim.x, v_at = kStages * 2 * kSBytes * threads, r_at = v_at + kStages * 2 * kVBytes * threads;
+  auto place = [&](int at, int bytes, int stage, int k) { return staged + at + ((stage * 2 + k) * threads + threadIdx.x) * bytes; };
   auto fetch = [&](int64_t row, int stage) {
     if (row < a.n) {
+      const char* ps = static_cast<const char*>(a.s) + row * a.s_stride * bytes_of(SK);
+      const char* pv = static_cast<const char*>(a.dv) + row * a.dv_stride * bytes_of(VK);
+      const char* pr = static_cast<const char*>(a.ds) + row * a.ds_stride * dk_bytes;
 #pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-        fetch_one(a.s, a.s_kind, row * a.s_stride, stage, i, 0);
-        fetch_one(a.dv, a.dv_kind, row * a.dv_stride, stage, i, ps);
-        if (pr != 0) fetch_one(a.ds, a.ds_kind, row * a.ds_stride, stage, i, ps + pv);
+      for (int k = 0; k < 2; ++k) {
+        if (cols[k] >= d) continue;
+        copy_quad<WIDE>(place(0, kSBytes, stage, k), ps + cols[k] * bytes_of(SK), SK, d - cols[k]);
+        copy_quad<WIDE>(place(v_at, kVBytes, stage, k), pv + cols[k] * bytes_of(VK), VK, d - cols[k]);
+        if (a.ds_kind != kNone) copy_quad<WIDE>(place(r_at, 4 * dk_bytes, stage, k), pr + cols[k] * dk_bytes, a.ds_kind, d - cols[k]);
       }
     }
-    copy_commit();
+    asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  auto value = [&](int stage, int i, int first, int kind, float (&v)[8]) {
-    Chunk c;
-    c.a = c.b = make_uint4(0u, 0u, 0u, 0u);
-    if (!VEC || (i * T + tid) * 8 < d) {
-      c.a = *slot(stage, i, first);
-      if (kind == MLPMOE_FP32) c.b = *slot(stage, i, first + 1);
-    }
-    to_f32(c, kind, v);
-  };
-  auto gain_of = [&](int i, float (&g)[8]) {      // from the L1 cache: eight registers a chunk are worth more
-    if (a.gain != nullptr) {
-      to_f32(load_chunk<VEC>(a.gain, MLPMOE_FP32, (i * T + tid) * 8, d), MLPMOE_FP32, g);
-    } else {
+  float gain[2][4], sum_g[2][4], sum_b[2][4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g[e] = 1.0f;
-    }
-  };
+  for (int k = 0; k < 2; ++k)
 #pragma unroll
-  for (int k = 0; k < STAGES; ++k) fetch(t + k * step, k);
+    for (int e = 0; e < 4; ++e) {
+      gain[k][e] = cols[k] + e < d ? (a.gain != nullptr ? a.gain[cols[k] + e] : 1.0f) : 0.0f;
+      sum_g[k][e] = sum_b[k][e] = 0.0f;
+    }
+#pragma unroll
+  for (int k = 0; k < kStages; ++k) fetch(t + k * step, k);
   int turn = 0, stage = 0;
   const float inv_d = 1.0f / static_cast<float>(d);
   for (; t < a.n; t += step) {
-    copy_wait<STAGES - 1>();
-    float z[NCH][8], v[NCH][8];
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    float z[2][4], v[2][4];
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      value(stage, i, 0, a.s_kind, z[i]);
-      value(stage, i, ps, a.dv_kind, v[i]);
+    for (int k = 0; k < 2; ++k) {
+      if (cols[k] < d) {
+        quad_of<SK>(place(0, kSBytes, stage, k), z[k]);
+        quad_of<VK>(place(v_at, kVBytes, stage, k), v[k]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[k][e] = v[k][e] = 0.0f;
+      }
     }
     float mean_h = 0.0f, ss, hz;
     if (LAYER) {
-      float sum[1] = {0.0f};
-#pragma unroll
-      for (int i = 0; i < NCH; ++i)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sum[0] += z[i][e];
-      row_sums<T, 1>(sum, red, turn);
+      float sum[1] = {(z[0][0] + z[0][1]) + (z[0][2] + z[0][3]) + ((z[1][0] + z[1][1]) + (z[1][2] + z[1][3]))};
+      block_sums<WARP, 1>(sum, red, turn, row_warps);
       const float mean = sum[0] * inv_d;
       float q[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-        float gain[8];
-        gain_of(i, gain);
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int col = (i * T + tid) * 8 + (VEC ? 0 : e);
-          z[i][e] = col < d ? z[i][e] - mean : 0.0f;
-          const float h = gain[e] * v[i][e];
-          q[0] += z[i][e] * z[i][e];
-          q[1] += h * z[i][e];
+        for (int e = 0; e < 4; ++e) {
+          z[k][e] = cols[k] + (WIDE ? 0 : e) < d ? z[k][e] - mean : 0.0f;
+          const float h = gain[k][e] * v[k][e];
+          q[0] = fmaf(z[k][e], z[k][e], q[0]);
+          q[1] = fmaf(h, z[k][e], q[1]);
           q[2] += h;
         }
-      }
-      row_sums<T, 3>(q, red, turn);
+      block_sums<WARP, 3>(q, red, turn, row_warps);
       ss = q[0];
       hz = q[1];
       mean_h = q[2] * inv_d;
     } else {
       float q[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-        float gain[8];
-        gain_of(i, gain);
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          q[0] += z[i][e] * z[i][e];
-          q[1] += gain[e] * v[i][e] * z[i][e];
+        for (int e = 0; e < 4; ++e) {
+          q[0] = fmaf(z[k][e], z[k][e], q[0]);
+          q[1] = fmaf(gain[k][e] * v[k][e], z[k][e], q[1]);
         }
-      }
-      row_sums<T, 2>(q, red, turn);
+      block_sums<WARP, 2>(q, red, turn, row_warps);
       ss = q[0];
       hz = q[1];
     }
-    const float inv = 1.0f / sqrtf(ss * inv_d + a.eps);
+    const float inv = rsqrtf(ss * inv_d + a.eps);
     const float along = hz * inv * inv * inv_d;
     char* px = static_cast<char*>(a.dx) + t * a.dx_stride * bytes_of(a.dx_kind);
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      float gain[8], r[8];
-      gain_of(i, gain);
-      if (pr != 0) {
-        value(stage, i, ps + pv, a.ds_kind, r);
+    for (int k = 0; k < 2; ++k) {
+      if (cols[k] >= d) continue;
+      float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (a.ds_kind == MLPMOE_FP32) quad_of<MLPMOE_FP32>(place(r_at, 16, stage, k), r);
+      if (a.ds_kind == MLPMOE_BF16) quad_of<MLPMOE_BF16>(place(r_at, 8, stage, k), r);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sum_g[k][e] = fmaf(v[k][e], z[k][e] * inv, sum_g[k][e]);
+        if (LAYER) sum_b[k][e] += v[k][e];
+        r[e] = fmaf(inv, fmaf(-z[k][e], along, fmaf(gain[k][e], v[k][e], -mean_h)), r[e]);
+      }
+      if (a.dx_kind == MLPMOE_FP32) {
+        float* p = reinterpret_cast<float*>(px) + cols[k];
+        if (WIDE) {
+          __stcs(reinterpret_cast<float4*>(p), make_float4(r[0], r[1], r[2], r[3]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (cols[k] + e < d) p[e] = r[e];
+        }
       } else {
+        __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(px) + cols[k];
+        if (WIDE) {
+          *reinterpret_cast<uint2*>(p) = make_uint2(pack2(r[0], r[1]), pack2(r[2], r[3]));
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = 0.0f;
+          for (int e = 0; e < 4; ++e)
+            if (cols[k] + e < d) p[e] = __float2bfloat16_rn(r[e]);
+        }
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sum_g[i][e] += v[i][e] * (z[i][e] * inv);
-        if (LAYER) sum_b[i][e] += v[i][e];
-        r[e] += inv * (gain[e] * v[i][e] - mean_h - z[i][e] * along);
-      }
-      const int col = (i * T + tid) * 8;
-      if (col < d) store8<VEC>(px, a.dx_kind, col, d, r);
     }
-    fetch(t + STAGES * step, stage);
-    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    fetch(t + kStages * step, stage);
+    stage ^= 1;
   }
   if (a.dgain == nullptr && a.dbias == nullptr) return;
   // the block's sums: to the result where it is the only block
-  float* out_g = gridDim.x == 1 ? a.dgain : a.partial + static_cast<int64_t>(blockIdx.x) * 2 * d;
-  float* out_b = gridDim.x == 1 ? a.dbias : a.partial + (static_cast<int64_t>(blockIdx.x) * 2 + 1) * d;
-  if (T == 32) {                           // the eight rows' sums first; the copies are done with shared memory
-    float* join = reinterpret_cast<float*>(staged);
+  float* out[2] = {gridDim.x == 1 ? a.dgain : a.partial + static_cast<int64_t>(blockIdx.x) * 2 * d,
+                   gridDim.x == 1 ? a.dbias : a.partial + (static_cast<int64_t>(blockIdx.x) * 2 + 1) * d};
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  float* join = reinterpret_cast<float*>(staged);      // WARP: the eight rows' sums first
 #pragma unroll
-    for (int which = 0; which < (LAYER ? 2 : 1); ++which) {
-      copy_wait<0>();
+  for (int which = 0; which < (LAYER ? 2 : 1); ++which) {
+    if (WARP) {
       __syncthreads();
 #pragma unroll
-      for (int e = 0; e < 8; ++e) join[threadIdx.x * 8 + e] = which == 0 ? sum_g[0][e] : sum_b[0][e];
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) join[(threadIdx.x / 32) * 256 + cols[k] + e] = which == 0 ? sum_g[k][e] : sum_b[k][e];
       __syncthreads();
-      float* out = which == 0 ? out_g : out_b;
-      if (threadIdx.x < d && out != nullptr) {
+      if (static_cast<int>(threadIdx.x) < d && out[which] != nullptr) {
         float sum = join[threadIdx.x];
 #pragma unroll
         for (int w = 1; w < 8; ++w) sum += join[w * 256 + threadIdx.x];
-        out[threadIdx.x] = sum;
+        out[which][threadIdx.x] = sum;
       }
-    }
-  } else {
+    } else if (out[which] != nullptr) {
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int col = (i * T + tid) * 8;
+      for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if (col + e >= d) continue;
-        if (out_g != nullptr) out_g[col + e] = sum_g[i][e];
-        if (LAYER && out_b != nullptr) out_b[col + e] = sum_b[LAYER ? i : 0][e];
-      }
+        for (int e = 0; e < 4; ++e)
+          if (cols[k] + e < d) out[which][cols[k] + e] = which == 0 ? sum_g[k][e] : sum_b[k][e];
     }
   }
 }
@@ -325,7 +346,7 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const __grid_constant__
   if (out == nullptr) return;
   float sum = 0.0f;
   if (col < a.d)
-#pragma unroll 4
+#pragma unroll 8
     for (int i = w; i < blocks; i += 32) sum += a.partial[(static_cast<int64_t>(i) * 2 + blockIdx.y) * a.d + col];
   part[w][lane] = sum;
   __syncthreads();
@@ -336,38 +357,38 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const __grid_constant__
   }
 }
 
-// How a row of d columns is dealt: threads of a row and chunks of a thread, stages of rows on their way, blocks per SM.  Registers and
-// shared memory (40 bytes a chunk of fp32 s, bf16 grad_out, fp32 grad_s, up to 96) allow that many, and few blocks leave few sums to join.
-struct Shape {
-  int threads, rows, chunks, stages, ctas;
-};
-constexpr Shape kShapes[] = {{256, 8, 1, 3, 3}, {128, 1, 1, 3, 6}, {256, 1, 1, 3, 3}, {512, 1, 1, 2, 2}, {1024, 1, 1, 2, 1}};
-int shape_of(int64_t d) { return d <= 256 ? 0 : (d <= 1024 ? 1 : (d <= 2048 ? 2 : (d <= 4096 ? 3 : 4))); }
+// Threads and blocks of a call: eight columns a thread, 1024 threads an SM (64 registers each, and two stages of up to 12 bytes a column in
+// shared memory), and four rows or more to a block where every SM has one, so that few sums are left to join.
+int threads_of(int64_t d) { return d <= 256 ? 256 : static_cast<int>((d + 255) / 256 * 32); }
 int blocks_of(int64_t n, int64_t d) {
-  const Shape s = kShapes[shape_of(d)];
-  const int64_t need = (n + s.rows - 1) / s.rows, most = static_cast<int64_t>(kSms) * s.ctas;
-  return static_cast<int>(need < most ? need : most);
+  const int64_t need = d <= 256 ? (n + 7) / 8 : n, most = static_cast<int64_t>(kSms) * (1024 / threads_of(d));
+  const int64_t few = (need + 3) / 4 > kSms ? (need + 3) / 4 : kSms;
+  const int64_t blocks = need < few ? need : few;
+  return static_cast<int>(blocks < most ? blocks : most);
 }
 
-template <bool LAYER, bool VEC, int SHAPE>
-cudaError_t launch_shape(const NormGradArgs& a, cudaStream_t st) {
-  constexpr Shape s = kShapes[SHAPE];
-  auto kernel = norm_backward_kernel<LAYER, VEC, s.rows == 8 ? 32 : s.threads, s.chunks, s.stages, s.ctas>;
-  const int bytes = s.stages * s.chunks * s.threads * 16, pieces = pieces_of(a.s_kind) + pieces_of(a.dv_kind) + pieces_of(a.ds_kind);
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 6 * bytes);      // the same for every call
+template <bool LAYER, bool WARP, bool WIDE, int SK, int VK>
+cudaError_t launch_kinds(const NormGradArgs& a, cudaStream_t st) {
+  auto kernel = norm_backward_kernel<LAYER, WARP, WIDE, SK, VK>;
+  const int threads = threads_of(a.d), most = kStages * 8 * (bytes_of(SK) + bytes_of(VK) + 4);
+  // the limit is the same for every call, whatever its own size
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most * (WARP ? 256 : 1024));
   if (e != cudaSuccess) return e;
-  return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks_of(a.n, a.d))), dim3(s.threads), static_cast<size_t>(pieces) * bytes, st, a);
+  const int bytes = kStages * 8 * threads * (bytes_of(SK) + bytes_of(VK) + (a.ds_kind == kNone ? 0 : bytes_of(a.ds_kind)));
+  return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks_of(a.n, a.d))), dim3(static_cast<unsigned>(threads)), static_cast<size_t>(bytes), st, a);
 }
-template <bool LAYER, bool VEC>
+template <bool LAYER, bool WARP, bool WIDE>
+cudaError_t launch_from(const NormGradArgs& a, cudaStream_t st) {
+  if (a.s_kind == MLPMOE_FP32)
+    return a.dv_kind == MLPMOE_FP32 ? launch_kinds<LAYER, WARP, WIDE, MLPMOE_FP32, MLPMOE_FP32>(a, st)
+                                    : launch_kinds<LAYER, WARP, WIDE, MLPMOE_FP32, MLPMOE_BF16>(a, st);
+  return a.dv_kind == MLPMOE_FP32 ? launch_kinds<LAYER, WARP, WIDE, MLPMOE_BF16, MLPMOE_FP32>(a, st)
+                                  : launch_kinds<LAYER, WARP, WIDE, MLPMOE_BF16, MLPMOE_BF16>(a, st);
+}
+template <bool LAYER, bool WIDE>
 cudaError_t launch_rows(const NormGradArgs& a, cudaStream_t st) {
-  if (a.d > kOnePassD) return launch_pdl(norm_backward_long_kernel<LAYER, VEC>, dim3(static_cast<unsigned>(a.n)), dim3(1024), 0, st, a);
-  switch (shape_of(a.d)) {
-    case 0: return launch_shape<LAYER, VEC, 0>(a, st);
-    case 1: return launch_shape<LAYER, VEC, 1>(a, st);
-    case 2: return launch_shape<LAYER, VEC, 2>(a, st);
-    case 3: return launch_shape<LAYER, VEC, 3>(a, st);
-    default: return launch_shape<LAYER, VEC, 4>(a, st);
-  }
+  if (a.d > kOnePassD) return launch_pdl(norm_backward_long_kernel<LAYER, WIDE>, dim3(static_cast<unsigned>(a.n)), dim3(1024), 0, st, a);
+  return a.d <= 256 ? launch_from<LAYER, true, WIDE>(a, st) : launch_from<LAYER, false, WIDE>(a, st);
 }
 
 int64_t stats_bytes(int64_t n, int64_t d) { return d > kOnePassD ? (n * 8 + 15) / 16 * 16 : 0; }
