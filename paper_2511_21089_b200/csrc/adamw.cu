@@ -112,10 +112,32 @@ __device__ __forceinline__ float max_nan(float a, float b) {      // a NaN wins
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
   return r;
 }
-__device__ __forceinline__ float sqrt_fast(float x) {             // off by 2^-23 at most
+__device__ __forceinline__ float max_nan(float a, float b, float c) {
   float r;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
+}
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float r;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ float sqrt_fast(float x) {             // off by 2^-23 at most; below 2^-126: 0
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float reciprocal_fast(float x) {       // off by 2^-23 at most, for x from 2^-126 to 2^126
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+// Smallest magnitude of eight values.
+__device__ __forceinline__ float low_of(const float (&x)[8]) {
+  float low = min3(fabsf(x[0]), fabsf(x[1]), fabsf(x[2]));
+  low = min3(low, fabsf(x[3]), fabsf(x[4]));
+  low = min3(low, fabsf(x[5]), fabsf(x[6]));
+  return fminf(low, fabsf(x[7]));
 }
 
 // Eight values of a block of 128 (16 neighbouring lanes) as codes, and the block's scale.  What is not finite becomes a NaN code and
@@ -124,12 +146,10 @@ __device__ __forceinline__ float sqrt_fast(float x) {             // off by 2^-2
 // longer shrink, to the value plus 2^-6.  Few elements lie there, so a thread without any skips that.
 template <bool NOISE, bool ROOT>
 __device__ __forceinline__ uint2 codes_of(const float (&x)[8], const uint32_t (&noise)[8], float& scale) {
-  float top = fabsf(x[0]), low = fabsf(x[0]);
-#pragma unroll
-  for (int e = 1; e < 8; ++e) {
-    top = max_nan(top, fabsf(x[e]));
-    if (NOISE || ROOT) low = fminf(low, fabsf(x[e]));
-  }
+  float top = max_nan(fabsf(x[0]), fabsf(x[1]), fabsf(x[2]));
+  top = max_nan(top, fabsf(x[3]), fabsf(x[4]));
+  top = max_nan(top, fabsf(x[5]), fabsf(x[6]));
+  top = max_nan(top, fabsf(x[7]));
 #pragma unroll
   for (int o = 1; o < kStateBlock / 8; o <<= 1) top = max_nan(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
   const bool fine = top <= FLT_MAX;
@@ -142,9 +162,9 @@ __device__ __forceinline__ uint2 codes_of(const float (&x)[8], const uint32_t (&
     for (int o = 1; o < kStateBlock / 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(half, top, o));
   }
   scale = fmaxf(top * (1.0f / kE4m3Max), kScaleMin);
-  const float inv = __fdividef(1.0f, scale);
+  const float inv = reciprocal_fast(scale);
   float y[8];
-  if (fine && (!(NOISE || ROOT) || low >= scale * (NOISE ? 0.0157f : 0.002f))) {
+  if (fine && (!(NOISE || ROOT) || low_of(x) >= scale * (NOISE ? 0.0157f : 0.002f))) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       y[e] = x[e] * inv;
@@ -189,7 +209,7 @@ struct Rates {
 };
 
 template <int K, int PK, int GK, bool EIGHT, bool NOISE>
-__global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_constant__ AdamArgs<K> a) {
+__global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_constant__ AdamArgs<K> a) {
   constexpr int kTurns = turns_of(EIGHT);
   __shared__ Rates shared_rates;
   ptx::griddep_launch_dependents();
@@ -269,10 +289,15 @@ __global__ void __launch_bounds__(kAdamThreads) adamw_kernel(const __grid_consta
       m[e] = fmaf(s.b1, m[e], g[e] * r.one_b1);
       v[e] = fmaf(y, y, s.b2 * v[e]);
       root[e] = sqrt_fast(v[e]);
-      p[e] = fmaf(-r.keep, p[e], p[e]);
-      p[e] = fmaf(-r.rate, __fdividef(m[e], fmaf(root[e], r.inv_root, s.eps)), p[e]);
       noise[e] = NOISE ? mix(r.key + static_cast<uint32_t>(i) * 0x9E3779B1u + e * 0x9E3779B1u) : 0u;
     }
+    if (low_of(v) < FLT_MIN) {               // (zeros among them)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) root[e] = sqrtf(v[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      p[e] = fmaf(-r.rate, m[e] * reciprocal_fast(fmaf(root[e], r.inv_root, s.eps)), fmaf(-r.keep, p[e], p[e]));
     if (i < n) {
       if (PK == MLPMOE_FP32 && t.copy != nullptr) put<MLPMOE_BF16>(t.copy, i, n, wide, p);
       if (NOISE && PK == MLPMOE_BF16) {

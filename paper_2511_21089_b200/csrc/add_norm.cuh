@@ -165,13 +165,14 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
 // to a row (no block barrier) where a row is 512 columns at most and there are many: 65536 x 512 60.6 us against 69.9,
 // while at 1200 rows both take 3.1.  Rows of more than 8192 columns that are not aligned spill up to 132 bytes a thread.  Two chunks to a thread for 8-bit output of longer rows, whose scales are half the
 // work: 16384 x 4096 111 us against 129 with one (bf16 output: 121 against 117, so it keeps one).
+// LayerNorm, with its second sum, takes two for every output: 16384 x 4096 to bf16 121 us against 139 (four: 129).
 template <bool LAYER, int XKIND, int RKIND, int OKIND, bool VEC>
 cudaError_t launch_shape(const NormArgs& a, cudaStream_t st) {
   const unsigned n = static_cast<unsigned>(a.n);
   if (a.d <= 512 && a.n > 4096) return launch_pdl(add_norm_kernel<LAYER, XKIND, RKIND, OKIND, VEC, 32, 2>, dim3((n + 7) / 8), dim3(256), 0, st, a);
   if (a.d <= 1024) return launch_pdl(add_norm_kernel<LAYER, XKIND, RKIND, OKIND, VEC, 128, 1>, dim3(n), dim3(128), 0, st, a);
   if (a.d <= 2048) return launch_pdl(add_norm_kernel<LAYER, XKIND, RKIND, OKIND, VEC, 256, 1>, dim3(n), dim3(256), 0, st, a);
-  if (a.d <= 4096 && OKIND == MLPMOE_E4M3 && a.n > 1024)
+  if (a.d <= 4096 && (LAYER || OKIND == MLPMOE_E4M3) && a.n > 1024)
     return launch_pdl(add_norm_kernel<LAYER, XKIND, RKIND, OKIND, VEC, 256, 2>, dim3(n), dim3(256), 0, st, a);
   if (a.d <= 4096) return launch_pdl(add_norm_kernel<LAYER, XKIND, RKIND, OKIND, VEC, 512, 1>, dim3(n), dim3(512), 0, st, a);
   if (a.d <= 8192) return launch_pdl(add_norm_kernel<LAYER, XKIND, RKIND, OKIND, VEC, 512, 2>, dim3(n), dim3(512), 0, st, a);

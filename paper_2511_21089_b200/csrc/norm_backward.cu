@@ -62,83 +62,76 @@ __device__ __forceinline__ void copy_quad(char* to, const char* from, int kind, 
   }
 }
 
-// Sums of V values over the threads of a row, the same bits in all of them: a warp (WARP), or the block's `warps` warps by way of
-// `red`, two sets used in turn, so that one barrier a call will do.
-template <bool WARP, int V>
-__device__ __forceinline__ void block_sums(float (&v)[V], float (*red)[32][4], int& turn, int warps) {
-  constexpr int L = lanes_of(V);
-  const int lane = threadIdx.x % 32;
-  float x = warp_sums<V>(v);
-  if (!WARP) {
-    float(*r)[4] = red[turn];
-    turn ^= 1;
-    if (lane % L == 0 && lane / L < V) r[threadIdx.x / 32][lane / L] = x;
-    __syncthreads();
-    x = 0.0f;
-    for (int i = lane % L; i < warps; i += L) x += r[i][lane / L];
-#pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) x += __shfl_xor_sync(0xFFFFFFFFu, x, o);
-  }
-#pragma unroll
-  for (int k = 0; k < V; ++k) v[k] = V == 1 ? x : __shfl_sync(0xFFFFFFFFu, x, k * L);
-}
-
 constexpr int kStages = 2;
 
-// A row to the block's threads (WARP: to each of its eight warps), two times four neighbouring columns a thread, whose sums over
+// A row to the block's T threads (T = 32: to each of its eight warps), Q times four neighbouring columns a thread, whose sums over
 // the block's rows stay in registers.  The next row is on its way to shared memory meanwhile; a thread reads only what it
-// copied itself, so that takes no barrier.  (The row ahead in registers, types told apart as it runs: 98 registers, 512 threads per SM, 258 us
-// at 16384 x 4096.)
-template <bool LAYER, bool WARP, bool WIDE, int SK, int VK>
-__global__ void __launch_bounds__(WARP ? 256 : 1024, WARP ? 4 : 1) norm_backward_kernel(const __grid_constant__ NormGradArgs a) {
+// copied itself, so that takes no barrier.  16384 x 4096, fp32 and bf16: 940 MB in
+// 149 us with the join (floor 146).  The row ahead in registers and types told apart as it runs: 258 (98 registers, 512 threads per SM); four
+// times four columns a thread: 159 (16 warps per SM).
+template <bool LAYER, int T, int Q, int CTAS, bool WIDE, int SK, int VK>
+__global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(const __grid_constant__ NormGradArgs a) {
+  constexpr bool WARP = T == 32;
+  constexpr int R = WARP ? 8 : 1, THREADS = WARP ? 256 : T, SB = bytes_of(SK), VB = bytes_of(VK);
   extern __shared__ char staged[];
-  __shared__ float red[2][32][4];
+  __shared__ float red[2][T / 32][4];
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
-  const int d = a.d, tid = WARP ? threadIdx.x % 32 : threadIdx.x, T = WARP ? 32 : blockDim.x;
-  const int dk_bytes = bytes_of(a.ds_kind), row_warps = blockDim.x / 32;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * (WARP ? 8 : 1);
-  int64_t t = static_cast<int64_t>(blockIdx.x) * (WARP ? 8 : 1) + (WARP ? threadIdx.x / 32 : 0);
-  const int cols[2] = {tid * 4, (tid + T) * 4};
-  // in shared memory: [stage][quad][thread] of s, then of dv, then of ds
-  constexpr int kSBytes = 4 * bytes_of(SK), kVBytes = 4 * bytes_of(VK);
-  const int threads = blockDim.x, v_at = kStages * 2 * kSBytes * threads, r_at = v_at + kStages * 2 * kVBytes * threads;
-  auto place = [&](int at, int bytes, int stage, int k) { return staged + at + ((stage * 2 + k) * threads + threadIdx.x) * bytes; };
-  auto fetch = [&](int64_t row, int stage) {
-    if (row < a.n) {
-      const char* ps = static_cast<const char*>(a.s) + row * a.s_stride * bytes_of(SK);
-      const char* pv = static_cast<const char*>(a.dv) + row * a.dv_stride * bytes_of(VK);
-      const char* pr = static_cast<const char*>(a.ds) + row * a.ds_stride * dk_bytes;
+  const int d = a.d, tid = WARP ? threadIdx.x % 32 : threadIdx.x, rb = bytes_of(a.ds_kind), xb = bytes_of(a.dx_kind);
+  const bool has_r = a.ds_kind != kNone, r32 = a.ds_kind == MLPMOE_FP32, x32 = a.dx_kind == MLPMOE_FP32;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * R, first = static_cast<int64_t>(blockIdx.x) * R + (WARP ? threadIdx.x / 32 : 0);
+  const int rows = first < a.n ? static_cast<int>((a.n - first + step - 1) / step) : 0;      // of this block or warp
+  const int col = tid * 4;                 // quad k: columns col + 4 T k ..
+  const char* ps = static_cast<const char*>(a.s) + (first * a.s_stride + col) * SB;
+  const char* pv = static_cast<const char*>(a.dv) + (first * a.dv_stride + col) * VB;
+  const char* pr = static_cast<const char*>(a.ds) + (first * a.ds_stride + col) * rb;
+  char* px = static_cast<char*>(a.dx) + (first * a.dx_stride + col) * xb;
+  const int64_t ds = step * a.s_stride * SB, dv = step * a.dv_stride * VB, dr = step * a.ds_stride * rb, dx = step * a.dx_stride * xb;
+  // in shared memory: [stage][quad][thread], 16 bytes of s, then 8 or 16 of dv, then room for 16 of ds
+  constexpr int S_AT = 0, V_AT = kStages * Q * THREADS * 4 * SB, R_AT = V_AT + kStages * Q * THREADS * 4 * VB;
+  char* const mine_s = staged + S_AT + threadIdx.x * 4 * SB;
+  char* const mine_v = staged + V_AT + threadIdx.x * 4 * VB;
+  char* const mine_r = staged + R_AT + threadIdx.x * 16;
+  auto fetch = [&](bool more, int stage) {      // the row at ps, pv, pr; then the one after it in turn
+    if (more) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (cols[k] >= d) continue;
-        copy_quad<WIDE>(place(0, kSBytes, stage, k), ps + cols[k] * bytes_of(SK), SK, d - cols[k]);
-        copy_quad<WIDE>(place(v_at, kVBytes, stage, k), pv + cols[k] * bytes_of(VK), VK, d - cols[k]);
-        if (a.ds_kind != kNone) copy_quad<WIDE>(place(r_at, 4 * dk_bytes, stage, k), pr + cols[k] * dk_bytes, a.ds_kind, d - cols[k]);
+      for (int k = 0; k < Q; ++k) {
+        const int c = 4 * T * k, left = d - col - c, at = stage * Q + k;
+        if (left <= 0) continue;
+        copy_quad<WIDE>(mine_s + at * (THREADS * 4 * SB), ps + c * SB, SK, left);
+        copy_quad<WIDE>(mine_v + at * (THREADS * 4 * VB), pv + c * VB, VK, left);
+        if (has_r) copy_quad<WIDE>(mine_r + at * (THREADS * 16), pr + c * rb, a.ds_kind, left);
       }
+      ps += ds;
+      pv += dv;
+      pr += dr;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  float gain[2][4], sum_g[2][4], sum_b[2][4];
+  float gain[Q][4], sum_g[Q][4], sum_b[LAYER ? Q : 1][4];
 #pragma unroll
-  for (int k = 0; k < 2; ++k)
+  for (int k = 0; k < Q; ++k)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      gain[k][e] = cols[k] + e < d ? (a.gain != nullptr ? a.gain[cols[k] + e] : 1.0f) : 0.0f;
-      sum_g[k][e] = sum_b[k][e] = 0.0f;
+      const int c = col + 4 * T * k + e;
+      gain[k][e] = c < d ? (a.gain != nullptr ? a.gain[c] : 1.0f) : 0.0f;
+      sum_g[k][e] = 0.0f;
+      if (LAYER) sum_b[k][e] = 0.0f;
     }
 #pragma unroll
-  for (int k = 0; k < kStages; ++k) fetch(t + k * step, k);
-  int turn = 0, stage = 0;
+  for (int k = 0; k < kStages; ++k) fetch(k < rows, k);
+  int turn = 0;
   const float inv_d = 1.0f / static_cast<float>(d);
-  for (; t < a.n; t += step) {
+  for (int i = 0; i < rows; ++i) {
+    const int stage = i % kStages;
     asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-    float z[2][4], v[2][4];
+    float z[Q][4], v[Q][4];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      if (cols[k] < d) {
-        quad_of<SK>(place(0, kSBytes, stage, k), z[k]);
-        quad_of<VK>(place(v_at, kVBytes, stage, k), v[k]);
+    for (int k = 0; k < Q; ++k) {
+      const int at = stage * Q + k;
+      if (col + 4 * T * k < d) {
+        quad_of<SK>(mine_s + at * (THREADS * 4 * SB), z[k]);
+        quad_of<VK>(mine_v + at * (THREADS * 4 * VB), v[k]);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[k][e] = v[k][e] = 0.0f;
@@ -146,89 +139,96 @@ __global__ void __launch_bounds__(WARP ? 256 : 1024, WARP ? 4 : 1) norm_backward
     }
     float mean_h = 0.0f, ss, hz;
     if (LAYER) {
-      float sum[1] = {(z[0][0] + z[0][1]) + (z[0][2] + z[0][3]) + ((z[1][0] + z[1][1]) + (z[1][2] + z[1][3]))};
-      block_sums<WARP, 1>(sum, red, turn, row_warps);
+      float sum[1] = {0.0f};
+#pragma unroll
+      for (int k = 0; k < Q; ++k) sum[0] += (z[k][0] + z[k][1]) + (z[k][2] + z[k][3]);
+      row_sums<T, 1>(sum, red, turn);
       const float mean = sum[0] * inv_d;
       float q[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < Q; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          z[k][e] = cols[k] + (WIDE ? 0 : e) < d ? z[k][e] - mean : 0.0f;
+          z[k][e] = col + 4 * T * k + (WIDE ? 0 : e) < d ? z[k][e] - mean : 0.0f;
           const float h = gain[k][e] * v[k][e];
           q[0] = fmaf(z[k][e], z[k][e], q[0]);
           q[1] = fmaf(h, z[k][e], q[1]);
           q[2] += h;
         }
-      block_sums<WARP, 3>(q, red, turn, row_warps);
+      row_sums<T, 3>(q, red, turn);
       ss = q[0];
       hz = q[1];
       mean_h = q[2] * inv_d;
     } else {
       float q[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < Q; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           q[0] = fmaf(z[k][e], z[k][e], q[0]);
           q[1] = fmaf(gain[k][e] * v[k][e], z[k][e], q[1]);
         }
-      block_sums<WARP, 2>(q, red, turn, row_warps);
+      row_sums<T, 2>(q, red, turn);
       ss = q[0];
       hz = q[1];
     }
     const float inv = rsqrtf(ss * inv_d + a.eps);
     const float along = hz * inv * inv * inv_d;
-    char* px = static_cast<char*>(a.dx) + t * a.dx_stride * bytes_of(a.dx_kind);
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      if (cols[k] >= d) continue;
+    for (int k = 0; k < Q; ++k) {
+      const int c = 4 * T * k, left = d - col - c, at = stage * Q + k;
+      if (left <= 0) continue;
       float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (a.ds_kind == MLPMOE_FP32) quad_of<MLPMOE_FP32>(place(r_at, 16, stage, k), r);
-      if (a.ds_kind == MLPMOE_BF16) quad_of<MLPMOE_BF16>(place(r_at, 8, stage, k), r);
+      if (has_r) {
+        if (r32) {
+          quad_of<MLPMOE_FP32>(mine_r + at * (THREADS * 16), r);
+        } else {
+          quad_of<MLPMOE_BF16>(mine_r + at * (THREADS * 16), r);
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         sum_g[k][e] = fmaf(v[k][e], z[k][e] * inv, sum_g[k][e]);
         if (LAYER) sum_b[k][e] += v[k][e];
         r[e] = fmaf(inv, fmaf(-z[k][e], along, fmaf(gain[k][e], v[k][e], -mean_h)), r[e]);
       }
-      if (a.dx_kind == MLPMOE_FP32) {
-        float* p = reinterpret_cast<float*>(px) + cols[k];
+      if (x32) {
+        float* p = reinterpret_cast<float*>(px) + c;
         if (WIDE) {
           __stcs(reinterpret_cast<float4*>(p), make_float4(r[0], r[1], r[2], r[3]));
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (cols[k] + e < d) p[e] = r[e];
+            if (e < left) p[e] = r[e];
         }
       } else {
-        __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(px) + cols[k];
+        __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(px) + c;
         if (WIDE) {
           *reinterpret_cast<uint2*>(p) = make_uint2(pack2(r[0], r[1]), pack2(r[2], r[3]));
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (cols[k] + e < d) p[e] = __float2bfloat16_rn(r[e]);
+            if (e < left) p[e] = __float2bfloat16_rn(r[e]);
         }
       }
     }
-    fetch(t + kStages * step, stage);
-    stage ^= 1;
+    px += dx;
+    fetch(i + kStages < rows, stage);
   }
   if (a.dgain == nullptr && a.dbias == nullptr) return;
   // the block's sums: to the result where it is the only block
   float* out[2] = {gridDim.x == 1 ? a.dgain : a.partial + static_cast<int64_t>(blockIdx.x) * 2 * d,
                    gridDim.x == 1 ? a.dbias : a.partial + (static_cast<int64_t>(blockIdx.x) * 2 + 1) * d};
   asm volatile("cp.async.wait_group 0;" ::: "memory");
-  float* join = reinterpret_cast<float*>(staged);      // WARP: the eight rows' sums first
+  float* join = reinterpret_cast<float*>(staged);      // T = 32: the eight rows' sums first
 #pragma unroll
   for (int which = 0; which < (LAYER ? 2 : 1); ++which) {
     if (WARP) {
       __syncthreads();
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < Q; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) join[(threadIdx.x / 32) * 256 + cols[k] + e] = which == 0 ? sum_g[k][e] : sum_b[k][e];
+        for (int e = 0; e < 4; ++e) join[(threadIdx.x / 32) * 256 + col + 4 * T * k + e] = which == 0 ? sum_g[k][e] : sum_b[LAYER ? k : 0][e];
       __syncthreads();
       if (static_cast<int>(threadIdx.x) < d && out[which] != nullptr) {
         float sum = join[threadIdx.x];
@@ -238,10 +238,12 @@ __global__ void __launch_bounds__(WARP ? 256 : 1024, WARP ? 4 : 1) norm_backward
       }
     } else if (out[which] != nullptr) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < Q; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (cols[k] + e < d) out[which][cols[k] + e] = which == 0 ? sum_g[k][e] : sum_b[k][e];
+        for (int e = 0; e < 4; ++e) {
+          const int c = col + 4 * T * k + e;
+          if (c < d) out[which][c] = which == 0 ? sum_g[k][e] : sum_b[LAYER ? k : 0][e];
+        }
     }
   }
 }
@@ -357,38 +359,50 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const __grid_constant__
   }
 }
 
-// Threads and blocks of a call: eight columns a thread, 1024 threads an SM (64 registers each, and two stages of up to 12 bytes a column in
-// shared memory), and four rows or more to a block where every SM has one, so that few sums are left to join.
-int threads_of(int64_t d) { return d <= 256 ? 256 : static_cast<int>((d + 255) / 256 * 32); }
+// Threads of a row and blocks per SM by the row's length.  A block has four rows or more where every SM has a block, so that few sums are
+// left to join.
+struct Shape {
+  int threads, quads, ctas;
+};
+constexpr Shape kShapes[] = {{32, 2, 4}, {128, 2, 8}, {256, 2, 4}, {512, 2, 2}, {1024, 2, 1}};
+int shape_of(int64_t d) { return d <= 256 ? 0 : (d <= 1024 ? 1 : (d <= 2048 ? 2 : (d <= 4096 ? 3 : 4))); }
 int blocks_of(int64_t n, int64_t d) {
-  const int64_t need = d <= 256 ? (n + 7) / 8 : n, most = static_cast<int64_t>(kSms) * (1024 / threads_of(d));
+  const int64_t need = d <= 256 ? (n + 7) / 8 : n, most = static_cast<int64_t>(kSms) * kShapes[shape_of(d)].ctas;
   const int64_t few = (need + 3) / 4 > kSms ? (need + 3) / 4 : kSms;
   const int64_t blocks = need < few ? need : few;
   return static_cast<int>(blocks < most ? blocks : most);
 }
 
-template <bool LAYER, bool WARP, bool WIDE, int SK, int VK>
+template <bool LAYER, bool WIDE, int SHAPE, int SK, int VK>
 cudaError_t launch_kinds(const NormGradArgs& a, cudaStream_t st) {
-  auto kernel = norm_backward_kernel<LAYER, WARP, WIDE, SK, VK>;
-  const int threads = threads_of(a.d), most = kStages * 8 * (bytes_of(SK) + bytes_of(VK) + 4);
-  // the limit is the same for every call, whatever its own size
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most * (WARP ? 256 : 1024));
-  if (e != cudaSuccess) return e;
-  const int bytes = kStages * 8 * threads * (bytes_of(SK) + bytes_of(VK) + (a.ds_kind == kNone ? 0 : bytes_of(a.ds_kind)));
-  return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks_of(a.n, a.d))), dim3(static_cast<unsigned>(threads)), static_cast<size_t>(bytes), st, a);
+  constexpr Shape s = kShapes[SHAPE];
+  constexpr int threads = s.threads == 32 ? 256 : s.threads, held = kStages * 4 * s.quads * threads * (bytes_of(SK) + bytes_of(VK));
+  constexpr int most = held + kStages * 16 * s.quads * threads;
+  auto kernel = norm_backward_kernel<LAYER, s.threads, s.quads, s.ctas, WIDE, SK, VK>;
+  if (most > 47 * 1024) {      // above what a kernel has anyway; the limit is the same for every call, whatever its own size
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks_of(a.n, a.d))), dim3(threads), static_cast<size_t>(a.ds_kind == kNone ? held : most), st, a);
 }
-template <bool LAYER, bool WARP, bool WIDE>
+template <bool LAYER, bool WIDE, int SHAPE>
 cudaError_t launch_from(const NormGradArgs& a, cudaStream_t st) {
   if (a.s_kind == MLPMOE_FP32)
-    return a.dv_kind == MLPMOE_FP32 ? launch_kinds<LAYER, WARP, WIDE, MLPMOE_FP32, MLPMOE_FP32>(a, st)
-                                    : launch_kinds<LAYER, WARP, WIDE, MLPMOE_FP32, MLPMOE_BF16>(a, st);
-  return a.dv_kind == MLPMOE_FP32 ? launch_kinds<LAYER, WARP, WIDE, MLPMOE_BF16, MLPMOE_FP32>(a, st)
-                                  : launch_kinds<LAYER, WARP, WIDE, MLPMOE_BF16, MLPMOE_BF16>(a, st);
+    return a.dv_kind == MLPMOE_FP32 ? launch_kinds<LAYER, WIDE, SHAPE, MLPMOE_FP32, MLPMOE_FP32>(a, st)
+                                    : launch_kinds<LAYER, WIDE, SHAPE, MLPMOE_FP32, MLPMOE_BF16>(a, st);
+  return a.dv_kind == MLPMOE_FP32 ? launch_kinds<LAYER, WIDE, SHAPE, MLPMOE_BF16, MLPMOE_FP32>(a, st)
+                                  : launch_kinds<LAYER, WIDE, SHAPE, MLPMOE_BF16, MLPMOE_BF16>(a, st);
 }
 template <bool LAYER, bool WIDE>
 cudaError_t launch_rows(const NormGradArgs& a, cudaStream_t st) {
   if (a.d > kOnePassD) return launch_pdl(norm_backward_long_kernel<LAYER, WIDE>, dim3(static_cast<unsigned>(a.n)), dim3(1024), 0, st, a);
-  return a.d <= 256 ? launch_from<LAYER, true, WIDE>(a, st) : launch_from<LAYER, false, WIDE>(a, st);
+  switch (shape_of(a.d)) {
+    case 0: return launch_from<LAYER, WIDE, 0>(a, st);
+    case 1: return launch_from<LAYER, WIDE, 1>(a, st);
+    case 2: return launch_from<LAYER, WIDE, 2>(a, st);
+    case 3: return launch_from<LAYER, WIDE, 3>(a, st);
+    default: return launch_from<LAYER, WIDE, 4>(a, st);
+  }
 }
 
 int64_t stats_bytes(int64_t n, int64_t d) { return d > kOnePassD ? (n * 8 + 15) / 16 * 16 : 0; }
