@@ -21,9 +21,10 @@ namespace mlpmoe {
 namespace {
 
 constexpr int kAdamThreads = 256;
-// Chunks of eight elements a thread: all of a block's loads are issued before its first use (two chunks: 36 registers of 8-bit states; one: 32 of fp32 ones).
-__host__ __device__ constexpr int turns_of(bool eight) { return eight ? 2 : 1; }
-__host__ __device__ constexpr int block_of(bool eight) { return kAdamThreads * 8 * turns_of(eight); }      // elements of a block
+constexpr int kAdamStep = kAdamThreads * 8;      // elements of a block's step
+constexpr int kAdamSteps = 16;                   // steps of a block at most
+constexpr int kSms = 148;
+constexpr int kAdamCtas = 3;                     // blocks of an SM
 constexpr int kStateBlock = 128;                               // elements of a scale
 constexpr float kE4m3Max = 448.0f;
 constexpr float kScaleMin = 1.17549435e-38f;                   // 2^-126
@@ -56,7 +57,7 @@ struct AdamSettings {
 template <int K>
 struct AdamArgs {
   AdamSettings s;
-  int count;
+  int count, steps;      // steps: of a block
   AdamTensor t[K];
 };
 
@@ -69,29 +70,35 @@ __host__ __device__ __forceinline__ uint32_t mix(uint32_t h) {
   return h ^ (h >> 16);
 }
 
-// Eight elements from i on, as they stand in memory, zeros past the end.
+// Eight elements at p, as they stand in memory; `left` of them exist (zeros for the rest), `whole`: all eight, and p is on 16 bytes.
 template <int KIND>
-__device__ __forceinline__ Chunk fetch(const void* base, int64_t i, int64_t n, bool wide) {
-  const char* p = static_cast<const char*>(base) + i * bytes_of(KIND);
-  if (wide && i + 8 <= n) return load_chunk<true>(p, KIND, 0, 8);
-  return load_chunk<false>(p, KIND, 0, i >= n ? 0 : static_cast<int>(n - i < 8 ? n - i : 8));
+__device__ __forceinline__ Chunk fetch(const char* p, bool whole, int left) {
+  if (whole) return load_chunk<true>(p, KIND, 0, 8);
+  return load_chunk<false>(p, KIND, 0, left);
 }
-__device__ __forceinline__ uint2 fetch_codes(const void* base, int64_t i, int64_t n, bool wide) {
-  const uint8_t* p = static_cast<const uint8_t*>(base) + i;
-  if (wide && i + 8 <= n) return *reinterpret_cast<const uint2*>(p);
+__device__ __forceinline__ uint2 fetch_codes(const char* p, bool whole, int left) {
+  if (whole) return *reinterpret_cast<const uint2*>(p);
   uint32_t w[2] = {0u, 0u};
 #pragma unroll
   for (int e = 0; e < 8; ++e)
-    if (i + e < n) w[e / 4] |= static_cast<uint32_t>(p[e]) << (8 * (e % 4));
+    if (e < left) w[e / 4] |= static_cast<uint32_t>(static_cast<uint8_t>(p[e])) << (8 * (e % 4));
   return make_uint2(w[0], w[1]);
 }
 template <int KIND>
-__device__ __forceinline__ void put(void* base, int64_t i, int64_t n, bool wide, const float (&v)[8]) {
-  char* p = static_cast<char*>(base) + i * bytes_of(KIND);
-  if (wide && i + 8 <= n) {
+__device__ __forceinline__ void put(char* p, bool whole, int left, const float (&v)[8]) {
+  if (whole) {
     store8<true>(p, KIND, 0, 8, v);
   } else {
-    store8<false>(p, KIND, 0, static_cast<int>(n - i < 8 ? n - i : 8), v);
+    store8<false>(p, KIND, 0, left, v);
+  }
+}
+__device__ __forceinline__ void put_codes(char* p, bool whole, int left, uint2 c) {
+  if (whole) {
+    *reinterpret_cast<uint2*>(p) = c;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p[e] = static_cast<char>((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
   }
 }
 
@@ -191,26 +198,22 @@ __device__ __forceinline__ uint2 codes_of(const float (&x)[8], const uint32_t (&
   for (int e = 0; e < 4; ++e) c[e] = __nv_cvt_float2_to_fp8x2(make_float2(y[2 * e], y[2 * e + 1]), __NV_SATFINITE, __NV_E4M3);
   return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
 }
-__device__ __forceinline__ void put_codes(void* base, float* scales, int64_t i, int64_t n, bool wide, uint2 c, float scale) {
-  if (i % kStateBlock == 0) scales[i / kStateBlock] = scale;
-  uint8_t* p = static_cast<uint8_t*>(base) + i;
-  if (wide && i + 8 <= n) {
-    *reinterpret_cast<uint2*>(p) = c;
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (i + e < n) p[e] = static_cast<uint8_t>((e < 4 ? c.x : c.y) >> (8 * (e & 3)));
-  }
-}
-
 struct Rates {
   float keep, rate, inv_root, one_b1, root_b2;     // lr wd; lr / (1 - b1^i); 1 / sqrt(1 - b2^i); (1 - b1) gs; sqrt(1 - b2) gs
   uint32_t key;
 };
 
+// A thread's elements of one step, as they stand in memory.
+template <bool EIGHT>
+struct Raw {
+  Chunk p, g, m, v;
+  uint2 m8, v8;
+  float m_scale, v_scale;
+};
+
+// A block to a stretch of one tensor, 2048 elements a step; the next step's loads are under way while one is computed.
 template <int K, int PK, int GK, bool EIGHT, bool NOISE>
-__global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_constant__ AdamArgs<K> a) {
-  constexpr int kTurns = turns_of(EIGHT);
+__global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __grid_constant__ AdamArgs<K> a) {
   __shared__ Rates shared_rates;
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
@@ -225,26 +228,39 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_con
   }
   const AdamTensor& t = a.t[lo];
   const AdamSettings& s = a.s;
+  const int64_t start = static_cast<int64_t>(blockIdx.x - t.first) * a.steps * kAdamStep, first = start + threadIdx.x * 8;
+  const int64_t rest = t.n - start;
+  const int count = static_cast<int>(rest < static_cast<int64_t>(a.steps) * kAdamStep ? rest : static_cast<int64_t>(a.steps) * kAdamStep);
   const bool wide = t.wide != 0;
-  const int64_t n = t.n, start = static_cast<int64_t>(blockIdx.x - t.first) * block_of(EIGHT);
-  Chunk cp[kTurns], cg[kTurns], cm[kTurns], cv[kTurns];
-  uint2 em[kTurns], ev[kTurns];
-  float ms[kTurns], vs[kTurns];
-#pragma unroll
-  for (int turn = 0; turn < kTurns; ++turn) {
-    const int64_t i = start + (turn * kAdamThreads + threadIdx.x) * 8;
-    cp[turn] = fetch<PK>(t.p, i, n, wide);
-    cg[turn] = fetch<GK>(t.g, i, n, wide);
+  constexpr int PB = bytes_of(PK), GB = bytes_of(GK), SB = EIGHT ? 1 : 4;
+  char* const p_at = static_cast<char*>(t.p) + first * PB;
+  const char* const g_at = static_cast<const char*>(t.g) + first * GB;
+  char* const m_at = static_cast<char*>(t.m) + first * SB;
+  char* const v_at = static_cast<char*>(t.v) + first * SB;
+  char* const copy_at = reinterpret_cast<char*>(t.copy + first);
+  float* const ms_at = t.m_scale + first / kStateBlock;
+  float* const vs_at = t.v_scale + first / kStateBlock;
+  const bool copies = PK == MLPMOE_FP32 && t.copy != nullptr;
+  const int mine = threadIdx.x * 8;
+  // at: of the step; whole: the step is full and its buffers are on 16 bytes
+  auto load = [&](int at, Raw<EIGHT>& r) {
+    const bool whole = wide && at + kAdamStep <= count;
+    const int left = min(8, count - at - mine);
+    if (!whole && left <= 0) return;
+    r.p = fetch<PK>(p_at + at * PB, whole, left);
+    r.g = fetch<GK>(g_at + at * GB, whole, left);
     if (EIGHT) {
-      em[turn] = fetch_codes(t.m, i, n, wide);
-      ev[turn] = fetch_codes(t.v, i, n, wide);
-      ms[turn] = i < n ? t.m_scale[i / kStateBlock] : 0.0f;
-      vs[turn] = i < n ? t.v_scale[i / kStateBlock] : 0.0f;
+      r.m8 = fetch_codes(m_at + at, whole, left);
+      r.v8 = fetch_codes(v_at + at, whole, left);
+      r.m_scale = ms_at[at / kStateBlock];
+      r.v_scale = vs_at[at / kStateBlock];
     } else {
-      cm[turn] = fetch<MLPMOE_FP32>(t.m, i, n, wide);
-      cv[turn] = fetch<MLPMOE_FP32>(t.v, i, n, wide);
+      r.m = fetch<MLPMOE_FP32>(m_at + at * 4, whole, left);
+      r.v = fetch<MLPMOE_FP32>(v_at + at * 4, whole, left);
     }
-  }
+  };
+  Raw<EIGHT> next = {};
+  load(0, next);
   if (threadIdx.x == 0) {                  // while the loads are under way
     int64_t step = s.step_device != nullptr ? *s.step_device : s.step;
     if (step < 1) step = 1;
@@ -257,39 +273,39 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_con
     r.one_b1 = s.one_b1 * gs;
     r.root_b2 = s.root_b2 * gs;
     r.key = mix(t.index ^ mix(s.key ^ static_cast<uint32_t>(step)));
-    if (start >> 32) r.key = mix(r.key ^ static_cast<uint32_t>(start >> 32));
     shared_rates = r;
   }
   __syncthreads();
   const Rates r = shared_rates;
-#pragma unroll
-  for (int turn = 0; turn < kTurns; ++turn) {
-    const int64_t i = start + (turn * kAdamThreads + threadIdx.x) * 8;
+#pragma unroll 1
+  for (int at = 0; at < count; at += kAdamStep) {
+    const Raw<EIGHT> now = next;
+    if (at + kAdamStep < count) load(at + kAdamStep, next);
+    const bool whole = wide && at + kAdamStep <= count;
+    const int left = min(8, count - at - mine);
     float p[8], g[8], m[8], v[8];
-    to_f32(cp[turn], PK, p);
-    to_f32(cg[turn], GK, g);
+    to_f32(now.p, PK, p);
+    to_f32(now.g, GK, g);
     if (EIGHT) {
-      values_of(em[turn], m);
-      values_of(ev[turn], v);
+      values_of(now.m8, m);
+      values_of(now.v8, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        m[e] *= ms[turn];
-        v[e] *= vs[turn];
+        m[e] *= now.m_scale;
+        v[e] *= now.v_scale;
         v[e] *= v[e];
       }
     } else {
-      to_f32(cm[turn], MLPMOE_FP32, m);
-      to_f32(cv[turn], MLPMOE_FP32, v);
+      to_f32(now.m, MLPMOE_FP32, m);
+      to_f32(now.v, MLPMOE_FP32, v);
     }
     float root[8];
-    uint32_t noise[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const float y = g[e] * r.root_b2;
       m[e] = fmaf(s.b1, m[e], g[e] * r.one_b1);
       v[e] = fmaf(y, y, s.b2 * v[e]);
       root[e] = sqrt_fast(v[e]);
-      noise[e] = NOISE ? mix(r.key + static_cast<uint32_t>(i) * 0x9E3779B1u + e * 0x9E3779B1u) : 0u;
     }
     if (low_of(v) < FLT_MIN) {               // (zeros among them)
 #pragma unroll
@@ -298,25 +314,42 @@ __global__ void __launch_bounds__(kAdamThreads, 4) adamw_kernel(const __grid_con
 #pragma unroll
     for (int e = 0; e < 8; ++e)
       p[e] = fmaf(-r.rate, m[e] * reciprocal_fast(fmaf(root[e], r.inv_root, s.eps)), fmaf(-r.keep, p[e], p[e]));
-    if (i < n) {
-      if (PK == MLPMOE_FP32 && t.copy != nullptr) put<MLPMOE_BF16>(t.copy, i, n, wide, p);
+    uint32_t noise[8];
+    if (NOISE) {
+      const int64_t i = first + at;
+      uint32_t key = r.key;
+      if (i >> 32) key = mix(key ^ static_cast<uint32_t>(i >> 32));      // (2048 elements of a step lie in the same 2^32)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) noise[e] = mix(key + static_cast<uint32_t>(i) * 0x9E3779B1u + e * 0x9E3779B1u);
+    }
+    if (whole || left > 0) {
+      if (copies) put<MLPMOE_BF16>(copy_at + at * 2, whole, left, p);
       if (NOISE && PK == MLPMOE_BF16) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (finite(p[e])) p[e] = __uint_as_float((__float_as_uint(p[e]) + (mix(noise[e] ^ 0x9E3779B1u) & 0xFFFFu)) & 0xFFFF0000u);
       }
-      put<PK>(t.p, i, n, wide, p);
+      put<PK>(p_at + at * PB, whole, left, p);
       if (!EIGHT) {
-        put<MLPMOE_FP32>(t.m, i, n, wide, m);
-        put<MLPMOE_FP32>(t.v, i, n, wide, v);
+        put<MLPMOE_FP32>(m_at + at * 4, whole, left, m);
+        put<MLPMOE_FP32>(v_at + at * 4, whole, left, v);
       }
     }
     if (EIGHT) {
+      if (!whole) {                        // what lies behind the end must not reach the last block's scales
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e >= left) m[e] = root[e] = 0.0f;
+      }
       float scale_m, scale_v;
       const uint2 code_m = codes_of<NOISE, false>(m, noise, scale_m), code_v = codes_of<NOISE, true>(root, noise, scale_v);
-      if (i < n) {
-        put_codes(t.m, t.m_scale, i, n, wide, code_m, scale_m);
-        put_codes(t.v, t.v_scale, i, n, wide, code_v, scale_v);
+      if (whole || left > 0) {
+        if (threadIdx.x % (kStateBlock / 8) == 0) {
+          ms_at[at / kStateBlock] = scale_m;
+          vs_at[at / kStateBlock] = scale_v;
+        }
+        put_codes(m_at + at, whole, left, code_m);
+        put_codes(v_at + at, whole, left, code_v);
       }
     }
   }
@@ -346,11 +379,17 @@ cudaError_t launch_adamw(const AdamSettings& s, const AdamTensor* t, int count, 
   AdamArgs<K> a;
   a.s = s;
   a.count = count;
+  // steps of a block: as many as leave every SM its blocks twice over
+  int64_t total = 0;
+  for (int i = 0; i < count; ++i) total += (t[i].n + kAdamStep - 1) / kAdamStep;
+  const int64_t most = total / (2 * kAdamCtas * kSms);
+  a.steps = most < 1 ? 1 : (most > kAdamSteps ? kAdamSteps : static_cast<int>(most));
+  const int64_t per = static_cast<int64_t>(a.steps) * kAdamStep;
   uint64_t blocks = 0;
   for (int i = 0; i < count; ++i) {
     a.t[i] = t[i];
     a.t[i].first = static_cast<uint32_t>(blocks);
-    blocks += (t[i].n + block_of(k.eight) - 1) / block_of(k.eight);
+    blocks += (t[i].n + per - 1) / per;
   }
   const unsigned grid = static_cast<unsigned>(blocks);
   if (k.p16)
@@ -422,7 +461,7 @@ extern "C" mlpmoe_status_t mlpmoe_adamw(const mlpmoe_adamw_tensor_t* tensors, in
     for (int32_t i = 0; i < n_tensors; ++i) {
       const mlpmoe_adamw_tensor_t& t = tensors[i];
       if (t.n == 0 || (t.param_dtype == MLPMOE_BF16) != k.p16 || (t.grad_dtype == MLPMOE_BF16) != k.g16 || (t.state_dtype == MLPMOE_E4M3) != k.eight) continue;
-      const int64_t need = (t.n + block_of(k.eight) - 1) / block_of(k.eight);
+      const int64_t need = (t.n + kAdamStep - 1) / kAdamStep;      // blocks at most
       if ((count == kAdamMany || blocks + need > INT32_MAX) && flush() != cudaSuccess) return MLPMOE_ERR_CUDA;
       AdamTensor& r = batch[count++];
       blocks += need;
