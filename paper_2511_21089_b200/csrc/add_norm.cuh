@@ -44,14 +44,26 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
   const char* xrow = static_cast<const char*>(a.x) + t * a.x_stride * kXBytes;
   const char* rrow = static_cast<const char*>(a.r) + t * a.r_stride * (RKIND == MLPMOE_FP32 ? 4 : 2);
   const int d = a.d;
+  // LayerNorm on rows that take no wide loads: neighbouring columns to neighbouring threads (8-bit scales need them in one thread)
+  constexpr bool SPREAD = LAYER && !VEC && OKIND != MLPMOE_E4M3;
+  auto load = [&](const void* row, int kind, int i) {
+    return SPREAD ? load_columns<false, T>(row, kind, i, tid, d) : load_chunk<VEC>(row, kind, (i * T + tid) * 8, d);
+  };
+  auto store = [&](void* row, int kind, int i, const float (&v)[8]) {
+    if (SPREAD) {
+      store_columns<false, T>(row, kind, i, tid, d, v);
+    } else if ((i * T + tid) * 8 < d) {
+      store8<VEC>(row, kind, (i * T + tid) * 8, d, v);
+    }
+  };
   float s[NCH][8];
   {
     Chunk x[NCH], r[NCH];               // all of the row's loads before the first use
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) x[i] = load_chunk<VEC>(xrow, XKIND, (i * T + tid) * 8, d);
+    for (int i = 0; i < NCH; ++i) x[i] = load(xrow, XKIND, i);
     if (RKIND != kNone) {
 #pragma unroll
-      for (int i = 0; i < NCH; ++i) r[i] = load_chunk<VEC>(rrow, RKIND, (i * T + tid) * 8, d);
+      for (int i = 0; i < NCH; ++i) r[i] = load(rrow, RKIND, i);
     }
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
@@ -72,10 +84,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
   if (a.x_out != nullptr) {
     char* xo = static_cast<char*>(a.x_out) + t * a.x_out_stride * kXBytes;
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) {
-      const int col = (i * T + tid) * 8;
-      if (col < d) store8<VEC>(xo, XKIND, col, d, s[i]);
-    }
+    for (int i = 0; i < NCH; ++i) store(xo, XKIND, i, s[i]);
   }
   if (LAYER) {                               // the mean first, then the squares of what is left: no cancellation
     int turn = 0;
@@ -87,7 +96,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
     for (int i = 0; i < NCH; ++i)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        s[i][j] = (VEC ? (i * T + tid) * 8 : (i * T + tid) * 8 + j) < d ? s[i][j] - mean : 0.0f;
+        s[i][j] = (SPREAD ? column<false, T>(i, tid, j) : (i * T + tid) * 8 + (VEC ? 0 : j)) < d ? s[i][j] - mean : 0.0f;
         ss += s[i][j] * s[i][j];
       }
     sum[0] = ss;
@@ -100,17 +109,16 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
   float row_max = 0.0f;
 #pragma unroll
   for (int i = 0; i < NCH; ++i) {
-    const int col = (i * T + tid) * 8;
     float g[8];
     if (a.gain != nullptr) {
-      to_f32(load_chunk<VEC>(a.gain, MLPMOE_FP32, col, d), MLPMOE_FP32, g);
+      to_f32(load(a.gain, MLPMOE_FP32, i), MLPMOE_FP32, g);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) g[j] = 1.0f;
     }
     float c[8];
     if (LAYER && a.bias != nullptr) {
-      to_f32(load_chunk<VEC>(a.bias, MLPMOE_FP32, col, d), MLPMOE_FP32, c);
+      to_f32(load(a.bias, MLPMOE_FP32, i), MLPMOE_FP32, c);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) c[j] = 0.0f;
@@ -155,10 +163,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
     }
   }
 #pragma unroll
-  for (int i = 0; i < NCH; ++i) {
-    const int col = (i * T + tid) * 8;
-    if (col < d) store8<VEC>(orow, OKIND, col, d, s[i]);
-  }
+  for (int i = 0; i < NCH; ++i) store(orow, OKIND, i, s[i]);
 }
 
 // A row to a block whose threads take eight columns each: all loads of a row are in flight at once and none is idle long.  A warp

@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(kMoveThreads) combine_kernel(const __grid_cons
   const int64_t u = static_cast<int64_t>(blockIdx.x) * (kMoveThreads / 32) + threadIdx.x / 32;
   const int64_t t = u / a.parts;
   if (t >= a.n) return;
-  const int c0 = static_cast<int>(u - t * a.parts) * (256 * NC) + lane * 8;
+  const int part = static_cast<int>(u - t * a.parts) * NC;      // its first 256 columns
   float acc[NC][8];
 #pragma unroll
   for (int i = 0; i < NC; ++i)
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(kMoveThreads) combine_kernel(const __grid_cons
   if (SK != kNone) {
     const char* p = static_cast<const char*>(a.residual) + t * a.residual_stride * bytes_of(SK);
 #pragma unroll
-    for (int i = 0; i < NC; ++i) res[i] = load_chunk<VEC>(p, SK, c0 + 256 * i, a.d);
+    for (int i = 0; i < NC; ++i) res[i] = load_columns<VEC, 32>(p, SK, part + i, lane, a.d);
   }
   for (int j0 = 0; j0 < a.slots; j0 += 32) {
     int32_t mine = j0 + lane < a.slots ? a.token_row[t * a.slots + j0 + lane] : -1;
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kMoveThreads) combine_kernel(const __grid_cons
         w[k] = __shfl_sync(0xFFFFFFFFu, w_mine, src);
         const char* p = static_cast<const char*>(a.rows) + r * a.rows_stride * bytes_of(RK);
 #pragma unroll
-        for (int i = 0; i < NC; ++i) v[k][i] = load_chunk<VEC>(p, RK, live != 0 ? c0 + 256 * i : a.d, a.d);
+        for (int i = 0; i < NC; ++i) v[k][i] = load_columns<VEC, 32>(p, RK, part + i, lane, live != 0 ? a.d : 0);
         if (live == 0) w[k] = 0.0f;
         live &= live - 1;
       }
@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(kMoveThreads) combine_kernel(const __grid_cons
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[i][e] += f[e];
     }
-    if (c0 + 256 * i < a.d) store8<VEC>(y, YK, c0 + 256 * i, a.d, acc[i]);
+    store_columns<VEC, 32>(y, YK, part + i, lane, a.d, acc[i]);
   }
 }
 
@@ -470,7 +470,7 @@ struct CombineGradArgs {
 // product with it and receives w * grad_y.  A row is read before it is written, by the same thread, so both may be one buffer.
 template <int GK, int RK, bool VEC, int T, int NCH>
 __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 32 ? 8 : (T < 1024 ? 1024 / T : 1)) combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
-  constexpr int kGradRows = NCH == 4 ? 1 : 4;       // rows of a token under way at a time: as many as there are registers for
+  constexpr int kGradRows = NCH == 4 ? 1 : (NCH == 2 && !VEC ? 2 : 4);       // rows of a token under way at a time: as many as there are registers for
   __shared__ float red[T / 32][32];
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
@@ -483,7 +483,7 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 32 ? 8 : (T < 1024 ? 1
     if (r >= a.offsets[b + 1] || r >= a.n_rows || r < 0) return;
     char* p = static_cast<char*>(a.grad_rows) + r * a.grad_rows_stride * bytes_of(RK);
     const float zero[8] = {};
-    for (int c = lane * 8; c < a.d; c += 256) store8<VEC>(p, RK, c, a.d, zero);
+    for (int i = 0; i * 256 < a.d; ++i) store_columns<VEC, 32>(p, RK, i, lane, a.d, zero);
     return;
   }
   const int tid = T == 32 ? lane : threadIdx.x;
@@ -494,7 +494,7 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 32 ? 8 : (T < 1024 ? 1
     const char* p = static_cast<const char*>(a.grad_y) + t * a.grad_y_stride * bytes_of(GK);
     Chunk c[NCH];
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) c[i] = load_chunk<VEC>(p, GK, (i * T + tid) * 8, a.d);
+    for (int i = 0; i < NCH; ++i) c[i] = load_columns<VEC, T>(p, GK, i, tid, a.d);
 #pragma unroll
     for (int i = 0; i < NCH; ++i) to_f32(c[i], GK, g[i]);
   }
@@ -523,7 +523,7 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 32 ? 8 : (T < 1024 ? 1
         for (int k = 0; k < kGradRows; ++k) {
           const char* p = static_cast<const char*>(a.rows) + r[k] * a.rows_stride * bytes_of(RK);
 #pragma unroll
-          for (int i = 0; i < NCH; ++i) c[k][i] = load_chunk<VEC>(p, RK, src[k] >= 0 ? (i * T + tid) * 8 : a.d, a.d);
+          for (int i = 0; i < NCH; ++i) c[k][i] = load_columns<VEC, T>(p, RK, i, tid, src[k] >= 0 ? a.d : 0);
         }
         float dot[kGradRows];
 #pragma unroll
@@ -551,11 +551,10 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 32 ? 8 : (T < 1024 ? 1
           char* p = static_cast<char*>(a.grad_rows) + r[k] * a.grad_rows_stride * bytes_of(RK);
 #pragma unroll
           for (int i = 0; i < NCH; ++i) {
-            const int col = (i * T + tid) * 8;
             float f[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[e] = w[k] * g[i][e];
-            if (col < a.d) store8<VEC>(p, RK, col, a.d, f);
+            store_columns<VEC, T>(p, RK, i, tid, a.d, f);
           }
         }
       }

@@ -44,27 +44,26 @@ __device__ __forceinline__ void quad_of(const char* p, float (&v)[4]) {
     v[0] = bf16_lo(u.x), v[1] = bf16_hi(u.x), v[2] = bf16_lo(u.y), v[3] = bf16_hi(u.y);
   }
 }
-// Four values, 4 KIND bytes each, on their way to shared memory; WIDE: in one copy, else one at a time and at once.
-template <bool WIDE>
-__device__ __forceinline__ void copy_quad(char* to, const char* from, int kind, int left) {
-  if (WIDE) {
-    if (kind == MLPMOE_FP32) {
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
-    } else {
-      asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
-    }
-  } else if (kind == MLPMOE_FP32) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) reinterpret_cast<float*>(to)[e] = e < left ? reinterpret_cast<const float*>(from)[e] : 0.0f;
+// Values on their way to shared memory: four neighbours in one copy, or one, in place at once where no copy is that short.
+__device__ __forceinline__ void copy_quad(char* to, const char* from, int kind) {
+  if (kind == MLPMOE_FP32) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
   } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) reinterpret_cast<uint16_t*>(to)[e] = e < left ? reinterpret_cast<const uint16_t*>(from)[e] : uint16_t{0};
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
+  }
+}
+__device__ __forceinline__ void copy_one(char* to, const char* from, int kind) {
+  if (kind == MLPMOE_FP32) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
+  } else {
+    *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(from);
   }
 }
 
 constexpr int kStages = 2;
 
-// A row to the block's T threads (T = 32: to each of its eight warps), Q times four neighbouring columns a thread, whose sums over
+// A row to the block's T threads (T = 32: to each of its eight warps), Q times four neighbouring columns a thread (not WIDE, where they
+// are loaded one at a time: columns T apart, so that a warp's loads are neighbours), whose sums over
 // the block's rows stay in registers.  The next row is on its way to shared memory meanwhile; a thread reads only what it
 // copied itself, so that takes no barrier.  16384 x 4096, fp32 and bf16: 940 MB in
 // 149 us with the join (floor 146).  The row ahead in registers and types told apart as it runs: 258 (98 registers, 512 threads per SM); four
@@ -81,7 +80,8 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
   const bool has_r = a.ds_kind != kNone, r32 = a.ds_kind == MLPMOE_FP32, x32 = a.dx_kind == MLPMOE_FP32;
   const int64_t step = static_cast<int64_t>(gridDim.x) * R, first = static_cast<int64_t>(blockIdx.x) * R + (WARP ? threadIdx.x / 32 : 0);
   const int rows = first < a.n ? static_cast<int>((a.n - first + step - 1) / step) : 0;      // of this block or warp
-  const int col = tid * 4;                 // quad k: columns col + 4 T k ..
+  const int col = WIDE ? tid * 4 : tid;    // its first
+  auto apart = [](int k, int e) { return WIDE ? 4 * T * k + e : (4 * k + e) * T; };      // of value e of quad k
   const char* ps = static_cast<const char*>(a.s) + (first * a.s_stride + col) * SB;
   const char* pv = static_cast<const char*>(a.dv) + (first * a.dv_stride + col) * VB;
   const char* pr = static_cast<const char*>(a.ds) + (first * a.ds_stride + col) * rb;
@@ -96,11 +96,23 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
     if (more) {
 #pragma unroll
       for (int k = 0; k < Q; ++k) {
-        const int c = 4 * T * k, left = d - col - c, at = stage * Q + k;
-        if (left <= 0) continue;
-        copy_quad<WIDE>(mine_s + at * (THREADS * 4 * SB), ps + c * SB, SK, left);
-        copy_quad<WIDE>(mine_v + at * (THREADS * 4 * VB), pv + c * VB, VK, left);
-        if (has_r) copy_quad<WIDE>(mine_r + at * (THREADS * 16), pr + c * rb, a.ds_kind, left);
+        const int at = stage * Q + k;
+        if (WIDE) {
+          const int c = apart(k, 0);
+          if (col + c >= d) continue;
+          copy_quad(mine_s + at * (THREADS * 4 * SB), ps + c * SB, SK);
+          copy_quad(mine_v + at * (THREADS * 4 * VB), pv + c * VB, VK);
+          if (has_r) copy_quad(mine_r + at * (THREADS * 16), pr + c * rb, a.ds_kind);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int c = apart(k, e);
+            if (col + c >= d) continue;
+            copy_one(mine_s + at * (THREADS * 4 * SB) + e * SB, ps + c * SB, SK);
+            copy_one(mine_v + at * (THREADS * 4 * VB) + e * VB, pv + c * VB, VK);
+            if (has_r) copy_one(mine_r + at * (THREADS * 16) + e * rb, pr + c * rb, a.ds_kind);
+          }
+        }
       }
       ps += ds;
       pv += dv;
@@ -113,7 +125,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
   for (int k = 0; k < Q; ++k)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const int c = col + 4 * T * k + e;
+      const int c = col + apart(k, e);
       gain[k][e] = c < d ? (a.gain != nullptr ? a.gain[c] : 1.0f) : 0.0f;
       sum_g[k][e] = 0.0f;
       if (LAYER) sum_b[k][e] = 0.0f;
@@ -129,12 +141,17 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
 #pragma unroll
     for (int k = 0; k < Q; ++k) {
       const int at = stage * Q + k;
-      if (col + 4 * T * k < d) {
+      if (!WIDE || col + apart(k, 0) < d) {
         quad_of<SK>(mine_s + at * (THREADS * 4 * SB), z[k]);
         quad_of<VK>(mine_v + at * (THREADS * 4 * VB), v[k]);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[k][e] = v[k][e] = 0.0f;
+      }
+      if (!WIDE) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col + apart(k, e) >= d) z[k][e] = v[k][e] = 0.0f;      // nobody copied that
       }
     }
     float mean_h = 0.0f, ss, hz;
@@ -149,7 +166,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
       for (int k = 0; k < Q; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          z[k][e] = col + 4 * T * k + (WIDE ? 0 : e) < d ? z[k][e] - mean : 0.0f;
+          z[k][e] = col + apart(k, WIDE ? 0 : e) < d ? z[k][e] - mean : 0.0f;
           const float h = gain[k][e] * v[k][e];
           q[0] = fmaf(z[k][e], z[k][e], q[0]);
           q[1] = fmaf(h, z[k][e], q[1]);
@@ -176,8 +193,8 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
     const float along = hz * inv * inv * inv_d;
 #pragma unroll
     for (int k = 0; k < Q; ++k) {
-      const int c = 4 * T * k, left = d - col - c, at = stage * Q + k;
-      if (left <= 0) continue;
+      const int c = apart(k, 0), at = stage * Q + k;
+      if (col + c >= d) continue;
       float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
       if (has_r) {
         if (r32) {
@@ -199,7 +216,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (e < left) p[e] = r[e];
+            if (col + apart(k, e) < d) p[apart(0, e)] = r[e];
         }
       } else {
         __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(px) + c;
@@ -208,7 +225,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
         } else {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            if (e < left) p[e] = __float2bfloat16_rn(r[e]);
+            if (col + apart(k, e) < d) p[apart(0, e)] = __float2bfloat16_rn(r[e]);
         }
       }
     }
@@ -228,7 +245,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
 #pragma unroll
       for (int k = 0; k < Q; ++k)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) join[(threadIdx.x / 32) * 256 + col + 4 * T * k + e] = which == 0 ? sum_g[k][e] : sum_b[LAYER ? k : 0][e];
+        for (int e = 0; e < 4; ++e) join[(threadIdx.x / 32) * 256 + col + apart(k, e)] = which == 0 ? sum_g[k][e] : sum_b[LAYER ? k : 0][e];
       __syncthreads();
       if (static_cast<int>(threadIdx.x) < d && out[which] != nullptr) {
         float sum = join[threadIdx.x];
@@ -241,7 +258,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
       for (int k = 0; k < Q; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int c = col + 4 * T * k + e;
+          const int c = col + apart(k, e);
           if (c < d) out[which][c] = which == 0 ? sum_g[k][e] : sum_b[LAYER ? k : 0][e];
         }
     }

@@ -97,6 +97,46 @@ __device__ __forceinline__ void store8(void* row, int kind, int col, int d, cons
   }
 }
 
+// The same for kernels that may deal a row's columns to its threads as they like: chunk i of thread `tid` of T.  VEC: eight neighbours,
+// (i T + tid) 8 + e.  Else, where they would be loaded one at a time, columns (8 i + e) T + tid: a warp's loads are neighbours.
+template <bool VEC, int T>
+__device__ __forceinline__ int column(int i, int tid, int e) { return VEC ? (i * T + tid) * 8 + e : (8 * i + e) * T + tid; }
+template <bool VEC, int T>
+__device__ __forceinline__ Chunk load_columns(const void* row, int kind, int i, int tid, int d) {
+  if (VEC) return load_chunk<true>(row, kind, column<VEC, T>(i, tid, 0), d);
+  uint32_t w[8];
+  Chunk c;
+  if (kind == MLPMOE_FP32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = column<VEC, T>(i, tid, e) < d ? static_cast<const uint32_t*>(row)[column<VEC, T>(i, tid, e)] : 0u;
+    c.a = make_uint4(w[0], w[1], w[2], w[3]);
+    c.b = make_uint4(w[4], w[5], w[6], w[7]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = column<VEC, T>(i, tid, e) < d ? static_cast<const uint16_t*>(row)[column<VEC, T>(i, tid, e)] : 0u;
+    c.a = make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4] | (w[5] << 16), w[6] | (w[7] << 16));
+    c.b = make_uint4(0u, 0u, 0u, 0u);
+  }
+  return c;
+}
+template <bool VEC, int T>
+__device__ __forceinline__ void store_columns(void* row, int kind, int i, int tid, int d, const float (&v)[8]) {
+  if (VEC) {
+    if (column<VEC, T>(i, tid, 0) < d) store8<true>(row, kind, column<VEC, T>(i, tid, 0), d, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int col = column<VEC, T>(i, tid, e);
+      if (col >= d) continue;
+      if (kind == MLPMOE_FP32) {
+        static_cast<float*>(row)[col] = v[e];
+      } else {
+        static_cast<__nv_bfloat16*>(row)[col] = __float2bfloat16_rn(v[e]);
+      }
+    }
+  }
+}
+
 // Sum (or maximum) over the T threads of a row, the same bits in all of them.  T = 32: the row's warp; else the block.
 template <int T, bool MAX>
 __device__ __forceinline__ float row_reduce(float v, float* red) {
