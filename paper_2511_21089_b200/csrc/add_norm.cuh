@@ -56,6 +56,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
       store8<VEC>(row, kind, (i * T + tid) * 8, d, v);
     }
   };
+  auto values = [&](const Chunk& c, int kind, float (&v)[8]) { columns_f32<!SPREAD>(c, kind, v); };
   float s[NCH][8];
   {
     Chunk x[NCH], r[NCH];               // all of the row's loads before the first use
@@ -67,10 +68,10 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
     }
 #pragma unroll
     for (int i = 0; i < NCH; ++i) {
-      to_f32(x[i], XKIND, s[i]);
+      values(x[i], XKIND, s[i]);
       if (RKIND != kNone) {
         float v[8];
-        to_f32(r[i], RKIND, v);
+        values(r[i], RKIND, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j) s[i][j] += v[j];
       }

@@ -268,7 +268,8 @@ int64_t sort_bytes(const SortArgs& a) { return sort_mask_bytes(a) + (a.tiles == 
 
 // ------------------------------------------------------------------------------------------------ rows to their branches
 constexpr int kMoveThreads = 256;
-constexpr int kMoveVecs = 4;          // 16 bytes each, per lane: a warp moves 2 KB of a row
+// Units of a lane: a warp moves 2 KB of a row, or 16 units a lane where they are short.
+__host__ __device__ constexpr int units_of(int bytes) { return bytes >= 4 ? 64 / bytes : 16; }
 
 struct DispatchArgs {
   const uint8_t* x;
@@ -278,42 +279,49 @@ struct DispatchArgs {
   const int32_t* token_row;
   uint8_t* rows;
   float* row_scale;
-  int64_t n, x_stride, rows_stride, d;    // strides and width in bytes
+  int64_t n, x_stride, rows_stride, units;    // strides in bytes; units of a row
   int64_t n_rows, token_blocks;
   int B, slots, scales, parts;            // parts: warps of a row; scales: scales of a row
 };
 
-// A row's bytes, copied or cleared: 16 at a time where all rows start on 16 bytes, then the rest one at a time.
-template <int ES>
-struct Elem {
-  using type = uint8_t;
+// What a lane moves at a time: the widest unit that all rows start on and consist of.
+template <int BYTES>
+struct Unit {
+  using type = uint4;
 };
 template <>
-struct Elem<2> {
+struct Unit<8> {
+  using type = uint2;
+};
+template <>
+struct Unit<4> {
+  using type = uint32_t;
+};
+template <>
+struct Unit<2> {
   using type = uint16_t;
 };
 template <>
-struct Elem<4> {
-  using type = uint32_t;
+struct Unit<1> {
+  using type = uint8_t;
 };
 
 // One warp to a token's part of a row: the part is read once and written to each of the token's rows.  Behind the tokens, one
 // warp to each row that aligning can have left between two branches: cleared, so that products over a branch's whole tiles see zeros.
-template <int ES, bool VEC>
+template <int BYTES>
 __global__ void __launch_bounds__(kMoveThreads) dispatch_kernel(const __grid_constant__ DispatchArgs a) {
+  using E = typename Unit<BYTES>::type;
+  constexpr int kVecs = units_of(BYTES);
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   const int lane = threadIdx.x % 32;
-  using E = typename Elem<ES>::type;
   if (blockIdx.x >= a.token_blocks) {
     const int64_t u = (blockIdx.x - a.token_blocks) * (kMoveThreads / 32) + threadIdx.x / 32;
     const int64_t b = u % a.B, i = u / a.B;
     const int64_t r = static_cast<int64_t>(a.offsets[b]) + a.counts[b] + i;
     if (r >= a.offsets[b + 1] || r >= a.n_rows || r < 0) return;
-    uint8_t* p = a.rows + r * a.rows_stride;
-    const int64_t whole = VEC ? a.d / 16 * 16 : 0;
-    for (int64_t c = lane * 16; c < whole; c += 512) *reinterpret_cast<uint4*>(p + c) = make_uint4(0u, 0u, 0u, 0u);
-    for (int64_t c = whole + lane * ES; c < a.d; c += 32 * ES) *reinterpret_cast<E*>(p + c) = 0;
+    E* p = reinterpret_cast<E*>(a.rows + r * a.rows_stride);
+    for (int64_t c = lane; c < a.units; c += 32) p[c] = E{};
     for (int s = lane; s < a.scales; s += 32) a.row_scale[r * a.scales + s] = 0.0f;
     return;
   }
@@ -321,34 +329,22 @@ __global__ void __launch_bounds__(kMoveThreads) dispatch_kernel(const __grid_con
   const int64_t t = u / a.parts;
   const int part = static_cast<int>(u - t * a.parts);
   if (t >= a.n) return;
-  const int64_t c0 = static_cast<int64_t>(part) * (512 * kMoveVecs);
-  const uint8_t* x = a.x + t * a.x_stride;
-  const int64_t whole = VEC ? a.d / 16 * 16 : 0;
-  uint4 v[kMoveVecs];
-  if (VEC) {
+  const int64_t c0 = static_cast<int64_t>(part) * (32 * kVecs) + lane;
+  const E* x = reinterpret_cast<const E*>(a.x + t * a.x_stride);
+  E v[kVecs];
 #pragma unroll
-    for (int i = 0; i < kMoveVecs; ++i) {
-      const int64_t c = c0 + (i * 32 + lane) * 16;
-      if (c < whole) v[i] = *reinterpret_cast<const uint4*>(x + c);
-    }
-  }
-  const int64_t rest_lo = whole > c0 ? whole : c0;      // elements that no 16 bytes hold
-  const int64_t rest_hi = a.d < c0 + 512 * kMoveVecs ? a.d : c0 + 512 * kMoveVecs;
+  for (int i = 0; i < kVecs; ++i)
+    if (c0 + i * 32 < a.units) v[i] = x[c0 + i * 32];
   for (int j0 = 0; j0 < a.slots; j0 += 32) {
     const int32_t mine = j0 + lane < a.slots ? a.token_row[t * a.slots + j0 + lane] : -1;
     uint32_t live = __ballot_sync(0xFFFFFFFFu, static_cast<uint32_t>(mine) < static_cast<uint64_t>(a.n_rows));
     while (live != 0) {
       const int64_t r = __shfl_sync(0xFFFFFFFFu, mine, __ffs(live) - 1);
       live &= live - 1;
-      uint8_t* p = a.rows + r * a.rows_stride;
-      if (VEC) {
+      E* p = reinterpret_cast<E*>(a.rows + r * a.rows_stride);
 #pragma unroll
-        for (int i = 0; i < kMoveVecs; ++i) {
-          const int64_t c = c0 + (i * 32 + lane) * 16;
-          if (c < whole) *reinterpret_cast<uint4*>(p + c) = v[i];
-        }
-      }
-      for (int64_t c = rest_lo + lane * ES; c < rest_hi; c += 32 * ES) *reinterpret_cast<E*>(p + c) = *reinterpret_cast<const E*>(x + c);
+      for (int i = 0; i < kVecs; ++i)
+        if (c0 + i * 32 < a.units) p[c0 + i * 32] = v[i];
       if (part == 0)
         for (int s = lane; s < a.scales; s += 32) a.row_scale[r * a.scales + s] = a.x_scale[t * a.scales + s];
     }
@@ -413,7 +409,7 @@ __global__ void __launch_bounds__(kMoveThreads) combine_kernel(const __grid_cons
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
           float f[8];
-          to_f32(v[k][i], RK, f);
+          columns_f32<VEC>(v[k][i], RK, f);
 #pragma unroll
           for (int e = 0; e < 8; ++e) acc[i][e] = fmaf(w[k], f[e], acc[i][e]);
         }
@@ -424,7 +420,7 @@ __global__ void __launch_bounds__(kMoveThreads) combine_kernel(const __grid_cons
   for (int i = 0; i < NC; ++i) {
     if (SK != kNone) {
       float f[8];
-      to_f32(res[i], SK, f);
+      columns_f32<VEC>(res[i], SK, f);
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[i][e] += f[e];
     }
@@ -496,7 +492,7 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 32 ? 8 : (T < 1024 ? 1
 #pragma unroll
     for (int i = 0; i < NCH; ++i) c[i] = load_columns<VEC, T>(p, GK, i, tid, a.d);
 #pragma unroll
-    for (int i = 0; i < NCH; ++i) to_f32(c[i], GK, g[i]);
+    for (int i = 0; i < NCH; ++i) columns_f32<VEC>(c[i], GK, g[i]);
   }
   for (int j0 = 0; j0 < a.slots; j0 += 32) {
     int32_t mine = j0 + lane < a.slots ? a.token_row[t * a.slots + j0 + lane] : -1;
@@ -532,7 +528,7 @@ __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 32 ? 8 : (T < 1024 ? 1
 #pragma unroll
           for (int i = 0; i < NCH; ++i) {
             float f[8];
-            to_f32(c[k][i], RK, f);
+            columns_f32<VEC>(c[k][i], RK, f);
 #pragma unroll
             for (int e = 0; e < 8; ++e) dot[k] = fmaf(g[i][e], f[e], dot[k]);
           }
@@ -694,26 +690,29 @@ mlpmoe_status_t mlpmoe_dispatch(const void* x, mlpmoe_dtype_t dtype, int64_t x_s
   a.n = n_tokens;
   a.x_stride = x_stride * es;
   a.rows_stride = rows_stride * es;
-  a.d = d_model * es;
+  const uintptr_t all = reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(rows) | static_cast<uintptr_t>(a.x_stride | a.rows_stride | d_model * es);
+  const int unit = static_cast<int>((all | 16) & -(all | 16));
+  a.units = d_model * es / unit;
   a.n_rows = n_rows;
   a.B = B;
   a.slots = slots;
   a.scales = dtype == MLPMOE_E4M3 ? static_cast<int>(group == 0 ? 1 : (d_model + group - 1) / group) : 0;
-  a.parts = static_cast<int>((a.d + 512 * kMoveVecs - 1) / (512 * kMoveVecs));
+  const int64_t part = 32 * units_of(unit);
+  a.parts = static_cast<int>((a.units + part - 1) / part);
   a.token_blocks = (n_tokens * a.parts + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
   const int64_t blocks = a.token_blocks + (pad_rows_of(B, align) + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
   if (blocks > INT32_MAX) return MLPMOE_ERR_UNSUPPORTED;
-  const bool vec = on(x, 16) && on(rows, 16) && a.x_stride % 16 == 0 && a.rows_stride % 16 == 0;
   const dim3 grid(static_cast<unsigned>(blocks)), block(kMoveThreads);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   pdl_overlap_enabled() = true;
   cudaError_t e;
-  if (es == 4)
-    e = vec ? launch_pdl(dispatch_kernel<4, true>, grid, block, 0, st, a) : launch_pdl(dispatch_kernel<4, false>, grid, block, 0, st, a);
-  else if (es == 2)
-    e = vec ? launch_pdl(dispatch_kernel<2, true>, grid, block, 0, st, a) : launch_pdl(dispatch_kernel<2, false>, grid, block, 0, st, a);
-  else
-    e = vec ? launch_pdl(dispatch_kernel<1, true>, grid, block, 0, st, a) : launch_pdl(dispatch_kernel<1, false>, grid, block, 0, st, a);
+  switch (unit) {
+    case 16: e = launch_pdl(dispatch_kernel<16>, grid, block, 0, st, a); break;
+    case 8: e = launch_pdl(dispatch_kernel<8>, grid, block, 0, st, a); break;
+    case 4: e = launch_pdl(dispatch_kernel<4>, grid, block, 0, st, a); break;
+    case 2: e = launch_pdl(dispatch_kernel<2>, grid, block, 0, st, a); break;
+    default: e = launch_pdl(dispatch_kernel<1>, grid, block, 0, st, a); break;
+  }
   return e == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
 }
 

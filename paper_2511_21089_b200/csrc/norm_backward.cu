@@ -44,7 +44,7 @@ __device__ __forceinline__ void quad_of(const char* p, float (&v)[4]) {
     v[0] = bf16_lo(u.x), v[1] = bf16_hi(u.x), v[2] = bf16_lo(u.y), v[3] = bf16_hi(u.y);
   }
 }
-// Values on their way to shared memory: four neighbours in one copy, or one, in place at once where no copy is that short.
+// Four neighbours on their way to shared memory.
 __device__ __forceinline__ void copy_quad(char* to, const char* from, int kind) {
   if (kind == MLPMOE_FP32) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
@@ -52,20 +52,36 @@ __device__ __forceinline__ void copy_quad(char* to, const char* from, int kind) 
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
   }
 }
-__device__ __forceinline__ void copy_one(char* to, const char* from, int kind) {
+// A row that takes no wide copies, by its T threads, in words of four bytes as they lie in memory: one fp32 value, or two of bf16, the first
+// of them column -1 where the row starts in the middle of a word (`odd`).  What stands beside the row is not read.
+template <int T>
+__device__ __forceinline__ void copy_words(char* to, const char* row, int kind, int d, int tid) {
   if (kind == MLPMOE_FP32) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
+    for (int c = tid; c < d; c += T) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(to + 4 * c)), "l"(row + 4 * c) : "memory");
   } else {
-    *reinterpret_cast<uint16_t*>(to) = *reinterpret_cast<const uint16_t*>(from);
+    const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1 & 1);
+    const char* word = row - 2 * odd;
+    for (int w = tid; 2 * w < d + odd; w += T) {
+      const int c = 2 * w - odd;
+      if (c >= 0 && c + 1 < d) {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(to + 4 * w)), "l"(word + 4 * w) : "memory");
+      } else {
+        const int one = c < 0 ? 0 : c;
+        reinterpret_cast<uint16_t*>(to)[one + odd] = reinterpret_cast<const uint16_t*>(row)[one];
+      }
+    }
   }
+}
+__device__ __forceinline__ float word_value(const char* row, int kind, int odd, int c) {
+  return kind == MLPMOE_FP32 ? reinterpret_cast<const float*>(row)[c] : bf16_lo(reinterpret_cast<const uint16_t*>(row)[c + odd]);
 }
 
 constexpr int kStages = 2;
 
 // A row to the block's T threads (T = 32: to each of its eight warps), Q times four neighbouring columns a thread (not WIDE, where they
-// are loaded one at a time: columns T apart, so that a warp's loads are neighbours), whose sums over
+// come in words of four bytes: columns T apart, so that a warp's accesses are neighbours), whose sums over
 // the block's rows stay in registers.  The next row is on its way to shared memory meanwhile; a thread reads only what it
-// copied itself, so that takes no barrier.  16384 x 4096, fp32 and bf16: 940 MB in
+// copied itself, so that takes no barrier (not WIDE: two).  16384 x 4096, fp32 and bf16: 940 MB in
 // 149 us with the join (floor 146).  The row ahead in registers and types told apart as it runs: 258 (98 registers, 512 threads per SM); four
 // times four columns a thread: 159 (16 warps per SM).
 template <bool LAYER, int T, int Q, int CTAS, bool WIDE, int SK, int VK>
@@ -80,39 +96,45 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
   const bool has_r = a.ds_kind != kNone, r32 = a.ds_kind == MLPMOE_FP32, x32 = a.dx_kind == MLPMOE_FP32;
   const int64_t step = static_cast<int64_t>(gridDim.x) * R, first = static_cast<int64_t>(blockIdx.x) * R + (WARP ? threadIdx.x / 32 : 0);
   const int rows = first < a.n ? static_cast<int>((a.n - first + step - 1) / step) : 0;      // of this block or warp
-  const int col = WIDE ? tid * 4 : tid;    // its first
+  const int col = WIDE ? tid * 4 : tid, base = WIDE ? col : 0;      // the thread's first column, and the pointers'
   auto apart = [](int k, int e) { return WIDE ? 4 * T * k + e : (4 * k + e) * T; };      // of value e of quad k
-  const char* ps = static_cast<const char*>(a.s) + (first * a.s_stride + col) * SB;
-  const char* pv = static_cast<const char*>(a.dv) + (first * a.dv_stride + col) * VB;
-  const char* pr = static_cast<const char*>(a.ds) + (first * a.ds_stride + col) * rb;
-  char* px = static_cast<char*>(a.dx) + (first * a.dx_stride + col) * xb;
+  const char* ps = static_cast<const char*>(a.s) + (first * a.s_stride + base) * SB;
+  const char* pv = static_cast<const char*>(a.dv) + (first * a.dv_stride + base) * VB;
+  const char* pr = static_cast<const char*>(a.ds) + (first * a.ds_stride + base) * rb;
+  char* px = static_cast<char*>(a.dx) + (first * a.dx_stride + base) * xb;
   const int64_t ds = step * a.s_stride * SB, dv = step * a.dv_stride * VB, dr = step * a.ds_stride * rb, dx = step * a.dx_stride * xb;
-  // in shared memory: [stage][quad][thread], 16 bytes of s, then 8 or 16 of dv, then room for 16 of ds
-  constexpr int S_AT = 0, V_AT = kStages * Q * THREADS * 4 * SB, R_AT = V_AT + kStages * Q * THREADS * 4 * VB;
-  char* const mine_s = staged + S_AT + threadIdx.x * 4 * SB;
-  char* const mine_v = staged + V_AT + threadIdx.x * 4 * VB;
-  char* const mine_r = staged + R_AT + threadIdx.x * 16;
+  // in shared memory: [stage][quad][thread], 4 SB bytes of s, then 4 VB of dv, then room for 16 of ds; not WIDE: [stage][row] of each in turn,
+  // with 16 bytes more, and the starts of the rows in their words
+  constexpr int V_AT = kStages * Q * THREADS * 4 * SB, R_AT = V_AT + kStages * Q * THREADS * 4 * VB;
+  constexpr int S_ROW = Q * T * 4 * SB + 16, V_ROW = Q * T * 4 * VB + 16, R_ROW = Q * T * 16 + 16;
+  char* const mine_s = WIDE ? staged + threadIdx.x * 4 * SB : staged + (WARP ? threadIdx.x / 32 : 0) * kStages * (S_ROW + V_ROW + (has_r ? R_ROW : 0));
+  char* const mine_v = WIDE ? staged + V_AT + threadIdx.x * 4 * VB : mine_s + kStages * S_ROW;
+  char* const mine_r = WIDE ? staged + R_AT + threadIdx.x * 16 : mine_v + kStages * V_ROW;
+  uint32_t odd = 0;                        // not WIDE: bits 4 stage + 0, 1, 2: s, dv, ds of the stage's row start in the middle of a word
+  auto sync_row = [&]() {
+    if (WARP) {
+      __syncwarp();
+    } else {
+      __syncthreads();
+    }
+  };
   auto fetch = [&](bool more, int stage) {      // the row at ps, pv, pr; then the one after it in turn
     if (more) {
+      if (WIDE) {
 #pragma unroll
-      for (int k = 0; k < Q; ++k) {
-        const int at = stage * Q + k;
-        if (WIDE) {
-          const int c = apart(k, 0);
+        for (int k = 0; k < Q; ++k) {
+          const int at = stage * Q + k, c = apart(k, 0);
           if (col + c >= d) continue;
           copy_quad(mine_s + at * (THREADS * 4 * SB), ps + c * SB, SK);
           copy_quad(mine_v + at * (THREADS * 4 * VB), pv + c * VB, VK);
           if (has_r) copy_quad(mine_r + at * (THREADS * 16), pr + c * rb, a.ds_kind);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int c = apart(k, e);
-            if (col + c >= d) continue;
-            copy_one(mine_s + at * (THREADS * 4 * SB) + e * SB, ps + c * SB, SK);
-            copy_one(mine_v + at * (THREADS * 4 * VB) + e * VB, pv + c * VB, VK);
-            if (has_r) copy_one(mine_r + at * (THREADS * 16) + e * rb, pr + c * rb, a.ds_kind);
-          }
         }
+      } else {
+        copy_words<T>(mine_s + stage * S_ROW, ps, SK, d, tid);
+        copy_words<T>(mine_v + stage * V_ROW, pv, VK, d, tid);
+        if (has_r) copy_words<T>(mine_r + stage * R_ROW, pr, a.ds_kind, d, tid);
+        const uint32_t bits = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(ps) >> 1 & 1) | (reinterpret_cast<uintptr_t>(pv) & 2) | ((reinterpret_cast<uintptr_t>(pr) & 2) << 1));
+        odd = (odd & ~(15u << (4 * stage))) | bits << (4 * stage);
       }
       ps += ds;
       pv += dv;
@@ -137,21 +159,24 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
   for (int i = 0; i < rows; ++i) {
     const int stage = i % kStages;
     asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    if (!WIDE) sync_row();                 // the others' copies too
     float z[Q][4], v[Q][4];
 #pragma unroll
     for (int k = 0; k < Q; ++k) {
       const int at = stage * Q + k;
-      if (!WIDE || col + apart(k, 0) < d) {
+      if (!WIDE) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int c = col + apart(k, e);
+          z[k][e] = c < d ? word_value(mine_s + stage * S_ROW, SK, odd >> (4 * stage) & 1, c) : 0.0f;
+          v[k][e] = c < d ? word_value(mine_v + stage * V_ROW, VK, odd >> (4 * stage + 1) & 1, c) : 0.0f;
+        }
+      } else if (col + apart(k, 0) < d) {
         quad_of<SK>(mine_s + at * (THREADS * 4 * SB), z[k]);
         quad_of<VK>(mine_v + at * (THREADS * 4 * VB), v[k]);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e) z[k][e] = v[k][e] = 0.0f;
-      }
-      if (!WIDE) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (col + apart(k, e) >= d) z[k][e] = v[k][e] = 0.0f;      // nobody copied that
       }
     }
     float mean_h = 0.0f, ss, hz;
@@ -196,7 +221,11 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
       const int c = apart(k, 0), at = stage * Q + k;
       if (col + c >= d) continue;
       float r[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (has_r) {
+      if (has_r && !WIDE) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (col + apart(k, e) < d) r[e] = word_value(mine_r + stage * R_ROW, a.ds_kind, odd >> (4 * stage + 2) & 1, col + apart(k, e));
+      } else if (has_r) {
         if (r32) {
           quad_of<MLPMOE_FP32>(mine_r + at * (THREADS * 16), r);
         } else {
@@ -210,7 +239,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
         r[e] = fmaf(inv, fmaf(-z[k][e], along, fmaf(gain[k][e], v[k][e], -mean_h)), r[e]);
       }
       if (x32) {
-        float* p = reinterpret_cast<float*>(px) + c;
+        float* p = reinterpret_cast<float*>(px) + (WIDE ? c : col + c);
         if (WIDE) {
           __stcs(reinterpret_cast<float4*>(p), make_float4(r[0], r[1], r[2], r[3]));
         } else {
@@ -219,7 +248,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
             if (col + apart(k, e) < d) p[apart(0, e)] = r[e];
         }
       } else {
-        __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(px) + c;
+        __nv_bfloat16* p = reinterpret_cast<__nv_bfloat16*>(px) + (WIDE ? c : col + c);
         if (WIDE) {
           *reinterpret_cast<uint2*>(p) = make_uint2(pack2(r[0], r[1]), pack2(r[2], r[3]));
         } else {
@@ -230,6 +259,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
       }
     }
     px += dx;
+    if (!WIDE) sync_row();                 // everybody is done with the stage
     fetch(i + kStages < rows, stage);
   }
   if (a.dgain == nullptr && a.dbias == nullptr) return;
@@ -393,8 +423,8 @@ int blocks_of(int64_t n, int64_t d) {
 template <bool LAYER, bool WIDE, int SHAPE, int SK, int VK>
 cudaError_t launch_kinds(const NormGradArgs& a, cudaStream_t st) {
   constexpr Shape s = kShapes[SHAPE];
-  constexpr int threads = s.threads == 32 ? 256 : s.threads, held = kStages * 4 * s.quads * threads * (bytes_of(SK) + bytes_of(VK));
-  constexpr int most = held + kStages * 16 * s.quads * threads;
+  constexpr int threads = s.threads == 32 ? 256 : s.threads, rows = s.threads == 32 ? 8 : 1, more = WIDE ? 0 : kStages * rows * 16;
+  constexpr int held = kStages * 4 * s.quads * threads * (bytes_of(SK) + bytes_of(VK)) + 2 * more, most = held + kStages * 16 * s.quads * threads + more;
   auto kernel = norm_backward_kernel<LAYER, s.threads, s.quads, s.ctas, WIDE, SK, VK>;
   if (most > 47 * 1024) {      // above what a kernel has anyway; the limit is the same for every call, whatever its own size
     const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);

@@ -103,21 +103,27 @@ template <bool VEC, int T>
 __device__ __forceinline__ int column(int i, int tid, int e) { return VEC ? (i * T + tid) * 8 + e : (8 * i + e) * T + tid; }
 template <bool VEC, int T>
 __device__ __forceinline__ Chunk load_columns(const void* row, int kind, int i, int tid, int d) {
-  if (VEC) return load_chunk<true>(row, kind, column<VEC, T>(i, tid, 0), d);
-  uint32_t w[8];
-  Chunk c;
-  if (kind == MLPMOE_FP32) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = column<VEC, T>(i, tid, e) < d ? static_cast<const uint32_t*>(row)[column<VEC, T>(i, tid, e)] : 0u;
-    c.a = make_uint4(w[0], w[1], w[2], w[3]);
-    c.b = make_uint4(w[4], w[5], w[6], w[7]);
+  if (VEC) {
+    return load_chunk<true>(row, kind, column<VEC, T>(i, tid, 0), d);
   } else {
+    uint32_t w[8];                    // a word each, bf16 too: packing them would wait for the loads
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w[e] = column<VEC, T>(i, tid, e) < d ? static_cast<const uint16_t*>(row)[column<VEC, T>(i, tid, e)] : 0u;
-    c.a = make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4] | (w[5] << 16), w[6] | (w[7] << 16));
-    c.b = make_uint4(0u, 0u, 0u, 0u);
+    for (int e = 0; e < 8; ++e) {
+      const int col = column<VEC, T>(i, tid, e);
+      w[e] = 0u;
+      if (col < d) w[e] = kind == MLPMOE_FP32 ? static_cast<const uint32_t*>(row)[col] : static_cast<const uint16_t*>(row)[col];
+    }
+    return Chunk{make_uint4(w[0], w[1], w[2], w[3]), make_uint4(w[4], w[5], w[6], w[7])};
   }
-  return c;
+}
+template <bool VEC>
+__device__ __forceinline__ void columns_f32(const Chunk& c, int kind, float (&v)[8]) {
+  if (VEC || kind == MLPMOE_FP32) {
+    to_f32(c, kind, v);
+  } else {
+    v[0] = bf16_lo(c.a.x), v[1] = bf16_lo(c.a.y), v[2] = bf16_lo(c.a.z), v[3] = bf16_lo(c.a.w);
+    v[4] = bf16_lo(c.b.x), v[5] = bf16_lo(c.b.y), v[6] = bf16_lo(c.b.z), v[7] = bf16_lo(c.b.w);
+  }
 }
 template <bool VEC, int T>
 __device__ __forceinline__ void store_columns(void* row, int kind, int i, int tid, int d, const float (&v)[8]) {
