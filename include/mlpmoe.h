@@ -552,7 +552,7 @@ typedef struct {
 } mlpmoe_adamw_settings_t;
 
 /*
- * One AdamW step over n_tensors tensors (a host array, not needed after the call), in fp32, a launch for up to 400 of the same types:
+ * One AdamW step over n_tensors tensors (a host array, not needed after the call), in fp32, a launch for up to 384 of the same types:
  *     g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *     param = param - lr * weight_decay * param - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
  * The param takes the new moments before they are rounded.  e4m3 moments: scale = max(max |finite value| / 448, 2^-126) of each 128

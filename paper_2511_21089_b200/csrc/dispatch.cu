@@ -21,8 +21,8 @@ constexpr int kMaxAlign = 1024;
 // per tile of tokens.  Second: each tile adds up the tiles before it, and every set bit's place is its branch's start plus
 // the bits before it.  A small batch is one tile and takes one launch.
 constexpr int kSortThreads = 512;
-constexpr int kSortTiles = 148;           // tiles aimed at: one block per SM; every tile reads every tile's counts
-constexpr int kSortScanTiles = 512;       // from here on those sums are made once, by a kernel of their own
+constexpr int kSortTiles = 592;           // tiles aimed at: four blocks per SM (131072 tokens x 32 branches: 23 us; one block per SM: 49)
+constexpr int kSortScanCounts = 16384;    // every tile adds up every tile's counts; from here on a kernel of its own does so once
 constexpr int kSortTileBits = 4096;       // words of 32 bits of one tile: 32 KB of shared memory with the places
 
 struct SortArgs {
@@ -138,7 +138,7 @@ template <bool ONE>      // one tile: the bits and their counts are made here
 __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_constant__ SortArgs a) {
   __shared__ uint32_t mask[kSortTileBits];
   __shared__ int32_t place[kSortTileBits];     // where the group's first token of the branch goes; before that scratch of the sums
-  __shared__ int32_t first[kMaxB], total[kMaxB], before[kMaxB], warp_sum[kMaxB / 32];
+  __shared__ int32_t first[kMaxB + 1], total[kMaxB], before[kMaxB], warp_sum[kMaxB / 32];
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, tile = blockIdx.x;
@@ -200,6 +200,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
     int32_t start = incl - padded;
     for (int i = 0; i < warp; ++i) start += warp_sum[i];
     first[tid] = start;
+    if (tid == a.B32 - 1) first[a.B32] = start + padded;
     if (tile == 0 && tid < a.B) {
       a.offsets[tid] = start;
       a.counts[tid] = total[tid];
@@ -208,11 +209,10 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
   }
   __syncthreads();
   // the rows between a branch's end and the next start belong to no token
-  for (int b = tile; b < a.B; b += gridDim.x) {
-    const int32_t end = first[b] + total[b], next = first[b] + (total[b] + a.align - 1) / a.align * a.align;
-    for (int32_t r = end + tid; r < next; r += kSortThreads)
-      if (r < a.rows) a.row_token[r] = -1;
-  }
+  if (a.align > 1)
+    for (int b = tile * (kSortThreads / 32) + warp; b < a.B; b += gridDim.x * (kSortThreads / 32))
+      for (int32_t r = first[b] + total[b] + lane; r < first[b + 1]; r += 32)
+        if (r < a.rows) a.row_token[r] = -1;
   if (tid < a.B32) {
     int32_t run = first[tid] + before[tid];
     for (int i = 0; i < n_groups; ++i) {
@@ -247,24 +247,30 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
   }
 }
 
-// Tiles of a batch: as many as there are SMs where a tile then has four groups of 32 tokens at least, more where a tile gets too large.
+// Tiles of a batch.  Up to 128 tokens one tile and one launch (32 branches: 2.6 us; 256 tokens 5.2, as two launches 4.8), else tiles of two
+// groups or more, four where there are many branches (8192 x 128: 9.9 us, two: 14.6), up to kSortTiles of them.
 void sort_plan(int64_t n, int32_t B, SortArgs* a) {
   a->n = n;
   a->B = B;
   a->B32 = (B + 31) / 32 * 32;
   a->groups = static_cast<int>((n + 31) / 32);
-  const int most = kSortTileBits / a->B32 < 32 ? kSortTileBits / a->B32 : 32;
+  const int most = kSortTileBits / a->B32 < 32 ? kSortTileBits / a->B32 : 32, least = a->groups <= 4 || a->B32 >= 128 ? 4 : 2;
   int g = (a->groups + kSortTiles - 1) / kSortTiles;
-  if (g < 4) g = 4;
-  if (g > most || a->groups <= most) g = most;
+  if (g < least) g = least;
+  if (g > most) g = most;
   a->tile_groups = g;
   a->tiles = a->groups <= g ? 1 : (a->groups + g - 1) / g;
-  a->scanned = a->tiles > kSortScanTiles;
+  a->scanned = static_cast<int64_t>(a->tiles) * a->B32 > kSortScanCounts;
 }
 
 int64_t round16(int64_t v) { return (v + 15) / 16 * 16; }
 int64_t sort_mask_bytes(const SortArgs& a) { return a.tiles == 1 ? 0 : round16(static_cast<int64_t>(a.groups) * a.B32 * 4); }
-int64_t sort_bytes(const SortArgs& a) { return sort_mask_bytes(a) + (a.tiles == 1 ? 16 : round16((static_cast<int64_t>(a.tiles) + 1) * a.B32 * 4)); }
+// (for as many tiles as any smaller batch has, too: a workspace serves every batch up to its own)
+int64_t sort_bytes(const SortArgs& a) {
+  if (a.tiles == 1) return 16;
+  const int64_t aimed = a.groups < kSortTiles ? a.groups : kSortTiles, tiles = a.tiles > aimed ? a.tiles : aimed;
+  return sort_mask_bytes(a) + round16((tiles + 1) * a.B32 * 4);
+}
 
 // ------------------------------------------------------------------------------------------------ rows to their branches
 constexpr int kMoveThreads = 256;
