@@ -246,17 +246,23 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
   auto load = [&](int at, Raw<EIGHT>& r) {
     const bool whole = wide && at + kAdamStep <= count;
     const int left = min(8, count - at - mine);
-    if (!whole && left <= 0) return;
-    r.p = fetch<PK>(p_at + at * PB, whole, left);
-    r.g = fetch<GK>(g_at + at * GB, whole, left);
-    if (EIGHT) {
-      r.m8 = fetch_codes(m_at + at, whole, left);
-      r.v8 = fetch_codes(v_at + at, whole, left);
-      r.m_scale = ms_at[at / kStateBlock];
-      r.v_scale = vs_at[at / kStateBlock];
-    } else {
-      r.m = fetch<MLPMOE_FP32>(m_at + at * 4, whole, left);
-      r.v = fetch<MLPMOE_FP32>(v_at + at * 4, whole, left);
+    auto all = [&](bool eight_there) {
+      r.p = fetch<PK>(p_at + at * PB, eight_there, left);
+      r.g = fetch<GK>(g_at + at * GB, eight_there, left);
+      if (EIGHT) {
+        r.m8 = fetch_codes(m_at + at, eight_there, left);
+        r.v8 = fetch_codes(v_at + at, eight_there, left);
+        r.m_scale = ms_at[at / kStateBlock];
+        r.v_scale = vs_at[at / kStateBlock];
+      } else {
+        r.m = fetch<MLPMOE_FP32>(m_at + at * 4, eight_there, left);
+        r.v = fetch<MLPMOE_FP32>(v_at + at * 4, eight_there, left);
+      }
+    };
+    if (whole) {                           // one branch a step, not one a buffer
+      all(true);
+    } else if (left > 0) {
+      all(false);
     }
   };
   Raw<EIGHT> next = {};
@@ -322,35 +328,43 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
 #pragma unroll
       for (int e = 0; e < 8; ++e) noise[e] = mix(key + static_cast<uint32_t>(i) * 0x9E3779B1u + e * 0x9E3779B1u);
     }
-    if (whole || left > 0) {
-      if (copies) put<MLPMOE_BF16>(copy_at + at * 2, whole, left, p);
-      if (NOISE && PK == MLPMOE_BF16) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (finite(p[e])) p[e] = __uint_as_float((__float_as_uint(p[e]) + (mix(noise[e] ^ 0x9E3779B1u) & 0xFFFFu)) & 0xFFFF0000u);
-      }
-      put<PK>(p_at + at * PB, whole, left, p);
-      if (!EIGHT) {
-        put<MLPMOE_FP32>(m_at + at * 4, whole, left, m);
-        put<MLPMOE_FP32>(v_at + at * 4, whole, left, v);
-      }
-    }
+    uint2 code_m, code_v;
+    float scale_m, scale_v;
     if (EIGHT) {
       if (!whole) {                        // what lies behind the end must not reach the last block's scales
 #pragma unroll
         for (int e = 0; e < 8; ++e)
           if (e >= left) m[e] = root[e] = 0.0f;
       }
-      float scale_m, scale_v;
-      const uint2 code_m = codes_of<NOISE, false>(m, noise, scale_m), code_v = codes_of<NOISE, true>(root, noise, scale_v);
-      if (whole || left > 0) {
+      code_m = codes_of<NOISE, false>(m, noise, scale_m);
+      code_v = codes_of<NOISE, true>(root, noise, scale_v);
+    }
+    float rounded[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      rounded[e] = p[e];
+      if (NOISE && PK == MLPMOE_BF16 && finite(p[e]))
+        rounded[e] = __uint_as_float((__float_as_uint(p[e]) + (mix(noise[e] ^ 0x9E3779B1u) & 0xFFFFu)) & 0xFFFF0000u);
+    }
+    auto all = [&](bool eight_there) {
+      if (copies) put<MLPMOE_BF16>(copy_at + at * 2, eight_there, left, p);
+      put<PK>(p_at + at * PB, eight_there, left, rounded);
+      if (EIGHT) {
         if (threadIdx.x % (kStateBlock / 8) == 0) {
           ms_at[at / kStateBlock] = scale_m;
           vs_at[at / kStateBlock] = scale_v;
         }
-        put_codes(m_at + at, whole, left, code_m);
-        put_codes(v_at + at, whole, left, code_v);
+        put_codes(m_at + at, eight_there, left, code_m);
+        put_codes(v_at + at, eight_there, left, code_v);
+      } else {
+        put<MLPMOE_FP32>(m_at + at * 4, eight_there, left, m);
+        put<MLPMOE_FP32>(v_at + at * 4, eight_there, left, v);
       }
+    };
+    if (whole) {
+      all(true);
+    } else if (left > 0) {
+      all(false);
     }
   }
 }
