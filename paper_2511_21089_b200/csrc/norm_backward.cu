@@ -52,34 +52,40 @@ __device__ __forceinline__ void copy_quad(char* to, const char* from, int kind) 
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(ptx::smem_u32(to)), "l"(from) : "memory");
   }
 }
-// A row that takes no wide copies, by its T threads, in words of four bytes as they lie in memory: one fp32 value, or two of bf16, the first
-// of them column -1 where the row starts in the middle of a word (`odd`).  What stands beside the row is not read.
+// A row that starts anywhere, by its T threads: what of it fills whole pieces of 16 bytes goes in those, the rest in words of four, to the same
+// place relative to 16 bytes.  What stands beside the row is not read: of a word that only half belongs to it (bf16, its first or
+// last value) a thread keeps the value for later, marked 1 or 2 above its 16 bits.
 template <int T>
-__device__ __forceinline__ void copy_words(char* to, const char* row, int kind, int d, int tid) {
-  if (kind == MLPMOE_FP32) {
-    for (int c = tid; c < d; c += T) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(to + 4 * c)), "l"(row + 4 * c) : "memory");
-  } else {
-    const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(row) >> 1 & 1);
-    const char* word = row - 2 * odd;
-    for (int w = tid; 2 * w < d + odd; w += T) {
-      const int c = 2 * w - odd;
-      if (c >= 0 && c + 1 < d) {
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(to + 4 * w)), "l"(word + 4 * w) : "memory");
-      } else {
-        const int one = c < 0 ? 0 : c;
-        reinterpret_cast<uint16_t*>(to)[one + odd] = reinterpret_cast<const uint16_t*>(row)[one];
-      }
+__device__ __forceinline__ uint32_t copy_row(char* to, const char* row, int bytes, int d, int tid) {
+  const int lead = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15), end = lead + d * bytes;
+  const char* from = row - lead;
+  for (int at = 16 * tid; at + 16 <= end; at += 16 * T)
+    if (at >= lead) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ptx::smem_u32(to + at)), "l"(from + at) : "memory");
+  uint32_t kept = 0;
+  if (tid < 8) {
+    const bool some = tid < 4 ? lead > 0 || end < 16 : end >= 16 && end % 16 != 0;      // the first piece, the last
+    const int at = (tid < 4 ? 0 : end / 16 * 16) + 4 * (tid % 4);
+    if (some && at >= lead && at + 4 <= end) {
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(ptx::smem_u32(to + at)), "l"(from + at) : "memory");
+    } else if (some && at + 2 == lead) {
+      kept = load_if<2>(row, true) | 1u << 16;
+    } else if (some && at >= lead && at + 2 == end) {
+      kept = load_if<2>(from + at, true) | 2u << 16;
     }
   }
+  return kept;
 }
-__device__ __forceinline__ float word_value(const char* row, int kind, int odd, int c) {
-  return kind == MLPMOE_FP32 ? reinterpret_cast<const float*>(row)[c] : bf16_lo(reinterpret_cast<const uint16_t*>(row)[c + odd]);
+__device__ __forceinline__ void put_kept(char* row, uint32_t kept, int d) {
+  if (kept != 0) *reinterpret_cast<uint16_t*>(row + (kept >> 17 ? 2 * (d - 1) : 0)) = static_cast<uint16_t>(kept);
+}
+__device__ __forceinline__ float row_value(const char* row, int kind, int c) {
+  return kind == MLPMOE_FP32 ? reinterpret_cast<const float*>(row)[c] : bf16_lo(reinterpret_cast<const uint16_t*>(row)[c]);
 }
 
 constexpr int kStages = 2;
 
 // A row to the block's T threads (T = 32: to each of its eight warps), Q times four neighbouring columns a thread (not WIDE, where they
-// come in words of four bytes: columns T apart, so that a warp's accesses are neighbours), whose sums over
+// start anywhere: columns T apart, so that a warp's accesses are neighbours), whose sums over
 // the block's rows stay in registers.  The next row is on its way to shared memory meanwhile; a thread reads only what it
 // copied itself, so that takes no barrier (not WIDE: two).  16384 x 4096, fp32 and bf16: 940 MB in
 // 149 us with the join (floor 146).  The row ahead in registers and types told apart as it runs: 258 (98 registers, 512 threads per SM); four
@@ -104,13 +110,17 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
   char* px = static_cast<char*>(a.dx) + (first * a.dx_stride + base) * xb;
   const int64_t ds = step * a.s_stride * SB, dv = step * a.dv_stride * VB, dr = step * a.ds_stride * rb, dx = step * a.dx_stride * xb;
   // in shared memory: [stage][quad][thread], 4 SB bytes of s, then 4 VB of dv, then room for 16 of ds; not WIDE: [stage][row] of each in turn,
-  // with 16 bytes more, and the starts of the rows in their words
+  // with 16 bytes more
   constexpr int V_AT = kStages * Q * THREADS * 4 * SB, R_AT = V_AT + kStages * Q * THREADS * 4 * VB;
   constexpr int S_ROW = Q * T * 4 * SB + 16, V_ROW = Q * T * 4 * VB + 16, R_ROW = Q * T * 16 + 16;
   char* const mine_s = WIDE ? staged + threadIdx.x * 4 * SB : staged + (WARP ? threadIdx.x / 32 : 0) * kStages * (S_ROW + V_ROW + (has_r ? R_ROW : 0));
   char* const mine_v = WIDE ? staged + V_AT + threadIdx.x * 4 * VB : mine_s + kStages * S_ROW;
   char* const mine_r = WIDE ? staged + R_AT + threadIdx.x * 16 : mine_v + kStages * V_ROW;
-  uint32_t odd = 0;                        // not WIDE: bits 4 stage + 0, 1, 2: s, dv, ds of the stage's row start in the middle of a word
+  // not WIDE: where the rows of s, dv and ds start in their 16 bytes, and the values kept for later; of this row and of the next
+  struct Edges {
+    uint32_t lead, s, v, r;
+  };
+  Edges now = {}, next = {}, fetched = {};
   auto sync_row = [&]() {
     if (WARP) {
       __syncwarp();
@@ -130,11 +140,10 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
           if (has_r) copy_quad(mine_r + at * (THREADS * 16), pr + c * rb, a.ds_kind);
         }
       } else {
-        copy_words<T>(mine_s + stage * S_ROW, ps, SK, d, tid);
-        copy_words<T>(mine_v + stage * V_ROW, pv, VK, d, tid);
-        if (has_r) copy_words<T>(mine_r + stage * R_ROW, pr, a.ds_kind, d, tid);
-        const uint32_t bits = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(ps) >> 1 & 1) | (reinterpret_cast<uintptr_t>(pv) & 2) | ((reinterpret_cast<uintptr_t>(pr) & 2) << 1));
-        odd = (odd & ~(15u << (4 * stage))) | bits << (4 * stage);
+        fetched.s = copy_row<T>(mine_s + stage * S_ROW, ps, SB, d, tid);
+        fetched.v = copy_row<T>(mine_v + stage * V_ROW, pv, VB, d, tid);
+        if (has_r) fetched.r = copy_row<T>(mine_r + stage * R_ROW, pr, rb, d, tid);
+        fetched.lead = static_cast<uint32_t>((reinterpret_cast<uintptr_t>(ps) & 15) | (reinterpret_cast<uintptr_t>(pv) & 15) << 4 | (reinterpret_cast<uintptr_t>(pr) & 15) << 8);
       }
       ps += ds;
       pv += dv;
@@ -153,13 +162,25 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
       if (LAYER) sum_b[k][e] = 0.0f;
     }
 #pragma unroll
-  for (int k = 0; k < kStages; ++k) fetch(k < rows, k);
+  for (int k = 0; k < kStages; ++k) {
+    fetch(k < rows, k);
+    now = next;
+    next = fetched;
+  }
   int turn = 0;
   const float inv_d = 1.0f / static_cast<float>(d);
   for (int i = 0; i < rows; ++i) {
     const int stage = i % kStages;
     asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
-    if (!WIDE) sync_row();                 // the others' copies too
+    const char* const row_s = mine_s + stage * S_ROW + (now.lead & 15);      // not WIDE
+    const char* const row_v = mine_v + stage * V_ROW + (now.lead >> 4 & 15);
+    const char* const row_r = mine_r + stage * R_ROW + (now.lead >> 8 & 15);
+    if (!WIDE) {
+      put_kept(const_cast<char*>(row_s), now.s, d);
+      put_kept(const_cast<char*>(row_v), now.v, d);
+      put_kept(const_cast<char*>(row_r), now.r, d);
+      sync_row();                          // the others' copies too
+    }
     float z[Q][4], v[Q][4];
 #pragma unroll
     for (int k = 0; k < Q; ++k) {
@@ -168,8 +189,8 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int c = col + apart(k, e);
-          z[k][e] = c < d ? word_value(mine_s + stage * S_ROW, SK, odd >> (4 * stage) & 1, c) : 0.0f;
-          v[k][e] = c < d ? word_value(mine_v + stage * V_ROW, VK, odd >> (4 * stage + 1) & 1, c) : 0.0f;
+          z[k][e] = c < d ? row_value(row_s, SK, c) : 0.0f;
+          v[k][e] = c < d ? row_value(row_v, VK, c) : 0.0f;
         }
       } else if (col + apart(k, 0) < d) {
         quad_of<SK>(mine_s + at * (THREADS * 4 * SB), z[k]);
@@ -224,7 +245,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
       if (has_r && !WIDE) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (col + apart(k, e) < d) r[e] = word_value(mine_r + stage * R_ROW, a.ds_kind, odd >> (4 * stage + 2) & 1, col + apart(k, e));
+          if (col + apart(k, e) < d) r[e] = row_value(row_r, a.ds_kind, col + apart(k, e));
       } else if (has_r) {
         if (r32) {
           quad_of<MLPMOE_FP32>(mine_r + at * (THREADS * 16), r);
@@ -261,6 +282,8 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
     px += dx;
     if (!WIDE) sync_row();                 // everybody is done with the stage
     fetch(i + kStages < rows, stage);
+    now = next;
+    next = fetched;
   }
   if (a.dgain == nullptr && a.dbias == nullptr) return;
   // the block's sums: to the result where it is the only block
@@ -411,7 +434,7 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const __grid_constant__
 struct Shape {
   int threads, quads, ctas;
 };
-constexpr Shape kShapes[] = {{32, 2, 4}, {128, 2, 8}, {256, 2, 4}, {512, 2, 2}, {1024, 2, 1}};
+constexpr Shape kShapes[] = {{32, 2, 3}, {128, 2, 8}, {256, 2, 4}, {512, 2, 2}, {1024, 2, 1}};
 int shape_of(int64_t d) { return d <= 256 ? 0 : (d <= 1024 ? 1 : (d <= 2048 ? 2 : (d <= 4096 ? 3 : 4))); }
 int blocks_of(int64_t n, int64_t d) {
   const int64_t need = d <= 256 ? (n + 7) / 8 : n, most = static_cast<int64_t>(kSms) * kShapes[shape_of(d)].ctas;
