@@ -422,7 +422,7 @@ mlpmoe_status_t mlpmoe_w4_get_status(const void* workspace, void* stream);
  *                 offsets[B] on are left as they were.  rows: at least what mlpmoe_sort_rows gives, which no selection exceeds
  *   token_row     device int32 [n_tokens x slots]: the rows of a token's branches, ascending b, then -1
  *   token_branch  device int32 [n_tokens x slots], or NULL: those branches, then -1
- *   workspace     device, 16-byte aligned, of the size that mlpmoe_sort_workspace gives
+ *   workspace     device, 16-byte aligned, of the size that mlpmoe_sort_workspace gives for n_tokens or more
  * 1 <= B <= 256, 1 <= align <= 1024, slots >= 1, at most 2^31 - 1 rows (more: MLPMOE_ERR_UNSUPPORTED).
  */
 mlpmoe_status_t mlpmoe_sort_tokens(const uint8_t* select, int64_t n_tokens, int32_t B, int32_t slots, int32_t align, int32_t* offsets,
@@ -463,8 +463,8 @@ mlpmoe_status_t mlpmoe_combine(const void* rows, mlpmoe_dtype_t rows_dtype, int6
  * Gradient of mlpmoe_combine (that of the residual is grad_y itself):
  *     grad_rows[token_row[t, j]] = weight[t, j] * grad_y[t];     grad_weight[t, j] = sum_c grad_y[t, c] * rows[token_row[t, j], c]
  * and 0 for the weight of a place without a row and for the rows between a branch's end and the next start.
- *   grad_rows    device, of rows_dtype, grad_rows_stride elements apart (0 = d_model), or NULL; may be rows itself (same stride).
- *                Rows from offsets[B] on are left as they were
+ *   grad_rows    device, of rows_dtype, grad_rows_stride elements apart (0 = d_model), or NULL; may be rows itself (same stride), must
+ *                not overlap grad_y.  Rows from offsets[B] on are left as they were.  A row stands in token_row once at most
  *   grad_weight  device fp32 [n_tokens x slots], or NULL (rows is not read then)
  *   B, slots, align, offsets, counts, token_row, n_rows, weight   as above (offsets and counts: only for grad_rows with align above 1)
  * d_model up to 32768 (more: MLPMOE_ERR_UNSUPPORTED).
@@ -498,7 +498,7 @@ typedef enum { MLPMOE_RMSNORM = 0, MLPMOE_LAYERNORM = 1 } mlpmoe_norm_t;
  *   grad_s    device, fp32 or bf16, or NULL: the gradient that reaches s on its other way, the residual stream
  *   grad_x    device, fp32 or bf16; may be grad_s itself (same type and stride), must not overlap s or grad_out
  *   grad_gain, grad_bias  device fp32 [d_model], or NULL (grad_bias: LayerNorm only); n_tokens = 0 clears them
- *   workspace device, 16-byte aligned, of the size that mlpmoe_norm_backward_workspace gives; not used if both are NULL
+ *   workspace device, 16-byte aligned, of the size that mlpmoe_norm_backward_workspace gives for n_tokens or more; not used if both are NULL
  * Strides in elements, 0 = d_model; any d_model up to 32768 (more: MLPMOE_ERR_UNSUPPORTED), any element alignment.
  */
 mlpmoe_status_t mlpmoe_norm_backward(mlpmoe_norm_t norm, const void* s, mlpmoe_dtype_t s_dtype, int64_t s_stride, const float* gain,
@@ -538,8 +538,12 @@ typedef struct {
  *                  that a captured graph can be replayed
  *   lr_device      device fp32 [1], read instead of lr if not NULL
  *   grad_scale     device fp32 [1], or NULL: every gradient is multiplied by it (clipping, a loss scale's reciprocal)
- *   stochastic     not 0: codes of e4m3 moments, and params in bf16, are rounded up with the probability of the part that
- *                  truncation would cut off, with 16 random bits each from a hash of (seed, step, place in the list, element)
+ *   stochastic     not 0: codes of e4m3 moments, and params in bf16, are rounded away from zero with the probability of the part
+ *                  that truncation would cut off, by 16 random bits each.  For element i of the tensor at `place` in the list
+ *                      key = mix(place ^ mix(mix(mix(seed mod 2^32) ^ (seed >> 32)) ^ (step mod 2^32)));  key = mix(key ^ (i >> 32)) from i = 2^32 on
+ *                      h = mix(key + 0x9E3779B1 * i)  (mod 2^32; mix: the 32-bit finaliser of MurmurHash3)
+ *                  m takes h's low 16 bits, sqrt(v) its high ones, a bf16 param the low ones of mix(h ^ 0x9E3779B1).
+ *                  0: to nearest, ties to even
  */
 typedef struct {
   double lr, beta1, beta2, eps;
@@ -557,7 +561,7 @@ typedef struct {
  *     param = param - lr * weight_decay * param - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
  * The param takes the new moments before they are rounded.  e4m3 moments: scale = max(max |finite value| / 448, 2^-126) of each 128
  * elements; a root above zero is stored as the smallest code at least.  A gradient that is not finite makes its own element's param
- * and moments not finite (a NaN code), other elements of its 128 keep theirs.
+ * and moments not finite (a NaN code), other elements of its 128 keep theirs; a square past fp32's range makes its v infinite.
  * Errors before anything is enqueued: MLPMOE_ERR_INVALID_ARG (NULL, a pointer off its element's alignment, a type or setting that is
  * not allowed), MLPMOE_ERR_UNSUPPORTED (more than 2^40 elements in a tensor).
  */

@@ -82,12 +82,15 @@ def mix32(h):
     return h ^ (h >> 16)
 
 
-def adamw_noise(seed, step, tensor, n):
-    """32 random bits for each of a tensor's first n < 2^32 elements."""
+def adamw_noise(seed, step, tensor, n, first=0):
+    """32 random bits for each of n elements of a tensor from `first` on (all in the same 2^32)."""
     key = mix32(mix32(mix32(seed & M32) ^ (seed >> 32)) ^ (step & M32))
-    key = np.uint64(mix32(tensor ^ key))
+    key = mix32(tensor ^ key)
+    if first >> 32:
+        key = mix32(key ^ (first >> 32))
+    key = np.uint64(key)
     with np.errstate(over="ignore"):
-        i = np.arange(n, dtype=np.uint64)
+        i = np.arange(n, dtype=np.uint64) + np.uint64(first & M32)
         h = (key + i * np.uint64(0x9E3779B1)) & np.uint64(M32)
         for shift, mul in ((16, 0x85EBCA6B), (13, 0xC2B2AE35)):
             h = ((h ^ (h >> np.uint64(shift))) * np.uint64(mul)) & np.uint64(M32)

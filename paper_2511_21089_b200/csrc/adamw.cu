@@ -10,7 +10,6 @@
 #include <math.h>
 
 #include <cfloat>
-#include <vector>
 
 #include "../../include/mlpmoe.h"
 #include "internal.h"

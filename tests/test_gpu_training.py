@@ -560,7 +560,8 @@ def test_adamw_in_eight_bits_follows_the_moments(lib):
                 g[1::128] = 2e-3                           # twice as large from here on
         got[stochastic] = (v.float() * vs.repeat_interleave(128)).view(-1, 128)[:, 1].cpu().numpy().astype(np.float64)
     want = np.sqrt(0.99 ** 150 * (1 - 0.99 ** 150) * 1e-6 + (1 - 0.99 ** 150) * 4e-6)
-    # 400 elements, each a random walk of at most a few steps of 2^-3: the mean is within a step's half
+    # 400 elements that wander by a few steps of 2^-3 each (deviation 6 % in the oracle's arithmetic), 1 % above on average, since
+    # the square's mean is above the mean's square: within half a step of e4m3
     assert abs(got[True].mean() / want - 1) < 2.0 ** -4
     assert np.all(np.abs(got[False] / want - 1) < 1.0)
 
@@ -759,3 +760,97 @@ def test_rows_and_elements_past_32_bit_offsets(lib):
     lo, hi = p.aminmax()
     assert float(lo) == float(hi) == -0.5
     assert bool((m.view(torch.uint8) == 0x7E).all()) and bool((v.view(torch.uint8) == 0x7E).all())      # 448: each is its block's largest
+
+
+def test_adamw_past_32_bit_elements(lib):
+    """Elements on both sides of 2^32, with noise: their codes, scales and params are the oracle's."""
+    n = (1 << 32) + 4096
+    if torch.cuda.mem_get_info()[0] < 6 * n + (4 << 30):
+        pytest.skip("not enough free memory")
+    p, g = (torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda").view(TORCH["e4m3"]) for _ in range(2))
+    ms, vs = (torch.zeros(n // 128, device="cuda") for _ in range(2))
+    rng = np.random.default_rng(2)
+    parts = {first: (dev(rng.normal(size=2048) * 0.02, "bf16"), dev(rng.normal(size=2048) * 1e-3, "bf16")) for first in (0, (1 << 32) - 2048, 1 << 32, n - 2048)}
+    for first, (pp, gg) in parts.items():
+        p[first:first + 2048], g[first:first + 2048] = pp, gg
+    tensors = lib.mlpmoe_adamw_tensors([dict(n=n, param=p, grad=g, m=m, v=v, m_scale=ms, v_scale=vs, param_dtype=lib.MLPMOE_BF16,
+                                             grad_dtype=lib.MLPMOE_BF16, state_dtype=lib.MLPMOE_E4M3)])
+    lib.mlpmoe_adamw(tensors, 1e-3, step=3, stochastic=True, seed=77, stream=stream_ptr())
+    torch.cuda.synchronize()
+    for first, (pp, gg) in parts.items():
+        want_p, want_m, want_v = oracle.adamw(host(pp), host(gg), 0.0, 0.0, 1e-3, 0.9, 0.999, 1e-8, 0.0, 3)
+        noise = oracle.adamw_noise(77, 3, 0, 2048, first)
+        at = slice(first, first + 2048)
+        for x, codes, is_root in ((want_m, m, False), (np.sqrt(want_v), v, True)):
+            assert np.mean(host(codes[at]) != oracle.adamw_blocks(x, is_root, noise)[0]) <= 2e-3
+        assert np.all(np.abs(host(p[at]) - want_p) <= 2 * BF16 * np.abs(want_p) + 1e-3 * 64 * U)
+    assert not bool(p[2048:1 << 20].any()) and not bool(m.view(torch.uint8)[2048:1 << 20].any())      # zeros stay zeros
+
+
+# ------------------------------------------------------------------------------------------------ the same bits, and several threads
+
+def test_the_same_bits_every_time(lib):
+    rng = np.random.default_rng(31)
+    plan = Plan(lib, selection(rng, 3000, 40, 5), 5, 16)
+    gy, rows, w = dev(rng.normal(size=(3000, 264))), dev(rng.normal(size=(plan.rows, 264)), "bf16"), dev(rng.normal(size=(3000, 5)))
+    s, gv = dev(rng.normal(size=(3000, 264))), dev(rng.normal(size=(3000, 264)), "bf16")
+    size = lib.mlpmoe_norm_backward_workspace(3000, 264)
+    work = torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def once():
+        out = [torch.zeros(3000, 264, device="cuda"), torch.zeros_like(rows), torch.zeros(3000, 5, device="cuda"), torch.zeros(3000, 264, device="cuda"),
+               torch.zeros(264, device="cuda"), torch.zeros(264, device="cuda")]
+        plan.run(lib)
+        lib.mlpmoe_combine(rows, plan.rows, plan.token_row.t, 5, out[0], 3000, 264, weight=w, residual=gy, stream=stream_ptr())
+        lib.mlpmoe_combine_backward(gy, rows, plan.rows, plan.token_row.t, 5, out[1], out[2], 3000, 264, weight=w, B=40, align=16,
+                                    offsets=plan.offsets.t, counts=plan.counts.t, stream=stream_ptr())
+        lib.mlpmoe_norm_backward(lib.MLPMOE_LAYERNORM, s, gv, out[3], 3000, 264, work, size, grad_s=gy, grad_gain=out[4], grad_bias=out[5], stream=stream_ptr())
+        return out
+    first = once()
+    for _ in range(3):
+        work.fill_(0xEE)
+        assert all(torch.equal(a, b) for a, b in zip(first, once()))
+
+
+def test_calls_from_two_threads(lib):
+    """Two host threads with sizes and types of their own, on streams of their own, as often as one thread after the other."""
+    import threading
+    jobs = []
+    for seed, (n, d, st, gt) in enumerate([(300, 4096, "fp32", "fp32"), (500, 520, "bf16", "bf16")]):
+        rng = np.random.default_rng(seed)
+        s, gv, gs = dev(rng.normal(size=(n, d)), st), dev(rng.normal(size=(n, d)), gt), dev(rng.normal(size=(n, d)))
+        size = lib.mlpmoe_norm_backward_workspace(n, d)
+        out = [torch.zeros(n, d, device="cuda"), torch.zeros(d, device="cuda"), torch.zeros(n, d, device="cuda")]
+        jobs.append((n, d, st, gt, s, gv, gs, size, torch.empty(size, dtype=torch.uint8, device="cuda"), out))
+
+    def run(job, stream):
+        n, d, st, gt, s, gv, gs, size, work, out = job
+        for _ in range(50):
+            lib.mlpmoe_norm_backward(lib.MLPMOE_RMSNORM, s, gv, out[0], n, d, work, size, grad_s=gs, grad_gain=out[1], s_dtype=kind(lib, st),
+                                     grad_out_dtype=kind(lib, gt), stream=stream)
+            lib.mlpmoe_add_layernorm(s, gs, None, out[2], n, d, x_dtype=kind(lib, st), out_dtype=lib.MLPMOE_FP32, stream=stream)
+    wants = []
+    for job in jobs:
+        run(job, stream_ptr())
+        torch.cuda.synchronize()
+        wants.append([t.clone() for t in job[-1]])
+        for t in job[-1]:
+            t.zero_()
+    torch.cuda.synchronize()
+    streams, errors = [torch.cuda.Stream() for _ in jobs], []
+
+    def guarded(job, stream):
+        try:
+            run(job, stream.cuda_stream)
+        except Exception as e:      # noqa: BLE001 - a thread's failure is the test's
+            errors.append(e)
+    threads = [threading.Thread(target=guarded, args=(job, stream)) for job, stream in zip(jobs, streams)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors
+    for job, want in zip(jobs, wants):
+        assert all(torch.equal(a, b) for a, b in zip(job[-1], want))

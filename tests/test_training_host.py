@@ -142,8 +142,9 @@ def test_sort_sizes(lib):
     for n in (0, 1, 1024, 1025, 40000, 700000):
         for B in (1, 32, 33, 256):
             assert lib.mlpmoe_sort_workspace(n, B) >= 16
-    sizes = [lib.mlpmoe_sort_workspace(n, 64) for n in (2000, 4000, 40000, 400000, 4000000)]
-    assert sizes == sorted(sizes)
+    for B in (3, 40, 64, 128, 250):                                     # a workspace serves every smaller batch
+        sizes = [lib.mlpmoe_sort_workspace(n, B) for n in range(0, 120000, 31)] + [lib.mlpmoe_sort_workspace(n, B) for n in range(10 ** 6, 10 ** 7, 99991)]
+        assert sizes == sorted(sizes)
     for call in (lambda: lib.mlpmoe_sort_rows(-1, 8, 2), lambda: lib.mlpmoe_sort_rows(1, 0, 2), lambda: lib.mlpmoe_sort_rows(1, 8, 0),
                  lambda: lib.mlpmoe_sort_rows(1, 8, 2, 0), lambda: lib.mlpmoe_sort_workspace(-1, 8), lambda: lib.mlpmoe_sort_workspace(1, 0)):
         with pytest.raises(lib.MlpmoeError) as e:
@@ -227,6 +228,9 @@ def test_add_layernorm_refusals(lib):
 def test_norm_backward_refusals(lib):
     size = lib.mlpmoe_norm_backward_workspace(10, 64)
     assert lib.mlpmoe_norm_backward_workspace(0, 64) > 0
+    for d in (8, 256, 257, 1024, 2000, 4096, 8192, 8193, 32768):        # a workspace serves every smaller batch
+        sizes = [lib.mlpmoe_norm_backward_workspace(n, d) for n in range(0, 20000, 7)]
+        assert sizes == sorted(sizes)
 
     def call(k=1, s=FAKE, st=1, ss=0, gain=FAKE, go=FAKE, got=0, gos=0, gs=None, gst=1, gss=0, gx=FAKE + 4096, gxt=1, gxs=0, gg=FAKE, gb=FAKE, n=10, d=64,
              w=FAKE, wb=size):
