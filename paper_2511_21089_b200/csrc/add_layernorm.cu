@@ -1,6 +1,7 @@
 // Residual addition + LayerNorm + (optionally) 8-bit output with scales in one pass (mlpmoe_add_layernorm):
 //     s = x + r,  x_out = s,  v = (s - mean(s)) / sqrt(var(s) + eps) * gain + bias,  out = v | e4m3(v / scale).
 // The kernel of mlpmoe_add_rmsnorm with one sum over the row more: HBM-bound, a row in registers between its one load and its one store.
+// 16384 x 4096 fp32 + bf16 to fp32 and bf16: 805 MB in 121 us in short runs, 127 to 134 over seconds.
 #include "add_norm.cuh"
 
 extern "C" mlpmoe_status_t mlpmoe_add_layernorm(const void* x, mlpmoe_dtype_t x_dtype, int64_t x_stride, const void* r,

@@ -2,7 +2,9 @@
 //     rows of branch b = the tokens that select b, ascending;   x_rows[r] = x[token of r];
 //     y[t] = residual[t] + sum_j w[t, j] y_rows[row_j of t];    d y_rows[row_j] = w[t, j] dy[t],  d w[t, j] = <dy[t], y_rows[row_j]>.
 // Moving and summing rows is bound by memory: each kernel works from the token's side, so that what is shared by a token's rows (x, dy,
-// y) crosses memory once and the rows themselves once.  Nothing waits for another block and nothing floating is added atomically.
+// y) crosses memory once and the rows themselves once.  8192 tokens x 4096 bf16, 8 of 32 branches: rows out 605 MB in 97 us (and 8 for the
+// order), sum with an fp32 residual 806 MB in 122, gradient 1142 MB in 174: 6.2 to 6.6 TB/s.  Rows that start anywhere go at 55 to 70 %
+// of that in bf16 (two bytes a load), as fast in fp32.  Nothing waits for another block and nothing floating is added atomically.
 #include "../../include/mlpmoe.h"
 #include "internal.h"
 #include "ptx.cuh"
@@ -451,7 +453,8 @@ struct CombineGradArgs {
 };
 
 // T threads to a token (T = 32: a warp of a block of four): grad_y stays in registers, each of the token's rows is read for its
-// product with it and receives w * grad_y.  A row is read before it is written, by the same thread, so both may be one buffer.
+// product with it and receives w * grad_y.  Four rows' loads are in flight at once and their products are reduced together (8192 x 4096,
+// 8 rows a token: 174 us; one row after the other 210).  A row is read before it is written, by the same thread, so both may be one buffer.
 template <int GK, int RK, bool VEC, int T, int NCH>
 __global__ void __launch_bounds__(T == 32 ? 128 : T, T == 32 ? 8 : (T < 1024 ? 1024 / T : 1)) combine_backward_kernel(const __grid_constant__ CombineGradArgs a) {
   constexpr int kGradRows = NCH == 4 ? 1 : (NCH == 2 && !VEC ? 2 : 4);       // rows of a token under way at a time: as many as there are registers for
