@@ -113,7 +113,8 @@ def test_sort_tokens_again_and_without_branches(lib):
 MOVES = [
     # n, B, slots, align, d, pad of the rows
     (1, 1, 1, 1, 1, 0), (1, 4, 2, 8, 4096, 0), (5, 3, 3, 1, 7, 1), (33, 8, 4, 16, 896, 0), (70, 16, 4, 1, 264, 8), (65, 33, 5, 4, 1000, 3), (64, 40, 40, 1, 136, 0),
-    (300, 12, 2, 128, 520, 0), (130, 9, 3, 2, 4097, 0), (40, 6, 2, 32, 8200, 8)]
+    (300, 12, 2, 128, 520, 0), (130, 9, 3, 2, 4097, 0), (40, 6, 2, 32, 8200, 8), (37, 5, 2, 1, 257, 0), (20, 4, 2, 4, 511, 2), (9, 3, 3, 1, 3, 0),
+    (50, 6, 6, 1, 2, 1), (31, 4, 2, 8, 256, 1), (29, 4, 2, 1, 1023, 4)]
 
 
 @pytest.mark.parametrize("n,B,slots,align,d,pad", MOVES)
@@ -258,7 +259,9 @@ LAYERS = [
     (297, 896, "fp32", "bf16", "e4m3", 128, 0), (301, 1001, "bf16", "fp32", "fp32", 0, 3), (298, 1032, "fp32", "none", "bf16", 0, 0),
     (310, 4096, "bf16", "bf16", "e4m3", 0, 16), (1, 8192, "fp32", "fp32", "bf16", 0, 0), (2, 8200, "bf16", "fp32", "e4m3", 128, 0),
     (2, 20001, "fp32", "bf16", "fp32", 0, 0), (1, 32768, "fp32", "bf16", "fp32", 0, 0), (4100, 512, "fp32", "bf16", "bf16", 0, 0),
-    (4099, 100, "bf16", "fp32", "fp32", 0, 3), (1030, 4096, "fp32", "bf16", "e4m3", 128, 0), (300, 2057, "fp32", "bf16", "fp32", 0, 3)]
+    (4099, 100, "bf16", "fp32", "fp32", 0, 3), (1030, 4096, "fp32", "bf16", "e4m3", 128, 0), (300, 2057, "fp32", "bf16", "fp32", 0, 3),
+    (77, 1001, "bf16", "bf16", "bf16", 0, 0), (50, 257, "bf16", "bf16", "bf16", 0, 2), (33, 1, "bf16", "bf16", "bf16", 0, 0), (40, 515, "bf16", "none", "bf16", 0, 1),
+    (5000, 131, "bf16", "bf16", "bf16", 0, 0), (1100, 4095, "bf16", "bf16", "bf16", 0, 0)]
 
 
 @pytest.mark.parametrize("n,d,xt,rt,ot,group,pad", LAYERS)
