@@ -561,7 +561,8 @@ typedef struct {
  *     param = param - lr * weight_decay * param - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
  * The param takes the new moments before they are rounded.  e4m3 moments: scale = max(max |finite value| / 448, 2^-126) of each 128
  * elements; a root above zero is stored as the smallest code at least.  A gradient that is not finite makes its own element's param
- * and moments not finite (a NaN code), other elements of its 128 keep theirs; a square past fp32's range makes its v infinite.
+ * and moments not finite (a NaN code), other elements of its 128 keep theirs; a square past fp32's range makes its v
+ * infinite (in 8 bits a NaN code).
  * Errors before anything is enqueued: MLPMOE_ERR_INVALID_ARG (NULL, a pointer off its element's alignment, a type or setting that is
  * not allowed), MLPMOE_ERR_UNSUPPORTED (more than 2^40 elements in a tensor).
  */

@@ -5,6 +5,8 @@
 // HBM-bound: s, dv and ds are read once, a block keeps its columns' sums over all of its rows in registers, the next rows are on
 // their way while a row is reduced, and the blocks' sums are joined by a second launch in a fixed order (5 us of 16384 x 4096, hidden
 // in part; none where one block has all rows).
+#include <atomic>
+
 #include "../../include/mlpmoe.h"
 #include "internal.h"
 #include "ptx.cuh"
@@ -436,13 +438,29 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const __grid_constant__
 struct Shape {
   int threads, quads, ctas;
 };
-constexpr Shape kShapes[] = {{32, 2, 3}, {128, 2, 8}, {256, 2, 4}, {512, 2, 2}, {1024, 2, 1}};
-int shape_of(int64_t d) { return d <= 256 ? 0 : (d <= 1024 ? 1 : (d <= 2048 ? 2 : (d <= 4096 ? 3 : 4))); }
+constexpr Shape kShapes[] = {{32, 2, 3}, {64, 2, 16}, {128, 2, 8}, {256, 2, 4}, {512, 2, 2}, {1024, 2, 1}};
+int shape_of(int64_t d) { return d <= 256 ? 0 : (d <= 512 ? 1 : (d <= 1024 ? 2 : (d <= 2048 ? 3 : (d <= 4096 ? 4 : 5)))); }
 int blocks_of(int64_t n, int64_t d) {
   const int64_t need = d <= 256 ? (n + 7) / 8 : n, most = static_cast<int64_t>(kSms) * kShapes[shape_of(d)].ctas;
   const int64_t few = (need + 3) / 4 > kSms ? (need + 3) / 4 : kSms;
   const int64_t blocks = need < few ? need : few;
   return static_cast<int>(blocks < most ? blocks : most);
+}
+
+// A kernel's shared memory, once on each device: `bytes` of it for a block, and the SM's split between it and the L1 cache at its most.  Both
+// kernels of a call ask for the same split: where the join got another, the next call's blocks, which start while it runs, did not
+// find room for four to an SM (16384 x 2048, calls one after the other: 101 us, 80 with another kernel between them).
+template <typename Kernel>
+cudaError_t set_shared(Kernel kernel, int bytes, std::atomic<uint64_t>& done) {
+  int device = 0;
+  cudaError_t e = cudaGetDevice(&device);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = device < 64 ? uint64_t{1} << device : 0;
+  if (done.load(std::memory_order_acquire) & bit) return cudaSuccess;
+  if (bytes > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
 template <bool LAYER, bool WIDE, int SHAPE, int SK, int VK>
@@ -451,10 +469,9 @@ cudaError_t launch_kinds(const NormGradArgs& a, cudaStream_t st) {
   constexpr int threads = s.threads == 32 ? 256 : s.threads, rows = s.threads == 32 ? 8 : 1, more = WIDE ? 0 : kStages * rows * 16;
   constexpr int held = kStages * 4 * s.quads * threads * (bytes_of(SK) + bytes_of(VK)) + 2 * more, most = held + kStages * 16 * s.quads * threads + more;
   auto kernel = norm_backward_kernel<LAYER, s.threads, s.quads, s.ctas, WIDE, SK, VK>;
-  if (most > 47 * 1024) {      // above what a kernel has anyway; the limit is the same for every call, whatever its own size
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-    if (e != cudaSuccess) return e;
-  }
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = set_shared(kernel, most, done);      // the same for every call, whatever its own size
+  if (e != cudaSuccess) return e;
   return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks_of(a.n, a.d))), dim3(threads), static_cast<size_t>(a.ds_kind == kNone ? held : most), st, a);
 }
 template <bool LAYER, bool WIDE, int SHAPE>
@@ -473,8 +490,16 @@ cudaError_t launch_rows(const NormGradArgs& a, cudaStream_t st) {
     case 1: return launch_from<LAYER, WIDE, 1>(a, st);
     case 2: return launch_from<LAYER, WIDE, 2>(a, st);
     case 3: return launch_from<LAYER, WIDE, 3>(a, st);
-    default: return launch_from<LAYER, WIDE, 4>(a, st);
+    case 4: return launch_from<LAYER, WIDE, 4>(a, st);
+    default: return launch_from<LAYER, WIDE, 5>(a, st);
   }
+}
+
+cudaError_t launch_join(const NormGradArgs& a, bool layer, int blocks, cudaStream_t st) {
+  static std::atomic<uint64_t> done{0};
+  const cudaError_t e = set_shared(norm_join_kernel, 0, done);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(norm_join_kernel, dim3(static_cast<unsigned>((a.d + 31) / 32), layer ? 2 : 1), dim3(1024), 0, st, a, blocks);
 }
 
 int64_t stats_bytes(int64_t n, int64_t d) { return d > kOnePassD ? (n * 8 + 15) / 16 * 16 : 0; }
@@ -524,10 +549,10 @@ mlpmoe_status_t mlpmoe_norm_backward(mlpmoe_norm_t norm, const void* s, mlpmoe_d
   a.dgain = grad_gain;
   a.dbias = grad_bias;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const dim3 join_grid(static_cast<unsigned>((d_model + 31) / 32), norm == MLPMOE_LAYERNORM ? 2 : 1);
+  const bool layer = norm == MLPMOE_LAYERNORM;
   pdl_overlap_enabled() = true;
   if (n_tokens == 0) {
-    if (sums && launch_pdl(norm_join_kernel, join_grid, dim3(1024), 0, st, a, 0) != cudaSuccess) return MLPMOE_ERR_CUDA;
+    if (sums && launch_join(a, layer, 0, st) != cudaSuccess) return MLPMOE_ERR_CUDA;
     return MLPMOE_OK;
   }
   if (!s || !grad_out || !grad_x || grad_x == s || grad_x == grad_out) return MLPMOE_ERR_INVALID_ARG;
@@ -554,7 +579,7 @@ mlpmoe_status_t mlpmoe_norm_backward(mlpmoe_norm_t norm, const void* s, mlpmoe_d
   a.stats = sums && d_model > kOnePassD ? static_cast<float*>(workspace) : nullptr;
   a.partial = sums ? reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + stats_bytes(n_tokens, d_model)) : nullptr;
   cudaError_t e;
-  if (norm == MLPMOE_LAYERNORM)
+  if (layer)
     e = vec ? launch_rows<true, true>(a, st) : launch_rows<true, false>(a, st);
   else
     e = vec ? launch_rows<false, true>(a, st) : launch_rows<false, false>(a, st);
@@ -564,12 +589,12 @@ mlpmoe_status_t mlpmoe_norm_backward(mlpmoe_norm_t norm, const void* s, mlpmoe_d
   if (d_model > kOnePassD) {
     blocks = static_cast<int>(n_tokens < kSplitRows ? n_tokens : kSplitRows);
     e = launch_pdl(norm_column_sums_kernel, dim3(static_cast<unsigned>((d_model + 255) / 256), static_cast<unsigned>(blocks)), dim3(256), 0, st, a,
-                   norm == MLPMOE_LAYERNORM ? 1 : 0);
+                   layer ? 1 : 0);
     if (e != cudaSuccess) return MLPMOE_ERR_CUDA;
   } else if (blocks == 1) {
     return MLPMOE_OK;
   }
-  return launch_pdl(norm_join_kernel, join_grid, dim3(1024), 0, st, a, blocks) == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
+  return launch_join(a, layer, blocks, st) == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
 }
 
 }  // extern "C"
