@@ -328,7 +328,8 @@ GRADS = [
     (600, 2048, "fp32", "bf16", "fp32", "fp32", 0), (301, 2057, "bf16", "fp32", "fp32", "fp32", 3), (500, 4096, "fp32", "bf16", "fp32", "fp32", 0),
     (310, 4096, "bf16", "bf16", "bf16", "bf16", 16), (150, 4104, "fp32", "bf16", "fp32", "fp32", 0), (200, 8192, "fp32", "bf16", "bf16", "fp32", 0),
     (149, 8191, "bf16", "fp32", "none", "fp32", 0), (3, 8200, "fp32", "bf16", "fp32", "fp32", 0), (200, 20001, "bf16", "fp32", "fp32", "bf16", 0),
-    (65, 32768, "fp32", "bf16", "fp32", "fp32", 0)]
+    (65, 32768, "fp32", "bf16", "fp32", "fp32", 0), (900, 512, "fp32", "bf16", "fp32", "fp32", 0), (333, 513, "bf16", "bf16", "fp32", "bf16", 0),
+    (2400, 400, "bf16", "fp32", "bf16", "fp32", 1), (1200, 1024, "fp32", "fp32", "fp32", "fp32", 0), (700, 1025, "bf16", "bf16", "bf16", "bf16", 0)]
 
 
 @pytest.mark.parametrize("n,d,st,gt,rt,xt,pad", GRADS)
