@@ -433,13 +433,18 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const __grid_constant__
   }
 }
 
-// Threads of a row and blocks per SM by the row's length.  A block has four rows or more where every SM has a block, so that few sums are
+// Threads of a row (eight columns each), quads of a thread and blocks per SM, by the row's length: threads without columns cost as much as
+// the others (12264 x 4104: 139 us with 640 threads, 180 with 1024).  A block has four rows or more where every SM has a block, so that few sums are
 // left to join.
 struct Shape {
   int threads, quads, ctas;
 };
-constexpr Shape kShapes[] = {{32, 2, 3}, {64, 2, 16}, {128, 2, 8}, {256, 2, 4}, {512, 2, 2}, {1024, 2, 1}};
-int shape_of(int64_t d) { return d <= 256 ? 0 : (d <= 512 ? 1 : (d <= 1024 ? 2 : (d <= 2048 ? 3 : (d <= 4096 ? 4 : 5)))); }
+constexpr Shape kShapes[] = {{32, 2, 3}, {64, 2, 16}, {96, 2, 10}, {128, 2, 8}, {192, 2, 5}, {256, 2, 4}, {320, 2, 3}, {512, 2, 2}, {640, 2, 1}, {1024, 2, 1}};
+int shape_of(int64_t d) {      // the first whose threads have the row's columns, eight each
+  int s = 0;
+  while (kShapes[s].threads * 8 < d) ++s;
+  return s;
+}
 int blocks_of(int64_t n, int64_t d) {
   const int64_t need = d <= 256 ? (n + 7) / 8 : n, most = static_cast<int64_t>(kSms) * kShapes[shape_of(d)].ctas;
   const int64_t few = (need + 3) / 4 > kSms ? (need + 3) / 4 : kSms;
@@ -491,7 +496,11 @@ cudaError_t launch_rows(const NormGradArgs& a, cudaStream_t st) {
     case 2: return launch_from<LAYER, WIDE, 2>(a, st);
     case 3: return launch_from<LAYER, WIDE, 3>(a, st);
     case 4: return launch_from<LAYER, WIDE, 4>(a, st);
-    default: return launch_from<LAYER, WIDE, 5>(a, st);
+    case 5: return launch_from<LAYER, WIDE, 5>(a, st);
+    case 6: return launch_from<LAYER, WIDE, 6>(a, st);
+    case 7: return launch_from<LAYER, WIDE, 7>(a, st);
+    case 8: return launch_from<LAYER, WIDE, 8>(a, st);
+    default: return launch_from<LAYER, WIDE, 9>(a, st);
   }
 }
 
@@ -560,8 +569,13 @@ mlpmoe_status_t mlpmoe_norm_backward(mlpmoe_norm_t norm, const void* s, mlpmoe_d
   if (!on(s, bytes_of(s_dtype)) || !on(grad_out, bytes_of(grad_out_dtype)) || !on(grad_x, bytes_of(grad_x_dtype)) ||
       (grad_s && !on(grad_s, bytes_of(grad_s_dtype))))
     return MLPMOE_ERR_INVALID_ARG;
-  const bool vec = d_model % 8 == 0 && s_stride % 8 == 0 && on(s, 16) && grad_out_stride % 8 == 0 && on(grad_out, 16) &&
-                   grad_x_stride % 8 == 0 && on(grad_x, 16) && (!grad_s || (grad_s_stride % 8 == 0 && on(grad_s, 16))) && on(gain, 16);
+  // wide: rows in pieces of four elements, of eight above kOnePassD
+  const int64_t piece = d_model > kOnePassD ? 8 : 4;
+  auto pieces = [&](const void* p, mlpmoe_dtype_t kind, int64_t stride) {
+    return stride % piece == 0 && on(p, kind == MLPMOE_FP32 ? 16 : (piece == 8 ? 16 : 8));
+  };
+  const bool vec = d_model % piece == 0 && pieces(s, s_dtype, s_stride) && pieces(grad_out, grad_out_dtype, grad_out_stride) &&
+                   pieces(grad_x, grad_x_dtype, grad_x_stride) && (!grad_s || pieces(grad_s, grad_s_dtype, grad_s_stride)) && on(gain, 16);
   a.s = s;
   a.dv = grad_out;
   a.ds = grad_s;

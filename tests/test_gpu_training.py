@@ -329,7 +329,10 @@ GRADS = [
     (310, 4096, "bf16", "bf16", "bf16", "bf16", 16), (150, 4104, "fp32", "bf16", "fp32", "fp32", 0), (200, 8192, "fp32", "bf16", "bf16", "fp32", 0),
     (149, 8191, "bf16", "fp32", "none", "fp32", 0), (3, 8200, "fp32", "bf16", "fp32", "fp32", 0), (200, 20001, "bf16", "fp32", "fp32", "bf16", 0),
     (65, 32768, "fp32", "bf16", "fp32", "fp32", 0), (900, 512, "fp32", "bf16", "fp32", "fp32", 0), (333, 513, "bf16", "bf16", "fp32", "bf16", 0),
-    (2400, 400, "bf16", "fp32", "bf16", "fp32", 1), (1200, 1024, "fp32", "fp32", "fp32", "fp32", 0), (700, 1025, "bf16", "bf16", "bf16", "bf16", 0)]
+    (2400, 400, "bf16", "fp32", "bf16", "fp32", 1), (1200, 1024, "fp32", "fp32", "fp32", "fp32", 0), (700, 1025, "bf16", "bf16", "bf16", "bf16", 0),
+    (300, 700, "fp32", "bf16", "fp32", "bf16", 0), (200, 1100, "bf16", "bf16", "bf16", "fp32", 4), (77, 4, "fp32", "bf16", "fp32", "bf16", 0),
+    (90, 12, "bf16", "bf16", "bf16", "bf16", 4), (310, 2500, "fp32", "fp32", "bf16", "bf16", 0), (180, 4100, "fp32", "bf16", "fp32", "fp32", 0),
+    (160, 5121, "bf16", "bf16", "fp32", "bf16", 0), (66, 8196, "fp32", "bf16", "fp32", "fp32", 0)]
 
 
 @pytest.mark.parametrize("n,d,st,gt,rt,xt,pad", GRADS)
