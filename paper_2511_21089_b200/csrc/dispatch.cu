@@ -5,6 +5,8 @@
 // y) crosses memory once and the rows themselves once.  8192 tokens x 4096 bf16, 8 of 32 branches: rows out 605 MB in 97 us (and 8 for the
 // order), sum with an fp32 residual 806 MB in 122, gradient 1142 MB in 174: 6.2 to 6.6 TB/s.  Rows that start anywhere go at 55 to 70 %
 // of that in bf16 (two bytes a load), as fast in fp32.  Nothing waits for another block and nothing floating is added atomically.
+#include <cooperative_groups.h>
+
 #include "../../include/mlpmoe.h"
 #include "internal.h"
 #include "ptx.cuh"
@@ -21,7 +23,7 @@ constexpr int kMaxAlign = 1024;
 // The selection as a matrix of bits, in squares of 32 tokens x 32 branches: a lane reads its token's row, and the square
 // transposed holds, for each branch, which of the 32 tokens are in it.  First kernel: the transposed bits and their counts
 // per tile of tokens.  Second: each tile adds up the tiles before it, and every set bit's place is its branch's start plus
-// the bits before it.  A small batch is one tile and takes one launch.
+// the bits before it.  A small batch is one tile, or one cluster's, and takes one launch.
 constexpr int kSortThreads = 512;
 constexpr int kSortTiles = 592;           // tiles aimed at: four blocks per SM (131072 tokens x 32 branches: 23 us; one block per SM: 49)
 constexpr int kSortScanCounts = 16384;    // every tile adds up every tile's counts; from here on a kernel of its own does so once
@@ -38,7 +40,7 @@ struct SortArgs {
   int32_t* token_row;
   int32_t* token_branch;
   int64_t n, rows;
-  int B, B32, slots, align, tile_groups, tiles, groups, wide, scanned;
+  int B, B32, slots, align, tile_groups, tiles, groups, wide, scanned, mode;
 };
 
 // Row lane, bit j -> row j, bit lane.
@@ -136,24 +138,45 @@ __global__ void __launch_bounds__(1024) sort_scan_kernel(const __grid_constant__
   if (w == 31) a.totals[b] = run;
 }
 
-template <bool ONE>      // one tile: the bits and their counts are made here
-__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_constant__ SortArgs a) {
+// How a batch is dealt: one tile, a tile to each block of one cluster, whose blocks read one another's counts from shared memory, or any
+// number of tiles, whose bits and counts another kernel has left in memory.
+enum SortMode { ONE, CLUSTER, MANY };
+constexpr int kSortCluster = 8;
+
+template <SortMode MODE>
+__device__ __forceinline__ void sort_place(const SortArgs& a) {
   __shared__ uint32_t mask[kSortTileBits];
   __shared__ int32_t place[kSortTileBits];     // where the group's first token of the branch goes; before that scratch of the sums
-  __shared__ int32_t first[kMaxB + 1], total[kMaxB], before[kMaxB], warp_sum[kMaxB / 32];
+  __shared__ int32_t first[kMaxB + 1], total[kMaxB], before[kMaxB], own[MODE == CLUSTER ? kMaxB : 1], warp_sum[kMaxB / 32];
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, tile = blockIdx.x;
   const int64_t g0 = static_cast<int64_t>(tile) * a.tile_groups;
-  const int n_groups = static_cast<int>(min(static_cast<int64_t>(a.tile_groups), a.groups - g0));
-  if (ONE) {
-    for (int i = warp; i < n_groups; i += kSortThreads / 32) group_bits(a, i, lane, [&](int b, uint32_t m) { mask[i * a.B32 + b] = m; });
+  const int n_groups = static_cast<int>(max(int64_t{0}, min(static_cast<int64_t>(a.tile_groups), a.groups - g0)));
+  if (MODE != MANY) {
+    for (int i = warp; i < n_groups; i += kSortThreads / 32) group_bits(a, g0 + i, lane, [&](int b, uint32_t m) { mask[i * a.B32 + b] = m; });
     __syncthreads();
     if (tid < a.B32) {
       int32_t sum = 0;
+#pragma unroll 4
       for (int i = 0; i < n_groups; ++i) sum += __popc(mask[i * a.B32 + tid]);
       before[tid] = 0;
-      total[tid] = sum;
+      (MODE == ONE ? total : own)[tid] = sum;
+    }
+    if (MODE == CLUSTER) {
+      const auto cluster = cooperative_groups::this_cluster();
+      cluster.sync();
+      if (tid < a.B32) {
+        int32_t sum = 0, sum_before = 0;
+#pragma unroll
+        for (int r = 0; r < kSortCluster; ++r) {
+          const int32_t c = *cluster.map_shared_rank(&own[tid], r);
+          sum += c;
+          sum_before += r < tile ? c : 0;
+        }
+        before[tid] = sum_before;
+        total[tid] = sum;
+      }
     }
   } else {
     for (int i = tid; i < n_groups * a.B32; i += kSortThreads) mask[i] = a.mask[g0 * a.B32 + i];
@@ -247,10 +270,16 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_c
         if (a.token_branch != nullptr) branches[slot] = -1;
       }
   }
+  if (MODE == CLUSTER) cooperative_groups::this_cluster().sync();      // nobody leaves while its counts are read
 }
 
-// Tiles of a batch.  Up to 128 tokens one tile and one launch (32 branches: 2.6 us; 256 tokens 5.2, as two launches 4.8), else tiles of two
-// groups or more, four where there are many branches (8192 x 128: 9.9 us, two: 14.6), up to kSortTiles of them.
+__global__ void __launch_bounds__(kSortThreads) sort_one_kernel(const __grid_constant__ SortArgs a) { sort_place<ONE>(a); }
+__global__ void __cluster_dims__(kSortCluster, 1, 1) __launch_bounds__(kSortThreads) sort_cluster_kernel(const __grid_constant__ SortArgs a) { sort_place<CLUSTER>(a); }
+__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(const __grid_constant__ SortArgs a) { sort_place<MANY>(a); }
+
+// Tiles of a batch.  Up to 128 tokens one block (32 branches: 2.6 us; 256 tokens 5.2), up to 1024, or 2048 from 128 branches on, one
+// cluster (256 x 32 3.8 us and 1024 x 32 4.5 where two launches take 4.8 and 5.1; 2048 x 32 6.3 and 5.4), else tiles of two groups or
+// more, four where there are many branches (8192 x 128: 9.9 us, two: 14.6), up to kSortTiles of them.
 void sort_plan(int64_t n, int32_t B, SortArgs* a) {
   a->n = n;
   a->B = B;
@@ -260,16 +289,21 @@ void sort_plan(int64_t n, int32_t B, SortArgs* a) {
   int g = (a->groups + kSortTiles - 1) / kSortTiles;
   if (g < least) g = least;
   if (g > most) g = most;
+  a->mode = a->groups <= g && a->groups <= 4 ? ONE : MANY;
+  if (a->mode == MANY && a->groups <= (a->B32 >= 128 ? 64 : 32)) {
+    a->mode = CLUSTER;
+    g = (a->groups + kSortCluster - 1) / kSortCluster;
+  }
   a->tile_groups = g;
-  a->tiles = a->groups <= g ? 1 : (a->groups + g - 1) / g;
+  a->tiles = a->mode == ONE ? 1 : (a->mode == CLUSTER ? kSortCluster : (a->groups + g - 1) / g);
   a->scanned = static_cast<int64_t>(a->tiles) * a->B32 > kSortScanCounts;
 }
 
 int64_t round16(int64_t v) { return (v + 15) / 16 * 16; }
-int64_t sort_mask_bytes(const SortArgs& a) { return a.tiles == 1 ? 0 : round16(static_cast<int64_t>(a.groups) * a.B32 * 4); }
+int64_t sort_mask_bytes(const SortArgs& a) { return a.mode != MANY ? 0 : round16(static_cast<int64_t>(a.groups) * a.B32 * 4); }
 // (for as many tiles as any smaller batch has, too: a workspace serves every batch up to its own)
 int64_t sort_bytes(const SortArgs& a) {
-  if (a.tiles == 1) return 16;
+  if (a.mode != MANY) return 16;
   const int64_t aimed = a.groups < kSortTiles ? a.groups : kSortTiles, tiles = a.tiles > aimed ? a.tiles : aimed;
   return sort_mask_bytes(a) + round16((tiles + 1) * a.B32 * 4);
 }
@@ -642,12 +676,14 @@ mlpmoe_status_t mlpmoe_sort_tokens(const uint8_t* select, int64_t n_tokens, int3
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   pdl_overlap_enabled() = true;
   cudaError_t e;
-  if (a.tiles == 1) {
-    e = launch_pdl(sort_place_kernel<true>, dim3(1), dim3(kSortThreads), 0, st, a);
+  if (a.mode == ONE) {
+    e = launch_pdl(sort_one_kernel, dim3(1), dim3(kSortThreads), 0, st, a);
+  } else if (a.mode == CLUSTER) {
+    e = launch_pdl(sort_cluster_kernel, dim3(kSortCluster), dim3(kSortThreads), 0, st, a);
   } else {
     e = launch_pdl(sort_count_kernel, dim3(static_cast<unsigned>(a.tiles)), dim3(kSortThreads), 0, st, a);
     if (e == cudaSuccess && a.scanned) e = launch_pdl(sort_scan_kernel, dim3(static_cast<unsigned>(a.B32 / 32)), dim3(1024), 0, st, a);
-    if (e == cudaSuccess) e = launch_pdl(sort_place_kernel<false>, dim3(static_cast<unsigned>(a.tiles)), dim3(kSortThreads), 0, st, a);
+    if (e == cudaSuccess) e = launch_pdl(sort_place_kernel, dim3(static_cast<unsigned>(a.tiles)), dim3(kSortThreads), 0, st, a);
   }
   return e == cudaSuccess ? MLPMOE_OK : MLPMOE_ERR_CUDA;
 }

@@ -73,7 +73,7 @@ class Plan:
 @pytest.mark.parametrize("n,B,slots,align,mean", [
     (0, 3, 2, 1, 1), (1, 1, 1, 1, 1), (1, 256, 256, 1024, 9), (2, 5, 3, 8, 2), (31, 16, 4, 1, 3), (33, 5, 2, 1, 2), (64, 16, 4, 8, 4), (1000, 31, 31, 1, 6),
     (1024, 128, 8, 128, 8), (512, 256, 5, 1, 5), (513, 256, 300, 16, 20), (1025, 33, 16, 4, 7), (5000, 100, 7, 1024, 4), (4099, 32, 40, 1, 30),
-    (30001, 256, 3, 16, 2), (40000, 7, 2, 1, 1), (200000, 4, 2, 128, 2), (530001, 3, 2, 1, 1)])
+    (129, 40, 3, 8, 4), (160, 256, 9, 128, 9), (1025, 32, 8, 1, 8), (1056, 128, 4, 2, 4), (2048, 256, 8, 64, 8), (2049, 129, 8, 1, 8), (30001, 256, 3, 16, 2), (40000, 7, 2, 1, 1), (200000, 4, 2, 128, 2), (530001, 3, 2, 1, 1)])
 def test_sort_tokens(lib, n, B, slots, align, mean):
     Plan(lib, selection(np.random.default_rng([n, B]), n, B, mean), slots, align).check()
 
