@@ -4,7 +4,7 @@
 // Moving and summing rows is bound by memory: each kernel works from the token's side, so that what is shared by a token's rows (x, dy,
 // y) crosses memory once and the rows themselves once.  8192 tokens x 4096 bf16, 8 of 32 branches: rows out 605 MB in 97 us (and 8 for the
 // order), sum with an fp32 residual 806 MB in 122, gradient 1142 MB in 174: 6.2 to 6.6 TB/s.  Rows that start anywhere go at 55 to 70 %
-// of that in bf16 (two bytes a load), as fast in fp32.  Nothing waits for another block and nothing floating is added atomically.
+// of that in bf16 (two bytes a load), as fast in fp32.  No block waits for one outside of its cluster and nothing floating is added atomically.
 #include <cooperative_groups.h>
 
 #include "../../include/mlpmoe.h"
