@@ -91,9 +91,10 @@ constexpr int kStages = 2;
 // start anywhere: columns T apart, so that a warp's accesses are neighbours), whose sums over
 // the block's rows stay in registers.  The next row is on its way to shared memory meanwhile; a thread reads only what it
 // copied itself, so that takes no barrier (not WIDE: two).  16384 x 4096, fp32 and bf16: 940 MB in
-// 149 us with the join (floor 146).  The row ahead in registers and types told apart as it runs: 258 (98 registers, 512 threads per SM); four
+// 157 us with the join over seconds (floor 146).  The row ahead in registers and types told apart as it runs: 258 (98 registers, 512 threads per SM); four
 // times four columns a thread: 159 (16 warps per SM).
-template <bool LAYER, int T, int Q, int CTAS, bool WIDE, int SK, int VK>
+// FULL: ds is there, and it and dx are fp32 (told apart as it runs, the same case takes 11 % more instructions and 167 us over seconds, not 157).
+template <bool LAYER, int T, int Q, int CTAS, bool WIDE, int SK, int VK, bool FULL>
 __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(const __grid_constant__ NormGradArgs a) {
   constexpr bool WARP = T == 32;
   constexpr int R = WARP ? 8 : 1, THREADS = WARP ? 256 : T, SB = bytes_of(SK), VB = bytes_of(VK);
@@ -101,8 +102,8 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
   __shared__ float red[2][T / 32][4];
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
-  const int d = a.d, tid = WARP ? threadIdx.x % 32 : threadIdx.x, rb = bytes_of(a.ds_kind), xb = bytes_of(a.dx_kind);
-  const bool has_r = a.ds_kind != kNone, r32 = a.ds_kind == MLPMOE_FP32, x32 = a.dx_kind == MLPMOE_FP32;
+  const int d = a.d, tid = WARP ? threadIdx.x % 32 : threadIdx.x, rb = FULL ? 4 : bytes_of(a.ds_kind), xb = FULL ? 4 : bytes_of(a.dx_kind);
+  const bool has_r = FULL || a.ds_kind != kNone, r32 = FULL || a.ds_kind == MLPMOE_FP32, x32 = FULL || a.dx_kind == MLPMOE_FP32;
   const int64_t step = static_cast<int64_t>(gridDim.x) * R, first = static_cast<int64_t>(blockIdx.x) * R + (WARP ? threadIdx.x / 32 : 0);
   const int rows = first < a.n ? static_cast<int>((a.n - first + step - 1) / step) : 0;      // of this block or warp
   const int col = WIDE ? tid * 4 : tid, base = WIDE ? col : 0;      // the thread's first column, and the pointers'
@@ -140,7 +141,7 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
           if (col + c >= d) continue;
           copy_quad(mine_s + at * (THREADS * 4 * SB), ps + c * SB, SK);
           copy_quad(mine_v + at * (THREADS * 4 * VB), pv + c * VB, VK);
-          if (has_r) copy_quad(mine_r + at * (THREADS * 16), pr + c * rb, a.ds_kind);
+          if (has_r) copy_quad(mine_r + at * (THREADS * 16), pr + c * rb, FULL ? MLPMOE_FP32 : a.ds_kind);
         }
       } else {
         fetched.s = copy_row<T>(mine_s + stage * S_ROW, ps, SB, d, tid);
@@ -468,16 +469,22 @@ cudaError_t set_shared(Kernel kernel, int bytes, std::atomic<uint64_t>& done) {
   return e;
 }
 
-template <bool LAYER, bool WIDE, int SHAPE, int SK, int VK>
-cudaError_t launch_kinds(const NormGradArgs& a, cudaStream_t st) {
+template <bool LAYER, bool WIDE, int SHAPE, int SK, int VK, bool FULL>
+cudaError_t launch_kernel(const NormGradArgs& a, cudaStream_t st) {
   constexpr Shape s = kShapes[SHAPE];
   constexpr int threads = s.threads == 32 ? 256 : s.threads, rows = s.threads == 32 ? 8 : 1, more = WIDE ? 0 : kStages * rows * 16;
   constexpr int held = kStages * 4 * s.quads * threads * (bytes_of(SK) + bytes_of(VK)) + 2 * more, most = held + kStages * 16 * s.quads * threads + more;
-  auto kernel = norm_backward_kernel<LAYER, s.threads, s.quads, s.ctas, WIDE, SK, VK>;
+  auto kernel = norm_backward_kernel<LAYER, s.threads, s.quads, s.ctas, WIDE, SK, VK, FULL>;
   static std::atomic<uint64_t> done{0};
   const cudaError_t e = set_shared(kernel, most, done);      // the same for every call, whatever its own size
   if (e != cudaSuccess) return e;
   return launch_pdl(kernel, dim3(static_cast<unsigned>(blocks_of(a.n, a.d))), dim3(threads), static_cast<size_t>(a.ds_kind == kNone ? held : most), st, a);
+}
+template <bool LAYER, bool WIDE, int SHAPE, int SK, int VK>
+cudaError_t launch_kinds(const NormGradArgs& a, cudaStream_t st) {
+  constexpr bool kStream = WIDE && SK == MLPMOE_FP32;      // an fp32 residual stream
+  if (kStream && a.ds_kind == MLPMOE_FP32 && a.dx_kind == MLPMOE_FP32) return launch_kernel<LAYER, WIDE, SHAPE, SK, VK, kStream>(a, st);
+  return launch_kernel<LAYER, WIDE, SHAPE, SK, VK, false>(a, st);
 }
 template <bool LAYER, bool WIDE, int SHAPE>
 cudaError_t launch_from(const NormGradArgs& a, cudaStream_t st) {
