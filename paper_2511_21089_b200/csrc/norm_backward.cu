@@ -98,7 +98,7 @@ template <bool LAYER, int T, int Q, int CTAS, bool WIDE, int SK, int VK, bool FU
 __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(const __grid_constant__ NormGradArgs a) {
   constexpr bool WARP = T == 32;
   constexpr int R = WARP ? 8 : 1, THREADS = WARP ? 256 : T, SB = bytes_of(SK), VB = bytes_of(VK);
-  extern __shared__ char staged[];
+  extern __shared__ __align__(16) char staged[];
   __shared__ float red[2][T / 32][4];
   ptx::griddep_launch_dependents();
   ptx::griddep_wait();
