@@ -9,6 +9,7 @@
 
 #include "../../include/mlpmoe.h"
 #include "internal.h"
+#include "norm_shapes.h"
 #include "ptx.cuh"
 #include "row_io.cuh"
 
@@ -16,10 +17,7 @@ namespace mlpmoe {
 namespace {
 
 constexpr int kNone = 2;
-constexpr int kSms = 148;
 constexpr int64_t kMaxD = 32768;
-constexpr int64_t kOnePassD = 8192;      // longer rows do not leave room for their columns' sums in registers
-constexpr int kSplitRows = 64;           // slices of the rows there, for the sums over tokens
 
 struct NormGradArgs {
   const void* s;
@@ -434,25 +432,6 @@ __global__ void __launch_bounds__(1024) norm_join_kernel(const __grid_constant__
   }
 }
 
-// Threads of a row (eight columns each), quads of a thread and blocks per SM, by the row's length: threads without columns cost as much as
-// the others (12264 x 4104: 139 us with 640 threads, 180 with 1024).  A block has four rows or more where every SM has a block, so that few sums are
-// left to join.
-struct Shape {
-  int threads, quads, ctas;
-};
-constexpr Shape kShapes[] = {{32, 2, 3}, {64, 2, 16}, {96, 2, 10}, {128, 2, 8}, {192, 2, 5}, {256, 2, 4}, {320, 2, 3}, {512, 2, 2}, {640, 2, 1}, {1024, 2, 1}};
-int shape_of(int64_t d) {      // the first whose threads have the row's columns, eight each
-  int s = 0;
-  while (kShapes[s].threads * 8 < d) ++s;
-  return s;
-}
-int blocks_of(int64_t n, int64_t d) {
-  const int64_t need = d <= 256 ? (n + 7) / 8 : n, most = static_cast<int64_t>(kSms) * kShapes[shape_of(d)].ctas;
-  const int64_t few = (need + 3) / 4 > kSms ? (need + 3) / 4 : kSms;
-  const int64_t blocks = need < few ? need : few;
-  return static_cast<int>(blocks < most ? blocks : most);
-}
-
 // A kernel's shared memory, once on each device: `bytes` of it for a block, and the SM's split between it and the L1 cache at its most.  Both
 // kernels of a call ask for the same split: where the join got another, the next call's blocks, which start while it runs, did not
 // find room for four to an SM (16384 x 2048, calls one after the other: 101 us, 80 with another kernel between them).
@@ -520,7 +499,7 @@ cudaError_t launch_join(const NormGradArgs& a, bool layer, int blocks, cudaStrea
 
 int64_t stats_bytes(int64_t n, int64_t d) { return d > kOnePassD ? (n * 8 + 15) / 16 * 16 : 0; }
 int64_t grad_bytes(int64_t n, int64_t d) {
-  const int64_t blocks = d > kOnePassD ? kSplitRows : blocks_of(n, d);
+  const int64_t blocks = d > kOnePassD ? kSplitRows : blocks_of(n, d);      // (of long rows always all of them)
   return stats_bytes(n, d) + (blocks > 0 ? blocks : 1) * 2 * d * 4;
 }
 
@@ -606,9 +585,8 @@ mlpmoe_status_t mlpmoe_norm_backward(mlpmoe_norm_t norm, const void* s, mlpmoe_d
     e = vec ? launch_rows<false, true>(a, st) : launch_rows<false, false>(a, st);
   if (e != cudaSuccess) return MLPMOE_ERR_CUDA;
   if (!sums) return MLPMOE_OK;
-  int blocks = blocks_of(n_tokens, d_model);
+  const int blocks = blocks_of(n_tokens, d_model);
   if (d_model > kOnePassD) {
-    blocks = static_cast<int>(n_tokens < kSplitRows ? n_tokens : kSplitRows);
     e = launch_pdl(norm_column_sums_kernel, dim3(static_cast<unsigned>((d_model + 255) / 256), static_cast<unsigned>(blocks)), dim3(256), 0, st, a,
                    layer ? 1 : 0);
     if (e != cudaSuccess) return MLPMOE_ERR_CUDA;
