@@ -387,10 +387,12 @@ def mlpmoe_norm_backward_workspace(n_tokens: int, d_model: int) -> int:
 
 
 def mlpmoe_norm_backward(norm: int, s, grad_out, grad_x, n_tokens: int, d_model: int, workspace=None, workspace_bytes: int = 0, gain=None,
-                         grad_s=None, grad_gain=None, grad_bias=None, eps: float = 1e-6, s_dtype: int = MLPMOE_FP32,
+                         grad_s=None, grad_gain=None, grad_bias=None, eps: Optional[float] = None, s_dtype: int = MLPMOE_FP32,
                          grad_out_dtype: int = MLPMOE_BF16, grad_s_dtype: int = MLPMOE_FP32, grad_x_dtype: int = MLPMOE_FP32,
                          s_stride: int = 0, grad_out_stride: int = 0, grad_s_stride: int = 0, grad_x_stride: int = 0, stream=None) -> None:
-    """norm: MLPMOE_RMSNORM or MLPMOE_LAYERNORM, with the eps of the forward call; s: its x_out."""
+    """norm: MLPMOE_RMSNORM or MLPMOE_LAYERNORM; eps: the forward call's (None: that call's default, 1e-6 or 1e-5); s: its x_out."""
+    if eps is None:
+        eps = 1e-5 if norm == MLPMOE_LAYERNORM else 1e-6
     _check(lib.mlpmoe_norm_backward(norm, _ptr(s), s_dtype, s_stride, _ptr(gain), _ptr(grad_out), grad_out_dtype, grad_out_stride, _ptr(grad_s),
                                     grad_s_dtype, grad_s_stride, _ptr(grad_x), grad_x_dtype, grad_x_stride, _ptr(grad_gain), _ptr(grad_bias),
                                     n_tokens, d_model, eps, _ptr(workspace), workspace_bytes, _stream(stream)), "mlpmoe_norm_backward")

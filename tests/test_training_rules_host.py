@@ -42,3 +42,23 @@ def test_norm_gradient_shapes_of_every_row_length(tmp_path, first, last, step):
     r = subprocess.run([compiler, "-std=c++17", "-fconstexpr-ops-limit=1000000000", "-fconstexpr-loop-limit=1000000", "-fsyntax-only", "-I", CSRC, str(source)],
                        capture_output=True, text=True)
     assert r.returncode == 0, r.stderr[-2000:]
+
+
+def test_a_norm_and_its_gradient_have_the_same_default_eps(lib, monkeypatch):
+    seen = {}
+
+    def taken(name, at):
+        def call(*args):
+            seen[name] = args[at]
+            return lib.MLPMOE_OK
+        monkeypatch.setattr(lib.lib, name, call)
+    for name in ("mlpmoe_add_rmsnorm", "mlpmoe_add_layernorm"):
+        taken(name, -2)                                  # eps, stream
+    taken("mlpmoe_norm_backward", -4)                    # eps, workspace, its bytes, stream
+    for norm, forward, name in ((lib.MLPMOE_RMSNORM, lib.mlpmoe_add_rmsnorm, "mlpmoe_add_rmsnorm"),
+                                (lib.MLPMOE_LAYERNORM, lib.mlpmoe_add_layernorm, "mlpmoe_add_layernorm")):
+        forward(0x10000, None, 0x20000, 0x30000, 4, 64)
+        lib.mlpmoe_norm_backward(norm, 0x20000, 0x40000, 0x50000, 4, 64)
+        assert seen["mlpmoe_norm_backward"] == seen[name]
+        lib.mlpmoe_norm_backward(norm, 0x20000, 0x40000, 0x50000, 4, 64, eps=0.25)
+        assert seen["mlpmoe_norm_backward"] == 0.25
