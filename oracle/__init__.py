@@ -49,5 +49,6 @@ from .training_oracle import (  # noqa: F401
     adamw_noise,
     e4m3_up_or_down,
     adamw_blocks,
+    bf16_up_or_down,
     adamw,
 )

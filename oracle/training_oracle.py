@@ -118,6 +118,13 @@ def adamw_blocks(x, root, noise=None):
     return codes, scales
 
 
+def bf16_up_or_down(p, noise):
+    """p, rounded to fp32, in bf16: away from zero where the 16 bits of mix32(noise ^ 0x9E3779B1) and the cut-off 16 bits make up a step."""
+    extra = np.array([mix32(int(h) ^ 0x9E3779B1) & 0xFFFF for h in noise], np.uint64)
+    bits = np.asarray(p, np.float64).astype(np.float32).view(np.uint32).astype(np.uint64)
+    return ((bits + extra) & np.uint64(0xFFFF0000)).astype(np.uint32).view(np.float32).astype(np.float64)
+
+
 def adamw(p, g, m, v, lr, beta1, beta2, eps, weight_decay, step, grad_scale=1.0):
     """(p, m, v) after the step, all in float64."""
     g = g * grad_scale

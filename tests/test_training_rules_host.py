@@ -1,9 +1,12 @@
-"""CPU-side tests of the rules by which the operators of a training step deal their work and default their arguments."""
+"""CPU-side tests of the rules by which the operators of a training step deal their work, default their arguments and round with noise."""
 import os
 import shutil
 import subprocess
 
+import numpy as np
 import pytest
+
+import oracle
 
 CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2511_21089_b200", "csrc")
 
@@ -62,3 +65,48 @@ def test_a_norm_and_its_gradient_have_the_same_default_eps(lib, monkeypatch):
         assert seen["mlpmoe_norm_backward"] == seen[name]
         lib.mlpmoe_norm_backward(norm, 0x20000, 0x40000, 0x50000, 4, 64, eps=0.25)
         assert seen["mlpmoe_norm_backward"] == 0.25
+
+
+# ----------------------------------------------------------------------------- params in bf16, rounded with noise
+
+def test_bf16_rounding_pins():
+    """The added bits are the low half of mix32(noise ^ 0x9E3779B1), and what is left below bf16 is cut off."""
+    for noise in (0, 1, 0x12345678, 0xFFFFFFFF):
+        low = oracle.mix32(noise ^ 0x9E3779B1) & 0xFFFF
+        for sign in (0, 0x80000000):
+            for cut, up in ((0, 0), (65535 - low, 0), (65536 - low, 1 if low else None), (65535, 1 if low else 0)):
+                if up is None:
+                    continue
+                bits = np.array([sign | 0x3F800000 + cut], np.uint32)
+                want = np.array([sign | 0x3F800000 + 0x10000 * up], np.uint32).view(np.float32)[0]
+                assert oracle.bf16_up_or_down(bits.view(np.float32).astype(np.float64), [noise])[0] == want, (noise, sign, cut)
+
+
+@pytest.mark.parametrize("p", [1.0, 1.0 + 2.0 ** -9, -1.003, 0.0199, 3e-5, -127.6])
+def test_bf16_rounding_has_the_right_mean(p):
+    noise = oracle.adamw_noise(5, 1, 0, 100000)
+    got = oracle.bf16_up_or_down(np.full(100000, p), noise)
+    p = float(np.float32(p))
+    step = 2.0 ** (np.floor(np.log2(abs(p))) - 7)
+    assert set(np.unique(np.abs(got))) <= {np.floor(abs(p) / step) * step, (np.floor(abs(p) / step) + 1) * step}
+    # a coin of deviation step / 2 at most, 100000 times
+    assert abs(got.mean() - p) <= 5 * step / 2 / np.sqrt(100000)
+
+
+def test_other_roundings_to_bf16_are_told_apart():
+    """Truncation, away from zero, to nearest, and other words of the noise give another neighbour for a fifth of the elements or more."""
+    rng = np.random.default_rng(6)
+    p, noise = (rng.normal(size=20000) * 0.02).astype(np.float32), oracle.adamw_noise(6, 2, 1, 20000)
+    want = oracle.bf16_up_or_down(p, noise)
+    bits = p.view(np.uint32).astype(np.uint64)
+
+    def plus(extra):
+        return ((bits + np.asarray(extra, np.uint64)) & np.uint64(0xFFFF0000)).astype(np.uint32).view(np.float32)
+    mixed = np.array([oracle.mix32(int(h) ^ 0x9E3779B1) for h in noise], np.uint64)
+    others = {"truncated": plus(0), "away": plus(0xFFFF), "nearest": plus(0x7FFF), "unmixed": plus(noise & np.uint64(0xFFFF)),
+              "high half": plus(mixed >> np.uint64(16))}
+    for name, other in others.items():
+        # two independent coins of the same odds differ for 2 q (1 - q), a third on average; nearest and a coin for a quarter
+        assert np.mean(other != want) > 0.2, name
+    assert abs(np.mean((np.abs(want) - np.abs(p)) / 2.0 ** (np.floor(np.log2(np.abs(p))) - 7))) < 5 * 0.5 / np.sqrt(20000)
+    assert np.mean((np.abs(others["truncated"]) - np.abs(p)) / 2.0 ** (np.floor(np.log2(np.abs(p))) - 7)) < -0.4
