@@ -1,4 +1,5 @@
-"""GPU tests of the operators of a training step, beside tests/test_gpu_training.py: bf16 params rounded with noise."""
+"""GPU tests of the operators of a training step, beside tests/test_gpu_training.py: rounding with noise and to nearest, scales, far offsets, very
+large batches."""
 import numpy as np
 import pytest
 import torch
@@ -83,3 +84,67 @@ def test_bf16_params_past_32_bit_elements_rounded_with_noise(lib):
         zero = np.zeros(2048)
         want, off = step_of((p0, g, zero, zero), 1e-3, 0.9, 0.999, 1e-8, 0.0, 3, 1.0)
         check_rounded_with_noise(host(p[first:first + 2048]), want, off, oracle.adamw_noise(78, 3, 0, 2048, first))
+
+
+# ------------------------------------------------------------------------------------------------ 8-bit moments: scales, and to nearest
+
+def test_scales_past_32_bit_elements(lib):
+    """The scales of the stretches on both sides of 2^32, and those of zeros everywhere else."""
+    parts, _, ms, vs = far_step(lib)
+    rest = torch.ones(ms.numel(), dtype=torch.bool, device="cuda")
+    for first, (_, g) in parts.items():
+        at = slice(first // 128, first // 128 + 16)
+        rest[at] = False
+        m, root = 0.1 * g, np.sqrt(0.001) * np.abs(g)
+        for x, scales, off in ((m, ms, 5 * U), (root, vs, 5 * U)):
+            want = oracle.adamw_blocks(x, False)[1]
+            # the largest value's error, then the quotient by 448: 3 u
+            assert np.all(np.abs(host(scales[at]) - want) <= (off + 3 * U) * want)
+    for scales in (ms, vs):
+        assert bool((scales[rest] == 2.0 ** -126).all())
+
+
+def test_roots_to_nearest_stay_behind(lib):
+    """The arithmetic of 300 steps to nearest in 64 bits, block by block, and that it does stay behind what the gradients ask for."""
+    n, lr, b1, b2, eps = 128 * 400, 1e-5, 0.9, 0.99, 1e-8
+    g = np.full(128, float(np.float32(1e-3)))
+    g[0] = float(np.float32(4e-3))
+    p, m, v = np.zeros(128), np.zeros(128), np.zeros(128)
+    gd = dev(np.tile(g, n // 128))
+    pd, md, vd = torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda").to(TORCH["e4m3"]), torch.zeros(n, device="cuda").to(TORCH["e4m3"])
+    ms, vs = torch.zeros(n // 128, device="cuda"), torch.zeros(n // 128, device="cuda")
+    tensors = lib.mlpmoe_adamw_tensors([dict(n=n, param=pd, grad=gd, m=md, v=vd, m_scale=ms, v_scale=vs, state_dtype=lib.MLPMOE_E4M3)])
+    for step in range(1, 301):
+        lib.mlpmoe_adamw(tensors, lr, b1, b2, eps, step=step, stream=stream_ptr())
+        p, m, v = oracle.adamw(p, g, m, v, lr, b1, b2, eps, 0.0, step)
+        (cm, sm), (cv, sv) = oracle.adamw_blocks(m, False), oracle.adamw_blocks(np.sqrt(v), True)
+        m, v = cm * sm[0], (cv * sv[0]) ** 2
+        if step == 150:
+            g[1] = float(np.float32(2e-3))
+            gd[1::128] = 2e-3
+    got = host((vd.float() * vs.repeat_interleave(128)).view(-1, 128))
+    assert np.all(got == got[0])                           # every block has the same values, and the rounding no noise
+    assert np.all(np.abs(got[0] - np.sqrt(v)) <= 2.0 ** -3 * np.sqrt(v))      # one step of e4m3, where a value lies at a border
+    want = np.sqrt(0.99 ** 150 * (1 - 0.99 ** 150) * 1e-6 + (1 - 0.99 ** 150) * 4e-6)
+    assert got[0, 1] < 0.75 * want
+
+
+# ------------------------------------------------------------------------------------------------ rows past 32-bit offsets
+
+def test_weights_gradient_of_rows_past_32_bit_offsets(lib):
+    d, R = 32768, 70000
+    far = [0, 40000, 65535, 65536, R - 1]
+    rng = np.random.default_rng(3)
+    x, gy = dev(rng.normal(size=(len(far), d)), "bf16"), dev(rng.normal(size=(len(far), d)), "bf16")
+    rows = torch.full((R, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    rows[far] = x
+    place = torch.tensor([[r] for r in far], dtype=torch.int32, device="cuda")
+    gw, alone = torch.empty(len(far), 1, device="cuda"), torch.empty(len(far), 1, device="cuda")
+    lib.mlpmoe_combine_backward(gy, rows, R, place, 1, None, alone, len(far), d, grad_y_dtype=lib.MLPMOE_BF16, stream=stream_ptr())
+    lib.mlpmoe_combine_backward(gy, rows, R, place, 1, rows, gw, len(far), d, grad_y_dtype=lib.MLPMOE_BF16, stream=stream_ptr())
+    torch.cuda.synchronize()
+    terms = host(gy) * host(x)
+    # a thread's 32 terms, five steps in a warp, 32 warps one after the other: fewer than 80 roundings of partial sums
+    for got in (alone, gw):
+        assert np.all(np.abs(host(got)[:, 0] - terms.sum(1)) <= 80 * U * np.abs(terms).sum(1))
+    assert torch.equal(rows[far], gy)
