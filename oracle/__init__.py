@@ -41,6 +41,7 @@ from .operators_oracle import (  # noqa: F401
 )
 from .training_oracle import (  # noqa: F401
     sort_tokens,
+    sort_tokens_of_many,
     combine,
     combine_grad,
     add_layernorm,

@@ -30,6 +30,24 @@ def sort_tokens(select, slots, align):
     return {"offsets": offsets, "counts": counts, "row_token": np.array(row_token, np.int64), "token_row": token_row, "token_branch": token_branch}
 
 
+def sort_tokens_of_many(select, slots, align):
+    """sort_tokens, a branch at a time."""
+    taken = select != 0
+    place = np.cumsum(taken, axis=1, dtype=np.int16)
+    taken &= place <= slots
+    n, B = taken.shape
+    counts = taken.sum(axis=0)
+    offsets = np.concatenate(([0], np.cumsum(-(-counts // align) * align)))
+    row_token = np.full(offsets[B], -1, np.int64)
+    token_row, token_branch = np.full((n, slots), -1, np.int64), np.full((n, slots), -1, np.int64)
+    for b in range(B):
+        t = np.flatnonzero(taken[:, b])
+        row = offsets[b] + np.arange(t.size)
+        row_token[row] = t
+        token_row[t, place[t, b] - 1], token_branch[t, place[t, b] - 1] = row, b
+    return {"offsets": offsets, "counts": counts, "row_token": row_token, "token_row": token_row, "token_branch": token_branch}
+
+
 def combine(rows, token_row, weight=None, residual=None):
     n, slots = token_row.shape
     y = np.zeros((n, rows.shape[1]))

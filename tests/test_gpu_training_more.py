@@ -5,9 +5,9 @@ import pytest
 import torch
 
 import oracle
-from tests.helpers import stream_ptr
+from tests.helpers import Guarded, stream_ptr
 from tests.test_gpu_operators import TORCH, U, dev, host
-from tests.test_gpu_training import TINY, Param
+from tests.test_gpu_training import TINY, Param, Plan, selection
 
 pytestmark = pytest.mark.gpu
 
@@ -148,3 +148,21 @@ def test_weights_gradient_of_rows_past_32_bit_offsets(lib):
     for got in (alone, gw):
         assert np.all(np.abs(host(got)[:, 0] - terms.sum(1)) <= 80 * U * np.abs(terms).sum(1))
     assert torch.equal(rows[far], gy)
+
+
+# ------------------------------------------------------------------------------------------------ the order of very large batches
+
+@pytest.mark.parametrize("n,B,slots,align,mean", [
+    (606208, 32, 2, 128, 1), (606209, 32, 2, 128, 1), (303105, 256, 1, 1, 2), (320001, 256, 2, 16, 2), (620001, 3, 2, 1, 1), (483000, 100, 3, 64, 2),
+    (2500001, 17, 1, 1, 1)])
+def test_sort_tokens_of_more_tiles_than_are_aimed_at(lib, monkeypatch, n, B, slots, align, mean):
+    """From 592 tiles of the largest size on, more tiles are made; and the workspace of a larger batch serves."""
+    monkeypatch.setattr(oracle, "sort_tokens", oracle.sort_tokens_of_many)
+    plan = Plan(lib, selection(np.random.default_rng([n, B]), n, B, mean), slots, align)
+    plan.check()
+    plan.work = Guarded((lib.mlpmoe_sort_workspace(3 * n, B),), torch.uint8)
+    plan.work.t.fill_(0xEE)
+    for buffer in (plan.offsets, plan.counts, plan.token_row, plan.token_branch):
+        buffer.t.fill_(-7)
+    plan.run(lib)
+    plan.check()

@@ -110,3 +110,25 @@ def test_other_roundings_to_bf16_are_told_apart():
         assert np.mean(other != want) > 0.2, name
     assert abs(np.mean((np.abs(want) - np.abs(p)) / 2.0 ** (np.floor(np.log2(np.abs(p))) - 7))) < 5 * 0.5 / np.sqrt(20000)
     assert np.mean((np.abs(others["truncated"]) - np.abs(p)) / 2.0 ** (np.floor(np.log2(np.abs(p))) - 7)) < -0.4
+
+
+# ----------------------------------------------------------------------------- the sorted order of many tokens
+
+@pytest.mark.parametrize("n,B,slots,align", [(1, 1, 1, 1), (70, 9, 2, 4), (200, 256, 300, 16), (333, 3, 1, 128)])
+def test_sorted_order_a_branch_at_a_time(n, B, slots, align):
+    rng = np.random.default_rng([n, B])
+    select = (rng.uniform(size=(n, B)) < 0.4).astype(np.uint8) * rng.integers(1, 256, (n, B)).astype(np.uint8)
+    want, got = oracle.sort_tokens(select, slots, align), oracle.sort_tokens_of_many(select, slots, align)
+    assert all(np.array_equal(want[name], got[name]) for name in want)
+
+
+def test_sort_workspace_serves_smaller_batches_past_the_largest_tiles(lib):
+    """Batches on both sides of the size from which tiles no longer grow and more of them are made."""
+    for B, most in ((3, 32), (64, 32), (128, 32), (129, 25), (200, 18), (256, 16)):
+        at = 592 * most * 32
+        sizes = [lib.mlpmoe_sort_workspace(n, B) for n in list(range(at - 64 * 31, at + 64 * 31, 31)) + [2 * at, 5 * at]]
+        assert sizes == sorted(sizes)
+        B32 = -(-B // 32) * 32
+        for n, size in ((at, sizes[64]), (2 * at, sizes[-2])):
+            groups = -(-n // 32)
+            assert size >= groups * B32 * 4 + (-(-groups // most) + 1) * B32 * 4      # the bits, and the tiles' counts with their totals
