@@ -166,3 +166,50 @@ def test_sort_tokens_of_more_tiles_than_are_aimed_at(lib, monkeypatch, n, B, slo
         buffer.t.fill_(-7)
     plan.run(lib)
     plan.check()
+
+
+# ------------------------------------------------------------------------------------------------ calls again
+
+def test_a_step_with_gradients_that_move(lib):
+    """A list whose gradients' addresses alone are renewed, against one built anew for every step."""
+    kinds = [(5000, "fp32", "bf16", "e4m3"), (777, "bf16", "fp32", "fp32"), (4096, "fp32", "fp32", "fp32")]
+    a, b = ([Param(np.random.default_rng(i), *k) for i, k in enumerate(kinds)] for _ in range(2))
+    tensors = lib.mlpmoe_adamw_tensors([dict(p.record(lib), grad=p.g.data_ptr()) for p in a])
+    rng = np.random.default_rng(5)
+    kept = []
+    for step in (1, 2, 3):
+        grads = [dev(rng.normal(size=n) * 1e-3, gt) for n, _, gt, _ in kinds]
+        kept.append(grads)                                 # the next step's lie elsewhere
+        for t, g in zip(tensors, grads):
+            t.grad = g.data_ptr()
+        lib.mlpmoe_adamw(tensors, 1e-3, step=step, stochastic=True, seed=4, stream=stream_ptr())
+        anew = lib.mlpmoe_adamw_tensors([dict(p.record(lib), grad=g) for p, g in zip(b, grads)])
+        lib.mlpmoe_adamw(anew, 1e-3, step=step, stochastic=True, seed=4, stream=stream_ptr())
+        torch.cuda.synchronize()
+        for x, y in zip(a, b):
+            for name in ("p", "m", "v"):
+                assert torch.equal(getattr(x, name).view(torch.uint8), getattr(y, name).view(torch.uint8)), (step, name)
+
+
+@pytest.mark.parametrize("pt,gt,state,copy,shift", [("fp32", "bf16", "e4m3", True, 0), ("bf16", "bf16", "e4m3", False, 0), ("bf16", "fp32", "fp32", False, 1)])
+def test_a_step_gives_the_same_bits_every_time(lib, pt, gt, state, copy, shift):
+    """Also while steps over other tensors are under way on another stream."""
+    params = Param(np.random.default_rng(8), 1 << 20, pt, gt, state, copy, shift)
+    other = Param(np.random.default_rng(9), 1 << 22, "fp32", "bf16", "e4m3")
+    start = [b.raw.clone() for b in params.guards]
+    one, two = (lib.mlpmoe_adamw_tensors([p.record(lib)]) for p in (params, other))
+    side = torch.cuda.Stream()
+    wants = None
+    for again in range(5):
+        for b, s in zip(params.guards, start):
+            b.raw.copy_(s)
+        torch.cuda.synchronize()
+        for _ in range(again):
+            lib.mlpmoe_adamw(two, 1e-3, step=1, stochastic=True, seed=2, stream=side.cuda_stream)
+        for step in (1, 2):
+            lib.mlpmoe_adamw(one, 1e-3, step=step, stochastic=True, seed=2, stream=stream_ptr())
+        torch.cuda.synchronize()
+        got = [b.raw.clone() for b in params.guards]
+        wants = wants or got
+        assert all(torch.equal(x, y) for x, y in zip(got, wants))
+    assert any(not torch.equal(x, y) for x, y in zip(start, wants))

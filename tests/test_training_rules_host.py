@@ -132,3 +132,26 @@ def test_sort_workspace_serves_smaller_batches_past_the_largest_tiles(lib):
         for n, size in ((at, sizes[64]), (2 * at, sizes[-2])):
             groups = -(-n // 32)
             assert size >= groups * B32 * 4 + (-(-groups // most) + 1) * B32 * 4      # the bits, and the tiles' counts with their totals
+
+
+# ----------------------------------------------------------------------------- the list of an optimizer step
+
+def test_a_list_of_tensors_takes_addresses_and_new_gradients(lib):
+    import gc
+    import weakref
+
+    import torch
+    p, g, m, v = (torch.zeros(8) for _ in range(4))
+    tensors = lib.mlpmoe_adamw_tensors([dict(n=8, param=p, grad=g.data_ptr(), m=m, v=v)])
+    gone, address = weakref.ref(g), g.data_ptr()
+    assert tensors[0].grad == address and tensors[0].param == p.data_ptr()
+    del g
+    gc.collect()
+    assert gone() is None                                  # an address keeps no tensor
+    kept = weakref.ref(m)
+    del m
+    gc.collect()
+    assert kept() is not None                              # a tensor is kept
+    new = torch.zeros(8)
+    tensors[0].grad = new.data_ptr()
+    assert tensors[0].grad == new.data_ptr() and tensors[0].m == kept().data_ptr() and tensors[0].n == 8
