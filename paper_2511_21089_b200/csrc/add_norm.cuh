@@ -169,7 +169,8 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T) add_norm_kernel(const __gri
 
 // A row to a block whose threads take eight columns each: all loads of a row are in flight at once and none is idle long.  A warp
 // to a row (no block barrier) where a row is 512 columns at most and there are many: 65536 x 512 60.6 us against 69.9,
-// while at 1200 rows both take 3.1.  Rows of more than 8192 columns that are not aligned spill up to 132 bytes a thread.  Two chunks to a thread for 8-bit output of longer rows, whose scales are half the
+// while at 1200 rows both take 3.1.  Rows of more than 8192 columns spill: RMSNorm of fp32 + fp32 that is not aligned 48 to 132 bytes a thread, LayerNorm of
+// aligned rows 4 to 80 (e4m3 or with an fp32 input) and of fp32 + fp32 to e4m3 that is not aligned 84.  Two chunks to a thread for 8-bit output of longer rows, whose scales are half the
 // work: 16384 x 4096 111 us against 129 with one (bf16 output: 121 against 117, so it keeps one).
 // LayerNorm, with its second sum, takes two for every output: 16384 x 4096 to bf16 121 us against 139 (four: 129).
 template <bool LAYER, int XKIND, int RKIND, int OKIND, bool VEC>

@@ -3,8 +3,9 @@
 //     y[t] = residual[t] + sum_j w[t, j] y_rows[row_j of t];    d y_rows[row_j] = w[t, j] dy[t],  d w[t, j] = <dy[t], y_rows[row_j]>.
 // Moving and summing rows is bound by memory: each kernel works from the token's side, so that what is shared by a token's rows (x, dy,
 // y) crosses memory once and the rows themselves once.  8192 tokens x 4096 bf16, 8 of 32 branches: rows out 605 MB in 97 us (and 8 for the
-// order), sum with an fp32 residual 806 MB in 122, gradient 1142 MB in 174: 6.2 to 6.6 TB/s.  Rows that start anywhere go at 55 to 70 %
-// of that in bf16 (two bytes a load), as fast in fp32.  No block waits for one outside of its cluster and nothing floating is added atomically.
+// order), sum with an fp32 residual 806 MB in 122, gradient 1142 MB in 174: 6.2 to 6.6 TB/s.  The same rows in e4m3 with their order: 58 us with a scale
+// a row, 66 with one per 32 columns (81 and 80 % of a copy, the order's 8 among them).  Rows that start anywhere go at 60 to 74 %
+// of a copy in bf16 (two bytes a load), as fast as others in fp32.  No block waits for one outside of its cluster and nothing floating is added atomically.
 #include <cooperative_groups.h>
 
 #include "../../include/mlpmoe.h"
@@ -23,7 +24,9 @@ constexpr int kMaxAlign = 1024;
 // The selection as a matrix of bits, in squares of 32 tokens x 32 branches: a lane reads its token's row, and the square
 // transposed holds, for each branch, which of the 32 tokens are in it.  First kernel: the transposed bits and their counts
 // per tile of tokens.  Second: each tile adds up the tiles before it, and every set bit's place is its branch's start plus
-// the bits before it.  A small batch is one tile, or one cluster's, and takes one launch.
+// the bits before it.  A small batch is one tile, or one cluster's, and takes one launch.  Large batches are far above what their bytes take (masks in turn, beyond the
+// L2 cache: 131072 x 32 25 us of 2.6, 131072 x 128 with 16 each 55 of 6.5): two or three launches whose blocks wait for one round trip after the other (the scan's loads
+// follow its stores), tiles with fewer groups than a block has warps, and a row's token written four bytes at a time.
 constexpr int kSortThreads = 512;
 constexpr int kSortTiles = 592;           // tiles aimed at: four blocks per SM (131072 tokens x 32 branches: 23 us; one block per SM: 49)
 constexpr int kSortScanCounts = 16384;    // every tile adds up every tile's counts; from here on a kernel of its own does so once
@@ -486,6 +489,8 @@ struct CombineGradArgs {
   int slots, d, B;
 };
 
+// Above 8192 columns one row is under way at a time, for want of registers: 4096 x 12288, 4 rows a token, 66 % of a copy in bf16 and 83 % in fp32; 2048 x 20000 69
+// and 74 %, 1024 x 32768 70 and 59 % (4096 x 8192: 92 and 88 %).
 // T threads to a token (T = 32: a warp of a block of four): grad_y stays in registers, each of the token's rows is read for its
 // product with it and receives w * grad_y.  Four rows' loads are in flight at once and their products are reduced together (8192 x 4096,
 // 8 rows a token: 174 us; one row after the other 210).  A row is read before it is written, by the same thread, so both may be one buffer.

@@ -91,7 +91,12 @@ constexpr int kStages = 2;
 // copied itself, so that takes no barrier (not WIDE: two).  16384 x 4096, fp32 and bf16: 940 MB in
 // 157 us with the join over seconds (floor 146).  The row ahead in registers and types told apart as it runs: 258 (98 registers, 512 threads per SM); four
 // times four columns a thread: 159 (16 warps per SM).
+// Not WIDE the time goes with the elements: past shared memory every value is a load and a store of two or four bytes with a bound of its own. 12288 x 4096
+// with rows 4101 apart 173 us (63 % of a copy), 12285 x 4097 241 (46 %), 16384 x 201 22 (33 %); all in bf16 206, 293 and 24 (30, 21 and 17 %).
+// Below about 1400 columns a block with one row at a time waits for its sums, and many blocks' column sums go through memory: 16384 x 1100 57 us (68 %),
+// x 1000 48 (74 %), x 400 28 (50 %), x 200 14.6 (49 %).
 // FULL: ds is there, and it and dx are fp32 (told apart as it runs, the same case takes 11 % more instructions and 167 us over seconds, not 157).
+// A stream in bf16 has no such kernel: 16384 x 4096 all in bf16 takes 152 us (RMSNorm 121) for 537 MB, 55 and 69 %.
 template <bool LAYER, int T, int Q, int CTAS, bool WIDE, int SK, int VK, bool FULL>
 __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(const __grid_constant__ NormGradArgs a) {
   constexpr bool WARP = T == 32;
@@ -321,8 +326,9 @@ __global__ void __launch_bounds__(T == 32 ? 256 : T, CTAS) norm_backward_kernel(
 }
 
 // Rows above 8192 columns, a block to a row: no room for the columns' sums, so the row's mean and inv go to memory for a kernel of
-// their own, and grad_out is read a second time (from the L2 cache) instead of being held.  2048 x 20000: 574 MB in 223 us, 40 % of a copy:
-// the sums read s and grad_out once more, and one row a block and SM leaves its loads alone with their latency.
+// their own, and grad_out is read a second time (from the L2 cache) instead of being held.  2048 x 20000, fp32 and bf16: 574 MB in 242 us (RMSNorm 218), 37 and
+// 41 % of a copy; 4096 x 12288 310 and 282, 35 and 39 %; all in bf16 23 to 29 %, odd rows 16 to 23 %.  The rows alone take 142 us (RMSNorm 129), one
+// row a block and SM, its loads alone with their latency; the rest are the sums, which read s and grad_out once more, two or four bytes a load.
 template <bool LAYER, bool VEC>
 __global__ void __launch_bounds__(1024, 1) norm_backward_long_kernel(const __grid_constant__ NormGradArgs a) {
   constexpr int T = 1024, NCH = 4;

@@ -9,8 +9,8 @@ constexpr int64_t kOnePassD = 8192;      // longer rows do not leave room for th
 constexpr int kSplitRows = 64;           // slices of the rows there, for the sums over tokens
 
 // Threads of a row (eight columns each), quads of a thread and blocks per SM, by the row's length: threads without columns cost as much as
-// the others (12264 x 4104: 139 us with 640 threads, 180 with 1024).  A block has four rows or more where every SM has a block, so that few sums are
-// left to join.
+// the others (12264 x 4104: 139 us with 640 threads, 180 with 1024).  Blocks: one for each row (up to 256 columns each eight rows) up to 148 of them, then 148
+// until each has four, then one for each four, up to what the SMs hold at once, so that few sums are left to join.
 struct Shape {
   int threads, quads, ctas;
 };
