@@ -559,10 +559,12 @@ typedef struct {
  * One AdamW step over n_tensors tensors (a host array, not needed after the call), in fp32, a launch for up to 384 of the same types:
  *     g = grad * grad_scale;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *     param = param - lr * weight_decay * param - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
- * The param takes the new moments before they are rounded.  e4m3 moments: scale = max(max |finite value| / 448, 2^-126) of each 128
- * elements; a root above zero is stored as the smallest code at least.  A gradient that is not finite makes its own element's param
- * and moments not finite (a NaN code), other elements of its 128 keep theirs; a square past fp32's range makes its v
- * infinite (in 8 bits a NaN code).
+ * The param takes the new moments before they are rounded.  e4m3 moments: scale = max(max |finite value| * fp32(1 / 448), 2^-126) of each
+ * 128 elements, code = value * fp32(1 / scale) rounded to e4m3; a root above zero is stored as the smallest code at least.  On the way from
+ * the stored moments and the gradient to the new moments the betas, 1 - beta (from double), every product, sum and root are rounded to fp32
+ * in the order written, with (1 - beta2) g before its product with g, so that codes and scales can be computed again bit by bit.
+ * A gradient that is not finite makes its own element's param and moments not finite (a NaN code), other elements of its 128 keep
+ * theirs; a square past fp32's range makes its v infinite (in 8 bits a NaN code).
  * Errors before anything is enqueued: MLPMOE_ERR_INVALID_ARG (NULL, a pointer off its element's alignment, a type or setting that is
  * not allowed), MLPMOE_ERR_UNSUPPORTED (more than 2^40 elements in a tensor).
  */

@@ -50,6 +50,7 @@ from .training_oracle import (  # noqa: F401
     adamw_noise,
     e4m3_up_or_down,
     adamw_blocks,
+    adamw_moments_fp32,
     bf16_up_or_down,
     adamw,
 )

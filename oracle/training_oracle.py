@@ -3,7 +3,7 @@ branches and summed back with the gradient, LayerNorm, the norms' gradient, and 
 formulas; shares no code with the CUDA library."""
 import numpy as np
 
-from .operators_oracle import quantize_e4m3
+from .operators_oracle import quantize_e4m3, round_to_e4m3
 
 M32 = 0xFFFFFFFF
 
@@ -134,6 +134,33 @@ def adamw_blocks(x, root, noise=None):
     if root:
         codes = np.where((x > 0) & (codes < 2.0 ** -9), 2.0 ** -9, codes)
     return codes, scales
+
+
+def adamw_moments_fp32(g, m, m_scale, v, v_scale, beta1, beta2, grad_scale=1.0, noise=None):
+    """(codes and scales of m, codes and scales of sqrt(v)) after a step, bit by bit: every product, sum and root rounded to fp32 in the
+    order of the formulas, scale = max * fp32(1 / 448), value = x * fp32(1 / scale).  m, v: codes as values; everything finite."""
+    f = np.float32
+    g, m, v = np.asarray(g, f) * f(grad_scale), np.asarray(m, f), np.asarray(v, f)
+    per = [np.repeat(np.asarray(s, f), 128)[:g.size] for s in (m_scale, v_scale)]
+    m, v = m * per[0], np.square(v * per[1])
+    m = f(beta1) * m + f(1.0 - beta1) * g
+    v = f(beta2) * v + f(1.0 - beta2) * g * g
+    out = []
+    for x, shift, root in ((m, 0, False), (np.sqrt(v), 16, True)):
+        top = np.array([np.abs(x[i:i + 128]).max() for i in range(0, x.size, 128)], f)
+        scale = np.maximum(top * (f(1) / f(448)), f(2.0 ** -126))
+        y = np.minimum(np.abs(x) * np.repeat(f(1) / scale, 128)[:x.size], f(448))
+        if noise is None:
+            codes = round_to_e4m3(y.astype(np.float64))
+        else:
+            base = np.where(y < f(2.0 ** -6), f(2.0 ** -6), f(0))
+            extra = ((noise >> np.uint64(shift)) & np.uint64(0xFFFF)).astype(np.uint32) * np.uint32(16) | np.uint32(8)
+            codes = (((y + base).view(np.uint32) + extra) & np.uint32(0xFFF00000)).view(f) - base
+            codes = np.minimum(codes, f(448)).astype(np.float64)
+        if root:
+            codes = np.where((x > 0) & (codes < 2.0 ** -9), 2.0 ** -9, codes)
+        out += [np.copysign(codes, x), scale.astype(np.float64)]
+    return tuple(out)
 
 
 def bf16_up_or_down(p, noise):

@@ -2,8 +2,8 @@
 //     g = grad * grad_scale;   m = b1 m + (1 - b1) g;   v = b2 v + (1 - b2) g^2;
 //     p = p - lr wd p - lr / (1 - b1^i) * m / (sqrt(v) / sqrt(1 - b2^i) + eps).
 // HBM-bound with moments in fp32 (100 M elements: 24 to 30 bytes each at 95 to 98 % of a copy).  In 8 bits the instructions come near the
-// memory's time: 63 an element with noise, 9 of them the hash; one Llama-shaped layer with fp32 params and a bf16 copy, 176 M elements:
-// 2.84 GB in 475 us (93 %), bf16 params and gradients 56 % with noise, 75 % without.  A moment in 8 bits is e4m3 with a scale per 128
+// memory's time: 71 an element with noise, 9 of them the hash (bf16 params, with a hash more, 85); one Llama-shaped layer with fp32 params and a bf16
+// copy, 176 M elements: 2.84 GB in 478 to 489 us (90 to 92 %), bf16 params and gradients 55 % with noise, 79 % without.  A moment in 8 bits is e4m3 with a scale per 128
 // elements, the second as its root: e4m3 spans 2^17 in the root, 2^34 in v.  A root above zero never becomes zero, which would make
 // the next quotient m / eps.  Stochastic rounding there, because a step moves v by 1 - b2 of itself, far below half a step of e4m3,
 // so that rounding to nearest would leave most elements where they are.
@@ -46,7 +46,7 @@ struct AdamTensor {
 };
 
 struct AdamSettings {
-  float lr, b1, b2, one_b1, root_b2, eps, log_b1, log_b2;
+  float lr, b1, b2, one_b1, one_b2, eps, log_b1, log_b2;
   const float* lr_device;
   const int64_t* step_device;
   const float* grad_scale;
@@ -140,6 +140,25 @@ __device__ __forceinline__ float reciprocal_fast(float x) {       // off by 2^-2
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
+__device__ __forceinline__ float min_nan(float a, float b, float c) {      // a NaN wins
+  float r;
+  asm("min.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// Root and reciprocal rounded to nearest: a Newton step from the one-instruction value, its residual exact in one fma (Markstein, "Computation of
+// elementary functions on the IBM RISC System/6000 processor", 1990).  Compared with the correctly rounded functions for every fp32 of the range: the root
+// from 2^-96 on (0, infinity and what is not normal give a NaN), the reciprocal from 2^-126 to 2^121.  With the functions themselves the Llama-shaped
+// layer takes 527 us.
+__device__ __forceinline__ float sqrt_newton(float x) {
+  float y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  const float r = __fmul_rn(x, y);
+  return fmaf(fmaf(-r, r, x), 0.5f * y, r);
+}
+__device__ __forceinline__ float reciprocal_newton(float x) {
+  const float r = reciprocal_fast(x);
+  return fmaf(r, fmaf(-x, r, 1.0f), r);
+}
 // Smallest magnitude of eight values.
 __device__ __forceinline__ float low_of(const float (&x)[8]) {
   float low = min3(fabsf(x[0]), fabsf(x[1]), fabsf(x[2]));
@@ -170,7 +189,7 @@ __device__ __forceinline__ uint2 codes_of(const float (&x)[8], const uint32_t (&
     for (int o = 1; o < kStateBlock / 8; o <<= 1) top = fmaxf(top, __shfl_xor_sync(half, top, o));
   }
   scale = fmaxf(top * (1.0f / kE4m3Max), kScaleMin);
-  const float inv = reciprocal_fast(scale);
+  const float inv = reciprocal_newton(scale);
   float y[8];
   if (fine && (!(NOISE || ROOT) || low_of(x) >= scale * (NOISE ? 0.0157f : 0.002f))) {
 #pragma unroll
@@ -200,7 +219,7 @@ __device__ __forceinline__ uint2 codes_of(const float (&x)[8], const uint32_t (&
   return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
 }
 struct Rates {
-  float keep, rate, inv_root, one_b1, root_b2;     // lr wd; lr / (1 - b1^i); 1 / sqrt(1 - b2^i); (1 - b1) gs; sqrt(1 - b2) gs
+  float keep, rate, inv_root, grad_scale;     // lr wd; lr / (1 - b1^i); 1 / sqrt(1 - b2^i)
   uint32_t key;
 };
 
@@ -272,13 +291,11 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
     int64_t step = s.step_device != nullptr ? *s.step_device : s.step;
     if (step < 1) step = 1;
     const float lr = s.lr_device != nullptr ? *s.lr_device : s.lr;
-    const float gs = s.grad_scale != nullptr ? *s.grad_scale : 1.0f;
     Rates r;
     r.keep = lr * t.decay;
     r.rate = lr / -expm1f(static_cast<float>(step) * s.log_b1);
     r.inv_root = 1.0f / sqrtf(-expm1f(static_cast<float>(step) * s.log_b2));
-    r.one_b1 = s.one_b1 * gs;
-    r.root_b2 = s.root_b2 * gs;
+    r.grad_scale = s.grad_scale != nullptr ? *s.grad_scale : 1.0f;
     r.key = mix(t.index ^ mix(s.key ^ static_cast<uint32_t>(step)));
     shared_rates = r;
   }
@@ -298,23 +315,27 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
       values_of(now.v8, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        m[e] *= now.m_scale;
-        v[e] *= now.v_scale;
-        v[e] *= v[e];
+        m[e] = __fmul_rn(m[e], now.m_scale);
+        v[e] = __fmul_rn(v[e], now.v_scale);
+        v[e] = __fmul_rn(v[e], v[e]);
       }
     } else {
       to_f32(now.m, MLPMOE_FP32, m);
       to_f32(now.v, MLPMOE_FP32, v);
     }
+    // Each product and sum is rounded by itself, in the formulas' order, and in 8 bits the root too, so that a code can be computed again bit by bit.  With
+    // fused sums and the approximate root one code in a million was its neighbour, and where it then was its block's largest, the next step's scale was off by
+    // up to 6 %.  8 instructions of the 71; fp32 params 477 -> 478 to 489 us, bf16 params with noise 265 -> 290 (105 M elements).
     float root[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float y = g[e] * r.root_b2;
-      m[e] = fmaf(s.b1, m[e], g[e] * r.one_b1);
-      v[e] = fmaf(y, y, s.b2 * v[e]);
-      root[e] = sqrt_fast(v[e]);
+      const float y = __fmul_rn(g[e], r.grad_scale);
+      m[e] = __fadd_rn(__fmul_rn(s.b1, m[e]), __fmul_rn(s.one_b1, y));
+      v[e] = __fadd_rn(__fmul_rn(s.b2, v[e]), __fmul_rn(__fmul_rn(s.one_b2, y), y));
+      root[e] = EIGHT ? sqrt_newton(v[e]) : sqrt_fast(v[e]);
     }
-    if (low_of(v) < FLT_MIN) {               // (zeros among them)
+    // zeros among them; in 8 bits also infinity
+    if (EIGHT ? !(min_nan(min_nan(min_nan(root[0], root[1], root[2]), root[3], root[4]), root[5], min_nan(root[6], root[7], root[7])) >= 0x1p-48f) : low_of(v) < FLT_MIN) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) root[e] = sqrtf(v[e]);
     }
@@ -451,7 +472,7 @@ extern "C" mlpmoe_status_t mlpmoe_adamw(const mlpmoe_adamw_tensor_t* tensors, in
   s.b1 = static_cast<float>(o.beta1);
   s.b2 = static_cast<float>(o.beta2);
   s.one_b1 = static_cast<float>(1.0 - o.beta1);
-  s.root_b2 = static_cast<float>(sqrt(1.0 - o.beta2));
+  s.one_b2 = static_cast<float>(1.0 - o.beta2);
   s.eps = static_cast<float>(o.eps);
   s.log_b1 = static_cast<float>(log(o.beta1));
   s.log_b2 = static_cast<float>(log(o.beta2));

@@ -213,3 +213,49 @@ def test_a_step_gives_the_same_bits_every_time(lib, pt, gt, state, copy, shift):
         wants = wants or got
         assert all(torch.equal(x, y) for x, y in zip(got, wants))
     assert any(not torch.equal(x, y) for x, y in zip(start, wants))
+
+
+# ------------------------------------------------------------------------------------------------ 8-bit moments bit by bit
+
+@pytest.mark.parametrize("n,pt,gt,shift", [(200003, "fp32", "bf16", 0), (128 * 1000, "bf16", "bf16", 0), (70001, "fp32", "fp32", 3), (50, "bf16", "fp32", 1)])
+@pytest.mark.parametrize("noisy,scale", [(False, None), (True, 0.5), (True, 0.37)])
+def test_codes_and_scales_bit_by_bit(lib, n, pt, gt, shift, noisy, scale):
+    """Three steps in a row: a code that were another one would move the next step's scale."""
+    rng = np.random.default_rng([n, 3])
+    param = Param(rng, n, pt, gt, "e4m3", shift=shift)
+    tensors = lib.mlpmoe_adamw_tensors([param.record(lib)])
+    state = [host(t) for t in (param.m, param.ms.t, param.v, param.vs.t)]
+    for step in (1, 2, 3):
+        param.g.copy_(dev(rng.normal(size=n) * 1e-3))
+        lib.mlpmoe_adamw(tensors, 1e-3, 0.9, 0.999, 1e-8, step=step, grad_scale=None if scale is None else dev([scale]), stochastic=noisy, seed=21,
+                         stream=stream_ptr())
+        torch.cuda.synchronize()
+        m, ms, v, vs = state
+        state = oracle.adamw_moments_fp32(host(param.g), m, ms, v, vs, 0.9, 0.999, 1.0 if scale is None else scale,
+                                          oracle.adamw_noise(21, step, 0, n) if noisy else None)
+        for name, got, want in zip(("m", "m_scale", "v", "v_scale"), (param.m, param.ms.t, param.v, param.vs.t), state):
+            assert np.array_equal(host(got), want), (step, name, int((host(got) != want).sum()))
+
+
+@pytest.mark.parametrize("noisy", [False, True])
+def test_codes_and_scales_bit_by_bit_of_every_size(lib, noisy):
+    """Gradients from 2^-80 to 2^55, with zeros, blocks of one size and blocks of many: squares below fp32's normal range among them."""
+    rng = np.random.default_rng(30)
+    n = 128 * 3000
+    size = np.where(np.arange(n) // 128 % 2 == 0, np.repeat(rng.uniform(-80, 55, n // 128), 128), rng.uniform(-80, 55, n))
+    param = Param(rng, n, "fp32", "fp32", "e4m3")
+    for t in (param.m, param.v, param.ms.t, param.vs.t):
+        t.zero_()
+    tensors = lib.mlpmoe_adamw_tensors([param.record(lib)])
+    state = [host(t) for t in (param.m, param.ms.t, param.v, param.vs.t)]
+    for step in (1, 2, 3):
+        g = rng.normal(size=n) * 2.0 ** size * (rng.uniform(size=n) < 0.9)
+        param.g.copy_(dev(g))
+        lib.mlpmoe_adamw(tensors, 1e-3, 0.9, 0.999, 1e-8, step=step, stochastic=noisy, seed=22, stream=stream_ptr())
+        torch.cuda.synchronize()
+        m, ms, v, vs = state
+        state = oracle.adamw_moments_fp32(host(param.g), m, ms, v, vs, 0.9, 0.999, 1.0, oracle.adamw_noise(22, step, 0, n) if noisy else None)
+        for name, got, want in zip(("m", "m_scale", "v", "v_scale"), (param.m, param.ms.t, param.v, param.vs.t), state):
+            assert np.array_equal(host(got), want), (step, name, int((host(got) != want).sum()))
+    for b in param.guards:
+        b.check()

@@ -155,3 +155,26 @@ def test_a_list_of_tensors_takes_addresses_and_new_gradients(lib):
     new = torch.zeros(8)
     tensors[0].grad = new.data_ptr()
     assert tensors[0].grad == new.data_ptr() and tensors[0].m == kept().data_ptr() and tensors[0].n == 8
+
+
+# ----------------------------------------------------------------------------- 8-bit moments bit by bit
+
+@pytest.mark.parametrize("noisy", [False, True])
+def test_moments_bit_by_bit_are_those_of_the_definition(noisy):
+    """The fp32 arithmetic against 64 bits: scales within its roundings, codes the same but next to a border."""
+    rng = np.random.default_rng(17)
+    n = 128 * 150 + 37
+    (m, ms), (v, vs) = oracle.adamw_blocks(rng.normal(size=n) * 3e-4, False), oracle.adamw_blocks(np.abs(rng.normal(size=n)) * 1e-3, True)
+    ms, vs = ms.astype(np.float32), vs.astype(np.float32)
+    g = (rng.normal(size=n) * 1e-3).astype(np.float32)
+    noise = oracle.adamw_noise(3, 5, 0, n) if noisy else None
+    cm, sm, cv, sv = oracle.adamw_moments_fp32(g, m, ms, v, vs, 0.9, 0.999, 0.37, noise)
+    _, m1, v1 = oracle.adamw(0.0, g.astype(np.float64), m * np.repeat(ms, 128)[:n].astype(np.float64),
+                             (v * np.repeat(vs, 128)[:n].astype(np.float64)) ** 2, 1e-3, 0.9, 0.999, 1e-8, 0.0, 5, float(np.float32(0.37)))
+    u = 2.0 ** -24
+    for x, root, codes, scales in ((m1, False, cm, sm), (np.sqrt(v1), True, cv, sv)):
+        want, want_scale = oracle.adamw_blocks(x, root, noise)
+        # constants, products and the sum 5 u of the terms (a sum of two that cancel: the block's largest does not), root and product 2 u each
+        assert np.all(np.abs(scales - want_scale) <= 12 * u * want_scale)
+        assert np.mean(codes != want) <= 2e-3
+        assert np.all(np.abs(codes - want) <= 2.0 ** -3 * np.maximum(np.abs(want), 2.0 ** -6))
