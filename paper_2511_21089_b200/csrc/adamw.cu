@@ -3,7 +3,7 @@
 //     p = p - lr wd p - lr / (1 - b1^i) * m / (sqrt(v) / sqrt(1 - b2^i) + eps).
 // HBM-bound with moments in fp32 (100 M elements: 24 to 30 bytes each at 95 to 98 % of a copy).  In 8 bits the instructions come near the
 // memory's time: 71 an element with noise, 9 of them the hash (bf16 params, with a hash more, 85); one Llama-shaped layer with fp32 params and a bf16
-// copy, 176 M elements: 2.84 GB in 478 to 489 us (90 to 92 %), bf16 params and gradients 55 % with noise, 79 % without.  A moment in 8 bits is e4m3 with a scale per 128
+// copy, 176 M elements: 2.84 GB in 478 to 514 us by the GPU (86 to 92 %), bf16 params and gradients 55 % with noise, 79 % without.  A moment in 8 bits is e4m3 with a scale per 128
 // elements, the second as its root: e4m3 spans 2^17 in the root, 2^34 in v.  A root above zero never becomes zero, which would make
 // the next quotient m / eps.  Stochastic rounding there, because a step moves v by 1 - b2 of itself, far below half a step of e4m3,
 // so that rounding to nearest would leave most elements where they are.
@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamCtas) adamw_kernel(const __
     }
     // Each product and sum is rounded by itself, in the formulas' order, and in 8 bits the root too, so that a code can be computed again bit by bit.  With
     // fused sums and the approximate root one code in a million was its neighbour, and where it then was its block's largest, the next step's scale was off by
-    // up to 6 %.  8 instructions of the 71; fp32 params 477 -> 478 to 489 us, bf16 params with noise 265 -> 290 (105 M elements).
+    // up to 6 %.  8 instructions of the 71; fp32 params 477 -> 478 to 489 us on one GPU, bf16 params with noise 265 -> 290 (105 M elements).
     float root[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
